@@ -74,6 +74,17 @@ const char* kernel_name(int kid) {
         case KID_SPLIT_WEIGHTS: return "split_weights_kernel";
         case KID_SPLIT_CRITIC: return "split_critic_kernel";
         case KID_SPLIT_POLICY: return "split_policy_kernel";
+        case KID_DISTILL: return "distill_kernel";
+        case KID_DISTILL_JOIN: return "distill_join_kernel";
+        case KID_DISTILL_GRAD: return "distill_grad_kernel";
+        case KID_TOP_LOGITS: return "top_logits_kernel";
+        case KID_TOP_MERGE: return "top_merge_kernel";
+        case KID_DELTA_STEP: return "delta_step_kernel";
+        case KID_DELTA_PREPARE: return "delta_prepare_kernel";
+        case KID_DELTA_SCAN: return "delta_scan_kernel";
+        case KID_DELTA_BACK_SCAN: return "delta_back_scan_kernel";
+        case KID_DELTA_BACK: return "delta_back_kernel";
+        case KID_DELTA_GROUP: return "delta_group_kernel";
         default: return "?";
     }
 }
@@ -146,6 +157,16 @@ struct pql_ctx {
     const float* wcache_actor;
     std::string err;
 };
+
+int32_t pql::ctx_fail(pql_ctx* ctx, int32_t code, const char* what, hipError_t e) {
+    try {
+        ctx->err = what;
+        if (e != hipSuccess) ctx->err.append(": ").append(hipGetErrorString(e));
+    } catch (...) {
+        ctx->err.clear();       // no memory for the text: the code alone
+    }
+    return code;
+}
 
 namespace {
 

@@ -1,0 +1,1193 @@
+// The gated delta rule (include/pql_student.h): a state S [dim_k][dim_v] per sequence and value head,
+//     S~ = exp(g_t) S,  r_t = v_t - S~^T k_t,  S = S~ + k_t (beta_t r_t)^T,  o_t = scale S^T q_t.
+//
+// One token or a few: delta_step_kernel keeps the state in registers and reads and writes it once; bound by that.
+//
+// Sequences go by chunks of 64 tokens.  With S0 the state before the chunk, G_i the sums of g in it, gam_i = e^{G_i},
+// Gam_ij = e^{G_i - G_j} (0 where a reset lies between), e_i = e^{G_last - G_i}, all tokens of a chunk follow from
+//     N_ij = Gam_ij k_i.k_j (i > j),  T = (I + N diag(beta))^-1,  X = V - gam o (K S0),  R = T X,  Y = beta o R,
+//     P_ij = Gam_ij q_i.k_j (i >= j),  O = scale (gam o (Q S0) + P Y),  S1 = e^{G_last} S0 + K^T (e o Y),
+// R being the errors r_t.  delta_prepare_kernel finds T and P of all chunks at once; delta_scan_kernel goes through the
+// chunks of one sequence, head and block of columns of the state (columns never mix).
+// Gradient, with dO scaled: delta_back_scan_kernel goes through the chunks in reverse,
+//     dY = P^T dO + e o (K dS1),  dX = T^T (beta o dY) = dV,  dS0 = e^{G_last} dS1 - K^T (gam o dX) + Q^T (gam o dO),
+// and delta_back_kernel takes all chunks at once for the rest,
+//     E = Gam o (dO Y^T) (i >= j),  F = -Gam o (dX R^T) (i > j),
+//     dQ = gam o (dO S0^T) + E K,
+//     dK = -gam o (dX S0^T) + (F diag(beta)) K + e o (Y dS1^T) + beta o (F^T K) + E^T Q,
+//     dbeta_j = dY_j.R_j + k_j.(F^T K)_j,
+//     dG_i = q_i.dQ_i + k_i.(first two terms of dK_i) - k_i.(last three),
+//     dG_last += sum_j k_j.(e o (Y dS1^T))_j + e^{G_last} <dS1, S0>,  dg_t = sum of dG_i from t to its segment's end.
+//
+// Arithmetic: products on the matrix cores with 32-bit results.  fp32 tokens: v_mfma_f32_16x16x4_f32.  bf16 tokens:
+// q, k and dO are exact operands; what has been computed (S, X, Y, T, P, ...) is split into three bf16 terms, which
+// together hold the 24 bits of an fp32 value, so that rounding to bf16 happens at the outputs only and the fp32 outputs
+// (states, gradients of gates) are as exact as with fp32 products.
+#include "pql_student_internal.h"
+
+namespace pql {
+namespace {
+
+constexpr int C = 64;                       // tokens per chunk
+constexpr int NB = 32;                      // state columns per workgroup of the scans
+constexpr float NEG_INF = -__builtin_inff();
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+// ---- operands of 16x16x32 products -----------------------------------------------------------
+// Lane l holds row (A) or column (B) l % 16, elements 8 (l / 16) .. + 7 of the contraction; results: column l % 16,
+// rows 4 (l / 16) .. + 3.
+struct F1 { bf16x8 h; };                    // exact bf16
+struct F3 { bf16x8 h, m, l; };              // an fp32 value as three bf16 terms
+struct FF { float v[8]; };
+__device__ __forceinline__ floatx4 mm(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ void mma(floatx4& c, const F1& a, const F1& b) { c = mm(a.h, b.h, c); }
+__device__ __forceinline__ void mma(floatx4& c, const F1& a, const F3& b) { c = mm(a.h, b.l, c); c = mm(a.h, b.m, c); c = mm(a.h, b.h, c); }
+__device__ __forceinline__ void mma(floatx4& c, const F3& a, const F1& b) { c = mm(a.l, b.h, c); c = mm(a.m, b.h, c); c = mm(a.h, b.h, c); }
+// terms below 2^-24 of the product are left out
+__device__ __forceinline__ void mma(floatx4& c, const F3& a, const F3& b) {
+    c = mm(a.l, b.h, c); c = mm(a.h, b.l, c); c = mm(a.m, b.m, c);
+    c = mm(a.m, b.h, c); c = mm(a.h, b.m, c); c = mm(a.h, b.h, c);
+}
+__device__ __forceinline__ void mma(floatx4& c, const FF& a, const FF& b) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
+}
+__device__ __forceinline__ void split3(float x, __bf16& h, __bf16& m, __bf16& l) {
+    h = (__bf16)x;
+    const float r = x - (float)h;
+    m = (__bf16)r;
+    l = (__bf16)(r - (float)m);
+}
+
+struct ModeB {                              // bf16 tokens
+    using E = bf16_t; using X = F1; using Y = F3;
+    static constexpr int PLANES = 3, PAD = 8;
+    static __device__ __forceinline__ Y computed(const float* x) {
+        F3 f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { __bf16 h, m, l; split3(x[j], h, m, l); f.h[j] = h; f.m[j] = m; f.l[j] = l; }
+        return f;
+    }
+    static __device__ __forceinline__ X exact(const float* x) {
+        F1 f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f.h[j] = (__bf16)x[j];
+        return f;
+    }
+};
+struct ModeF {                              // fp32 tokens
+    using E = float; using X = FF; using Y = FF;
+    static constexpr int PLANES = 1, PAD = 4;
+    static __device__ __forceinline__ Y computed(const float* x) {
+        FF f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f.v[j] = x[j];
+        return f;
+    }
+    static __device__ __forceinline__ X exact(const float* x) { return computed(x); }
+};
+
+// A matrix in LDS, [rows][cols], contraction along the columns, rows padded by 16 bytes.  Computed values take
+// M::PLANES planes, exact ones a single one.
+template <typename M, int ROWS, int COLS, bool EXACT> struct Tile {
+    using E = typename M::E;
+    static constexpr int LD = COLS + M::PAD, PLANES = EXACT ? 1 : M::PLANES;
+    static constexpr int BYTES = ROWS * LD * PLANES * (int)sizeof(E);
+    E* p;
+    __device__ __forceinline__ explicit Tile(void* q) : p((E*)q) {}
+    __device__ __forceinline__ void put4(int row, int k, floatx4 x) const {
+        E* o = p + row * LD + k;
+        if constexpr (sizeof(E) == 4) {
+            *(floatx4*)o = x;
+        } else if constexpr (EXACT) {
+            bf16x4 h;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[i] = (__bf16)x[i];
+            *(bf16x4*)o = h;
+        } else {
+            bf16x4 h, m, l;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { __bf16 a, b, c; split3(x[i], a, b, c); h[i] = a; m[i] = b; l[i] = c; }
+            *(bf16x4*)o = h; *(bf16x4*)(o + ROWS * LD) = m; *(bf16x4*)(o + 2 * ROWS * LD) = l;
+        }
+    }
+    __device__ __forceinline__ void put1(int row, int k, float x) const {
+        E* o = p + row * LD + k;
+        if constexpr (PLANES == 3) {
+            __bf16 h, m, l;
+            split3(x, h, m, l);
+            o[0] = h; o[ROWS * LD] = m; o[2 * ROWS * LD] = l;
+        } else {
+            o[0] = (E)x;
+        }
+    }
+    __device__ __forceinline__ floatx4 get4(int row, int k) const {       // exact tiles only
+        const E* o = p + row * LD + k;
+        floatx4 x;
+        if constexpr (sizeof(E) == 4) {
+            x = *(const floatx4*)o;
+        } else {
+            const bf16x4 h = *(const bf16x4*)o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = (float)h[i];
+        }
+        return x;
+    }
+    __device__ __forceinline__ auto frag(int row, int k) const {
+        const E* o = p + row * LD + k;
+        if constexpr (sizeof(E) == 4) {
+            FF f;
+            const floatx4 a = *(const floatx4*)o, b = *(const floatx4*)(o + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { f.v[i] = a[i]; f.v[4 + i] = b[i]; }
+            return f;
+        } else if constexpr (EXACT) {
+            return F1{*(const bf16x8*)o};
+        } else {
+            return F3{*(const bf16x8*)o, *(const bf16x8*)(o + ROWS * LD), *(const bf16x8*)(o + 2 * ROWS * LD)};
+        }
+    }
+};
+
+// ---- tokens in memory -----------------------------------------------------------------------
+// Eight consecutive elements d .. d + 7 of one token row; zeros from dim on and where the token does not count.
+template <typename E, bool AL>
+__device__ __forceinline__ void load8(const E* row, int d, int dim, bool ok, float* x) {
+    if (AL) {                               // 16-byte aligned rows of a multiple of 8 elements
+        if (ok && d < dim) {
+            if constexpr (sizeof(E) == 4) {
+                const floatx4 a = *(const floatx4*)(row + d), b = *(const floatx4*)(row + d + 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+            } else {
+                const bf16x8 a = *(const bf16x8*)(row + d);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = ok && d + i < dim ? to_float(row[d + i]) : 0.f;
+    }
+}
+// Eight consecutive fp32 values of a padded array of the library's own.
+__device__ __forceinline__ void load8(const float* p, float* x) {
+    const floatx4 a = *(const floatx4*)p, b = *(const floatx4*)(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+}
+// The chunk's tokens transposed: tile[d][token], d < D.
+template <typename M, int D, bool AL, typename T>
+__device__ __forceinline__ void stage_transposed(const T& tile, const typename M::E* base, int64_t stride_t, int len, int dim, int d0 = 0) {
+    for (int u = threadIdx.x; u < D / 8 * 16; u += 256) {
+        const int t = u % 16 * 4, d = u / 16 * 8;
+        float x[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load8<typename M::E, AL>(base + (t + i) * stride_t, d0 + d, dim, t + i < len, x[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) tile.put4(d + j, t, floatx4{x[0][j], x[1][j], x[2][j], x[3][j]});
+    }
+}
+
+// ---- gates of a chunk -------------------------------------------------------------------------
+struct Gates {
+    double sum[C];                          // G_i; double, so that differences of long sums stay exact
+    int part[C];                            // resets up to and including the token
+    float beta[C], gam[C], end[C];
+    float last;                             // e^{G_last}, 0 after a reset in the chunk
+};
+// By the first wavefront; a barrier follows.
+__device__ __forceinline__ void gates_of(Gates& s, const float* g, int64_t g_stride, const float* beta, int64_t b_stride, int len) {
+    const int i = threadIdx.x;
+    if (i >= 64) return;
+    float x = i < len ? g[i * g_stride] : 0.f;
+    const unsigned long long resets = __ballot(x == NEG_INF);
+    if (x == NEG_INF) x = 0.f;
+    double sum = x;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) { const double o = __shfl_up(sum, d); if (i >= d) sum += o; }
+    const int part = __popcll(resets & (~0ull >> (63 - i))), all = __popcll(resets);
+    const double total = __shfl(sum, 63);
+    s.sum[i] = sum;
+    s.part[i] = part;
+    s.beta[i] = i < len ? beta[i * b_stride] : 0.f;
+    s.gam[i] = part == 0 ? expf((float)sum) : 0.f;
+    s.end[i] = part == all ? expf((float)(total - sum)) : 0.f;
+    if (i == 63) s.last = all == 0 ? expf((float)total) : 0.f;
+}
+// f x, and 0 for f = 0 whatever x is: behind a reset nothing is left of a state that is not finite.
+__device__ __forceinline__ float damp(float f, float x) { return f == 0.f ? 0.f : f * x; }
+__device__ __forceinline__ float decay(const Gates& s, int i, int j) {
+    return s.part[i] == s.part[j] ? expf((float)(s.sum[i] - s.sum[j])) : 0.f;
+}
+
+struct Where {                              // one sequence and head
+    int b, h, hk, len, bh;
+};
+__device__ __forceinline__ Where where_of(const DeltaArgs& a, int bh) {
+    Where w;
+    w.bh = bh + a.bh0; w.b = w.bh / a.heads_v; w.h = w.bh - w.b * a.heads_v; w.hk = w.h / a.group;
+    w.len = a.lengths ? min(max(a.lengths[w.b], 0), a.steps) : a.steps;
+    return w;
+}
+template <typename E> __device__ __forceinline__ const E* at(const DeltaSeq& s, int b, int64_t t, int h) {
+    return (const E*)s.p + b * s.b + t * s.t + h * s.h;
+}
+template <typename E> __device__ __forceinline__ E* at_out(const DeltaSeq& s, int b, int64_t t, int h) {
+    return (E*)s.p + b * s.b + t * s.t + h * s.h;
+}
+
+// =============================================================================================
+// One token or a few.  A workgroup holds up to 4 LX columns of one state in registers: lanes along the columns (four
+// each), 256 / LX groups of rows.  With z = S~^T k and w = S~^T q found together, u = beta (v - z) and
+// o = scale (w + (q.k) u) need one reduction per token instead of two.
+// =============================================================================================
+template <typename E, int LX, bool VEC>
+__global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a) {
+    constexpr int RY = 256 / LX, NR = PQL_DELTA_MAX_DIM_K / RY;
+    __shared__ float s_k[2][PQL_DELTA_MAX_DIM_K], s_q[2][PQL_DELTA_MAX_DIM_K];
+    __shared__ float s_red[2][4][LX * 8];
+    const Where w = where_of(a, blockIdx.x);
+    const int t = threadIdx.x, lx = t % LX, ry = t / LX, c0 = blockIdx.y * LX * 4;
+    const int dk = a.dim_k, dv = a.dim_v;
+    const int64_t base = (int64_t)w.bh * dk * dv;
+    float s[NR][4];
+    auto col = [&](int j) { return c0 + (VEC ? lx * 4 + j : lx + LX * j); };
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+        const int r = ry + RY * i;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+        if (a.state && r < dk) {
+            const float* p = a.state + base + (int64_t)r * dv;
+            if (VEC) {
+                if (col(0) < dv) {
+                    const floatx4 x = *(const floatx4*)(p + col(0));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[i][j] = x[j];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (col(j) < dv) s[i][j] = p[col(j)];
+            }
+        }
+    }
+    for (int n = 0; n < a.steps; ++n) {
+        const int slot = n & 1;
+        E* out = at_out<E>(a.out, w.b, n, w.h);
+        if (n >= w.len) {
+            if (ry == 0)
+                for (int j = 0; j < 4; ++j) if (col(j) < dv) out[col(j)] = from_float<E>(0.f);
+            continue;
+        }
+        if (t < PQL_DELTA_MAX_DIM_K) s_k[slot][t] = t < dk ? to_float(at<E>(a.k, w.b, n, w.hk)[t]) : 0.f;
+        else s_q[slot][t - PQL_DELTA_MAX_DIM_K] = t - PQL_DELTA_MAX_DIM_K < dk ? to_float(at<E>(a.q, w.b, n, w.hk)[t - PQL_DELTA_MAX_DIM_K]) : 0.f;
+        const float alpha = expf(*at<float>(a.g, w.b, n, w.h)), beta = *at<float>(a.beta, w.b, n, w.h);
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = col(j) < dv ? to_float(at<E>(a.v, w.b, n, w.h)[col(j)]) : 0.f;
+        __syncthreads();
+        float z[8] = {}, qk = 0.f;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int r = ry + RY * i;
+            const float k = s_k[slot][r], q = s_q[slot][r];
+            qk += q * k;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[i][j] = damp(alpha, s[i][j]);
+                z[j] += s[i][j] * k;
+                z[4 + j] += s[i][j] * q;
+            }
+        }
+        // the lanes of a wavefront that hold the same columns, then the four wavefronts
+#pragma unroll
+        for (int d = LX; d < 64; d *= 2) {
+            qk += __shfl_xor(qk, d);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] += __shfl_xor(z[j], d);
+        }
+        __shared__ float s_qk[2][4];
+        if ((t & 63) < LX) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s_red[slot][t >> 6][j * LX + lx] = z[j];
+            if (lx == 0) s_qk[slot][t >> 6] = qk;
+        }
+        __syncthreads();
+        qk = s_qk[slot][0] + s_qk[slot][1] + s_qk[slot][2] + s_qk[slot][3];
+        float u[4], o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float zz = 0.f, zq = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { zz += s_red[slot][i][j * LX + lx]; zq += s_red[slot][i][(4 + j) * LX + lx]; }
+            u[j] = beta * (v[j] - zz);
+            o[j] = a.scale * (zq + qk * u[j]);
+        }
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const float k = s_k[slot][ry + RY * i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[i][j] += k * u[j];
+        }
+        if (ry == 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (col(j) < dv) out[col(j)] = from_float<E>(o[j]);
+        }
+    }
+    if (a.state_out == a.state && w.len == 0) return;
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+        const int r = ry + RY * i;
+        if (r >= dk) continue;
+        float* p = a.state_out + base + (int64_t)r * dv;
+        if (VEC) {
+            if (col(0) < dv) *(floatx4*)(p + col(0)) = floatx4{s[i][0], s[i][1], s[i][2], s[i][3]};
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (col(j) < dv) p[col(j)] = s[i][j];
+        }
+    }
+}
+
+// =============================================================================================
+// Chunks: T and P of every chunk.
+// =============================================================================================
+__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
+
+// In place: the strictly lower triangular part of m [C][LDM] becomes (I + m)^-1 with unit diagonal and zeros above.
+// Blocks of 16: those on the diagonal by substitution (stable whatever the keys; a product of powers is not), then
+// block columns downwards, T_ij = -T_ii sum_{j <= k < i} m_ik T_kj, each wavefront one column.
+constexpr int LDM = C + 1;
+__device__ __forceinline__ void invert(float (*m)[LDM], float (*t)[LDM], float (*scratch)[16][17]) {
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, q = l >> 4;
+    for (int i = threadIdx.x; i < C * C; i += 256) t[i / C][i % C] = 0.f;
+    __syncthreads();
+    if (l < 16) {
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            x[i] = i == l ? 1.f : 0.f;
+#pragma unroll
+            for (int k = 0; k < i; ++k) x[i] -= m[16 * w + i][16 * w + k] * x[k];
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t[16 * w + i][16 * w + l] = x[i];
+    }
+    __syncthreads();
+    for (int i = w + 1; i < C / 16; ++i) {
+        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int k = w; k < i; ++k)
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(m[16 * i + c][16 * k + 4 * s + q], t[16 * k + 4 * s + q][16 * w + c], acc, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) scratch[w][4 * q + r][c] = acc[r];
+        wave_fence();
+        floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+            o = __builtin_amdgcn_mfma_f32_16x16x4f32(t[16 * i + c][16 * i + 4 * s + q], scratch[w][4 * s + q][c], o, 0, 0, 0);
+        wave_fence();
+#pragma unroll
+        for (int r = 0; r < 4; ++r) t[16 * i + 4 * q + r][16 * w + c] = -o[r];
+        wave_fence();
+    }
+    __syncthreads();
+}
+
+template <typename M, int DK, bool AL>
+__global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
+    using E = typename M::E;
+    __shared__ Gates s_g;
+    __shared__ float s_m[C][LDM], s_t[C][LDM], s_x[4][16][17];
+    const Where w = where_of(a, blockIdx.y);
+    const int ch = blockIdx.x, left = w.len - ch * C;
+    if (left <= 0) return;
+    const int len = min(left, C);
+    const int64_t t0 = (int64_t)ch * C;
+    gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, q = l >> 4;
+    const E* kp = at<E>(a.k, w.b, t0, w.hk);
+    const E* qp = at<E>(a.q, w.b, t0, w.hk);
+    floatx4 kk[4] = {}, qk[4] = {};
+#pragma unroll
+    for (int d = 0; d < DK; d += 32) {
+        float x[8];
+        const int row = 16 * wave + c;
+        load8<E, AL>(kp + row * a.k.t, d + 8 * q, a.dim_k, row < len, x);
+        const auto fk = M::exact(x);
+        load8<E, AL>(qp + row * a.q.t, d + 8 * q, a.dim_k, row < len, x);
+        const auto fq = M::exact(x);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            if (n > wave) break;
+            load8<E, AL>(kp + (16 * n + c) * a.k.t, d + 8 * q, a.dim_k, 16 * n + c < len, x);
+            const auto f = M::exact(x);
+            mma(kk[n], fk, f);
+            mma(qk[n], fq, f);
+        }
+    }
+    __syncthreads();
+    float* P = a.P + ((int64_t)w.bh * a.chunks + ch) * C * C;
+    float* T = a.T + ((int64_t)w.bh * a.chunks + ch) * C * C;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const int j = 16 * n + c;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * wave + 4 * q + r;
+            const float f = i >= j ? decay(s_g, i, j) : 0.f;
+            P[i * C + j] = f * qk[n][r];
+            s_m[i][j] = i > j ? f * kk[n][r] * s_g.beta[j] : 0.f;
+        }
+    }
+    __syncthreads();
+    invert(s_m, s_t, s_x);
+    for (int i = threadIdx.x; i < C * C; i += 256) T[i] = s_t[i / C][i % C];
+}
+
+// =============================================================================================
+// Chunks in order: outputs and states, NB columns per workgroup.
+// =============================================================================================
+template <typename M, int DK> struct ScanLds {
+    using S = Tile<M, NB, DK, false>;       // S^T [column][dim_k]
+    using X = Tile<M, NB, C, false>;        // X^T, Y^T, (e o Y)^T [column][token]
+    using K = Tile<M, DK, C, true>;         // K^T [dim_k][token]
+    static constexpr int S0 = 0, X0 = S0 + S::BYTES, Y0 = X0 + X::BYTES, Z0 = Y0 + X::BYTES, K0 = Z0 + X::BYTES, BYTES = K0 + K::BYTES;
+};
+template <typename E> __device__ __forceinline__ void zero_rows(const DeltaSeq& s, const Where& w, int from, int to, int c0, int n) {
+    for (int i = threadIdx.x; i < (to - from) * n; i += 256) at_out<E>(s, w.b, from + i / n, w.h)[c0 + i % n] = from_float<E>(0.f);
+}
+template <typename M, int DK, bool AL>
+__global__ __launch_bounds__(256) void delta_scan_kernel(DeltaArgs a) {
+    using E = typename M::E;
+    using L = ScanLds<M, DK>;
+    constexpr int RS = DK / 64, NT = NB / 16;       // 16-row strips of the state per wavefront, column tiles
+    extern __shared__ __align__(16) unsigned char lds[];
+    __shared__ Gates s_g;
+    const typename L::S tS(lds + L::S0);
+    const typename L::X tX(lds + L::X0), tY(lds + L::Y0), tZ(lds + L::Z0);
+    const typename L::K tK(lds + L::K0);
+    const Where w = where_of(a, blockIdx.y);
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, q = l >> 4, c0 = blockIdx.x * NB;
+    const int dk = a.dim_k, dv = a.dim_v;
+    floatx4 S[RS][NT];
+#pragma unroll
+    for (int s = 0; s < RS; ++s)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int col = c0 + 16 * n + c, row = 16 * (wave * RS + s) + 4 * q;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                S[s][n][r] = a.state && row + r < dk && col < dv ? a.state[((int64_t)w.bh * dk + row + r) * dv + col] : 0.f;
+            tS.put4(16 * n + c, row, S[s][n]);
+        }
+    const int chunks = (w.len + C - 1) / C;
+    for (int ch = 0; ch < chunks; ++ch) {
+        const int len = min(w.len - ch * C, C);
+        const int64_t t0 = (int64_t)ch * C, at_chunk = (int64_t)w.bh * a.chunks + ch;
+        const E* kp = at<E>(a.k, w.b, t0, w.hk);
+        const E* qp = at<E>(a.q, w.b, t0, w.hk);
+        gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
+        stage_transposed<M, DK, AL>(tK, kp, a.k.t, len, dk);
+        if (a.S) {
+            float* o = a.S + at_chunk * DK * a.dvp;
+#pragma unroll
+            for (int s = 0; s < RS; ++s)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[(int64_t)(16 * (wave * RS + s) + 4 * q + r) * a.dvp + c0 + 16 * n + c] = S[s][n][r];
+        }
+        __syncthreads();                    // states, K^T and gates are there
+        floatx4 z[NT] = {}, o1[NT] = {};
+        const int row = 16 * wave + c;
+#pragma unroll
+        for (int d = 0; d < DK; d += 32) {
+            float x[8];
+            load8<E, AL>(kp + row * a.k.t, d + 8 * q, dk, row < len, x);
+            const auto fk = M::exact(x);
+            load8<E, AL>(qp + row * a.q.t, d + 8 * q, dk, row < len, x);
+            const auto fq = M::exact(x);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const auto f = tS.frag(16 * n + c, d + 8 * q);
+                mma(z[n], fk, f);
+                mma(o1[n], fq, f);
+            }
+        }
+        const int i0 = 16 * wave + 4 * q;   // this lane's tokens
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int col = c0 + 16 * n + c;
+            floatx4 x;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float v = i0 + r < len && col < dv ? to_float(at<E>(a.v, w.b, t0 + i0 + r, w.h)[col]) : 0.f;
+                x[r] = v - damp(s_g.gam[i0 + r], z[n][r]);
+            }
+            tX.put4(16 * n + c, i0, x);
+        }
+        __syncthreads();
+        floatx4 rr[NT] = {};
+        const float* T = a.T + at_chunk * C * C + row * C;
+        for (int k = 0; k < 16 * (wave + 1); k += 32) {
+            float x[8];
+            load8(T + k + 8 * q, x);
+            const auto f = M::computed(x);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma(rr[n], f, tX.frag(16 * n + c, k + 8 * q));
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            floatx4 y, z2;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { y[r] = s_g.beta[i0 + r] * rr[n][r]; z2[r] = s_g.end[i0 + r] * y[r]; }
+            tY.put4(16 * n + c, i0, y);
+            tZ.put4(16 * n + c, i0, z2);
+            if (a.R) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) a.R[(at_chunk * C + i0 + r) * a.dvp + c0 + 16 * n + c] = rr[n][r];
+            }
+        }
+        __syncthreads();
+        floatx4 o2[NT] = {};
+        const float* P = a.P + at_chunk * C * C + row * C;
+        for (int k = 0; k < 16 * (wave + 1); k += 32) {
+            float x[8];
+            load8(P + k + 8 * q, x);
+            const auto f = M::computed(x);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma(o2[n], f, tY.frag(16 * n + c, k + 8 * q));
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int col = c0 + 16 * n + c;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (t0 + i0 + r < a.steps && col < dv)
+                    at_out<E>(a.out, w.b, t0 + i0 + r, w.h)[col] = from_float<E>(a.scale * (damp(s_g.gam[i0 + r], o1[n][r]) + o2[n][r]));
+        }
+        const float last = s_g.last;
+#pragma unroll
+        for (int s = 0; s < RS; ++s) {
+            const int r0 = 16 * (wave * RS + s);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) S[s][n] = last == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : S[s][n] * last;
+#pragma unroll
+            for (int k = 0; k < C; k += 32) {
+                const auto f = tK.frag(r0 + c, k + 8 * q);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma(S[s][n], f, tZ.frag(16 * n + c, k + 8 * q));
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
+        }
+        __syncthreads();                    // K^T and the gates are free again
+    }
+    const int n = min(NB, dv - c0);
+    if (a.steps > chunks * C) zero_rows<E>(a.out, w, chunks * C, a.steps, c0, n);
+    if (!a.state_out) return;
+#pragma unroll
+    for (int s = 0; s < RS; ++s)
+#pragma unroll
+        for (int m = 0; m < NT; ++m) {
+            const int col = c0 + 16 * m + c, r0 = 16 * (wave * RS + s) + 4 * q;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r0 + r < dk && col < dv) a.state_out[((int64_t)w.bh * dk + r0 + r) * dv + col] = S[s][m][r];
+        }
+}
+
+// =============================================================================================
+// Gradient, chunks in reverse order: dV, and what delta_back_kernel needs of every chunk (dS1, dY, dX).
+// =============================================================================================
+template <typename M, int DK> struct BackScanLds {
+    using S = Tile<M, NB, DK, false>;       // dS^T [column][dim_k]
+    using O = Tile<M, NB, C, true>;         // dO^T [column][token]
+    using X = Tile<M, NB, C, false>;        // dR^T, (gam o dX)^T, (gam o dO)^T [column][token]
+    using K = Tile<M, DK, C, true>;         // K^T, Q^T [dim_k][token]
+    static constexpr int S0 = 0, O0 = S0 + S::BYTES, X0 = O0 + O::BYTES, Y0 = X0 + X::BYTES, Z0 = Y0 + X::BYTES, K0 = Z0 + X::BYTES,
+                         Q0 = K0 + K::BYTES, BYTES = Q0 + K::BYTES;
+};
+template <typename M, int DK, bool AL>
+__global__ __launch_bounds__(256) void delta_back_scan_kernel(DeltaArgs a) {
+    using E = typename M::E;
+    using L = BackScanLds<M, DK>;
+    constexpr int RS = DK / 64, NT = NB / 16;
+    extern __shared__ __align__(16) unsigned char lds[];
+    __shared__ Gates s_g;
+    const typename L::S tS(lds + L::S0);
+    const typename L::O tO(lds + L::O0);
+    const typename L::X tR(lds + L::X0), tX(lds + L::Y0), tG(lds + L::Z0);
+    const typename L::K tK(lds + L::K0), tQ(lds + L::Q0);
+    const Where w = where_of(a, blockIdx.y);
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, q = l >> 4, c0 = blockIdx.x * NB;
+    const int dk = a.dim_k, dv = a.dim_v;
+    floatx4 S[RS][NT];
+#pragma unroll
+    for (int s = 0; s < RS; ++s)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int col = c0 + 16 * n + c, row = 16 * (wave * RS + s) + 4 * q;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                S[s][n][r] = a.state_grad && row + r < dk && col < dv ? a.state_grad[((int64_t)w.bh * dk + row + r) * dv + col] : 0.f;
+            tS.put4(16 * n + c, row, S[s][n]);
+        }
+    const int chunks = (w.len + C - 1) / C;
+    for (int ch = chunks - 1; ch >= 0; --ch) {
+        const int len = min(w.len - ch * C, C);
+        const int64_t t0 = (int64_t)ch * C, at_chunk = (int64_t)w.bh * a.chunks + ch;
+        const E* kp = at<E>(a.k, w.b, t0, w.hk);
+        gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
+        stage_transposed<M, DK, AL>(tK, kp, a.k.t, len, dk);
+        stage_transposed<M, DK, AL>(tQ, at<E>(a.q, w.b, t0, w.hk), a.q.t, len, dk);
+        stage_transposed<M, NB, AL>(tO, at<E>(a.out_grad, w.b, t0, w.h), a.out_grad.t, len, dv, c0);
+        {
+            float* o = a.dS + at_chunk * DK * a.dvp;
+#pragma unroll
+            for (int s = 0; s < RS; ++s)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[(int64_t)(16 * (wave * RS + s) + 4 * q + r) * a.dvp + c0 + 16 * n + c] = S[s][n][r];
+        }
+        __syncthreads();
+        const int i0 = 16 * wave + 4 * q, row = 16 * wave + c;
+        floatx4 y1[NT] = {}, y2[NT] = {};
+#pragma unroll
+        for (int d = 0; d < DK; d += 32) {
+            float x[8];
+            load8<E, AL>(kp + row * a.k.t, d + 8 * q, dk, row < len, x);
+            const auto f = M::exact(x);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma(y1[n], f, tS.frag(16 * n + c, d + 8 * q));
+        }
+        const float* P = a.P + at_chunk * C * C;
+        for (int k = wave / 2 * 32; k < C; k += 32) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = P[(k + 8 * q + j) * C + row];
+            const auto f = M::computed(x);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma(y2[n], f, tO.frag(16 * n + c, k + 8 * q));
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            floatx4 dr, go;
+            const floatx4 o = tO.get4(16 * n + c, i0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float dy = a.scale * y2[n][r] + s_g.end[i0 + r] * y1[n][r];
+                a.dY[(at_chunk * C + i0 + r) * a.dvp + c0 + 16 * n + c] = dy;
+                dr[r] = s_g.beta[i0 + r] * dy;
+                go[r] = a.scale * s_g.gam[i0 + r] * o[r];
+            }
+            tR.put4(16 * n + c, i0, dr);
+            tG.put4(16 * n + c, i0, go);
+        }
+        __syncthreads();
+        floatx4 dx[NT] = {};
+        const float* T = a.T + at_chunk * C * C;
+        for (int k = wave / 2 * 32; k < C; k += 32) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = T[(k + 8 * q + j) * C + row];
+            const auto f = M::computed(x);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma(dx[n], f, tR.frag(16 * n + c, k + 8 * q));
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int col = c0 + 16 * n + c;
+            floatx4 gx;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                a.dX[(at_chunk * C + i0 + r) * a.dvp + col] = dx[n][r];
+                if (t0 + i0 + r < a.steps && col < dv)
+                    at_out<E>(a.dv, w.b, t0 + i0 + r, w.h)[col] = from_float<E>(i0 + r < len ? dx[n][r] : 0.f);
+                gx[r] = -s_g.gam[i0 + r] * dx[n][r];
+            }
+            tX.put4(16 * n + c, i0, gx);
+        }
+        __syncthreads();
+        const float last = s_g.last;
+#pragma unroll
+        for (int s = 0; s < RS; ++s) {
+            const int r0 = 16 * (wave * RS + s);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) S[s][n] = last == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : S[s][n] * last;
+#pragma unroll
+            for (int k = 0; k < C; k += 32) {
+                const auto fk = tK.frag(r0 + c, k + 8 * q);
+                const auto fq = tQ.frag(r0 + c, k + 8 * q);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    mma(S[s][n], fk, tX.frag(16 * n + c, k + 8 * q));
+                    mma(S[s][n], fq, tG.frag(16 * n + c, k + 8 * q));
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
+        }
+        __syncthreads();
+    }
+    const int n = min(NB, dv - c0);
+    if (a.steps > chunks * C) zero_rows<E>(a.dv, w, chunks * C, a.steps, c0, n);
+    if (!a.dstate) return;
+#pragma unroll
+    for (int s = 0; s < RS; ++s)
+#pragma unroll
+        for (int m = 0; m < NT; ++m) {
+            const int col = c0 + 16 * m + c, r0 = 16 * (wave * RS + s) + 4 * q;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r0 + r < dk && col < dv) a.dstate[((int64_t)w.bh * dk + r0 + r) * dv + col] = S[s][m][r];
+        }
+}
+
+// =============================================================================================
+// Gradient, all chunks at once: dQ, dK, dbeta, dg.  A wavefront takes 16 tokens; contractions over the columns read
+// their operands straight from memory, those over tokens from LDS.
+// =============================================================================================
+template <typename M, int DK> struct BackLds {
+    using W = Tile<M, C, C, false>;         // E, E^T, F diag(beta), F^T
+    using K = Tile<M, DK, C, true>;         // K^T, Q^T
+    static constexpr int E0 = 0, ET0 = E0 + W::BYTES, F0 = ET0 + W::BYTES, FT0 = F0 + W::BYTES, K0 = FT0 + W::BYTES, Q0 = K0 + K::BYTES,
+                         BYTES = Q0 + K::BYTES;
+};
+__device__ __forceinline__ float sum16(float x) {      // over the 16 lanes that hold one row of a result
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) x += __shfl_xor(x, d);
+    return x;
+}
+template <typename M, int DK, bool AL>
+__global__ __launch_bounds__(256) void delta_back_kernel(DeltaArgs a) {
+    using E = typename M::E;
+    using L = BackLds<M, DK>;
+    constexpr int NK = DK / 16;
+    extern __shared__ __align__(16) unsigned char lds[];
+    __shared__ Gates s_g;
+    __shared__ float s_dG[C], s_ext[4];
+    const typename L::W tE(lds + L::E0), tET(lds + L::ET0), tF(lds + L::F0), tFT(lds + L::FT0);
+    const typename L::K tK(lds + L::K0), tQ(lds + L::Q0);
+    const Where w = where_of(a, blockIdx.y);
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, q = l >> 4;
+    const int dk = a.dim_k, ch = blockIdx.x;
+    const int64_t t0 = (int64_t)ch * C, at_chunk = (int64_t)w.bh * a.chunks + ch;
+    const int len = min(w.len - ch * C, C), rows = min(a.steps - ch * C, C);
+    // one value head per key head: straight to the results; else to one row per value head, added up afterwards
+    auto put = [&](const DeltaSeq& s, float* part, int i, int d, float x) {
+        if (part) part[(((int64_t)w.b * a.steps + t0 + i) * a.heads_v + w.h) * dk + d] = x;
+        else at_out<E>(s, w.b, t0 + i, w.h)[d] = from_float<E>(x);
+    };
+    if (len <= 0) {
+        for (int i = threadIdx.x; i < rows * dk; i += 256) { put(a.dq, a.part_q, i / dk, i % dk, 0.f); put(a.dk, a.part_k, i / dk, i % dk, 0.f); }
+        for (int i = threadIdx.x; i < rows; i += 256) { *at_out<float>(a.dg, w.b, t0 + i, w.h) = 0.f; *at_out<float>(a.dbeta, w.b, t0 + i, w.h) = 0.f; }
+        return;
+    }
+    gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
+    stage_transposed<M, DK, AL>(tK, at<E>(a.k, w.b, t0, w.hk), a.k.t, len, dk);
+    stage_transposed<M, DK, AL>(tQ, at<E>(a.q, w.b, t0, w.hk), a.q.t, len, dk);
+    __syncthreads();
+    const int row = 16 * wave + c, i0 = 16 * wave + 4 * q;
+    const float* R = a.R + at_chunk * C * a.dvp;
+    const float* dX = a.dX + at_chunk * C * a.dvp;
+    const float* dY = a.dY + at_chunk * C * a.dvp;
+    const float* S0 = a.S + at_chunk * DK * a.dvp;
+    const float* S1 = a.dS + at_chunk * DK * a.dvp;
+    const E* dO = at<E>(a.out_grad, w.b, t0, w.h);
+    floatx4 dq[NK] = {}, ks[NK] = {}, ke[NK] = {}, e[4] = {}, f[4] = {};
+    float yr = 0.f, ss = 0.f;               // dY.R of row `row` (this lane's columns), <dS1, S0> of this lane's elements
+    for (int d = 0; d < a.dvp; d += 32) {
+        float x[8], y[8];
+        load8<E, AL>(dO + row * a.out_grad.t, d + 8 * q, a.dim_v, row < len, x);
+        const auto fo = M::exact(x);
+        load8(dX + row * a.dvp + d + 8 * q, x);
+        const auto fx = M::computed(x);
+        load8(R + row * a.dvp + d + 8 * q, x);
+        load8(dY + row * a.dvp + d + 8 * q, y);
+        const float beta = s_g.beta[row];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { yr += x[j] * y[j]; x[j] *= beta; }
+        const auto fy = M::computed(x);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            if (n > wave) break;
+            load8(R + (16 * n + c) * a.dvp + d + 8 * q, x);
+            const auto g = M::computed(x);
+            mma(f[n], fx, g);
+            const float b = s_g.beta[16 * n + c];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] *= b;
+            const auto h = M::computed(x);
+            mma(e[n], fo, h);
+        }
+#pragma unroll
+        for (int n = 0; n < NK; ++n) {
+            load8(S0 + (16 * n + c) * a.dvp + d + 8 * q, x);
+            load8(S1 + (16 * n + c) * a.dvp + d + 8 * q, y);
+            if ((n & 3) == wave) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) ss += x[j] * y[j];
+            }
+            const auto g = M::computed(x);
+            mma(dq[n], fo, g);
+            mma(ks[n], fx, g);
+            mma(ke[n], fy, M::computed(y));
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const int j = 16 * n + c;
+        floatx4 x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = i0 + r;
+            const float g = i >= j ? decay(s_g, i, j) : 0.f;
+            e[n][r] *= a.scale * g;
+            f[n][r] = i > j ? -g * f[n][r] : 0.f;
+            x[r] = f[n][r] * s_g.beta[j];
+        }
+        // rows of the transposes are columns here: four consecutive elements of one row each; of the others one at a time
+        tET.put4(j, i0, e[n]);
+        tFT.put4(j, i0, f[n]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { tE.put1(i0 + r, j, e[n][r]); tF.put1(i0 + r, j, x[r]); }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float g = s_g.gam[i0 + r], en = s_g.end[i0 + r];
+#pragma unroll
+        for (int n = 0; n < NK; ++n) { dq[n][r] = damp(a.scale * g, dq[n][r]); ks[n][r] = damp(-g, ks[n][r]); ke[n][r] = damp(en, ke[n][r]); }
+    }
+    __syncthreads();
+    floatx4 ft[NK] = {};                    // F^T K
+    for (int k = 0; k < 16 * (wave + 1); k += 32) {     // E and F diag(beta): lower triangles
+        const auto fe = tE.frag(row, k + 8 * q);
+        const auto ff = tF.frag(row, k + 8 * q);
+#pragma unroll
+        for (int n = 0; n < NK; ++n) {
+            const auto g = tK.frag(16 * n + c, k + 8 * q);
+            mma(dq[n], fe, g);
+            mma(ks[n], ff, g);
+        }
+    }
+    float kdot_end[4] = {}, kdot[4] = {}, kft[4] = {};
+#pragma unroll
+    for (int n = 0; n < NK; ++n) {          // before E^T Q joins it: the part of dG_last
+        const floatx4 kv = tK.get4(16 * n + c, i0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) kdot_end[r] += kv[r] * ke[n][r];
+    }
+    for (int k = wave / 2 * 32; k < C; k += 32) {
+        const auto fe = tET.frag(row, k + 8 * q);
+        const auto ff = tFT.frag(row, k + 8 * q);
+#pragma unroll
+        for (int n = 0; n < NK; ++n) {
+            mma(ke[n], fe, tQ.frag(16 * n + c, k + 8 * q));
+            mma(ft[n], ff, tK.frag(16 * n + c, k + 8 * q));
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NK; ++n) {
+        const floatx4 kv = tK.get4(16 * n + c, i0), qv = tQ.get4(16 * n + c, i0);
+        const int d = 16 * n + c;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            kft[r] += kv[r] * ft[n][r];
+            const float rest = ke[n][r] + s_g.beta[i0 + r] * ft[n][r];
+            kdot[r] += qv[r] * dq[n][r] + kv[r] * (ks[n][r] - rest);
+            if (i0 + r < rows && d < dk) {
+                const bool in = i0 + r < len;
+                put(a.dq, a.part_q, i0 + r, d, in ? dq[n][r] : 0.f);
+                put(a.dk, a.part_k, i0 + r, d, in ? ks[n][r] + rest : 0.f);
+            }
+        }
+    }
+    // dY.R of one row lies in the lanes c, c + 16, c + 32, c + 48
+    yr += __shfl_xor(yr, 16);
+    yr += __shfl_xor(yr, 32);
+    float ext = 0.f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float b = sum16(kft[r]) + __shfl(yr, 4 * q + r);
+        const float g = sum16(kdot[r]);
+        ext += sum16(kdot_end[r]);
+        if (c == 0) {
+            s_dG[i0 + r] = g;
+            if (i0 + r < rows) *at_out<float>(a.dbeta, w.b, t0 + i0 + r, w.h) = i0 + r < len ? b : 0.f;
+        }
+    }
+    ss = sum16(ss);                         // over the wavefront: 16 lanes here, the four groups of them below
+    float both = ext + damp(s_g.last, ss);
+    both += __shfl_xor(both, 16);
+    both += __shfl_xor(both, 32);
+    if (l == 0) s_ext[wave] = both;
+    __syncthreads();
+    if (wave == 0) {                        // sums from the end to each token, within its segment
+        float x = s_dG[l];
+        if (l == 63) x += s_ext[0] + s_ext[1] + s_ext[2] + s_ext[3];
+        const int part = s_g.part[l];
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const float o = __shfl_down(x, d);
+            const int p = __shfl_down(part, d);
+            if (l + d < 64 && p == part) x += o;
+        }
+        if (l < rows) *at_out<float>(a.dg, w.b, t0 + l, w.h) =
+            l < len && *at<float>(a.g, w.b, t0 + l, w.h) != NEG_INF ? x : 0.f;
+    }
+}
+
+// dq and dk of shared key heads: the sum over their value heads, in order.
+template <typename E>
+__global__ __launch_bounds__(256) void delta_group_kernel(DeltaArgs a) {
+    const int64_t all = (int64_t)a.batch * a.steps * a.heads_k * a.dim_k;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < 2 * all; i += (int64_t)gridDim.x * 256) {
+        const bool second = i >= all;
+        const int64_t j = second ? i - all : i;
+        const int d = (int)(j % a.dim_k);
+        const int64_t r = j / a.dim_k;      // (b, t, key head)
+        const int h = (int)(r % a.heads_k);
+        const int64_t bt = r / a.heads_k;
+        const float* p = (second ? a.part_k : a.part_q) + (bt * a.heads_v + (int64_t)h * a.group) * a.dim_k + d;
+        float x = p[0];
+        for (int g = 1; g < a.group; ++g) x += p[(int64_t)g * a.dim_k];
+        *(at_out<E>(second ? a.dk : a.dq, (int)(bt / a.steps), bt % a.steps, h) + d) = from_float<E>(x);
+    }
+}
+
+// ---- launches -------------------------------------------------------------------------------
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+struct Plan {                               // padded sizes, and where things lie in `saved` and the workspace
+    int dkp, dvp, chunks;
+    size_t T, P, R, S, saved;               // offsets in bytes
+    size_t dX, dY, dS, part_q, part_k, back;
+};
+bool shape_ok(const pql_delta_shape& s) {
+    return s.batch >= 0 && s.steps >= 0 && s.heads_k >= 1 && s.heads_v >= 1 && s.heads_v % s.heads_k == 0 && s.dim_k >= 1 &&
+           s.dim_k <= PQL_DELTA_MAX_DIM_K && s.dim_v >= 1 && s.dim_v <= PQL_DELTA_MAX_DIM_V && (s.dtype == PQL_F32 || s.dtype == PQL_BF16) &&
+           s.scale == s.scale && s.steps <= (1 << 30) && s.heads_v <= 65535 && (int64_t)s.batch * s.heads_v <= 0x7fffffffLL / 256;
+}
+Plan plan_of(const pql_delta_shape& s) {
+    Plan p;
+    p.dkp = s.dim_k <= 64 ? 64 : 128;
+    p.dvp = (s.dim_v + NB - 1) / NB * NB;
+    p.chunks = (s.steps + C - 1) / C;
+    const size_t n = (size_t)s.batch * s.heads_v * p.chunks;
+    size_t o = 0;
+    auto take = [&](size_t floats) { const size_t at = o; o += up256(floats * 4); return at; };
+    p.T = take(n * C * C); p.P = take(n * C * C); p.R = take(n * C * p.dvp); p.S = take(n * p.dkp * p.dvp);
+    p.saved = o;
+    o = 0;
+    p.dX = take(n * C * p.dvp); p.dY = take(n * C * p.dvp); p.dS = take(n * p.dkp * p.dvp);
+    const size_t part = s.heads_v == s.heads_k ? 0 : (size_t)s.batch * s.steps * s.heads_v * s.dim_k;
+    p.part_q = take(part); p.part_k = take(part);
+    p.back = o;
+    return p;
+}
+DeltaSeq seq(const pql_seq& s) { return DeltaSeq{s.data, s.stride_b, s.stride_t, s.stride_h}; }
+bool rows_aligned(const pql_seq& s, int dim, int dtype) {
+    const int n = dtype == PQL_F32 ? 4 : 8;             // elements in 16 bytes
+    return ((uintptr_t)s.data & 15) == 0 && s.stride_b % n == 0 && s.stride_t % n == 0 && s.stride_h % n == 0 && dim % 8 == 0;
+}
+// Elements of an output must not share a place: a stride of 0 is for inputs only.
+bool apart(const pql_seq& s, const pql_delta_shape& x, int heads) {
+    return (x.batch <= 1 || s.stride_b != 0) && (x.steps <= 1 || s.stride_t != 0) && (heads <= 1 || s.stride_h != 0);
+}
+DeltaArgs args_of(const pql_delta_shape& s, const pql_delta_input& in) {
+    DeltaArgs a{};
+    a.batch = s.batch; a.steps = s.steps; a.heads_k = s.heads_k; a.heads_v = s.heads_v; a.group = s.heads_v / s.heads_k;
+    a.dim_k = s.dim_k; a.dim_v = s.dim_v; a.scale = s.scale;
+    a.q = seq(in.q); a.k = seq(in.k); a.v = seq(in.v); a.g = seq(in.log_decay); a.beta = seq(in.beta);
+    a.lengths = in.lengths; a.state = in.state;
+    return a;
+}
+int32_t check_input(pql_ctx* c, const pql_delta_shape* s, const pql_delta_input* in, const char* shape_text, const char* null_text, const char* align_text) {
+    if (!s || !in) return ctx_fail(c, PQL_ERR_NULL, null_text);
+    if (!shape_ok(*s)) return ctx_fail(c, PQL_ERR_INVALID_ARG, shape_text);
+    if (s->batch == 0) return PQL_OK;
+    const unsigned es = s->dtype == PQL_F32 ? 4 : 2;
+    if (s->steps > 0 && (!in->q.data || !in->k.data || !in->v.data || !in->log_decay.data || !in->beta.data)) return ctx_fail(c, PQL_ERR_NULL, null_text);
+    if (((uintptr_t)in->q.data | (uintptr_t)in->k.data | (uintptr_t)in->v.data) & (es - 1)) return ctx_fail(c, PQL_ERR_ALIGNMENT, align_text);
+    if ((((uintptr_t)in->log_decay.data | (uintptr_t)in->beta.data | (uintptr_t)in->lengths) & 3) || ((uintptr_t)in->state & 15))
+        return ctx_fail(c, PQL_ERR_ALIGNMENT, align_text);
+    return PQL_OK;
+}
+
+template <typename E, int LX, bool VEC> hipError_t step_launch(const DeltaArgs& a, hipStream_t st) {
+    const double states = 8.0 * a.batch * a.heads_v * a.dim_k * a.dim_v;
+    const double tokens = (double)a.batch * a.steps * (2.0 * a.heads_k * a.dim_k + 2.0 * a.heads_v * a.dim_v) * sizeof(E);
+    const ProfSlot ps = prof_slot();
+    PQL_LAUNCH(ps, (delta_step_kernel<E, LX, VEC>), dim3((unsigned)(a.batch * a.heads_v), (unsigned)((a.dim_v + 4 * LX - 1) / (4 * LX))), dim3(256), 0, st, a);
+    prof_commit(ps, KID_DELTA_STEP, 6.0 * a.batch * a.steps * a.heads_v * a.dim_k * a.dim_v, states + tokens);
+    return hipGetLastError();
+}
+template <typename E> hipError_t step_dispatch(const DeltaArgs& a, hipStream_t st) {
+    const bool vec = a.dim_v % 4 == 0;
+    if (a.dim_v <= 32) return vec ? step_launch<E, 8, true>(a, st) : step_launch<E, 8, false>(a, st);
+    if (a.dim_v <= 64) return vec ? step_launch<E, 16, true>(a, st) : step_launch<E, 16, false>(a, st);
+    return vec ? step_launch<E, 32, true>(a, st) : step_launch<E, 32, false>(a, st);
+}
+
+// blockIdx.y counts sequences times heads, at most 65535 a launch: batches are cut.
+template <typename F> hipError_t by_batch(const DeltaArgs& a, F&& f) {
+    const int most = 65535 / a.heads_v;
+    for (int b = 0; b < a.batch; b += most) {
+        DeltaArgs x = a;
+        x.batch = a.batch - b < most ? a.batch - b : most;
+        x.bh0 = b * a.heads_v;
+        const hipError_t e = f(x);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+template <typename K> hipError_t launch(K kernel, LdsLimit& lim, size_t lds, dim3 grid, const DeltaArgs& a, int kid, double flops, double bytes, hipStream_t st) {
+    if (lds > 32768) {
+        const hipError_t e = set_lds_limit((const void*)kernel, lds, lim);
+        if (e != hipSuccess) return e;
+    }
+    const ProfSlot ps = prof_slot();
+    PQL_LAUNCH(ps, kernel, grid, dim3(256), lds, st, a);
+    prof_commit(ps, kid, flops, bytes);
+    return hipGetLastError();
+}
+// Work of one token and value head that the chunked form cannot do without, and the token tensors' bytes.
+double token_heads(const DeltaArgs& a) { return (double)a.batch * a.steps * a.heads_v; }
+template <typename M, int DK, bool AL> hipError_t forward_launch(const DeltaArgs& all, hipStream_t st) {
+    static LdsLimit l_prep, l_scan;
+    return by_batch(all, [&](const DeltaArgs& a) {
+        const double th = token_heads(a), es = sizeof(typename M::E);
+        hipError_t e = hipSuccess;
+        if (a.chunks > 0)
+            e = launch(delta_prepare_kernel<M, DK, AL>, l_prep, 0, dim3(a.chunks, a.batch * a.heads_v), a, KID_DELTA_PREPARE,
+                       th * 4.0 * C * a.dim_k, th * (2 * es * a.dim_k + 8.0 * C), st);
+        if (e == hipSuccess)
+            e = launch(delta_scan_kernel<M, DK, AL>, l_scan, ScanLds<M, DK>::BYTES, dim3(a.dvp / NB, a.batch * a.heads_v), a, KID_DELTA_SCAN,
+                       th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C), st);
+        return e;
+    });
+}
+template <typename M, int DK, bool AL> hipError_t backward_launch(const DeltaArgs& all, hipStream_t st) {
+    static LdsLimit l_scan, l_back;
+    hipError_t e = by_batch(all, [&](const DeltaArgs& a) {
+        const double th = token_heads(a), es = sizeof(typename M::E);
+        hipError_t e = launch(delta_back_scan_kernel<M, DK, AL>, l_scan, BackScanLds<M, DK>::BYTES, dim3(a.dvp / NB, a.batch * a.heads_v), a,
+                              KID_DELTA_BACK_SCAN, th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C + 8.0 * a.dim_v), st);
+        if (e == hipSuccess && a.chunks > 0)
+            e = launch(delta_back_kernel<M, DK, AL>, l_back, BackLds<M, DK>::BYTES, dim3(a.chunks, a.batch * a.heads_v), a, KID_DELTA_BACK,
+                       th * (6.0 * a.dim_k * a.dim_v + 4.0 * C * a.dim_v + 8.0 * C * a.dim_k), th * (es * (4 * a.dim_k + a.dim_v) + 12.0 * a.dim_v), st);
+        return e;
+    });
+    if (e != hipSuccess || all.group == 1 || all.steps == 0) return e;
+    const int64_t n = 2 * (int64_t)all.batch * all.steps * all.heads_k * all.dim_k;
+    const int64_t blocks = (n + 255) / 256 < 4096 ? (n + 255) / 256 : 4096;
+    const ProfSlot ps = prof_slot();
+    PQL_LAUNCH(ps, delta_group_kernel<typename M::E>, dim3((unsigned)blocks), dim3(256), 0, st, all);
+    prof_commit(ps, KID_DELTA_GROUP, 0.0, (double)n * (4.0 * all.group + sizeof(typename M::E)));
+    return hipGetLastError();
+}
+template <typename M, bool BACK> hipError_t chunks_dispatch(const DeltaArgs& a, bool al, int dkp, hipStream_t st) {
+    if (BACK) {
+        if (dkp == 64) return al ? backward_launch<M, 64, true>(a, st) : backward_launch<M, 64, false>(a, st);
+        return al ? backward_launch<M, 128, true>(a, st) : backward_launch<M, 128, false>(a, st);
+    }
+    if (dkp == 64) return al ? forward_launch<M, 64, true>(a, st) : forward_launch<M, 64, false>(a, st);
+    return al ? forward_launch<M, 128, true>(a, st) : forward_launch<M, 128, false>(a, st);
+}
+void set_saved(DeltaArgs& a, const Plan& p, char* base, bool states) {
+    a.chunks = p.chunks; a.dvp = p.dvp;
+    a.T = (float*)(base + p.T); a.P = (float*)(base + p.P);
+    if (states) { a.R = (float*)(base + p.R); a.S = (float*)(base + p.S); }
+}
+}  // namespace
+}  // namespace pql
+
+using namespace pql;
+
+extern "C" {
+
+int32_t pql_delta_step(pql_ctx* c, const pql_delta_shape* s, const pql_delta_input* in, float* state_out, pql_seq out, void* stream) {
+    if (!c) return PQL_ERR_NULL;
+    const int32_t rc = check_input(c, s, in, "pql_delta_step: bad shape", "pql_delta_step: null pointer", "pql_delta_step: misaligned pointer");
+    if (rc != PQL_OK || s->batch == 0) return rc;
+    if (!state_out || (!out.data && s->steps > 0)) return ctx_fail(c, PQL_ERR_NULL, "pql_delta_step: null pointer");
+    if (!apart(out, *s, s->heads_v)) return ctx_fail(c, PQL_ERR_INVALID_ARG, "pql_delta_step: outputs share memory (stride 0)");
+    if (((uintptr_t)state_out & 15) || ((uintptr_t)out.data & (s->dtype == PQL_F32 ? 3 : 1)))
+        return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_delta_step: misaligned pointer");
+    DeltaArgs a = args_of(*s, *in);
+    a.out = seq(out); a.state_out = state_out;
+    const hipError_t e = s->dtype == PQL_F32 ? step_dispatch<float>(a, (hipStream_t)stream) : step_dispatch<bf16_t>(a, (hipStream_t)stream);
+    return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_delta_step", e);
+}
+
+int64_t pql_delta_saved_bytes(const pql_delta_shape* s) {
+    if (!s) return PQL_ERR_NULL;
+    return shape_ok(*s) ? (int64_t)plan_of(*s).saved : PQL_ERR_INVALID_ARG;
+}
+int64_t pql_delta_workspace_bytes(const pql_delta_shape* s, int32_t backward) {
+    if (!s) return PQL_ERR_NULL;
+    if (!shape_ok(*s)) return PQL_ERR_INVALID_ARG;
+    const Plan p = plan_of(*s);
+    const size_t forward = p.R;             // T and P, where the caller keeps nothing
+    return (int64_t)(backward && p.back > forward ? p.back : forward);
+}
+
+int32_t pql_delta_forward(pql_ctx* c, const pql_delta_shape* s, const pql_delta_input* in, pql_seq out, float* state_out, void* saved,
+                          void* workspace, void* stream) {
+    if (!c) return PQL_ERR_NULL;
+    const int32_t rc = check_input(c, s, in, "pql_delta_forward: bad shape", "pql_delta_forward: null pointer", "pql_delta_forward: misaligned pointer");
+    if (rc != PQL_OK || s->batch == 0) return rc;
+    if (s->steps > 0 && (!out.data || (!saved && !workspace))) return ctx_fail(c, PQL_ERR_NULL, "pql_delta_forward: null pointer");
+    if (!apart(out, *s, s->heads_v)) return ctx_fail(c, PQL_ERR_INVALID_ARG, "pql_delta_forward: outputs share memory (stride 0)");
+    if (((uintptr_t)state_out & 15) || ((uintptr_t)out.data & (s->dtype == PQL_F32 ? 3 : 1)) || ((uintptr_t)saved & 255) || ((uintptr_t)workspace & 255))
+        return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_delta_forward: misaligned pointer");
+    const Plan p = plan_of(*s);
+    DeltaArgs a = args_of(*s, *in);
+    a.out = seq(out); a.state_out = state_out;
+    set_saved(a, p, (char*)(saved ? saved : workspace), saved != nullptr);
+    const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype);
+    const hipError_t e = s->dtype == PQL_F32 ? chunks_dispatch<ModeF, false>(a, al, p.dkp, (hipStream_t)stream)
+                                             : chunks_dispatch<ModeB, false>(a, al, p.dkp, (hipStream_t)stream);
+    return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_delta_forward", e);
+}
+
+int32_t pql_delta_backward(pql_ctx* c, const pql_delta_shape* s, const pql_delta_input* in, const void* saved, pql_seq out_grad,
+                           const float* state_out_grad, const pql_delta_grad* g, void* workspace, void* stream) {
+    if (!c) return PQL_ERR_NULL;
+    const int32_t rc = check_input(c, s, in, "pql_delta_backward: bad shape", "pql_delta_backward: null pointer", "pql_delta_backward: misaligned pointer");
+    if (rc != PQL_OK || (s->batch == 0 && g)) return rc;
+    if (!g || (s->steps > 0 && (!saved || !workspace || !out_grad.data || !g->q.data || !g->k.data || !g->v.data || !g->log_decay.data || !g->beta.data)))
+        return ctx_fail(c, PQL_ERR_NULL, "pql_delta_backward: null pointer");
+    if (!apart(g->q, *s, s->heads_k) || !apart(g->k, *s, s->heads_k) || !apart(g->v, *s, s->heads_v) ||
+        !apart(g->log_decay, *s, s->heads_v) || !apart(g->beta, *s, s->heads_v))
+        return ctx_fail(c, PQL_ERR_INVALID_ARG, "pql_delta_backward: gradients share memory (stride 0)");
+    const unsigned es = s->dtype == PQL_F32 ? 4 : 2;
+    if ((((uintptr_t)out_grad.data | (uintptr_t)g->q.data | (uintptr_t)g->k.data | (uintptr_t)g->v.data) & (es - 1)) ||
+        (((uintptr_t)g->log_decay.data | (uintptr_t)g->beta.data) & 3) || (((uintptr_t)state_out_grad | (uintptr_t)g->state) & 15) ||
+        (((uintptr_t)saved | (uintptr_t)workspace) & 255))
+        return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_delta_backward: misaligned pointer");
+    const Plan p = plan_of(*s);
+    DeltaArgs a = args_of(*s, *in);
+    set_saved(a, p, (char*)saved, true);
+    char* w = (char*)workspace;
+    a.out_grad = seq(out_grad); a.state_grad = state_out_grad;
+    a.dq = seq(g->q); a.dk = seq(g->k); a.dv = seq(g->v); a.dg = seq(g->log_decay); a.dbeta = seq(g->beta); a.dstate = g->state;
+    a.dX = (float*)(w + p.dX); a.dY = (float*)(w + p.dY); a.dS = (float*)(w + p.dS);
+    if (a.group > 1) { a.part_q = (float*)(w + p.part_q); a.part_k = (float*)(w + p.part_k); }
+    const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype) && rows_aligned(out_grad, s->dim_v, s->dtype);
+    const hipError_t e = s->dtype == PQL_F32 ? chunks_dispatch<ModeF, true>(a, al, p.dkp, (hipStream_t)stream)
+                                             : chunks_dispatch<ModeB, true>(a, al, p.dkp, (hipStream_t)stream);
+    return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_delta_backward", e);
+}
+
+}  // extern "C"

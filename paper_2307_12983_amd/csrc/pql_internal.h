@@ -22,10 +22,15 @@ enum KernelId : int {
     KID_NORMALIZE = 29, KID_DIST_CRITIC = 30, KID_DIST_POLICY = 31, KID_SAC_SAMPLE = 32, KID_SAC_GRAD = 33,
     KID_SAC_ALPHA = 34, KID_MFMA_PROBE = 35, KID_LAYER_ROWTILE = 36, KID_NARROW_ROWTILE = 37, KID_CHAIN_CRITIC = 38,
     KID_CHAIN_POLICY = 39, KID_CHAIN_ACT = 40, KID_FUSED_ACT16 = 41, KID_SPLIT_WEIGHTS = 42, KID_SPLIT_CRITIC = 43,
-    KID_SPLIT_POLICY = 44, KID_COUNT = 45
+    KID_SPLIT_POLICY = 44,
+    KID_DISTILL = 45, KID_DISTILL_JOIN = 46, KID_DISTILL_GRAD = 47, KID_TOP_LOGITS = 48, KID_TOP_MERGE = 49, KID_DELTA_STEP = 50,
+    KID_DELTA_PREPARE = 51, KID_DELTA_SCAN = 52, KID_DELTA_BACK_SCAN = 53, KID_DELTA_BACK = 54, KID_DELTA_GROUP = 55,
+    KID_COUNT = 56
 };
 const char* kernel_name(int kid);
 bool prof_active();
+// Records `what` (and the HIP error's text, if there is one) as ctx's last error; returns the code.  Never throws.
+int32_t ctx_fail(pql_ctx* ctx, int32_t code, const char* what, hipError_t e = hipSuccess);
 // One timed launch: when profiling is on, prof_slot() hands out an event pair that PQL_LAUNCH
 // attaches to the kernel dispatch itself (the events then carry the dispatch's own begin / end
 // timestamps, with no marker commands in between); prof_commit() files the launch under its

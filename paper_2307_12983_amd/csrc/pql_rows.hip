@@ -1,0 +1,883 @@
+// Operators on rows of logits (include/pql_student.h): a teacher's largest logits of every row, and the
+// distillation loss against such lists with its gradient.  All of them are bound by reading the logits once and, where
+// there is a gradient, writing it once; everything else is arranged around that.
+//
+// Rows of at most SMALL_VOCAB logits are held by a group of 8 to 64 lanes of one wavefront, one element per lane and
+// register, so that a wavefront works on up to eight rows and its reductions take three to six steps.  Longer rows have
+// a workgroup each, which reads 16 bytes per lane and keeps the row in registers between the two uses; few long rows are
+// cut into pieces, joined by a second launch through the workspace.
+#include "pql_student_internal.h"
+
+namespace pql {
+namespace {
+
+constexpr int SMALL_VOCAB = 1024;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float NEG_INF = -__builtin_inff();
+
+// ---- reductions -----------------------------------------------------------------------------
+template <int G> __device__ __forceinline__ float group_max(float x) {
+#pragma unroll
+    for (int d = 1; d < G; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
+    return x;
+}
+template <int G, typename V> __device__ __forceinline__ V group_sum(V x) {
+#pragma unroll
+    for (int d = 1; d < G; d *= 2) x += __shfl_xor(x, d);
+    return x;
+}
+// Over a workgroup of NT threads; every thread gets the result.  `s` holds NT / 64 values and may be used again after the
+// next barrier (each call begins with one).
+template <int NT> __device__ __forceinline__ float block_max(float x, float* s) {
+    x = group_max<64>(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = s[0];
+#pragma unroll
+    for (int i = 1; i < NT / 64; ++i) x = fmaxf(x, s[i]);
+    return x;
+}
+template <int NT, typename V> __device__ __forceinline__ V block_sum(V x, V* s) {
+    x = group_sum<64>(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = s[0];
+#pragma unroll
+    for (int i = 1; i < NT / 64; ++i) x += s[i];
+    return x;
+}
+
+// ---- a stretch of one row, read 16 bytes per lane --------------------------------------------
+// Elements [0, len) at p, of any alignment: `head` elements up to the first 16-byte boundary, `vecs` granules of VEC
+// elements, `tail` elements.  Head and tail together are fewer than 2 * VEC <= 16, one for each of the first threads.
+template <typename E> struct Stretch {
+    static constexpr int VEC = 16 / (int)sizeof(E);
+    const E* p;
+    int len, head, vecs, tail;
+    __device__ __forceinline__ Stretch(const E* q, int n) : p(q), len(n) {
+        const int to = (int)((16 - ((uintptr_t)q & 15)) & 15) / (int)sizeof(E);
+        head = to < n ? to : n;
+        vecs = (n - head) / VEC;
+        tail = n - head - vecs * VEC;
+    }
+    // the place of this thread's single element, or -1
+    __device__ __forceinline__ int single(int t) const {
+        return t < head ? t : t < head + tail ? len - tail + (t - head) : -1;
+    }
+    __device__ __forceinline__ int place(int v) const { return head + v * VEC; }
+    __device__ __forceinline__ uint4 granule(int v) const { return *(const uint4*)(p + place(v)); }
+};
+template <typename E> __device__ __forceinline__ void unpack(uint4 g, float* x);
+template <> __device__ __forceinline__ void unpack<float>(uint4 g, float* x) {
+    x[0] = __uint_as_float(g.x); x[1] = __uint_as_float(g.y); x[2] = __uint_as_float(g.z); x[3] = __uint_as_float(g.w);
+}
+template <> __device__ __forceinline__ void unpack<bf16_t>(uint4 g, float* x) {
+    const unsigned u[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+}
+template <typename E> __device__ __forceinline__ void store_granule(E* p, bool aligned, const float* x) {
+    constexpr int VEC = 16 / (int)sizeof(E);
+    if (aligned) {
+        union { E e[VEC]; uint4 u; } w;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) w.e[i] = from_float<E>(x[i]);
+        *(uint4*)p = w.u;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) p[i] = from_float<E>(x[i]);
+    }
+}
+
+// ---- the teacher's list ------------------------------------------------------------------------
+// p_k = softmax of the valid entries' values / t, by the first `top` threads of a workgroup.  Entries of one answer are
+// added up at the first of them, in the order of the list: `sum` is the whole mass of this thread's answer if it is that
+// first entry (`owner`).  Returns whether the row has a valid entry at all.
+struct Entry { int index; float p, log_p, sum; bool owner; };
+template <int NT>
+__device__ __forceinline__ bool teacher_entries(const DistillArgs& a, int64_t n, Entry& e, int* s_index, float* s_p, float* s_red) {
+    const int k = threadIdx.x;
+    e.index = -1; e.p = 0.f; e.log_p = 0.f; e.sum = 0.f; e.owner = false;
+    float y = NEG_INF;
+    if (k < a.top) {
+        const int i = a.index[n * a.top + k];
+        if ((unsigned)i < (unsigned)a.vocab) y = a.value[n * a.top + k];
+        if (y != NEG_INF) e.index = i;
+    }
+    const float big = block_max<NT>(y, s_red);
+    const bool some = __syncthreads_or(e.index >= 0);
+    const float shift = big == NEG_INF ? 0.f : big;
+    const float x = (y - shift) * a.inv_temp, m = e.index >= 0 ? expf(x) : 0.f;
+    const float total = block_sum<NT>(m, s_red);
+    if (e.index >= 0) { e.p = m / total; e.log_p = x - logf(total); }
+    if (k < a.top) { s_index[k] = e.index; s_p[k] = e.p; }
+    __syncthreads();
+    if (e.index >= 0) {
+        e.owner = true;
+        for (int i = 0; i < a.top; ++i)
+            if (s_index[i] == e.index) {
+                if (i < k) { e.owner = false; break; }
+                e.sum += s_p[i];
+            }
+    }
+    return some;
+}
+// One entry's share of the loss: p (log p - log q) with log q = (z - m) / t - log(s); nothing for p = 0, +inf where the
+// student has the answer at -inf (also in a row that holds nothing else).
+__device__ __forceinline__ float entry_loss(const Entry& e, float z, float m, float inv_temp, float log_s) {
+    return e.p == 0.f ? 0.f : z == NEG_INF ? -NEG_INF : e.p * (e.log_p - ((z - m) * inv_temp - log_s));
+}
+
+// =============================================================================================
+// Small vocabularies: a group of G lanes per row.
+// =============================================================================================
+template <typename E, int G, int R, bool BACK>
+__global__ __launch_bounds__(256) void distill_small_kernel(DistillArgs a) {
+    constexpr int ROWS = 256 / G;
+    extern __shared__ float lds[];
+    const int g = threadIdx.x / G, l = threadIdx.x & (G - 1);
+    float* s_p = lds + (size_t)g * (2 * a.top);             // the list's masses, then its indices
+    int* s_index = (int*)(s_p + a.top);
+    float* s_t = lds + (size_t)ROWS * 2 * a.top + (size_t)g * a.vocab;      // target mass of every answer
+    const int64_t n = (int64_t)blockIdx.x * ROWS + g;
+    const bool in = n < a.rows;
+    const float w = !in ? 0.f : a.weight ? a.weight[n] : 1.f;
+    float big = NEG_INF;
+    int valid = 0;
+    for (int k = l; k < a.top; k += G) {
+        const int i = in ? a.index[n * a.top + k] : -1;
+        const float y = (unsigned)i < (unsigned)a.vocab ? a.value[n * a.top + k] : NEG_INF;
+        const bool ok = y != NEG_INF;
+        s_index[k] = ok ? i : -1;
+        s_p[k] = y;
+        valid |= ok;
+        big = fmaxf(big, y);
+    }
+    big = group_max<G>(big);
+    const bool read = w != 0.f && group_sum<G>(valid) != 0;
+    float z[R];
+    const E* row = (const E*)a.z + n * a.stride;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int j = l + G * r;
+        z[r] = read && j < a.vocab ? to_float(row[j]) : NEG_INF;
+        if (j < a.vocab) s_t[j] = 0.f;
+    }
+    const float shift = big == NEG_INF ? 0.f : big;
+    float total = 0.f;
+    for (int k = l; k < a.top; k += G) total += s_index[k] >= 0 ? expf((s_p[k] - shift) * a.inv_temp) : 0.f;
+    total = group_sum<G>(total);
+    const float log_total = logf(total);
+    float plogp = 0.f;
+    for (int k = l; k < a.top; k += G) {
+        if (s_index[k] < 0) continue;
+        const float x = (s_p[k] - shift) * a.inv_temp, p = expf(x) / total;
+        if (p != 0.f) plogp += p * (x - log_total);
+        s_p[k] = p;
+    }
+    __syncthreads();
+    for (int k = l; k < a.top; k += G) {                    // entries of one answer are added in the list's order
+        const int i = s_index[k];
+        if (i < 0) continue;
+        float sum = 0.f;
+        bool owner = true;
+        for (int q = 0; q < a.top; ++q)
+            if (s_index[q] == i) {
+                if (q < k) { owner = false; break; }
+                sum += s_p[q];
+            }
+        if (owner) s_t[i] = sum;
+    }
+    __syncthreads();
+    const float c = LOG2E * a.inv_temp;
+    float m = 0.f, inv = 0.f;
+    if (BACK) {
+        m = read ? a.lse[n] : 0.f;                          // q = exp(z / t - lse)
+    } else {
+        m = z[0];
+#pragma unroll
+        for (int r = 1; r < R; ++r) m = fmaxf(m, z[r]);
+        m = group_max<G>(m);
+        if (m == NEG_INF) m = 0.f;
+    }
+    float s = 0.f, q[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        q[r] = BACK ? exp2f(fmaf(-m, a.temp, z[r]) * c) : exp2f((z[r] - m) * c);
+        s += q[r];
+    }
+    if (BACK) {
+        inv = 1.f;
+        if (m == NEG_INF) inv = 0.f;
+    } else {
+        s = group_sum<G>(s);
+        inv = s > 0.f || s != s ? 1.f / s : 0.f;
+        const float log_s = logf(s);
+        float loss = plogp;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int j = l + G * r;
+            const float t = j < a.vocab ? s_t[j] : 0.f;
+            if (t != 0.f) loss -= z[r] == NEG_INF ? NEG_INF : t * ((z[r] - m) * a.inv_temp - log_s);
+        }
+        loss = group_sum<G>(loss);
+        if (l == 0 && in) {
+            a.loss_out[n] = read ? w * a.temp * a.temp * loss : 0.f;
+            a.lse_out[n] = read ? m * a.inv_temp + log_s : 0.f;
+        }
+    }
+    if (a.grad == nullptr || !in) return;
+    E* out = (E*)a.grad + n * a.grad_stride;
+    const float f = w * a.temp;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int j = l + G * r;
+        if (j < a.vocab) out[j] = from_float<E>(read ? f * ((inv > 0.f || inv != inv ? q[r] * inv : 0.f) - s_t[j]) : 0.f);
+    }
+}
+
+// =============================================================================================
+// Long rows.  A piece is a stretch of a row; one workgroup per piece.
+// =============================================================================================
+// Running maximum and sum of exp((z - m) c) over a stretch, of this thread's elements.
+template <typename E, int NT>
+__device__ __forceinline__ void stretch_stats(const Stretch<E>& st, float c, float& m, float& s) {
+    constexpr int VEC = Stretch<E>::VEC, UNROLL = 4;
+    m = NEG_INF; s = 0.f;
+    const int t = threadIdx.x;
+    const int one = st.single(t);
+    if (one >= 0) { m = to_float(st.p[one]); s = m == NEG_INF ? 0.f : 1.f; }
+    int v = t;
+    for (; v < st.vecs; v += UNROLL * NT) {
+        uint4 g[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) if (v + u * NT < st.vecs) g[u] = st.granule(v + u * NT);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            if (v + u * NT >= st.vecs) break;
+            float x[VEC], b = m;
+            unpack<E>(g[u], x);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) b = fmaxf(b, x[i]);
+            const float ref = b == NEG_INF ? 0.f : b;
+            s *= exp2f((m - ref) * c);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s += exp2f((x[i] - ref) * c);
+            m = b;
+        }
+    }
+}
+// The same joined over the workgroup; m is 0 where the stretch holds nothing but -inf (and s = 0).
+template <int NT> __device__ __forceinline__ void join_stats(float c, float& m, float& s, float* s_red) {
+    const float b = block_max<NT>(m, s_red), ref = b == NEG_INF ? 0.f : b;
+    s *= exp2f((m - ref) * c);
+    if (m == NEG_INF) s = s != s ? s : 0.f;
+    s = block_sum<NT>(s, s_red);
+    m = ref;
+}
+// Gradient of a stretch: f * exp2((z - m t) c) * inv for every element, the listed answers patched afterwards.  m t is
+// the row's maximum (t = 1), or the log-sum-exp times the temperature: one rounding of a difference that is small where
+// the result is not.
+template <typename E, int NT>
+__device__ __forceinline__ void stretch_grad(const Stretch<E>& st, E* out, float c, float m, float t_m, float inv, float f) {
+    constexpr int VEC = Stretch<E>::VEC, UNROLL = 4;
+    const int t = threadIdx.x;
+    const float fi = f * inv;
+    const bool aligned = (((uintptr_t)(out + st.head)) & 15) == 0;
+    const int one = st.single(t);
+    if (one >= 0) out[one] = from_float<E>(exp2f(fmaf(-m, t_m, to_float(st.p[one])) * c) * fi);
+    for (int v = t; v < st.vecs; v += UNROLL * NT) {
+        uint4 g[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) if (v + u * NT < st.vecs) g[u] = st.granule(v + u * NT);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            if (v + u * NT >= st.vecs) break;
+            float x[VEC];
+            unpack<E>(g[u], x);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[i] = exp2f(fmaf(-m, t_m, x[i]) * c) * fi;
+            store_granule<E>(out + st.place(v + u * NT), aligned, x);
+        }
+    }
+}
+template <typename E, int NT> __device__ __forceinline__ void zero_stretch(E* out, int len) {
+    for (int j = threadIdx.x; j < len; j += NT) out[j] = from_float<E>(0.f);
+}
+
+// One workgroup per row: statistics, then the gradient from a second read of the row.
+template <typename E, int NT>
+__global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a) {
+    __shared__ int s_index[PQL_MAX_TOP];
+    __shared__ float s_p[PQL_MAX_TOP], s_red[NT / 64];
+    const int64_t n = blockIdx.x;
+    const float w = a.weight ? a.weight[n] : 1.f;
+    Entry e;
+    const bool some = teacher_entries<NT>(a, n, e, s_index, s_p, s_red);
+    E* out = (E*)a.grad + n * a.grad_stride;
+    if (!some || w == 0.f) {
+        if (threadIdx.x == 0) { a.loss_out[n] = 0.f; a.lse_out[n] = 0.f; }
+        if (a.grad) zero_stretch<E, NT>(out, a.vocab);
+        return;
+    }
+    const E* row = (const E*)a.z + n * a.stride;
+    const Stretch<E> st(row, a.vocab);
+    const float zk = e.index >= 0 ? to_float(row[e.index]) : 0.f;
+    const float c = LOG2E * a.inv_temp;
+    float m, s;
+    stretch_stats<E, NT>(st, c, m, s);
+    join_stats<NT>(c, m, s, s_red);
+    const float log_s = logf(s), inv = s > 0.f || s != s ? 1.f / s : 0.f;
+    const float loss = block_sum<NT>(e.index >= 0 ? entry_loss(e, zk, m, a.inv_temp, log_s) : 0.f, s_red);
+    if (threadIdx.x == 0) {
+        a.loss_out[n] = w * a.temp * a.temp * loss;
+        a.lse_out[n] = m * a.inv_temp + log_s;
+    }
+    if (!a.grad) return;
+    const float f = w * a.temp;
+    stretch_grad<E, NT>(st, out, c, m, 1.f, inv, f);
+    __syncthreads();                        // the dense gradient of the listed answers lies before its correction
+    if (e.owner) out[e.index] = from_float<E>(f * ((inv != 0.f ? exp2f((zk - m) * c) * inv : 0.f) - e.sum));
+}
+
+// Few rows: pieces of a.piece elements.  First launch: each piece's maximum and sum, and the logits of the listed
+// answers that lie in it (a second launch that writes over the logits could no longer read them).
+template <typename E, int NT>
+__global__ __launch_bounds__(NT) void distill_part_kernel(DistillArgs a) {
+    __shared__ float s_red[NT / 64];
+    const int64_t n = blockIdx.y;
+    const int j0 = blockIdx.x * a.piece, len = min(a.piece, a.vocab - j0);
+    if (a.weight && a.weight[n] == 0.f) return;
+    const E* row = (const E*)a.z + n * a.stride;
+    for (int k = threadIdx.x; k < a.top; k += NT) {
+        const int i = a.index[n * a.top + k];
+        if (i >= j0 && i < j0 + len) a.part_z[n * a.top + k] = to_float(row[i]);
+    }
+    float m, s;
+    const float c = LOG2E * a.inv_temp;
+    stretch_stats<E, NT>(Stretch<E>(row + j0, len), c, m, s);
+    join_stats<NT>(c, m, s, s_red);
+    if (threadIdx.x == 0) {
+        float* o = a.part + 2 * (n * a.pieces + blockIdx.x);
+        o[0] = s == 0.f ? NEG_INF : m;
+        o[1] = s;
+    }
+}
+// Second launch (JOIN), or the whole backward call: the gradient of one piece.
+template <typename E, int NT, bool JOIN>
+__global__ __launch_bounds__(NT) void distill_piece_kernel(DistillArgs a) {
+    __shared__ int s_index[PQL_MAX_TOP];
+    __shared__ float s_p[PQL_MAX_TOP], s_red[NT / 64];
+    const int64_t n = blockIdx.y;
+    const int j0 = blockIdx.x * a.piece, len = min(a.piece, a.vocab - j0);
+    const float w = a.weight ? a.weight[n] : 1.f;
+    Entry e;
+    const bool some = teacher_entries<NT>(a, n, e, s_index, s_p, s_red);
+    E* out = (E*)a.grad + n * a.grad_stride + j0;
+    if (!some || w == 0.f) {
+        if (JOIN && blockIdx.x == 0 && threadIdx.x == 0) { a.loss_out[n] = 0.f; a.lse_out[n] = 0.f; }
+        if (a.grad) zero_stretch<E, NT>(out, len);
+        return;
+    }
+    const E* row = (const E*)a.z + n * a.stride + j0;
+    const float c = LOG2E * a.inv_temp;
+    float m, inv, zk = 0.f;
+    const float t_m = JOIN ? 1.f : a.temp;
+    const bool mine = e.index >= j0 && e.index < j0 + len;
+    if (JOIN) {
+        float pm = NEG_INF, ps = 0.f;
+        if ((int)threadIdx.x < a.pieces) {
+            pm = a.part[2 * (n * a.pieces + threadIdx.x)];
+            ps = a.part[2 * (n * a.pieces + threadIdx.x) + 1];
+        }
+        join_stats<NT>(c, pm, ps, s_red);
+        m = pm;
+        const float log_s = logf(ps);
+        inv = ps > 0.f || ps != ps ? 1.f / ps : 0.f;
+        if (e.index >= 0) zk = a.part_z[n * a.top + threadIdx.x];
+        if (blockIdx.x == 0) {
+            const float loss = block_sum<NT>(e.index >= 0 ? entry_loss(e, zk, m, a.inv_temp, log_s) : 0.f, s_red);
+            if (threadIdx.x == 0) {
+                a.loss_out[n] = w * a.temp * a.temp * loss;
+                a.lse_out[n] = m * a.inv_temp + log_s;
+            }
+        }
+        if (!a.grad) return;
+    } else {
+        const float lse = a.lse[n];
+        m = lse == NEG_INF ? 0.f : lse;                     // exp(z / t - lse) = exp2((z - t lse) c)
+        inv = lse == NEG_INF ? 0.f : 1.f;
+        if (mine) zk = to_float(row[e.index - j0]);
+        __syncthreads();                                    // read before the gradient may be written over the logits
+    }
+    const float f = w * a.temp;
+    stretch_grad<E, NT>(Stretch<E>(row, len), out, c, m, t_m, inv, f);
+    __syncthreads();
+    if (e.owner && mine) out[e.index - j0] = from_float<E>(f * ((inv != 0.f ? exp2f(fmaf(-m, t_m, zk) * c) * inv : 0.f) - e.sum));
+}
+
+// =============================================================================================
+// The largest logits of every row.  Order: by value, equal values by ascending index.  Values are compared through
+// unsigned keys in the same order; 0 stands for -inf and NaN, which are never selected.
+// =============================================================================================
+__device__ __forceinline__ unsigned key_of(float x) {
+    const unsigned u = __float_as_uint(x);
+    const unsigned k = u & 0x80000000u ? ~u : u | 0x80000000u;
+    return x != x || x == NEG_INF ? 0u : x == 0.f ? 0x80000000u : k;      // -0 and +0 are equal
+}
+// the value in the bits it had: zeros come back as +0
+__device__ __forceinline__ float value_of(unsigned k) {
+    return k == 0u ? NEG_INF : __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
+
+// Small vocabularies: G lanes per row.  The K-th largest key is found bit by bit (largest t with at least K keys >= t),
+// the keys above it and, in index order, as many equal ones as there is room for go to LDS, and each is written at its
+// rank among them.
+template <typename E, int G, int R>
+__global__ __launch_bounds__(256) void top_small_kernel(TopArgs a) {
+    constexpr int ROWS = 256 / G;
+    extern __shared__ unsigned lds_u[];
+    const int g = threadIdx.x / G, l = threadIdx.x & (G - 1);
+    unsigned* s_key = lds_u + (size_t)g * 2 * a.top;
+    int* s_index = (int*)(s_key + a.top);
+    const int64_t n = (int64_t)blockIdx.x * ROWS + g;
+    const bool in = n < a.rows;
+    const E* row = (const E*)a.z + n * a.stride;
+    unsigned key[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int j = l + G * r;
+        key[r] = in && j < a.vocab ? key_of(to_float(row[j])) : 0u;
+    }
+    unsigned t = 0;
+    int at_least = G * R;                   // keys >= t
+    for (int bit = 31; bit >= 0; --bit) {
+        const unsigned u = t | (1u << bit);
+        int cnt = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) cnt += key[r] >= u;
+        cnt = group_sum<G>(cnt);
+        if (at_least != a.top && cnt >= a.top) { t = u; at_least = cnt; }
+        if (__all(at_least == a.top)) break;
+    }
+    if (t == 0) t = 1;                      // fewer than K keys that may be selected: all of them
+    // places: keys above t first, then equal ones by index; lanes in order within a register, registers in order
+    int above = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) above += key[r] > t;
+    int base = above;                       // exclusive prefix of `above` over the group's lanes
+#pragma unroll
+    for (int d = 1; d < G; d *= 2) { const int o = __shfl_up(base, d, G); if (l >= d) base += o; }
+    const int n_above = __shfl(base, G - 1, G);
+    base -= above;
+    int eq_base = n_above;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (key[r] > t) { s_key[base] = key[r]; s_index[base] = l + G * r; ++base; }
+        const unsigned long long mask = __ballot(key[r] == t) >> ((threadIdx.x & 63) / G * G);
+        const unsigned long long grp = G == 64 ? mask : mask & ((1ull << (G & 63)) - 1);
+        const int pos = eq_base + __popcll(grp & ((1ull << l) - 1));
+        if (key[r] == t && pos < a.top) { s_key[pos] = key[r]; s_index[pos] = l + G * r; }
+        eq_base += __popcll(grp);
+    }
+    const int found = min(eq_base, a.top);
+    __syncthreads();
+    if (!in) return;
+    for (int k = l; k < a.top; k += G) {
+        int rank = k, index = -1;
+        unsigned mine = 0;
+        if (k < found) {
+            mine = s_key[k]; index = s_index[k];
+            rank = 0;
+            for (int i = 0; i < found; ++i) {
+                const unsigned o = s_key[i];
+                rank += o > mine || (o == mine && s_index[i] < index);
+            }
+        }
+        a.index_out[n * a.top + rank] = index;
+        a.value_out[n * a.top + rank] = value_of(mine);
+    }
+}
+
+// Long rows.  Every thread's largest key is found in one pass; the K-th largest of those bounds the row's K-th largest
+// from below, and few elements reach it: a second pass collects them, and each is written at its rank.  Where more than
+// CAND reach it (many equal values), the K-th largest key of the row itself is found by digits, and equal ones are taken
+// in index order.
+constexpr int CAND = 2048;
+template <int NT>
+__device__ __forceinline__ unsigned kth_largest_of_threads(unsigned mine, int k, int* s_cnt) {
+    unsigned t = 0;                         // the largest t with at least k of the threads' keys >= t
+    for (int bit = 31; bit >= 0; --bit) {
+        const unsigned u = t | (1u << bit);
+        const int c = __popcll(__ballot(mine >= u));
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) s_cnt[threadIdx.x >> 6] = c;
+        __syncthreads();
+        int cnt = 0;
+#pragma unroll
+        for (int i = 0; i < NT / 64; ++i) cnt += s_cnt[i];
+        if (cnt >= k) t = u;
+    }
+    return t;
+}
+template <typename E, int NT, typename F>
+__device__ __forceinline__ void for_each_key(const Stretch<E>& st, F&& f) {
+    constexpr int VEC = Stretch<E>::VEC, UNROLL = 4;
+    const int t = threadIdx.x, one = st.single(t);
+    if (one >= 0) f(key_of(to_float(st.p[one])), one);
+    for (int v = t; v < st.vecs; v += UNROLL * NT) {
+        uint4 g[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) if (v + u * NT < st.vecs) g[u] = st.granule(v + u * NT);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            if (v + u * NT >= st.vecs) break;
+            float x[VEC];
+            unpack<E>(g[u], x);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) f(key_of(x[i]), st.place(v + u * NT) + i);
+        }
+    }
+}
+// Writes n candidates (at most CAND, distinct) at their ranks; places without one get -1.
+template <int NT>
+__device__ __forceinline__ void write_ranked(const unsigned* s_key, const int* s_index, int n, int top, int base, int* index_out, float* value_out) {
+    for (int k = threadIdx.x; k < n; k += NT) {
+        const unsigned mine = s_key[k];
+        const int index = s_index[k];
+        int rank = 0;
+        for (int i = 0; i < n; ++i) {
+            const unsigned o = s_key[i];
+            rank += o > mine || (o == mine && s_index[i] < index);
+        }
+        if (rank < top) { index_out[rank] = base + index; value_out[rank] = value_of(mine); }
+    }
+    for (int k = threadIdx.x; k < top; k += NT)
+        if (k >= n) { index_out[k] = -1; value_out[k] = NEG_INF; }
+}
+template <typename E, int NT>
+__global__ __launch_bounds__(NT) void top_row_kernel(TopArgs a) {
+    __shared__ unsigned s_key[CAND];
+    __shared__ int s_index[CAND], s_cnt[NT / 64], s_n;
+    const int64_t n = blockIdx.y;
+    const int j0 = blockIdx.x * a.piece, len = min(a.piece, a.vocab - j0);
+    const Stretch<E> st((const E*)a.z + n * a.stride + j0, len);
+    const int64_t o = (n * gridDim.x + blockIdx.x) * a.top;
+    unsigned big = 0;
+    for_each_key<E, NT>(st, [&](unsigned k, int) { big = max(big, k); });
+    if (threadIdx.x == 0) s_n = 0;
+    unsigned t = kth_largest_of_threads<NT>(big, a.top, s_cnt);
+    if (t == 0) t = 1;                      // fewer than K threads hold one that may be selected
+    for_each_key<E, NT>(st, [&](unsigned k, int j) {
+        if (k >= t) {
+            const int at = atomicAdd(&s_n, 1);
+            if (at < CAND) { s_key[at] = k; s_index[at] = j; }
+        }
+    });
+    __syncthreads();
+    int found = s_n;
+    if (found > CAND) {
+        // the K-th largest key of the stretch, bit by bit from the bound on; then the keys above it in any order and
+        // the equal ones by index
+        unsigned lo = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+            const unsigned u = lo | (1u << bit);
+            int c = 0;
+            for_each_key<E, NT>(st, [&](unsigned k, int) { c += k >= u; });
+            if (block_sum<NT>(c, s_cnt) >= a.top) lo = u;
+        }
+        if (lo == 0) lo = 1;
+        __syncthreads();
+        if (threadIdx.x == 0) s_n = 0;
+        __syncthreads();
+        for_each_key<E, NT>(st, [&](unsigned k, int j) {
+            if (k > lo) { const int at = atomicAdd(&s_n, 1); s_key[at] = k; s_index[at] = j; }     // fewer than K
+        });
+        __syncthreads();
+        found = s_n;
+        for (int b = 0; b < len && found < a.top; b += NT) {        // in index order, NT elements at a time
+            const int j = b + threadIdx.x;
+            const bool eq = j < len && key_of(to_float(st.p[j])) == lo;
+            const unsigned long long mask = __ballot(eq);
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) s_cnt[threadIdx.x >> 6] = __popcll(mask);
+            __syncthreads();
+            int at = found + __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1));
+            int all = 0;
+            for (int i = 0; i < NT / 64; ++i) { if (i < (int)(threadIdx.x >> 6)) at += s_cnt[i]; all += s_cnt[i]; }
+            if (eq && at < a.top) { s_key[at] = lo; s_index[at] = j; }
+            found = min(a.top, found + all);
+        }
+        __syncthreads();
+    }
+    write_ranked<NT>(s_key, s_index, found, a.top, j0, a.pieces > 1 ? a.part_index + o : a.index_out + o,
+                     a.pieces > 1 ? a.part_value + o : a.value_out + o);
+}
+// Joins the lists of a row's pieces (each in descending order): an element's rank is the sum over the lists of the
+// elements before it.  Pieces come in index order, so an equal value of an earlier piece goes first.
+template <int NT>
+__global__ __launch_bounds__(NT) void top_merge_kernel(TopArgs a) {
+    extern __shared__ unsigned lds_m[];
+    const int64_t n = blockIdx.x;
+    const int all = a.pieces * a.top;
+    for (int i = threadIdx.x; i < all; i += NT) {
+        const int64_t at = n * all + i;
+        lds_m[i] = a.part_index[at] < 0 ? 0u : key_of(a.part_value[at]);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < all; i += NT) {
+        const unsigned mine = lds_m[i];
+        const int list = i / a.top;
+        int rank = 0;
+        if (mine == 0) continue;
+        for (int q = 0; q < a.pieces && rank < a.top; ++q) {
+            if (q == list) { rank += i - list * a.top; continue; }
+            int lo = 0, hi = a.top;         // elements of list q before mine: greater ones, and equal ones if q < list
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                const unsigned o = lds_m[q * a.top + mid];
+                if (o > mine || (o == mine && q < list)) lo = mid + 1; else hi = mid;
+            }
+            rank += lo;
+        }
+        if (rank < a.top) {
+            a.index_out[n * a.top + rank] = a.part_index[n * all + i];
+            a.value_out[n * a.top + rank] = value_of(mine);
+        }
+    }
+    int have = 0;
+    for (int i = threadIdx.x; i < all; i += NT) have += lds_m[i] != 0;
+    __shared__ int s_cnt[NT / 64];
+    have = block_sum<NT>(have, s_cnt);
+    for (int k = threadIdx.x; k < a.top; k += NT)
+        if (k >= have) { a.index_out[n * a.top + k] = -1; a.value_out[n * a.top + k] = NEG_INF; }
+}
+
+// ---- launches -------------------------------------------------------------------------------
+constexpr int NT_LONG = 512;
+constexpr int64_t MAX_GRID = 0x7fffffff;
+
+// Pieces of a long row: one, unless there are too few rows to fill the card's 256 CUs twice; never under 4096 elements.
+int pieces_of(int64_t rows, int vocab, int most) {
+    if (rows >= 512 || vocab <= SMALL_VOCAB) return 1;
+    int64_t p = (1024 + rows - 1) / (rows > 0 ? rows : 1);
+    const int64_t by_len = (vocab + 4095) / 4096;
+    if (p > by_len) p = by_len;
+    if (p > most) p = most;
+    return (int)(p < 1 ? 1 : p);
+}
+int piece_len(int vocab, int pieces) {      // a multiple of 64 elements: pieces keep the row's alignment
+    const int len = (vocab + pieces - 1) / pieces;
+    return pieces == 1 ? vocab : (len + 63) / 64 * 64;
+}
+bool dtype_ok(int32_t d) { return d == PQL_F32 || d == PQL_BF16; }
+int elem(int32_t d) { return d == PQL_F32 ? 4 : 2; }
+bool logits_ok(const pql_logits& z) {
+    return z.rows >= 0 && z.rows <= MAX_GRID && z.vocab >= 1 && z.vocab <= (1 << 30) && z.stride >= z.vocab && dtype_ok(z.dtype);
+}
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+#define SMALL_CASES(X) X(8, 4) X(8, 8) X(16, 8) X(32, 8) X(64, 8) X(64, 16)
+template <typename E, bool BACK> hipError_t distill_small_launch(const DistillArgs& a, int kid, double bytes, hipStream_t st) {
+#define PQL_SMALL(G, R)                                                                                              \
+    if (a.vocab <= G * R) {                                                                                          \
+        constexpr int ROWS = 256 / G;                                                                                \
+        const size_t lds = (size_t)ROWS * (2 * a.top + a.vocab) * 4;                                                 \
+        const ProfSlot ps = prof_slot();                                                                             \
+        PQL_LAUNCH(ps, (distill_small_kernel<E, G, R, BACK>), dim3((unsigned)((a.rows + ROWS - 1) / ROWS)), dim3(256), lds, st, a); \
+        prof_commit(ps, kid, 0.0, bytes);                                                                            \
+        return hipGetLastError();                                                                                    \
+    }
+    SMALL_CASES(PQL_SMALL)
+#undef PQL_SMALL
+    return hipErrorInvalidValue;
+}
+template <typename E> hipError_t top_small_launch(const TopArgs& a, double bytes, hipStream_t st) {
+#define PQL_SMALL(G, R)                                                                                              \
+    if (a.vocab <= G * R) {                                                                                          \
+        constexpr int ROWS = 256 / G;                                                                                \
+        const ProfSlot ps = prof_slot();                                                                             \
+        PQL_LAUNCH(ps, (top_small_kernel<E, G, R>), dim3((unsigned)((a.rows + ROWS - 1) / ROWS)), dim3(256),         \
+                   (size_t)ROWS * 2 * a.top * 4, st, a);                                                             \
+        prof_commit(ps, KID_TOP_LOGITS, 0.0, bytes);                                                                 \
+        return hipGetLastError();                                                                                    \
+    }
+    SMALL_CASES(PQL_SMALL)
+#undef PQL_SMALL
+    return hipErrorInvalidValue;
+}
+
+// grid.y holds at most 65535 rows: longer calls go in parts
+constexpr int64_t ROWS_PER_LAUNCH = 65535;
+template <typename E> DistillArgs from_row(DistillArgs a, int64_t n, int64_t rows) {
+    a.z = (const E*)a.z + n * a.stride;
+    if (a.grad) a.grad = (E*)a.grad + n * a.grad_stride;
+    a.index += n * a.top; a.value += n * a.top;
+    if (a.weight) a.weight += n;
+    if (a.lse) a.lse += n;
+    if (a.loss_out) a.loss_out += n;
+    if (a.lse_out) a.lse_out += n;
+    a.rows = rows;
+    return a;
+}
+template <typename E> hipError_t distill_launch(const DistillArgs& a, bool back, hipStream_t st) {
+    const double read = (double)a.rows * a.vocab * sizeof(E), lists = (double)a.rows * a.top * 8;
+    const double bytes = read * (a.grad ? 2 : 1) + lists + 12.0 * a.rows;
+    if (a.vocab <= SMALL_VOCAB)
+        return back ? distill_small_launch<E, true>(a, KID_DISTILL_GRAD, bytes, st) : distill_small_launch<E, false>(a, KID_DISTILL, bytes, st);
+    if (back) {
+        for (int64_t n = 0; n < a.rows; n += ROWS_PER_LAUNCH) {
+            const DistillArgs b = from_row<E>(a, n, a.rows - n < ROWS_PER_LAUNCH ? a.rows - n : ROWS_PER_LAUNCH);
+            const ProfSlot ps = prof_slot();
+            PQL_LAUNCH(ps, (distill_piece_kernel<E, NT_LONG, false>), dim3(a.pieces, (unsigned)b.rows), dim3(NT_LONG), 0, st, b);
+            prof_commit(ps, KID_DISTILL_GRAD, 0.0, bytes * b.rows / a.rows);
+        }
+    } else if (a.pieces > 1) {
+        ProfSlot ps = prof_slot();
+        PQL_LAUNCH(ps, (distill_part_kernel<E, NT_LONG>), dim3(a.pieces, (unsigned)a.rows), dim3(NT_LONG), 0, st, a);
+        prof_commit(ps, KID_DISTILL, 0.0, read);
+        ps = prof_slot();
+        PQL_LAUNCH(ps, (distill_piece_kernel<E, NT_LONG, true>), dim3(a.grad ? a.pieces : 1, (unsigned)a.rows), dim3(NT_LONG), 0, st, a);
+        prof_commit(ps, KID_DISTILL_JOIN, 0.0, a.grad ? bytes : lists);
+    } else {
+        const ProfSlot ps = prof_slot();
+        PQL_LAUNCH(ps, (distill_row_kernel<E, NT_LONG>), dim3((unsigned)a.rows), dim3(NT_LONG), 0, st, a);
+        prof_commit(ps, KID_DISTILL, 0.0, bytes);
+    }
+    return hipGetLastError();
+}
+template <typename E> hipError_t top_launch(const TopArgs& a, hipStream_t st) {
+    const double bytes = (double)a.rows * a.vocab * sizeof(E) + (double)a.rows * a.top * 8;
+    if (a.vocab <= SMALL_VOCAB) return top_small_launch<E>(a, bytes, st);
+    for (int64_t n = 0; n < a.rows; n += ROWS_PER_LAUNCH) {
+        TopArgs b = a;
+        b.rows = a.rows - n < ROWS_PER_LAUNCH ? a.rows - n : ROWS_PER_LAUNCH;
+        b.z = (const E*)a.z + n * a.stride;
+        b.index_out += n * a.top; b.value_out += n * a.top;
+        const ProfSlot ps = prof_slot();
+        PQL_LAUNCH(ps, (top_row_kernel<E, NT_LONG>), dim3(a.pieces, (unsigned)b.rows), dim3(NT_LONG), 0, st, b);
+        prof_commit(ps, KID_TOP_LOGITS, 0.0, bytes * b.rows / a.rows);
+    }
+    if (a.pieces > 1) {
+        const ProfSlot ps = prof_slot();
+        PQL_LAUNCH(ps, top_merge_kernel<256>, dim3((unsigned)a.rows), dim3(256), (size_t)a.pieces * a.top * 4, st, a);
+        prof_commit(ps, KID_TOP_MERGE, 0.0, (double)a.rows * a.top * 8 * (a.pieces + 1));
+    }
+    return hipGetLastError();
+}
+int top_pieces(const pql_logits& z, int top) {      // the lists of a row's pieces are merged in 32 KB of LDS
+    return pieces_of(z.rows, z.vocab, 8192 / top);
+}
+bool misaligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) != 0; }
+int32_t check_logits(pql_ctx* c, const pql_logits& z, const char* text) {
+    if (!logits_ok(z)) return ctx_fail(c, PQL_ERR_INVALID_ARG, text);
+    return PQL_OK;
+}
+}  // namespace
+}  // namespace pql
+
+using namespace pql;
+
+extern "C" {
+
+int64_t pql_top_logits_workspace_bytes(const pql_logits* z, int32_t top) {
+    if (!z) return PQL_ERR_NULL;
+    if (!logits_ok(*z) || top < 1 || top > PQL_MAX_TOP || top > z->vocab) return PQL_ERR_INVALID_ARG;
+    const int p = top_pieces(*z, top);
+    return p > 1 ? (int64_t)up256((size_t)z->rows * p * top * 8) : 0;
+}
+
+int32_t pql_top_logits(pql_ctx* c, pql_logits z, int32_t top, int32_t* index_out, float* value_out, void* workspace, void* stream) {
+    if (!c) return PQL_ERR_NULL;
+    if (check_logits(c, z, "pql_top_logits: bad rows, vocab, stride or dtype") != PQL_OK) return PQL_ERR_INVALID_ARG;
+    if (top < 1 || top > PQL_MAX_TOP || top > z.vocab) return ctx_fail(c, PQL_ERR_INVALID_ARG, "pql_top_logits: bad top");
+    if (z.rows == 0) return PQL_OK;
+    if (!z.data || !index_out || !value_out) return ctx_fail(c, PQL_ERR_NULL, "pql_top_logits: null pointer");
+    TopArgs a{};
+    a.pieces = top_pieces(z, top);
+    if (a.pieces > 1 && !workspace) return ctx_fail(c, PQL_ERR_NULL, "pql_top_logits: null workspace");
+    if (misaligned(z.data, elem(z.dtype)) || misaligned(index_out, 4) || misaligned(value_out, 4) || misaligned(workspace, 256))
+        return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_top_logits: misaligned pointer");
+    a.z = z.data; a.rows = z.rows; a.stride = z.stride; a.vocab = z.vocab; a.top = top;
+    a.piece = piece_len(z.vocab, a.pieces);
+    a.pieces = (z.vocab + a.piece - 1) / a.piece;
+    a.index_out = index_out; a.value_out = value_out;
+    a.part_index = (int*)workspace;
+    a.part_value = (float*)workspace + (size_t)z.rows * a.pieces * top;
+    const hipError_t e = z.dtype == PQL_F32 ? top_launch<float>(a, (hipStream_t)stream) : top_launch<bf16_t>(a, (hipStream_t)stream);
+    return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_top_logits", e);
+}
+
+int64_t pql_distill_workspace_bytes(const pql_logits* z) {
+    if (!z) return PQL_ERR_NULL;
+    if (!logits_ok(*z)) return PQL_ERR_INVALID_ARG;
+    const int p = pieces_of(z->rows, z->vocab, 256);
+    return p > 1 ? (int64_t)up256((size_t)z->rows * (2 * p + PQL_MAX_TOP) * 4) : 0;
+}
+
+static int32_t distill_check(pql_ctx* c, const pql_logits& z, const pql_teacher& t, float temperature, const pql_logits& grad, bool need_grad) {
+    if (check_logits(c, z, "pql_distill: bad rows, vocab, stride or dtype of the logits") != PQL_OK) return PQL_ERR_INVALID_ARG;
+    if (t.top < 1 || t.top > PQL_MAX_TOP || t.top > z.vocab) return ctx_fail(c, PQL_ERR_INVALID_ARG, "pql_distill: bad top");
+    if (!(temperature > 0.f) || temperature > 3.0e38f || 1.f / temperature > 3.0e38f) return ctx_fail(c, PQL_ERR_INVALID_ARG, "pql_distill: bad temperature");
+    if (grad.data || need_grad) {
+        if (check_logits(c, grad, "pql_distill: bad rows, vocab, stride or dtype of the gradient") != PQL_OK) return PQL_ERR_INVALID_ARG;
+        if (grad.rows != z.rows || grad.vocab != z.vocab || grad.dtype != z.dtype)
+            return ctx_fail(c, PQL_ERR_INVALID_ARG, "pql_distill: gradient of another shape or type than the logits");
+        if (grad.data == z.data && grad.stride != z.stride && z.rows > 1)
+            return ctx_fail(c, PQL_ERR_INVALID_ARG, "pql_distill: a gradient in the logits' place needs their stride");
+    }
+    if (z.rows == 0) return PQL_OK;
+    if (!z.data || !t.index || !t.value || (need_grad && !grad.data)) return ctx_fail(c, PQL_ERR_NULL, "pql_distill: null pointer");
+    if (misaligned(z.data, elem(z.dtype)) || misaligned(grad.data, elem(z.dtype)) || misaligned(t.index, 4) || misaligned(t.value, 4))
+        return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_distill: misaligned pointer");
+    return PQL_OK;
+}
+static DistillArgs distill_args(const pql_logits& z, const pql_teacher& t, float temperature, const float* weight, const pql_logits& grad, int pieces) {
+    DistillArgs a{};
+    a.z = z.data; a.rows = z.rows; a.stride = z.stride; a.vocab = z.vocab;
+    a.index = t.index; a.value = t.value; a.top = t.top;
+    a.temp = temperature; a.inv_temp = 1.f / temperature;
+    a.weight = weight;
+    a.grad = grad.data; a.grad_stride = grad.stride;
+    a.piece = piece_len(z.vocab, pieces);
+    a.pieces = (z.vocab + a.piece - 1) / a.piece;
+    return a;
+}
+
+int32_t pql_distill_loss(pql_ctx* c, pql_logits z, pql_teacher t, float temperature, const float* row_weight,
+                         float* loss_out, float* lse_out, pql_logits grad, void* workspace, void* stream) {
+    if (!c) return PQL_ERR_NULL;
+    const int32_t rc = distill_check(c, z, t, temperature, grad, false);
+    if (rc != PQL_OK || z.rows == 0) return rc;
+    if (!loss_out || !lse_out) return ctx_fail(c, PQL_ERR_NULL, "pql_distill_loss: null pointer");
+    const int pieces = pieces_of(z.rows, z.vocab, 256);
+    if (pieces > 1 && !workspace) return ctx_fail(c, PQL_ERR_NULL, "pql_distill_loss: null workspace");
+    if (misaligned(workspace, 256) || misaligned(loss_out, 4) || misaligned(lse_out, 4) || misaligned(row_weight, 4))
+        return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_distill_loss: misaligned pointer");
+    DistillArgs a = distill_args(z, t, temperature, row_weight, grad, pieces);
+    a.loss_out = loss_out; a.lse_out = lse_out;
+    a.part = (float*)workspace;
+    a.part_z = (float*)workspace + (size_t)z.rows * 2 * a.pieces;
+    const hipError_t e = z.dtype == PQL_F32 ? distill_launch<float>(a, false, (hipStream_t)stream)
+                                            : distill_launch<bf16_t>(a, false, (hipStream_t)stream);
+    return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_distill_loss", e);
+}
+
+int32_t pql_distill_backward(pql_ctx* c, pql_logits z, pql_teacher t, float temperature, const float* lse,
+                             const float* loss_grad, pql_logits grad, void* stream) {
+    if (!c) return PQL_ERR_NULL;
+    const int32_t rc = distill_check(c, z, t, temperature, grad, true);
+    if (rc != PQL_OK || z.rows == 0) return rc;
+    if (!lse || !loss_grad) return ctx_fail(c, PQL_ERR_NULL, "pql_distill_backward: null pointer");
+    if (misaligned(lse, 4) || misaligned(loss_grad, 4)) return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_distill_backward: misaligned pointer");
+    // every piece works out the list's masses anew: 16384 elements keep that below a tenth of it
+    DistillArgs a = distill_args(z, t, temperature, loss_grad, grad, z.vocab <= SMALL_VOCAB ? 1 : (z.vocab + 16383) / 16384);
+    a.lse = lse;
+    const hipError_t e = z.dtype == PQL_F32 ? distill_launch<float>(a, true, (hipStream_t)stream)
+                                            : distill_launch<bf16_t>(a, true, (hipStream_t)stream);
+    return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_distill_backward", e);
+}
+
+}  // extern "C"

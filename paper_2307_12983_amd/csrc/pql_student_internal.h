@@ -1,0 +1,55 @@
+// Internal declarations of the student's operators (include/pql_student.h): element types and argument blocks.
+#pragma once
+
+#include "pql_internal.h"
+#include "pql_student.h"
+
+namespace pql {
+
+using bf16_t = __bf16;
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(bf16_t x) { return (float)x; }
+template <typename E> __device__ __forceinline__ E from_float(float x) { return (E)x; }      // bf16: to nearest even
+
+struct DistillArgs {
+    const void* z;
+    int64_t rows, stride, grad_stride;
+    int vocab, top, pieces, piece;      // pieces of `piece` logits a row
+    float temp, inv_temp;
+    const int* index; const float* value;
+    const float* weight;                // per row, NULL: ones
+    const float* lse;                   // backward only
+    float *loss_out, *lse_out;
+    void* grad;
+    float* part;                        // [rows][pieces][2]: maximum (-inf: nothing finite) and sum of each piece
+    float* part_z;                      // [rows][top]: logits of the listed answers
+};
+
+struct TopArgs {
+    const void* z;
+    int64_t rows, stride;
+    int vocab, top, pieces, piece;
+    int* index_out; float* value_out;
+    int* part_index; float* part_value; // [rows][pieces][top]
+};
+
+struct DeltaSeq { void* p; int64_t b, t, h; };
+struct DeltaArgs {
+    int batch, steps, heads_k, heads_v, group, dim_k, dim_v;
+    int chunks, dvp;                    // chunks of a full sequence; dim_v padded for the arrays below
+    int bh0;                            // first (sequence, head) of this launch
+    float scale;
+    DeltaSeq q, k, v, g, beta, out;
+    const int* lengths;
+    const float* state;
+    float* state_out;
+    // per (sequence, head, chunk), fp32: T, P [64][64], R [64][dvp], S [dim_k padded][dvp] (before the chunk); R, S may be NULL
+    float *T, *P, *R, *S;
+    // gradient: dX, dY [64][dvp], dS [dim_k padded][dvp] (after the chunk); dq, dk per value head where those are shared
+    DeltaSeq out_grad, dq, dk, dv, dg, dbeta;
+    const float* state_grad;
+    float* dstate;
+    float *dX, *dY, *dS, *part_q, *part_k;
+};
+
+}  // namespace pql
