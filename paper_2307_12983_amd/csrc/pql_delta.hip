@@ -29,7 +29,6 @@ namespace pql {
 namespace {
 
 constexpr int C = 64;                       // tokens per chunk
-constexpr int NB = 32;                      // state columns per workgroup of the scans
 constexpr float NEG_INF = -__builtin_inff();
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -402,41 +401,207 @@ __device__ __forceinline__ void invert(float (*m)[LDM], float (*t)[LDM], float (
     __syncthreads();
 }
 
+// ---- what the prepare kernel leaves for the others, all in operand order --------------------------------------------
+// T and P (rows of A operands) and, for the gradient, their transposes: the six 16 x 32 blocks that are not all zero,
+// [block][term][lane][8], computed values split already.  Rows 16 w .. of T and P need the contraction blocks 0 .. w / 2, those of the transposes
+// w / 2 .. 1.
+constexpr int BLOCKS = 6;
+template <typename M> constexpr int BLOCK = 64 * 8 * M::PLANES;          // elements of a block
+template <typename M> constexpr int TRI = BLOCKS * BLOCK<M>;
+__device__ __forceinline__ constexpr int tri_block(int w, int ks) { return w < 2 ? w : 2 * w - 2 + ks; }            // 0 1 2 3 4 5
+__device__ __forceinline__ constexpr int tri_block_t(int w, int ks) { return w < 2 ? 2 * w + ks : 2 + w; }
+// K^T, Q^T: [dim_k / 16][2][lane][8] of the tokens' type, one per key head.
+template <typename E> __device__ __forceinline__ int64_t kt_at(const DeltaArgs& a, const Where& w, int ch, int dkp) {
+    return (((int64_t)w.b * a.heads_k + w.hk) * a.chunks + ch) * dkp * C;
+}
+// Gates: gam[64], end[64], beta[64], e^{G_last}.
+constexpr int GATES = 4 * C;
+template <typename M> __device__ __forceinline__ typename M::X load_operand(const typename M::E* p) {
+    if constexpr (sizeof(typename M::E) == 4) {
+        FF f;
+        const floatx4 a = *(const floatx4*)p, b = *(const floatx4*)(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f.v[i] = a[i]; f.v[4 + i] = b[i]; }
+        return f;
+    } else {
+        return F1{*(const bf16x8*)p};
+    }
+}
+template <typename M> __device__ __forceinline__ typename M::Y load_split(const char* p, unsigned lane_bytes) {
+    if constexpr (M::PLANES == 3)
+        return F3{*(const bf16x8*)(p + lane_bytes), *(const bf16x8*)(p + 1024 + lane_bytes), *(const bf16x8*)(p + 2048 + lane_bytes)};
+    else
+        return load_operand<M>((const float*)(p + 2 * lane_bytes));
+}
+// An operand straight from a token row.
+template <typename M, bool AL> __device__ __forceinline__ typename M::X row_operand(const typename M::E* row, int d, int dim, bool ok) {
+    float x[8];
+    load8<typename M::E, AL>(row, d, dim, ok, x);
+    return M::exact(x);
+}
+
+// Token tensors of a loop over chunks.  AL (aligned rows, strides that keep a chunk's offsets below 2^30 bytes): through
+// buffer descriptors, one per chunk; rows and elements that do not exist get an offset outside them, loads of which return
+// zeros and stores of which are dropped.  No branch then stands between a chunk's loads and stores, and the compiler can
+// tell which of them a use has to wait for.
+constexpr int NOWHERE = 0x7ffffffc;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tokens(const char* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, 0x40000000, 0x00020000);
+}
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+// The operands of one wavefront's 16 token rows.
+template <typename M, int DK, bool AL> struct RowOperands {
+    using E = typename M::E;
+    static constexpr int ND = DK / 32, ES = sizeof(E);
+    const char* base;                       // token 0
+    int64_t stride;                         // bytes
+    int len, dk, row, q;
+    typename M::X f[ND];
+    __device__ __forceinline__ RowOperands(const DeltaSeq& s, const Where& w, int h, int dk_, int row_, int q_)
+        : base((const char*)at<E>(s, w.b, 0, h)), stride(s.t * (int64_t)ES), len(w.len), dk(dk_), row(row_), q(q_) {}
+    __device__ __forceinline__ void load(int ch) {
+        const char* p = base + (int64_t)ch * C * stride;
+        const bool ok = ch * C + row < len;
+        if constexpr (AL) {
+            const auto r = tokens(p);
+            const int off = row * (int)stride + 8 * q * ES;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                const int o = ok && 32 * d + 8 * q < dk ? off : NOWHERE - 32 * d * ES;
+                const uintx4 x = __builtin_amdgcn_raw_buffer_load_b128(r, o + 32 * d * ES, 0, 0);
+                if constexpr (ES == 2) {
+                    f[d].h = __builtin_bit_cast(bf16x8, x);
+                } else {
+                    const floatx4 lo = __builtin_bit_cast(floatx4, x);
+                    const floatx4 hi = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(r, o + 32 * d * ES + (ok && 32 * d + 8 * q < dk ? 16 : 0), 0, 0));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { f[d].v[i] = lo[i]; f[d].v[4 + i] = hi[i]; }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int d = 0; d < ND; ++d) f[d] = row_operand<M, false>((const E*)(p + row * stride), 32 * d + 8 * q, dk, ok);
+        }
+    }
+};
+// The same for results laid out as [4 tokens][column]: element (i0 + r, col + 16 n).
+template <typename M, int NT, bool AL> struct ColumnValues {
+    using E = typename M::E;
+    static constexpr int ES = sizeof(E);
+    const char* base;
+    int64_t stride;
+    int len, dim, i0, col;
+    unsigned raw[NT][4];
+    __device__ __forceinline__ ColumnValues(const DeltaSeq& s, const Where& w, int dim_, int i0_, int col_)
+        : base((const char*)at<E>(s, w.b, 0, w.h)), stride(s.t * (int64_t)ES), len(w.len), dim(dim_), i0(i0_), col(col_) {}
+    __device__ __forceinline__ void load(int ch) {
+        const char* p = base + (int64_t)ch * C * stride;
+        const auto rs = tokens(p);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const bool ok = ch * C + i0 + r < len && col + 16 * n < dim;
+                if constexpr (AL) {
+                    const int o = ok ? (i0 + r) * (int)stride + (col + 16 * n) * ES : NOWHERE;
+                    if constexpr (ES == 2) raw[n][r] = (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, o, 0, 0);
+                    else raw[n][r] = __builtin_amdgcn_raw_buffer_load_b32(rs, o, 0, 0);
+                } else {
+                    raw[n][r] = ok ? bits(*(const E*)(p + (i0 + r) * stride + (int64_t)(col + 16 * n) * ES)) : 0u;
+                }
+            }
+    }
+    static __device__ __forceinline__ unsigned bits(E x) {
+        if constexpr (ES == 2) return __builtin_bit_cast(unsigned short, x);
+        else return __builtin_bit_cast(unsigned, x);
+    }
+    __device__ __forceinline__ floatx4 get(int n) const {
+        floatx4 x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = __uint_as_float(ES == 2 ? raw[n][r] << 16 : raw[n][r]);
+        return x;
+    }
+    // writes them; rows behind the length are zeros, rows behind `steps` are not there
+    static __device__ __forceinline__ void put(const DeltaSeq& s, const Where& w, int steps, int dim, int ch, int i0, int col, const floatx4 (&x)[NT]) {
+        char* p = (char*)at_out<E>(s, w.b, (int64_t)ch * C, w.h);
+        const int64_t stride = s.t * (int64_t)ES;
+        const auto rs = tokens(p);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bool ok = ch * C + i0 + r < steps && col + 16 * n < dim;
+                const unsigned v = bits(from_float<E>(ch * C + i0 + r < w.len ? x[n][r] : 0.f));
+                if constexpr (AL) {
+                    const int o = ok ? (i0 + r) * (int)stride + (col + 16 * n) * ES : NOWHERE;
+                    if constexpr (ES == 2) __builtin_amdgcn_raw_buffer_store_b16((unsigned short)v, rs, o, 0, 0);
+                    else __builtin_amdgcn_raw_buffer_store_b32(v, rs, o, 0, 0);
+                } else if (ok) {
+                    char* o = p + (i0 + r) * stride + (int64_t)(col + 16 * n) * ES;
+                    if constexpr (ES == 2) *(unsigned short*)o = (unsigned short)v;
+                    else *(unsigned*)o = v;
+                }
+            }
+    }
+};
+// A 16 x 16 NT tile of results to a padded fp32 array of the library's own, rows r0 + 4 q .. of `ld` floats.
+template <int NT> __device__ __forceinline__ void put_padded(float* base, int r0, int ld, int q, int c0, int c, const floatx4 (&x)[NT]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        char* p = (char*)(base + (int64_t)(r0 + r) * ld + c0);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) *(float*)(p + (unsigned)(4 * (4 * q * ld + c + 16 * n))) = x[n][r];
+    }
+}
+
 template <typename M, int DK, bool AL>
 __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
     using E = typename M::E;
+    using KT = Tile<M, DK, C, true>;
+    extern __shared__ __align__(16) unsigned char lds[];
     __shared__ Gates s_g;
-    __shared__ float s_m[C][LDM], s_t[C][LDM], s_x[4][16][17];
+    __shared__ float s_x[4][16][17];
+    float (*const s_m)[LDM] = (float (*)[LDM])lds;
+    float (*const s_t)[LDM] = s_m + C;
+    float (*const s_p)[LDM] = s_t + C;
     const Where w = where_of(a, blockIdx.y);
     const int ch = blockIdx.x, left = w.len - ch * C;
     if (left <= 0) return;
     const int len = min(left, C);
-    const int64_t t0 = (int64_t)ch * C;
-    gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
+    const int64_t t0 = (int64_t)ch * C, at_chunk = (int64_t)w.bh * a.chunks + ch;
     const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, q = l >> 4;
     const E* kp = at<E>(a.k, w.b, t0, w.hk);
     const E* qp = at<E>(a.q, w.b, t0, w.hk);
+    gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
+    if (w.h % a.group == 0) {               // this key head's transposes
+        const KT tile(lds);
+        for (int which = 0; which < (a.QT ? 2 : 1); ++which) {
+            stage_transposed<M, DK, AL>(tile, which ? qp : kp, which ? a.q.t : a.k.t, len, a.dim_k);
+            __syncthreads();
+            E* o = (E*)(which ? a.QT : a.KT) + kt_at<E>(a, w, ch, DK);
+            for (int i = threadIdx.x; i < DK / 16 * 2 * 64; i += 256) {
+                const E* from = tile.p + ((i >> 7) * 16 + (i & 15)) * KT::LD + (i >> 6 & 1) * 32 + (i >> 4 & 3) * 8;
+                *(uint4*)(o + i * 8) = *(const uint4*)from;
+                if (sizeof(E) == 4) *(uint4*)(o + i * 8 + 4) = *(const uint4*)(from + 4);
+            }
+            __syncthreads();
+        }
+    }
     floatx4 kk[4] = {}, qk[4] = {};
 #pragma unroll
     for (int d = 0; d < DK; d += 32) {
-        float x[8];
         const int row = 16 * wave + c;
-        load8<E, AL>(kp + row * a.k.t, d + 8 * q, a.dim_k, row < len, x);
-        const auto fk = M::exact(x);
-        load8<E, AL>(qp + row * a.q.t, d + 8 * q, a.dim_k, row < len, x);
-        const auto fq = M::exact(x);
+        const auto fk = row_operand<M, AL>(kp + row * a.k.t, d + 8 * q, a.dim_k, row < len);
+        const auto fq = row_operand<M, AL>(qp + row * a.q.t, d + 8 * q, a.dim_k, row < len);
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             if (n > wave) break;
-            load8<E, AL>(kp + (16 * n + c) * a.k.t, d + 8 * q, a.dim_k, 16 * n + c < len, x);
-            const auto f = M::exact(x);
+            const auto f = row_operand<M, AL>(kp + (16 * n + c) * a.k.t, d + 8 * q, a.dim_k, 16 * n + c < len);
             mma(kk[n], fk, f);
             mma(qk[n], fq, f);
         }
     }
-    __syncthreads();
-    float* P = a.P + ((int64_t)w.bh * a.chunks + ch) * C * C;
-    float* T = a.T + ((int64_t)w.bh * a.chunks + ch) * C * C;
+    __syncthreads();                        // gates are there
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
         const int j = 16 * n + c;
@@ -444,156 +609,192 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
         for (int r = 0; r < 4; ++r) {
             const int i = 16 * wave + 4 * q + r;
             const float f = i >= j ? decay(s_g, i, j) : 0.f;
-            P[i * C + j] = f * qk[n][r];
+            s_p[i][j] = f * qk[n][r];
             s_m[i][j] = i > j ? f * kk[n][r] * s_g.beta[j] : 0.f;
         }
     }
     __syncthreads();
     invert(s_m, s_t, s_x);
-    for (int i = threadIdx.x; i < C * C; i += 256) T[i] = s_t[i / C][i % C];
+    auto put = [&](void* base, int i, const float* x) {      // eight values of block i / 64, lane i % 64
+        E* o = (E*)base + at_chunk * TRI<M> + (i >> 6) * BLOCK<M> + (i & 63) * 8;
+        const auto f = M::computed(x);
+        if constexpr (M::PLANES == 3) {
+            *(bf16x8*)o = f.h; *(bf16x8*)(o + 512) = f.m; *(bf16x8*)(o + 1024) = f.l;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = f.v[j];
+        }
+    };
+    for (int i = threadIdx.x; i < BLOCKS * 64; i += 256) {
+        const int blk = i >> 6, bw = blk < 2 ? blk : 2 + (blk - 2) / 2, ks = blk < 2 ? 0 : blk & 1;
+        const int row = 16 * bw + (i & 15), k = 32 * ks + (i >> 4 & 3) * 8;
+        put(a.T, i, &s_t[row][k]);
+        put(a.P, i, &s_p[row][k]);
+        if (a.TT) {
+            const int tw = blk < 4 ? blk / 2 : blk - 2, tk = blk < 4 ? blk & 1 : 1;
+            const int col = 16 * tw + (i & 15), r0 = 32 * tk + (i >> 4 & 3) * 8;
+            float t[8], p[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { t[j] = s_t[r0 + j][col]; p[j] = s_p[r0 + j][col]; }
+            put(a.TT, i, t);
+            put(a.PT, i, p);
+        }
+    }
+    float* g = a.G + at_chunk * GATES;
+    if (threadIdx.x < C) {
+        g[threadIdx.x] = s_g.gam[threadIdx.x];
+        g[C + threadIdx.x] = s_g.end[threadIdx.x];
+        g[2 * C + threadIdx.x] = s_g.beta[threadIdx.x];
+        if (threadIdx.x == 0) g[3 * C] = s_g.last;
+    }
 }
 
 // =============================================================================================
-// Chunks in order: outputs and states, NB columns per workgroup.
+// Chunks in order: outputs and states, 16 NT columns per workgroup.  Nothing but the state's own chain K S, T X, K^T Y
+// waits for a chunk: all operands of the next one are requested into registers as soon as this one's have been used.
 // =============================================================================================
-template <typename M, int DK> struct ScanLds {
-    using S = Tile<M, NB, DK, false>;       // S^T [column][dim_k]
-    using X = Tile<M, NB, C, false>;        // X^T, Y^T, (e o Y)^T [column][token]
-    using K = Tile<M, DK, C, true>;         // K^T [dim_k][token]
-    static constexpr int S0 = 0, X0 = S0 + S::BYTES, Y0 = X0 + X::BYTES, Z0 = Y0 + X::BYTES, K0 = Z0 + X::BYTES, BYTES = K0 + K::BYTES;
+template <typename M, int DK, int NT> struct ScanLds {
+    using S = Tile<M, 16 * NT, DK, false>;          // S^T [column][dim_k]
+    using X = Tile<M, 16 * NT, C, false>;           // X^T, Y^T, (e o Y)^T [column][token]
+    static constexpr int S0 = 0, X0 = S0 + S::BYTES, Y0 = X0 + X::BYTES, Z0 = Y0 + X::BYTES, BYTES = Z0 + X::BYTES;
 };
 template <typename E> __device__ __forceinline__ void zero_rows(const DeltaSeq& s, const Where& w, int from, int to, int c0, int n) {
     for (int i = threadIdx.x; i < (to - from) * n; i += 256) at_out<E>(s, w.b, from + i / n, w.h)[c0 + i % n] = from_float<E>(0.f);
 }
-template <typename M, int DK, bool AL>
+// The two blocks of a wavefront's rows of T, P or their transposes.  Blocks that are zero are not there: the other one is
+// loaded twice (a load in a branch would make later waits longer) and not used.
+template <typename M, bool TRANSPOSED> __device__ __forceinline__ void load_tri(const void* base, int64_t at_chunk, int wave, int l, typename M::Y (&x)[2]) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+    {
+        const int k = TRANSPOSED ? max(ks, wave / 2) : min(ks, wave / 2);
+        x[ks] = load_split<M>((const char*)base + (at_chunk * TRI<M> + (TRANSPOSED ? tri_block_t(wave, k) : tri_block(wave, k)) * BLOCK<M>) * (int)sizeof(typename M::E), 16 * l);
+    }
+}
+template <typename M, int DK, int NT, bool AL, bool KEEP>
 __global__ __launch_bounds__(256) void delta_scan_kernel(DeltaArgs a) {
     using E = typename M::E;
-    using L = ScanLds<M, DK>;
-    constexpr int RS = DK / 64, NT = NB / 16;       // 16-row strips of the state per wavefront, column tiles
+    using L = ScanLds<M, DK, NT>;
+    constexpr int RS = DK / 64, ND = DK / 32;       // 16-row strips of the state per wavefront, contraction steps
     extern __shared__ __align__(16) unsigned char lds[];
-    __shared__ Gates s_g;
     const typename L::S tS(lds + L::S0);
     const typename L::X tX(lds + L::X0), tY(lds + L::Y0), tZ(lds + L::Z0);
-    const typename L::K tK(lds + L::K0);
     const Where w = where_of(a, blockIdx.y);
-    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, q = l >> 4, c0 = blockIdx.x * NB;
-    const int dk = a.dim_k, dv = a.dim_v;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, q = l >> 4, c0 = blockIdx.x * 16 * NT;
+    const int dk = a.dim_k, dv = a.dim_v, row = 16 * wave + c, i0 = 16 * wave + 4 * q;
+    const int chunks = (w.len + C - 1) / C;
+    const int64_t first = (int64_t)w.bh * a.chunks;
+    RowOperands<M, DK, AL> K(a.k, w, w.hk, dk, row, q), Q(a.q, w, w.hk, dk, row, q);
+    ColumnValues<M, NT, AL> V(a.v, w, dv, i0, c0 + c);
+    typename M::X kt[RS][2];
+    typename M::Y tr[2], pr[2];
+    floatx4 gam, end, beta;
+    float last;
+    auto load_gates = [&](int ch) {
+        const char* g = (const char*)(a.G + (first + ch) * GATES);
+        const unsigned at = 4 * i0;
+        gam = *(const floatx4*)(g + at);
+        end = *(const floatx4*)(g + 4 * C + at);
+        beta = *(const floatx4*)(g + 8 * C + at);
+        last = *(const float*)(g + 12 * C);
+    };
+    auto load_kt = [&](int ch) {
+        const char* p = (const char*)((const E*)a.KT + kt_at<E>(a, w, ch, DK));
+#pragma unroll
+        for (int s = 0; s < RS; ++s)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                kt[s][k] = load_operand<M>((const E*)(p + (2 * (wave * RS + s) + k) * 512 * (int)sizeof(E) + (unsigned)(l * 8 * (int)sizeof(E))));
+    };
+    auto keep_state = [&](int ch, const floatx4 (&S)[RS][NT]) {
+#pragma unroll
+        for (int s = 0; s < RS; ++s) put_padded<NT>(a.S + (first + ch) * DK * a.dvp, 16 * (wave * RS + s), a.dvp, q, c0, c, S[s]);
+    };
+    if (chunks > 0) {
+        K.load(0); Q.load(0); V.load(0); load_gates(0);
+        load_tri<M, false>(a.T, first, wave, l, tr);
+        load_tri<M, false>(a.P, first, wave, l, pr);
+        load_kt(0);
+    }
     floatx4 S[RS][NT];
 #pragma unroll
     for (int s = 0; s < RS; ++s)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int col = c0 + 16 * n + c, row = 16 * (wave * RS + s) + 4 * q;
+            const int col = c0 + 16 * n + c, r0 = 16 * (wave * RS + s) + 4 * q;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                S[s][n][r] = a.state && row + r < dk && col < dv ? a.state[((int64_t)w.bh * dk + row + r) * dv + col] : 0.f;
-            tS.put4(16 * n + c, row, S[s][n]);
+                S[s][n][r] = a.state && r0 + r < dk && col < dv ? a.state[((int64_t)w.bh * dk + r0 + r) * dv + col] : 0.f;
+            tS.put4(16 * n + c, r0, S[s][n]);
         }
-    const int chunks = (w.len + C - 1) / C;
     for (int ch = 0; ch < chunks; ++ch) {
-        const int len = min(w.len - ch * C, C);
-        const int64_t t0 = (int64_t)ch * C, at_chunk = (int64_t)w.bh * a.chunks + ch;
-        const E* kp = at<E>(a.k, w.b, t0, w.hk);
-        const E* qp = at<E>(a.q, w.b, t0, w.hk);
-        gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
-        stage_transposed<M, DK, AL>(tK, kp, a.k.t, len, dk);
-        if (a.S) {
-            float* o = a.S + at_chunk * DK * a.dvp;
+        const int next = min(ch + 1, chunks - 1);
+        const int64_t at_chunk = first + ch;
+        __syncthreads();                            // the state is in LDS
+        floatx4 z[NT] = {}, o[NT] = {};
 #pragma unroll
-            for (int s = 0; s < RS; ++s)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o[(int64_t)(16 * (wave * RS + s) + 4 * q + r) * a.dvp + c0 + 16 * n + c] = S[s][n][r];
-        }
-        __syncthreads();                    // states, K^T and gates are there
-        floatx4 z[NT] = {}, o1[NT] = {};
-        const int row = 16 * wave + c;
-#pragma unroll
-        for (int d = 0; d < DK; d += 32) {
-            float x[8];
-            load8<E, AL>(kp + row * a.k.t, d + 8 * q, dk, row < len, x);
-            const auto fk = M::exact(x);
-            load8<E, AL>(qp + row * a.q.t, d + 8 * q, dk, row < len, x);
-            const auto fq = M::exact(x);
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const auto f = tS.frag(16 * n + c, d + 8 * q);
-                mma(z[n], fk, f);
-                mma(o1[n], fq, f);
+                const auto f = tS.frag(16 * n + c, 32 * d + 8 * q);
+                mma(z[n], K.f[d], f);
+                mma(o[n], Q.f[d], f);
             }
-        }
-        const int i0 = 16 * wave + 4 * q;   // this lane's tokens
+        K.load(next); Q.load(next);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int col = c0 + 16 * n + c;
+            const floatx4 v = V.get(n);
             floatx4 x;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float v = i0 + r < len && col < dv ? to_float(at<E>(a.v, w.b, t0 + i0 + r, w.h)[col]) : 0.f;
-                x[r] = v - damp(s_g.gam[i0 + r], z[n][r]);
-            }
+            for (int r = 0; r < 4; ++r) { x[r] = v[r] - damp(gam[r], z[n][r]); o[n][r] = damp(gam[r], o[n][r]); }
             tX.put4(16 * n + c, i0, x);
         }
+        V.load(next);
+        if (KEEP) keep_state(ch, S);
         __syncthreads();
         floatx4 rr[NT] = {};
-        const float* T = a.T + at_chunk * C * C + row * C;
-        for (int k = 0; k < 16 * (wave + 1); k += 32) {
-            float x[8];
-            load8(T + k + 8 * q, x);
-            const auto f = M::computed(x);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma(rr[n], f, tX.frag(16 * n + c, k + 8 * q));
+        for (int k = 0; k < 2; ++k) {
+            if (k > wave / 2) break;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma(rr[n], tr[k], tX.frag(16 * n + c, 32 * k + 8 * q));
         }
+        load_tri<M, false>(a.T, first + next, wave, l, tr);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            floatx4 y, z2;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) { y[r] = s_g.beta[i0 + r] * rr[n][r]; z2[r] = s_g.end[i0 + r] * y[r]; }
+            const floatx4 y = beta * rr[n];
             tY.put4(16 * n + c, i0, y);
-            tZ.put4(16 * n + c, i0, z2);
-            if (a.R) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) a.R[(at_chunk * C + i0 + r) * a.dvp + c0 + 16 * n + c] = rr[n][r];
-            }
+            tZ.put4(16 * n + c, i0, end * y);
         }
+        if (KEEP) put_padded<NT>(a.R + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, rr);
         __syncthreads();
-        floatx4 o2[NT] = {};
-        const float* P = a.P + at_chunk * C * C + row * C;
-        for (int k = 0; k < 16 * (wave + 1); k += 32) {
-            float x[8];
-            load8(P + k + 8 * q, x);
-            const auto f = M::computed(x);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) mma(o2[n], f, tY.frag(16 * n + c, k + 8 * q));
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int col = c0 + 16 * n + c;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (t0 + i0 + r < a.steps && col < dv)
-                    at_out<E>(a.out, w.b, t0 + i0 + r, w.h)[col] = from_float<E>(a.scale * (damp(s_g.gam[i0 + r], o1[n][r]) + o2[n][r]));
-        }
-        const float last = s_g.last;
 #pragma unroll
         for (int s = 0; s < RS; ++s) {
             const int r0 = 16 * (wave * RS + s);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) S[s][n] = last == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : S[s][n] * last;
+            for (int n = 0; n < NT; ++n) {
+                S[s][n] = last == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : S[s][n] * last;
 #pragma unroll
-            for (int k = 0; k < C; k += 32) {
-                const auto f = tK.frag(r0 + c, k + 8 * q);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) mma(S[s][n], f, tZ.frag(16 * n + c, k + 8 * q));
+                for (int k = 0; k < 2; ++k) mma(S[s][n], kt[s][k], tZ.frag(16 * n + c, 32 * k + 8 * q));
+                tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
             }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
         }
-        __syncthreads();                    // K^T and the gates are free again
+        load_kt(next);
+        load_gates(next);
+        floatx4 o2[NT] = {};
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (k > wave / 2) break;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma(o2[n], pr[k], tY.frag(16 * n + c, 32 * k + 8 * q));
+        }
+        load_tri<M, false>(a.P, first + next, wave, l, pr);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[n] = a.scale * (o[n] + o2[n]);
+        ColumnValues<M, NT, AL>::put(a.out, w, a.steps, dv, ch, i0, c0 + c, o);
     }
-    const int n = min(NB, dv - c0);
-    if (a.steps > chunks * C) zero_rows<E>(a.out, w, chunks * C, a.steps, c0, n);
+    const int n = min(16 * NT, dv - c0);
+    if (n > 0 && a.steps > chunks * C) zero_rows<E>(a.out, w, chunks * C, a.steps, c0, n);
     if (!a.state_out) return;
 #pragma unroll
     for (int s = 0; s < RS; ++s)
@@ -609,139 +810,137 @@ __global__ __launch_bounds__(256) void delta_scan_kernel(DeltaArgs a) {
 // =============================================================================================
 // Gradient, chunks in reverse order: dV, and what delta_back_kernel needs of every chunk (dS1, dY, dX).
 // =============================================================================================
-template <typename M, int DK> struct BackScanLds {
-    using S = Tile<M, NB, DK, false>;       // dS^T [column][dim_k]
-    using O = Tile<M, NB, C, true>;         // dO^T [column][token]
-    using X = Tile<M, NB, C, false>;        // dR^T, (gam o dX)^T, (gam o dO)^T [column][token]
-    using K = Tile<M, DK, C, true>;         // K^T, Q^T [dim_k][token]
-    static constexpr int S0 = 0, O0 = S0 + S::BYTES, X0 = O0 + O::BYTES, Y0 = X0 + X::BYTES, Z0 = Y0 + X::BYTES, K0 = Z0 + X::BYTES,
-                         Q0 = K0 + K::BYTES, BYTES = Q0 + K::BYTES;
+template <typename M, int DK, int NT> struct BackScanLds {
+    using S = Tile<M, 16 * NT, DK, false>;          // dS^T [column][dim_k]
+    using O = Tile<M, 16 * NT, C, true>;            // dO^T [column][token]
+    using X = Tile<M, 16 * NT, C, false>;           // dR^T, (gam o dX)^T, (gam o dO)^T [column][token]
+    static constexpr int S0 = 0, O0 = S0 + S::BYTES, X0 = O0 + O::BYTES, Y0 = X0 + X::BYTES, Z0 = Y0 + X::BYTES, BYTES = Z0 + X::BYTES;
 };
-template <typename M, int DK, bool AL>
+template <typename M, int DK, int NT, bool AL>
 __global__ __launch_bounds__(256) void delta_back_scan_kernel(DeltaArgs a) {
     using E = typename M::E;
-    using L = BackScanLds<M, DK>;
-    constexpr int RS = DK / 64, NT = NB / 16;
+    using L = BackScanLds<M, DK, NT>;
+    constexpr int RS = DK / 64, ND = DK / 32;
     extern __shared__ __align__(16) unsigned char lds[];
-    __shared__ Gates s_g;
     const typename L::S tS(lds + L::S0);
     const typename L::O tO(lds + L::O0);
     const typename L::X tR(lds + L::X0), tX(lds + L::Y0), tG(lds + L::Z0);
-    const typename L::K tK(lds + L::K0), tQ(lds + L::Q0);
     const Where w = where_of(a, blockIdx.y);
-    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, q = l >> 4, c0 = blockIdx.x * NB;
-    const int dk = a.dim_k, dv = a.dim_v;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, q = l >> 4, c0 = blockIdx.x * 16 * NT;
+    const int dk = a.dim_k, dv = a.dim_v, row = 16 * wave + c, i0 = 16 * wave + 4 * q;
+    const int chunks = (w.len + C - 1) / C;
+    const int64_t first = (int64_t)w.bh * a.chunks;
+    RowOperands<M, DK, AL> K(a.k, w, w.hk, dk, row, q);
+    ColumnValues<M, NT, AL> O(a.out_grad, w, dv, i0, c0 + c);
+    typename M::X kt[RS][2], qt[RS][2];
+    typename M::Y tr[2], pr[2];
+    floatx4 go[NT], gam, end, beta;
+    float last;
+    auto load_gates = [&](int ch) {
+        const char* g = (const char*)(a.G + (first + ch) * GATES);
+        const unsigned at = 4 * i0;
+        gam = *(const floatx4*)(g + at);
+        end = *(const floatx4*)(g + 4 * C + at);
+        beta = *(const floatx4*)(g + 8 * C + at);
+        last = *(const float*)(g + 12 * C);
+    };
+    auto load_kt = [&](int ch) {
+        const int64_t o = kt_at<E>(a, w, ch, DK);
+#pragma unroll
+        for (int s = 0; s < RS; ++s)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int blk = (2 * (wave * RS + s) + k) * 512 * (int)sizeof(E);
+                const unsigned lane = l * 8 * (int)sizeof(E);
+                kt[s][k] = load_operand<M>((const E*)((const char*)((const E*)a.KT + o) + blk + lane));
+                qt[s][k] = load_operand<M>((const E*)((const char*)((const E*)a.QT + o) + blk + lane));
+            }
+    };
+    if (chunks > 0) {
+        O.load(chunks - 1); K.load(chunks - 1); load_gates(chunks - 1);
+        load_tri<M, true>(a.PT, first + chunks - 1, wave, l, pr);
+        load_tri<M, true>(a.TT, first + chunks - 1, wave, l, tr);
+        load_kt(chunks - 1);
+    }
     floatx4 S[RS][NT];
 #pragma unroll
     for (int s = 0; s < RS; ++s)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int col = c0 + 16 * n + c, row = 16 * (wave * RS + s) + 4 * q;
+            const int col = c0 + 16 * n + c, r0 = 16 * (wave * RS + s) + 4 * q;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                S[s][n][r] = a.state_grad && row + r < dk && col < dv ? a.state_grad[((int64_t)w.bh * dk + row + r) * dv + col] : 0.f;
-            tS.put4(16 * n + c, row, S[s][n]);
+                S[s][n][r] = a.state_grad && r0 + r < dk && col < dv ? a.state_grad[((int64_t)w.bh * dk + r0 + r) * dv + col] : 0.f;
+            tS.put4(16 * n + c, r0, S[s][n]);
         }
-    const int chunks = (w.len + C - 1) / C;
+    if (chunks > 0) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) { go[n] = O.get(n); tO.put4(16 * n + c, i0, go[n]); }
+    }
     for (int ch = chunks - 1; ch >= 0; --ch) {
-        const int len = min(w.len - ch * C, C);
-        const int64_t t0 = (int64_t)ch * C, at_chunk = (int64_t)w.bh * a.chunks + ch;
-        const E* kp = at<E>(a.k, w.b, t0, w.hk);
-        gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
-        stage_transposed<M, DK, AL>(tK, kp, a.k.t, len, dk);
-        stage_transposed<M, DK, AL>(tQ, at<E>(a.q, w.b, t0, w.hk), a.q.t, len, dk);
-        stage_transposed<M, NB, AL>(tO, at<E>(a.out_grad, w.b, t0, w.h), a.out_grad.t, len, dv, c0);
-        {
-            float* o = a.dS + at_chunk * DK * a.dvp;
-#pragma unroll
-            for (int s = 0; s < RS; ++s)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o[(int64_t)(16 * (wave * RS + s) + 4 * q + r) * a.dvp + c0 + 16 * n + c] = S[s][n][r];
-        }
-        __syncthreads();
-        const int i0 = 16 * wave + 4 * q, row = 16 * wave + c;
+        const int next = max(ch - 1, 0);
+        const int64_t at_chunk = first + ch;
+        __syncthreads();                            // dS and dO are in LDS
+        O.load(next);
         floatx4 y1[NT] = {}, y2[NT] = {};
 #pragma unroll
-        for (int d = 0; d < DK; d += 32) {
-            float x[8];
-            load8<E, AL>(kp + row * a.k.t, d + 8 * q, dk, row < len, x);
-            const auto f = M::exact(x);
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma(y1[n], f, tS.frag(16 * n + c, d + 8 * q));
+            for (int n = 0; n < NT; ++n) mma(y1[n], K.f[d], tS.frag(16 * n + c, 32 * d + 8 * q));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (k < wave / 2) continue;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma(y2[n], pr[k], tO.frag(16 * n + c, 32 * k + 8 * q));
         }
-        const float* P = a.P + at_chunk * C * C;
-        for (int k = wave / 2 * 32; k < C; k += 32) {
-            float x[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = P[(k + 8 * q + j) * C + row];
-            const auto f = M::computed(x);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) mma(y2[n], f, tO.frag(16 * n + c, k + 8 * q));
-        }
+        K.load(next);
+        load_tri<M, true>(a.PT, first + next, wave, l, pr);
+        floatx4 dy[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            floatx4 dr, go;
-            const floatx4 o = tO.get4(16 * n + c, i0);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float dy = a.scale * y2[n][r] + s_g.end[i0 + r] * y1[n][r];
-                a.dY[(at_chunk * C + i0 + r) * a.dvp + c0 + 16 * n + c] = dy;
-                dr[r] = s_g.beta[i0 + r] * dy;
-                go[r] = a.scale * s_g.gam[i0 + r] * o[r];
-            }
-            tR.put4(16 * n + c, i0, dr);
-            tG.put4(16 * n + c, i0, go);
+            for (int r = 0; r < 4; ++r) dy[n][r] = a.scale * y2[n][r] + damp(end[r], y1[n][r]);
+            tR.put4(16 * n + c, i0, beta * dy[n]);
+            tG.put4(16 * n + c, i0, a.scale * gam * go[n]);
         }
+        put_padded<NT>(a.dY + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, dy);
+#pragma unroll
+        for (int s = 0; s < RS; ++s) put_padded<NT>(a.dS + at_chunk * DK * a.dvp, 16 * (wave * RS + s), a.dvp, q, c0, c, S[s]);
         __syncthreads();
         floatx4 dx[NT] = {};
-        const float* T = a.T + at_chunk * C * C;
-        for (int k = wave / 2 * 32; k < C; k += 32) {
-            float x[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = T[(k + 8 * q + j) * C + row];
-            const auto f = M::computed(x);
+        for (int k = 0; k < 2; ++k) {
+            if (k < wave / 2) continue;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma(dx[n], f, tR.frag(16 * n + c, k + 8 * q));
+            for (int n = 0; n < NT; ++n) mma(dx[n], tr[k], tR.frag(16 * n + c, 32 * k + 8 * q));
         }
+        load_tri<M, true>(a.TT, first + next, wave, l, tr);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int col = c0 + 16 * n + c;
-            floatx4 gx;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                a.dX[(at_chunk * C + i0 + r) * a.dvp + col] = dx[n][r];
-                if (t0 + i0 + r < a.steps && col < dv)
-                    at_out<E>(a.dv, w.b, t0 + i0 + r, w.h)[col] = from_float<E>(i0 + r < len ? dx[n][r] : 0.f);
-                gx[r] = -s_g.gam[i0 + r] * dx[n][r];
-            }
-            tX.put4(16 * n + c, i0, gx);
-        }
+        for (int n = 0; n < NT; ++n) tX.put4(16 * n + c, i0, -gam * dx[n]);
+        put_padded<NT>(a.dX + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, dx);
+        ColumnValues<M, NT, AL>::put(a.dv, w, a.steps, dv, ch, i0, c0 + c, dx);
         __syncthreads();
-        const float last = s_g.last;
 #pragma unroll
         for (int s = 0; s < RS; ++s) {
             const int r0 = 16 * (wave * RS + s);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) S[s][n] = last == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : S[s][n] * last;
+            for (int n = 0; n < NT; ++n) {
+                S[s][n] = last == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : S[s][n] * last;
 #pragma unroll
-            for (int k = 0; k < C; k += 32) {
-                const auto fk = tK.frag(r0 + c, k + 8 * q);
-                const auto fq = tQ.frag(r0 + c, k + 8 * q);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    mma(S[s][n], fk, tX.frag(16 * n + c, k + 8 * q));
-                    mma(S[s][n], fq, tG.frag(16 * n + c, k + 8 * q));
+                for (int k = 0; k < 2; ++k) {
+                    mma(S[s][n], kt[s][k], tX.frag(16 * n + c, 32 * k + 8 * q));
+                    mma(S[s][n], qt[s][k], tG.frag(16 * n + c, 32 * k + 8 * q));
                 }
+                tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
             }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
         }
-        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < NT; ++n) { go[n] = O.get(n); tO.put4(16 * n + c, i0, go[n]); }
+        load_kt(next);
+        load_gates(next);
     }
-    const int n = min(NB, dv - c0);
-    if (a.steps > chunks * C) zero_rows<E>(a.dv, w, chunks * C, a.steps, c0, n);
+    const int n = min(16 * NT, dv - c0);
+    if (n > 0 && a.steps > chunks * C) zero_rows<E>(a.dv, w, chunks * C, a.steps, c0, n);
     if (!a.dstate) return;
 #pragma unroll
     for (int s = 0; s < RS; ++s)
@@ -970,7 +1169,8 @@ __global__ __launch_bounds__(256) void delta_group_kernel(DeltaArgs a) {
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 struct Plan {                               // padded sizes, and where things lie in `saved` and the workspace
     int dkp, dvp, chunks;
-    size_t T, P, R, S, saved;               // offsets in bytes
+    size_t T, P, G, KT, forward;            // offsets in bytes; `forward`: what a call without `saved` needs
+    size_t TT, PT, QT, R, S, saved;
     size_t dX, dY, dS, part_q, part_k, back;
 };
 bool shape_ok(const pql_delta_shape& s) {
@@ -981,24 +1181,30 @@ bool shape_ok(const pql_delta_shape& s) {
 Plan plan_of(const pql_delta_shape& s) {
     Plan p;
     p.dkp = s.dim_k <= 64 ? 64 : 128;
-    p.dvp = (s.dim_v + NB - 1) / NB * NB;
+    p.dvp = (s.dim_v + 31) / 32 * 32;
     p.chunks = (s.steps + C - 1) / C;
-    const size_t n = (size_t)s.batch * s.heads_v * p.chunks;
+    const size_t n = (size_t)s.batch * s.heads_v * p.chunks, nk = (size_t)s.batch * s.heads_k * p.chunks, es = s.dtype == PQL_F32 ? 4 : 2;
+    const size_t tri = s.dtype == PQL_F32 ? TRI<ModeF> * sizeof(float) : TRI<ModeB> * sizeof(bf16_t);
     size_t o = 0;
-    auto take = [&](size_t floats) { const size_t at = o; o += up256(floats * 4); return at; };
-    p.T = take(n * C * C); p.P = take(n * C * C); p.R = take(n * C * p.dvp); p.S = take(n * p.dkp * p.dvp);
+    auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
+    p.T = take(n * tri); p.P = take(n * tri); p.G = take(n * GATES * 4); p.KT = take(nk * p.dkp * C * es);
+    p.forward = o;
+    p.TT = take(n * tri); p.PT = take(n * tri); p.QT = take(nk * p.dkp * C * es);
+    p.R = take(n * C * p.dvp * 4); p.S = take(n * p.dkp * p.dvp * 4);
     p.saved = o;
     o = 0;
-    p.dX = take(n * C * p.dvp); p.dY = take(n * C * p.dvp); p.dS = take(n * p.dkp * p.dvp);
+    p.dX = take(n * C * p.dvp * 4); p.dY = take(n * C * p.dvp * 4); p.dS = take(n * p.dkp * p.dvp * 4);
     const size_t part = s.heads_v == s.heads_k ? 0 : (size_t)s.batch * s.steps * s.heads_v * s.dim_k;
-    p.part_q = take(part); p.part_k = take(part);
+    p.part_q = take(part * 4); p.part_k = take(part * 4);
     p.back = o;
     return p;
 }
 DeltaSeq seq(const pql_seq& s) { return DeltaSeq{s.data, s.stride_b, s.stride_t, s.stride_h}; }
+// Whether the kernels may load 16 bytes of a row at a time, with 32-bit offsets within a chunk of tokens.
 bool rows_aligned(const pql_seq& s, int dim, int dtype) {
     const int n = dtype == PQL_F32 ? 4 : 8;             // elements in 16 bytes
-    return ((uintptr_t)s.data & 15) == 0 && s.stride_b % n == 0 && s.stride_t % n == 0 && s.stride_h % n == 0 && dim % 8 == 0;
+    return ((uintptr_t)s.data & 15) == 0 && s.stride_b % n == 0 && s.stride_t % n == 0 && s.stride_h % n == 0 && dim % 8 == 0 && s.stride_t >= 0 &&
+           s.stride_t < (1 << 21);
 }
 // Elements of an output must not share a place: a stride of 0 is for inputs only.
 bool apart(const pql_seq& s, const pql_delta_shape& x, int heads) {
@@ -1061,28 +1267,41 @@ template <typename K> hipError_t launch(K kernel, LdsLimit& lim, size_t lds, dim
     prof_commit(ps, kid, flops, bytes);
     return hipGetLastError();
 }
+// 16 columns of the state per workgroup instead of 32 while those are fewer than the card's CUs: a chunk's chain is
+// shorter then, and there are more of them.
+bool narrow(const DeltaArgs& a) { return (int64_t)a.batch * a.heads_v * (a.dvp / 32) < 256; }
 // Work of one token and value head that the chunked form cannot do without, and the token tensors' bytes.
 double token_heads(const DeltaArgs& a) { return (double)a.batch * a.steps * a.heads_v; }
 template <typename M, int DK, bool AL> hipError_t forward_launch(const DeltaArgs& all, hipStream_t st) {
-    static LdsLimit l_prep, l_scan;
+    static LdsLimit l_prep;
     return by_batch(all, [&](const DeltaArgs& a) {
         const double th = token_heads(a), es = sizeof(typename M::E);
         hipError_t e = hipSuccess;
         if (a.chunks > 0)
-            e = launch(delta_prepare_kernel<M, DK, AL>, l_prep, 0, dim3(a.chunks, a.batch * a.heads_v), a, KID_DELTA_PREPARE,
+            e = launch(delta_prepare_kernel<M, DK, AL>, l_prep, 3 * C * LDM * 4, dim3(a.chunks, a.batch * a.heads_v), a, KID_DELTA_PREPARE,
                        th * 4.0 * C * a.dim_k, th * (2 * es * a.dim_k + 8.0 * C), st);
-        if (e == hipSuccess)
-            e = launch(delta_scan_kernel<M, DK, AL>, l_scan, ScanLds<M, DK>::BYTES, dim3(a.dvp / NB, a.batch * a.heads_v), a, KID_DELTA_SCAN,
-                       th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C), st);
+        const double flops = th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, bytes = th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C);
+        auto scan = [&](auto kernel, LdsLimit& lim, int nt, size_t lds) {
+            return launch(kernel, lim, lds, dim3(a.dvp / (16 * nt), a.batch * a.heads_v), a, KID_DELTA_SCAN, flops, bytes, st);
+        };
+        if (e != hipSuccess) return e;
+        static LdsLimit lim[4];
+        if (narrow(a)) e = a.S ? scan(delta_scan_kernel<M, DK, 1, AL, true>, lim[0], 1, ScanLds<M, DK, 1>::BYTES)
+                               : scan(delta_scan_kernel<M, DK, 1, AL, false>, lim[1], 1, ScanLds<M, DK, 1>::BYTES);
+        else e = a.S ? scan(delta_scan_kernel<M, DK, 2, AL, true>, lim[2], 2, ScanLds<M, DK, 2>::BYTES)
+                     : scan(delta_scan_kernel<M, DK, 2, AL, false>, lim[3], 2, ScanLds<M, DK, 2>::BYTES);
         return e;
     });
 }
 template <typename M, int DK, bool AL> hipError_t backward_launch(const DeltaArgs& all, hipStream_t st) {
-    static LdsLimit l_scan, l_back;
+    static LdsLimit l_scan, l_narrow, l_back;
     hipError_t e = by_batch(all, [&](const DeltaArgs& a) {
         const double th = token_heads(a), es = sizeof(typename M::E);
-        hipError_t e = launch(delta_back_scan_kernel<M, DK, AL>, l_scan, BackScanLds<M, DK>::BYTES, dim3(a.dvp / NB, a.batch * a.heads_v), a,
-                              KID_DELTA_BACK_SCAN, th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C + 8.0 * a.dim_v), st);
+        const double flops = th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, bytes = th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C + 8.0 * a.dim_v);
+        hipError_t e = narrow(a) ? launch(delta_back_scan_kernel<M, DK, 1, AL>, l_narrow, BackScanLds<M, DK, 1>::BYTES, dim3(a.dvp / 16, a.batch * a.heads_v), a,
+                                          KID_DELTA_BACK_SCAN, flops, bytes, st)
+                                 : launch(delta_back_scan_kernel<M, DK, 2, AL>, l_scan, BackScanLds<M, DK, 2>::BYTES, dim3(a.dvp / 32, a.batch * a.heads_v), a,
+                                          KID_DELTA_BACK_SCAN, flops, bytes, st);
         if (e == hipSuccess && a.chunks > 0)
             e = launch(delta_back_kernel<M, DK, AL>, l_back, BackLds<M, DK>::BYTES, dim3(a.chunks, a.batch * a.heads_v), a, KID_DELTA_BACK,
                        th * (6.0 * a.dim_k * a.dim_v + 4.0 * C * a.dim_v + 8.0 * C * a.dim_k), th * (es * (4 * a.dim_k + a.dim_v) + 12.0 * a.dim_v), st);
@@ -1104,10 +1323,12 @@ template <typename M, bool BACK> hipError_t chunks_dispatch(const DeltaArgs& a, 
     if (dkp == 64) return al ? forward_launch<M, 64, true>(a, st) : forward_launch<M, 64, false>(a, st);
     return al ? forward_launch<M, 128, true>(a, st) : forward_launch<M, 128, false>(a, st);
 }
-void set_saved(DeltaArgs& a, const Plan& p, char* base, bool states) {
+void set_saved(DeltaArgs& a, const Plan& p, char* base, bool keep) {
     a.chunks = p.chunks; a.dvp = p.dvp;
-    a.T = (float*)(base + p.T); a.P = (float*)(base + p.P);
-    if (states) { a.R = (float*)(base + p.R); a.S = (float*)(base + p.S); }
+    a.T = base + p.T; a.P = base + p.P; a.G = (float*)(base + p.G); a.KT = base + p.KT;
+    if (!keep) return;
+    a.TT = base + p.TT; a.PT = base + p.PT; a.QT = base + p.QT;
+    a.R = (float*)(base + p.R); a.S = (float*)(base + p.S);
 }
 }  // namespace
 }  // namespace pql
@@ -1138,8 +1359,7 @@ int64_t pql_delta_workspace_bytes(const pql_delta_shape* s, int32_t backward) {
     if (!s) return PQL_ERR_NULL;
     if (!shape_ok(*s)) return PQL_ERR_INVALID_ARG;
     const Plan p = plan_of(*s);
-    const size_t forward = p.R;             // T and P, where the caller keeps nothing
-    return (int64_t)(backward && p.back > forward ? p.back : forward);
+    return (int64_t)(backward && p.back > p.forward ? p.back : p.forward);
 }
 
 int32_t pql_delta_forward(pql_ctx* c, const pql_delta_shape* s, const pql_delta_input* in, pql_seq out, float* state_out, void* saved,
@@ -1155,7 +1375,8 @@ int32_t pql_delta_forward(pql_ctx* c, const pql_delta_shape* s, const pql_delta_
     DeltaArgs a = args_of(*s, *in);
     a.out = seq(out); a.state_out = state_out;
     set_saved(a, p, (char*)(saved ? saved : workspace), saved != nullptr);
-    const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype);
+    const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype) && rows_aligned(in->v, s->dim_v, s->dtype) &&
+                    rows_aligned(out, s->dim_v, s->dtype);
     const hipError_t e = s->dtype == PQL_F32 ? chunks_dispatch<ModeF, false>(a, al, p.dkp, (hipStream_t)stream)
                                              : chunks_dispatch<ModeB, false>(a, al, p.dkp, (hipStream_t)stream);
     return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_delta_forward", e);
@@ -1184,7 +1405,8 @@ int32_t pql_delta_backward(pql_ctx* c, const pql_delta_shape* s, const pql_delta
     a.dq = seq(g->q); a.dk = seq(g->k); a.dv = seq(g->v); a.dg = seq(g->log_decay); a.dbeta = seq(g->beta); a.dstate = g->state;
     a.dX = (float*)(w + p.dX); a.dY = (float*)(w + p.dY); a.dS = (float*)(w + p.dS);
     if (a.group > 1) { a.part_q = (float*)(w + p.part_q); a.part_k = (float*)(w + p.part_k); }
-    const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype) && rows_aligned(out_grad, s->dim_v, s->dtype);
+    const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype) && rows_aligned(out_grad, s->dim_v, s->dtype) &&
+                    rows_aligned(g->v, s->dim_v, s->dtype);
     const hipError_t e = s->dtype == PQL_F32 ? chunks_dispatch<ModeF, true>(a, al, p.dkp, (hipStream_t)stream)
                                              : chunks_dispatch<ModeB, true>(a, al, p.dkp, (hipStream_t)stream);
     return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_delta_backward", e);

@@ -43,8 +43,10 @@ struct DeltaArgs {
     const int* lengths;
     const float* state;
     float* state_out;
-    // per (sequence, head, chunk), fp32: T, P [64][64], R [64][dvp], S [dim_k padded][dvp] (before the chunk); R, S may be NULL
-    float *T, *P, *R, *S;
+    // per (sequence, head, chunk), fp32: T and P in operand order, gates; K^T per key head, of the tokens' type.  What only
+    // the gradient reads may be NULL: T^T, P^T, Q^T, R [64][dvp], S [dim_k padded][dvp] (before the chunk)
+    void *T, *P, *TT, *PT, *KT, *QT;
+    float *G, *R, *S;
     // gradient: dX, dY [64][dvp], dS [dim_k padded][dvp] (after the chunk); dq, dk per value head where those are shared
     DeltaSeq out_grad, dq, dk, dv, dg, dbeta;
     const float* state_grad;
