@@ -28,7 +28,7 @@
 namespace pql {
 namespace {
 
-constexpr int C = 64;                       // tokens per chunk
+constexpr int MAXC = 64;                    // most tokens per chunk (C below: 64, or 32 where sequences are that short)
 constexpr float NEG_INF = -__builtin_inff();
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -113,6 +113,16 @@ template <typename M, int ROWS, int COLS, bool EXACT> struct Tile {
             *(bf16x4*)o = h; *(bf16x4*)(o + ROWS * LD) = m; *(bf16x4*)(o + 2 * ROWS * LD) = l;
         }
     }
+    __device__ __forceinline__ void put8(int row, int k, const float* x) const {
+        E* o = p + row * LD + k;
+        const auto f = M::computed(x);
+        if constexpr (PLANES == 3) {
+            *(bf16x8*)o = f.h; *(bf16x8*)(o + ROWS * LD) = f.m; *(bf16x8*)(o + 2 * ROWS * LD) = f.l;
+        } else {
+            *(floatx4*)o = floatx4{f.v[0], f.v[1], f.v[2], f.v[3]};
+            *(floatx4*)(o + 4) = floatx4{f.v[4], f.v[5], f.v[6], f.v[7]};
+        }
+    }
     __device__ __forceinline__ void put1(int row, int k, float x) const {
         E* o = p + row * LD + k;
         if constexpr (PLANES == 3) {
@@ -182,10 +192,10 @@ __device__ __forceinline__ void load8(const float* p, float* x) {
     for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
 }
 // The chunk's tokens transposed: tile[d][token], d < D.
-template <typename M, int D, bool AL, typename T>
+template <typename M, int C, int D, bool AL, typename T>
 __device__ __forceinline__ void stage_transposed(const T& tile, const typename M::E* base, int64_t stride_t, int len, int dim, int d0 = 0) {
-    for (int u = threadIdx.x; u < D / 8 * 16; u += 256) {
-        const int t = u % 16 * 4, d = u / 16 * 8;
+    for (int u = threadIdx.x; u < D / 8 * (C / 4); u += 4 * C) {
+        const int t = u % (C / 4) * 4, d = u / (C / 4) * 8;
         float x[4][8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) load8<typename M::E, AL>(base + (t + i) * stride_t, d0 + d, dim, t + i < len, x[i]);
@@ -196,9 +206,9 @@ __device__ __forceinline__ void stage_transposed(const T& tile, const typename M
 
 // ---- gates of a chunk -------------------------------------------------------------------------
 struct Gates {
-    double sum[C];                          // G_i; double, so that differences of long sums stay exact
-    int part[C];                            // resets up to and including the token
-    float beta[C], gam[C], end[C];
+    double sum[MAXC];                       // G_i; double, so that differences of long sums stay exact
+    int part[MAXC];                         // resets up to and including the token
+    float beta[MAXC], gam[MAXC], end[MAXC];
     float last;                             // e^{G_last}, 0 after a reset in the chunk
 };
 // By the first wavefront; a barrier follows.
@@ -358,64 +368,73 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a) {
 // =============================================================================================
 // Chunks: T and P of every chunk.
 // =============================================================================================
-__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
-
-// In place: the strictly lower triangular part of m [C][LDM] becomes (I + m)^-1 with unit diagonal and zeros above.
-// Blocks of 16: those on the diagonal by substitution (stable whatever the keys; a product of powers is not), then
-// block columns downwards, T_ij = -T_ii sum_{j <= k < i} m_ik T_kj, each wavefront one column.
-constexpr int LDM = C + 1;
-__device__ __forceinline__ void invert(float (*m)[LDM], float (*t)[LDM], float (*scratch)[16][17]) {
-    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, q = l >> 4;
-    for (int i = threadIdx.x; i < C * C; i += 256) t[i / C][i % C] = 0.f;
-    __syncthreads();
-    if (l < 16) {
-        float x[16];
+// t = (I + m)^-1 of a strictly lower triangular m.  Blocks of 16: those on the diagonal by substitution (stable whatever the
+// keys; a series of powers is not), one wavefront each; then T_ij = -T_ii sum_{j <= k < i} m_ik T_kj downwards, one block
+// column per wavefront.  With the contraction index 4 (l / 16) + s in step s, a result is the next product's right operand
+// as it lies in the registers, so a column needs nothing from LDS but m and the diagonal.  Blocks (0, 1) and (2, 3), which
+// operands of 32 columns cover, are zeroed; others above the diagonal are not written.
+template <int C> struct Matrix { static constexpr int LD = C + 4; float v[C][LD]; };
+template <int C> __device__ __forceinline__ void invert(const Matrix<C>& m, Matrix<C>& t) {
+    constexpr int NW = C / 16;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, q = l >> 4;
+    float x[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            x[i] = i == l ? 1.f : 0.f;
+    for (int i = 0; i < 16; ++i) {
+        float y = i == c ? 1.f : 0.f;
 #pragma unroll
-            for (int k = 0; k < i; ++k) x[i] -= m[16 * w + i][16 * w + k] * x[k];
+        for (int k = 0; k < i; k += 4) {
+            const floatx4 r = *(const floatx4*)&m.v[16 * w + i][16 * w + k];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (k + j < i) y -= r[j] * x[k + j];
         }
+        x[i] = y;
+    }
+    floatx4 col[NW];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) t[16 * w + i][16 * w + l] = x[i];
+    for (int r = 0; r < 4; ++r) {
+        const float d = q == 0 ? x[r] : q == 1 ? x[4 + r] : q == 2 ? x[8 + r] : x[12 + r];
+#pragma unroll
+        for (int k = 0; k < NW; ++k) col[k][r] = d;        // only [w] is read
+        t.v[16 * w + 4 * q + r][16 * w + c] = d;
+        if (w & 1) t.v[16 * (w - 1) + 4 * q + r][16 * w + c] = 0.f;
     }
     __syncthreads();
-    for (int i = w + 1; i < C / 16; ++i) {
-        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int k = w; k < i; ++k)
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
-                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(m[16 * i + c][16 * k + 4 * s + q], t[16 * k + 4 * s + q][16 * w + c], acc, 0, 0, 0);
+    for (int i = 1; i < NW; ++i) {
+        if (i <= w) continue;
+        floatx4 acc = {0.f, 0.f, 0.f, 0.f}, o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int r = 0; r < 4; ++r) scratch[w][4 * q + r][c] = acc[r];
-        wave_fence();
-        floatx4 o = {0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < i; ++k) {
+            if (k < w) continue;
+            const floatx4 r = *(const floatx4*)&m.v[16 * i + c][16 * k + 4 * q];
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-            o = __builtin_amdgcn_mfma_f32_16x16x4f32(t[16 * i + c][16 * i + 4 * s + q], scratch[w][4 * s + q][c], o, 0, 0, 0);
-        wave_fence();
+            for (int s = 0; s < 4; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(r[s], col[k][s], acc, 0, 0, 0);
+        }
+        const floatx4 r = *(const floatx4*)&t.v[16 * i + c][16 * i + 4 * q];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) t[16 * i + 4 * q + r][16 * w + c] = -o[r];
-        wave_fence();
+        for (int s = 0; s < 4; ++s) o = __builtin_amdgcn_mfma_f32_16x16x4f32(r[s], acc[s], o, 0, 0, 0);
+        col[i] = -o;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) t.v[16 * i + 4 * q + s][16 * w + c] = -o[s];
     }
     __syncthreads();
 }
 
 // ---- what the prepare kernel leaves for the others, all in operand order --------------------------------------------
-// T and P (rows of A operands) and, for the gradient, their transposes: the six 16 x 32 blocks that are not all zero,
-// [block][term][lane][8], computed values split already.  Rows 16 w .. of T and P need the contraction blocks 0 .. w / 2, those of the transposes
-// w / 2 .. 1.
-constexpr int BLOCKS = 6;
+// T and P (rows of A operands) and, for the gradient, their transposes: the 16 x 32 blocks that are not all zero (six of
+// 64 tokens, two of 32), [block][term][lane][8], computed values split already.  Rows 16 w .. of T and P need the
+// contraction blocks 0 .. w / 2, those of the transposes w / 2 .. C / 32 - 1.
+template <int C> constexpr int BLOCKS = C == 64 ? 6 : 2;
 template <typename M> constexpr int BLOCK = 64 * 8 * M::PLANES;          // elements of a block
-template <typename M> constexpr int TRI = BLOCKS * BLOCK<M>;
-__device__ __forceinline__ constexpr int tri_block(int w, int ks) { return w < 2 ? w : 2 * w - 2 + ks; }            // 0 1 2 3 4 5
-__device__ __forceinline__ constexpr int tri_block_t(int w, int ks) { return w < 2 ? 2 * w + ks : 2 + w; }
-// K^T, Q^T: [dim_k / 16][2][lane][8] of the tokens' type, one per key head.
-template <typename E> __device__ __forceinline__ int64_t kt_at(const DeltaArgs& a, const Where& w, int ch, int dkp) {
+template <typename M, int C> constexpr int TRI = BLOCKS<C> * BLOCK<M>;
+template <int C> __device__ __forceinline__ constexpr int tri_block(int w, int ks) { return C == 32 || w < 2 ? w : 2 * w - 2 + ks; }        // 64: 0 1 2 3 4 5
+template <int C> __device__ __forceinline__ constexpr int tri_block_t(int w, int ks) { return C == 32 ? w : w < 2 ? 2 * w + ks : 2 + w; }
+// K^T, Q^T: [dim_k / 16][C / 32][lane][8] of the tokens' type, one per key head.
+template <typename E, int C> __device__ __forceinline__ int64_t kt_at(const DeltaArgs& a, const Where& w, int ch, int dkp) {
     return (((int64_t)w.b * a.heads_k + w.hk) * a.chunks + ch) * dkp * C;
 }
-// Gates: gam[64], end[64], beta[64], e^{G_last}.
-constexpr int GATES = 4 * C;
+// Gates: gam[C], end[C], beta[C], e^{G_last}.
+template <int C> constexpr int GATES = 4 * C;
 template <typename M> __device__ __forceinline__ typename M::X load_operand(const typename M::E* p) {
     if constexpr (sizeof(typename M::E) == 4) {
         FF f;
@@ -450,7 +469,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tokens(const char* p) {
 }
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 // The operands of one wavefront's 16 token rows.
-template <typename M, int DK, bool AL> struct RowOperands {
+template <typename M, int C, int DK, bool AL> struct RowOperands {
     using E = typename M::E;
     static constexpr int ND = DK / 32, ES = sizeof(E);
     const char* base;                       // token 0
@@ -485,7 +504,7 @@ template <typename M, int DK, bool AL> struct RowOperands {
     }
 };
 // The same for results laid out as [4 tokens][column]: element (i0 + r, col + 16 n).
-template <typename M, int NT, bool AL> struct ColumnValues {
+template <typename M, int C, int NT, bool AL> struct ColumnValues {
     using E = typename M::E;
     static constexpr int ES = sizeof(E);
     const char* base;
@@ -554,47 +573,46 @@ template <int NT> __device__ __forceinline__ void put_padded(float* base, int r0
     }
 }
 
-template <typename M, int DK, bool AL>
-__global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
+template <typename M, int C, int DK, bool AL>
+__global__ __launch_bounds__(4 * C) void delta_prepare_kernel(DeltaArgs a) {
     using E = typename M::E;
     using KT = Tile<M, DK, C, true>;
+    constexpr int NW = C / 16, KS = C / 32;
     extern __shared__ __align__(16) unsigned char lds[];
     __shared__ Gates s_g;
-    __shared__ float s_x[4][16][17];
-    float (*const s_m)[LDM] = (float (*)[LDM])lds;
-    float (*const s_t)[LDM] = s_m + C;
-    float (*const s_p)[LDM] = s_t + C;
+    Matrix<C>& s_m = *(Matrix<C>*)lds;
+    Matrix<C>& s_t = *(Matrix<C>*)(lds + sizeof(Matrix<C>));     // P first, then T
     const Where w = where_of(a, blockIdx.y);
     const int ch = blockIdx.x, left = w.len - ch * C;
     if (left <= 0) return;
     const int len = min(left, C);
     const int64_t t0 = (int64_t)ch * C, at_chunk = (int64_t)w.bh * a.chunks + ch;
-    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, q = l >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, q = l >> 4;
     const E* kp = at<E>(a.k, w.b, t0, w.hk);
     const E* qp = at<E>(a.q, w.b, t0, w.hk);
     gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
     if (w.h % a.group == 0) {               // this key head's transposes
         const KT tile(lds);
         for (int which = 0; which < (a.QT ? 2 : 1); ++which) {
-            stage_transposed<M, DK, AL>(tile, which ? qp : kp, which ? a.q.t : a.k.t, len, a.dim_k);
+            stage_transposed<M, C, DK, AL>(tile, which ? qp : kp, which ? a.q.t : a.k.t, len, a.dim_k);
             __syncthreads();
-            E* o = (E*)(which ? a.QT : a.KT) + kt_at<E>(a, w, ch, DK);
-            for (int i = threadIdx.x; i < DK / 16 * 2 * 64; i += 256) {
-                const E* from = tile.p + ((i >> 7) * 16 + (i & 15)) * KT::LD + (i >> 6 & 1) * 32 + (i >> 4 & 3) * 8;
+            E* o = (E*)(which ? a.QT : a.KT) + kt_at<E, C>(a, w, ch, DK);
+            for (int i = threadIdx.x; i < DK / 16 * KS * 64; i += 4 * C) {
+                const E* from = tile.p + ((i / (64 * KS)) * 16 + (i & 15)) * KT::LD + (i / 64 % KS) * 32 + (i >> 4 & 3) * 8;
                 *(uint4*)(o + i * 8) = *(const uint4*)from;
                 if (sizeof(E) == 4) *(uint4*)(o + i * 8 + 4) = *(const uint4*)(from + 4);
             }
             __syncthreads();
         }
     }
-    floatx4 kk[4] = {}, qk[4] = {};
+    floatx4 kk[NW] = {}, qk[NW] = {};
 #pragma unroll
     for (int d = 0; d < DK; d += 32) {
         const int row = 16 * wave + c;
         const auto fk = row_operand<M, AL>(kp + row * a.k.t, d + 8 * q, a.dim_k, row < len);
         const auto fq = row_operand<M, AL>(qp + row * a.q.t, d + 8 * q, a.dim_k, row < len);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
+        for (int n = 0; n < NW; ++n) {
             if (n > wave) break;
             const auto f = row_operand<M, AL>(kp + (16 * n + c) * a.k.t, d + 8 * q, a.dim_k, 16 * n + c < len);
             mma(kk[n], fk, f);
@@ -603,44 +621,47 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
     }
     __syncthreads();                        // gates are there
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
+    for (int n = 0; n < NW; ++n) {
         const int j = 16 * n + c;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = 16 * wave + 4 * q + r;
-            const float f = i >= j ? decay(s_g, i, j) : 0.f;
-            s_p[i][j] = f * qk[n][r];
-            s_m[i][j] = i > j ? f * kk[n][r] * s_g.beta[j] : 0.f;
+            const float f = n <= wave && i >= j ? decay(s_g, i, j) : 0.f;
+            s_t.v[i][j] = f * qk[n][r];
+            s_m.v[i][j] = i > j ? f * kk[n][r] * s_g.beta[j] : 0.f;
         }
     }
     __syncthreads();
-    invert(s_m, s_t, s_x);
+    // a matrix and its transpose in operand order
     auto put = [&](void* base, int i, const float* x) {      // eight values of block i / 64, lane i % 64
-        E* o = (E*)base + at_chunk * TRI<M> + (i >> 6) * BLOCK<M> + (i & 63) * 8;
+        E* o = (E*)base + at_chunk * TRI<M, C> + (i >> 6) * BLOCK<M> + (i & 63) * 8;
         const auto f = M::computed(x);
         if constexpr (M::PLANES == 3) {
             *(bf16x8*)o = f.h; *(bf16x8*)(o + 512) = f.m; *(bf16x8*)(o + 1024) = f.l;
         } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = f.v[j];
+            *(floatx4*)o = floatx4{f.v[0], f.v[1], f.v[2], f.v[3]};
+            *(floatx4*)(o + 4) = floatx4{f.v[4], f.v[5], f.v[6], f.v[7]};
         }
     };
-    for (int i = threadIdx.x; i < BLOCKS * 64; i += 256) {
-        const int blk = i >> 6, bw = blk < 2 ? blk : 2 + (blk - 2) / 2, ks = blk < 2 ? 0 : blk & 1;
-        const int row = 16 * bw + (i & 15), k = 32 * ks + (i >> 4 & 3) * 8;
-        put(a.T, i, &s_t[row][k]);
-        put(a.P, i, &s_p[row][k]);
-        if (a.TT) {
-            const int tw = blk < 4 ? blk / 2 : blk - 2, tk = blk < 4 ? blk & 1 : 1;
-            const int col = 16 * tw + (i & 15), r0 = 32 * tk + (i >> 4 & 3) * 8;
-            float t[8], p[8];
+    auto emit = [&](const Matrix<C>& x, void* rows, void* columns) {
+        for (int i = threadIdx.x; i < BLOCKS<C> * 64; i += 4 * C) {
+            const int blk = i >> 6, bw = C == 32 || blk < 2 ? blk : 2 + (blk - 2) / 2, ks = C == 32 || blk < 2 ? 0 : blk & 1;
+            float y[8];
+            load8(&x.v[16 * bw + (i & 15)][32 * ks + (i >> 4 & 3) * 8], y);
+            put(rows, i, y);
+            if (columns) {
+                const int tw = C == 32 ? blk : blk < 4 ? blk / 2 : blk - 2, tk = C == 32 ? 0 : blk < 4 ? blk & 1 : 1;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { t[j] = s_t[r0 + j][col]; p[j] = s_p[r0 + j][col]; }
-            put(a.TT, i, t);
-            put(a.PT, i, p);
+                for (int j = 0; j < 8; ++j) y[j] = x.v[32 * tk + (i >> 4 & 3) * 8 + j][16 * tw + (i & 15)];
+                put(columns, i, y);
+            }
         }
-    }
-    float* g = a.G + at_chunk * GATES;
+    };
+    emit(s_t, a.P, a.PT);
+    __syncthreads();
+    invert<C>(s_m, s_t);
+    emit(s_t, a.T, a.TT);
+    float* g = a.G + at_chunk * GATES<C>;
     if (threadIdx.x < C) {
         g[threadIdx.x] = s_g.gam[threadIdx.x];
         g[C + threadIdx.x] = s_g.end[threadIdx.x];
@@ -653,29 +674,29 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
 // Chunks in order: outputs and states, 16 NT columns per workgroup.  Nothing but the state's own chain K S, T X, K^T Y
 // waits for a chunk: all operands of the next one are requested into registers as soon as this one's have been used.
 // =============================================================================================
-template <typename M, int DK, int NT> struct ScanLds {
+template <typename M, int C, int DK, int NT> struct ScanLds {
     using S = Tile<M, 16 * NT, DK, false>;          // S^T [column][dim_k]
     using X = Tile<M, 16 * NT, C, false>;           // X^T, Y^T, (e o Y)^T [column][token]
     static constexpr int S0 = 0, X0 = S0 + S::BYTES, Y0 = X0 + X::BYTES, Z0 = Y0 + X::BYTES, BYTES = Z0 + X::BYTES;
 };
-template <typename E> __device__ __forceinline__ void zero_rows(const DeltaSeq& s, const Where& w, int from, int to, int c0, int n) {
-    for (int i = threadIdx.x; i < (to - from) * n; i += 256) at_out<E>(s, w.b, from + i / n, w.h)[c0 + i % n] = from_float<E>(0.f);
+template <int THREADS, typename E> __device__ __forceinline__ void zero_rows(const DeltaSeq& s, const Where& w, int from, int to, int c0, int n) {
+    for (int i = threadIdx.x; i < (to - from) * n; i += THREADS) at_out<E>(s, w.b, from + i / n, w.h)[c0 + i % n] = from_float<E>(0.f);
 }
 // The two blocks of a wavefront's rows of T, P or their transposes.  Blocks that are zero are not there: the other one is
 // loaded twice (a load in a branch would make later waits longer) and not used.
-template <typename M, bool TRANSPOSED> __device__ __forceinline__ void load_tri(const void* base, int64_t at_chunk, int wave, int l, typename M::Y (&x)[2]) {
+template <typename M, int C, bool TRANSPOSED> __device__ __forceinline__ void load_tri(const void* base, int64_t at_chunk, int wave, int l, typename M::Y (&x)[C / 32]) {
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    for (int ks = 0; ks < C / 32; ++ks)
     {
         const int k = TRANSPOSED ? max(ks, wave / 2) : min(ks, wave / 2);
-        x[ks] = load_split<M>((const char*)base + (at_chunk * TRI<M> + (TRANSPOSED ? tri_block_t(wave, k) : tri_block(wave, k)) * BLOCK<M>) * (int)sizeof(typename M::E), 16 * l);
+        x[ks] = load_split<M>((const char*)base + (at_chunk * TRI<M, C> + (TRANSPOSED ? tri_block_t<C>(wave, k) : tri_block<C>(wave, k)) * BLOCK<M>) * (int)sizeof(typename M::E), 16 * l);
     }
 }
-template <typename M, int DK, int NT, bool AL, bool KEEP>
-__global__ __launch_bounds__(256) void delta_scan_kernel(DeltaArgs a) {
+template <typename M, int C, int DK, int NT, bool AL, bool KEEP>
+__global__ __launch_bounds__(4 * C) void delta_scan_kernel(DeltaArgs a) {
     using E = typename M::E;
-    using L = ScanLds<M, DK, NT>;
-    constexpr int RS = DK / 64, ND = DK / 32;       // 16-row strips of the state per wavefront, contraction steps
+    using L = ScanLds<M, C, DK, NT>;
+    constexpr int RS = DK / C, KS = C / 32, ND = DK / 32;       // 16-row strips of the state per wavefront, contraction steps
     extern __shared__ __align__(16) unsigned char lds[];
     const typename L::S tS(lds + L::S0);
     const typename L::X tX(lds + L::X0), tY(lds + L::Y0), tZ(lds + L::Z0);
@@ -684,14 +705,14 @@ __global__ __launch_bounds__(256) void delta_scan_kernel(DeltaArgs a) {
     const int dk = a.dim_k, dv = a.dim_v, row = 16 * wave + c, i0 = 16 * wave + 4 * q;
     const int chunks = (w.len + C - 1) / C;
     const int64_t first = (int64_t)w.bh * a.chunks;
-    RowOperands<M, DK, AL> K(a.k, w, w.hk, dk, row, q), Q(a.q, w, w.hk, dk, row, q);
-    ColumnValues<M, NT, AL> V(a.v, w, dv, i0, c0 + c);
-    typename M::X kt[RS][2];
-    typename M::Y tr[2], pr[2];
+    RowOperands<M, C, DK, AL> K(a.k, w, w.hk, dk, row, q), Q(a.q, w, w.hk, dk, row, q);
+    ColumnValues<M, C, NT, AL> V(a.v, w, dv, i0, c0 + c);
+    typename M::X kt[RS][KS];
+    typename M::Y tr[KS], pr[KS];
     floatx4 gam, end, beta;
     float last;
     auto load_gates = [&](int ch) {
-        const char* g = (const char*)(a.G + (first + ch) * GATES);
+        const char* g = (const char*)(a.G + (first + ch) * GATES<C>);
         const unsigned at = 4 * i0;
         gam = *(const floatx4*)(g + at);
         end = *(const floatx4*)(g + 4 * C + at);
@@ -699,12 +720,12 @@ __global__ __launch_bounds__(256) void delta_scan_kernel(DeltaArgs a) {
         last = *(const float*)(g + 12 * C);
     };
     auto load_kt = [&](int ch) {
-        const char* p = (const char*)((const E*)a.KT + kt_at<E>(a, w, ch, DK));
+        const char* p = (const char*)((const E*)a.KT + kt_at<E, C>(a, w, ch, DK));
 #pragma unroll
         for (int s = 0; s < RS; ++s)
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-                kt[s][k] = load_operand<M>((const E*)(p + (2 * (wave * RS + s) + k) * 512 * (int)sizeof(E) + (unsigned)(l * 8 * (int)sizeof(E))));
+            for (int k = 0; k < KS; ++k)
+                kt[s][k] = load_operand<M>((const E*)(p + (KS * (wave * RS + s) + k) * 512 * (int)sizeof(E) + (unsigned)(l * 8 * (int)sizeof(E))));
     };
     auto keep_state = [&](int ch, const floatx4 (&S)[RS][NT]) {
 #pragma unroll
@@ -712,8 +733,8 @@ __global__ __launch_bounds__(256) void delta_scan_kernel(DeltaArgs a) {
     };
     if (chunks > 0) {
         K.load(0); Q.load(0); V.load(0); load_gates(0);
-        load_tri<M, false>(a.T, first, wave, l, tr);
-        load_tri<M, false>(a.P, first, wave, l, pr);
+        load_tri<M, C, false>(a.T, first, wave, l, tr);
+        load_tri<M, C, false>(a.P, first, wave, l, pr);
         load_kt(0);
     }
     floatx4 S[RS][NT];
@@ -754,12 +775,12 @@ __global__ __launch_bounds__(256) void delta_scan_kernel(DeltaArgs a) {
         __syncthreads();
         floatx4 rr[NT] = {};
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < KS; ++k) {
             if (k > wave / 2) break;
 #pragma unroll
             for (int n = 0; n < NT; ++n) mma(rr[n], tr[k], tX.frag(16 * n + c, 32 * k + 8 * q));
         }
-        load_tri<M, false>(a.T, first + next, wave, l, tr);
+        load_tri<M, C, false>(a.T, first + next, wave, l, tr);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const floatx4 y = beta * rr[n];
@@ -775,7 +796,7 @@ __global__ __launch_bounds__(256) void delta_scan_kernel(DeltaArgs a) {
             for (int n = 0; n < NT; ++n) {
                 S[s][n] = last == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : S[s][n] * last;
 #pragma unroll
-                for (int k = 0; k < 2; ++k) mma(S[s][n], kt[s][k], tZ.frag(16 * n + c, 32 * k + 8 * q));
+                for (int k = 0; k < KS; ++k) mma(S[s][n], kt[s][k], tZ.frag(16 * n + c, 32 * k + 8 * q));
                 tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
             }
         }
@@ -783,18 +804,18 @@ __global__ __launch_bounds__(256) void delta_scan_kernel(DeltaArgs a) {
         load_gates(next);
         floatx4 o2[NT] = {};
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < KS; ++k) {
             if (k > wave / 2) break;
 #pragma unroll
             for (int n = 0; n < NT; ++n) mma(o2[n], pr[k], tY.frag(16 * n + c, 32 * k + 8 * q));
         }
-        load_tri<M, false>(a.P, first + next, wave, l, pr);
+        load_tri<M, C, false>(a.P, first + next, wave, l, pr);
 #pragma unroll
         for (int n = 0; n < NT; ++n) o[n] = a.scale * (o[n] + o2[n]);
-        ColumnValues<M, NT, AL>::put(a.out, w, a.steps, dv, ch, i0, c0 + c, o);
+        ColumnValues<M, C, NT, AL>::put(a.out, w, a.steps, dv, ch, i0, c0 + c, o);
     }
     const int n = min(16 * NT, dv - c0);
-    if (n > 0 && a.steps > chunks * C) zero_rows<E>(a.out, w, chunks * C, a.steps, c0, n);
+    if (n > 0 && a.steps > chunks * C) zero_rows<4 * C, E>(a.out, w, chunks * C, a.steps, c0, n);
     if (!a.state_out) return;
 #pragma unroll
     for (int s = 0; s < RS; ++s)
@@ -810,17 +831,17 @@ __global__ __launch_bounds__(256) void delta_scan_kernel(DeltaArgs a) {
 // =============================================================================================
 // Gradient, chunks in reverse order: dV, and what delta_back_kernel needs of every chunk (dS1, dY, dX).
 // =============================================================================================
-template <typename M, int DK, int NT> struct BackScanLds {
+template <typename M, int C, int DK, int NT> struct BackScanLds {
     using S = Tile<M, 16 * NT, DK, false>;          // dS^T [column][dim_k]
     using O = Tile<M, 16 * NT, C, true>;            // dO^T [column][token]
     using X = Tile<M, 16 * NT, C, false>;           // dR^T, (gam o dX)^T, (gam o dO)^T [column][token]
     static constexpr int S0 = 0, O0 = S0 + S::BYTES, X0 = O0 + O::BYTES, Y0 = X0 + X::BYTES, Z0 = Y0 + X::BYTES, BYTES = Z0 + X::BYTES;
 };
-template <typename M, int DK, int NT, bool AL>
-__global__ __launch_bounds__(256) void delta_back_scan_kernel(DeltaArgs a) {
+template <typename M, int C, int DK, int NT, bool AL>
+__global__ __launch_bounds__(4 * C) void delta_back_scan_kernel(DeltaArgs a) {
     using E = typename M::E;
-    using L = BackScanLds<M, DK, NT>;
-    constexpr int RS = DK / 64, ND = DK / 32;
+    using L = BackScanLds<M, C, DK, NT>;
+    constexpr int RS = DK / C, KS = C / 32, ND = DK / 32;
     extern __shared__ __align__(16) unsigned char lds[];
     const typename L::S tS(lds + L::S0);
     const typename L::O tO(lds + L::O0);
@@ -830,14 +851,14 @@ __global__ __launch_bounds__(256) void delta_back_scan_kernel(DeltaArgs a) {
     const int dk = a.dim_k, dv = a.dim_v, row = 16 * wave + c, i0 = 16 * wave + 4 * q;
     const int chunks = (w.len + C - 1) / C;
     const int64_t first = (int64_t)w.bh * a.chunks;
-    RowOperands<M, DK, AL> K(a.k, w, w.hk, dk, row, q);
-    ColumnValues<M, NT, AL> O(a.out_grad, w, dv, i0, c0 + c);
-    typename M::X kt[RS][2], qt[RS][2];
-    typename M::Y tr[2], pr[2];
+    RowOperands<M, C, DK, AL> K(a.k, w, w.hk, dk, row, q);
+    ColumnValues<M, C, NT, AL> O(a.out_grad, w, dv, i0, c0 + c);
+    typename M::X kt[RS][KS], qt[RS][KS];
+    typename M::Y tr[KS], pr[KS];
     floatx4 go[NT], gam, end, beta;
     float last;
     auto load_gates = [&](int ch) {
-        const char* g = (const char*)(a.G + (first + ch) * GATES);
+        const char* g = (const char*)(a.G + (first + ch) * GATES<C>);
         const unsigned at = 4 * i0;
         gam = *(const floatx4*)(g + at);
         end = *(const floatx4*)(g + 4 * C + at);
@@ -845,12 +866,12 @@ __global__ __launch_bounds__(256) void delta_back_scan_kernel(DeltaArgs a) {
         last = *(const float*)(g + 12 * C);
     };
     auto load_kt = [&](int ch) {
-        const int64_t o = kt_at<E>(a, w, ch, DK);
+        const int64_t o = kt_at<E, C>(a, w, ch, DK);
 #pragma unroll
         for (int s = 0; s < RS; ++s)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int blk = (2 * (wave * RS + s) + k) * 512 * (int)sizeof(E);
+            for (int k = 0; k < KS; ++k) {
+                const int blk = (KS * (wave * RS + s) + k) * 512 * (int)sizeof(E);
                 const unsigned lane = l * 8 * (int)sizeof(E);
                 kt[s][k] = load_operand<M>((const E*)((const char*)((const E*)a.KT + o) + blk + lane));
                 qt[s][k] = load_operand<M>((const E*)((const char*)((const E*)a.QT + o) + blk + lane));
@@ -858,8 +879,8 @@ __global__ __launch_bounds__(256) void delta_back_scan_kernel(DeltaArgs a) {
     };
     if (chunks > 0) {
         O.load(chunks - 1); K.load(chunks - 1); load_gates(chunks - 1);
-        load_tri<M, true>(a.PT, first + chunks - 1, wave, l, pr);
-        load_tri<M, true>(a.TT, first + chunks - 1, wave, l, tr);
+        load_tri<M, C, true>(a.PT, first + chunks - 1, wave, l, pr);
+        load_tri<M, C, true>(a.TT, first + chunks - 1, wave, l, tr);
         load_kt(chunks - 1);
     }
     floatx4 S[RS][NT];
@@ -888,13 +909,13 @@ __global__ __launch_bounds__(256) void delta_back_scan_kernel(DeltaArgs a) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) mma(y1[n], K.f[d], tS.frag(16 * n + c, 32 * d + 8 * q));
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < KS; ++k) {
             if (k < wave / 2) continue;
 #pragma unroll
             for (int n = 0; n < NT; ++n) mma(y2[n], pr[k], tO.frag(16 * n + c, 32 * k + 8 * q));
         }
         K.load(next);
-        load_tri<M, true>(a.PT, first + next, wave, l, pr);
+        load_tri<M, C, true>(a.PT, first + next, wave, l, pr);
         floatx4 dy[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -909,16 +930,16 @@ __global__ __launch_bounds__(256) void delta_back_scan_kernel(DeltaArgs a) {
         __syncthreads();
         floatx4 dx[NT] = {};
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < KS; ++k) {
             if (k < wave / 2) continue;
 #pragma unroll
             for (int n = 0; n < NT; ++n) mma(dx[n], tr[k], tR.frag(16 * n + c, 32 * k + 8 * q));
         }
-        load_tri<M, true>(a.TT, first + next, wave, l, tr);
+        load_tri<M, C, true>(a.TT, first + next, wave, l, tr);
 #pragma unroll
         for (int n = 0; n < NT; ++n) tX.put4(16 * n + c, i0, -gam * dx[n]);
         put_padded<NT>(a.dX + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, dx);
-        ColumnValues<M, NT, AL>::put(a.dv, w, a.steps, dv, ch, i0, c0 + c, dx);
+        ColumnValues<M, C, NT, AL>::put(a.dv, w, a.steps, dv, ch, i0, c0 + c, dx);
         __syncthreads();
 #pragma unroll
         for (int s = 0; s < RS; ++s) {
@@ -927,7 +948,7 @@ __global__ __launch_bounds__(256) void delta_back_scan_kernel(DeltaArgs a) {
             for (int n = 0; n < NT; ++n) {
                 S[s][n] = last == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : S[s][n] * last;
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
+                for (int k = 0; k < KS; ++k) {
                     mma(S[s][n], kt[s][k], tX.frag(16 * n + c, 32 * k + 8 * q));
                     mma(S[s][n], qt[s][k], tG.frag(16 * n + c, 32 * k + 8 * q));
                 }
@@ -940,7 +961,7 @@ __global__ __launch_bounds__(256) void delta_back_scan_kernel(DeltaArgs a) {
         load_gates(next);
     }
     const int n = min(16 * NT, dv - c0);
-    if (n > 0 && a.steps > chunks * C) zero_rows<E>(a.dv, w, chunks * C, a.steps, c0, n);
+    if (n > 0 && a.steps > chunks * C) zero_rows<4 * C, E>(a.dv, w, chunks * C, a.steps, c0, n);
     if (!a.dstate) return;
 #pragma unroll
     for (int s = 0; s < RS; ++s)
@@ -954,33 +975,39 @@ __global__ __launch_bounds__(256) void delta_back_scan_kernel(DeltaArgs a) {
 }
 
 // =============================================================================================
-// Gradient, all chunks at once: dQ, dK, dbeta, dg.  A wavefront takes 16 tokens; contractions over the columns read
-// their operands straight from memory, those over tokens from LDS.
+// Gradient, all chunks at once: dQ, dK, dbeta, dg.  Two wavefronts per 16 tokens, each with half of dim_k.  First the
+// contractions over the columns, 32 at a time: what all wavefronts need (R, Y, S0, dS1) is brought from memory, split and put
+// into LDS once for all of them, the next 32 columns being on their way meanwhile; then those over tokens with E and F in
+// LDS, K^T and Q^T straight from memory.
 // =============================================================================================
-template <typename M, int DK> struct BackLds {
+template <typename M, int C, int DK> struct BackLds {
+    using R = Tile<M, C, 32, false>;        // R, Y
+    using S = Tile<M, DK, 32, false>;       // S0, dS1
     using W = Tile<M, C, C, false>;         // E, E^T, F diag(beta), F^T
-    using K = Tile<M, DK, C, true>;         // K^T, Q^T
-    static constexpr int E0 = 0, ET0 = E0 + W::BYTES, F0 = ET0 + W::BYTES, FT0 = F0 + W::BYTES, K0 = FT0 + W::BYTES, Q0 = K0 + K::BYTES,
-                         BYTES = Q0 + K::BYTES;
+    static constexpr int R0 = 0, Y0 = R0 + R::BYTES, S0 = Y0 + R::BYTES, S1 = S0 + S::BYTES, FIRST = S1 + S::BYTES;
+    static constexpr int E0 = 0, ET0 = E0 + W::BYTES, F0 = ET0 + W::BYTES, FT0 = F0 + W::BYTES, SECOND = FT0 + W::BYTES;
+    static constexpr int BYTES = FIRST > SECOND ? FIRST : SECOND;
 };
 __device__ __forceinline__ float sum16(float x) {      // over the 16 lanes that hold one row of a result
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) x += __shfl_xor(x, d);
     return x;
 }
-template <typename M, int DK, bool AL>
-__global__ __launch_bounds__(256) void delta_back_kernel(DeltaArgs a) {
+template <typename M, int C, int DK, bool AL>
+__global__ __launch_bounds__(8 * C) void delta_back_kernel(DeltaArgs a) {
     using E = typename M::E;
-    using L = BackLds<M, DK>;
-    constexpr int NK = DK / 16;
+    using L = BackLds<M, C, DK>;
+    constexpr int NW = C / 16, KS = C / 32, NK = DK / 32, THREADS = 8 * C, SU = 8 * DK / THREADS;      // NK: 16-column tiles of a wavefront's half
     extern __shared__ __align__(16) unsigned char lds[];
     __shared__ Gates s_g;
-    __shared__ float s_dG[C], s_ext[4];
+    __shared__ float s_dG[2][C], s_b[2][C], s_ext[2 * NW];
+    const typename L::R tR(lds + L::R0), tY(lds + L::Y0);
+    const typename L::S tS0(lds + L::S0), tS1(lds + L::S1);
     const typename L::W tE(lds + L::E0), tET(lds + L::ET0), tF(lds + L::F0), tFT(lds + L::FT0);
-    const typename L::K tK(lds + L::K0), tQ(lds + L::Q0);
     const Where w = where_of(a, blockIdx.y);
-    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, q = l >> 4;
-    const int dk = a.dim_k, ch = blockIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, q = l >> 4;
+    const int strip = wave % NW, half = wave / NW, n0 = half * NK;
+    const int dk = a.dim_k, ch = blockIdx.x, dvp = a.dvp;
     const int64_t t0 = (int64_t)ch * C, at_chunk = (int64_t)w.bh * a.chunks + ch;
     const int len = min(w.len - ch * C, C), rows = min(a.steps - ch * C, C);
     // one value head per key head: straight to the results; else to one row per value head, added up afterwards
@@ -989,78 +1016,110 @@ __global__ __launch_bounds__(256) void delta_back_kernel(DeltaArgs a) {
         else at_out<E>(s, w.b, t0 + i, w.h)[d] = from_float<E>(x);
     };
     if (len <= 0) {
-        for (int i = threadIdx.x; i < rows * dk; i += 256) { put(a.dq, a.part_q, i / dk, i % dk, 0.f); put(a.dk, a.part_k, i / dk, i % dk, 0.f); }
-        for (int i = threadIdx.x; i < rows; i += 256) { *at_out<float>(a.dg, w.b, t0 + i, w.h) = 0.f; *at_out<float>(a.dbeta, w.b, t0 + i, w.h) = 0.f; }
+        for (int i = threadIdx.x; i < rows * dk; i += THREADS) { put(a.dq, a.part_q, i / dk, i % dk, 0.f); put(a.dk, a.part_k, i / dk, i % dk, 0.f); }
+        for (int i = threadIdx.x; i < rows; i += THREADS) { *at_out<float>(a.dg, w.b, t0 + i, w.h) = 0.f; *at_out<float>(a.dbeta, w.b, t0 + i, w.h) = 0.f; }
         return;
     }
     gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
-    stage_transposed<M, DK, AL>(tK, at<E>(a.k, w.b, t0, w.hk), a.k.t, len, dk);
-    stage_transposed<M, DK, AL>(tQ, at<E>(a.q, w.b, t0, w.hk), a.q.t, len, dk);
-    __syncthreads();
-    const int row = 16 * wave + c, i0 = 16 * wave + 4 * q;
-    const float* R = a.R + at_chunk * C * a.dvp;
-    const float* dX = a.dX + at_chunk * C * a.dvp;
-    const float* dY = a.dY + at_chunk * C * a.dvp;
-    const float* S0 = a.S + at_chunk * DK * a.dvp;
-    const float* S1 = a.dS + at_chunk * DK * a.dvp;
+    const int row = 16 * strip + c, i0 = 16 * strip + 4 * q;
+    const float* R = a.R + at_chunk * C * dvp;
+    const float* dX = a.dX + at_chunk * C * dvp;
+    const float* dY = a.dY + at_chunk * C * dvp;
+    const float* S0 = a.S + at_chunk * DK * dvp;
+    const float* S1 = a.dS + at_chunk * DK * dvp;
     const E* dO = at<E>(a.out_grad, w.b, t0, w.h);
-    floatx4 dq[NK] = {}, ks[NK] = {}, ke[NK] = {}, e[4] = {}, f[4] = {};
-    float yr = 0.f, ss = 0.f;               // dY.R of row `row` (this lane's columns), <dS1, S0> of this lane's elements
-    for (int d = 0; d < a.dvp; d += 32) {
-        float x[8], y[8];
-        load8<E, AL>(dO + row * a.out_grad.t, d + 8 * q, a.dim_v, row < len, x);
-        const auto fo = M::exact(x);
-        load8(dX + row * a.dvp + d + 8 * q, x);
-        const auto fx = M::computed(x);
-        load8(R + row * a.dvp + d + 8 * q, x);
-        load8(dY + row * a.dvp + d + 8 * q, y);
-        const float beta = s_g.beta[row];
+    // what the next 32 columns need: this thread's share of the matrices in LDS, this wavefront's rows of dX and dO
+    float xr[8], xs[SU][8], xx[8];
+    typename M::X fo;
+    const int unit = threadIdx.x;           // eight columns (unit % 4) of row unit / 4, of R or of S0 and dS1
+    auto load = [&](int d) {
+        if (unit < 4 * C) load8(R + (unit >> 2) * dvp + d + (unit & 3) * 8, xr);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { yr += x[j] * y[j]; x[j] *= beta; }
-        const auto fy = M::computed(x);
+        for (int i = 0; i < SU; ++i) {
+            const int u = unit + i * THREADS, r = u >> 2;
+            load8((r < DK ? S0 + r * dvp : S1 + (r - DK) * dvp) + d + (u & 3) * 8, xs[i]);
+        }
+        load8(dX + row * dvp + d + 8 * q, xx);
+        fo = row_operand<M, AL>(dO + row * a.out_grad.t, d + 8 * q, a.dim_v, row < len);
+    };
+    load(0);
+    floatx4 dq[NK] = {}, ks[NK] = {}, ke[NK] = {}, ef[NW] = {};     // ef: E (first half of the wavefronts) or F
+    float yr = 0.f, ss = 0.f;               // dY.R of row `row` (this lane's columns), <dS1, S0> of this thread's elements
+    __syncthreads();                        // gates are there
+    for (int d = 0; d < dvp; d += 32) {
+        if (unit < 4 * C) {
+            const int r = unit >> 2, k = (unit & 3) * 8;
+            const float beta = s_g.beta[r];
+            tR.put8(r, k, xr);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            if (n > wave) break;
-            load8(R + (16 * n + c) * a.dvp + d + 8 * q, x);
-            const auto g = M::computed(x);
-            mma(f[n], fx, g);
-            const float b = s_g.beta[16 * n + c];
+            for (int j = 0; j < 8; ++j) xr[j] *= beta;
+            tY.put8(r, k, xr);
+        }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] *= b;
-            const auto h = M::computed(x);
-            mma(e[n], fo, h);
+        for (int i = 0; i < SU; ++i) {
+            const int u = unit + i * THREADS, r = u >> 2;
+            if (r < DK) tS0.put8(r, (u & 3) * 8, xs[i]);
+            else tS1.put8(r - DK, (u & 3) * 8, xs[i]);
+        }
+        const auto fx = M::computed(xx);
+        const auto fd = fo;
+        if (half == 0) {                    // dY.R; exact in 32 bits, outside the split products
+            float x[8], y[8];
+            load8(R + row * dvp + d + 8 * q, x);
+            load8(dY + row * dvp + d + 8 * q, y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) yr += x[j] * y[j];
+        }
+        if (d + 32 < dvp) load(d + 32);
+        __syncthreads();
+        const auto fy = tY.frag(row, 8 * q);
+        if (half == 0) {
+#pragma unroll
+            for (int n = 0; n < NW; ++n)
+                if (n <= strip) mma(ef[n], fd, tY.frag(16 * n + c, 8 * q));
+        } else {
+#pragma unroll
+            for (int n = 0; n < NW; ++n)
+                if (n <= strip) mma(ef[n], fx, tR.frag(16 * n + c, 8 * q));
         }
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
-            load8(S0 + (16 * n + c) * a.dvp + d + 8 * q, x);
-            load8(S1 + (16 * n + c) * a.dvp + d + 8 * q, y);
-            if ((n & 3) == wave) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) ss += x[j] * y[j];
-            }
-            const auto g = M::computed(x);
-            mma(dq[n], fo, g);
+            const auto g = tS0.frag(16 * (n0 + n) + c, 8 * q);
+            mma(dq[n], fd, g);
             mma(ks[n], fx, g);
-            mma(ke[n], fy, M::computed(y));
+            mma(ke[n], fy, tS1.frag(16 * (n0 + n) + c, 8 * q));
         }
+        __syncthreads();
     }
+    for (int i = threadIdx.x; i < DK * dvp / 4; i += THREADS) {     // <dS1, S0>, from the caches
+        const floatx4 x = ((const floatx4*)S0)[i], y = ((const floatx4*)S1)[i];
+        ss += x[0] * y[0] + x[1] * y[1] + x[2] * y[2] + x[3] * y[3];
+    }
+    // K^T and Q^T of this half, as right operands and as values beside the results
+    const E* KT = (const E*)a.KT + kt_at<E, C>(a, w, ch, DK);
+    const E* QT = (const E*)a.QT + kt_at<E, C>(a, w, ch, DK);
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
+    for (int n = 0; n < NW; ++n) {
         const int j = 16 * n + c;
-        floatx4 x;
+        const float beta = s_g.beta[j];
+        floatx4 x = ef[n], y;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = i0 + r;
-            const float g = i >= j ? decay(s_g, i, j) : 0.f;
-            e[n][r] *= a.scale * g;
-            f[n][r] = i > j ? -g * f[n][r] : 0.f;
-            x[r] = f[n][r] * s_g.beta[j];
+            const float g = n <= strip && i >= j ? decay(s_g, i, j) : 0.f;
+            x[r] = half == 0 ? damp(a.scale * g, x[r]) : i > j ? damp(-g, x[r]) : 0.f;
+            y[r] = half == 0 ? x[r] : x[r] * beta;
         }
         // rows of the transposes are columns here: four consecutive elements of one row each; of the others one at a time
-        tET.put4(j, i0, e[n]);
-        tFT.put4(j, i0, f[n]);
+        if (half == 0) {
+            tET.put4(j, i0, x);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) { tE.put1(i0 + r, j, e[n][r]); tF.put1(i0 + r, j, x[r]); }
+            for (int r = 0; r < 4; ++r) tE.put1(i0 + r, j, y[r]);
+        } else {
+            tFT.put4(j, i0, x);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) tF.put1(i0 + r, j, y[r]);
+        }
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -1069,41 +1128,43 @@ __global__ __launch_bounds__(256) void delta_back_kernel(DeltaArgs a) {
         for (int n = 0; n < NK; ++n) { dq[n][r] = damp(a.scale * g, dq[n][r]); ks[n][r] = damp(-g, ks[n][r]); ke[n][r] = damp(en, ke[n][r]); }
     }
     __syncthreads();
-    floatx4 ft[NK] = {};                    // F^T K
-    for (int k = 0; k < 16 * (wave + 1); k += 32) {     // E and F diag(beta): lower triangles
-        const auto fe = tE.frag(row, k + 8 * q);
-        const auto ff = tF.frag(row, k + 8 * q);
+    auto values = [&](const E* T, int n) {              // tokens i0 .. i0 + 3 of column 16 (n0 + n) + c
+        const E* p = T + (KS * (n0 + n) + strip / 2) * 512 + (c + 16 * (2 * (strip & 1) + (q >> 1))) * 8 + 4 * (q & 1);
+        floatx4 x;
+        if constexpr (sizeof(E) == 4) {
+            x = *(const floatx4*)p;
+        } else {
+            const bf16x4 h = *(const bf16x4*)p;
 #pragma unroll
-        for (int n = 0; n < NK; ++n) {
-            const auto g = tK.frag(16 * n + c, k + 8 * q);
-            mma(dq[n], fe, g);
-            mma(ks[n], ff, g);
+            for (int r = 0; r < 4; ++r) x[r] = (float)h[r];
         }
-    }
-    float kdot_end[4] = {}, kdot[4] = {}, kft[4] = {};
-#pragma unroll
-    for (int n = 0; n < NK; ++n) {          // before E^T Q joins it: the part of dG_last
-        const floatx4 kv = tK.get4(16 * n + c, i0);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) kdot_end[r] += kv[r] * ke[n][r];
-    }
-    for (int k = wave / 2 * 32; k < C; k += 32) {
-        const auto fe = tET.frag(row, k + 8 * q);
-        const auto ff = tFT.frag(row, k + 8 * q);
-#pragma unroll
-        for (int n = 0; n < NK; ++n) {
-            mma(ke[n], fe, tQ.frag(16 * n + c, k + 8 * q));
-            mma(ft[n], ff, tK.frag(16 * n + c, k + 8 * q));
-        }
-    }
+        return x;
+    };
+    floatx4 kdot = {}, kft = {};
+    float ext = 0.f;
 #pragma unroll
     for (int n = 0; n < NK; ++n) {
-        const floatx4 kv = tK.get4(16 * n + c, i0), qv = tQ.get4(16 * n + c, i0);
-        const int d = 16 * n + c;
+        floatx4 ft = {};                    // F^T K
+        const floatx4 kv = values(KT, n), qv = values(QT, n);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) ext += kv[r] * ke[n][r];          // before E^T Q joins it: the part of dG_last
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const auto fk = load_operand<M>(KT + ((KS * (n0 + n) + k) * 64 + l) * 8);
+            if (k <= strip / 2) {           // E and F diag(beta): lower triangles
+                mma(dq[n], tE.frag(row, 32 * k + 8 * q), fk);
+                mma(ks[n], tF.frag(row, 32 * k + 8 * q), fk);
+            }
+            if (k >= strip / 2) {
+                mma(ke[n], tET.frag(row, 32 * k + 8 * q), load_operand<M>(QT + ((KS * (n0 + n) + k) * 64 + l) * 8));
+                mma(ft, tFT.frag(row, 32 * k + 8 * q), fk);
+            }
+        }
+        const int d = 16 * (n0 + n) + c;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            kft[r] += kv[r] * ft[n][r];
-            const float rest = ke[n][r] + s_g.beta[i0 + r] * ft[n][r];
+            kft[r] += kv[r] * ft[r];
+            const float rest = ke[n][r] + s_g.beta[i0 + r] * ft[r];
             kdot[r] += qv[r] * dq[n][r] + kv[r] * (ks[n][r] - rest);
             if (i0 + r < rows && d < dk) {
                 const bool in = i0 + r < len;
@@ -1112,38 +1173,36 @@ __global__ __launch_bounds__(256) void delta_back_kernel(DeltaArgs a) {
             }
         }
     }
-    // dY.R of one row lies in the lanes c, c + 16, c + 32, c + 48
+    // dY.R of one row lies in the lanes c, c + 16, c + 32, c + 48 (zero in the second half's wavefronts)
     yr += __shfl_xor(yr, 16);
     yr += __shfl_xor(yr, 32);
-    float ext = 0.f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const float b = sum16(kft[r]) + __shfl(yr, 4 * q + r);
-        const float g = sum16(kdot[r]);
-        ext += sum16(kdot_end[r]);
-        if (c == 0) {
-            s_dG[i0 + r] = g;
-            if (i0 + r < rows) *at_out<float>(a.dbeta, w.b, t0 + i0 + r, w.h) = i0 + r < len ? b : 0.f;
-        }
+        const float b = sum16(kft[r]) + __shfl(yr, 4 * q + r), g = sum16(kdot[r]);
+        if (c == 0) { s_dG[half][i0 + r] = g; s_b[half][i0 + r] = b; }
     }
-    ss = sum16(ss);                         // over the wavefront: 16 lanes here, the four groups of them below
-    float both = ext + damp(s_g.last, ss);
-    both += __shfl_xor(both, 16);
-    both += __shfl_xor(both, 32);
-    if (l == 0) s_ext[wave] = both;
+    ext += damp(s_g.last, ss);
+    ext = sum16(ext);
+    ext += __shfl_xor(ext, 16);
+    ext += __shfl_xor(ext, 32);
+    if (l == 0) s_ext[wave] = ext;
     __syncthreads();
     if (wave == 0) {                        // sums from the end to each token, within its segment
-        float x = s_dG[l];
-        if (l == 63) x += s_ext[0] + s_ext[1] + s_ext[2] + s_ext[3];
+        float x = l < C ? s_dG[0][l] + s_dG[1][l] : 0.f;
+        if (l == C - 1)
+#pragma unroll
+            for (int i = 0; i < 2 * NW; ++i) x += s_ext[i];
         const int part = s_g.part[l];
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
+        for (int d = 1; d < C; d *= 2) {
             const float o = __shfl_down(x, d);
             const int p = __shfl_down(part, d);
-            if (l + d < 64 && p == part) x += o;
+            if (l + d < C && p == part) x += o;
         }
-        if (l < rows) *at_out<float>(a.dg, w.b, t0 + l, w.h) =
-            l < len && *at<float>(a.g, w.b, t0 + l, w.h) != NEG_INF ? x : 0.f;
+        if (l < rows) {
+            *at_out<float>(a.dg, w.b, t0 + l, w.h) = l < len && *at<float>(a.g, w.b, t0 + l, w.h) != NEG_INF ? x : 0.f;
+            *at_out<float>(a.dbeta, w.b, t0 + l, w.h) = l < len ? s_b[0][l] + s_b[1][l] : 0.f;
+        }
     }
 }
 
@@ -1168,7 +1227,7 @@ __global__ __launch_bounds__(256) void delta_group_kernel(DeltaArgs a) {
 // ---- launches -------------------------------------------------------------------------------
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 struct Plan {                               // padded sizes, and where things lie in `saved` and the workspace
-    int dkp, dvp, chunks;
+    int c, dkp, dvp, chunks;                // c: tokens per chunk; 32 where no sequence is longer: half the rows of 64 would be empty
     size_t T, P, G, KT, forward;            // offsets in bytes; `forward`: what a call without `saved` needs
     size_t TT, PT, QT, R, S, saved;
     size_t dX, dY, dS, part_q, part_k, back;
@@ -1182,18 +1241,19 @@ Plan plan_of(const pql_delta_shape& s) {
     Plan p;
     p.dkp = s.dim_k <= 64 ? 64 : 128;
     p.dvp = (s.dim_v + 31) / 32 * 32;
-    p.chunks = (s.steps + C - 1) / C;
+    p.c = s.steps <= 32 ? 32 : 64;
+    p.chunks = (s.steps + p.c - 1) / p.c;
     const size_t n = (size_t)s.batch * s.heads_v * p.chunks, nk = (size_t)s.batch * s.heads_k * p.chunks, es = s.dtype == PQL_F32 ? 4 : 2;
-    const size_t tri = s.dtype == PQL_F32 ? TRI<ModeF> * sizeof(float) : TRI<ModeB> * sizeof(bf16_t);
+    const size_t tri = s.dtype == PQL_F32 ? (p.c == 32 ? TRI<ModeF, 32> : TRI<ModeF, 64>) * sizeof(float) : (p.c == 32 ? TRI<ModeB, 32> : TRI<ModeB, 64>) * sizeof(bf16_t);
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
-    p.T = take(n * tri); p.P = take(n * tri); p.G = take(n * GATES * 4); p.KT = take(nk * p.dkp * C * es);
+    p.T = take(n * tri); p.P = take(n * tri); p.G = take(n * 4 * p.c * 4); p.KT = take(nk * p.dkp * p.c * es);
     p.forward = o;
-    p.TT = take(n * tri); p.PT = take(n * tri); p.QT = take(nk * p.dkp * C * es);
-    p.R = take(n * C * p.dvp * 4); p.S = take(n * p.dkp * p.dvp * 4);
+    p.TT = take(n * tri); p.PT = take(n * tri); p.QT = take(nk * p.dkp * p.c * es);
+    p.R = take(n * p.c * p.dvp * 4); p.S = take(n * p.dkp * p.dvp * 4);
     p.saved = o;
     o = 0;
-    p.dX = take(n * C * p.dvp * 4); p.dY = take(n * C * p.dvp * 4); p.dS = take(n * p.dkp * p.dvp * 4);
+    p.dX = take(n * p.c * p.dvp * 4); p.dY = take(n * p.c * p.dvp * 4); p.dS = take(n * p.dkp * p.dvp * 4);
     const size_t part = s.heads_v == s.heads_k ? 0 : (size_t)s.batch * s.steps * s.heads_v * s.dim_k;
     p.part_q = take(part * 4); p.part_k = take(part * 4);
     p.back = o;
@@ -1257,13 +1317,13 @@ template <typename F> hipError_t by_batch(const DeltaArgs& a, F&& f) {
     }
     return hipSuccess;
 }
-template <typename K> hipError_t launch(K kernel, LdsLimit& lim, size_t lds, dim3 grid, const DeltaArgs& a, int kid, double flops, double bytes, hipStream_t st) {
+template <typename K> hipError_t launch(K kernel, LdsLimit& lim, size_t lds, dim3 grid, int threads, const DeltaArgs& a, int kid, double flops, double bytes, hipStream_t st) {
     if (lds > 32768) {
         const hipError_t e = set_lds_limit((const void*)kernel, lds, lim);
         if (e != hipSuccess) return e;
     }
     const ProfSlot ps = prof_slot();
-    PQL_LAUNCH(ps, kernel, grid, dim3(256), lds, st, a);
+    PQL_LAUNCH(ps, kernel, grid, dim3(threads), lds, st, a);
     prof_commit(ps, kid, flops, bytes);
     return hipGetLastError();
 }
@@ -1272,56 +1332,61 @@ template <typename K> hipError_t launch(K kernel, LdsLimit& lim, size_t lds, dim
 bool narrow(const DeltaArgs& a) { return (int64_t)a.batch * a.heads_v * (a.dvp / 32) < 256; }
 // Work of one token and value head that the chunked form cannot do without, and the token tensors' bytes.
 double token_heads(const DeltaArgs& a) { return (double)a.batch * a.steps * a.heads_v; }
-template <typename M, int DK, bool AL> hipError_t forward_launch(const DeltaArgs& all, hipStream_t st) {
-    static LdsLimit l_prep;
-    return by_batch(all, [&](const DeltaArgs& a) {
-        const double th = token_heads(a), es = sizeof(typename M::E);
-        hipError_t e = hipSuccess;
-        if (a.chunks > 0)
-            e = launch(delta_prepare_kernel<M, DK, AL>, l_prep, 3 * C * LDM * 4, dim3(a.chunks, a.batch * a.heads_v), a, KID_DELTA_PREPARE,
-                       th * 4.0 * C * a.dim_k, th * (2 * es * a.dim_k + 8.0 * C), st);
-        const double flops = th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, bytes = th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C);
-        auto scan = [&](auto kernel, LdsLimit& lim, int nt, size_t lds) {
-            return launch(kernel, lim, lds, dim3(a.dvp / (16 * nt), a.batch * a.heads_v), a, KID_DELTA_SCAN, flops, bytes, st);
-        };
-        if (e != hipSuccess) return e;
-        static LdsLimit lim[4];
-        if (narrow(a)) e = a.S ? scan(delta_scan_kernel<M, DK, 1, AL, true>, lim[0], 1, ScanLds<M, DK, 1>::BYTES)
-                               : scan(delta_scan_kernel<M, DK, 1, AL, false>, lim[1], 1, ScanLds<M, DK, 1>::BYTES);
-        else e = a.S ? scan(delta_scan_kernel<M, DK, 2, AL, true>, lim[2], 2, ScanLds<M, DK, 2>::BYTES)
-                     : scan(delta_scan_kernel<M, DK, 2, AL, false>, lim[3], 2, ScanLds<M, DK, 2>::BYTES);
-        return e;
-    });
-}
-template <typename M, int DK, bool AL> hipError_t backward_launch(const DeltaArgs& all, hipStream_t st) {
-    static LdsLimit l_scan, l_narrow, l_back;
-    hipError_t e = by_batch(all, [&](const DeltaArgs& a) {
-        const double th = token_heads(a), es = sizeof(typename M::E);
-        const double flops = th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, bytes = th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C + 8.0 * a.dim_v);
-        hipError_t e = narrow(a) ? launch(delta_back_scan_kernel<M, DK, 1, AL>, l_narrow, BackScanLds<M, DK, 1>::BYTES, dim3(a.dvp / 16, a.batch * a.heads_v), a,
-                                          KID_DELTA_BACK_SCAN, flops, bytes, st)
-                                 : launch(delta_back_scan_kernel<M, DK, 2, AL>, l_scan, BackScanLds<M, DK, 2>::BYTES, dim3(a.dvp / 32, a.batch * a.heads_v), a,
-                                          KID_DELTA_BACK_SCAN, flops, bytes, st);
-        if (e == hipSuccess && a.chunks > 0)
-            e = launch(delta_back_kernel<M, DK, AL>, l_back, BackLds<M, DK>::BYTES, dim3(a.chunks, a.batch * a.heads_v), a, KID_DELTA_BACK,
-                       th * (6.0 * a.dim_k * a.dim_v + 4.0 * C * a.dim_v + 8.0 * C * a.dim_k), th * (es * (4 * a.dim_k + a.dim_v) + 12.0 * a.dim_v), st);
-        return e;
-    });
-    if (e != hipSuccess || all.group == 1 || all.steps == 0) return e;
-    const int64_t n = 2 * (int64_t)all.batch * all.steps * all.heads_k * all.dim_k;
-    const int64_t blocks = (n + 255) / 256 < 4096 ? (n + 255) / 256 : 4096;
-    const ProfSlot ps = prof_slot();
-    PQL_LAUNCH(ps, delta_group_kernel<typename M::E>, dim3((unsigned)blocks), dim3(256), 0, st, all);
-    prof_commit(ps, KID_DELTA_GROUP, 0.0, (double)n * (4.0 * all.group + sizeof(typename M::E)));
-    return hipGetLastError();
-}
-template <typename M, bool BACK> hipError_t chunks_dispatch(const DeltaArgs& a, bool al, int dkp, hipStream_t st) {
-    if (BACK) {
-        if (dkp == 64) return al ? backward_launch<M, 64, true>(a, st) : backward_launch<M, 64, false>(a, st);
-        return al ? backward_launch<M, 128, true>(a, st) : backward_launch<M, 128, false>(a, st);
+template <typename M, int C, int DK, bool AL> struct Chunked {
+    static hipError_t forward(const DeltaArgs& all, hipStream_t st) {
+        return by_batch(all, [&](const DeltaArgs& a) {
+            static LdsLimit l_prep, lim[4];
+            const double th = token_heads(a), es = sizeof(typename M::E);
+            const double flops = th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, bytes = th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C);
+            hipError_t e = hipSuccess;
+            if (a.chunks > 0)
+                e = launch(delta_prepare_kernel<M, C, DK, AL>, l_prep, prepare_lds(), dim3(a.chunks, a.batch * a.heads_v), 4 * C, a, KID_DELTA_PREPARE,
+                           th * 4.0 * C * a.dim_k, th * (2 * es * a.dim_k + 8.0 * C), st);
+            if (e != hipSuccess) return e;
+            auto scan = [&](auto kernel, LdsLimit& lim, int nt, size_t lds) {
+                return launch(kernel, lim, lds, dim3(a.dvp / (16 * nt), a.batch * a.heads_v), 4 * C, a, KID_DELTA_SCAN, flops, bytes, st);
+            };
+            if (narrow(a)) return a.S ? scan(delta_scan_kernel<M, C, DK, 1, AL, true>, lim[0], 1, ScanLds<M, C, DK, 1>::BYTES)
+                                      : scan(delta_scan_kernel<M, C, DK, 1, AL, false>, lim[1], 1, ScanLds<M, C, DK, 1>::BYTES);
+            return a.S ? scan(delta_scan_kernel<M, C, DK, 2, AL, true>, lim[2], 2, ScanLds<M, C, DK, 2>::BYTES)
+                       : scan(delta_scan_kernel<M, C, DK, 2, AL, false>, lim[3], 2, ScanLds<M, C, DK, 2>::BYTES);
+        });
     }
-    if (dkp == 64) return al ? forward_launch<M, 64, true>(a, st) : forward_launch<M, 64, false>(a, st);
-    return al ? forward_launch<M, 128, true>(a, st) : forward_launch<M, 128, false>(a, st);
+    static hipError_t backward(const DeltaArgs& all, hipStream_t st) {
+        const hipError_t e = by_batch(all, [&](const DeltaArgs& a) {
+            static LdsLimit l_scan, l_narrow, l_back;
+            const double th = token_heads(a), es = sizeof(typename M::E);
+            const double flops = th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, bytes = th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C + 8.0 * a.dim_v);
+            hipError_t e = narrow(a) ? launch(delta_back_scan_kernel<M, C, DK, 1, AL>, l_narrow, BackScanLds<M, C, DK, 1>::BYTES,
+                                              dim3(a.dvp / 16, a.batch * a.heads_v), 4 * C, a, KID_DELTA_BACK_SCAN, flops, bytes, st)
+                                     : launch(delta_back_scan_kernel<M, C, DK, 2, AL>, l_scan, BackScanLds<M, C, DK, 2>::BYTES,
+                                              dim3(a.dvp / 32, a.batch * a.heads_v), 4 * C, a, KID_DELTA_BACK_SCAN, flops, bytes, st);
+            if (e == hipSuccess && a.chunks > 0)
+                e = launch(delta_back_kernel<M, C, DK, AL>, l_back, BackLds<M, C, DK>::BYTES, dim3(a.chunks, a.batch * a.heads_v), 8 * C, a, KID_DELTA_BACK,
+                           th * (6.0 * a.dim_k * a.dim_v + 4.0 * C * a.dim_v + 8.0 * C * a.dim_k), th * (es * (4 * a.dim_k + a.dim_v) + 12.0 * a.dim_v), st);
+            return e;
+        });
+        if (e != hipSuccess || all.group == 1 || all.steps == 0) return e;
+        const int64_t n = 2 * (int64_t)all.batch * all.steps * all.heads_k * all.dim_k;
+        const int64_t blocks = (n + 255) / 256 < 4096 ? (n + 255) / 256 : 4096;
+        const ProfSlot ps = prof_slot();
+        PQL_LAUNCH(ps, delta_group_kernel<typename M::E>, dim3((unsigned)blocks), dim3(256), 0, st, all);
+        prof_commit(ps, KID_DELTA_GROUP, 0.0, (double)n * (4.0 * all.group + sizeof(typename M::E)));
+        return hipGetLastError();
+    }
+    static size_t prepare_lds() {
+        const size_t m = 2 * sizeof(Matrix<C>), t = Tile<M, DK, C, true>::BYTES;
+        return m > t ? m : t;
+    }
+    static hipError_t run(const DeltaArgs& a, bool back, hipStream_t st) { return back ? backward(a, st) : forward(a, st); }
+};
+template <typename M> hipError_t chunks_dispatch(const DeltaArgs& a, bool back, bool al, const Plan& p, hipStream_t st) {
+    if (p.c == 32) {
+        if (p.dkp == 64) return al ? Chunked<M, 32, 64, true>::run(a, back, st) : Chunked<M, 32, 64, false>::run(a, back, st);
+        return al ? Chunked<M, 32, 128, true>::run(a, back, st) : Chunked<M, 32, 128, false>::run(a, back, st);
+    }
+    if (p.dkp == 64) return al ? Chunked<M, 64, 64, true>::run(a, back, st) : Chunked<M, 64, 64, false>::run(a, back, st);
+    return al ? Chunked<M, 64, 128, true>::run(a, back, st) : Chunked<M, 64, 128, false>::run(a, back, st);
 }
 void set_saved(DeltaArgs& a, const Plan& p, char* base, bool keep) {
     a.chunks = p.chunks; a.dvp = p.dvp;
@@ -1377,8 +1442,8 @@ int32_t pql_delta_forward(pql_ctx* c, const pql_delta_shape* s, const pql_delta_
     set_saved(a, p, (char*)(saved ? saved : workspace), saved != nullptr);
     const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype) && rows_aligned(in->v, s->dim_v, s->dtype) &&
                     rows_aligned(out, s->dim_v, s->dtype);
-    const hipError_t e = s->dtype == PQL_F32 ? chunks_dispatch<ModeF, false>(a, al, p.dkp, (hipStream_t)stream)
-                                             : chunks_dispatch<ModeB, false>(a, al, p.dkp, (hipStream_t)stream);
+    const hipError_t e = s->dtype == PQL_F32 ? chunks_dispatch<ModeF>(a, false, al, p, (hipStream_t)stream)
+                                             : chunks_dispatch<ModeB>(a, false, al, p, (hipStream_t)stream);
     return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_delta_forward", e);
 }
 
@@ -1407,8 +1472,8 @@ int32_t pql_delta_backward(pql_ctx* c, const pql_delta_shape* s, const pql_delta
     if (a.group > 1) { a.part_q = (float*)(w + p.part_q); a.part_k = (float*)(w + p.part_k); }
     const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype) && rows_aligned(out_grad, s->dim_v, s->dtype) &&
                     rows_aligned(g->v, s->dim_v, s->dtype);
-    const hipError_t e = s->dtype == PQL_F32 ? chunks_dispatch<ModeF, true>(a, al, p.dkp, (hipStream_t)stream)
-                                             : chunks_dispatch<ModeB, true>(a, al, p.dkp, (hipStream_t)stream);
+    const hipError_t e = s->dtype == PQL_F32 ? chunks_dispatch<ModeF>(a, true, al, p, (hipStream_t)stream)
+                                             : chunks_dispatch<ModeB>(a, true, al, p, (hipStream_t)stream);
     return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_delta_backward", e);
 }
 

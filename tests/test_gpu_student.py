@@ -441,3 +441,21 @@ def test_kernels_are_timed_under_their_names(env):
     assert set(names) == {"delta_step_kernel", "delta_prepare_kernel", "delta_scan_kernel", "delta_back_scan_kernel",
                           "delta_back_kernel", "delta_group_kernel"}
     assert all(k["launches"] == 1 and k["total_ms"] > 0 for k in names.values())
+
+
+SHORT = [(3, 32, 2, 4, 64, 64), (2, 31, 1, 2, 128, 96), (5, 17, 1, 1, 72, 36), (2, 16, 3, 3, 20, 130)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size", SHORT)
+def test_windows_of_at_most_32_tokens(env, size, dtype):
+    n, t = size[:2]
+    lens = [t, 0, 1, t - 1, 9][:n]
+    d = Delta(env, *size, dtype=dtype, lengths=lens, resets=[(0, 0), (0, 7), (0, 8), (0, t - 1), (3, 3)], seed=t)
+    out, state = d.want()
+    want = d.want_grads()
+    got = d.forward(True)
+    close(got[0], out, "out")
+    close(got[1], state, "state")
+    for name, x, y in zip(("dq", "dk", "dv", "dg", "dbeta", "dstate"), d.backward(got[2]), want):
+        close(x, y, name)
