@@ -54,21 +54,36 @@ __device__ __forceinline__ void mma(floatx4& c, const FF& a, const FF& b) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
 }
-__device__ __forceinline__ void split3(float x, __bf16& h, __bf16& m, __bf16& l) {
-    h = (__bf16)x;
-    const float r = x - (float)h;
-    m = (__bf16)r;
-    l = (__bf16)(r - (float)m);
+// x = h + m + l exactly: the nearest bf16 (8 bits), the next 8 bits of the rest, and what is left.  Two values at a time,
+// each term of both in one register.
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+struct Split2 { unsigned h, m, l; };
+__device__ __forceinline__ Split2 split2(float x, float y) {
+    Split2 s;
+    s.h = __builtin_bit_cast(unsigned, __builtin_convertvector((floatx2{x, y}), bf16x2));
+    const float rx = x - __uint_as_float(s.h << 16), ry = y - __uint_as_float(s.h & 0xffff0000u);
+    const unsigned mx = __float_as_uint(rx), my = __float_as_uint(ry);
+    s.m = __builtin_amdgcn_perm(my, mx, 0x07060302);
+    const float lx = rx - __uint_as_float(mx & 0xffff0000u), ly = ry - __uint_as_float(my & 0xffff0000u);
+    s.l = __builtin_amdgcn_perm(__float_as_uint(ly), __float_as_uint(lx), 0x07060302);
+    return s;
 }
+typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+// Products for results that are rounded to bf16: the first two terms (16 bits) of what has been computed.
+__device__ __forceinline__ void mma_out(floatx4& c, const F1& a, const F3& b) { c = mm(a.h, b.m, c); c = mm(a.h, b.h, c); }
+__device__ __forceinline__ void mma_out(floatx4& c, const F3& a, const F3& b) { c = mm(a.m, b.h, c); c = mm(a.h, b.m, c); c = mm(a.h, b.h, c); }
+__device__ __forceinline__ void mma_out(floatx4& c, const FF& a, const FF& b) { mma(c, a, b); }
 
 struct ModeB {                              // bf16 tokens
     using E = bf16_t; using X = F1; using Y = F3;
     static constexpr int PLANES = 3, PAD = 8;
     static __device__ __forceinline__ Y computed(const float* x) {
-        F3 f;
+        uintx4 h, m, l;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { __bf16 h, m, l; split3(x[j], h, m, l); f.h[j] = h; f.m[j] = m; f.l[j] = l; }
-        return f;
+        for (int j = 0; j < 4; ++j) { const Split2 s = split2(x[2 * j], x[2 * j + 1]); h[j] = s.h; m[j] = s.m; l[j] = s.l; }
+        return F3{__builtin_bit_cast(bf16x8, h), __builtin_bit_cast(bf16x8, m), __builtin_bit_cast(bf16x8, l)};
     }
     static __device__ __forceinline__ X exact(const float* x) {
         F1 f;
@@ -107,10 +122,8 @@ template <typename M, int ROWS, int COLS, bool EXACT> struct Tile {
             for (int i = 0; i < 4; ++i) h[i] = (__bf16)x[i];
             *(bf16x4*)o = h;
         } else {
-            bf16x4 h, m, l;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { __bf16 a, b, c; split3(x[i], a, b, c); h[i] = a; m[i] = b; l[i] = c; }
-            *(bf16x4*)o = h; *(bf16x4*)(o + ROWS * LD) = m; *(bf16x4*)(o + 2 * ROWS * LD) = l;
+            const Split2 s = split2(x[0], x[1]), t = split2(x[2], x[3]);
+            *(uintx2*)o = uintx2{s.h, t.h}; *(uintx2*)(o + ROWS * LD) = uintx2{s.m, t.m}; *(uintx2*)(o + 2 * ROWS * LD) = uintx2{s.l, t.l};
         }
     }
     __device__ __forceinline__ void put8(int row, int k, const float* x) const {
@@ -126,9 +139,8 @@ template <typename M, int ROWS, int COLS, bool EXACT> struct Tile {
     __device__ __forceinline__ void put1(int row, int k, float x) const {
         E* o = p + row * LD + k;
         if constexpr (PLANES == 3) {
-            __bf16 h, m, l;
-            split3(x, h, m, l);
-            o[0] = h; o[ROWS * LD] = m; o[2 * ROWS * LD] = l;
+            const Split2 s = split2(x, 0.f);
+            *(unsigned short*)o = (unsigned short)s.h; *(unsigned short*)(o + ROWS * LD) = (unsigned short)s.m; *(unsigned short*)(o + 2 * ROWS * LD) = (unsigned short)s.l;
         } else {
             o[0] = (E)x;
         }
@@ -244,6 +256,20 @@ __device__ __forceinline__ Where where_of(const DeltaArgs& a, int bh) {
     w.bh = bh + a.bh0; w.b = w.bh / a.heads_v; w.h = w.bh - w.b * a.heads_v; w.hk = w.h / a.group;
     w.len = a.lengths ? min(max(a.lengths[w.b], 0), a.steps) : a.steps;
     return w;
+}
+// Workgroup `id` of a scan over n (sequence, head) pairs with `blocks` column blocks each.  Workgroups go round the eight XCDs
+// in turn; the blocks of one pair, which read the same q, k, T, P and K^T, are given to one XCD so that its L2 serves all but
+// the first (4 x 2048 tokens, 16 heads: MEASURED).
+__device__ __forceinline__ void place_of(int id, int n, int blocks, int& bh, int& block) {
+    const int whole = n & ~7;
+    if (id < whole * blocks) {
+        const int slot = id >> 3;
+        bh = slot / blocks * 8 + (id & 7);
+        block = slot % blocks;
+    } else {
+        bh = whole + (id - whole * blocks) / blocks;
+        block = (id - whole * blocks) % blocks;
+    }
 }
 template <typename E> __device__ __forceinline__ const E* at(const DeltaSeq& s, int b, int64_t t, int h) {
     return (const E*)s.p + b * s.b + t * s.t + h * s.h;
@@ -446,12 +472,6 @@ template <typename M> __device__ __forceinline__ typename M::X load_operand(cons
         return F1{*(const bf16x8*)p};
     }
 }
-template <typename M> __device__ __forceinline__ typename M::Y load_split(const char* p, unsigned lane_bytes) {
-    if constexpr (M::PLANES == 3)
-        return F3{*(const bf16x8*)(p + lane_bytes), *(const bf16x8*)(p + 1024 + lane_bytes), *(const bf16x8*)(p + 2048 + lane_bytes)};
-    else
-        return load_operand<M>((const float*)(p + 2 * lane_bytes));
-}
 // An operand straight from a token row.
 template <typename M, bool AL> __device__ __forceinline__ typename M::X row_operand(const typename M::E* row, int d, int dim, bool ok) {
     float x[8];
@@ -467,7 +487,12 @@ constexpr int NOWHERE = 0x7ffffffc;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tokens(const char* p) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, 0x40000000, 0x00020000);
 }
-typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void load_ff(__amdgpu_buffer_rsrc_t rs, int lane, int at, FF& f) {
+    const floatx4 a = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rs, lane, at, 0));
+    const floatx4 b = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rs, lane, at + 16, 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f.v[i] = a[i]; f.v[4 + i] = b[i]; }
+}
 // The operands of one wavefront's 16 token rows.
 template <typename M, int C, int DK, bool AL> struct RowOperands {
     using E = typename M::E;
@@ -565,12 +590,12 @@ template <typename M, int C, int NT, bool AL> struct ColumnValues {
 };
 // A 16 x 16 NT tile of results to a padded fp32 array of the library's own, rows r0 + 4 q .. of `ld` floats.
 template <int NT> __device__ __forceinline__ void put_padded(float* base, int r0, int ld, int q, int c0, int c, const floatx4 (&x)[NT]) {
+    const auto rs = tokens((const char*)(base + (int64_t)r0 * ld + c0));
+    const int lane = 4 * (4 * q * ld + c);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        char* p = (char*)(base + (int64_t)(r0 + r) * ld + c0);
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) *(float*)(p + (unsigned)(4 * (4 * q * ld + c + 16 * n))) = x[n][r];
-    }
+        for (int n = 0; n < NT; ++n) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[n][r]), rs, lane, 4 * (r * ld + 16 * n), 0);
 }
 
 template <typename M, int C, int DK, bool AL>
@@ -671,307 +696,379 @@ __global__ __launch_bounds__(4 * C) void delta_prepare_kernel(DeltaArgs a) {
 }
 
 // =============================================================================================
-// Chunks in order: outputs and states, 16 NT columns per workgroup.  Nothing but the state's own chain K S, T X, K^T Y
-// waits for a chunk: all operands of the next one are requested into registers as soon as this one's have been used.
+// Chunks in order: outputs and states, 16 NT columns per workgroup.  Half of the wavefronts (one per SIMD, 16 tokens each)
+// carry the chain K S, X, T X, K^T Y that every chunk has to wait for, the other half what only the outputs need, Q S and
+// P Y, in the gaps of the first.  All operands of a chunk are requested into registers as soon as the previous chunk's
+// have been used.
 // =============================================================================================
 template <typename M, int C, int DK, int NT> struct ScanLds {
     using S = Tile<M, 16 * NT, DK, false>;          // S^T [column][dim_k]
     using X = Tile<M, 16 * NT, C, false>;           // X^T, Y^T, (e o Y)^T [column][token]
     static constexpr int S0 = 0, X0 = S0 + S::BYTES, Y0 = X0 + X::BYTES, Z0 = Y0 + X::BYTES, BYTES = Z0 + X::BYTES;
 };
-template <int THREADS, typename E> __device__ __forceinline__ void zero_rows(const DeltaSeq& s, const Where& w, int from, int to, int c0, int n) {
-    for (int i = threadIdx.x; i < (to - from) * n; i += THREADS) at_out<E>(s, w.b, from + i / n, w.h)[c0 + i % n] = from_float<E>(0.f);
+// By one wavefront.
+template <typename E> __device__ __forceinline__ void zero_rows(const DeltaSeq& s, const Where& w, int from, int to, int c0, int n) {
+    for (int i = threadIdx.x & 63; i < (to - from) * n; i += 64) at_out<E>(s, w.b, from + i / n, w.h)[c0 + i % n] = from_float<E>(0.f);
 }
-// The two blocks of a wavefront's rows of T, P or their transposes.  Blocks that are zero are not there: the other one is
+// The C / 32 blocks of a wavefront's rows of T, P or their transposes.  Blocks that are zero are not there: another one is
 // loaded twice (a load in a branch would make later waits longer) and not used.
 template <typename M, int C, bool TRANSPOSED> __device__ __forceinline__ void load_tri(const void* base, int64_t at_chunk, int wave, int l, typename M::Y (&x)[C / 32]) {
+    const auto rs = tokens((const char*)base + at_chunk * TRI<M, C> * (int)sizeof(typename M::E));
 #pragma unroll
-    for (int ks = 0; ks < C / 32; ++ks)
-    {
+    for (int ks = 0; ks < C / 32; ++ks) {
         const int k = TRANSPOSED ? max(ks, wave / 2) : min(ks, wave / 2);
-        x[ks] = load_split<M>((const char*)base + (at_chunk * TRI<M, C> + (TRANSPOSED ? tri_block_t<C>(wave, k) : tri_block<C>(wave, k)) * BLOCK<M>) * (int)sizeof(typename M::E), 16 * l);
+        const int at = (TRANSPOSED ? tri_block_t<C>(wave, k) : tri_block<C>(wave, k)) * BLOCK<M> * (int)sizeof(typename M::E);
+        if constexpr (M::PLANES == 3) {
+            x[ks].h = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * l, at, 0));
+            x[ks].m = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * l, at + 1024, 0));
+            x[ks].l = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * l, at + 2048, 0));
+        } else {
+            load_ff(rs, 32 * l, at, x[ks]);
+        }
     }
 }
+// The wavefront's strips of K^T or Q^T.
+template <typename M, int C, int RS> __device__ __forceinline__ void load_kt(const void* base, int64_t at, int wave, int l, typename M::X (&x)[RS][C / 32]) {
+    constexpr int ES = sizeof(typename M::E);
+    const auto rs = tokens((const char*)base + at * ES);
+#pragma unroll
+    for (int s = 0; s < RS; ++s)
+#pragma unroll
+        for (int k = 0; k < C / 32; ++k) {
+            const int o = (C / 32 * (wave * RS + s) + k) * 512 * ES;
+            if constexpr (ES == 2) x[s][k].h = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * l, o, 0));
+            else load_ff(rs, 32 * l, o, x[s][k]);
+        }
+}
+struct ChunkGates {                         // of this lane's tokens i0 .. i0 + 3
+    floatx4 gam, end, beta;
+    float last;
+    template <int C> __device__ __forceinline__ void load(const float* G, int64_t at_chunk, int i0) {
+        const auto rs = tokens((const char*)(G + at_chunk * GATES<C>));
+        gam = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rs, 4 * i0, 0, 0));
+        end = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rs, 4 * i0, 4 * C, 0));
+        beta = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rs, 4 * i0, 8 * C, 0));
+        last = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, 0, 12 * C, 0));
+    }
+};
+// The state (or its gradient) of a wavefront: rows 16 (wave RS + s) + 4 q + r, columns c0 + 16 n + c.
+template <int RS, int NT> __device__ __forceinline__ void load_state(const float* p, const Where& w, int wave, int q, int col, int dk, int dv, floatx4 (&S)[RS][NT]) {
+#pragma unroll
+    for (int s = 0; s < RS; ++s)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r0 = 16 * (wave * RS + s) + 4 * q;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                S[s][n][r] = p && r0 + r < dk && col + 16 * n < dv ? p[((int64_t)w.bh * dk + r0 + r) * dv + col + 16 * n] : 0.f;
+        }
+}
+template <int RS, int NT> __device__ __forceinline__ void store_state(float* p, const Where& w, int wave, int q, int col, int dk, int dv, const floatx4 (&S)[RS][NT]) {
+    if (!p) return;
+#pragma unroll
+    for (int s = 0; s < RS; ++s)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r0 = 16 * (wave * RS + s) + 4 * q;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r0 + r < dk && col + 16 * n < dv) p[((int64_t)w.bh * dk + r0 + r) * dv + col + 16 * n] = S[s][n][r];
+        }
+}
 template <typename M, int C, int DK, int NT, bool AL, bool KEEP>
-__global__ __launch_bounds__(4 * C) void delta_scan_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(8 * C) void delta_scan_kernel(DeltaArgs a) {
     using E = typename M::E;
     using L = ScanLds<M, C, DK, NT>;
-    constexpr int RS = DK / C, KS = C / 32, ND = DK / 32;       // 16-row strips of the state per wavefront, contraction steps
+    constexpr int RS = DK / C, KS = C / 32, ND = DK / 32, NW = C / 16;      // 16-row strips of the state per wavefront, contraction steps
     extern __shared__ __align__(16) unsigned char lds[];
     const typename L::S tS(lds + L::S0);
     const typename L::X tX(lds + L::X0), tY(lds + L::Y0), tZ(lds + L::Z0);
-    const Where w = where_of(a, blockIdx.y);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, q = l >> 4, c0 = blockIdx.x * 16 * NT;
+    int bh, block;
+    place_of(blockIdx.x, a.batch * a.heads_v, a.dvp / (16 * NT), bh, block);
+    const Where w = where_of(a, bh);
+    const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all % NW, l = threadIdx.x & 63, c = l & 15, q = l >> 4, c0 = block * 16 * NT;
     const int dk = a.dim_k, dv = a.dim_v, row = 16 * wave + c, i0 = 16 * wave + 4 * q;
     const int chunks = (w.len + C - 1) / C;
     const int64_t first = (int64_t)w.bh * a.chunks;
-    RowOperands<M, C, DK, AL> K(a.k, w, w.hk, dk, row, q), Q(a.q, w, w.hk, dk, row, q);
-    ColumnValues<M, C, NT, AL> V(a.v, w, dv, i0, c0 + c);
-    typename M::X kt[RS][KS];
-    typename M::Y tr[KS], pr[KS];
-    floatx4 gam, end, beta;
-    float last;
-    auto load_gates = [&](int ch) {
-        const char* g = (const char*)(a.G + (first + ch) * GATES<C>);
-        const unsigned at = 4 * i0;
-        gam = *(const floatx4*)(g + at);
-        end = *(const floatx4*)(g + 4 * C + at);
-        beta = *(const floatx4*)(g + 8 * C + at);
-        last = *(const float*)(g + 12 * C);
-    };
-    auto load_kt = [&](int ch) {
-        const char* p = (const char*)((const E*)a.KT + kt_at<E, C>(a, w, ch, DK));
+    ChunkGates G;
+    if (all < NW) {                                 // the chain
+        RowOperands<M, C, DK, AL> K(a.k, w, w.hk, dk, row, q);
+        ColumnValues<M, C, NT, AL> V(a.v, w, dv, i0, c0 + c);
+        typename M::X kt[RS][KS];
+        typename M::Y T[KS];
+        floatx4 S[RS][NT];
+        if (chunks > 0) {
+            K.load(0); V.load(0); G.load<C>(a.G, first, i0);
+            load_tri<M, C, false>(a.T, first, wave, l, T);
+            load_kt<M, C, RS>(a.KT, kt_at<E, C>(a, w, 0, DK), wave, l, kt);
+        }
+        load_state<RS, NT>(a.state, w, wave, q, c0 + c, dk, dv, S);
 #pragma unroll
         for (int s = 0; s < RS; ++s)
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
-                kt[s][k] = load_operand<M>((const E*)(p + (KS * (wave * RS + s) + k) * 512 * (int)sizeof(E) + (unsigned)(l * 8 * (int)sizeof(E))));
-    };
-    auto keep_state = [&](int ch, const floatx4 (&S)[RS][NT]) {
+            for (int n = 0; n < NT; ++n) tS.put4(16 * n + c, 16 * (wave * RS + s) + 4 * q, S[s][n]);
+        for (int ch = 0; ch < chunks; ++ch) {
+            const int next = min(ch + 1, chunks - 1);
+            const int64_t at_chunk = first + ch;
+            __syncthreads();                        // 1: the state is in LDS
+            floatx4 z[NT] = {};
 #pragma unroll
-        for (int s = 0; s < RS; ++s) put_padded<NT>(a.S + (first + ch) * DK * a.dvp, 16 * (wave * RS + s), a.dvp, q, c0, c, S[s]);
-    };
-    if (chunks > 0) {
-        K.load(0); Q.load(0); V.load(0); load_gates(0);
-        load_tri<M, C, false>(a.T, first, wave, l, tr);
-        load_tri<M, C, false>(a.P, first, wave, l, pr);
-        load_kt(0);
-    }
-    floatx4 S[RS][NT];
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-    for (int s = 0; s < RS; ++s)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int col = c0 + 16 * n + c, r0 = 16 * (wave * RS + s) + 4 * q;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                S[s][n][r] = a.state && r0 + r < dk && col < dv ? a.state[((int64_t)w.bh * dk + r0 + r) * dv + col] : 0.f;
-            tS.put4(16 * n + c, r0, S[s][n]);
-        }
-    for (int ch = 0; ch < chunks; ++ch) {
-        const int next = min(ch + 1, chunks - 1);
-        const int64_t at_chunk = first + ch;
-        __syncthreads();                            // the state is in LDS
-        floatx4 z[NT] = {}, o[NT] = {};
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
+                for (int n = 0; n < NT; ++n) mma(z[n], K.f[d], tS.frag(16 * n + c, 32 * d + 8 * q));
+            K.load(next);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const auto f = tS.frag(16 * n + c, 32 * d + 8 * q);
-                mma(z[n], K.f[d], f);
-                mma(o[n], Q.f[d], f);
+                const floatx4 v = V.get(n);
+                floatx4 x;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = v[r] - damp(G.gam[r], z[n][r]);
+                tX.put4(16 * n + c, i0, x);
             }
-        K.load(next); Q.load(next);
+            V.load(next);
+            __syncthreads();                        // 2: X
+            floatx4 rr[NT] = {};
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const floatx4 v = V.get(n);
-            floatx4 x;
+            for (int k = 0; k < KS; ++k) {
+                if (k > wave / 2) break;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) { x[r] = v[r] - damp(gam[r], z[n][r]); o[n][r] = damp(gam[r], o[n][r]); }
-            tX.put4(16 * n + c, i0, x);
-        }
-        V.load(next);
-        if (KEEP) keep_state(ch, S);
-        __syncthreads();
-        floatx4 rr[NT] = {};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            if (k > wave / 2) break;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) mma(rr[n], tr[k], tX.frag(16 * n + c, 32 * k + 8 * q));
-        }
-        load_tri<M, C, false>(a.T, first + next, wave, l, tr);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const floatx4 y = beta * rr[n];
-            tY.put4(16 * n + c, i0, y);
-            tZ.put4(16 * n + c, i0, end * y);
-        }
-        if (KEEP) put_padded<NT>(a.R + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, rr);
-        __syncthreads();
-#pragma unroll
-        for (int s = 0; s < RS; ++s) {
-            const int r0 = 16 * (wave * RS + s);
+                for (int n = 0; n < NT; ++n) mma(rr[n], T[k], tX.frag(16 * n + c, 32 * k + 8 * q));
+            }
+            load_tri<M, C, false>(a.T, first + next, wave, l, T);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                S[s][n] = last == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : S[s][n] * last;
-#pragma unroll
-                for (int k = 0; k < KS; ++k) mma(S[s][n], kt[s][k], tZ.frag(16 * n + c, 32 * k + 8 * q));
-                tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
+                const floatx4 y = G.beta * rr[n];
+                tZ.put4(16 * n + c, i0, G.end * y);
+                tY.put4(16 * n + c, i0, y);
             }
+            const float last = G.last;
+            if (KEEP) {
+#pragma unroll
+                for (int s = 0; s < RS; ++s) put_padded<NT>(a.S + at_chunk * DK * a.dvp, 16 * (wave * RS + s), a.dvp, q, c0, c, S[s]);
+                put_padded<NT>(a.R + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, rr);
+            }
+            __syncthreads();                        // 3: Y; all have read the state
+#pragma unroll
+            for (int s = 0; s < RS; ++s) {
+                const int r0 = 16 * (wave * RS + s);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[s][n][r] = damp(last, S[s][n][r]);
+#pragma unroll
+                    for (int k = 0; k < KS; ++k) mma(S[s][n], kt[s][k], tZ.frag(16 * n + c, 32 * k + 8 * q));
+                    tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
+                }
+            }
+            load_kt<M, C, RS>(a.KT, kt_at<E, C>(a, w, next, DK), wave, l, kt);
+            G.load<C>(a.G, first + next, i0);
         }
-        load_kt(next);
-        load_gates(next);
-        floatx4 o2[NT] = {};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            if (k > wave / 2) break;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) mma(o2[n], pr[k], tY.frag(16 * n + c, 32 * k + 8 * q));
+        store_state<RS, NT>(a.state_out, w, wave, q, c0 + c, dk, dv, S);
+    } else {                                        // the outputs: rounded to the tokens' type, two terms of S, P, Y are enough
+        RowOperands<M, C, DK, AL> Q(a.q, w, w.hk, dk, row, q);
+        typename M::Y P[KS];
+        if (chunks > 0) {
+            Q.load(0); G.load<C>(a.G, first, i0);
+            load_tri<M, C, false>(a.P, first, wave, l, P);
         }
-        load_tri<M, C, false>(a.P, first + next, wave, l, pr);
+        for (int ch = 0; ch < chunks; ++ch) {
+            const int next = min(ch + 1, chunks - 1);
+            __syncthreads();                        // 1
+            floatx4 o[NT] = {};
 #pragma unroll
-        for (int n = 0; n < NT; ++n) o[n] = a.scale * (o[n] + o2[n]);
-        ColumnValues<M, C, NT, AL>::put(a.out, w, a.steps, dv, ch, i0, c0 + c, o);
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma_out(o[n], Q.f[d], tS.frag(16 * n + c, 32 * d + 8 * q));
+            Q.load(next);
+            __syncthreads();                        // 2
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[n][r] = damp(G.gam[r], o[n][r]);
+            G.load<C>(a.G, first + next, i0);
+            __syncthreads();                        // 3
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                if (k > wave / 2) break;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma_out(o[n], P[k], tY.frag(16 * n + c, 32 * k + 8 * q));
+            }
+            load_tri<M, C, false>(a.P, first + next, wave, l, P);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[n] *= a.scale;
+            ColumnValues<M, C, NT, AL>::put(a.out, w, a.steps, dv, ch, i0, c0 + c, o);
+        }
+        const int n = min(16 * NT, dv - c0);
+        if (n > 0 && a.steps > chunks * C && all == NW) zero_rows<E>(a.out, w, chunks * C, a.steps, c0, n);
     }
-    const int n = min(16 * NT, dv - c0);
-    if (n > 0 && a.steps > chunks * C) zero_rows<4 * C, E>(a.out, w, chunks * C, a.steps, c0, n);
-    if (!a.state_out) return;
-#pragma unroll
-    for (int s = 0; s < RS; ++s)
-#pragma unroll
-        for (int m = 0; m < NT; ++m) {
-            const int col = c0 + 16 * m + c, r0 = 16 * (wave * RS + s) + 4 * q;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (r0 + r < dk && col < dv) a.state_out[((int64_t)w.bh * dk + r0 + r) * dv + col] = S[s][m][r];
-        }
 }
 
 // =============================================================================================
-// Gradient, chunks in reverse order: dV, and what delta_back_kernel needs of every chunk (dS1, dY, dX).
+// Gradient, chunks in reverse order: dV, and what delta_back_kernel needs of every chunk (dS1, dX, dY).  Again half of the
+// wavefronts carry the chain K dS, dY, T^T dR, K^T dX; the other half find what it adds from outside, P^T dO and
+// Q^T (gam o dO), one chunk ahead, and hand it over in LDS in the layout of the results.
 // =============================================================================================
 template <typename M, int C, int DK, int NT> struct BackScanLds {
     using S = Tile<M, 16 * NT, DK, false>;          // dS^T [column][dim_k]
     using O = Tile<M, 16 * NT, C, true>;            // dO^T [column][token]
     using X = Tile<M, 16 * NT, C, false>;           // dR^T, (gam o dX)^T, (gam o dO)^T [column][token]
-    static constexpr int S0 = 0, O0 = S0 + S::BYTES, X0 = O0 + O::BYTES, Y0 = X0 + X::BYTES, Z0 = Y0 + X::BYTES, BYTES = Z0 + X::BYTES;
+    static constexpr int S0 = 0, O0 = S0 + S::BYTES, X0 = O0 + O::BYTES, Y0 = X0 + X::BYTES, G0 = Y0 + X::BYTES, P0 = G0 + X::BYTES,
+                         Q0 = P0 + C * 16 * NT * 4, BYTES = Q0 + DK * 16 * NT * 4;      // P0, Q0: results of P^T dO, Q^T (gam o dO)
 };
 template <typename M, int C, int DK, int NT, bool AL>
-__global__ __launch_bounds__(4 * C) void delta_back_scan_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(8 * C) void delta_back_scan_kernel(DeltaArgs a) {
     using E = typename M::E;
     using L = BackScanLds<M, C, DK, NT>;
-    constexpr int RS = DK / C, KS = C / 32, ND = DK / 32;
+    constexpr int RS = DK / C, KS = C / 32, ND = DK / 32, NW = C / 16;
     extern __shared__ __align__(16) unsigned char lds[];
     const typename L::S tS(lds + L::S0);
     const typename L::O tO(lds + L::O0);
-    const typename L::X tR(lds + L::X0), tX(lds + L::Y0), tG(lds + L::Z0);
-    const Where w = where_of(a, blockIdx.y);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, q = l >> 4, c0 = blockIdx.x * 16 * NT;
+    const typename L::X tR(lds + L::X0), tX(lds + L::Y0), tG(lds + L::G0);
+    int bh, block;
+    place_of(blockIdx.x, a.batch * a.heads_v, a.dvp / (16 * NT), bh, block);
+    const Where w = where_of(a, bh);
+    const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all % NW, l = threadIdx.x & 63, c = l & 15, q = l >> 4, c0 = block * 16 * NT;
+    floatx4* const tP = (floatx4*)(lds + L::P0) + wave * NT * 64 + l;               // [n * 64]
+    floatx4* const tQ = (floatx4*)(lds + L::Q0) + wave * RS * NT * 64 + l;          // [(s * NT + n) * 64]
     const int dk = a.dim_k, dv = a.dim_v, row = 16 * wave + c, i0 = 16 * wave + 4 * q;
     const int chunks = (w.len + C - 1) / C;
     const int64_t first = (int64_t)w.bh * a.chunks;
-    RowOperands<M, C, DK, AL> K(a.k, w, w.hk, dk, row, q);
-    ColumnValues<M, C, NT, AL> O(a.out_grad, w, dv, i0, c0 + c);
-    typename M::X kt[RS][KS], qt[RS][KS];
-    typename M::Y tr[KS], pr[KS];
-    floatx4 go[NT], gam, end, beta;
-    float last;
-    auto load_gates = [&](int ch) {
-        const char* g = (const char*)(a.G + (first + ch) * GATES<C>);
-        const unsigned at = 4 * i0;
-        gam = *(const floatx4*)(g + at);
-        end = *(const floatx4*)(g + 4 * C + at);
-        beta = *(const floatx4*)(g + 8 * C + at);
-        last = *(const float*)(g + 12 * C);
-    };
-    auto load_kt = [&](int ch) {
-        const int64_t o = kt_at<E, C>(a, w, ch, DK);
+    ChunkGates G;
+    if (all < NW) {                                 // the chain
+        RowOperands<M, C, DK, AL> K(a.k, w, w.hk, dk, row, q);
+        typename M::X kt[RS][KS];
+        typename M::Y T[KS];
+        floatx4 S[RS][NT];
+        if (chunks > 0) {
+            K.load(chunks - 1); G.load<C>(a.G, first + chunks - 1, i0);
+            load_tri<M, C, true>(a.TT, first + chunks - 1, wave, l, T);
+            load_kt<M, C, RS>(a.KT, kt_at<E, C>(a, w, chunks - 1, DK), wave, l, kt);
+        }
+        load_state<RS, NT>(a.state_grad, w, wave, q, c0 + c, dk, dv, S);
 #pragma unroll
         for (int s = 0; s < RS; ++s)
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const int blk = (KS * (wave * RS + s) + k) * 512 * (int)sizeof(E);
-                const unsigned lane = l * 8 * (int)sizeof(E);
-                kt[s][k] = load_operand<M>((const E*)((const char*)((const E*)a.KT + o) + blk + lane));
-                qt[s][k] = load_operand<M>((const E*)((const char*)((const E*)a.QT + o) + blk + lane));
-            }
-    };
-    if (chunks > 0) {
-        O.load(chunks - 1); K.load(chunks - 1); load_gates(chunks - 1);
-        load_tri<M, C, true>(a.PT, first + chunks - 1, wave, l, pr);
-        load_tri<M, C, true>(a.TT, first + chunks - 1, wave, l, tr);
-        load_kt(chunks - 1);
-    }
-    floatx4 S[RS][NT];
+            for (int n = 0; n < NT; ++n) tS.put4(16 * n + c, 16 * (wave * RS + s) + 4 * q, S[s][n]);
+        if (chunks > 0) __syncthreads();            // 0: the helpers' dO
+        for (int ch = chunks - 1; ch >= 0; --ch) {
+            const int next = max(ch - 1, 0);
+            const int64_t at_chunk = first + ch;
+            __syncthreads();                        // 1: dS, P^T dO, Q^T (gam o dO)
+            floatx4 y[NT] = {}, gq[RS][NT];
 #pragma unroll
-    for (int s = 0; s < RS; ++s)
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int col = c0 + 16 * n + c, r0 = 16 * (wave * RS + s) + 4 * q;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                S[s][n][r] = a.state_grad && r0 + r < dk && col < dv ? a.state_grad[((int64_t)w.bh * dk + r0 + r) * dv + col] : 0.f;
-            tS.put4(16 * n + c, r0, S[s][n]);
-        }
-    if (chunks > 0) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) { go[n] = O.get(n); tO.put4(16 * n + c, i0, go[n]); }
-    }
-    for (int ch = chunks - 1; ch >= 0; --ch) {
-        const int next = max(ch - 1, 0);
-        const int64_t at_chunk = first + ch;
-        __syncthreads();                            // dS and dO are in LDS
-        O.load(next);
-        floatx4 y1[NT] = {}, y2[NT] = {};
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) mma(y1[n], K.f[d], tS.frag(16 * n + c, 32 * d + 8 * q));
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            if (k < wave / 2) continue;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) mma(y2[n], pr[k], tO.frag(16 * n + c, 32 * k + 8 * q));
-        }
-        K.load(next);
-        load_tri<M, C, true>(a.PT, first + next, wave, l, pr);
-        floatx4 dy[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) dy[n][r] = a.scale * y2[n][r] + damp(end[r], y1[n][r]);
-            tR.put4(16 * n + c, i0, beta * dy[n]);
-            tG.put4(16 * n + c, i0, a.scale * gam * go[n]);
-        }
-        put_padded<NT>(a.dY + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, dy);
-#pragma unroll
-        for (int s = 0; s < RS; ++s) put_padded<NT>(a.dS + at_chunk * DK * a.dvp, 16 * (wave * RS + s), a.dvp, q, c0, c, S[s]);
-        __syncthreads();
-        floatx4 dx[NT] = {};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            if (k < wave / 2) continue;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) mma(dx[n], tr[k], tR.frag(16 * n + c, 32 * k + 8 * q));
-        }
-        load_tri<M, C, true>(a.TT, first + next, wave, l, tr);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) tX.put4(16 * n + c, i0, -gam * dx[n]);
-        put_padded<NT>(a.dX + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, dx);
-        ColumnValues<M, C, NT, AL>::put(a.dv, w, a.steps, dv, ch, i0, c0 + c, dx);
-        __syncthreads();
-#pragma unroll
-        for (int s = 0; s < RS; ++s) {
-            const int r0 = 16 * (wave * RS + s);
+                for (int n = 0; n < NT; ++n) mma(y[n], K.f[d], tS.frag(16 * n + c, 32 * d + 8 * q));
+            K.load(next);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                S[s][n] = last == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : S[s][n] * last;
+                const floatx4 p = tP[n * 64];
 #pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    mma(S[s][n], kt[s][k], tX.frag(16 * n + c, 32 * k + 8 * q));
-                    mma(S[s][n], qt[s][k], tG.frag(16 * n + c, 32 * k + 8 * q));
-                }
-                tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
+                for (int r = 0; r < 4; ++r) y[n][r] = a.scale * p[r] + damp(G.end[r], y[n][r]);
+                tR.put4(16 * n + c, i0, G.beta * y[n]);
             }
-        }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) { go[n] = O.get(n); tO.put4(16 * n + c, i0, go[n]); }
-        load_kt(next);
-        load_gates(next);
+            for (int s = 0; s < RS; ++s)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) gq[s][n] = tQ[(s * NT + n) * 64];
+            __syncthreads();                        // 2: dR; P^T dO and Q^T (gam o dO) are taken
+            put_padded<NT>(a.dY + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, y);
+#pragma unroll
+            for (int s = 0; s < RS; ++s) put_padded<NT>(a.dS + at_chunk * DK * a.dvp, 16 * (wave * RS + s), a.dvp, q, c0, c, S[s]);
+            floatx4 dx[NT] = {};
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                if (k < wave / 2) continue;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma(dx[n], T[k], tR.frag(16 * n + c, 32 * k + 8 * q));
+            }
+            load_tri<M, C, true>(a.TT, first + next, wave, l, T);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) tX.put4(16 * n + c, i0, -G.gam * dx[n]);
+            const float last = G.last;
+            __syncthreads();                        // 3: dX; all have read dS
+#pragma unroll
+            for (int s = 0; s < RS; ++s) {
+                const int r0 = 16 * (wave * RS + s);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[s][n][r] = damp(last, S[s][n][r]) + gq[s][n][r];
+#pragma unroll
+                    for (int k = 0; k < KS; ++k) mma(S[s][n], kt[s][k], tX.frag(16 * n + c, 32 * k + 8 * q));
+                    tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
+                }
+            }
+            load_kt<M, C, RS>(a.KT, kt_at<E, C>(a, w, next, DK), wave, l, kt);
+            G.load<C>(a.G, first + next, i0);
+            put_padded<NT>(a.dX + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, dx);
+            ColumnValues<M, C, NT, AL>::put(a.dv, w, a.steps, dv, ch, i0, c0 + c, dx);
+        }
+        store_state<RS, NT>(a.dstate, w, wave, q, c0 + c, dk, dv, S);
+    } else {                                        // P^T dO and Q^T (gam o dO), a chunk ahead of the chain
+        ColumnValues<M, C, NT, AL> O(a.out_grad, w, dv, i0, c0 + c);
+        typename M::X qt[RS][KS];
+        typename M::Y P[KS];
+        auto load = [&](int ch) {
+            load_tri<M, C, true>(a.PT, first + ch, wave, l, P);
+            load_kt<M, C, RS>(a.QT, kt_at<E, C>(a, w, ch, DK), wave, l, qt);
+        };
+        auto put = [&] {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const floatx4 o = O.get(n);
+                tO.put4(16 * n + c, i0, o);
+                tG.put4(16 * n + c, i0, a.scale * G.gam * o);
+            }
+        };
+        floatx4 p[NT], g[RS][NT];
+        auto products = [&] {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                p[n] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+                    if (k >= wave / 2) mma(p[n], P[k], tO.frag(16 * n + c, 32 * k + 8 * q));
+#pragma unroll
+                for (int s = 0; s < RS; ++s) {
+                    g[s][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = 0; k < KS; ++k) mma(g[s][n], qt[s][k], tG.frag(16 * n + c, 32 * k + 8 * q));
+                }
+            }
+        };
+        auto hand_over = [&] {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                tP[n * 64] = p[n];
+#pragma unroll
+                for (int s = 0; s < RS; ++s) tQ[(s * NT + n) * 64] = g[s][n];
+            }
+        };
+        if (chunks > 0) {
+            O.load(chunks - 1); G.load<C>(a.G, first + chunks - 1, i0);
+            load(chunks - 1);
+            put();
+            O.load(max(chunks - 2, 0)); G.load<C>(a.G, first + max(chunks - 2, 0), i0);
+            __syncthreads();                        // 0
+            products();
+            hand_over();
+            load(max(chunks - 2, 0));
+        }
+        for (int ch = chunks - 1; ch >= 0; --ch) {  // the chunk before `ch` here
+            const int after = max(ch - 2, 0);
+            __syncthreads();                        // 1: dO of the last chunk has been used
+            put();
+            O.load(after); G.load<C>(a.G, first + after, i0);
+            __syncthreads();                        // 2: the new dO is there
+            products();
+            load(after);
+            __syncthreads();                        // 3: and what was handed over before has been taken
+            hand_over();
+        }
+        const int n = min(16 * NT, dv - c0);
+        if (n > 0 && a.steps > chunks * C && all == NW) zero_rows<E>(a.dv, w, chunks * C, a.steps, c0, n);
     }
-    const int n = min(16 * NT, dv - c0);
-    if (n > 0 && a.steps > chunks * C) zero_rows<4 * C, E>(a.dv, w, chunks * C, a.steps, c0, n);
-    if (!a.dstate) return;
-#pragma unroll
-    for (int s = 0; s < RS; ++s)
-#pragma unroll
-        for (int m = 0; m < NT; ++m) {
-            const int col = c0 + 16 * m + c, r0 = 16 * (wave * RS + s) + 4 * q;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (r0 + r < dk && col < dv) a.dstate[((int64_t)w.bh * dk + r0 + r) * dv + col] = S[s][m][r];
-        }
 }
 
 // =============================================================================================
@@ -1344,7 +1441,7 @@ template <typename M, int C, int DK, bool AL> struct Chunked {
                            th * 4.0 * C * a.dim_k, th * (2 * es * a.dim_k + 8.0 * C), st);
             if (e != hipSuccess) return e;
             auto scan = [&](auto kernel, LdsLimit& lim, int nt, size_t lds) {
-                return launch(kernel, lim, lds, dim3(a.dvp / (16 * nt), a.batch * a.heads_v), 4 * C, a, KID_DELTA_SCAN, flops, bytes, st);
+                return launch(kernel, lim, lds, dim3(a.dvp / (16 * nt) * a.batch * a.heads_v), 8 * C, a, KID_DELTA_SCAN, flops, bytes, st);
             };
             if (narrow(a)) return a.S ? scan(delta_scan_kernel<M, C, DK, 1, AL, true>, lim[0], 1, ScanLds<M, C, DK, 1>::BYTES)
                                       : scan(delta_scan_kernel<M, C, DK, 1, AL, false>, lim[1], 1, ScanLds<M, C, DK, 1>::BYTES);
@@ -1358,9 +1455,9 @@ template <typename M, int C, int DK, bool AL> struct Chunked {
             const double th = token_heads(a), es = sizeof(typename M::E);
             const double flops = th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, bytes = th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C + 8.0 * a.dim_v);
             hipError_t e = narrow(a) ? launch(delta_back_scan_kernel<M, C, DK, 1, AL>, l_narrow, BackScanLds<M, C, DK, 1>::BYTES,
-                                              dim3(a.dvp / 16, a.batch * a.heads_v), 4 * C, a, KID_DELTA_BACK_SCAN, flops, bytes, st)
+                                              dim3(a.dvp / 16 * a.batch * a.heads_v), 8 * C, a, KID_DELTA_BACK_SCAN, flops, bytes, st)
                                      : launch(delta_back_scan_kernel<M, C, DK, 2, AL>, l_scan, BackScanLds<M, C, DK, 2>::BYTES,
-                                              dim3(a.dvp / 32, a.batch * a.heads_v), 4 * C, a, KID_DELTA_BACK_SCAN, flops, bytes, st);
+                                              dim3(a.dvp / 32 * a.batch * a.heads_v), 8 * C, a, KID_DELTA_BACK_SCAN, flops, bytes, st);
             if (e == hipSuccess && a.chunks > 0)
                 e = launch(delta_back_kernel<M, C, DK, AL>, l_back, BackLds<M, C, DK>::BYTES, dim3(a.chunks, a.batch * a.heads_v), 8 * C, a, KID_DELTA_BACK,
                            th * (6.0 * a.dim_k * a.dim_v + 4.0 * C * a.dim_v + 8.0 * C * a.dim_k), th * (es * (4 * a.dim_k + a.dim_v) + 12.0 * a.dim_v), st);
