@@ -71,10 +71,34 @@ __device__ __forceinline__ Split2 split2(float x, float y) {
 }
 typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+// A sum of products on a chain that others wait for: independent accumulators by the size of the terms, joined at the end.
+struct Acc {
+    floatx4 a[3] = {};
+    __device__ __forceinline__ void add(const F1& x, const F3& y) { a[2] = mm(x.h, y.l, a[2]); a[1] = mm(x.h, y.m, a[1]); a[0] = mm(x.h, y.h, a[0]); }
+    __device__ __forceinline__ void add(const F3& x, const F1& y) { a[2] = mm(x.l, y.h, a[2]); a[1] = mm(x.m, y.h, a[1]); a[0] = mm(x.h, y.h, a[0]); }
+    __device__ __forceinline__ void add(const F3& x, const F3& y) {
+        a[2] = mm(x.l, y.h, a[2]); a[1] = mm(x.m, y.h, a[1]); a[0] = mm(x.h, y.h, a[0]);
+        a[2] = mm(x.h, y.l, a[2]); a[1] = mm(x.h, y.m, a[1]); a[2] = mm(x.m, y.m, a[2]);
+    }
+    __device__ __forceinline__ void add(const FF& x, const FF& y) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) a[j & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.v[j], y.v[j], a[j & 1], 0, 0, 0);
+    }
+    __device__ __forceinline__ floatx4 sum() const { return a[2] + a[1] + a[0]; }
+};
 // Products for results that are rounded to bf16: the first two terms (16 bits) of what has been computed.
 __device__ __forceinline__ void mma_out(floatx4& c, const F1& a, const F3& b) { c = mm(a.h, b.m, c); c = mm(a.h, b.h, c); }
 __device__ __forceinline__ void mma_out(floatx4& c, const F3& a, const F3& b) { c = mm(a.m, b.h, c); c = mm(a.h, b.m, c); c = mm(a.h, b.h, c); }
 __device__ __forceinline__ void mma_out(floatx4& c, const FF& a, const FF& b) { mma(c, a, b); }
+
+// Results of matrix instructions must not be read for some cycles.  The compiler sees to that, but not on every path where
+// branches lie between (a short side of a branch is missed when a long one has been looked at first; a result was read too
+// early that way): behind products in branches all results are waited for, and nothing is moved across.
+__device__ __forceinline__ void settle() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 3");
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 struct ModeB {                              // bf16 tokens
     using E = bf16_t; using X = F1; using Y = F3;
@@ -156,6 +180,13 @@ template <typename M, int ROWS, int COLS, bool EXACT> struct Tile {
             for (int i = 0; i < 4; ++i) x[i] = (float)h[i];
         }
         return x;
+    }
+    // the operands of N 16-row tiles (rows row + 16 n) over K steps of 32, all requested at once
+    template <int K, int N, typename F> __device__ __forceinline__ void frags(int row, int k, F (&f)[K][N]) const {
+#pragma unroll
+        for (int d = 0; d < K; ++d)
+#pragma unroll
+            for (int n = 0; n < N; ++n) f[d][n] = frag(row + 16 * n, k + 32 * d);
     }
     __device__ __forceinline__ auto frag(int row, int k) const {
         const E* o = p + row * LD + k;
@@ -436,9 +467,11 @@ template <int C> __device__ __forceinline__ void invert(const Matrix<C>& m, Matr
 #pragma unroll
             for (int s = 0; s < 4; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(r[s], col[k][s], acc, 0, 0, 0);
         }
+        settle();
         const floatx4 r = *(const floatx4*)&t.v[16 * i + c][16 * i + 4 * q];
 #pragma unroll
         for (int s = 0; s < 4; ++s) o = __builtin_amdgcn_mfma_f32_16x16x4f32(r[s], acc[s], o, 0, 0, 0);
+        settle();
         col[i] = -o;
 #pragma unroll
         for (int s = 0; s < 4; ++s) t.v[16 * i + 4 * q + s][16 * w + c] = -o[s];
@@ -474,9 +507,15 @@ template <typename M> __device__ __forceinline__ typename M::X load_operand(cons
 }
 // An operand straight from a token row.
 template <typename M, bool AL> __device__ __forceinline__ typename M::X row_operand(const typename M::E* row, int d, int dim, bool ok) {
-    float x[8];
-    load8<typename M::E, AL>(row, d, dim, ok, x);
-    return M::exact(x);
+    if constexpr (AL && sizeof(typename M::E) == 2) {
+        F1 f = {};
+        if (ok && d < dim) f.h = *(const bf16x8*)(row + d);
+        return f;
+    } else {
+        float x[8];
+        load8<typename M::E, AL>(row, d, dim, ok, x);
+        return M::exact(x);
+    }
 }
 
 // Token tensors of a loop over chunks.  AL (aligned rows, strides that keep a chunk's offsets below 2^30 bytes): through
@@ -493,63 +532,58 @@ __device__ __forceinline__ void load_ff(__amdgpu_buffer_rsrc_t rs, int lane, int
 #pragma unroll
     for (int i = 0; i < 4; ++i) { f.v[i] = a[i]; f.v[4 + i] = b[i]; }
 }
+// Everything a loop over chunks reads or writes walks with it: a scalar pointer that is moved by one chunk (C tokens, in the
+// direction of the loop), lane offsets that do not change.  `go(false)` stays: the last chunk is requested twice.
 // The operands of one wavefront's 16 token rows.
 template <typename M, int C, int DK, bool AL> struct RowOperands {
     using E = typename M::E;
     static constexpr int ND = DK / 32, ES = sizeof(E);
-    const char* base;                       // token 0
-    int64_t stride;                         // bytes
-    int len, dk, row, q;
+    const char* p;
+    int64_t step, stride;
+    int left, turn, dk, row, q, lane;       // tokens from this chunk on, C or -C
     typename M::X f[ND];
-    __device__ __forceinline__ RowOperands(const DeltaSeq& s, const Where& w, int h, int dk_, int row_, int q_)
-        : base((const char*)at<E>(s, w.b, 0, h)), stride(s.t * (int64_t)ES), len(w.len), dk(dk_), row(row_), q(q_) {}
-    __device__ __forceinline__ void load(int ch) {
-        const char* p = base + (int64_t)ch * C * stride;
-        const bool ok = ch * C + row < len;
+    __device__ __forceinline__ RowOperands(const DeltaSeq& s, const Where& w, int h, int dk_, int row_, int q_, int ch, int dir)
+        : p((const char*)at<E>(s, w.b, (int64_t)ch * C, h)), step(dir * C * s.t * (int64_t)ES), stride(s.t * (int64_t)ES), left(w.len - ch * C), turn(dir * C), dk(dk_),
+          row(row_), q(q_), lane(AL ? row_ * ((int)s.t * ES) + 8 * q_ * ES : 0) {}
+    __device__ __forceinline__ void load() {
+        const bool ok = row < left;
         if constexpr (AL) {
             const auto r = tokens(p);
-            const int off = row * (int)stride + 8 * q * ES;
 #pragma unroll
             for (int d = 0; d < ND; ++d) {
-                const int o = ok && 32 * d + 8 * q < dk ? off : NOWHERE - 32 * d * ES;
-                const uintx4 x = __builtin_amdgcn_raw_buffer_load_b128(r, o + 32 * d * ES, 0, 0);
-                if constexpr (ES == 2) {
-                    f[d].h = __builtin_bit_cast(bf16x8, x);
-                } else {
-                    const floatx4 lo = __builtin_bit_cast(floatx4, x);
-                    const floatx4 hi = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(r, o + 32 * d * ES + (ok && 32 * d + 8 * q < dk ? 16 : 0), 0, 0));
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) { f[d].v[i] = lo[i]; f[d].v[4 + i] = hi[i]; }
-                }
+                const int o = ok && 32 * d + 8 * q < dk ? lane + 32 * d * ES : NOWHERE - 16;
+                if constexpr (ES == 2) f[d].h = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0));
+                else load_ff(r, o, 0, f[d]);
             }
         } else {
 #pragma unroll
             for (int d = 0; d < ND; ++d) f[d] = row_operand<M, false>((const E*)(p + row * stride), 32 * d + 8 * q, dk, ok);
         }
     }
+    __device__ __forceinline__ void go(bool more) { p += more ? step : 0; left -= more ? turn : 0; }
 };
-// The same for results laid out as [4 tokens][column]: element (i0 + r, col + 16 n).
+// Token tensors in the layout of results, [4 tokens][column]: element (i0 + r, col + 16 n).
 template <typename M, int C, int NT, bool AL> struct ColumnValues {
     using E = typename M::E;
     static constexpr int ES = sizeof(E);
-    const char* base;
-    int64_t stride;
-    int len, dim, i0, col;
+    const char* p;
+    int64_t step, stride;
+    int left, turn, dim, i0, col, lane;
     unsigned raw[NT][4];
-    __device__ __forceinline__ ColumnValues(const DeltaSeq& s, const Where& w, int dim_, int i0_, int col_)
-        : base((const char*)at<E>(s, w.b, 0, w.h)), stride(s.t * (int64_t)ES), len(w.len), dim(dim_), i0(i0_), col(col_) {}
-    __device__ __forceinline__ void load(int ch) {
-        const char* p = base + (int64_t)ch * C * stride;
+    __device__ __forceinline__ ColumnValues(const DeltaSeq& s, const Where& w, int dim_, int i0_, int col_, int ch, int dir)
+        : p((const char*)at<E>(s, w.b, (int64_t)ch * C, w.h)), step(dir * C * s.t * (int64_t)ES), stride(s.t * (int64_t)ES), left(w.len - ch * C),
+          turn(dir * C), dim(dim_), i0(i0_), col(col_), lane(AL ? i0_ * ((int)s.t * ES) + col_ * ES : 0) {}
+    __device__ __forceinline__ void load() {
         const auto rs = tokens(p);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const bool ok = ch * C + i0 + r < len && col + 16 * n < dim;
+                const bool ok = i0 + r < left && col + 16 * n < dim;
                 if constexpr (AL) {
-                    const int o = ok ? (i0 + r) * (int)stride + (col + 16 * n) * ES : NOWHERE;
-                    if constexpr (ES == 2) raw[n][r] = (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, o, 0, 0);
-                    else raw[n][r] = __builtin_amdgcn_raw_buffer_load_b32(rs, o, 0, 0);
+                    const int o = ok ? lane + 16 * n * ES : NOWHERE;
+                    if constexpr (ES == 2) raw[n][r] = (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, o, r * (int)stride, 0);
+                    else raw[n][r] = __builtin_amdgcn_raw_buffer_load_b32(rs, o, r * (int)stride, 0);
                 } else {
                     raw[n][r] = ok ? bits(*(const E*)(p + (i0 + r) * stride + (int64_t)(col + 16 * n) * ES)) : 0u;
                 }
@@ -565,37 +599,43 @@ template <typename M, int C, int NT, bool AL> struct ColumnValues {
         for (int r = 0; r < 4; ++r) x[r] = __uint_as_float(ES == 2 ? raw[n][r] << 16 : raw[n][r]);
         return x;
     }
-    // writes them; rows behind the length are zeros, rows behind `steps` are not there
-    static __device__ __forceinline__ void put(const DeltaSeq& s, const Where& w, int steps, int dim, int ch, int i0, int col, const floatx4 (&x)[NT]) {
-        char* p = (char*)at_out<E>(s, w.b, (int64_t)ch * C, w.h);
-        const int64_t stride = s.t * (int64_t)ES;
+    // Writes x to the first `there` rows; rows behind the sequence's length are zeros.
+    __device__ __forceinline__ void put(int there, const floatx4 (&x)[NT]) const {
+        char* o8 = const_cast<char*>(p);
         const auto rs = tokens(p);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const bool ok = ch * C + i0 + r < steps && col + 16 * n < dim;
-                const unsigned v = bits(from_float<E>(ch * C + i0 + r < w.len ? x[n][r] : 0.f));
+                const bool ok = i0 + r < there && col + 16 * n < dim;
+                const unsigned v = bits(from_float<E>(i0 + r < left ? x[n][r] : 0.f));
                 if constexpr (AL) {
-                    const int o = ok ? (i0 + r) * (int)stride + (col + 16 * n) * ES : NOWHERE;
-                    if constexpr (ES == 2) __builtin_amdgcn_raw_buffer_store_b16((unsigned short)v, rs, o, 0, 0);
-                    else __builtin_amdgcn_raw_buffer_store_b32(v, rs, o, 0, 0);
+                    const int o = ok ? lane + 16 * n * ES : NOWHERE;
+                    if constexpr (ES == 2) __builtin_amdgcn_raw_buffer_store_b16((unsigned short)v, rs, o, r * (int)stride, 0);
+                    else __builtin_amdgcn_raw_buffer_store_b32(v, rs, o, r * (int)stride, 0);
                 } else if (ok) {
-                    char* o = p + (i0 + r) * stride + (int64_t)(col + 16 * n) * ES;
+                    char* o = o8 + (i0 + r) * stride + (int64_t)(col + 16 * n) * ES;
                     if constexpr (ES == 2) *(unsigned short*)o = (unsigned short)v;
                     else *(unsigned*)o = v;
                 }
             }
     }
+    __device__ __forceinline__ void go(bool more) { p += more ? step : 0; left -= more ? turn : 0; }
 };
-// A 16 x 16 NT tile of results to a padded fp32 array of the library's own, rows r0 + 4 q .. of `ld` floats.
-template <int NT> __device__ __forceinline__ void put_padded(float* base, int r0, int ld, int q, int c0, int c, const floatx4 (&x)[NT]) {
-    const auto rs = tokens((const char*)(base + (int64_t)r0 * ld + c0));
-    const int lane = 4 * (4 * q * ld + c);
+// An array of the library's own with a fixed number of bytes per chunk.
+struct Chunks {
+    const char* p;
+    int64_t step;
+    __device__ __forceinline__ Chunks(const void* base, int64_t first, int64_t bytes, int ch, int dir) : p((const char*)base + (first + ch) * bytes), step(dir * bytes) {}
+    __device__ __forceinline__ void go(bool more) { p += more ? step : 0; }
+};
+// Results to a padded fp32 array, rows r0 + 4 q + r (lane = the byte offset of row 4 q plus the wavefront's and lane's column).
+template <int NT> __device__ __forceinline__ void put_padded(const char* p, int lane, int r0, int ld4, const floatx4 (&x)[NT]) {
+    const auto rs = tokens(p);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[n][r]), rs, lane, 4 * (r * ld + 16 * n), 0);
+        for (int n = 0; n < NT; ++n) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[n][r]), rs, lane, (r0 + r) * ld4 + 64 * n, 0);
 }
 
 template <typename M, int C, int DK, bool AL>
@@ -644,6 +684,7 @@ __global__ __launch_bounds__(4 * C) void delta_prepare_kernel(DeltaArgs a) {
             mma(qk[n], fq, f);
         }
     }
+    settle();
     __syncthreads();                        // gates are there
 #pragma unroll
     for (int n = 0; n < NW; ++n) {
@@ -710,27 +751,28 @@ template <typename M, int C, int DK, int NT> struct ScanLds {
 template <typename E> __device__ __forceinline__ void zero_rows(const DeltaSeq& s, const Where& w, int from, int to, int c0, int n) {
     for (int i = threadIdx.x & 63; i < (to - from) * n; i += 64) at_out<E>(s, w.b, from + i / n, w.h)[c0 + i % n] = from_float<E>(0.f);
 }
-// The C / 32 blocks of a wavefront's rows of T, P or their transposes.  Blocks that are zero are not there: another one is
-// loaded twice (a load in a branch would make later waits longer) and not used.
-template <typename M, int C, bool TRANSPOSED> __device__ __forceinline__ void load_tri(const void* base, int64_t at_chunk, int wave, int l, typename M::Y (&x)[C / 32]) {
-    const auto rs = tokens((const char*)base + at_chunk * TRI<M, C> * (int)sizeof(typename M::E));
+// The C / 32 blocks of a wavefront's rows of T, P or their transposes.  Blocks that are zero are not there: they are asked for
+// outside the descriptor and come as zeros, so that no branch stands among a chunk's loads and products.
+template <typename M, int C, bool TRANSPOSED> __device__ __forceinline__ void load_tri(const Chunks& base, int wave, int l, typename M::Y (&x)[C / 32]) {
+    const auto rs = tokens(base.p);
 #pragma unroll
     for (int ks = 0; ks < C / 32; ++ks) {
-        const int k = TRANSPOSED ? max(ks, wave / 2) : min(ks, wave / 2);
-        const int at = (TRANSPOSED ? tri_block_t<C>(wave, k) : tri_block<C>(wave, k)) * BLOCK<M> * (int)sizeof(typename M::E);
+        const bool there = TRANSPOSED ? ks >= wave / 2 : ks <= wave / 2;
+        const int at = there ? (TRANSPOSED ? tri_block_t<C>(wave, ks) : tri_block<C>(wave, ks)) * BLOCK<M> * (int)sizeof(typename M::E) : 0;
         if constexpr (M::PLANES == 3) {
-            x[ks].h = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * l, at, 0));
-            x[ks].m = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * l, at + 1024, 0));
-            x[ks].l = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * l, at + 2048, 0));
+            const int lane = there ? 16 * l : NOWHERE;
+            x[ks].h = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, lane, at, 0));
+            x[ks].m = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, lane, at + 1024, 0));
+            x[ks].l = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, lane, at + 2048, 0));
         } else {
-            load_ff(rs, 32 * l, at, x[ks]);
+            load_ff(rs, there ? 32 * l : NOWHERE - 16, at, x[ks]);
         }
     }
 }
 // The wavefront's strips of K^T or Q^T.
-template <typename M, int C, int RS> __device__ __forceinline__ void load_kt(const void* base, int64_t at, int wave, int l, typename M::X (&x)[RS][C / 32]) {
+template <typename M, int C, int RS> __device__ __forceinline__ void load_kt(const Chunks& base, int wave, int l, typename M::X (&x)[RS][C / 32]) {
     constexpr int ES = sizeof(typename M::E);
-    const auto rs = tokens((const char*)base + at * ES);
+    const auto rs = tokens(base.p);
 #pragma unroll
     for (int s = 0; s < RS; ++s)
 #pragma unroll
@@ -743,8 +785,8 @@ template <typename M, int C, int RS> __device__ __forceinline__ void load_kt(con
 struct ChunkGates {                         // of this lane's tokens i0 .. i0 + 3
     floatx4 gam, end, beta;
     float last;
-    template <int C> __device__ __forceinline__ void load(const float* G, int64_t at_chunk, int i0) {
-        const auto rs = tokens((const char*)(G + at_chunk * GATES<C>));
+    template <int C> __device__ __forceinline__ void load(const Chunks& base, int i0) {
+        const auto rs = tokens(base.p);
         gam = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rs, 4 * i0, 0, 0));
         end = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rs, 4 * i0, 4 * C, 0));
         beta = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rs, 4 * i0, 8 * C, 0));
@@ -776,7 +818,7 @@ template <int RS, int NT> __device__ __forceinline__ void store_state(float* p, 
         }
 }
 template <typename M, int C, int DK, int NT, bool AL, bool KEEP>
-__global__ __launch_bounds__(8 * C) void delta_scan_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128 ? 2 : 4, DK == 128 ? 2 : 4))) void delta_scan_kernel(DeltaArgs a) {
     using E = typename M::E;
     using L = ScanLds<M, C, DK, NT>;
     constexpr int RS = DK / C, KS = C / 32, ND = DK / 32, NW = C / 16;      // 16-row strips of the state per wavefront, contraction steps
@@ -790,17 +832,23 @@ __global__ __launch_bounds__(8 * C) void delta_scan_kernel(DeltaArgs a) {
     const int dk = a.dim_k, dv = a.dim_v, row = 16 * wave + c, i0 = 16 * wave + 4 * q;
     const int chunks = (w.len + C - 1) / C;
     const int64_t first = (int64_t)w.bh * a.chunks;
-    ChunkGates G;
+    constexpr int64_t tri_bytes = TRI<M, C> * (int)sizeof(E), kt_bytes = DK * C * (int)sizeof(E);
+    const int64_t first_k = ((int64_t)w.b * a.heads_k + w.hk) * a.chunks;
+    ChunkGates G, Gn;                               // this chunk's, the next one's
+    Chunks pG(a.G, first, GATES<C> * 4, 0, 1);
     if (all < NW) {                                 // the chain
-        RowOperands<M, C, DK, AL> K(a.k, w, w.hk, dk, row, q);
-        ColumnValues<M, C, NT, AL> V(a.v, w, dv, i0, c0 + c);
+        RowOperands<M, C, DK, AL> K(a.k, w, w.hk, dk, row, q, 0, 1);
+        ColumnValues<M, C, NT, AL> V(a.v, w, dv, i0, c0 + c, 0, 1);
+        Chunks pT(a.T, first, tri_bytes, 0, 1), pK(a.KT, first_k, kt_bytes, 0, 1);
+        Chunks pS(a.S + c0, first, (int64_t)DK * a.dvp * 4, 0, 1), pR(a.R + c0, first, (int64_t)C * a.dvp * 4, 0, 1);
+        const int ld4 = 4 * a.dvp, lane_s = (16 * wave * RS + 4 * q) * ld4 + 4 * c, lane_r = (16 * wave + 4 * q) * ld4 + 4 * c;
         typename M::X kt[RS][KS];
         typename M::Y T[KS];
         floatx4 S[RS][NT];
         if (chunks > 0) {
-            K.load(0); V.load(0); G.load<C>(a.G, first, i0);
-            load_tri<M, C, false>(a.T, first, wave, l, T);
-            load_kt<M, C, RS>(a.KT, kt_at<E, C>(a, w, 0, DK), wave, l, kt);
+            K.load(); V.load(); G.load<C>(pG, i0);
+            load_tri<M, C, false>(pT, wave, l, T);
+            load_kt<M, C, RS>(pK, wave, l, kt);
         }
         load_state<RS, NT>(a.state, w, wave, q, c0 + c, dk, dv, S);
 #pragma unroll
@@ -808,33 +856,47 @@ __global__ __launch_bounds__(8 * C) void delta_scan_kernel(DeltaArgs a) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) tS.put4(16 * n + c, 16 * (wave * RS + s) + 4 * q, S[s][n]);
         for (int ch = 0; ch < chunks; ++ch) {
-            const int next = min(ch + 1, chunks - 1);
-            const int64_t at_chunk = first + ch;
+            const bool more = ch + 1 < chunks;
             __syncthreads();                        // 1: the state is in LDS
-            floatx4 z[NT] = {};
+            Acc za[NT];
+            {
+                typename M::Y f[ND][NT];
+                tS.template frags<ND, NT>(c, 8 * q, f);
 #pragma unroll
-            for (int d = 0; d < ND; ++d)
+                for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma(z[n], K.f[d], tS.frag(16 * n + c, 32 * d + 8 * q));
-            K.load(next);
+                    for (int n = 0; n < NT; ++n) za[n].add(K.f[d], f[d][n]);
+            }
+            pG.go(more);
+            Gn.load<C>(pG, i0);
+            K.go(more);
+            K.load();
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const floatx4 v = V.get(n);
+                const floatx4 v = V.get(n), z = za[n].sum();
                 floatx4 x;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = v[r] - damp(G.gam[r], z[n][r]);
+                for (int r = 0; r < 4; ++r) x[r] = v[r] - damp(G.gam[r], z[r]);
                 tX.put4(16 * n + c, i0, x);
             }
-            V.load(next);
+            V.go(more);
+            V.load();
             __syncthreads();                        // 2: X
-            floatx4 rr[NT] = {};
+            Acc ra[NT];
+            {
+                typename M::Y f[KS][NT];
+                tX.template frags<KS, NT>(c, 8 * q, f);
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                if (k > wave / 2) break;
+                for (int k = 0; k < KS; ++k) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma(rr[n], T[k], tX.frag(16 * n + c, 32 * k + 8 * q));
+                    for (int n = 0; n < NT; ++n) ra[n].add(T[k], f[k][n]);
+                }
             }
-            load_tri<M, C, false>(a.T, first + next, wave, l, T);
+            floatx4 rr[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) rr[n] = ra[n].sum();
+            pT.go(more);
+            load_tri<M, C, false>(pT, wave, l, T);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const floatx4 y = G.beta * rr[n];
@@ -844,10 +906,14 @@ __global__ __launch_bounds__(8 * C) void delta_scan_kernel(DeltaArgs a) {
             const float last = G.last;
             if (KEEP) {
 #pragma unroll
-                for (int s = 0; s < RS; ++s) put_padded<NT>(a.S + at_chunk * DK * a.dvp, 16 * (wave * RS + s), a.dvp, q, c0, c, S[s]);
-                put_padded<NT>(a.R + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, rr);
+                for (int s = 0; s < RS; ++s) put_padded<NT>(pS.p, lane_s, 16 * s, ld4, S[s]);
+                put_padded<NT>(pR.p, lane_r, 0, ld4, rr);
+                pS.go(true);
+                pR.go(true);
             }
             __syncthreads();                        // 3: Y; all have read the state
+            typename M::Y f[KS][NT];
+            tZ.template frags<KS, NT>(c, 8 * q, f);
 #pragma unroll
             for (int s = 0; s < RS; ++s) {
                 const int r0 = 16 * (wave * RS + s);
@@ -855,48 +921,66 @@ __global__ __launch_bounds__(8 * C) void delta_scan_kernel(DeltaArgs a) {
                 for (int n = 0; n < NT; ++n) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) S[s][n][r] = damp(last, S[s][n][r]);
+                    Acc sa;
+                    sa.a[0] = S[s][n];
 #pragma unroll
-                    for (int k = 0; k < KS; ++k) mma(S[s][n], kt[s][k], tZ.frag(16 * n + c, 32 * k + 8 * q));
+                    for (int k = 0; k < KS; ++k) sa.add(kt[s][k], f[k][n]);
+                    S[s][n] = sa.sum();
                     tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
                 }
             }
-            load_kt<M, C, RS>(a.KT, kt_at<E, C>(a, w, next, DK), wave, l, kt);
-            G.load<C>(a.G, first + next, i0);
+            pK.go(more);
+            load_kt<M, C, RS>(pK, wave, l, kt);
+            G = Gn;
         }
         store_state<RS, NT>(a.state_out, w, wave, q, c0 + c, dk, dv, S);
     } else {                                        // the outputs: rounded to the tokens' type, two terms of S, P, Y are enough
-        RowOperands<M, C, DK, AL> Q(a.q, w, w.hk, dk, row, q);
+        RowOperands<M, C, DK, AL> Q(a.q, w, w.hk, dk, row, q, 0, 1);
+        ColumnValues<M, C, NT, AL> O(a.out, w, dv, i0, c0 + c, 0, 1);
+        Chunks pP(a.P, first, tri_bytes, 0, 1);
         typename M::Y P[KS];
         if (chunks > 0) {
-            Q.load(0); G.load<C>(a.G, first, i0);
-            load_tri<M, C, false>(a.P, first, wave, l, P);
+            Q.load(); G.load<C>(pG, i0);
+            load_tri<M, C, false>(pP, wave, l, P);
         }
         for (int ch = 0; ch < chunks; ++ch) {
-            const int next = min(ch + 1, chunks - 1);
+            const bool more = ch + 1 < chunks;
             __syncthreads();                        // 1
             floatx4 o[NT] = {};
+            {
+                typename M::Y f[ND][NT];
+                tS.template frags<ND, NT>(c, 8 * q, f);
 #pragma unroll
-            for (int d = 0; d < ND; ++d)
+                for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma_out(o[n], Q.f[d], tS.frag(16 * n + c, 32 * d + 8 * q));
-            Q.load(next);
+                    for (int n = 0; n < NT; ++n) mma_out(o[n], Q.f[d], f[d][n]);
+            }
+            pG.go(more);
+            Gn.load<C>(pG, i0);
+            Q.go(more);
+            Q.load();
             __syncthreads();                        // 2
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) o[n][r] = damp(G.gam[r], o[n][r]);
-            G.load<C>(a.G, first + next, i0);
+            G = Gn;
             __syncthreads();                        // 3
+            {
+                typename M::Y f[KS][NT];
+                tY.template frags<KS, NT>(c, 8 * q, f);
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                if (k > wave / 2) break;
+                for (int k = 0; k < KS; ++k) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma_out(o[n], P[k], tY.frag(16 * n + c, 32 * k + 8 * q));
+                    for (int n = 0; n < NT; ++n) mma_out(o[n], P[k], f[k][n]);
+                }
             }
-            load_tri<M, C, false>(a.P, first + next, wave, l, P);
+            pP.go(more);
+            load_tri<M, C, false>(pP, wave, l, P);
 #pragma unroll
             for (int n = 0; n < NT; ++n) o[n] *= a.scale;
-            ColumnValues<M, C, NT, AL>::put(a.out, w, a.steps, dv, ch, i0, c0 + c, o);
+            O.put(a.steps - ch * C, o);
+            O.go(true);
         }
         const int n = min(16 * NT, dv - c0);
         if (n > 0 && a.steps > chunks * C && all == NW) zero_rows<E>(a.out, w, chunks * C, a.steps, c0, n);
@@ -916,7 +1000,7 @@ template <typename M, int C, int DK, int NT> struct BackScanLds {
                          Q0 = P0 + C * 16 * NT * 4, BYTES = Q0 + DK * 16 * NT * 4;      // P0, Q0: results of P^T dO, Q^T (gam o dO)
 };
 template <typename M, int C, int DK, int NT, bool AL>
-__global__ __launch_bounds__(8 * C) void delta_back_scan_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128 ? 2 : 1, DK == 128 ? 2 : 8))) void delta_back_scan_kernel(DeltaArgs a) {
     using E = typename M::E;
     using L = BackScanLds<M, C, DK, NT>;
     constexpr int RS = DK / C, KS = C / 32, ND = DK / 32, NW = C / 16;
@@ -933,16 +1017,25 @@ __global__ __launch_bounds__(8 * C) void delta_back_scan_kernel(DeltaArgs a) {
     const int dk = a.dim_k, dv = a.dim_v, row = 16 * wave + c, i0 = 16 * wave + 4 * q;
     const int chunks = (w.len + C - 1) / C;
     const int64_t first = (int64_t)w.bh * a.chunks;
-    ChunkGates G;
+    constexpr int64_t tri_bytes = TRI<M, C> * (int)sizeof(E), kt_bytes = DK * C * (int)sizeof(E);
+    const int64_t first_k = ((int64_t)w.b * a.heads_k + w.hk) * a.chunks;
+    const int end = max(chunks - 1, 0);
+    ChunkGates G, Gn;
+    Chunks pG(a.G, first, GATES<C> * 4, end, -1);
     if (all < NW) {                                 // the chain
-        RowOperands<M, C, DK, AL> K(a.k, w, w.hk, dk, row, q);
+        RowOperands<M, C, DK, AL> K(a.k, w, w.hk, dk, row, q, end, -1);
+        ColumnValues<M, C, NT, AL> dV(a.dv, w, dv, i0, c0 + c, end, -1);
+        Chunks pT(a.TT, first, tri_bytes, end, -1), pK(a.KT, first_k, kt_bytes, end, -1);
+        Chunks pS(a.dS + c0, first, (int64_t)DK * a.dvp * 4, end, -1), pX(a.dX + c0, first, (int64_t)C * a.dvp * 4, end, -1),
+            pY(a.dY + c0, first, (int64_t)C * a.dvp * 4, end, -1);
+        const int ld4 = 4 * a.dvp, lane_s = (16 * wave * RS + 4 * q) * ld4 + 4 * c, lane_r = (16 * wave + 4 * q) * ld4 + 4 * c;
         typename M::X kt[RS][KS];
         typename M::Y T[KS];
         floatx4 S[RS][NT];
         if (chunks > 0) {
-            K.load(chunks - 1); G.load<C>(a.G, first + chunks - 1, i0);
-            load_tri<M, C, true>(a.TT, first + chunks - 1, wave, l, T);
-            load_kt<M, C, RS>(a.KT, kt_at<E, C>(a, w, chunks - 1, DK), wave, l, kt);
+            K.load(); G.load<C>(pG, i0);
+            load_tri<M, C, true>(pT, wave, l, T);
+            load_kt<M, C, RS>(pK, wave, l, kt);
         }
         load_state<RS, NT>(a.state_grad, w, wave, q, c0 + c, dk, dv, S);
 #pragma unroll
@@ -951,15 +1044,24 @@ __global__ __launch_bounds__(8 * C) void delta_back_scan_kernel(DeltaArgs a) {
             for (int n = 0; n < NT; ++n) tS.put4(16 * n + c, 16 * (wave * RS + s) + 4 * q, S[s][n]);
         if (chunks > 0) __syncthreads();            // 0: the helpers' dO
         for (int ch = chunks - 1; ch >= 0; --ch) {
-            const int next = max(ch - 1, 0);
-            const int64_t at_chunk = first + ch;
+            const bool more = ch > 0;
             __syncthreads();                        // 1: dS, P^T dO, Q^T (gam o dO)
-            floatx4 y[NT] = {}, gq[RS][NT];
+            floatx4 y[NT], gq[RS][NT];
+            {
+                Acc ya[NT];
+                typename M::Y f[ND][NT];
+                tS.template frags<ND, NT>(c, 8 * q, f);
 #pragma unroll
-            for (int d = 0; d < ND; ++d)
+                for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma(y[n], K.f[d], tS.frag(16 * n + c, 32 * d + 8 * q));
-            K.load(next);
+                    for (int n = 0; n < NT; ++n) ya[n].add(K.f[d], f[d][n]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) y[n] = ya[n].sum();
+            }
+            pG.go(more);
+            Gn.load<C>(pG, i0);
+            K.go(more);
+            K.load();
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const floatx4 p = tP[n * 64];
@@ -972,21 +1074,32 @@ __global__ __launch_bounds__(8 * C) void delta_back_scan_kernel(DeltaArgs a) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) gq[s][n] = tQ[(s * NT + n) * 64];
             __syncthreads();                        // 2: dR; P^T dO and Q^T (gam o dO) are taken
-            put_padded<NT>(a.dY + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, y);
+            floatx4 dx[NT];
+            {
+                Acc xa[NT];
+                typename M::Y f[KS][NT];
+                tR.template frags<KS, NT>(c, 8 * q, f);
 #pragma unroll
-            for (int s = 0; s < RS; ++s) put_padded<NT>(a.dS + at_chunk * DK * a.dvp, 16 * (wave * RS + s), a.dvp, q, c0, c, S[s]);
-            floatx4 dx[NT] = {};
+                for (int k = 0; k < KS; ++k) {
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                if (k < wave / 2) continue;
+                    for (int n = 0; n < NT; ++n) xa[n].add(T[k], f[k][n]);
+                }
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma(dx[n], T[k], tR.frag(16 * n + c, 32 * k + 8 * q));
+                for (int n = 0; n < NT; ++n) dx[n] = xa[n].sum();
             }
-            load_tri<M, C, true>(a.TT, first + next, wave, l, T);
+            pT.go(more);
+            load_tri<M, C, true>(pT, wave, l, T);
 #pragma unroll
             for (int n = 0; n < NT; ++n) tX.put4(16 * n + c, i0, -G.gam * dx[n]);
+            put_padded<NT>(pY.p, lane_r, 0, ld4, y);
+            pY.go(true);
+#pragma unroll
+            for (int s = 0; s < RS; ++s) put_padded<NT>(pS.p, lane_s, 16 * s, ld4, S[s]);
+            pS.go(true);
             const float last = G.last;
             __syncthreads();                        // 3: dX; all have read dS
+            typename M::Y f[KS][NT];
+            tX.template frags<KS, NT>(c, 8 * q, f);
 #pragma unroll
             for (int s = 0; s < RS; ++s) {
                 const int r0 = 16 * (wave * RS + s);
@@ -994,24 +1107,42 @@ __global__ __launch_bounds__(8 * C) void delta_back_scan_kernel(DeltaArgs a) {
                 for (int n = 0; n < NT; ++n) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) S[s][n][r] = damp(last, S[s][n][r]) + gq[s][n][r];
+                    Acc sa;
+                    sa.a[0] = S[s][n];
 #pragma unroll
-                    for (int k = 0; k < KS; ++k) mma(S[s][n], kt[s][k], tX.frag(16 * n + c, 32 * k + 8 * q));
+                    for (int k = 0; k < KS; ++k) sa.add(kt[s][k], f[k][n]);
+                    S[s][n] = sa.sum();
                     tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
                 }
             }
-            load_kt<M, C, RS>(a.KT, kt_at<E, C>(a, w, next, DK), wave, l, kt);
-            G.load<C>(a.G, first + next, i0);
-            put_padded<NT>(a.dX + at_chunk * C * a.dvp, 16 * wave, a.dvp, q, c0, c, dx);
-            ColumnValues<M, C, NT, AL>::put(a.dv, w, a.steps, dv, ch, i0, c0 + c, dx);
+            pK.go(more);
+            load_kt<M, C, RS>(pK, wave, l, kt);
+            G = Gn;
+            put_padded<NT>(pX.p, lane_r, 0, ld4, dx);
+            pX.go(true);
+            dV.put(a.steps - ch * C, dx);
+            dV.go(true);
         }
         store_state<RS, NT>(a.dstate, w, wave, q, c0 + c, dk, dv, S);
     } else {                                        // P^T dO and Q^T (gam o dO), a chunk ahead of the chain
-        ColumnValues<M, C, NT, AL> O(a.out_grad, w, dv, i0, c0 + c);
+        ColumnValues<M, C, NT, AL> O(a.out_grad, w, dv, i0, c0 + c, end, -1);
+        Chunks pP(a.PT, first, tri_bytes, end, -1), pQ(a.QT, first_k, kt_bytes, end, -1);
         typename M::X qt[RS][KS];
         typename M::Y P[KS];
-        auto load = [&](int ch) {
-            load_tri<M, C, true>(a.PT, first + ch, wave, l, P);
-            load_kt<M, C, RS>(a.QT, kt_at<E, C>(a, w, ch, DK), wave, l, qt);
+        auto load = [&] {
+            load_tri<M, C, true>(pP, wave, l, P);
+            load_kt<M, C, RS>(pQ, wave, l, qt);
+        };
+        auto load_next = [&](bool more) {
+            pP.go(more);
+            pQ.go(more);
+            load();
+        };
+        auto load_o = [&](bool more) {
+            O.go(more);
+            O.load();
+            pG.go(more);
+            G.load<C>(pG, i0);
         };
         auto put = [&] {
 #pragma unroll
@@ -1027,8 +1158,7 @@ __global__ __launch_bounds__(8 * C) void delta_back_scan_kernel(DeltaArgs a) {
             for (int n = 0; n < NT; ++n) {
                 p[n] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int k = 0; k < KS; ++k)
-                    if (k >= wave / 2) mma(p[n], P[k], tO.frag(16 * n + c, 32 * k + 8 * q));
+                for (int k = 0; k < KS; ++k) mma(p[n], P[k], tO.frag(16 * n + c, 32 * k + 8 * q));
 #pragma unroll
                 for (int s = 0; s < RS; ++s) {
                     g[s][n] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -1046,23 +1176,23 @@ __global__ __launch_bounds__(8 * C) void delta_back_scan_kernel(DeltaArgs a) {
             }
         };
         if (chunks > 0) {
-            O.load(chunks - 1); G.load<C>(a.G, first + chunks - 1, i0);
-            load(chunks - 1);
+            load_o(false);
+            load();
             put();
-            O.load(max(chunks - 2, 0)); G.load<C>(a.G, first + max(chunks - 2, 0), i0);
+            load_o(chunks > 1);
             __syncthreads();                        // 0
             products();
             hand_over();
-            load(max(chunks - 2, 0));
+            load_next(chunks > 1);
         }
         for (int ch = chunks - 1; ch >= 0; --ch) {  // the chunk before `ch` here
-            const int after = max(ch - 2, 0);
+            const bool more = ch > 1;
             __syncthreads();                        // 1: dO of the last chunk has been used
             put();
-            O.load(after); G.load<C>(a.G, first + after, i0);
+            load_o(more);
             __syncthreads();                        // 2: the new dO is there
             products();
-            load(after);
+            load_next(more);
             __syncthreads();                        // 3: and what was handed over before has been taken
             hand_over();
         }
@@ -1073,15 +1203,16 @@ __global__ __launch_bounds__(8 * C) void delta_back_scan_kernel(DeltaArgs a) {
 
 // =============================================================================================
 // Gradient, all chunks at once: dQ, dK, dbeta, dg.  Two wavefronts per 16 tokens, each with half of dim_k.  First the
-// contractions over the columns, 32 at a time: what all wavefronts need (R, Y, S0, dS1) is brought from memory, split and put
-// into LDS once for all of them, the next 32 columns being on their way meanwhile; then those over tokens with E and F in
-// LDS, K^T and Q^T straight from memory.
+// contractions over the columns, 32 at a time: everything but dO is brought from memory, split and put into LDS once for all
+// wavefronts, the next 32 columns being on their way meanwhile; then those over tokens with E and F in LDS, K^T and Q^T
+// straight from memory.  With a.heads_wg = group a workgroup takes the value heads of one key head one after the other and
+// adds dQ and dK up in registers; where that leaves too few workgroups, it takes one, and delta_group_kernel adds.
 // =============================================================================================
 template <typename M, int C, int DK> struct BackLds {
-    using R = Tile<M, C, 32, false>;        // R, Y
+    using R = Tile<M, C, 32, false>;        // R, Y, dX
     using S = Tile<M, DK, 32, false>;       // S0, dS1
     using W = Tile<M, C, C, false>;         // E, E^T, F diag(beta), F^T
-    static constexpr int R0 = 0, Y0 = R0 + R::BYTES, S0 = Y0 + R::BYTES, S1 = S0 + S::BYTES, FIRST = S1 + S::BYTES;
+    static constexpr int R0 = 0, Y0 = R0 + R::BYTES, X0 = Y0 + R::BYTES, S0 = X0 + R::BYTES, S1 = S0 + S::BYTES, FIRST = S1 + S::BYTES;
     static constexpr int E0 = 0, ET0 = E0 + W::BYTES, F0 = ET0 + W::BYTES, FT0 = F0 + W::BYTES, SECOND = FT0 + W::BYTES;
     static constexpr int BYTES = FIRST > SECOND ? FIRST : SECOND;
 };
@@ -1090,216 +1221,252 @@ __device__ __forceinline__ float sum16(float x) {      // over the 16 lanes that
     for (int d = 1; d < 16; d *= 2) x += __shfl_xor(x, d);
     return x;
 }
-template <typename M, int C, int DK, bool AL>
+template <typename M, int C, int DK, bool AL, bool MANY>
 __global__ __launch_bounds__(8 * C) void delta_back_kernel(DeltaArgs a) {
     using E = typename M::E;
     using L = BackLds<M, C, DK>;
-    constexpr int NW = C / 16, KS = C / 32, NK = DK / 32, THREADS = 8 * C, SU = 8 * DK / THREADS;      // NK: 16-column tiles of a wavefront's half
+    constexpr int NW = C / 16, KS = C / 32, NK = DK / 32, THREADS = 8 * C, UN = 8 * DK / THREADS;      // NK: 16-column tiles of a wavefront's half
     extern __shared__ __align__(16) unsigned char lds[];
     __shared__ Gates s_g;
-    __shared__ float s_dG[2][C], s_b[2][C], s_ext[2 * NW];
-    const typename L::R tR(lds + L::R0), tY(lds + L::Y0);
+    __shared__ float s_dG[2][C], s_b[2][C], s_yr[C], s_ext[2 * NW];
+    const typename L::R tR(lds + L::R0), tY(lds + L::Y0), tX(lds + L::X0);
     const typename L::S tS0(lds + L::S0), tS1(lds + L::S1);
     const typename L::W tE(lds + L::E0), tET(lds + L::ET0), tF(lds + L::F0), tFT(lds + L::FT0);
-    const Where w = where_of(a, blockIdx.y);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, q = l >> 4;
+    const int heads = MANY ? a.heads_wg : 1, per_seq = a.heads_v / heads;
+    Where w = where_of(a, MANY ? (int)blockIdx.y / per_seq * a.heads_v + (int)blockIdx.y % per_seq * heads : (int)blockIdx.y);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int strip = wave % NW, half = wave / NW, n0 = half * NK;
     const int dk = a.dim_k, ch = blockIdx.x, dvp = a.dvp;
-    const int64_t t0 = (int64_t)ch * C, at_chunk = (int64_t)w.bh * a.chunks + ch;
+    const int64_t t0 = (int64_t)ch * C;
     const int len = min(w.len - ch * C, C), rows = min(a.steps - ch * C, C);
-    // one value head per key head: straight to the results; else to one row per value head, added up afterwards
     auto put = [&](const DeltaSeq& s, float* part, int i, int d, float x) {
         if (part) part[(((int64_t)w.b * a.steps + t0 + i) * a.heads_v + w.h) * dk + d] = x;
-        else at_out<E>(s, w.b, t0 + i, w.h)[d] = from_float<E>(x);
+        else at_out<E>(s, w.b, t0 + i, w.hk)[d] = from_float<E>(x);
     };
     if (len <= 0) {
         for (int i = threadIdx.x; i < rows * dk; i += THREADS) { put(a.dq, a.part_q, i / dk, i % dk, 0.f); put(a.dk, a.part_k, i / dk, i % dk, 0.f); }
-        for (int i = threadIdx.x; i < rows; i += THREADS) { *at_out<float>(a.dg, w.b, t0 + i, w.h) = 0.f; *at_out<float>(a.dbeta, w.b, t0 + i, w.h) = 0.f; }
+        for (int i = threadIdx.x; i < rows * heads; i += THREADS) {
+            *at_out<float>(a.dg, w.b, t0 + i / heads, w.h + i % heads) = 0.f;
+            *at_out<float>(a.dbeta, w.b, t0 + i / heads, w.h + i % heads) = 0.f;
+        }
         return;
     }
-    gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
-    const int row = 16 * strip + c, i0 = 16 * strip + 4 * q;
-    const float* R = a.R + at_chunk * C * dvp;
-    const float* dX = a.dX + at_chunk * C * dvp;
-    const float* dY = a.dY + at_chunk * C * dvp;
-    const float* S0 = a.S + at_chunk * DK * dvp;
-    const float* S1 = a.dS + at_chunk * DK * dvp;
-    const E* dO = at<E>(a.out_grad, w.b, t0, w.h);
-    // what the next 32 columns need: this thread's share of the matrices in LDS, this wavefront's rows of dX and dO
-    float xr[8], xs[SU][8], xx[8];
-    typename M::X fo;
-    const int unit = threadIdx.x;           // eight columns (unit % 4) of row unit / 4, of R or of S0 and dS1
-    auto load = [&](int d) {
-        if (unit < 4 * C) load8(R + (unit >> 2) * dvp + d + (unit & 3) * 8, xr);
+    const int64_t kt0 = kt_at<E, C>(a, w, ch, DK);
+    floatx4 sum_q[NK], sum_k[NK];
+    if (MANY) {
 #pragma unroll
-        for (int i = 0; i < SU; ++i) {
-            const int u = unit + i * THREADS, r = u >> 2;
-            load8((r < DK ? S0 + r * dvp : S1 + (r - DK) * dvp) + d + (u & 3) * 8, xs[i]);
-        }
-        load8(dX + row * dvp + d + 8 * q, xx);
-        fo = row_operand<M, AL>(dO + row * a.out_grad.t, d + 8 * q, a.dim_v, row < len);
-    };
-    load(0);
-    floatx4 dq[NK] = {}, ks[NK] = {}, ke[NK] = {}, ef[NW] = {};     // ef: E (first half of the wavefronts) or F
-    float yr = 0.f, ss = 0.f;               // dY.R of row `row` (this lane's columns), <dS1, S0> of this thread's elements
-    __syncthreads();                        // gates are there
-    for (int d = 0; d < dvp; d += 32) {
-        if (unit < 4 * C) {
-            const int r = unit >> 2, k = (unit & 3) * 8;
-            const float beta = s_g.beta[r];
-            tR.put8(r, k, xr);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) xr[j] *= beta;
-            tY.put8(r, k, xr);
-        }
-#pragma unroll
-        for (int i = 0; i < SU; ++i) {
-            const int u = unit + i * THREADS, r = u >> 2;
-            if (r < DK) tS0.put8(r, (u & 3) * 8, xs[i]);
-            else tS1.put8(r - DK, (u & 3) * 8, xs[i]);
-        }
-        const auto fx = M::computed(xx);
-        const auto fd = fo;
-        if (half == 0) {                    // dY.R; exact in 32 bits, outside the split products
-            float x[8], y[8];
-            load8(R + row * dvp + d + 8 * q, x);
-            load8(dY + row * dvp + d + 8 * q, y);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) yr += x[j] * y[j];
-        }
-        if (d + 32 < dvp) load(d + 32);
-        __syncthreads();
-        const auto fy = tY.frag(row, 8 * q);
-        if (half == 0) {
-#pragma unroll
-            for (int n = 0; n < NW; ++n)
-                if (n <= strip) mma(ef[n], fd, tY.frag(16 * n + c, 8 * q));
-        } else {
-#pragma unroll
-            for (int n = 0; n < NW; ++n)
-                if (n <= strip) mma(ef[n], fx, tR.frag(16 * n + c, 8 * q));
-        }
-#pragma unroll
-        for (int n = 0; n < NK; ++n) {
-            const auto g = tS0.frag(16 * (n0 + n) + c, 8 * q);
-            mma(dq[n], fd, g);
-            mma(ks[n], fx, g);
-            mma(ke[n], fy, tS1.frag(16 * (n0 + n) + c, 8 * q));
-        }
-        __syncthreads();
+        for (int n = 0; n < NK; ++n) sum_q[n] = sum_k[n] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
-    for (int i = threadIdx.x; i < DK * dvp / 4; i += THREADS) {     // <dS1, S0>, from the caches
-        const floatx4 x = ((const floatx4*)S0)[i], y = ((const floatx4*)S1)[i];
-        ss += x[0] * y[0] + x[1] * y[1] + x[2] * y[2] + x[3] * y[3];
-    }
-    // K^T and Q^T of this half, as right operands and as values beside the results
-    const E* KT = (const E*)a.KT + kt_at<E, C>(a, w, ch, DK);
-    const E* QT = (const E*)a.QT + kt_at<E, C>(a, w, ch, DK);
+    for (int head = 0; head < heads; ++head, ++w.h, ++w.bh) {
+        // lane numbers anew for every head: what is worked out from them would otherwise be kept over the loop, in registers
+        // that are not there
+        int unit = threadIdx.x;
+        if (MANY) asm volatile("" : "+v"(unit));
+        const int l = unit & 63, c = l & 15, q = l >> 4, row = 16 * strip + c, i0 = 16 * strip + 4 * q;
+        const int64_t at_chunk = (int64_t)w.bh * a.chunks + ch;
+        if (head) __syncthreads();          // the last one's gates and sums have been used
+        gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
+        const bool first = unit < 4 * C;    // this thread's share of R and dY, or of dX: eight columns of one row
+        const int ur = (first ? unit : unit - 4 * C) >> 2, uk = (unit & 3) * 8;
+        const float* RX = (first ? a.R : a.dX) + (at_chunk * C + ur) * dvp + uk;
+        const float* dY = a.dY + (at_chunk * C + ur) * dvp + uk;
+        const float* S0 = a.S + (at_chunk * DK + (unit >> 3)) * dvp + (unit & 7) * 4;       // and of S0 and dS1: four columns of some rows
+        const float* S1 = a.dS + (at_chunk * DK + (unit >> 3)) * dvp + (unit & 7) * 4;
+        const E* dO = at<E>(a.out_grad, w.b, t0, w.h) + row * a.out_grad.t;
+        float rx[8], dy[8];
+        floatx4 s0[UN], s1[UN];
+        typename M::X fo;
+        auto load = [&](int d) {
+            load8(RX + d, rx);
+            if (first) load8(dY + d, dy);
 #pragma unroll
-    for (int n = 0; n < NW; ++n) {
-        const int j = 16 * n + c;
-        const float beta = s_g.beta[j];
-        floatx4 x = ef[n], y;
+            for (int i = 0; i < UN; ++i) {
+                s0[i] = *(const floatx4*)(S0 + i * (THREADS / 8) * dvp + d);
+                s1[i] = *(const floatx4*)(S1 + i * (THREADS / 8) * dvp + d);
+            }
+            fo = row_operand<M, AL>(dO, d + 8 * q, a.dim_v, row < len);
+        };
+        load(0);
+        floatx4 dq[NK] = {}, ks[NK] = {}, ke[NK] = {}, ef[NW] = {};     // ef: E (first half of the wavefronts) or F
+        float yr = 0.f, ss = 0.f;           // dY.R of row ur, <dS1, S0>: this thread's elements
+        __syncthreads();                    // gates are there
+        for (int d = 0; d < dvp; d += 32) {
+            if (first) {
+                const float beta = s_g.beta[ur];
+                tR.put8(ur, uk, rx);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { yr += rx[j] * dy[j]; rx[j] *= beta; }
+                tY.put8(ur, uk, rx);
+            } else {
+                tX.put8(ur, uk, rx);
+            }
+#pragma unroll
+            for (int i = 0; i < UN; ++i) {
+                const int r = (unit >> 3) + i * (THREADS / 8);
+                tS0.put4(r, (unit & 7) * 4, s0[i]);
+                tS1.put4(r, (unit & 7) * 4, s1[i]);
+                const floatx4 p = s0[i] * s1[i];
+                ss += p[0] + p[1] + p[2] + p[3];
+            }
+            const auto fd = fo;
+            if (d + 32 < dvp) load(d + 32);
+            __syncthreads();
+            const auto fy = tY.frag(row, 8 * q);
+            const auto fx = tX.frag(row, 8 * q);
+            if (half == 0) {
+#pragma unroll
+                for (int n = 0; n < NW; ++n)
+                    if (n <= strip) mma(ef[n], fd, tY.frag(16 * n + c, 8 * q));
+            } else {
+#pragma unroll
+                for (int n = 0; n < NW; ++n)
+                    if (n <= strip) mma(ef[n], fx, tR.frag(16 * n + c, 8 * q));
+            }
+#pragma unroll
+            for (int n = 0; n < NK; ++n) {
+                const auto g = tS0.frag(16 * (n0 + n) + c, 8 * q);
+                mma(dq[n], fd, g);
+                mma(ks[n], fx, g);
+                mma(ke[n], fy, tS1.frag(16 * (n0 + n) + c, 8 * q));
+            }
+            settle();
+            __syncthreads();
+        }
+        // K^T and Q^T of this half: right operands.  The same for every head, but too many registers to keep.
+        int64_t kt = kt0;
+        if (MANY) asm volatile("" : "+s"(kt));
+        const E* KT = (const E*)a.KT + kt;
+        const E* QT = (const E*)a.QT + kt;
+        typename M::X fk[NK][KS], fq[NK][KS];
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                fk[n][k] = load_operand<M>(KT + ((KS * (n0 + n) + k) * 64 + l) * 8);
+                fq[n][k] = load_operand<M>(QT + ((KS * (n0 + n) + k) * 64 + l) * 8);
+            }
+        yr += __shfl_xor(yr, 1);
+        yr += __shfl_xor(yr, 2);
+        if (first && (unit & 3) == 0) s_yr[ur] = yr;
+#pragma unroll
+        for (int n = 0; n < NW; ++n) {
+            const int j = 16 * n + c;
+            const float beta = s_g.beta[j];
+            floatx4 x = ef[n], y;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = i0 + r;
+                const float g = n <= strip && i >= j ? decay(s_g, i, j) : 0.f;
+                x[r] = half == 0 ? damp(a.scale * g, x[r]) : i > j ? damp(-g, x[r]) : 0.f;
+                y[r] = half == 0 ? x[r] : x[r] * beta;
+            }
+            // rows of the transposes are columns here: four consecutive elements of one row each; of the others one at a time
+            if (half == 0) {
+                tET.put4(j, i0, x);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) tE.put1(i0 + r, j, y[r]);
+            } else {
+                tFT.put4(j, i0, x);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) tF.put1(i0 + r, j, y[r]);
+            }
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int i = i0 + r;
-            const float g = n <= strip && i >= j ? decay(s_g, i, j) : 0.f;
-            x[r] = half == 0 ? damp(a.scale * g, x[r]) : i > j ? damp(-g, x[r]) : 0.f;
-            y[r] = half == 0 ? x[r] : x[r] * beta;
+            const float g = s_g.gam[i0 + r], en = s_g.end[i0 + r];
+#pragma unroll
+            for (int n = 0; n < NK; ++n) { dq[n][r] = damp(a.scale * g, dq[n][r]); ks[n][r] = damp(-g, ks[n][r]); ke[n][r] = damp(en, ke[n][r]); }
         }
-        // rows of the transposes are columns here: four consecutive elements of one row each; of the others one at a time
-        if (half == 0) {
-            tET.put4(j, i0, x);
+        auto values = [&](const E* T, int n) {          // tokens i0 .. i0 + 3 of column 16 (n0 + n) + c
+            const E* p = T + (KS * (n0 + n) + strip / 2) * 512 + (c + 16 * (2 * (strip & 1) + (q >> 1))) * 8 + 4 * (q & 1);
+            floatx4 x;
+            if constexpr (sizeof(E) == 4) {
+                x = *(const floatx4*)p;
+            } else {
+                const bf16x4 h = *(const bf16x4*)p;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) tE.put1(i0 + r, j, y[r]);
-        } else {
-            tFT.put4(j, i0, x);
+                for (int r = 0; r < 4; ++r) x[r] = (float)h[r];
+            }
+            return x;
+        };
+        floatx4 kv[NK], qv[NK];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) tF.put1(i0 + r, j, y[r]);
-        }
-    }
+        for (int n = 0; n < NK; ++n) { kv[n] = values(KT, n); qv[n] = values(QT, n); }
+        __syncthreads();
+        floatx4 ft[NK] = {};                // F^T K
+        float ext = 0.f;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float g = s_g.gam[i0 + r], en = s_g.end[i0 + r];
+        for (int n = 0; n < NK; ++n)
 #pragma unroll
-        for (int n = 0; n < NK; ++n) { dq[n][r] = damp(a.scale * g, dq[n][r]); ks[n][r] = damp(-g, ks[n][r]); ke[n][r] = damp(en, ke[n][r]); }
-    }
-    __syncthreads();
-    auto values = [&](const E* T, int n) {              // tokens i0 .. i0 + 3 of column 16 (n0 + n) + c
-        const E* p = T + (KS * (n0 + n) + strip / 2) * 512 + (c + 16 * (2 * (strip & 1) + (q >> 1))) * 8 + 4 * (q & 1);
-        floatx4 x;
-        if constexpr (sizeof(E) == 4) {
-            x = *(const floatx4*)p;
-        } else {
-            const bf16x4 h = *(const bf16x4*)p;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = (float)h[r];
-        }
-        return x;
-    };
-    floatx4 kdot = {}, kft = {};
-    float ext = 0.f;
-#pragma unroll
-    for (int n = 0; n < NK; ++n) {
-        floatx4 ft = {};                    // F^T K
-        const floatx4 kv = values(KT, n), qv = values(QT, n);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) ext += kv[r] * ke[n][r];          // before E^T Q joins it: the part of dG_last
+            for (int r = 0; r < 4; ++r) ext += kv[n][r] * ke[n][r];   // before E^T Q joins it: the part of dG_last
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            const auto fk = load_operand<M>(KT + ((KS * (n0 + n) + k) * 64 + l) * 8);
             if (k <= strip / 2) {           // E and F diag(beta): lower triangles
-                mma(dq[n], tE.frag(row, 32 * k + 8 * q), fk);
-                mma(ks[n], tF.frag(row, 32 * k + 8 * q), fk);
+                const auto fe = tE.frag(row, 32 * k + 8 * q);
+                const auto ff = tF.frag(row, 32 * k + 8 * q);
+#pragma unroll
+                for (int n = 0; n < NK; ++n) { mma(dq[n], fe, fk[n][k]); mma(ks[n], ff, fk[n][k]); }
             }
             if (k >= strip / 2) {
-                mma(ke[n], tET.frag(row, 32 * k + 8 * q), load_operand<M>(QT + ((KS * (n0 + n) + k) * 64 + l) * 8));
-                mma(ft, tFT.frag(row, 32 * k + 8 * q), fk);
+                const auto fe = tET.frag(row, 32 * k + 8 * q);
+                const auto ff = tFT.frag(row, 32 * k + 8 * q);
+#pragma unroll
+                for (int n = 0; n < NK; ++n) { mma(ke[n], fe, fq[n][k]); mma(ft[n], ff, fk[n][k]); }
             }
         }
-        const int d = 16 * (n0 + n) + c;
+        settle();
+        floatx4 kdot = {}, kft = {};
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                kft[r] += kv[n][r] * ft[n][r];
+                const float rest = ke[n][r] + s_g.beta[i0 + r] * ft[n][r];
+                kdot[r] += qv[n][r] * dq[n][r] + kv[n][r] * (ks[n][r] - rest);
+                sum_q[n][r] = MANY ? sum_q[n][r] + dq[n][r] : dq[n][r];
+                sum_k[n][r] = MANY ? sum_k[n][r] + ks[n][r] + rest : ks[n][r] + rest;
+            }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            kft[r] += kv[r] * ft[r];
-            const float rest = ke[n][r] + s_g.beta[i0 + r] * ft[r];
-            kdot[r] += qv[r] * dq[n][r] + kv[r] * (ks[n][r] - rest);
-            if (i0 + r < rows && d < dk) {
-                const bool in = i0 + r < len;
-                put(a.dq, a.part_q, i0 + r, d, in ? dq[n][r] : 0.f);
-                put(a.dk, a.part_k, i0 + r, d, in ? ks[n][r] + rest : 0.f);
+            const float b = sum16(kft[r]), g = sum16(kdot[r]);
+            if (c == 0) { s_dG[half][i0 + r] = g; s_b[half][i0 + r] = b; }
+        }
+        ext += damp(s_g.last, ss);
+        ext = sum16(ext);
+        ext += __shfl_xor(ext, 16);
+        ext += __shfl_xor(ext, 32);
+        if (l == 0) s_ext[wave] = ext;
+        __syncthreads();
+        if (wave == 0) {                    // sums from the end to each token, within its segment
+            float x = l < C ? s_dG[0][l] + s_dG[1][l] : 0.f;
+            if (l == C - 1)
+#pragma unroll
+                for (int i = 0; i < 2 * NW; ++i) x += s_ext[i];
+            const int part = s_g.part[l];
+#pragma unroll
+            for (int d = 1; d < C; d *= 2) {
+                const float o = __shfl_down(x, d);
+                const int p = __shfl_down(part, d);
+                if (l + d < C && p == part) x += o;
+            }
+            if (l < rows) {
+                *at_out<float>(a.dg, w.b, t0 + l, w.h) = l < len && *at<float>(a.g, w.b, t0 + l, w.h) != NEG_INF ? x : 0.f;
+                *at_out<float>(a.dbeta, w.b, t0 + l, w.h) = l < len ? s_yr[l] + s_b[0][l] + s_b[1][l] : 0.f;
             }
         }
     }
-    // dY.R of one row lies in the lanes c, c + 16, c + 32, c + 48 (zero in the second half's wavefronts)
-    yr += __shfl_xor(yr, 16);
-    yr += __shfl_xor(yr, 32);
+    const int c = threadIdx.x & 15, i0 = 16 * strip + ((threadIdx.x & 63) >> 4) * 4;
+    w.h -= 1;                               // the head whose row of the partial sums this is (heads_wg = 1)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float b = sum16(kft[r]) + __shfl(yr, 4 * q + r), g = sum16(kdot[r]);
-        if (c == 0) { s_dG[half][i0 + r] = g; s_b[half][i0 + r] = b; }
-    }
-    ext += damp(s_g.last, ss);
-    ext = sum16(ext);
-    ext += __shfl_xor(ext, 16);
-    ext += __shfl_xor(ext, 32);
-    if (l == 0) s_ext[wave] = ext;
-    __syncthreads();
-    if (wave == 0) {                        // sums from the end to each token, within its segment
-        float x = l < C ? s_dG[0][l] + s_dG[1][l] : 0.f;
-        if (l == C - 1)
+    for (int n = 0; n < NK; ++n) {
+        const int d = 16 * (n0 + n) + c;
 #pragma unroll
-            for (int i = 0; i < 2 * NW; ++i) x += s_ext[i];
-        const int part = s_g.part[l];
-#pragma unroll
-        for (int d = 1; d < C; d *= 2) {
-            const float o = __shfl_down(x, d);
-            const int p = __shfl_down(part, d);
-            if (l + d < C && p == part) x += o;
-        }
-        if (l < rows) {
-            *at_out<float>(a.dg, w.b, t0 + l, w.h) = l < len && *at<float>(a.g, w.b, t0 + l, w.h) != NEG_INF ? x : 0.f;
-            *at_out<float>(a.dbeta, w.b, t0 + l, w.h) = l < len ? s_b[0][l] + s_b[1][l] : 0.f;
-        }
+        for (int r = 0; r < 4; ++r)
+            if (i0 + r < rows && d < dk) {
+                const bool in = i0 + r < len;
+                put(a.dq, a.part_q, i0 + r, d, in ? sum_q[n][r] : 0.f);
+                put(a.dk, a.part_k, i0 + r, d, in ? sum_k[n][r] : 0.f);
+            }
     }
 }
 
@@ -1324,6 +1491,7 @@ __global__ __launch_bounds__(256) void delta_group_kernel(DeltaArgs a) {
 // ---- launches -------------------------------------------------------------------------------
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 struct Plan {                               // padded sizes, and where things lie in `saved` and the workspace
+    int heads_wg;                           // value heads that one workgroup of delta_back_kernel takes: those of a key head where that fills the card
     int c, dkp, dvp, chunks;                // c: tokens per chunk; 32 where no sequence is longer: half the rows of 64 would be empty
     size_t T, P, G, KT, forward;            // offsets in bytes; `forward`: what a call without `saved` needs
     size_t TT, PT, QT, R, S, saved;
@@ -1351,7 +1519,8 @@ Plan plan_of(const pql_delta_shape& s) {
     p.saved = o;
     o = 0;
     p.dX = take(n * p.c * p.dvp * 4); p.dY = take(n * p.c * p.dvp * 4); p.dS = take(n * p.dkp * p.dvp * 4);
-    const size_t part = s.heads_v == s.heads_k ? 0 : (size_t)s.batch * s.steps * s.heads_v * s.dim_k;
+    p.heads_wg = (int64_t)s.batch * s.heads_k * p.chunks < 512 ? 1 : s.heads_v / s.heads_k;
+    const size_t part = s.heads_v == s.heads_k || p.heads_wg > 1 ? 0 : (size_t)s.batch * s.steps * s.heads_v * s.dim_k;
     p.part_q = take(part * 4); p.part_k = take(part * 4);
     p.back = o;
     return p;
@@ -1451,19 +1620,21 @@ template <typename M, int C, int DK, bool AL> struct Chunked {
     }
     static hipError_t backward(const DeltaArgs& all, hipStream_t st) {
         const hipError_t e = by_batch(all, [&](const DeltaArgs& a) {
-            static LdsLimit l_scan, l_narrow, l_back;
+            static LdsLimit l_scan, l_narrow, l_back[2];
             const double th = token_heads(a), es = sizeof(typename M::E);
             const double flops = th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, bytes = th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C + 8.0 * a.dim_v);
             hipError_t e = narrow(a) ? launch(delta_back_scan_kernel<M, C, DK, 1, AL>, l_narrow, BackScanLds<M, C, DK, 1>::BYTES,
                                               dim3(a.dvp / 16 * a.batch * a.heads_v), 8 * C, a, KID_DELTA_BACK_SCAN, flops, bytes, st)
                                      : launch(delta_back_scan_kernel<M, C, DK, 2, AL>, l_scan, BackScanLds<M, C, DK, 2>::BYTES,
                                               dim3(a.dvp / 32 * a.batch * a.heads_v), 8 * C, a, KID_DELTA_BACK_SCAN, flops, bytes, st);
-            if (e == hipSuccess && a.chunks > 0)
-                e = launch(delta_back_kernel<M, C, DK, AL>, l_back, BackLds<M, C, DK>::BYTES, dim3(a.chunks, a.batch * a.heads_v), 8 * C, a, KID_DELTA_BACK,
-                           th * (6.0 * a.dim_k * a.dim_v + 4.0 * C * a.dim_v + 8.0 * C * a.dim_k), th * (es * (4 * a.dim_k + a.dim_v) + 12.0 * a.dim_v), st);
-            return e;
+            if (e != hipSuccess || a.chunks == 0) return e;
+            auto parallel = [&](auto kernel, LdsLimit& lim) {
+                return launch(kernel, lim, BackLds<M, C, DK>::BYTES, dim3(a.chunks, a.batch * (a.heads_v / a.heads_wg)), 8 * C, a, KID_DELTA_BACK,
+                              th * (6.0 * a.dim_k * a.dim_v + 4.0 * C * a.dim_v + 8.0 * C * a.dim_k), th * (es * (4 * a.dim_k + a.dim_v) + 12.0 * a.dim_v), st);
+            };
+            return a.heads_wg > 1 ? parallel(delta_back_kernel<M, C, DK, AL, true>, l_back[0]) : parallel(delta_back_kernel<M, C, DK, AL, false>, l_back[1]);
         });
-        if (e != hipSuccess || all.group == 1 || all.steps == 0) return e;
+        if (e != hipSuccess || all.part_q == nullptr || all.steps == 0) return e;
         const int64_t n = 2 * (int64_t)all.batch * all.steps * all.heads_k * all.dim_k;
         const int64_t blocks = (n + 255) / 256 < 4096 ? (n + 255) / 256 : 4096;
         const ProfSlot ps = prof_slot();
@@ -1566,7 +1737,8 @@ int32_t pql_delta_backward(pql_ctx* c, const pql_delta_shape* s, const pql_delta
     a.out_grad = seq(out_grad); a.state_grad = state_out_grad;
     a.dq = seq(g->q); a.dk = seq(g->k); a.dv = seq(g->v); a.dg = seq(g->log_decay); a.dbeta = seq(g->beta); a.dstate = g->state;
     a.dX = (float*)(w + p.dX); a.dY = (float*)(w + p.dY); a.dS = (float*)(w + p.dS);
-    if (a.group > 1) { a.part_q = (float*)(w + p.part_q); a.part_k = (float*)(w + p.part_k); }
+    a.heads_wg = p.heads_wg;
+    if (a.group > 1 && p.heads_wg == 1) { a.part_q = (float*)(w + p.part_q); a.part_k = (float*)(w + p.part_k); }
     const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype) && rows_aligned(out_grad, s->dim_v, s->dtype) &&
                     rows_aligned(g->v, s->dim_v, s->dtype);
     const hipError_t e = s->dtype == PQL_F32 ? chunks_dispatch<ModeF>(a, true, al, p, (hipStream_t)stream)

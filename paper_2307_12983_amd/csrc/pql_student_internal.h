@@ -38,6 +38,7 @@ struct DeltaArgs {
     int batch, steps, heads_k, heads_v, group, dim_k, dim_v;
     int chunks, dvp;                    // chunks of a full sequence; dim_v padded for the arrays below
     int bh0;                            // first (sequence, head) of this launch
+    int heads_wg;                       // value heads per workgroup of the gradient's parallel part
     float scale;
     DeltaSeq q, k, v, g, beta, out;
     const int* lengths;

@@ -459,3 +459,14 @@ def test_windows_of_at_most_32_tokens(env, size, dtype):
     close(got[1], state, "state")
     for name, x, y in zip(("dq", "dk", "dv", "dg", "dbeta", "dstate"), d.backward(got[2]), want):
         close(x, y, name)
+
+
+@pytest.mark.parametrize("dtype,size", [("float32", (512, 3, 1, 2, 16, 8)), ("bfloat16", (86, 130, 2, 6, 8, 12)), ("float32", (43, 129, 4, 8, 70, 8))])
+def test_gradients_of_shared_heads_in_large_calls(env, dtype, size):
+    """Enough chunks for one workgroup to take all value heads of a key head."""
+    n, t = size[:2]
+    rng = np.random.default_rng(1)
+    lens = rng.integers(0, t + 1, n).tolist()
+    d = Delta(env, *size, dtype=dtype, lengths=lens, resets=[(b, int(rng.integers(0, t))) for b in range(0, n, 3)], seed=7)
+    for name, got, want in zip(("dq", "dk", "dv", "dg", "dbeta", "dstate"), d.backward(d.forward(True)[2]), d.want_grads()):
+        close(got, want, name)
