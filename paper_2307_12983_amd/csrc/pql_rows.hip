@@ -15,17 +15,29 @@ constexpr int SMALL_VOCAB = 1024;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -__builtin_inff();
 
+// 2^x by the one instruction: results below 2^-126 become 0, which no sum or gradient here can tell from their value.
+__device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
+
 // ---- reductions -----------------------------------------------------------------------------
-template <int G> __device__ __forceinline__ float group_max(float x) {
-#pragma unroll
-    for (int d = 1; d < G; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
-    return x;
+// Lane i gets the value of the lane that differs in one bit of the number; below 16 as a modifier of the instruction that
+// uses it (mirrors instead of the bits 4 and 8: lanes of one half hold equal values by then), above through the LDS crossbar.
+template <int D> __device__ __forceinline__ int other(int x) {
+    if constexpr (D == 1) return __builtin_amdgcn_update_dpp(x, x, 0xB1, 0xf, 0xf, false);
+    else if constexpr (D == 2) return __builtin_amdgcn_update_dpp(x, x, 0x4E, 0xf, 0xf, false);
+    else if constexpr (D == 4) return __builtin_amdgcn_update_dpp(x, x, 0x141, 0xf, 0xf, false);
+    else if constexpr (D == 8) return __builtin_amdgcn_update_dpp(x, x, 0x140, 0xf, 0xf, false);
+    else return __shfl_xor(x, D);
 }
-template <int G, typename V> __device__ __forceinline__ V group_sum(V x) {
-#pragma unroll
-    for (int d = 1; d < G; d *= 2) x += __shfl_xor(x, d);
-    return x;
+template <int D> __device__ __forceinline__ float other(float x) { return __int_as_float(other<D>(__float_as_int(x))); }
+template <int D> __device__ __forceinline__ unsigned other(unsigned x) { return (unsigned)other<D>((int)x); }
+template <int G, int D = 1, typename V, typename F> __device__ __forceinline__ V group_reduce(V x, F f) {
+    if constexpr (D < G) return group_reduce<G, 2 * D>(f(x, other<D>(x)), f);
+    else return x;
 }
+template <int G> __device__ __forceinline__ float group_max(float x) { return group_reduce<G>(x, [](float a, float b) { return fmaxf(a, b); }); }
+template <int G> __device__ __forceinline__ unsigned group_max(unsigned x) { return group_reduce<G>(x, [](unsigned a, unsigned b) { return a > b ? a : b; }); }
+template <int G> __device__ __forceinline__ int group_min(int x) { return group_reduce<G>(x, [](int a, int b) { return a < b ? a : b; }); }
+template <int G, typename V> __device__ __forceinline__ V group_sum(V x) { return group_reduce<G>(x, [](V a, V b) { return a + b; }); }
 // Over a workgroup of NT threads; every thread gets the result.  `s` holds NT / 64 values and may be used again after the
 // next barrier (each call begins with one).
 template <int NT> __device__ __forceinline__ float block_max(float x, float* s) {
@@ -78,51 +90,108 @@ template <> __device__ __forceinline__ void unpack<bf16_t>(uint4 g, float* x) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
 }
+// A stretch held in registers, NV granules and at most one single element per thread of NT; what lies behind it is -inf.
+template <typename E, int NT, int NV> struct Held {
+    static constexpr int VEC = Stretch<E>::VEC;
+    uint4 g[NV];
+    float one;
+    int at;                                 // place of the single element, or -1
+    __device__ __forceinline__ explicit Held(const Stretch<E>& st, int t = threadIdx.x) {
+        const unsigned low = sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u;
+        at = st.single(t);
+        one = at >= 0 ? to_float(st.p[at]) : NEG_INF;
+        // all requests go out together: places behind the end read the last granule, and are overwritten
+        if (st.vecs == 0) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) g[i] = make_uint4(low, low, low, low);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) g[i] = st.granule(min(t + i * NT, st.vecs - 1));
+        if (st.vecs < NT * NV) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (t + i * NT >= st.vecs) g[i] = make_uint4(low, low, low, low);
+        }
+    }
+    // The granule's values.  Taken apart anew at every use: kept, the values of 16-bit granules would need twice the registers.
+    __device__ __forceinline__ void values(int i, float* x) {
+        if (sizeof(E) == 2) asm volatile("" : "+v"(g[i].x), "+v"(g[i].y), "+v"(g[i].z), "+v"(g[i].w));
+        unpack<E>(g[i], x);
+    }
+    template <typename F> __device__ __forceinline__ void each(F&& f) {       // f(value, its place in the granule)
+        f(one, 0);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float x[VEC];
+            values(i, x);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) f(x[j], j);
+        }
+    }
+};
+// Packed by hand: written as elements in both branches, the two become one that stores them singly.
+__device__ __forceinline__ unsigned pack2(float x, float y) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((f2{x, y}), b2));
+}
 template <typename E> __device__ __forceinline__ void store_granule(E* p, bool aligned, const float* x) {
-    constexpr int VEC = 16 / (int)sizeof(E);
+    uint4 u;
+    if constexpr (sizeof(E) == 4) u = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    else u = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
     if (aligned) {
-        union { E e[VEC]; uint4 u; } w;
+        *(uint4*)p = u;
+        return;
+    }
+    const unsigned w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) w.e[i] = from_float<E>(x[i]);
-        *(uint4*)p = w.u;
-    } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) p[i] = from_float<E>(x[i]);
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(E) == 4) {
+            ((unsigned*)p)[i] = w[i];
+        } else {
+            ((unsigned short*)p)[2 * i] = (unsigned short)w[i];
+            ((unsigned short*)p)[2 * i + 1] = (unsigned short)(w[i] >> 16);
+        }
     }
 }
 
 // ---- the teacher's list ------------------------------------------------------------------------
 // p_k = softmax of the valid entries' values / t, by the first `top` threads of a workgroup.  Entries of one answer are
 // added up at the first of them, in the order of the list: `sum` is the whole mass of this thread's answer if it is that
-// first entry (`owner`).  Returns whether the row has a valid entry at all.
-struct Entry { int index; float p, log_p, sum; bool owner; };
-template <int NT>
-__device__ __forceinline__ bool teacher_entries(const DistillArgs& a, int64_t n, Entry& e, int* s_index, float* s_p, float* s_red) {
+// first entry (`owner`).
+struct Entry { int index; float y, p, log_p, sum; bool owner; };
+// What of a row's list and weight this thread holds: requested together, one wait.
+__device__ __forceinline__ float entry_of(const DistillArgs& a, int64_t n, Entry& e) {
     const int k = threadIdx.x;
-    e.index = -1; e.p = 0.f; e.log_p = 0.f; e.sum = 0.f; e.owner = false;
+    int i = -1;
     float y = NEG_INF;
-    if (k < a.top) {
-        const int i = a.index[n * a.top + k];
-        if ((unsigned)i < (unsigned)a.vocab) y = a.value[n * a.top + k];
-        if (y != NEG_INF) e.index = i;
-    }
-    const float big = block_max<NT>(y, s_red);
-    const bool some = __syncthreads_or(e.index >= 0);
-    const float shift = big == NEG_INF ? 0.f : big;
-    const float x = (y - shift) * a.inv_temp, m = e.index >= 0 ? expf(x) : 0.f;
+    if (k < a.top) { i = a.index[n * a.top + k]; y = a.value[n * a.top + k]; }
+    const float w = a.weight ? a.weight[n] : 1.f;
+    const bool ok = (unsigned)i < (unsigned)a.vocab && y != NEG_INF;
+    e.index = ok ? i : -1;
+    e.y = ok ? y : NEG_INF;
+    return w;
+}
+template <int NT>
+__device__ __forceinline__ void entry_masses(const DistillArgs& a, Entry& e, int* s_index, float* s_p, float* s_red) {
+    const int k = threadIdx.x;
+    e.p = 0.f; e.log_p = 0.f; e.sum = 0.f; e.owner = false;
+    const float big = block_max<NT>(e.y, s_red);
+    const float x = (e.y - (big == NEG_INF ? 0.f : big)) * a.inv_temp, m = e.index >= 0 ? expf(x) : 0.f;
     const float total = block_sum<NT>(m, s_red);
     if (e.index >= 0) { e.p = m / total; e.log_p = x - logf(total); }
     if (k < a.top) { s_index[k] = e.index; s_p[k] = e.p; }
     __syncthreads();
-    if (e.index >= 0) {
+    if (e.index >= 0) {                     // no early end: the reads of the whole list are then on their way together
         e.owner = true;
-        for (int i = 0; i < a.top; ++i)
-            if (s_index[i] == e.index) {
-                if (i < k) { e.owner = false; break; }
-                e.sum += s_p[i];
-            }
+#pragma unroll 8
+        for (int i = 0; i < a.top; ++i) {
+            const bool same = s_index[i] == e.index;
+            e.owner = e.owner && !(same && i < k);
+            e.sum += same ? s_p[i] : 0.f;
+        }
     }
-    return some;
 }
 // One entry's share of the loss: p (log p - log q) with log q = (z - m) / t - log(s); nothing for p = 0, +inf where the
 // student has the answer at -inf (also in a row that holds nothing else).
@@ -183,11 +252,12 @@ __global__ __launch_bounds__(256) void distill_small_kernel(DistillArgs a) {
         if (i < 0) continue;
         float sum = 0.f;
         bool owner = true;
-        for (int q = 0; q < a.top; ++q)
-            if (s_index[q] == i) {
-                if (q < k) { owner = false; break; }
-                sum += s_p[q];
-            }
+#pragma unroll 8
+        for (int q = 0; q < a.top; ++q) {
+            const bool same = s_index[q] == i;
+            owner = owner && !(same && q < k);
+            sum += same ? s_p[q] : 0.f;
+        }
         if (owner) s_t[i] = sum;
     }
     __syncthreads();
@@ -205,7 +275,7 @@ __global__ __launch_bounds__(256) void distill_small_kernel(DistillArgs a) {
     float s = 0.f, q[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        q[r] = BACK ? exp2f(fmaf(-m, a.temp, z[r]) * c) : exp2f((z[r] - m) * c);
+        q[r] = BACK ? exp2_raw(fmaf(-m, a.temp, z[r]) * c) : exp2_raw((z[r] - m) * c);
         s += q[r];
     }
     if (BACK) {
@@ -239,6 +309,132 @@ __global__ __launch_bounds__(256) void distill_small_kernel(DistillArgs a) {
 }
 
 // =============================================================================================
+// Rows of up to 64 NV granules: one wavefront per row, the row in its registers.  A workgroup per row would spend more time
+// in barriers and waiting for its own first loads than on the row (65536 rows of 1500 bf16: MEASURED).
+// =============================================================================================
+__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
+
+template <typename E, int NV, bool BACK>
+__global__ __launch_bounds__(256) void distill_wave_kernel(DistillArgs a) {
+    constexpr int VEC = Stretch<E>::VEC, Q = PQL_MAX_TOP / 64;
+    __shared__ int s_index_all[4][PQL_MAX_TOP];
+    __shared__ float s_p_all[4][PQL_MAX_TOP];
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63;
+    const int64_t n = (int64_t)blockIdx.x * 4 + wave;
+    if (n >= a.rows) return;                // wavefronts share nothing
+    int* s_index = s_index_all[wave];
+    float* s_p = s_p_all[wave];
+    int index[Q];
+    float y[Q], zk[Q] = {}, sum[Q] = {}, big = NEG_INF;
+    const float w = a.weight ? a.weight[n] : 1.f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int k = l + 64 * q;
+        index[q] = -1; y[q] = NEG_INF;
+        if (k < a.top) { index[q] = a.index[n * a.top + k]; y[q] = a.value[n * a.top + k]; }
+    }
+    bool some = false;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const bool ok = (unsigned)index[q] < (unsigned)a.vocab && y[q] != NEG_INF;
+        if (!ok) { index[q] = -1; y[q] = NEG_INF; }
+        some |= ok;
+        big = fmaxf(big, y[q]);
+    }
+    E* out = (E*)a.grad + n * a.grad_stride;
+    if (!__any(some) || w == 0.f) {
+        if (!BACK && l == 0) { a.loss_out[n] = 0.f; a.lse_out[n] = 0.f; }
+        if (a.grad) for (int j = l; j < a.vocab; j += 64) out[j] = from_float<E>(0.f);
+        return;
+    }
+    const E* row = (const E*)a.z + n * a.stride;
+    const Stretch<E> st(row, a.vocab);
+    Held<E, 64, NV> h(st, l);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) if (index[q] >= 0) zk[q] = to_float(row[index[q]]);
+    const float lse = BACK ? a.lse[n] : 0.f;
+    // the list's masses; entries of one answer are added up at the first of them, in the order of the list
+    big = group_max<64>(big);
+    if (big == NEG_INF) big = 0.f;
+    float total = 0.f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) total += index[q] >= 0 ? expf((y[q] - big) * a.inv_temp) : 0.f;
+    total = group_sum<64>(total);
+    const float log_total = logf(total);
+    bool owner[Q];
+    float lp[Q];                            // log p
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int k = l + 64 * q;
+        const float x = (y[q] - big) * a.inv_temp;
+        lp[q] = x - log_total;
+        owner[q] = index[q] >= 0;
+        y[q] = owner[q] ? expf(x) / total : 0.f;                     // p from here on
+        if (k < a.top) { s_index[k] = index[q]; s_p[k] = y[q]; }
+    }
+    wave_fence();
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        if (64 * q >= a.top) break;
+        const int k = l + 64 * q;
+#pragma unroll 8
+        for (int i = 0; i < a.top; ++i) {
+            const bool same = s_index[i] == index[q];
+            owner[q] = owner[q] && !(same && i < k);
+            sum[q] += same ? s_p[i] : 0.f;
+        }
+    }
+    const float c = LOG2E * a.inv_temp, t_m = BACK ? a.temp : 1.f;
+    float m, inv;
+    if (BACK) {
+        m = lse == NEG_INF ? 0.f : lse;
+        inv = lse == NEG_INF ? 0.f : 1.f;
+    } else {
+        m = NEG_INF;
+        h.each([&](float x, int) { m = fmaxf(m, x); });
+        m = group_max<64>(m);
+        if (m == NEG_INF) m = 0.f;
+        float part[4] = {};
+        h.each([&](float x, int j) { part[j & 3] += exp2_raw((x - m) * c); });
+        const float s = group_sum<64>((part[0] + part[1]) + (part[2] + part[3])), log_s = logf(s);
+        inv = s > 0.f || s != s ? 1.f / s : 0.f;
+        float loss = 0.f;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            Entry e;
+            e.p = y[q];
+            e.log_p = lp[q];
+            if (index[q] >= 0) loss += entry_loss(e, zk[q], m, a.inv_temp, log_s);
+        }
+        loss = group_sum<64>(loss);
+        if (l == 0) {
+            a.loss_out[n] = w * a.temp * a.temp * loss;
+            a.lse_out[n] = m * a.inv_temp + log_s;
+        }
+        if (!a.grad) return;
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q) asm volatile("" ::"v"(zk[q]));       // they are there before the gradient may be written over them
+    const float f = w * a.temp, fi = f * inv;
+    const bool aligned = (((uintptr_t)(out + st.head)) & 15) == 0;
+    if (h.at >= 0) out[h.at] = from_float<E>(exp2_raw(fmaf(-m, t_m, h.one) * c) * fi);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int v = l + i * 64;
+        if (v >= st.vecs) break;
+        float x[VEC];
+        h.values(i, x);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[j] = exp2_raw(fmaf(-m, t_m, x[j]) * c) * fi;
+        store_granule<E>(out + st.place(v), aligned, x);
+    }
+    wave_fence();                           // the dense gradient of the listed answers lies before its correction
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+        if (owner[q]) out[index[q]] = from_float<E>(f * ((inv != 0.f ? exp2_raw(fmaf(-m, t_m, zk[q]) * c) * inv : 0.f) - sum[q]));
+}
+
+// =============================================================================================
 // Long rows.  A piece is a stretch of a row; one workgroup per piece.
 // =============================================================================================
 // Running maximum and sum of exp((z - m) c) over a stretch, of this thread's elements.
@@ -262,9 +458,9 @@ __device__ __forceinline__ void stretch_stats(const Stretch<E>& st, float c, flo
 #pragma unroll
             for (int i = 0; i < VEC; ++i) b = fmaxf(b, x[i]);
             const float ref = b == NEG_INF ? 0.f : b;
-            s *= exp2f((m - ref) * c);
+            s *= exp2_raw((m - ref) * c);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) s += exp2f((x[i] - ref) * c);
+            for (int i = 0; i < VEC; ++i) s += exp2_raw((x[i] - ref) * c);
             m = b;
         }
     }
@@ -272,7 +468,7 @@ __device__ __forceinline__ void stretch_stats(const Stretch<E>& st, float c, flo
 // The same joined over the workgroup; m is 0 where the stretch holds nothing but -inf (and s = 0).
 template <int NT> __device__ __forceinline__ void join_stats(float c, float& m, float& s, float* s_red) {
     const float b = block_max<NT>(m, s_red), ref = b == NEG_INF ? 0.f : b;
-    s *= exp2f((m - ref) * c);
+    s *= exp2_raw((m - ref) * c);
     if (m == NEG_INF) s = s != s ? s : 0.f;
     s = block_sum<NT>(s, s_red);
     m = ref;
@@ -287,7 +483,7 @@ __device__ __forceinline__ void stretch_grad(const Stretch<E>& st, E* out, float
     const float fi = f * inv;
     const bool aligned = (((uintptr_t)(out + st.head)) & 15) == 0;
     const int one = st.single(t);
-    if (one >= 0) out[one] = from_float<E>(exp2f(fmaf(-m, t_m, to_float(st.p[one])) * c) * fi);
+    if (one >= 0) out[one] = from_float<E>(exp2_raw(fmaf(-m, t_m, to_float(st.p[one])) * c) * fi);
     for (int v = t; v < st.vecs; v += UNROLL * NT) {
         uint4 g[UNROLL];
 #pragma unroll
@@ -298,7 +494,7 @@ __device__ __forceinline__ void stretch_grad(const Stretch<E>& st, E* out, float
             float x[VEC];
             unpack<E>(g[u], x);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) x[i] = exp2f(fmaf(-m, t_m, x[i]) * c) * fi;
+            for (int i = 0; i < VEC; ++i) x[i] = exp2_raw(fmaf(-m, t_m, x[i]) * c) * fi;
             store_granule<E>(out + st.place(v + u * NT), aligned, x);
         }
     }
@@ -307,39 +503,75 @@ template <typename E, int NT> __device__ __forceinline__ void zero_stretch(E* ou
     for (int j = threadIdx.x; j < len; j += NT) out[j] = from_float<E>(0.f);
 }
 
-// One workgroup per row: statistics, then the gradient from a second read of the row.
-template <typename E, int NT>
+// One workgroup per row.  NV > 0: the row stays in registers between its statistics and its gradient, NV granules a thread;
+// NV = 0, rows that do not fit: it is read again.
+template <typename E, int NT, int NV>
 __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a) {
+    constexpr int VEC = Stretch<E>::VEC;
     __shared__ int s_index[PQL_MAX_TOP];
     __shared__ float s_p[PQL_MAX_TOP], s_red[NT / 64];
     const int64_t n = blockIdx.x;
-    const float w = a.weight ? a.weight[n] : 1.f;
-    Entry e;
-    const bool some = teacher_entries<NT>(a, n, e, s_index, s_p, s_red);
     E* out = (E*)a.grad + n * a.grad_stride;
-    if (!some || w == 0.f) {
+    const E* row = (const E*)a.z + n * a.stride;
+    Entry e;
+    const float w = entry_of(a, n, e);
+    if (!__syncthreads_or(e.index >= 0) || w == 0.f) {
         if (threadIdx.x == 0) { a.loss_out[n] = 0.f; a.lse_out[n] = 0.f; }
         if (a.grad) zero_stretch<E, NT>(out, a.vocab);
         return;
     }
-    const E* row = (const E*)a.z + n * a.stride;
     const Stretch<E> st(row, a.vocab);
-    const float zk = e.index >= 0 ? to_float(row[e.index]) : 0.f;
     const float c = LOG2E * a.inv_temp;
+    const float zk = e.index >= 0 ? to_float(row[e.index]) : 0.f;
     float m, s;
-    stretch_stats<E, NT>(st, c, m, s);
-    join_stats<NT>(c, m, s, s_red);
-    const float log_s = logf(s), inv = s > 0.f || s != s ? 1.f / s : 0.f;
-    const float loss = block_sum<NT>(e.index >= 0 ? entry_loss(e, zk, m, a.inv_temp, log_s) : 0.f, s_red);
-    if (threadIdx.x == 0) {
-        a.loss_out[n] = w * a.temp * a.temp * loss;
-        a.lse_out[n] = m * a.inv_temp + log_s;
+    if constexpr (NV > 0) {
+        Held<E, NT, NV> h(st);              // on its way while the list is worked out
+        entry_masses<NT>(a, e, s_index, s_p, s_red);
+        m = NEG_INF;
+        h.each([&](float x, int) { m = fmaxf(m, x); });
+        m = block_max<NT>(m, s_red);
+        if (m == NEG_INF) m = 0.f;
+        float part[4] = {};                 // four sums: one would wait for itself
+        h.each([&](float x, int j) { part[j & 3] += exp2_raw((x - m) * c); });
+        s = block_sum<NT>((part[0] + part[1]) + (part[2] + part[3]), s_red);
+        const float log_s = logf(s), inv = s > 0.f || s != s ? 1.f / s : 0.f;
+        const float loss = block_sum<NT>(e.index >= 0 ? entry_loss(e, zk, m, a.inv_temp, log_s) : 0.f, s_red);
+        if (threadIdx.x == 0) {
+            a.loss_out[n] = w * a.temp * a.temp * loss;
+            a.lse_out[n] = m * a.inv_temp + log_s;
+        }
+        if (!a.grad) return;
+        const float f = w * a.temp, fi = f * inv;
+        const bool aligned = (((uintptr_t)(out + st.head)) & 15) == 0;
+        if (h.at >= 0) out[h.at] = from_float<E>(exp2_raw((h.one - m) * c) * fi);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = threadIdx.x + i * NT;
+            if (v >= st.vecs) break;
+            float x[VEC];
+            h.values(i, x);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) x[j] = exp2_raw((x[j] - m) * c) * fi;
+            store_granule<E>(out + st.place(v), aligned, x);
+        }
+        __syncthreads();                    // the dense gradient of the listed answers lies before its correction
+        if (e.owner) out[e.index] = from_float<E>(f * ((inv != 0.f ? exp2_raw((zk - m) * c) * inv : 0.f) - e.sum));
+    } else {
+        entry_masses<NT>(a, e, s_index, s_p, s_red);
+        stretch_stats<E, NT>(st, c, m, s);
+        join_stats<NT>(c, m, s, s_red);
+        const float log_s = logf(s), inv = s > 0.f || s != s ? 1.f / s : 0.f;
+        const float loss = block_sum<NT>(e.index >= 0 ? entry_loss(e, zk, m, a.inv_temp, log_s) : 0.f, s_red);
+        if (threadIdx.x == 0) {
+            a.loss_out[n] = w * a.temp * a.temp * loss;
+            a.lse_out[n] = m * a.inv_temp + log_s;
+        }
+        if (!a.grad) return;
+        const float f = w * a.temp;
+        stretch_grad<E, NT>(st, out, c, m, 1.f, inv, f);
+        __syncthreads();
+        if (e.owner) out[e.index] = from_float<E>(f * ((inv != 0.f ? exp2_raw((zk - m) * c) * inv : 0.f) - e.sum));
     }
-    if (!a.grad) return;
-    const float f = w * a.temp;
-    stretch_grad<E, NT>(st, out, c, m, 1.f, inv, f);
-    __syncthreads();                        // the dense gradient of the listed answers lies before its correction
-    if (e.owner) out[e.index] = from_float<E>(f * ((inv != 0.f ? exp2f((zk - m) * c) * inv : 0.f) - e.sum));
 }
 
 // Few rows: pieces of a.piece elements.  First launch: each piece's maximum and sum, and the logits of the listed
@@ -372,15 +604,15 @@ __global__ __launch_bounds__(NT) void distill_piece_kernel(DistillArgs a) {
     __shared__ float s_p[PQL_MAX_TOP], s_red[NT / 64];
     const int64_t n = blockIdx.y;
     const int j0 = blockIdx.x * a.piece, len = min(a.piece, a.vocab - j0);
-    const float w = a.weight ? a.weight[n] : 1.f;
     Entry e;
-    const bool some = teacher_entries<NT>(a, n, e, s_index, s_p, s_red);
+    const float w = entry_of(a, n, e);
     E* out = (E*)a.grad + n * a.grad_stride + j0;
-    if (!some || w == 0.f) {
+    if (!__syncthreads_or(e.index >= 0) || w == 0.f) {
         if (JOIN && blockIdx.x == 0 && threadIdx.x == 0) { a.loss_out[n] = 0.f; a.lse_out[n] = 0.f; }
         if (a.grad) zero_stretch<E, NT>(out, len);
         return;
     }
+    entry_masses<NT>(a, e, s_index, s_p, s_red);
     const E* row = (const E*)a.z + n * a.stride + j0;
     const float c = LOG2E * a.inv_temp;
     float m, inv, zk = 0.f;
@@ -415,7 +647,7 @@ __global__ __launch_bounds__(NT) void distill_piece_kernel(DistillArgs a) {
     const float f = w * a.temp;
     stretch_grad<E, NT>(Stretch<E>(row, len), out, c, m, t_m, inv, f);
     __syncthreads();
-    if (e.owner && mine) out[e.index - j0] = from_float<E>(f * ((inv != 0.f ? exp2f(fmaf(-m, t_m, zk) * c) * inv : 0.f) - e.sum));
+    if (e.owner && mine) out[e.index - j0] = from_float<E>(f * ((inv != 0.f ? exp2_raw(fmaf(-m, t_m, zk) * c) * inv : 0.f) - e.sum));
 }
 
 // =============================================================================================
@@ -501,32 +733,77 @@ __global__ __launch_bounds__(256) void top_small_kernel(TopArgs a) {
     }
 }
 
+// Short lists of small vocabularies: K rounds of the largest key left and its lowest index (V = 51, K = 8: MEASURED).
+template <typename E, int G, int R>
+__global__ __launch_bounds__(256) void top_rounds_kernel(TopArgs a) {
+    constexpr int ROWS = 256 / G;
+    const int g = threadIdx.x / G, l = threadIdx.x & (G - 1);
+    const int64_t n = (int64_t)blockIdx.x * ROWS + g;
+    if ((int64_t)blockIdx.x * ROWS + (threadIdx.x & ~63) / G >= a.rows) return;       // whole wavefronts
+    const bool in = n < a.rows;
+    const E* row = (const E*)a.z + n * a.stride;
+    unsigned key[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int j = l + G * r;
+        key[r] = in && j < a.vocab ? key_of(to_float(row[j])) : 0u;
+    }
+    // results stay with the lanes until a group's row of them can be written together
+    int index = -1;
+    unsigned value = 0;
+    for (int k = 0; k < a.top; ++k) {
+        unsigned big = key[0];
+#pragma unroll
+        for (int r = 1; r < R; ++r) big = max(big, key[r]);
+        big = group_max<G>(big);
+        int at = 0x7fffffff;
+#pragma unroll
+        for (int r = R - 1; r >= 0; --r) at = key[r] == big ? l + G * r : at;
+        at = group_min<G>(at);
+#pragma unroll
+        for (int r = 0; r < R; ++r) key[r] = l + G * r == at ? 0u : key[r];
+        if ((k & (G - 1)) == l) { index = big ? at : -1; value = big; }
+        if ((k & (G - 1)) == G - 1 || k == a.top - 1) {
+            const int place = (k & ~(G - 1)) + l;
+            if (in && place <= k) {
+                a.index_out[n * a.top + place] = index;
+                a.value_out[n * a.top + place] = value_of(value);
+            }
+        }
+    }
+}
+
 // Long rows.  Every thread's largest key is found in one pass; the K-th largest of those bounds the row's K-th largest
 // from below, and few elements reach it: a second pass collects them, and each is written at its rank.  Where more than
 // CAND reach it (many equal values), the K-th largest key of the row itself is found by digits, and equal ones are taken
 // in index order.
 constexpr int CAND = 2048;
 template <int NT>
-__device__ __forceinline__ unsigned kth_largest_of_threads(unsigned mine, int k, int* s_cnt) {
-    unsigned t = 0;                         // the largest t with at least k of the threads' keys >= t
-    for (int bit = 31; bit >= 0; --bit) {
-        const unsigned u = t | (1u << bit);
-        const int c = __popcll(__ballot(mine >= u));
+__device__ __forceinline__ unsigned kth_largest_of_threads(unsigned mine, int k, unsigned (*s_cnt)[NT / 64]) {
+    unsigned t = 0;                         // the largest t with at least k of the threads' keys >= t, two bits a round
+#pragma unroll 1
+    for (int bit = 30; bit >= 0; bit -= 2) {
+        const unsigned u = 1u << bit;
+        // counts of three thresholds, at most NT <= 1023 each
+        const unsigned c = __popcll(__ballot(mine >= t + u)) | __popcll(__ballot(mine >= t + 2 * u)) << 10 | __popcll(__ballot(mine >= t + 3 * u)) << 20;
+        unsigned* s = s_cnt[bit >> 1 & 1];  // two buffers: one barrier a round
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = c;
         __syncthreads();
-        if ((threadIdx.x & 63) == 0) s_cnt[threadIdx.x >> 6] = c;
-        __syncthreads();
-        int cnt = 0;
+        unsigned all = 0;
 #pragma unroll
-        for (int i = 0; i < NT / 64; ++i) cnt += s_cnt[i];
-        if (cnt >= k) t = u;
+        for (int i = 0; i < NT / 64; ++i) all += s[i];
+        const int kk = k;
+        t += (int)(all >> 20) >= kk ? 3 * u : (int)(all >> 10 & 1023) >= kk ? 2 * u : (int)(all & 1023) >= kk ? u : 0u;
     }
     return t;
 }
+// The value that a key t >= 1 stands for, as a bound for comparisons: x >= bound exactly where key_of(x) >= t.
+__device__ __forceinline__ float bound_of(unsigned t) { return t <= 0x00800000u ? -3.402823466e38f : value_of(t); }
 template <typename E, int NT, typename F>
-__device__ __forceinline__ void for_each_key(const Stretch<E>& st, F&& f) {
+__device__ __forceinline__ void for_each(const Stretch<E>& st, F&& f) {        // f(value, place)
     constexpr int VEC = Stretch<E>::VEC, UNROLL = 4;
     const int t = threadIdx.x, one = st.single(t);
-    if (one >= 0) f(key_of(to_float(st.p[one])), one);
+    if (one >= 0) f(to_float(st.p[one]), one);
     for (int v = t; v < st.vecs; v += UNROLL * NT) {
         uint4 g[UNROLL];
 #pragma unroll
@@ -537,14 +814,18 @@ __device__ __forceinline__ void for_each_key(const Stretch<E>& st, F&& f) {
             float x[VEC];
             unpack<E>(g[u], x);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) f(key_of(x[i]), st.place(v + u * NT) + i);
+            for (int i = 0; i < VEC; ++i) f(x[i], st.place(v + u * NT) + i);
         }
     }
 }
+template <typename E, int NT, typename F>
+__device__ __forceinline__ void for_each_key(const Stretch<E>& st, F&& f) {
+    for_each<E, NT>(st, [&](float x, int j) { f(key_of(x), j); });
+}
 // Writes n candidates (at most CAND, distinct) at their ranks; places without one get -1.
 template <int NT>
-__device__ __forceinline__ void write_ranked(const unsigned* s_key, const int* s_index, int n, int top, int base, int* index_out, float* value_out) {
-    for (int k = threadIdx.x; k < n; k += NT) {
+__device__ __forceinline__ void write_ranked(const unsigned* s_key, const int* s_index, int n, int top, int base, int* index_out, float* value_out, int t = threadIdx.x) {
+    for (int k = t; k < n; k += NT) {
         const unsigned mine = s_key[k];
         const int index = s_index[k];
         int rank = 0;
@@ -554,28 +835,138 @@ __device__ __forceinline__ void write_ranked(const unsigned* s_key, const int* s
         }
         if (rank < top) { index_out[rank] = base + index; value_out[rank] = value_of(mine); }
     }
-    for (int k = threadIdx.x; k < top; k += NT)
+    for (int k = t; k < top; k += NT)
         if (k >= n) { index_out[k] = -1; value_out[k] = NEG_INF; }
 }
-template <typename E, int NT>
+// Rows of up to 64 NV granules and lists of up to 64: one wavefront per row, the same steps without barriers.
+template <typename E, int NV>
+__global__ __launch_bounds__(256) void top_wave_kernel(TopArgs a) {
+    constexpr int SOME = 256, VEC = Stretch<E>::VEC;
+    __shared__ unsigned s_key_all[4][SOME];
+    __shared__ int s_index_all[4][SOME], s_n_all[4];
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63;
+    const int64_t n = (int64_t)blockIdx.x * 4 + wave;
+    if (n >= a.rows) return;                // wavefronts share nothing
+    unsigned* s_key = s_key_all[wave];
+    int* s_index = s_index_all[wave];
+    int* s_n = &s_n_all[wave];
+    const Stretch<E> st((const E*)a.z + n * a.stride, a.vocab);
+    Held<E, 64, NV> h(st, l);
+    if (l == 0) *s_n = 0;
+    float most = NEG_INF;
+    h.each([&](float x, int) { most = fmaxf(most, x); });
+    const unsigned big = key_of(most);
+    unsigned t = 0;                         // the largest t with at least K lanes' keys >= t
+    for (int bit = 31; bit >= 0; --bit) {
+        const unsigned u = t | (1u << bit);
+        if (__popcll(__ballot(big >= u)) >= a.top) t = u;
+    }
+    if (t == 0) t = 1;
+    wave_fence();
+    const float bound = bound_of(t);
+    auto collect = [&](float x, int j, bool room) {
+        const int at = atomicAdd(s_n, 1);
+        if (room || at < SOME) { s_key[at] = key_of(x); s_index[at] = j; }
+    };
+    if (h.one >= bound) collect(h.one, h.at, false);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float x[VEC], b = NEG_INF;
+        h.values(i, x);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) b = fmaxf(b, x[j]);
+        if (b >= bound) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) if (x[j] >= bound) collect(x[j], st.place(l + i * 64) + j, false);
+        }
+    }
+    wave_fence();
+    int found = *(volatile int*)s_n;
+    if (found > SOME) {                     // many equal values: the K-th largest key itself, then equal ones by index
+        unsigned lo = 0;
+#pragma unroll 1
+        for (int bit = 31; bit >= 0; --bit) {
+            const unsigned u = lo | (1u << bit);
+            int c = 0;
+            h.each([&](float x, int) { c += key_of(x) >= u; });
+            if (group_sum<64>(c) >= a.top) lo = u;
+        }
+        if (lo == 0) lo = 1;
+        wave_fence();
+        if (l == 0) *s_n = 0;
+        wave_fence();
+        if (key_of(h.one) > lo) collect(h.one, h.at, true);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float x[VEC];
+            h.values(i, x);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) if (key_of(x[j]) > lo) collect(x[j], st.place(l + i * 64) + j, true);     // fewer than K
+        }
+        wave_fence();
+        found = *(volatile int*)s_n;
+        for (int b = 0; b < a.vocab && found < a.top; b += 64) {
+            const int j = b + l;
+            const bool eq = j < a.vocab && key_of(to_float(st.p[j])) == lo;
+            const unsigned long long mask = __ballot(eq);
+            const int at = found + __popcll(mask & ((1ull << l) - 1));
+            if (eq && at < a.top) { s_key[at] = lo; s_index[at] = j; }
+            found = min(a.top, found + __popcll(mask));
+        }
+        wave_fence();
+    }
+    write_ranked<64>(s_key, s_index, found, a.top, 0, a.index_out + n * a.top, a.value_out + n * a.top, l);
+}
+
+// NV > 0: the stretch stays in registers between the two passes, NV granules a thread.
+template <typename E, int NT, int NV>
 __global__ __launch_bounds__(NT) void top_row_kernel(TopArgs a) {
-    __shared__ unsigned s_key[CAND];
+    __shared__ unsigned s_key[CAND], s_two[2][NT / 64];
     __shared__ int s_index[CAND], s_cnt[NT / 64], s_n;
     const int64_t n = blockIdx.y;
     const int j0 = blockIdx.x * a.piece, len = min(a.piece, a.vocab - j0);
     const Stretch<E> st((const E*)a.z + n * a.stride + j0, len);
     const int64_t o = (n * gridDim.x + blockIdx.x) * a.top;
     unsigned big = 0;
-    for_each_key<E, NT>(st, [&](unsigned k, int) { big = max(big, k); });
     if (threadIdx.x == 0) s_n = 0;
-    unsigned t = kth_largest_of_threads<NT>(big, a.top, s_cnt);
-    if (t == 0) t = 1;                      // fewer than K threads hold one that may be selected
-    for_each_key<E, NT>(st, [&](unsigned k, int j) {
+    auto collect = [&](unsigned k, int j, unsigned t) {
         if (k >= t) {
             const int at = atomicAdd(&s_n, 1);
             if (at < CAND) { s_key[at] = k; s_index[at] = j; }
         }
-    });
+    };
+    if constexpr (NV > 0) {
+        Held<E, NT, NV> h(st);
+        float most = NEG_INF;               // compared as they are; only the threads' results as keys
+        h.each([&](float x, int) { most = fmaxf(most, x); });
+        big = key_of(most);
+        unsigned t = kth_largest_of_threads<NT>(big, a.top, s_two);
+        if (t == 0) t = 1;                  // fewer than K threads hold one that may be selected
+        if (big >= t) {                     // few threads
+            const float bound = bound_of(t);
+            if (h.one >= bound) collect(key_of(h.one), h.at, t);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float x[Stretch<E>::VEC], b = NEG_INF;
+                h.values(i, x);
+#pragma unroll
+                for (int j = 0; j < Stretch<E>::VEC; ++j) b = fmaxf(b, x[j]);
+                if (b >= bound) {
+#pragma unroll
+                    for (int j = 0; j < Stretch<E>::VEC; ++j)
+                        if (x[j] >= bound) collect(key_of(x[j]), st.place(threadIdx.x + i * NT) + j, t);
+                }
+            }
+        }
+    } else {
+        float most = NEG_INF;
+        for_each<E, NT>(st, [&](float x, int) { most = fmaxf(most, x); });
+        big = key_of(most);
+        unsigned t = kth_largest_of_threads<NT>(big, a.top, s_two);
+        if (t == 0) t = 1;
+        const float bound = bound_of(t);
+        if (big >= t) for_each<E, NT>(st, [&](float x, int j) { if (x >= bound) collect(key_of(x), j, t); });
+    }
     __syncthreads();
     int found = s_n;
     if (found > CAND) {
@@ -657,6 +1048,8 @@ __global__ __launch_bounds__(NT) void top_merge_kernel(TopArgs a) {
 
 // ---- launches -------------------------------------------------------------------------------
 constexpr int NT_LONG = 512;
+// One wavefront per row: rows of at most 16 KB, and enough of them to give every SIMD two.
+constexpr int64_t WAVE_VECS = 64 * 16, WAVE_ROWS = 2048;
 constexpr int64_t MAX_GRID = 0x7fffffff;
 
 // Pieces of a long row: one, unless there are too few rows to fill the card's 256 CUs twice; never under 4096 elements.
@@ -699,8 +1092,9 @@ template <typename E> hipError_t top_small_launch(const TopArgs& a, double bytes
     if (a.vocab <= G * R) {                                                                                          \
         constexpr int ROWS = 256 / G;                                                                                \
         const ProfSlot ps = prof_slot();                                                                             \
-        PQL_LAUNCH(ps, (top_small_kernel<E, G, R>), dim3((unsigned)((a.rows + ROWS - 1) / ROWS)), dim3(256),         \
-                   (size_t)ROWS * 2 * a.top * 4, st, a);                                                             \
+        const dim3 grid((unsigned)((a.rows + ROWS - 1) / ROWS));                                                     \
+        if (a.top <= 16) PQL_LAUNCH(ps, (top_rounds_kernel<E, G, R>), grid, dim3(256), 0, st, a);                    \
+        else PQL_LAUNCH(ps, (top_small_kernel<E, G, R>), grid, dim3(256), (size_t)ROWS * 2 * a.top * 4, st, a);      \
         prof_commit(ps, KID_TOP_LOGITS, 0.0, bytes);                                                                 \
         return hipGetLastError();                                                                                    \
     }
@@ -727,7 +1121,17 @@ template <typename E> hipError_t distill_launch(const DistillArgs& a, bool back,
     const double bytes = read * (a.grad ? 2 : 1) + lists + 12.0 * a.rows;
     if (a.vocab <= SMALL_VOCAB)
         return back ? distill_small_launch<E, true>(a, KID_DISTILL_GRAD, bytes, st) : distill_small_launch<E, false>(a, KID_DISTILL, bytes, st);
-    if (back) {
+    const int64_t vecs = (int64_t)a.vocab * (int)sizeof(E) / 16;
+    const dim3 by_row((unsigned)a.rows), by_wave((unsigned)((a.rows + 3) / 4));
+    if (vecs <= WAVE_VECS && a.rows >= WAVE_ROWS) {
+        const ProfSlot ps = prof_slot();
+#define PQL_WAVE(NV)                                                                                            \
+    if (back) PQL_LAUNCH(ps, (distill_wave_kernel<E, NV, true>), by_wave, dim3(256), 0, st, a);                 \
+    else PQL_LAUNCH(ps, (distill_wave_kernel<E, NV, false>), by_wave, dim3(256), 0, st, a)
+        if (vecs <= 64 * 4) { PQL_WAVE(4); } else if (vecs <= 64 * 8) { PQL_WAVE(8); } else { PQL_WAVE(16); }
+#undef PQL_WAVE
+        prof_commit(ps, back ? KID_DISTILL_GRAD : KID_DISTILL, 0.0, bytes);
+    } else if (back) {
         for (int64_t n = 0; n < a.rows; n += ROWS_PER_LAUNCH) {
             const DistillArgs b = from_row<E>(a, n, a.rows - n < ROWS_PER_LAUNCH ? a.rows - n : ROWS_PER_LAUNCH);
             const ProfSlot ps = prof_slot();
@@ -743,7 +1147,12 @@ template <typename E> hipError_t distill_launch(const DistillArgs& a, bool back,
         prof_commit(ps, KID_DISTILL_JOIN, 0.0, a.grad ? bytes : lists);
     } else {
         const ProfSlot ps = prof_slot();
-        PQL_LAUNCH(ps, (distill_row_kernel<E, NT_LONG>), dim3((unsigned)a.rows), dim3(NT_LONG), 0, st, a);
+        // the loss alone needs every logit once; rows over 128 KB do not stay in registers
+        if (!a.grad || vecs > 512 * 16) PQL_LAUNCH(ps, (distill_row_kernel<E, 512, 0>), by_row, dim3(512), 0, st, a);
+        else if (vecs <= 256 * 4) PQL_LAUNCH(ps, (distill_row_kernel<E, 256, 4>), by_row, dim3(256), 0, st, a);
+        else if (vecs <= 256 * 8) PQL_LAUNCH(ps, (distill_row_kernel<E, 256, 8>), by_row, dim3(256), 0, st, a);
+        else if (vecs <= 512 * 8) PQL_LAUNCH(ps, (distill_row_kernel<E, 512, 8>), by_row, dim3(512), 0, st, a);
+        else PQL_LAUNCH(ps, (distill_row_kernel<E, 512, 16>), by_row, dim3(512), 0, st, a);
         prof_commit(ps, KID_DISTILL, 0.0, bytes);
     }
     return hipGetLastError();
@@ -751,13 +1160,27 @@ template <typename E> hipError_t distill_launch(const DistillArgs& a, bool back,
 template <typename E> hipError_t top_launch(const TopArgs& a, hipStream_t st) {
     const double bytes = (double)a.rows * a.vocab * sizeof(E) + (double)a.rows * a.top * 8;
     if (a.vocab <= SMALL_VOCAB) return top_small_launch<E>(a, bytes, st);
+    const int64_t vecs = (int64_t)a.piece * (int)sizeof(E) / 16;
+    if (a.pieces == 1 && vecs <= WAVE_VECS && a.top <= 64 && a.rows >= WAVE_ROWS) {
+        const dim3 grid((unsigned)((a.rows + 3) / 4));
+        const ProfSlot ps = prof_slot();
+        if (vecs <= 64 * 4) PQL_LAUNCH(ps, (top_wave_kernel<E, 4>), grid, dim3(256), 0, st, a);
+        else if (vecs <= 64 * 8) PQL_LAUNCH(ps, (top_wave_kernel<E, 8>), grid, dim3(256), 0, st, a);
+        else PQL_LAUNCH(ps, (top_wave_kernel<E, 16>), grid, dim3(256), 0, st, a);
+        prof_commit(ps, KID_TOP_LOGITS, 0.0, bytes);
+        return hipGetLastError();
+    }
     for (int64_t n = 0; n < a.rows; n += ROWS_PER_LAUNCH) {
         TopArgs b = a;
         b.rows = a.rows - n < ROWS_PER_LAUNCH ? a.rows - n : ROWS_PER_LAUNCH;
         b.z = (const E*)a.z + n * a.stride;
         b.index_out += n * a.top; b.value_out += n * a.top;
         const ProfSlot ps = prof_slot();
-        PQL_LAUNCH(ps, (top_row_kernel<E, NT_LONG>), dim3(a.pieces, (unsigned)b.rows), dim3(NT_LONG), 0, st, b);
+        const dim3 grid(a.pieces, (unsigned)b.rows);
+        if (vecs <= 256 * 4) PQL_LAUNCH(ps, (top_row_kernel<E, 256, 4>), grid, dim3(256), 0, st, b);
+        else if (vecs <= 256 * 8) PQL_LAUNCH(ps, (top_row_kernel<E, 256, 8>), grid, dim3(256), 0, st, b);
+        else if (vecs <= 512 * 8) PQL_LAUNCH(ps, (top_row_kernel<E, 512, 8>), grid, dim3(512), 0, st, b);
+        else PQL_LAUNCH(ps, (top_row_kernel<E, 512, 0>), grid, dim3(512), 0, st, b);
         prof_commit(ps, KID_TOP_LOGITS, 0.0, bytes * b.rows / a.rows);
     }
     if (a.pieces > 1) {

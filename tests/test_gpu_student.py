@@ -470,3 +470,74 @@ def test_gradients_of_shared_heads_in_large_calls(env, dtype, size):
     d = Delta(env, *size, dtype=dtype, lengths=lens, resets=[(b, int(rng.integers(0, t))) for b in range(0, n, 3)], seed=7)
     for name, got, want in zip(("dq", "dk", "dv", "dg", "dbeta", "dstate"), d.backward(d.forward(True)[2]), d.want_grads()):
         close(got, want, name)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("vocab", [4100, 9001, 20011, 40003, 70001, 140009])
+def test_rows_of_every_length_class(env, vocab, dtype):
+    """One workgroup per row, from rows that a few registers hold to rows that none do: loss, gradient, selection."""
+    torch, S, ctx = env
+    rows, top = 530, 9
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    z = (2 * torch.randn((rows, vocab + 1), generator=g, device="cuda")).to(getattr(torch, dtype))[:, 1:]
+    z[3], z[4, 5:] = float("-inf"), float("-inf")
+    pick = [0, 1, 3, 4, rows - 1]
+    index = torch.randint(0, vocab, (rows, top), generator=g, device="cuda", dtype=torch.int32)
+    index[4] = torch.arange(top, device="cuda", dtype=torch.int32) % 5
+    value = torch.randn((rows, top), generator=g, device="cuda")
+    d = S.Logits(z)
+    loss, lse = (torch.full((rows,), 7.0, device="cuda") for _ in range(2))
+    grad = torch.full((rows, vocab), 7.0, dtype=z.dtype, device="cuda")
+    ctx.pql_distill_loss(d, S.Teacher(index, value), 1.5, None, loss, lse, S.Logits(grad), S.workspace(ctx.distill_workspace_bytes(d)))
+    want = O.distill(z[pick].double().cpu().numpy(), index[pick].cpu().numpy(), value[pick].cpu().numpy(), 1.5)
+    for name, x, y in zip(("loss", "lse", "grad"), (loss, lse, grad), want):
+        close(x[pick], y, name)
+    i, v = torch.full((rows, top), 7, dtype=torch.int32, device="cuda"), torch.full((rows, top), 7.0, device="cuda")
+    ctx.pql_top_logits(d, top, i, v, S.workspace(ctx.top_logits_workspace_bytes(d, top)))
+    want_i, want_v = O.top_logits(z[pick].double().cpu().numpy(), top)
+    assert np.array_equal(i[pick].cpu().numpy(), want_i) and np.array_equal(v[pick].double().cpu().numpy(), want_v)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("vocab,top,levels", [(1025, 9, 0), (1500, 64, 0), (2053, 65, 0), (4095, 30, 0), (4096, 3, 40), (8000, 64, 3), (2600, 200, 5)])
+def test_many_rows_of_medium_length(env, vocab, top, levels, dtype):
+    """Enough rows for one wavefront each: selection with and without ties, loss, gradient in one call and by itself, in place."""
+    torch, S, ctx = env
+    rows, temp = 2051, 1.25
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    z = 2 * torch.randn((rows, vocab + 3), generator=g, device="cuda")
+    if levels:
+        z = torch.randint(0, levels, z.shape, generator=g, device="cuda").float()
+    z = z.to(getattr(torch, dtype))[:, 2:2 + vocab]
+    z[1], z[2, 7:], z[3, ::2] = float("-inf"), float("-inf"), float("-inf")
+    z[5, 100:110] = float("nan")
+    pick = [0, 1, 2, 3, 4, 5, 6, 7, rows - 2, rows - 1]
+    host = lambda t: t[pick].double().cpu().numpy()  # noqa: E731
+    i, v = torch.full((rows, top), 7, dtype=torch.int32, device="cuda"), torch.full((rows, top), 7.0, device="cuda")
+    d = S.Logits(z)
+    ctx.pql_top_logits(d, top, i, v, S.workspace(ctx.top_logits_workspace_bytes(d, top)))
+    want_i, want_v = O.top_logits(host(z), top)
+    assert np.array_equal(i[pick].cpu().numpy(), want_i) and np.array_equal(host(v), want_v)
+    z[5] = z[6]
+    i[0, top // 2:] = -1                                # a short list, an empty one, an answer twice, a row of no weight
+    i[4] = -1
+    i[7, -1] = i[7, 0]
+    weight = torch.rand((rows,), generator=g, device="cuda") + 0.5
+    weight[6] = 0.0
+    y = torch.where(torch.isfinite(v), v, 0.0) + torch.randn(v.shape, generator=g, device="cuda")
+    t = S.Teacher(i, y)
+    loss, lse = (torch.full((rows,), 7.0, device="cuda") for _ in range(2))
+    grad = torch.full((rows, vocab), 7.0, dtype=z.dtype, device="cuda")
+    ws = S.workspace(ctx.distill_workspace_bytes(d))
+    want = O.distill(host(z), i[pick].cpu().numpy(), host(y), temp, host(weight))
+    ctx.pql_distill_loss(d, t, temp, weight, loss, lse, S.Logits(grad), ws)
+    for name, x, w in zip(("loss", "lse", "grad"), (loss, lse, grad), want):
+        close(x[pick], w, name)
+    ctx.pql_distill_loss(d, t, temp, None, loss.fill_(7), lse.fill_(7), None, ws)
+    plain = O.distill(host(z), i[pick].cpu().numpy(), host(y), temp)
+    close(loss[pick], plain[0], "loss alone")
+    close(lse[pick], plain[1], "lse alone")
+    ctx.pql_distill_backward(d, t, temp, lse, weight, S.Logits(grad.fill_(7)))
+    close(grad[pick], want[2], "gradient by itself")
+    ctx.pql_distill_backward(d, t, temp, lse, weight, d)
+    close(z[pick], want[2], "gradient in place")
