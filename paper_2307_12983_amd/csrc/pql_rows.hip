@@ -173,25 +173,34 @@ __device__ __forceinline__ float entry_of(const DistillArgs& a, int64_t n, Entry
     e.y = ok ? y : NEG_INF;
     return w;
 }
+// The mass of one answer, entry k's, over a list that is padded with -1 to a multiple of four; whether k is its first entry.
+// No early end: the reads of the whole list are then on their way together.
+__device__ __forceinline__ void sum_of_answer(const int* s_index, const float* s_p, int top, int k, int index, bool& owner, float& sum) {
+    owner = true;
+    sum = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < top; i += 4) {
+        const int4 j = *(const int4*)(s_index + i);
+        const float4 p = *(const float4*)(s_p + i);
+        owner = owner && !((j.x == index && i < k) || (j.y == index && i + 1 < k) || (j.z == index && i + 2 < k) || (j.w == index && i + 3 < k));
+        sum += j.x == index ? p.x : 0.f;
+        sum += j.y == index ? p.y : 0.f;
+        sum += j.z == index ? p.z : 0.f;
+        sum += j.w == index ? p.w : 0.f;
+    }
+}
 template <int NT>
-__device__ __forceinline__ void entry_masses(const DistillArgs& a, Entry& e, int* s_index, float* s_p, float* s_red) {
+__device__ __forceinline__ void entry_masses(const DistillArgs& a, Entry& e, int* s_index, float* s_p, float* s_red) {      // the sums only where there is a gradient
     const int k = threadIdx.x;
     e.p = 0.f; e.log_p = 0.f; e.sum = 0.f; e.owner = false;
     const float big = block_max<NT>(e.y, s_red);
     const float x = (e.y - (big == NEG_INF ? 0.f : big)) * a.inv_temp, m = e.index >= 0 ? expf(x) : 0.f;
     const float total = block_sum<NT>(m, s_red);
     if (e.index >= 0) { e.p = m / total; e.log_p = x - logf(total); }
-    if (k < a.top) { s_index[k] = e.index; s_p[k] = e.p; }
+    if (!a.grad) return;
+    if (k < PQL_MAX_TOP) { s_index[k] = e.index; s_p[k] = e.p; }     // -1 behind the list
     __syncthreads();
-    if (e.index >= 0) {                     // no early end: the reads of the whole list are then on their way together
-        e.owner = true;
-#pragma unroll 8
-        for (int i = 0; i < a.top; ++i) {
-            const bool same = s_index[i] == e.index;
-            e.owner = e.owner && !(same && i < k);
-            e.sum += same ? s_p[i] : 0.f;
-        }
-    }
+    if (e.index >= 0) sum_of_answer(s_index, s_p, a.top, k, e.index, e.owner, e.sum);
 }
 // One entry's share of the loss: p (log p - log q) with log q = (z - m) / t - log(s); nothing for p = 0, +inf where the
 // student has the answer at -inf (also in a row that holds nothing else).
@@ -317,8 +326,8 @@ __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_A
 template <typename E, int NV, bool BACK>
 __global__ __launch_bounds__(256) void distill_wave_kernel(DistillArgs a) {
     constexpr int VEC = Stretch<E>::VEC, Q = PQL_MAX_TOP / 64;
-    __shared__ int s_index_all[4][PQL_MAX_TOP];
-    __shared__ float s_p_all[4][PQL_MAX_TOP];
+    __shared__ __align__(16) int s_index_all[4][PQL_MAX_TOP];
+    __shared__ __align__(16) float s_p_all[4][PQL_MAX_TOP];
     const int wave = threadIdx.x >> 6, l = threadIdx.x & 63;
     const int64_t n = (int64_t)blockIdx.x * 4 + wave;
     if (n >= a.rows) return;                // wavefronts share nothing
@@ -370,19 +379,15 @@ __global__ __launch_bounds__(256) void distill_wave_kernel(DistillArgs a) {
         lp[q] = x - log_total;
         owner[q] = index[q] >= 0;
         y[q] = owner[q] ? expf(x) / total : 0.f;                     // p from here on
-        if (k < a.top) { s_index[k] = index[q]; s_p[k] = y[q]; }
+        if (64 * q < a.top) { s_index[k] = index[q]; s_p[k] = y[q]; }      // -1 behind the list
     }
     wave_fence();
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
         if (64 * q >= a.top) break;
-        const int k = l + 64 * q;
-#pragma unroll 8
-        for (int i = 0; i < a.top; ++i) {
-            const bool same = s_index[i] == index[q];
-            owner[q] = owner[q] && !(same && i < k);
-            sum[q] += same ? s_p[i] : 0.f;
-        }
+        bool first;
+        sum_of_answer(s_index, s_p, a.top, l + 64 * q, index[q], first, sum[q]);
+        owner[q] = owner[q] && first;
     }
     const float c = LOG2E * a.inv_temp, t_m = BACK ? a.temp : 1.f;
     float m, inv;
@@ -508,8 +513,8 @@ template <typename E, int NT> __device__ __forceinline__ void zero_stretch(E* ou
 template <typename E, int NT, int NV>
 __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a) {
     constexpr int VEC = Stretch<E>::VEC;
-    __shared__ int s_index[PQL_MAX_TOP];
-    __shared__ float s_p[PQL_MAX_TOP], s_red[NT / 64];
+    __shared__ __align__(16) int s_index[PQL_MAX_TOP];
+    __shared__ __align__(16) float s_p[PQL_MAX_TOP], s_red[NT / 64];
     const int64_t n = blockIdx.x;
     E* out = (E*)a.grad + n * a.grad_stride;
     const E* row = (const E*)a.z + n * a.stride;
@@ -600,8 +605,8 @@ __global__ __launch_bounds__(NT) void distill_part_kernel(DistillArgs a) {
 // Second launch (JOIN), or the whole backward call: the gradient of one piece.
 template <typename E, int NT, bool JOIN>
 __global__ __launch_bounds__(NT) void distill_piece_kernel(DistillArgs a) {
-    __shared__ int s_index[PQL_MAX_TOP];
-    __shared__ float s_p[PQL_MAX_TOP], s_red[NT / 64];
+    __shared__ __align__(16) int s_index[PQL_MAX_TOP];
+    __shared__ __align__(16) float s_p[PQL_MAX_TOP], s_red[NT / 64];
     const int64_t n = blockIdx.y;
     const int j0 = blockIdx.x * a.piece, len = min(a.piece, a.vocab - j0);
     Entry e;
@@ -612,9 +617,8 @@ __global__ __launch_bounds__(NT) void distill_piece_kernel(DistillArgs a) {
         if (a.grad) zero_stretch<E, NT>(out, len);
         return;
     }
-    entry_masses<NT>(a, e, s_index, s_p, s_red);
     const E* row = (const E*)a.z + n * a.stride + j0;
-    const float c = LOG2E * a.inv_temp;
+    const float c = LOG2E * a.inv_temp, f = w * a.temp;
     float m, inv, zk = 0.f;
     const float t_m = JOIN ? 1.f : a.temp;
     const bool mine = e.index >= j0 && e.index < j0 + len;
@@ -624,11 +628,13 @@ __global__ __launch_bounds__(NT) void distill_piece_kernel(DistillArgs a) {
             pm = a.part[2 * (n * a.pieces + threadIdx.x)];
             ps = a.part[2 * (n * a.pieces + threadIdx.x) + 1];
         }
+        if (e.index >= 0) zk = a.part_z[n * a.top + threadIdx.x];
         join_stats<NT>(c, pm, ps, s_red);
         m = pm;
         const float log_s = logf(ps);
         inv = ps > 0.f || ps != ps ? 1.f / ps : 0.f;
-        if (e.index >= 0) zk = a.part_z[n * a.top + threadIdx.x];
+        if (a.grad) stretch_grad<E, NT>(Stretch<E>(row, len), out, c, m, t_m, inv, f);
+        entry_masses<NT>(a, e, s_index, s_p, s_red);        // meanwhile
         if (blockIdx.x == 0) {
             const float loss = block_sum<NT>(e.index >= 0 ? entry_loss(e, zk, m, a.inv_temp, log_s) : 0.f, s_red);
             if (threadIdx.x == 0) {
@@ -643,10 +649,10 @@ __global__ __launch_bounds__(NT) void distill_piece_kernel(DistillArgs a) {
         inv = lse == NEG_INF ? 0.f : 1.f;
         if (mine) zk = to_float(row[e.index - j0]);
         __syncthreads();                                    // read before the gradient may be written over the logits
+        stretch_grad<E, NT>(Stretch<E>(row, len), out, c, m, t_m, inv, f);
+        entry_masses<NT>(a, e, s_index, s_p, s_red);        // meanwhile
     }
-    const float f = w * a.temp;
-    stretch_grad<E, NT>(Stretch<E>(row, len), out, c, m, t_m, inv, f);
-    __syncthreads();
+    __syncthreads();                        // the dense gradient of the listed answers lies before its correction
     if (e.owner && mine) out[e.index - j0] = from_float<E>(f * ((inv != 0.f ? exp2_raw(fmaf(-m, t_m, zk) * c) * inv : 0.f) - e.sum));
 }
 
@@ -733,44 +739,75 @@ __global__ __launch_bounds__(256) void top_small_kernel(TopArgs a) {
     }
 }
 
-// Short lists of small vocabularies: K rounds of the largest key left and its lowest index (V = 51, K = 8: MEASURED).
+// Short lists of small vocabularies: K rounds of the largest key left.  A key's low bits make room for its index, reversed, so
+// that one comparison finds the value and the lowest place of equal ones, and the element found is the only one that equals
+// it.  16-bit values lose nothing by that.  Where two of the K + 1 largest of a row agree in the bits that are left, the
+// wavefront starts again with whole keys.
+template <int G, int R, bool EXACT, typename F>
+__device__ __forceinline__ void top_rounds(unsigned (&key)[R], int l, int rounds, F&& found) {
+#pragma unroll 1
+    for (int k = 0; k < rounds; ++k) {
+        unsigned big = key[0];
+#pragma unroll
+        for (int r = 1; r < R; ++r) big = max(big, key[r]);
+        big = group_max<G>(big);
+        int at = 0;
+        if (EXACT) {
+            at = 0x7fffffff;
+#pragma unroll
+            for (int r = R - 1; r >= 0; --r) at = key[r] == big ? l + G * r : at;
+            at = group_min<G>(at);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) key[r] = (EXACT ? l + G * r == at : key[r] == big) ? 0u : key[r];
+        found(k, big, at);
+    }
+}
 template <typename E, int G, int R>
 __global__ __launch_bounds__(256) void top_rounds_kernel(TopArgs a) {
-    constexpr int ROWS = 256 / G;
+    constexpr int ROWS = 256 / G, ALL = G * R, BITS = ALL <= 32 ? 5 : ALL <= 64 ? 6 : ALL <= 128 ? 7 : ALL <= 256 ? 8 : ALL <= 512 ? 9 : 10;
+    constexpr unsigned LOW = (1u << BITS) - 1;
     const int g = threadIdx.x / G, l = threadIdx.x & (G - 1);
     const int64_t n = (int64_t)blockIdx.x * ROWS + g;
     if ((int64_t)blockIdx.x * ROWS + (threadIdx.x & ~63) / G >= a.rows) return;       // whole wavefronts
     const bool in = n < a.rows;
     const E* row = (const E*)a.z + n * a.stride;
     unsigned key[R];
+    auto load = [&] {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int j = l + G * r;
-        key[r] = in && j < a.vocab ? key_of(to_float(row[j])) : 0u;
-    }
+        for (int r = 0; r < R; ++r) {
+            const int j = l + G * r;
+            key[r] = in && j < a.vocab ? key_of(to_float(row[j])) : 0u;
+        }
+    };
     // results stay with the lanes until a group's row of them can be written together
     int index = -1;
-    unsigned value = 0;
-    for (int k = 0; k < a.top; ++k) {
-        unsigned big = key[0];
-#pragma unroll
-        for (int r = 1; r < R; ++r) big = max(big, key[r]);
-        big = group_max<G>(big);
-        int at = 0x7fffffff;
-#pragma unroll
-        for (int r = R - 1; r >= 0; --r) at = key[r] == big ? l + G * r : at;
-        at = group_min<G>(at);
-#pragma unroll
-        for (int r = 0; r < R; ++r) key[r] = l + G * r == at ? 0u : key[r];
-        if ((k & (G - 1)) == l) { index = big ? at : -1; value = big; }
-        if ((k & (G - 1)) == G - 1 || k == a.top - 1) {
-            const int place = (k & ~(G - 1)) + l;
-            if (in && place <= k) {
-                a.index_out[n * a.top + place] = index;
-                a.value_out[n * a.top + place] = value_of(value);
-            }
+    auto write = [&](int k) {
+        if ((k & (G - 1)) != G - 1 && k != a.top - 1) return;
+        const int place = (k & ~(G - 1)) + l;
+        if (in && place <= k) {
+            a.index_out[n * a.top + place] = index;
+            a.value_out[n * a.top + place] = index < 0 ? NEG_INF : to_float(row[index]) + 0.f;        // + 0: zeros come back as +0
         }
-    }
+    };
+    load();
+#pragma unroll
+    for (int r = 0; r < R; ++r) key[r] = key[r] ? (key[r] & ~LOW) | (unsigned)(ALL - 1 - (l + G * r)) : 0u;
+    unsigned last = 0;
+    bool near = false;
+    top_rounds<G, R, false>(key, l, a.top + (sizeof(E) == 4 ? 1 : 0), [&](int k, unsigned big, int) {
+        near |= k > 0 && big != 0 && ((big ^ last) & ~LOW) == 0;
+        last = big;
+        if (k >= a.top) return;
+        if ((k & (G - 1)) == l) index = big ? ALL - 1 - (int)(big & LOW) : -1;
+        write(k);
+    });
+    if (sizeof(E) == 2 || !__any(near)) return;
+    load();
+    top_rounds<G, R, true>(key, l, a.top, [&](int k, unsigned big, int at) {
+        if ((k & (G - 1)) == l) index = big ? at : -1;
+        write(k);
+    });
 }
 
 // Long rows.  Every thread's largest key is found in one pass; the K-th largest of those bounds the row's K-th largest
@@ -1072,7 +1109,7 @@ bool logits_ok(const pql_logits& z) {
 }
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-#define SMALL_CASES(X) X(8, 4) X(8, 8) X(16, 8) X(32, 8) X(64, 8) X(64, 16)
+#define SMALL_CASES(X) X(8, 4) X(8, 7) X(8, 8) X(16, 8) X(32, 8) X(64, 8) X(64, 16)
 template <typename E, bool BACK> hipError_t distill_small_launch(const DistillArgs& a, int kid, double bytes, hipStream_t st) {
 #define PQL_SMALL(G, R)                                                                                              \
     if (a.vocab <= G * R) {                                                                                          \
@@ -1295,8 +1332,11 @@ int32_t pql_distill_backward(pql_ctx* c, pql_logits z, pql_teacher t, float temp
     if (rc != PQL_OK || z.rows == 0) return rc;
     if (!lse || !loss_grad) return ctx_fail(c, PQL_ERR_NULL, "pql_distill_backward: null pointer");
     if (misaligned(lse, 4) || misaligned(loss_grad, 4)) return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_distill_backward: misaligned pointer");
-    // every piece works out the list's masses anew: 16384 elements keep that below a tenth of it
-    DistillArgs a = distill_args(z, t, temperature, loss_grad, grad, z.vocab <= SMALL_VOCAB ? 1 : (z.vocab + 16383) / 16384);
+    // every piece works out the list's masses anew: 16384 elements keep that below a tenth of it; fewer where there are few rows
+    int pieces = z.vocab <= SMALL_VOCAB ? 1 : (z.vocab + 16383) / 16384;
+    const int few = pieces_of(z.rows, z.vocab, 1 << 30);
+    if (few > pieces) pieces = few;
+    DistillArgs a = distill_args(z, t, temperature, loss_grad, grad, pieces);
     a.lse = lse;
     const hipError_t e = z.dtype == PQL_F32 ? distill_launch<float>(a, true, (hipStream_t)stream)
                                             : distill_launch<bf16_t>(a, true, (hipStream_t)stream);
