@@ -208,20 +208,18 @@ template <typename M, int ROWS, int COLS, bool EXACT> struct Tile {
 // Eight consecutive elements d .. d + 7 of one token row; zeros from dim on and where the token does not count.
 template <typename E, bool AL>
 __device__ __forceinline__ void load8(const E* row, int d, int dim, bool ok, float* x) {
-    if (AL) {                               // 16-byte aligned rows of a multiple of 8 elements
-        if (ok && d < dim) {
-            if constexpr (sizeof(E) == 4) {
-                const floatx4 a = *(const floatx4*)(row + d), b = *(const floatx4*)(row + d + 4);
+    if (AL) {                               // 16-byte aligned rows of a multiple of 16 bytes
+        if constexpr (sizeof(E) == 4) {
+            floatx4 a = {}, b = {};
+            if (ok && d < dim) a = *(const floatx4*)(row + d);
+            if (ok && d + 4 < dim) b = *(const floatx4*)(row + d + 4);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
-            } else {
-                const bf16x8 a = *(const bf16x8*)(row + d);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
-            }
+            for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
         } else {
+            bf16x8 a = {};
+            if (ok && d < dim) a = *(const bf16x8*)(row + d);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+            for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
         }
     } else {
 #pragma unroll
@@ -526,9 +524,9 @@ constexpr int NOWHERE = 0x7ffffffc;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tokens(const char* p) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, 0x40000000, 0x00020000);
 }
-__device__ __forceinline__ void load_ff(__amdgpu_buffer_rsrc_t rs, int lane, int at, FF& f) {
+__device__ __forceinline__ void load_ff(__amdgpu_buffer_rsrc_t rs, int lane, int lane4, int at, FF& f) {
     const floatx4 a = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rs, lane, at, 0));
-    const floatx4 b = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rs, lane, at + 16, 0));
+    const floatx4 b = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rs, lane4, at, 0));
 #pragma unroll
     for (int i = 0; i < 4; ++i) { f.v[i] = a[i]; f.v[4 + i] = b[i]; }
 }
@@ -553,7 +551,7 @@ template <typename M, int C, int DK, bool AL> struct RowOperands {
             for (int d = 0; d < ND; ++d) {
                 const int o = ok && 32 * d + 8 * q < dk ? lane + 32 * d * ES : NOWHERE - 16;
                 if constexpr (ES == 2) f[d].h = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0));
-                else load_ff(r, o, 0, f[d]);
+                else load_ff(r, o, ok && 32 * d + 8 * q + 4 < dk ? o + 16 : NOWHERE - 16, 0, f[d]);
             }
         } else {
 #pragma unroll
@@ -765,7 +763,8 @@ template <typename M, int C, bool TRANSPOSED> __device__ __forceinline__ void lo
             x[ks].m = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, lane, at + 1024, 0));
             x[ks].l = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, lane, at + 2048, 0));
         } else {
-            load_ff(rs, there ? 32 * l : NOWHERE - 16, at, x[ks]);
+            const int lane = there ? 32 * l : NOWHERE - 32;
+            load_ff(rs, lane, lane + 16, at, x[ks]);
         }
     }
 }
@@ -779,7 +778,7 @@ template <typename M, int C, int RS> __device__ __forceinline__ void load_kt(con
         for (int k = 0; k < C / 32; ++k) {
             const int o = (C / 32 * (wave * RS + s) + k) * 512 * ES;
             if constexpr (ES == 2) x[s][k].h = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * l, o, 0));
-            else load_ff(rs, 32 * l, o, x[s][k]);
+            else load_ff(rs, 32 * l, 32 * l + 16, o, x[s][k]);
         }
 }
 struct ChunkGates {                         // of this lane's tokens i0 .. i0 + 3
@@ -1000,7 +999,7 @@ template <typename M, int C, int DK, int NT> struct BackScanLds {
                          Q0 = P0 + C * 16 * NT * 4, BYTES = Q0 + DK * 16 * NT * 4;      // P0, Q0: results of P^T dO, Q^T (gam o dO)
 };
 template <typename M, int C, int DK, int NT, bool AL>
-__global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128 ? 2 : 1, DK == 128 ? 2 : 8))) void delta_back_scan_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128 ? 2 : AL ? 3 : 1, DK == 128 ? 2 : 8))) void delta_back_scan_kernel(DeltaArgs a) {
     using E = typename M::E;
     using L = BackScanLds<M, C, DK, NT>;
     constexpr int RS = DK / C, KS = C / 32, ND = DK / 32, NW = C / 16;
@@ -1526,11 +1525,11 @@ Plan plan_of(const pql_delta_shape& s) {
     return p;
 }
 DeltaSeq seq(const pql_seq& s) { return DeltaSeq{s.data, s.stride_b, s.stride_t, s.stride_h}; }
-// Whether the kernels may load 16 bytes of a row at a time, with 32-bit offsets within a chunk of tokens.
+// Whether a chunk of tokens can be reached with 32-bit offsets, and whether, beyond that, 16 bytes of a row may be loaded at a time.
+bool rows_near(const pql_seq& s) { return s.stride_t >= 0 && s.stride_t < (1 << 21); }
 bool rows_aligned(const pql_seq& s, int dim, int dtype) {
     const int n = dtype == PQL_F32 ? 4 : 8;             // elements in 16 bytes
-    return ((uintptr_t)s.data & 15) == 0 && s.stride_b % n == 0 && s.stride_t % n == 0 && s.stride_h % n == 0 && dim % 8 == 0 && s.stride_t >= 0 &&
-           s.stride_t < (1 << 21);
+    return ((uintptr_t)s.data & 15) == 0 && s.stride_b % n == 0 && s.stride_t % n == 0 && s.stride_h % n == 0 && dim % n == 0 && rows_near(s);
 }
 // Elements of an output must not share a place: a stride of 0 is for inputs only.
 bool apart(const pql_seq& s, const pql_delta_shape& x, int heads) {
@@ -1708,8 +1707,7 @@ int32_t pql_delta_forward(pql_ctx* c, const pql_delta_shape* s, const pql_delta_
     DeltaArgs a = args_of(*s, *in);
     a.out = seq(out); a.state_out = state_out;
     set_saved(a, p, (char*)(saved ? saved : workspace), saved != nullptr);
-    const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype) && rows_aligned(in->v, s->dim_v, s->dtype) &&
-                    rows_aligned(out, s->dim_v, s->dtype);
+    const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype) && rows_near(in->v) && rows_near(out);
     const hipError_t e = s->dtype == PQL_F32 ? chunks_dispatch<ModeF>(a, false, al, p, (hipStream_t)stream)
                                              : chunks_dispatch<ModeB>(a, false, al, p, (hipStream_t)stream);
     return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_delta_forward", e);
@@ -1739,8 +1737,7 @@ int32_t pql_delta_backward(pql_ctx* c, const pql_delta_shape* s, const pql_delta
     a.dX = (float*)(w + p.dX); a.dY = (float*)(w + p.dY); a.dS = (float*)(w + p.dS);
     a.heads_wg = p.heads_wg;
     if (a.group > 1 && p.heads_wg == 1) { a.part_q = (float*)(w + p.part_q); a.part_k = (float*)(w + p.part_k); }
-    const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype) && rows_aligned(out_grad, s->dim_v, s->dtype) &&
-                    rows_aligned(g->v, s->dim_v, s->dtype);
+    const bool al = rows_aligned(in->q, s->dim_k, s->dtype) && rows_aligned(in->k, s->dim_k, s->dtype) && rows_aligned(out_grad, s->dim_v, s->dtype) && rows_near(g->v);
     const hipError_t e = s->dtype == PQL_F32 ? chunks_dispatch<ModeF>(a, true, al, p, (hipStream_t)stream)
                                              : chunks_dispatch<ModeB>(a, true, al, p, (hipStream_t)stream);
     return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_delta_backward", e);
