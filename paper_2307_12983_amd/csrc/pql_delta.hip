@@ -737,8 +737,8 @@ __global__ __launch_bounds__(4 * C) void delta_prepare_kernel(DeltaArgs a) {
 // =============================================================================================
 // Chunks in order: outputs and states, 16 NT columns per workgroup.  Half of the wavefronts (one per SIMD, 16 tokens each)
 // carry the chain K S, X, T X, K^T Y that every chunk has to wait for, the other half what only the outputs need, Q S and
-// P Y, in the gaps of the first.  All operands of a chunk are requested into registers as soon as the previous chunk's
-// have been used.
+// P Y, in the gaps of the first.  All operands of a chunk are requested into registers, the next chunk's K, V and T once the
+// products that wait for LDS have asked for theirs, K^T two phases before it is used.
 // =============================================================================================
 template <typename M, int C, int DK, int NT> struct ScanLds {
     using S = Tile<M, 16 * NT, DK, false>;          // S^T [column][dim_k]
@@ -817,7 +817,7 @@ template <int RS, int NT> __device__ __forceinline__ void store_state(float* p, 
         }
 }
 template <typename M, int C, int DK, int NT, bool AL, bool KEEP>
-__global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128 ? 2 : 4, DK == 128 ? 2 : 4))) void delta_scan_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128 || !AL ? 2 : 4, DK == 128 || !AL ? 2 : 4))) void delta_scan_kernel(DeltaArgs a) {
     using E = typename M::E;
     using L = ScanLds<M, C, DK, NT>;
     constexpr int RS = DK / C, KS = C / 32, ND = DK / 32, NW = C / 16;      // 16-row strips of the state per wavefront, contraction steps
@@ -847,7 +847,6 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
         if (chunks > 0) {
             K.load(); V.load(); G.load<C>(pG, i0);
             load_tri<M, C, false>(pT, wave, l, T);
-            load_kt<M, C, RS>(pK, wave, l, kt);
         }
         load_state<RS, NT>(a.state, w, wave, q, c0 + c, dk, dv, S);
 #pragma unroll
@@ -861,15 +860,13 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
             {
                 typename M::Y f[ND][NT];
                 tS.template frags<ND, NT>(c, 8 * q, f);
+                load_kt<M, C, RS>(pK, wave, l, kt);
+                pK.go(true);
 #pragma unroll
                 for (int d = 0; d < ND; ++d)
 #pragma unroll
                     for (int n = 0; n < NT; ++n) za[n].add(K.f[d], f[d][n]);
             }
-            pG.go(more);
-            Gn.load<C>(pG, i0);
-            K.go(more);
-            K.load();
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const floatx4 v = V.get(n), z = za[n].sum();
@@ -878,13 +875,17 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
                 for (int r = 0; r < 4; ++r) x[r] = v[r] - damp(G.gam[r], z[r]);
                 tX.put4(16 * n + c, i0, x);
             }
-            V.go(more);
-            V.load();
             __syncthreads();                        // 2: X
             Acc ra[NT];
             {
                 typename M::Y f[KS][NT];
                 tX.template frags<KS, NT>(c, 8 * q, f);
+                pG.go(more);
+                Gn.load<C>(pG, i0);
+                K.go(more);
+                K.load();
+                V.go(more);
+                V.load();
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
 #pragma unroll
@@ -894,8 +895,6 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
             floatx4 rr[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) rr[n] = ra[n].sum();
-            pT.go(more);
-            load_tri<M, C, false>(pT, wave, l, T);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const floatx4 y = G.beta * rr[n];
@@ -913,6 +912,8 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
             __syncthreads();                        // 3: Y; all have read the state
             typename M::Y f[KS][NT];
             tZ.template frags<KS, NT>(c, 8 * q, f);
+            pT.go(more);
+            load_tri<M, C, false>(pT, wave, l, T);
 #pragma unroll
             for (int s = 0; s < RS; ++s) {
                 const int r0 = 16 * (wave * RS + s);
@@ -928,8 +929,6 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
                     tS.put4(16 * n + c, r0 + 4 * q, S[s][n]);
                 }
             }
-            pK.go(more);
-            load_kt<M, C, RS>(pK, wave, l, kt);
             G = Gn;
         }
         store_state<RS, NT>(a.state_out, w, wave, q, c0 + c, dk, dv, S);
