@@ -1517,7 +1517,7 @@ Plan plan_of(const pql_delta_shape& s) {
     p.saved = o;
     o = 0;
     p.dX = take(n * p.c * p.dvp * 4); p.dY = take(n * p.c * p.dvp * 4); p.dS = take(n * p.dkp * p.dvp * 4);
-    p.heads_wg = (int64_t)s.batch * s.heads_k * p.chunks < 512 ? 1 : s.heads_v / s.heads_k;
+    p.heads_wg = (int64_t)s.batch * s.heads_k * p.chunks < 256 ? 1 : s.heads_v / s.heads_k;
     const size_t part = s.heads_v == s.heads_k || p.heads_wg > 1 ? 0 : (size_t)s.batch * s.steps * s.heads_v * s.dim_k;
     p.part_q = take(part * 4); p.part_k = take(part * 4);
     p.back = o;

@@ -319,7 +319,7 @@ __global__ __launch_bounds__(256) void distill_small_kernel(DistillArgs a) {
 
 // =============================================================================================
 // Rows of up to 64 NV granules: one wavefront per row, the row in its registers.  A workgroup per row would spend more time
-// in barriers and waiting for its own first loads than on the row (65536 rows of 1500 bf16: MEASURED).
+// in barriers and waiting for its own first loads than on the row (65536 rows of 1500 bf16, loss and gradient: 121 and 263 us).
 // =============================================================================================
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
 
@@ -859,17 +859,23 @@ template <typename E, int NT, typename F>
 __device__ __forceinline__ void for_each_key(const Stretch<E>& st, F&& f) {
     for_each<E, NT>(st, [&](float x, int j) { f(key_of(x), j); });
 }
-// Writes n candidates (at most CAND, distinct) at their ranks; places without one get -1.
+// Writes n candidates (at most CAND, distinct; keys 16-byte aligned) at their ranks; places without one get -1.
 template <int NT>
 __device__ __forceinline__ void write_ranked(const unsigned* s_key, const int* s_index, int n, int top, int base, int* index_out, float* value_out, int t = threadIdx.x) {
     for (int k = t; k < n; k += NT) {
         const unsigned mine = s_key[k];
         const int index = s_index[k];
-        int rank = 0;
-        for (int i = 0; i < n; ++i) {
-            const unsigned o = s_key[i];
-            rank += o > mine || (o == mine && s_index[i] < index);
+        int rank = 0, same = 0;
+        const uint4* four = (const uint4*)s_key;
+#pragma unroll 4
+        for (int i = 0; i < n / 4; ++i) {       // reads that do not depend on each other
+            const uint4 o = four[i];
+            rank += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+            same += (o.x == mine) + (o.y == mine) + (o.z == mine) + (o.w == mine);
         }
+        for (int i = n & ~3; i < n; ++i) { rank += s_key[i] > mine; same += s_key[i] == mine; }
+        if (same > 1)
+            for (int i = 0; i < n; ++i) rank += s_key[i] == mine && s_index[i] < index;
         if (rank < top) { index_out[rank] = base + index; value_out[rank] = value_of(mine); }
     }
     for (int k = t; k < top; k += NT)
@@ -879,7 +885,7 @@ __device__ __forceinline__ void write_ranked(const unsigned* s_key, const int* s
 template <typename E, int NV>
 __global__ __launch_bounds__(256) void top_wave_kernel(TopArgs a) {
     constexpr int SOME = 256, VEC = Stretch<E>::VEC;
-    __shared__ unsigned s_key_all[4][SOME];
+    __shared__ __align__(16) unsigned s_key_all[4][SOME];
     __shared__ int s_index_all[4][SOME], s_n_all[4];
     const int wave = threadIdx.x >> 6, l = threadIdx.x & 63;
     const int64_t n = (int64_t)blockIdx.x * 4 + wave;
@@ -956,9 +962,10 @@ __global__ __launch_bounds__(256) void top_wave_kernel(TopArgs a) {
 }
 
 // NV > 0: the stretch stays in registers between the two passes, NV granules a thread.
-template <typename E, int NT, int NV>
-__global__ __launch_bounds__(NT) void top_row_kernel(TopArgs a) {
-    __shared__ unsigned s_key[CAND], s_two[2][NT / 64];
+template <typename E, int NT, int NV, bool MERGE>
+__device__ __forceinline__ void top_of_stretch(const TopArgs& a) {
+    __shared__ __align__(16) unsigned s_key[CAND];
+    __shared__ unsigned s_two[2][NT / 64];
     __shared__ int s_index[CAND], s_cnt[NT / 64], s_n;
     const int64_t n = blockIdx.y;
     const int j0 = blockIdx.x * a.piece, len = min(a.piece, a.vocab - j0);
@@ -1040,64 +1047,43 @@ __global__ __launch_bounds__(NT) void top_row_kernel(TopArgs a) {
         }
         __syncthreads();
     }
+    if constexpr (MERGE) {
+        for (int i = threadIdx.x; i < min(found, CAND); i += NT) s_index[i] = a.part_index[n * a.vocab + s_index[i]];
+        __syncthreads();
+    }
     write_ranked<NT>(s_key, s_index, found, a.top, j0, a.pieces > 1 ? a.part_index + o : a.index_out + o,
                      a.pieces > 1 ? a.part_value + o : a.value_out + o);
 }
-// Joins the lists of a row's pieces (each in descending order): an element's rank is the sum over the lists of the
-// elements before it.  Pieces come in index order, so an equal value of an earlier piece goes first.
-template <int NT>
-__global__ __launch_bounds__(NT) void top_merge_kernel(TopArgs a) {
-    extern __shared__ unsigned lds_m[];
-    const int64_t n = blockIdx.x;
-    const int all = a.pieces * a.top;
-    for (int i = threadIdx.x; i < all; i += NT) {
-        const int64_t at = n * all + i;
-        lds_m[i] = a.part_index[at] < 0 ? 0u : key_of(a.part_value[at]);
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < all; i += NT) {
-        const unsigned mine = lds_m[i];
-        const int list = i / a.top;
-        int rank = 0;
-        if (mine == 0) continue;
-        for (int q = 0; q < a.pieces && rank < a.top; ++q) {
-            if (q == list) { rank += i - list * a.top; continue; }
-            int lo = 0, hi = a.top;         // elements of list q before mine: greater ones, and equal ones if q < list
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                const unsigned o = lds_m[q * a.top + mid];
-                if (o > mine || (o == mine && q < list)) lo = mid + 1; else hi = mid;
-            }
-            rank += lo;
-        }
-        if (rank < a.top) {
-            a.index_out[n * a.top + rank] = a.part_index[n * all + i];
-            a.value_out[n * a.top + rank] = value_of(mine);
-        }
-    }
-    int have = 0;
-    for (int i = threadIdx.x; i < all; i += NT) have += lds_m[i] != 0;
-    __shared__ int s_cnt[NT / 64];
-    have = block_sum<NT>(have, s_cnt);
-    for (int k = threadIdx.x; k < a.top; k += NT)
-        if (k >= have) { a.index_out[n * a.top + k] = -1; a.value_out[n * a.top + k] = NEG_INF; }
-}
+template <typename E, int NT, int NV>
+__global__ __launch_bounds__(NT) void top_row_kernel(TopArgs a) { top_of_stretch<E, NT, NV, false>(a); }
+// Joins the lists of a row's pieces: the same selection from their values, the places found being looked up in the lists'
+// indices.  Equal values lie in index order (within a list by its order, lists by that of the pieces), so places rank as
+// indices would.
+template <int NV>
+__global__ __launch_bounds__(256) void top_merge_kernel(TopArgs a) { top_of_stretch<float, 256, NV, true>(a); }
 
 // ---- launches -------------------------------------------------------------------------------
 constexpr int NT_LONG = 512;
-// One wavefront per row: rows of at most 16 KB, and enough of them to give every SIMD two.
+// One wavefront per row: rows of at most 16 KB, and enough of them to give every SIMD two.  Loss and gradient, bf16, by
+// wavefronts and by workgroups: 2048 rows of 1500 8 and 12 us, of 4000 12 and 14, of 8000 19 and 18; 65536 rows of 1500 121
+// and 263, of 4000 208 and 318, of 8000 415 and 414; 512 rows of 8000 11 and 9.  Selection of 32, 65536 rows: 116 and 357,
+// 158 and 384, 289 and 408 us.
 constexpr int64_t WAVE_VECS = 64 * 16, WAVE_ROWS = 2048;
 constexpr int64_t MAX_GRID = 0x7fffffff;
 
-// Pieces of a long row: one, unless there are too few rows to fill the card's 256 CUs twice; never under 4096 elements.
-int pieces_of(int64_t rows, int vocab, int most) {
-    if (rows >= 512 || vocab <= SMALL_VOCAB) return 1;
+// Pieces of a long row, of `least` elements or more: one where there is a row for every CU, else as many as give 1024
+// workgroups.  fp32 rows of 131072, in pieces and whole: loss and gradient of one row 11 and 46 us, of 128 rows 46 and 55, of
+// 255 rows 75 and 69; the 8 largest of one row 13 and 22 us, of 128 rows 27 and 30, of 255 rows 40 and 39.
+int pieces_of(int64_t rows, int vocab, int least, int most) {
+    if (rows >= 256 || vocab <= SMALL_VOCAB) return 1;
     int64_t p = (1024 + rows - 1) / (rows > 0 ? rows : 1);
-    const int64_t by_len = (vocab + 4095) / 4096;
+    const int64_t by_len = vocab / least;
     if (p > by_len) p = by_len;
     if (p > most) p = most;
     return (int)(p < 1 ? 1 : p);
 }
+// A second launch takes 4 us: one row of 5000 whole 8 us, in two pieces 10; of 20000 whole 13 us, in five 11.
+int distill_pieces(const pql_logits& z, int most) { return pieces_of(z.rows, z.vocab, 4096, most); }
 int piece_len(int vocab, int pieces) {      // a multiple of 64 elements: pieces keep the row's alignment
     const int len = (vocab + pieces - 1) / pieces;
     return pieces == 1 ? vocab : (len + 63) / 64 * 64;
@@ -1124,14 +1110,19 @@ template <typename E, bool BACK> hipError_t distill_small_launch(const DistillAr
 #undef PQL_SMALL
     return hipErrorInvalidValue;
 }
+// Longest list that is taken by rounds, one entry each, in a group of G lanes; longer ones by bits of the key.  By rounds and by
+// bits, fp32: 327680 rows of 51, list of 16 53 and 62 us, of 48 127 and 219; 150000 of 100, list of 16 50 and 53, of 24 71
+// and 65; 16384 of 1000, list of 8 36 and 41, of 12 43 and 42, of 16 52 and 44.
+constexpr int ROUNDS(int g) { return g == 8 ? 64 : g == 64 ? 12 : 16; }
 template <typename E> hipError_t top_small_launch(const TopArgs& a, double bytes, hipStream_t st) {
 #define PQL_SMALL(G, R)                                                                                              \
     if (a.vocab <= G * R) {                                                                                          \
         constexpr int ROWS = 256 / G;                                                                                \
         const ProfSlot ps = prof_slot();                                                                             \
         const dim3 grid((unsigned)((a.rows + ROWS - 1) / ROWS));                                                     \
-        if (a.top <= 16) PQL_LAUNCH(ps, (top_rounds_kernel<E, G, R>), grid, dim3(256), 0, st, a);                    \
-        else PQL_LAUNCH(ps, (top_small_kernel<E, G, R>), grid, dim3(256), (size_t)ROWS * 2 * a.top * 4, st, a);      \
+        if (a.top <= ROUNDS(G)) PQL_LAUNCH(ps, (top_rounds_kernel<E, G, R>), grid, dim3(256), 0, st, a);             \
+        else if constexpr (G > 8)                                                                                    \
+            PQL_LAUNCH(ps, (top_small_kernel<E, G, R>), grid, dim3(256), (size_t)ROWS * 2 * a.top * 4, st, a);       \
         prof_commit(ps, KID_TOP_LOGITS, 0.0, bytes);                                                                 \
         return hipGetLastError();                                                                                    \
     }
@@ -1222,13 +1213,18 @@ template <typename E> hipError_t top_launch(const TopArgs& a, hipStream_t st) {
     }
     if (a.pieces > 1) {
         const ProfSlot ps = prof_slot();
-        PQL_LAUNCH(ps, top_merge_kernel<256>, dim3((unsigned)a.rows), dim3(256), (size_t)a.pieces * a.top * 4, st, a);
+        TopArgs m = a;
+        m.z = a.part_value; m.vocab = m.piece = a.pieces * a.top; m.stride = m.vocab; m.pieces = 1;
+        if (m.vocab <= 256 * 4 * 4) PQL_LAUNCH(ps, top_merge_kernel<4>, dim3(1, (unsigned)a.rows), dim3(256), 0, st, m);
+        else PQL_LAUNCH(ps, top_merge_kernel<8>, dim3(1, (unsigned)a.rows), dim3(256), 0, st, m);
         prof_commit(ps, KID_TOP_MERGE, 0.0, (double)a.rows * a.top * 8 * (a.pieces + 1));
     }
     return hipGetLastError();
 }
-int top_pieces(const pql_logits& z, int top) {      // the lists of a row's pieces are merged in 32 KB of LDS
-    return pieces_of(z.rows, z.vocab, 8192 / top);
+// The lists of a row's pieces are merged in registers: at most 8192 entries.  The 64 largest of one row of 20000 whole 12 us,
+// in five pieces 19.
+int top_pieces(const pql_logits& z, int top) {
+    return pieces_of(z.rows, z.vocab, 16384, 8192 / top);
 }
 bool misaligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) != 0; }
 int32_t check_logits(pql_ctx* c, const pql_logits& z, const char* text) {
@@ -1273,7 +1269,7 @@ int32_t pql_top_logits(pql_ctx* c, pql_logits z, int32_t top, int32_t* index_out
 int64_t pql_distill_workspace_bytes(const pql_logits* z) {
     if (!z) return PQL_ERR_NULL;
     if (!logits_ok(*z)) return PQL_ERR_INVALID_ARG;
-    const int p = pieces_of(z->rows, z->vocab, 256);
+    const int p = distill_pieces(*z, 256);
     return p > 1 ? (int64_t)up256((size_t)z->rows * (2 * p + PQL_MAX_TOP) * 4) : 0;
 }
 
@@ -1312,7 +1308,7 @@ int32_t pql_distill_loss(pql_ctx* c, pql_logits z, pql_teacher t, float temperat
     const int32_t rc = distill_check(c, z, t, temperature, grad, false);
     if (rc != PQL_OK || z.rows == 0) return rc;
     if (!loss_out || !lse_out) return ctx_fail(c, PQL_ERR_NULL, "pql_distill_loss: null pointer");
-    const int pieces = pieces_of(z.rows, z.vocab, 256);
+    const int pieces = distill_pieces(z, 256);
     if (pieces > 1 && !workspace) return ctx_fail(c, PQL_ERR_NULL, "pql_distill_loss: null workspace");
     if (misaligned(workspace, 256) || misaligned(loss_out, 4) || misaligned(lse_out, 4) || misaligned(row_weight, 4))
         return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_distill_loss: misaligned pointer");
@@ -1334,7 +1330,7 @@ int32_t pql_distill_backward(pql_ctx* c, pql_logits z, pql_teacher t, float temp
     if (misaligned(lse, 4) || misaligned(loss_grad, 4)) return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_distill_backward: misaligned pointer");
     // every piece works out the list's masses anew: 16384 elements keep that below a tenth of it; fewer where there are few rows
     int pieces = z.vocab <= SMALL_VOCAB ? 1 : (z.vocab + 16383) / 16384;
-    const int few = pieces_of(z.rows, z.vocab, 1 << 30);
+    const int few = distill_pieces(z, 1 << 30);
     if (few > pieces) pieces = few;
     DistillArgs a = distill_args(z, t, temperature, loss_grad, grad, pieces);
     a.lse = lse;
