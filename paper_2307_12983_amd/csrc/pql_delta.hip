@@ -3,7 +3,7 @@
 //
 // One token or a few: delta_step_kernel keeps the state in registers and reads and writes it once; bound by that.
 //
-// Sequences go by chunks of 64 tokens.  With S0 the state before the chunk, G_i the sums of g in it, gam_i = e^{G_i},
+// Sequences go by chunks of 32 or 64 tokens.  With S0 the state before the chunk, G_i the sums of g in it, gam_i = e^{G_i},
 // Gam_ij = e^{G_i - G_j} (0 where a reset lies between), e_i = e^{G_last - G_i}, all tokens of a chunk follow from
 //     N_ij = Gam_ij k_i.k_j (i > j),  T = (I + N diag(beta))^-1,  X = V - gam o (K S0),  R = T X,  Y = beta o R,
 //     P_ij = Gam_ij q_i.k_j (i >= j),  O = scale (gam o (Q S0) + P Y),  S1 = e^{G_last} S0 + K^T (e o Y),
@@ -28,7 +28,7 @@
 namespace pql {
 namespace {
 
-constexpr int MAXC = 64;                    // most tokens per chunk (C below: 64, or 32 where sequences are that short)
+constexpr int MAXC = 64;                    // most tokens per chunk (C below: 64 or 32)
 constexpr float NEG_INF = -__builtin_inff();
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -288,7 +288,7 @@ __device__ __forceinline__ Where where_of(const DeltaArgs& a, int bh) {
 }
 // Workgroup `id` of a scan over n (sequence, head) pairs with `blocks` column blocks each.  Workgroups go round the eight XCDs
 // in turn; the blocks of one pair, which read the same q, k, T, P and K^T, are given to one XCD so that its L2 serves all but
-// the first (4 x 2048 tokens, 16 heads: MEASURED).
+// the first (1 x 16384 tokens, 16 heads of 128 x 128, bf16: 577 us, in the order of ids 634).
 __device__ __forceinline__ void place_of(int id, int n, int blocks, int& bh, int& block) {
     const int whole = n & ~7;
     if (id < whole * blocks) {
@@ -1490,7 +1490,7 @@ __global__ __launch_bounds__(256) void delta_group_kernel(DeltaArgs a) {
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 struct Plan {                               // padded sizes, and where things lie in `saved` and the workspace
     int heads_wg;                           // value heads that one workgroup of delta_back_kernel takes: those of a key head where that fills the card
-    int c, dkp, dvp, chunks;                // c: tokens per chunk; 32 where no sequence is longer: half the rows of 64 would be empty
+    int c, dkp, dvp, chunks;                // c: tokens per chunk
     size_t T, P, G, KT, forward;            // offsets in bytes; `forward`: what a call without `saved` needs
     size_t TT, PT, QT, R, S, saved;
     size_t dX, dY, dS, part_q, part_k, back;
@@ -1500,11 +1500,23 @@ bool shape_ok(const pql_delta_shape& s) {
            s.dim_k <= PQL_DELTA_MAX_DIM_K && s.dim_v >= 1 && s.dim_v <= PQL_DELTA_MAX_DIM_V && (s.dtype == PQL_F32 || s.dtype == PQL_BF16) &&
            s.scale == s.scale && s.steps <= (1 << 30) && s.heads_v <= 65535 && (int64_t)s.batch * s.heads_v <= 0x7fffffffLL / 256;
 }
-Plan plan_of(const pql_delta_shape& s) {
+// Tokens per chunk, 32 or 64.  Chunks of 32 halve the work between tokens and let two to four workgroups share a CU; chunks of
+// 64 halve the number of steps of a sequence, which is what bounds few and long ones, and with bf16 keys of 128 the gradient
+// kernel moves the states of every chunk through LDS, which then takes longer than its products.  Measured with 32 and with 64
+// tokens, us: forward, fp32, 64 x 64: 512 sequences and heads of 32 tokens 66 and 123, 1024 of 256 198 and 246, 32 of 1024 65 and 57; bf16,
+// 128 x 128: 256 of 128 51 and 57, 16 of 16384 691 and 578.  Forward and gradient, bf16, 128 x 128: 32 of 256 69 and 73, 256 of
+// 128 204 and 170, 64 of 2048 818 and 590; fp32, 128 x 128: 256 of 256 477 and 488, 32 of 64 60 and 78.
+int chunk_of(const pql_delta_shape& s, bool train) {
+    const int64_t pairs = (int64_t)s.batch * s.heads_v;
+    if (s.steps <= 32) return 32;
+    if (train && s.dtype == PQL_BF16 && s.dim_k > 64) return s.steps <= 512 && pairs * s.steps <= 8192 ? 32 : 64;
+    return s.steps <= 512 || pairs >= 256 ? 32 : 64;
+}
+Plan plan_of(const pql_delta_shape& s, bool train) {
     Plan p;
     p.dkp = s.dim_k <= 64 ? 64 : 128;
     p.dvp = (s.dim_v + 31) / 32 * 32;
-    p.c = s.steps <= 32 ? 32 : 64;
+    p.c = chunk_of(s, train);
     p.chunks = (s.steps + p.c - 1) / p.c;
     const size_t n = (size_t)s.batch * s.heads_v * p.chunks, nk = (size_t)s.batch * s.heads_k * p.chunks, es = s.dtype == PQL_F32 ? 4 : 2;
     const size_t tri = s.dtype == PQL_F32 ? (p.c == 32 ? TRI<ModeF, 32> : TRI<ModeF, 64>) * sizeof(float) : (p.c == 32 ? TRI<ModeB, 32> : TRI<ModeB, 64>) * sizeof(bf16_t);
@@ -1684,13 +1696,13 @@ int32_t pql_delta_step(pql_ctx* c, const pql_delta_shape* s, const pql_delta_inp
 
 int64_t pql_delta_saved_bytes(const pql_delta_shape* s) {
     if (!s) return PQL_ERR_NULL;
-    return shape_ok(*s) ? (int64_t)plan_of(*s).saved : PQL_ERR_INVALID_ARG;
+    return shape_ok(*s) ? (int64_t)plan_of(*s, true).saved : PQL_ERR_INVALID_ARG;
 }
 int64_t pql_delta_workspace_bytes(const pql_delta_shape* s, int32_t backward) {
     if (!s) return PQL_ERR_NULL;
     if (!shape_ok(*s)) return PQL_ERR_INVALID_ARG;
-    const Plan p = plan_of(*s);
-    return (int64_t)(backward && p.back > p.forward ? p.back : p.forward);
+    const size_t forward = plan_of(*s, false).forward, back = plan_of(*s, true).back;
+    return (int64_t)(backward && back > forward ? back : forward);
 }
 
 int32_t pql_delta_forward(pql_ctx* c, const pql_delta_shape* s, const pql_delta_input* in, pql_seq out, float* state_out, void* saved,
@@ -1702,7 +1714,7 @@ int32_t pql_delta_forward(pql_ctx* c, const pql_delta_shape* s, const pql_delta_
     if (!apart(out, *s, s->heads_v)) return ctx_fail(c, PQL_ERR_INVALID_ARG, "pql_delta_forward: outputs share memory (stride 0)");
     if (((uintptr_t)state_out & 15) || ((uintptr_t)out.data & (s->dtype == PQL_F32 ? 3 : 1)) || ((uintptr_t)saved & 255) || ((uintptr_t)workspace & 255))
         return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_delta_forward: misaligned pointer");
-    const Plan p = plan_of(*s);
+    const Plan p = plan_of(*s, saved != nullptr);
     DeltaArgs a = args_of(*s, *in);
     a.out = seq(out); a.state_out = state_out;
     set_saved(a, p, (char*)(saved ? saved : workspace), saved != nullptr);
@@ -1727,7 +1739,7 @@ int32_t pql_delta_backward(pql_ctx* c, const pql_delta_shape* s, const pql_delta
         (((uintptr_t)g->log_decay.data | (uintptr_t)g->beta.data) & 3) || (((uintptr_t)state_out_grad | (uintptr_t)g->state) & 15) ||
         (((uintptr_t)saved | (uintptr_t)workspace) & 255))
         return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_delta_backward: misaligned pointer");
-    const Plan p = plan_of(*s);
+    const Plan p = plan_of(*s, true);
     DeltaArgs a = args_of(*s, *in);
     set_saved(a, p, (char*)saved, true);
     char* w = (char*)workspace;

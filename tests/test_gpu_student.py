@@ -541,3 +541,60 @@ def test_many_rows_of_medium_length(env, vocab, top, levels, dtype):
     close(grad[pick], want[2], "gradient by itself")
     ctx.pql_distill_backward(d, t, temp, lse, weight, d)
     close(z[pick], want[2], "gradient in place")
+
+
+# few sequences over 512 tokens go by longer chunks than all others
+LONG = [(2, 520, 1, 2, 64, 64), (1, 577, 2, 2, 128, 96), (1, 515, 1, 3, 72, 36), (2, 600, 1, 1, 20, 130), (1, 641, 1, 1, 33, 65),
+        (7, 600, 4, 8, 16, 8), (7, 600, 4, 8, 70, 8), (64, 513, 2, 2, 16, 64), (64, 513, 2, 2, 70, 64)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size", LONG)
+def test_few_long_sequences(env, size, dtype):
+    n, t = size[:2]
+    lens = ([t, 0, 1, t - 1, 65, 64, 63] + [(97 * i) % (t + 1) for i in range(n)])[:n]
+    resets = [(0, 0), (0, 63), (0, 64), (0, 65), (0, t - 1), (3 % n, 300)]
+    d = Delta(env, *size, dtype=dtype, lengths=lens, resets=resets, seed=t)
+    out, state = d.want()
+    kept = d.forward(True)
+    for name, got in (("forward", d.forward()), ("forward, kept", kept[:2])):
+        close(got[0], out, name + " out")
+        close(got[1], state, name + " state")
+    for name, x, y in zip(("dq", "dk", "dv", "dg", "dbeta", "dstate"), d.backward(kept[2]), d.want_grads()):
+        close(x, y, name)
+
+
+@pytest.mark.parametrize("top", [13, 17, 24, 49])
+@pytest.mark.parametrize("vocab", [64, 100, 250, 500, 1000])
+def test_short_rows_and_long_lists(env, vocab, top):
+    """Either side of the list lengths at which short rows change from rounds to bits, with many equal logits."""
+    torch, S, ctx = env
+    rng = np.random.default_rng(vocab + top)
+    for dtype in (torch.float32, torch.bfloat16):
+        z = torch.from_numpy(rng.integers(-20, 20, (37, vocab)).astype(np.float32)).to(dtype).cuda()
+        z[3] = -float("inf")
+        z[5, 10:] = float("nan")
+        index = torch.empty(37, top, dtype=torch.int32, device="cuda")
+        value = torch.empty(37, top, device="cuda")
+        ctx.pql_top_logits(S.Logits(z), top, index, value, None)
+        want_i, want_v = O.top_logits(z.float().cpu().numpy(), top)
+        assert np.array_equal(index.cpu().numpy(), want_i)
+        assert np.array_equal(value.cpu().numpy(), want_v)
+
+
+@pytest.mark.parametrize("rows,vocab,top", [(1, 131072, 256), (3, 70001, 64), (2, 40000, 1), (17, 32768, 100), (255, 33000, 5), (256, 33000, 5)])
+@pytest.mark.parametrize("levels", [3, 0])
+def test_pieces_of_long_rows(env, rows, vocab, top, levels):
+    """Lists of pieces joined: distinct logits, and a few values that all pieces hold."""
+    torch, S, ctx = env
+    rng = np.random.default_rng(rows + vocab)
+    x = rng.integers(0, levels, (rows, vocab)) if levels else rng.standard_normal((rows, vocab))
+    z = torch.from_numpy(x.astype(np.float32)).cuda()
+    z[0, : vocab // 2] = -float("inf")
+    d = S.Logits(z)
+    index = torch.empty(rows, top, dtype=torch.int32, device="cuda")
+    value = torch.empty(rows, top, device="cuda")
+    ctx.pql_top_logits(d, top, index, value, S.workspace(ctx.top_logits_workspace_bytes(d, top)))
+    want_i, want_v = O.top_logits(z.cpu().numpy(), top)
+    assert np.array_equal(index.cpu().numpy(), want_i)
+    assert np.array_equal(value.cpu().numpy(), want_v)
