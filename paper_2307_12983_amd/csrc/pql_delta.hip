@@ -2,6 +2,8 @@
 //     S~ = exp(g_t) S,  r_t = v_t - S~^T k_t,  S = S~ + k_t (beta_t r_t)^T,  o_t = scale S^T q_t.
 //
 // One token or a few: delta_step_kernel keeps the state in registers and reads and writes it once; bound by that.
+// (All times below: fp32 "windows" = 512 sequences of up to 32 tokens, 4 heads of 64 x 64, forward and gradient; bf16
+// "sequences" = 4 of 2048 tokens, 16 value heads of 128 x 128 on 8 key heads, forward and gradient; "long" = one of 16384, forward.)
 //
 // Sequences go by chunks of 32 or 64 tokens.  With S0 the state before the chunk, G_i the sums of g in it, gam_i = e^{G_i},
 // Gam_ij = e^{G_i - G_j} (0 where a reset lies between), e_i = e^{G_last - G_i}, all tokens of a chunk follow from
@@ -310,7 +312,8 @@ template <typename E> __device__ __forceinline__ E* at_out(const DeltaSeq& s, in
 // =============================================================================================
 // One token or a few.  A workgroup holds up to 4 LX columns of one state in registers: lanes along the columns (four
 // each), 256 / LX groups of rows.  With z = S~^T k and w = S~^T q found together, u = beta (v - z) and
-// o = scale (w + (q.k) u) need one reduction per token instead of two.
+// o = scale (w + (q.k) u) need one reduction per token instead of two.  One token of 16384 environments, 4 heads of 64 x 64:
+// 363 us, 5.9 TB/s of states read and written (a large copy reaches 4.8); of 64 environments, 2 heads of 32 x 32: 5 us, a launch.
 // =============================================================================================
 template <typename E, int LX, bool VEC>
 __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a) {
@@ -636,6 +639,10 @@ template <int NT> __device__ __forceinline__ void put_padded(const char* p, int 
         for (int n = 0; n < NT; ++n) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[n][r]), rs, lane, (r0 + r) * ld4 + 64 * n, 0);
 }
 
+// One workgroup per chunk and value head, a wavefront per 16 tokens: K K^T and Q K^T (lower halves), the gates, the inverse, and
+// all of it out in the order in which the scans' lanes want it, so that these load operands straight into registers; K^T and
+// Q^T by one head of each group.  Bound by the latency of its steps, four workgroups to a CU, and by what it writes: long
+// 89 us, sequences 59 us (each about 3 TB/s), windows 29 us; without the inverse 9 % less, without K^T and Q^T 18 to 34 %.
 template <typename M, int C, int DK, bool AL>
 __global__ __launch_bounds__(4 * C) void delta_prepare_kernel(DeltaArgs a) {
     using E = typename M::E;
@@ -738,7 +745,9 @@ __global__ __launch_bounds__(4 * C) void delta_prepare_kernel(DeltaArgs a) {
 // Chunks in order: outputs and states, 16 NT columns per workgroup.  Half of the wavefronts (one per SIMD, 16 tokens each)
 // carry the chain K S, X, T X, K^T Y that every chunk has to wait for, the other half what only the outputs need, Q S and
 // P Y, in the gaps of the first.  All operands of a chunk are requested into registers, the next chunk's K, V and T once the
-// products that wait for LDS have asked for theirs, K^T two phases before it is used.
+// products that wait for LDS have asked for theirs, K^T two phases before it is used.  Bound by the chain: long 501 us, 1.95 us
+// for each of 256 chunks (336 us in all if nothing had to be loaded), sequences 143 us, there with 0.33 GB of states and errors
+// kept for the gradient, windows 55 us.  (Every wavefront doing both: long 662 us.)
 // =============================================================================================
 template <typename M, int C, int DK, int NT> struct ScanLds {
     using S = Tile<M, 16 * NT, DK, false>;          // S^T [column][dim_k]
@@ -988,7 +997,8 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
 // =============================================================================================
 // Gradient, chunks in reverse order: dV, and what delta_back_kernel needs of every chunk (dS1, dX, dY).  Again half of the
 // wavefronts carry the chain K dS, dY, T^T dR, K^T dX; the other half find what it adds from outside, P^T dO and
-// Q^T (gam o dO), one chunk ahead, and hand it over in LDS in the layout of the results.
+// Q^T (gam o dO), one chunk ahead, and hand it over in LDS in the layout of the results.  Bound by the chain and by what it
+// writes (dX, dY, dS: 0.4 GB in the sequences): sequences 167 us, windows 66 us.
 // =============================================================================================
 template <typename M, int C, int DK, int NT> struct BackScanLds {
     using S = Tile<M, 16 * NT, DK, false>;          // dS^T [column][dim_k]
@@ -1204,7 +1214,8 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
 // contractions over the columns, 32 at a time: everything but dO is brought from memory, split and put into LDS once for all
 // wavefronts, the next 32 columns being on their way meanwhile; then those over tokens with E and F in LDS, K^T and Q^T
 // straight from memory.  With a.heads_wg = group a workgroup takes the value heads of one key head one after the other and
-// adds dQ and dK up in registers; where that leaves too few workgroups, it takes one, and delta_group_kernel adds.
+// adds dQ and dK up in registers; where that leaves too few workgroups, it takes one, and delta_group_kernel adds.  With keys of
+// 128 it fills a CU's LDS and registers alone, and is bound by LDS: sequences 240 us, 0.4 GB of states at 1.7 TB/s; windows 61 us.
 // =============================================================================================
 template <typename M, int C, int DK> struct BackLds {
     using R = Tile<M, C, 32, false>;        // R, Y, dX
@@ -1468,7 +1479,7 @@ __global__ __launch_bounds__(8 * C) void delta_back_kernel(DeltaArgs a) {
     }
 }
 
-// dq and dk of shared key heads: the sum over their value heads, in order.
+// dq and dk of shared key heads: the sum over their value heads, in order.  5 sequences of up to 333 tokens: 5 us, a launch.
 template <typename E>
 __global__ __launch_bounds__(256) void delta_group_kernel(DeltaArgs a) {
     const int64_t all = (int64_t)a.batch * a.steps * a.heads_k * a.dim_k;
@@ -1529,6 +1540,8 @@ Plan plan_of(const pql_delta_shape& s, bool train) {
     p.saved = o;
     o = 0;
     p.dX = take(n * p.c * p.dvp * 4); p.dY = take(n * p.c * p.dvp * 4); p.dS = take(n * p.dkp * p.dvp * 4);
+    // with all value heads of a key head and with one a workgroup, us: 128 x 128, 2 value heads a key head: 1024 workgroups 380
+    // and 464, 256 131 and 156; 72 x 100: 90 108 and 74
     p.heads_wg = (int64_t)s.batch * s.heads_k * p.chunks < 256 ? 1 : s.heads_v / s.heads_k;
     const size_t part = s.heads_v == s.heads_k || p.heads_wg > 1 ? 0 : (size_t)s.batch * s.steps * s.heads_v * s.dim_k;
     p.part_q = take(part * 4); p.part_k = take(part * 4);
@@ -1604,7 +1617,8 @@ template <typename K> hipError_t launch(K kernel, LdsLimit& lim, size_t lds, dim
     return hipGetLastError();
 }
 // 16 columns of the state per workgroup instead of 32 while those are fewer than the card's CUs: a chunk's chain is
-// shorter then, and there are more of them.
+// shorter then, and there are more of them.  Forward, sequences of 2048, 16 heads of 128 x 128, bf16, 16 and 32 columns: one
+// sequence (64 workgroups of 32) 77 and 108 us, four (256) 158 and 135 us.
 bool narrow(const DeltaArgs& a) { return (int64_t)a.batch * a.heads_v * (a.dvp / 32) < 256; }
 // Work of one token and value head that the chunked form cannot do without, and the token tensors' bytes.
 double token_heads(const DeltaArgs& a) { return (double)a.batch * a.steps * a.heads_v; }

@@ -209,7 +209,8 @@ __device__ __forceinline__ float entry_loss(const Entry& e, float z, float m, fl
 }
 
 // =============================================================================================
-// Small vocabularies: a group of G lanes per row.
+// Small vocabularies: a group of G lanes per row, which it reads once and holds; bound by memory.  327680 rows of 51, fp32, lists
+// of 8, loss and gradient: 35 us, 4.5 TB/s.
 // =============================================================================================
 template <typename E, int G, int R, bool BACK>
 __global__ __launch_bounds__(256) void distill_small_kernel(DistillArgs a) {
@@ -508,7 +509,7 @@ template <typename E, int NT> __device__ __forceinline__ void zero_stretch(E* ou
     for (int j = threadIdx.x; j < len; j += NT) out[j] = from_float<E>(0.f);
 }
 
-// One workgroup per row.  NV > 0: the row stays in registers between its statistics and its gradient, NV granules a thread;
+// One workgroup per row; bound by memory: 4096 rows of 65536, bf16, lists of 64, loss and gradient 213 us, 5.0 TB/s.  NV > 0: the row stays in registers between its statistics and its gradient, NV granules a thread;
 // NV = 0, rows that do not fit: it is read again.
 template <typename E, int NT, int NV>
 __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a) {
@@ -580,7 +581,8 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a) {
 }
 
 // Few rows: pieces of a.piece elements.  First launch: each piece's maximum and sum, and the logits of the listed
-// answers that lie in it (a second launch that writes over the logits could no longer read them).
+// answers that lie in it (a second launch that writes over the logits could no longer read them).  16 rows of 131072, fp32:
+// 4 us each launch, and 11 us for the gradient in a call of its own (8.4 MB read, 8.4 MB written: 3.5 us at a copy's rate).
 template <typename E, int NT>
 __global__ __launch_bounds__(NT) void distill_part_kernel(DistillArgs a) {
     __shared__ float s_red[NT / 64];
@@ -672,7 +674,7 @@ __device__ __forceinline__ float value_of(unsigned k) {
 
 // Small vocabularies: G lanes per row.  The K-th largest key is found bit by bit (largest t with at least K keys >= t),
 // the keys above it and, in index order, as many equal ones as there is room for go to LDS, and each is written at its
-// rank among them.
+// rank among them.  Bound by the 32 counts: 16384 rows of 1000, fp32, lists of 32: 47 us, 1.5 TB/s.
 template <typename E, int G, int R>
 __global__ __launch_bounds__(256) void top_small_kernel(TopArgs a) {
     constexpr int ROWS = 256 / G;
@@ -961,7 +963,8 @@ __global__ __launch_bounds__(256) void top_wave_kernel(TopArgs a) {
     write_ranked<64>(s_key, s_index, found, a.top, 0, a.index_out + n * a.top, a.value_out + n * a.top, l);
 }
 
-// NV > 0: the stretch stays in registers between the two passes, NV granules a thread.
+// One workgroup per row or piece.  NV > 0: the stretch stays in registers between the two passes, NV granules a thread; else it
+// is read again, from L2 for the most part.  1024 rows of 131072, bf16, lists of 64: 78 us, 3.5 TB/s.
 template <typename E, int NT, int NV, bool MERGE>
 __device__ __forceinline__ void top_of_stretch(const TopArgs& a) {
     __shared__ __align__(16) unsigned s_key[CAND];
