@@ -254,11 +254,20 @@ struct Gates {
     float beta[MAXC], gam[MAXC], end[MAXC];
     float last;                             // e^{G_last}, 0 after a reset in the chunk
 };
-// By the first wavefront; a barrier follows.
-__device__ __forceinline__ void gates_of(Gates& s, const float* g, int64_t g_stride, const float* beta, int64_t b_stride, int len) {
+// By the first wavefront, from the token values that it has requested before; a barrier follows.
+struct GateValues {
+    float g = 0.f, beta = 0.f;
+    __device__ __forceinline__ void load(const float* g_, int64_t g_stride, const float* beta_, int64_t b_stride, int len) {
+        const int i = threadIdx.x;
+        if (i >= min(len, 64)) return;
+        g = g_[i * g_stride];
+        beta = beta_[i * b_stride];
+    }
+};
+__device__ __forceinline__ void gates_of(Gates& s, const GateValues& v) {
     const int i = threadIdx.x;
     if (i >= 64) return;
-    float x = i < len ? g[i * g_stride] : 0.f;
+    float x = v.g;
     const unsigned long long resets = __ballot(x == NEG_INF);
     if (x == NEG_INF) x = 0.f;
     double sum = x;
@@ -268,7 +277,7 @@ __device__ __forceinline__ void gates_of(Gates& s, const float* g, int64_t g_str
     const double total = __shfl(sum, 63);
     s.sum[i] = sum;
     s.part[i] = part;
-    s.beta[i] = i < len ? beta[i * b_stride] : 0.f;
+    s.beta[i] = v.beta;
     s.gam[i] = part == 0 ? expf((float)sum) : 0.f;
     s.end[i] = part == all ? expf((float)(total - sum)) : 0.f;
     if (i == 63) s.last = all == 0 ? expf((float)total) : 0.f;
@@ -660,7 +669,9 @@ __global__ __launch_bounds__(4 * C) void delta_prepare_kernel(DeltaArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, q = l >> 4;
     const E* kp = at<E>(a.k, w.b, t0, w.hk);
     const E* qp = at<E>(a.q, w.b, t0, w.hk);
-    gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
+    GateValues v;
+    v.load(at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
+    gates_of(s_g, v);
     if (w.h % a.group == 0) {               // this key head's transposes
         const KT tile(lds);
         for (int which = 0; which < (a.QT ? 2 : 1); ++which) {
@@ -1266,6 +1277,8 @@ __global__ __launch_bounds__(8 * C) void delta_back_kernel(DeltaArgs a) {
 #pragma unroll
         for (int n = 0; n < NK; ++n) sum_q[n] = sum_k[n] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
+    GateValues v;
+    v.load(at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
     for (int head = 0; head < heads; ++head, ++w.h, ++w.bh) {
         // lane numbers anew for every head: what is worked out from them would otherwise be kept over the loop, in registers
         // that are not there
@@ -1274,7 +1287,6 @@ __global__ __launch_bounds__(8 * C) void delta_back_kernel(DeltaArgs a) {
         const int l = unit & 63, c = l & 15, q = l >> 4, row = 16 * strip + c, i0 = 16 * strip + 4 * q;
         const int64_t at_chunk = (int64_t)w.bh * a.chunks + ch;
         if (head) __syncthreads();          // the last one's gates and sums have been used
-        gates_of(s_g, at<float>(a.g, w.b, t0, w.h), a.g.t, at<float>(a.beta, w.b, t0, w.h), a.beta.t, len);
         const bool first = unit < 4 * C;    // this thread's share of R and dY, or of dX: eight columns of one row
         const int ur = (first ? unit : unit - 4 * C) >> 2, uk = (unit & 3) * 8;
         const float* RX = (first ? a.R : a.dX) + (at_chunk * C + ur) * dvp + uk;
@@ -1296,6 +1308,8 @@ __global__ __launch_bounds__(8 * C) void delta_back_kernel(DeltaArgs a) {
             fo = row_operand<M, AL>(dO, d + 8 * q, a.dim_v, row < len);
         };
         load(0);
+        gates_of(s_g, v);
+        if (MANY && head + 1 < heads) v.load(at<float>(a.g, w.b, t0, w.h + 1), a.g.t, at<float>(a.beta, w.b, t0, w.h + 1), a.beta.t, len);
         floatx4 dq[NK] = {}, ks[NK] = {}, ke[NK] = {}, ef[NW] = {};     // ef: E (first half of the wavefronts) or F
         float yr = 0.f, ss = 0.f;           // dY.R of row ur, <dS1, S0>: this thread's elements
         __syncthreads();                    // gates are there
@@ -1452,6 +1466,7 @@ __global__ __launch_bounds__(8 * C) void delta_back_kernel(DeltaArgs a) {
 #pragma unroll
                 for (int i = 0; i < 2 * NW; ++i) x += s_ext[i];
             const int part = s_g.part[l];
+            const bool reset = part != (l ? s_g.part[l - 1] : 0);       // a log decay of -inf
 #pragma unroll
             for (int d = 1; d < C; d *= 2) {
                 const float o = __shfl_down(x, d);
@@ -1459,7 +1474,7 @@ __global__ __launch_bounds__(8 * C) void delta_back_kernel(DeltaArgs a) {
                 if (l + d < C && p == part) x += o;
             }
             if (l < rows) {
-                *at_out<float>(a.dg, w.b, t0 + l, w.h) = l < len && *at<float>(a.g, w.b, t0 + l, w.h) != NEG_INF ? x : 0.f;
+                *at_out<float>(a.dg, w.b, t0 + l, w.h) = l < len && !reset ? x : 0.f;
                 *at_out<float>(a.dbeta, w.b, t0 + l, w.h) = l < len ? s_yr[l] + s_b[0][l] + s_b[1][l] : 0.f;
             }
         }
