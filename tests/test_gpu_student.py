@@ -598,3 +598,28 @@ def test_pieces_of_long_rows(env, rows, vocab, top, levels):
     want_i, want_v = O.top_logits(z.cpu().numpy(), top)
     assert np.array_equal(index.cpu().numpy(), want_i)
     assert np.array_equal(value.cpu().numpy(), want_v)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size", [(1, 40, 1, 2, 64, 64), (1, 40, 1, 1, 100, 24), (128, 40, 2, 2, 64, 64), (128, 40, 2, 2, 72, 64),
+                                  (1, 520, 1, 1, 64, 16), (1, 520, 1, 1, 128, 40), (64, 513, 2, 2, 16, 64)])
+def test_tokens_far_apart(env, size, dtype):
+    """Tokens 2^21 elements and more from one to the next: a chunk is out of reach of 32-bit offsets."""
+    torch, S, ctx = env
+    d = Delta(env, *size, dtype=dtype, resets=[(0, 0), (0, 33)], seed=3)
+
+    def far(x):
+        n, t, h, dim = x.shape
+        big = torch.empty((t - 1) * 2 ** 21 + n * h * dim, dtype=x.dtype, device="cuda")
+        y = big.as_strided(x.shape, (h * dim, 2 ** 21, dim, 1))
+        y.copy_(x)
+        return y
+    d.v, d.do, d.k = far(d.v), far(d.do), far(d.k)
+    d.given = S.DeltaInput(d.q, d.k, d.v, d.g, d.beta, d.lengths, d.state)
+    out, state = d.want()
+    kept = d.forward(True)
+    for name, got in (("step", d.step()), ("forward", d.forward()), ("forward, kept", kept[:2])):
+        close(got[0], out, name + " out")
+        close(got[1], state, name + " state")
+    for name, x, y in zip(("dq", "dk", "dv", "dg", "dbeta", "dstate"), d.backward(kept[2]), d.want_grads()):
+        close(x, y, name)
