@@ -498,7 +498,7 @@ template <typename M> constexpr int BLOCK = 64 * 8 * M::PLANES;          // elem
 template <typename M, int C> constexpr int TRI = BLOCKS<C> * BLOCK<M>;
 template <int C> __device__ __forceinline__ constexpr int tri_block(int w, int ks) { return C == 32 || w < 2 ? w : 2 * w - 2 + ks; }        // 64: 0 1 2 3 4 5
 template <int C> __device__ __forceinline__ constexpr int tri_block_t(int w, int ks) { return C == 32 ? w : w < 2 ? 2 * w + ks : 2 + w; }
-// K^T, Q^T: [dim_k / 16][C / 32][lane][8] of the tokens' type, one per key head.
+// K^T, Q^T: [dim_k / 16][C / 32][lane][8] of the tokens' type, one per key head; K, Q for narrow scans: [C / 16][dim_k / 32][lane][8].
 template <typename E, int C> __device__ __forceinline__ int64_t kt_at(const DeltaArgs& a, const Where& w, int ch, int dkp) {
     return (((int64_t)w.b * a.heads_k + w.hk) * a.chunks + ch) * dkp * C;
 }
@@ -514,6 +514,11 @@ template <typename M> __device__ __forceinline__ typename M::X load_operand(cons
     } else {
         return F1{*(const bf16x8*)p};
     }
+}
+__device__ __forceinline__ void store_operand(bf16_t* p, const F1& f) { *(bf16x8*)p = f.h; }
+__device__ __forceinline__ void store_operand(float* p, const FF& f) {
+    *(floatx4*)p = floatx4{f.v[0], f.v[1], f.v[2], f.v[3]};
+    *(floatx4*)(p + 4) = floatx4{f.v[4], f.v[5], f.v[6], f.v[7]};
 }
 // An operand straight from a token row.
 template <typename M, bool AL> __device__ __forceinline__ typename M::X row_operand(const typename M::E* row, int d, int dim, bool ok) {
@@ -552,8 +557,8 @@ template <typename M, int C, int DK, bool AL> struct RowOperands {
     int64_t step, stride;
     int left, turn, dk, row, q, lane;       // tokens from this chunk on, C or -C
     typename M::X f[ND];
-    __device__ __forceinline__ RowOperands(const DeltaSeq& s, const Where& w, int h, int dk_, int row_, int q_, int ch, int dir)
-        : p((const char*)at<E>(s, w.b, (int64_t)ch * C, h)), step(dir * C * s.t * (int64_t)ES), stride(s.t * (int64_t)ES), left(w.len - ch * C), turn(dir * C), dk(dk_),
+    __device__ __forceinline__ RowOperands(const DeltaSeq& s, const void*, int64_t, const Where& w, int dk_, int row_, int q_, int ch, int dir)
+        : p((const char*)at<E>(s, w.b, (int64_t)ch * C, w.hk)), step(dir * C * s.t * (int64_t)ES), stride(s.t * (int64_t)ES), left(w.len - ch * C), turn(dir * C), dk(dk_),
           row(row_), q(q_), lane(AL ? row_ * ((int)s.t * ES) + 8 * q_ * ES : 0) {}
     __device__ __forceinline__ void load() {
         const bool ok = row < left;
@@ -639,6 +644,29 @@ struct Chunks {
     __device__ __forceinline__ Chunks(const void* base, int64_t first, int64_t bytes, int ch, int dir) : p((const char*)base + (first + ch) * bytes), step(dir * bytes) {}
     __device__ __forceinline__ void go(bool more) { p += more ? step : 0; }
 };
+// The same from the copy in operand order that the prepare kernel makes for narrow scans, 1 KB in a row a load; a load of the token rows
+// touches 16 of them, and the eight wavefronts' loads keep the caches' front end busy for half of a chunk's time.  One
+// sequence of 16384, 16 heads of 128 x 128, bf16: scan 437 us instead of 500, prepare 99 instead of 89.  Where a scan is not bound by
+// its chain the copy costs more than it gives (1024 sequences and heads of 256 tokens, 64 x 64, fp32: 242 us instead of 198).
+template <typename M, int C, int DK> struct OrderedRows {
+    static constexpr int ND = DK / 32, ES = sizeof(typename M::E);
+    Chunks p;
+    int lane;
+    typename M::X f[ND];
+    __device__ __forceinline__ OrderedRows(const DeltaSeq&, const void* copy, int64_t first, const Where&, int, int row, int q, int ch, int dir)
+        : p((const char*)copy + row / 16 * ND * 512 * ES, first, DK * C * ES, ch, dir), lane((row % 16 + 16 * q) * 8 * ES) {}
+    __device__ __forceinline__ void load() {
+        const auto rs = tokens(p.p);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            if constexpr (ES == 2) f[d].h = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, lane, 512 * ES * d, 0));
+            else load_ff(rs, lane, lane + 16, 512 * ES * d, f[d]);
+        }
+    }
+    __device__ __forceinline__ void go(bool more) { p.go(more); }
+};
+template <typename M, int C, int DK, int NT, bool AL> struct RowsOf { typedef RowOperands<M, C, DK, AL> T; };
+template <typename M, int C, int DK, bool AL> struct RowsOf<M, C, DK, 1, AL> { typedef OrderedRows<M, C, DK> T; };
 // Results to a padded fp32 array, rows r0 + 4 q + r (lane = the byte offset of row 4 q plus the wavefront's and lane's column).
 template <int NT> __device__ __forceinline__ void put_padded(const char* p, int lane, int r0, int ld4, const floatx4 (&x)[NT]) {
     const auto rs = tokens(p);
@@ -692,6 +720,11 @@ __global__ __launch_bounds__(4 * C) void delta_prepare_kernel(DeltaArgs a) {
         const int row = 16 * wave + c;
         const auto fk = row_operand<M, AL>(kp + row * a.k.t, d + 8 * q, a.dim_k, row < len);
         const auto fq = row_operand<M, AL>(qp + row * a.q.t, d + 8 * q, a.dim_k, row < len);
+        if (a.narrow && w.h % a.group == 0) {       // this key head's rows in operand order
+            const int64_t o = kt_at<E, C>(a, w, ch, DK) + ((DK / 32 * wave + d / 32) * 64 + l) * 8;
+            store_operand((E*)a.KO + o, fk);
+            store_operand((E*)a.QO + o, fq);
+        }
 #pragma unroll
         for (int n = 0; n < NW; ++n) {
             if (n > wave) break;
@@ -856,7 +889,7 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
     ChunkGates G, Gn;                               // this chunk's, the next one's
     Chunks pG(a.G, first, GATES<C> * 4, 0, 1);
     if (all < NW) {                                 // the chain
-        RowOperands<M, C, DK, AL> K(a.k, w, w.hk, dk, row, q, 0, 1);
+        typename RowsOf<M, C, DK, NT, AL>::T K(a.k, a.KO, first_k, w, dk, row, q, 0, 1);
         ColumnValues<M, C, NT, AL> V(a.v, w, dv, i0, c0 + c, 0, 1);
         Chunks pT(a.T, first, tri_bytes, 0, 1), pK(a.KT, first_k, kt_bytes, 0, 1);
         Chunks pS(a.S + c0, first, (int64_t)DK * a.dvp * 4, 0, 1), pR(a.R + c0, first, (int64_t)C * a.dvp * 4, 0, 1);
@@ -953,7 +986,7 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
         }
         store_state<RS, NT>(a.state_out, w, wave, q, c0 + c, dk, dv, S);
     } else {                                        // the outputs: rounded to the tokens' type, two terms of S, P, Y are enough
-        RowOperands<M, C, DK, AL> Q(a.q, w, w.hk, dk, row, q, 0, 1);
+        typename RowsOf<M, C, DK, NT, AL>::T Q(a.q, a.QO, first_k, w, dk, row, q, 0, 1);
         ColumnValues<M, C, NT, AL> O(a.out, w, dv, i0, c0 + c, 0, 1);
         Chunks pP(a.P, first, tri_bytes, 0, 1);
         typename M::Y P[KS];
@@ -1042,7 +1075,7 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
     ChunkGates G, Gn;
     Chunks pG(a.G, first, GATES<C> * 4, end, -1);
     if (all < NW) {                                 // the chain
-        RowOperands<M, C, DK, AL> K(a.k, w, w.hk, dk, row, q, end, -1);
+        typename RowsOf<M, C, DK, NT, AL>::T K(a.k, a.KO, first_k, w, dk, row, q, end, -1);
         ColumnValues<M, C, NT, AL> dV(a.dv, w, dv, i0, c0 + c, end, -1);
         Chunks pT(a.TT, first, tri_bytes, end, -1), pK(a.KT, first_k, kt_bytes, end, -1);
         Chunks pS(a.dS + c0, first, (int64_t)DK * a.dvp * 4, end, -1), pX(a.dX + c0, first, (int64_t)C * a.dvp * 4, end, -1),
@@ -1517,7 +1550,8 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 struct Plan {                               // padded sizes, and where things lie in `saved` and the workspace
     int heads_wg;                           // value heads that one workgroup of delta_back_kernel takes: those of a key head where that fills the card
     int c, dkp, dvp, chunks;                // c: tokens per chunk
-    size_t T, P, G, KT, forward;            // offsets in bytes; `forward`: what a call without `saved` needs
+    bool narrow;
+    size_t T, P, G, KT, KO, QO, forward;            // offsets in bytes; `forward`: what a call without `saved` needs
     size_t TT, PT, QT, R, S, saved;
     size_t dX, dY, dS, part_q, part_k, back;
 };
@@ -1549,6 +1583,11 @@ Plan plan_of(const pql_delta_shape& s, bool train) {
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
     p.T = take(n * tri); p.P = take(n * tri); p.G = take(n * 4 * p.c * 4); p.KT = take(nk * p.dkp * p.c * es);
+    // 16 columns of the state per workgroup instead of 32 while those are fewer than the card's CUs: a chunk's chain is
+    // shorter then, and there are more of them.  Forward, sequences of 2048, 16 heads of 128 x 128, bf16, 16 and 32 columns: one
+    // sequence (64 workgroups of 32) 66 and 102 us, four (256) 159 and 135 us.
+    p.narrow = (int64_t)s.batch * s.heads_v * (p.dvp / 32) < 256;
+    p.KO = take(p.narrow ? nk * p.dkp * p.c * es : 0); p.QO = take(p.narrow ? nk * p.dkp * p.c * es : 0);
     p.forward = o;
     p.TT = take(n * tri); p.PT = take(n * tri); p.QT = take(nk * p.dkp * p.c * es);
     p.R = take(n * p.c * p.dvp * 4); p.S = take(n * p.dkp * p.dvp * 4);
@@ -1631,10 +1670,6 @@ template <typename K> hipError_t launch(K kernel, LdsLimit& lim, size_t lds, dim
     prof_commit(ps, kid, flops, bytes);
     return hipGetLastError();
 }
-// 16 columns of the state per workgroup instead of 32 while those are fewer than the card's CUs: a chunk's chain is
-// shorter then, and there are more of them.  Forward, sequences of 2048, 16 heads of 128 x 128, bf16, 16 and 32 columns: one
-// sequence (64 workgroups of 32) 77 and 108 us, four (256) 158 and 135 us.
-bool narrow(const DeltaArgs& a) { return (int64_t)a.batch * a.heads_v * (a.dvp / 32) < 256; }
 // Work of one token and value head that the chunked form cannot do without, and the token tensors' bytes.
 double token_heads(const DeltaArgs& a) { return (double)a.batch * a.steps * a.heads_v; }
 template <typename M, int C, int DK, bool AL> struct Chunked {
@@ -1651,7 +1686,7 @@ template <typename M, int C, int DK, bool AL> struct Chunked {
             auto scan = [&](auto kernel, LdsLimit& lim, int nt, size_t lds) {
                 return launch(kernel, lim, lds, dim3(a.dvp / (16 * nt) * a.batch * a.heads_v), 8 * C, a, KID_DELTA_SCAN, flops, bytes, st);
             };
-            if (narrow(a)) return a.S ? scan(delta_scan_kernel<M, C, DK, 1, AL, true>, lim[0], 1, ScanLds<M, C, DK, 1>::BYTES)
+            if (a.narrow) return a.S ? scan(delta_scan_kernel<M, C, DK, 1, AL, true>, lim[0], 1, ScanLds<M, C, DK, 1>::BYTES)
                                       : scan(delta_scan_kernel<M, C, DK, 1, AL, false>, lim[1], 1, ScanLds<M, C, DK, 1>::BYTES);
             return a.S ? scan(delta_scan_kernel<M, C, DK, 2, AL, true>, lim[2], 2, ScanLds<M, C, DK, 2>::BYTES)
                        : scan(delta_scan_kernel<M, C, DK, 2, AL, false>, lim[3], 2, ScanLds<M, C, DK, 2>::BYTES);
@@ -1662,7 +1697,7 @@ template <typename M, int C, int DK, bool AL> struct Chunked {
             static LdsLimit l_scan, l_narrow, l_back[2];
             const double th = token_heads(a), es = sizeof(typename M::E);
             const double flops = th * (6.0 * a.dim_k + 4.0 * C) * a.dim_v, bytes = th * (es * (2 * a.dim_k + 2 * a.dim_v) + 8.0 * C + 8.0 * a.dim_v);
-            hipError_t e = narrow(a) ? launch(delta_back_scan_kernel<M, C, DK, 1, AL>, l_narrow, BackScanLds<M, C, DK, 1>::BYTES,
+            hipError_t e = a.narrow ? launch(delta_back_scan_kernel<M, C, DK, 1, AL>, l_narrow, BackScanLds<M, C, DK, 1>::BYTES,
                                               dim3(a.dvp / 16 * a.batch * a.heads_v), 8 * C, a, KID_DELTA_BACK_SCAN, flops, bytes, st)
                                      : launch(delta_back_scan_kernel<M, C, DK, 2, AL>, l_scan, BackScanLds<M, C, DK, 2>::BYTES,
                                               dim3(a.dvp / 32 * a.batch * a.heads_v), 8 * C, a, KID_DELTA_BACK_SCAN, flops, bytes, st);
@@ -1696,8 +1731,8 @@ template <typename M> hipError_t chunks_dispatch(const DeltaArgs& a, bool back, 
     return al ? Chunked<M, 64, 128, true>::run(a, back, st) : Chunked<M, 64, 128, false>::run(a, back, st);
 }
 void set_saved(DeltaArgs& a, const Plan& p, char* base, bool keep) {
-    a.chunks = p.chunks; a.dvp = p.dvp;
-    a.T = base + p.T; a.P = base + p.P; a.G = (float*)(base + p.G); a.KT = base + p.KT;
+    a.chunks = p.chunks; a.dvp = p.dvp; a.narrow = p.narrow;
+    a.T = base + p.T; a.P = base + p.P; a.G = (float*)(base + p.G); a.KT = base + p.KT; a.KO = base + p.KO; a.QO = base + p.QO;
     if (!keep) return;
     a.TT = base + p.TT; a.PT = base + p.PT; a.QT = base + p.QT;
     a.R = (float*)(base + p.R); a.S = (float*)(base + p.S);

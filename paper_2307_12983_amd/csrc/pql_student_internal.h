@@ -38,15 +38,16 @@ struct DeltaArgs {
     int batch, steps, heads_k, heads_v, group, dim_k, dim_v;
     int chunks, dvp;                    // chunks of a full sequence; dim_v padded for the arrays below
     int bh0;                            // first (sequence, head) of this launch
+    int narrow;                         // scans take 16 columns a workgroup
     int heads_wg;                       // value heads per workgroup of the gradient's parallel part
     float scale;
     DeltaSeq q, k, v, g, beta, out;
     const int* lengths;
     const float* state;
     float* state_out;
-    // per (sequence, head, chunk), fp32: T and P in operand order, gates; K^T per key head, of the tokens' type.  What only
+    // per (sequence, head, chunk), fp32: T and P in operand order, gates; K^T and, for narrow scans, K and Q per key head, of the tokens' type.  What only
     // the gradient reads may be NULL: T^T, P^T, Q^T, R [64][dvp], S [dim_k padded][dvp] (before the chunk)
-    void *T, *P, *TT, *PT, *KT, *QT;
+    void *T, *P, *TT, *PT, *KT, *QT, *KO, *QO;
     float *G, *R, *S;
     // gradient: dX, dY [64][dvp], dS [dim_k padded][dvp] (after the chunk); dq, dk per value head where those are shared
     DeltaSeq out_grad, dq, dk, dv, dg, dbeta;
