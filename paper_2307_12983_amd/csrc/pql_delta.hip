@@ -299,7 +299,7 @@ __device__ __forceinline__ Where where_of(const DeltaArgs& a, int bh) {
 }
 // Workgroup `id` of a scan over n (sequence, head) pairs with `blocks` column blocks each.  Workgroups go round the eight XCDs
 // in turn; the blocks of one pair, which read the same q, k, T, P and K^T, are given to one XCD so that its L2 serves all but
-// the first (1 x 16384 tokens, 16 heads of 128 x 128, bf16: 577 us, in the order of ids 634).
+// the first (1 x 16384 tokens, 16 heads of 128 x 128, bf16: 529 us, in the order of ids 580).
 __device__ __forceinline__ void place_of(int id, int n, int blocks, int& bh, int& block) {
     const int whole = n & ~7;
     if (id < whole * blocks) {
@@ -679,7 +679,7 @@ template <int NT> __device__ __forceinline__ void put_padded(const char* p, int 
 // One workgroup per chunk and value head, a wavefront per 16 tokens: K K^T and Q K^T (lower halves), the gates, the inverse, and
 // all of it out in the order in which the scans' lanes want it, so that these load operands straight into registers; K^T and
 // Q^T by one head of each group.  Bound by the latency of its steps, four workgroups to a CU, and by what it writes: long
-// 89 us, sequences 59 us (each about 3 TB/s), windows 29 us; without the inverse 9 % less, without K^T and Q^T 18 to 34 %.
+// 99 us, sequences 60 us (each about 3 TB/s), windows 29 us; without the inverse 9 % less, without K^T and Q^T 18 to 34 %.
 template <typename M, int C, int DK, bool AL>
 __global__ __launch_bounds__(4 * C) void delta_prepare_kernel(DeltaArgs a) {
     using E = typename M::E;
@@ -789,8 +789,8 @@ __global__ __launch_bounds__(4 * C) void delta_prepare_kernel(DeltaArgs a) {
 // Chunks in order: outputs and states, 16 NT columns per workgroup.  Half of the wavefronts (one per SIMD, 16 tokens each)
 // carry the chain K S, X, T X, K^T Y that every chunk has to wait for, the other half what only the outputs need, Q S and
 // P Y, in the gaps of the first.  All operands of a chunk are requested into registers, the next chunk's K, V and T once the
-// products that wait for LDS have asked for theirs, K^T two phases before it is used.  Bound by the chain: long 501 us, 1.95 us
-// for each of 256 chunks (336 us in all if nothing had to be loaded), sequences 143 us, there with 0.33 GB of states and errors
+// products that wait for LDS have asked for theirs, K^T two phases before it is used.  Bound by the chain: long 435 us, 1.7 us
+// for each of 256 chunks (336 us in all if nothing had to be loaded), sequences 142 us, there with 0.33 GB of states and errors
 // kept for the gradient, windows 55 us.  (Every wavefront doing both: long 662 us.)
 // =============================================================================================
 template <typename M, int C, int DK, int NT> struct ScanLds {
@@ -1563,9 +1563,9 @@ bool shape_ok(const pql_delta_shape& s) {
 // Tokens per chunk, 32 or 64.  Chunks of 32 halve the work between tokens and let two to four workgroups share a CU; chunks of
 // 64 halve the number of steps of a sequence, which is what bounds few and long ones, and with bf16 keys of 128 the gradient
 // kernel moves the states of every chunk through LDS, which then takes longer than its products.  Measured with 32 and with 64
-// tokens, us: forward, fp32, 64 x 64: 512 sequences and heads of 32 tokens 66 and 123, 1024 of 256 198 and 246, 32 of 1024 65 and 57; bf16,
-// 128 x 128: 256 of 128 51 and 57, 16 of 16384 691 and 578.  Forward and gradient, bf16, 128 x 128: 32 of 256 69 and 73, 256 of
-// 128 204 and 170, 64 of 2048 818 and 590; fp32, 128 x 128: 256 of 256 477 and 488, 32 of 64 60 and 78.
+// tokens, us: forward, fp32, 64 x 64: 2048 sequences times heads of 32 tokens 66 and 123, 1024 of 256 198 and 246, 32 of 1024 65 and 59; bf16,
+// 128 x 128: 256 of 128 51 and 57, 16 of 16384 690 and 533.  Forward and gradient, bf16, 128 x 128: 256 of 128 204
+// and 170, 64 of 2048 815 and 579; few, 4 of 128, 49 and 58; fp32, 128 x 128: 256 of 256 465 and 477, 32 of 64 59 and 75.
 int chunk_of(const pql_delta_shape& s, bool train) {
     const int64_t pairs = (int64_t)s.batch * s.heads_v;
     if (s.steps <= 32) return 32;
