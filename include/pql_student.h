@@ -49,8 +49,9 @@ typedef struct {
  * (stride_h = 1 when dense); lengths[batch] (int32, or NULL: all `steps`): tokens of each sequence that count,
  * clamped to [0, steps]; what lies behind them is not read; state: fp32 [batch][heads_v][dim_k][dim_v]
  * contiguous, 16-byte aligned, or NULL (zeros).
- * log_decay <= 0; -inf forgets the whole state before the token (the first token of an episode).  Nothing is
- * normalised here: with keys of unit length and beta in [0, 2] the state stays bounded. */
+ * log_decay <= 0; -inf, and any other value whose exponential is 0 in fp32 (below about -104, the type's lowest among
+ * them), forgets the whole state before the token (the first token of an episode).  Nothing is normalised here: with
+ * keys of unit length and beta in [0, 2] the state stays bounded. */
 typedef struct {
     pql_seq q, k, v, log_decay, beta;
     const int32_t* lengths;
@@ -85,8 +86,9 @@ int32_t pql_delta_forward(pql_ctx* ctx, const pql_delta_shape* shape, const pql_
 /* Gradient of a loss whose gradients with respect to the outputs are out_grad (dtype) and, for the last
  * states, state_out_grad (fp32, laid out as the state; NULL: zeros).  input and saved: as given to and left by
  * pql_delta_forward of the same shape; input.state must still hold what the call read (do not let state_out
- * overwrite it).  The gradient of a log_decay of -inf is 0.  Key heads shared by several value heads receive
- * the sum over them, always added in the same order.  workspace: pql_delta_workspace_bytes(shape, 1) bytes. */
+ * overwrite it).  The gradient of a log_decay that forgets the state is 0.  Key heads shared by several value
+ * heads receive the sum over them, always added in the same order.  workspace: pql_delta_workspace_bytes(shape, 1)
+ * bytes. */
 int32_t pql_delta_backward(pql_ctx* ctx, const pql_delta_shape* shape, const pql_delta_input* input, const void* saved,
                            pql_seq out_grad, const float* state_out_grad, const pql_delta_grad* grads,
                            void* workspace, void* stream);

@@ -6,7 +6,7 @@
 // "sequences" = 4 of 2048 tokens, 16 value heads of 128 x 128 on 8 key heads, forward and gradient; "long" = one of 16384, forward.)
 //
 // Sequences go by chunks of 32 or 64 tokens.  With S0 the state before the chunk, G_i the sums of g in it, gam_i = e^{G_i},
-// Gam_ij = e^{G_i - G_j} (0 where a reset lies between), e_i = e^{G_last - G_i}, all tokens of a chunk follow from
+// Gam_ij = e^{G_i - G_j} (0 where a reset lies between: a g for which e^g is 0 in fp32), e_i = e^{G_last - G_i}, all tokens of a chunk follow from
 //     N_ij = Gam_ij k_i.k_j (i > j),  T = (I + N diag(beta))^-1,  X = V - gam o (K S0),  R = T X,  Y = beta o R,
 //     P_ij = Gam_ij q_i.k_j (i >= j),  O = scale (gam o (Q S0) + P Y),  S1 = e^{G_last} S0 + K^T (e o Y),
 // R being the errors r_t.  delta_prepare_kernel finds T and P of all chunks at once; delta_scan_kernel goes through the
@@ -31,7 +31,6 @@ namespace pql {
 namespace {
 
 constexpr int MAXC = 64;                    // most tokens per chunk (C below: 64 or 32)
-constexpr float NEG_INF = -__builtin_inff();
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -249,12 +248,14 @@ __device__ __forceinline__ void stage_transposed(const T& tile, const typename M
 
 // ---- gates of a chunk -------------------------------------------------------------------------
 struct Gates {
-    double sum[MAXC];                       // G_i; double, so that differences of long sums stay exact
+    double sum[MAXC];                       // G_i, counted from the last reset on; double, so that differences of long sums stay exact
     int part[MAXC];                         // resets up to and including the token
     float beta[MAXC], gam[MAXC], end[MAXC];
     float last;                             // e^{G_last}, 0 after a reset in the chunk
 };
-// By the first wavefront, from the token values that it has requested before; a barrier follows.
+// By the first wavefront, from the token values that it has requested before; a barrier follows.  Every g for which e^g is 0 in
+// fp32, as the recurrent form has it, is a reset, and sums begin anew behind it: kept in the sum, a g of -1e12 would cost all
+// that follow the bits of their differences, and one that is not a number would reach beyond the reset.
 struct GateValues {
     float g = 0.f, beta = 0.f;
     __device__ __forceinline__ void load(const float* g_, int64_t g_stride, const float* beta_, int64_t b_stride, int len) {
@@ -267,13 +268,13 @@ struct GateValues {
 __device__ __forceinline__ void gates_of(Gates& s, const GateValues& v) {
     const int i = threadIdx.x;
     if (i >= 64) return;
-    float x = v.g;
-    const unsigned long long resets = __ballot(x == NEG_INF);
-    if (x == NEG_INF) x = 0.f;
-    double sum = x;
+    const bool reset = expf(v.g) == 0.f;
+    const unsigned long long resets = __ballot(reset), before = resets & (~0ull >> (63 - i));
+    const int start = before ? 63 - __clzll(before) : 0;        // the last reset's place
+    double sum = reset ? 0.f : v.g;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) { const double o = __shfl_up(sum, d); if (i >= d) sum += o; }
-    const int part = __popcll(resets & (~0ull >> (63 - i))), all = __popcll(resets);
+    for (int d = 1; d < 64; d *= 2) { const double o = __shfl_up(sum, d); if (i - d >= start) sum += o; }
+    const int part = __popcll(before), all = __popcll(resets);
     const double total = __shfl(sum, 63);
     s.sum[i] = sum;
     s.part[i] = part;
@@ -1499,7 +1500,7 @@ __global__ __launch_bounds__(8 * C) void delta_back_kernel(DeltaArgs a) {
 #pragma unroll
                 for (int i = 0; i < 2 * NW; ++i) x += s_ext[i];
             const int part = s_g.part[l];
-            const bool reset = part != (l ? s_g.part[l - 1] : 0);       // a log decay of -inf
+            const bool reset = part != (l ? s_g.part[l - 1] : 0);       // a log decay that leaves nothing
 #pragma unroll
             for (int d = 1; d < C; d *= 2) {
                 const float o = __shfl_down(x, d);
