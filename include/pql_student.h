@@ -51,7 +51,11 @@ typedef struct {
  * contiguous, 16-byte aligned, or NULL (zeros).
  * log_decay <= 0; -inf, and any other value whose exponential is 0 in fp32 (below about -104, the type's lowest among
  * them), forgets the whole state before the token (the first token of an episode).  Nothing is normalised here: with
- * keys of unit length and beta in [0, 2] the state stays bounded. */
+ * keys of unit length and beta in [0, 2] the state stays bounded.
+ * Values that are not finite reach what the recurrence takes them to: later tokens of their own episode, nothing
+ * before them and nothing from the next token that forgets the state on, in either form.  Gradients of other episodes
+ * are what they would be without them; within the episode they need not be finite.  Sequences with such values are worked
+ * through token by token in every form, which takes longer (about 1.5 us a token). */
 typedef struct {
     pql_seq q, k, v, log_decay, beta;
     const int32_t* lengths;

@@ -233,7 +233,8 @@ __device__ __forceinline__ void load8(const float* p, float* x) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
 }
-// The chunk's tokens transposed: tile[d][token], d < D.
+// The chunk's tokens transposed: tile[d][token], d < D.  Values that are not finite are left out: these are operands in which all
+// tokens of a chunk meet, with a factor of 0 where they must not.  Such a token's own results still show it, through its row operands.
 template <typename M, int C, int D, bool AL, typename T>
 __device__ __forceinline__ void stage_transposed(const T& tile, const typename M::E* base, int64_t stride_t, int len, int dim, int d0 = 0) {
     for (int u = threadIdx.x; u < D / 8 * (C / 4); u += 4 * C) {
@@ -242,7 +243,12 @@ __device__ __forceinline__ void stage_transposed(const T& tile, const typename M
 #pragma unroll
         for (int i = 0; i < 4; ++i) load8<typename M::E, AL>(base + (t + i) * stride_t, d0 + d, dim, t + i < len, x[i]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) tile.put4(d + j, t, floatx4{x[0][j], x[1][j], x[2][j], x[3][j]});
+        for (int j = 0; j < 8; ++j) {
+            floatx4 y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = __builtin_isfinite(x[i][j]) ? x[i][j] : 0.f;
+            tile.put4(d + j, t, y);
+        }
     }
 }
 
@@ -285,6 +291,12 @@ __device__ __forceinline__ void gates_of(Gates& s, const GateValues& v) {
 }
 // f x, and 0 for f = 0 whatever x is: behind a reset nothing is left of a state that is not finite.
 __device__ __forceinline__ float damp(float f, float x) { return f == 0.f ? 0.f : f * x; }
+// 0 as long as all it is given is finite, and not a number from then on.
+__device__ __forceinline__ float watch(float odd, floatx4 x) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) odd = fmaf(x[r], 0.f, odd);
+    return odd;
+}
 __device__ __forceinline__ float decay(const Gates& s, int i, int j) {
     return s.part[i] == s.part[j] ? expf((float)(s.sum[i] - s.sum[j])) : 0.f;
 }
@@ -835,6 +847,117 @@ template <typename M, int C, int RS> __device__ __forceinline__ void load_kt(con
             else load_ff(rs, 32 * l, 32 * l + 16, o, x[s][k]);
         }
 }
+// The lane's number, found anew: what depends on it behind a loop is then not kept in registers over the loop.
+__device__ __forceinline__ int lane_anew() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)); }
+// A sequence and 16 NT columns of its state once more, token by token: for those in which something has come up that is not
+// finite.  A product over a chunk has a factor of 0 wherever a token must not reach another one (behind a reset, or the later of
+// the two), and that does not stop such a value; here tokens meet through the state alone, and the results are those of
+// delta_step_kernel.  What the scans watch is enough: whatever such a value spoils in a chunk is not finite itself and shows in an output
+// (dV in the gradient) or in the last state.  THREADS / COLS groups of rows, a column per thread, two barriers a token: 1.5 us a token (one of
+// 16384, 16 heads of 128 x 128, bf16: 24 ms instead of 0.4; the windows 0.17 ms instead of 0.05); finite sequences pay nothing measurable.
+template <int C, int DK, int NT> struct ByTokens {
+    static constexpr int THREADS = 8 * C, COLS = 16 * NT, G = THREADS / COLS, R = DK / G;
+    struct Lds { float k[DK], q[DK], a[G][COLS], b[G][COLS], qk[G]; };
+    static constexpr int BYTES = 2 * sizeof(Lds);
+    static_assert(DK % G == 0 && THREADS >= 2 * DK, "rows and loads go round evenly");
+    Lds* s;
+    int t, c, g, col;
+    bool real;                                      // a column of the state, not padding
+    __device__ __forceinline__ ByTokens(void* lds, int thread, int c0, int dv) : s((Lds*)lds), t(thread), c(t % COLS), g(t / COLS), col(c0 + c), real(col < dv) {}
+    __device__ __forceinline__ int row(int i) const { return g + G * i; }
+    template <typename E> __device__ __forceinline__ void tokens_in(Lds& l, const DeltaArgs& a, const Where& w, int n) const {
+        if (t < DK) l.k[t] = t < a.dim_k ? to_float(at<E>(a.k, w.b, n, w.hk)[t]) : 0.f;
+        else if (t < 2 * DK) l.q[t - DK] = t - DK < a.dim_k ? to_float(at<E>(a.q, w.b, n, w.hk)[t - DK]) : 0.f;
+    }
+    __device__ __forceinline__ void load(const float* p, const Where& w, const DeltaArgs& a, float (&x)[R]) const {
+#pragma unroll
+        for (int i = 0; i < R; ++i) x[i] = p && real && row(i) < a.dim_k ? p[((int64_t)w.bh * a.dim_k + row(i)) * a.dim_v + col] : 0.f;
+    }
+    __device__ __forceinline__ void store(float* p, const Where& w, const DeltaArgs& a, const float (&x)[R]) const {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (p && real && row(i) < a.dim_k) p[((int64_t)w.bh * a.dim_k + row(i)) * a.dim_v + col] = x[i];
+    }
+    __device__ __forceinline__ void keep(float* p, int64_t chunk, const DeltaArgs& a, const float (&x)[R]) const {
+#pragma unroll
+        for (int i = 0; i < R; ++i) p[(chunk * DK + row(i)) * a.dvp + col] = x[i];
+    }
+    template <typename E> __device__ __forceinline__ void forward(const DeltaArgs& a, const Where& w, bool kept) const {
+        const int64_t first = (int64_t)w.bh * a.chunks;
+        float x[R];
+        load(a.state, w, a, x);
+        for (int n = 0; n < w.len; ++n) {
+            Lds& l = s[n & 1];
+            if (kept && n % C == 0) keep(a.S, first + n / C, a, x);
+            tokens_in<E>(l, a, w, n);
+            const float alpha = expf(*at<float>(a.g, w.b, n, w.h)), beta = *at<float>(a.beta, w.b, n, w.h);
+            const float v = real ? to_float(at<E>(a.v, w.b, n, w.h)[col]) : 0.f;
+            __syncthreads();
+            float z = 0.f, o = 0.f, qk = 0.f;
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const float k = l.k[row(i)], q = l.q[row(i)];
+                x[i] = damp(alpha, x[i]);
+                z += x[i] * k; o += x[i] * q; qk += q * k;
+            }
+            l.a[g][c] = z; l.b[g][c] = o;
+            if (c == 0) l.qk[g] = qk;
+            __syncthreads();
+            z = o = qk = 0.f;
+            for (int i = 0; i < G; ++i) { z += l.a[i][c]; o += l.b[i][c]; qk += l.qk[i]; }
+            const float r = real ? v - z : 0.f, u = real ? beta * r : 0.f;
+#pragma unroll
+            for (int i = 0; i < R; ++i) x[i] = row(i) < a.dim_k ? x[i] + l.k[row(i)] * u : 0.f;
+            if (g == 0 && real) at_out<E>(a.out, w.b, n, w.h)[col] = from_float<E>(a.scale * (o + qk * u));
+            if (g == 0 && kept) a.R[(first * C + n) * a.dvp + col] = r;
+        }
+        if (kept)
+            for (int n = w.len + g; n % C != 0 && n / C == (w.len - 1) / C; n += G) a.R[(first * C + n) * a.dvp + col] = 0.f;
+        store(a.state_out, w, a, x);
+    }
+    // y is the state's gradient without what the chunk's later tokens take of it: dY is what a chunk's products give.
+    template <typename E> __device__ __forceinline__ void backward(const DeltaArgs& a, const Where& w) const {
+        const int64_t first = (int64_t)w.bh * a.chunks;
+        float x[R], y[R];
+        load(a.state_grad, w, a, x);
+        for (int n = w.len + g; n % C != 0 && n / C == (w.len - 1) / C; n += G) a.dX[(first * C + n) * a.dvp + col] = a.dY[(first * C + n) * a.dvp + col] = 0.f;
+        for (int n = w.len - 1; n >= 0; --n) {
+            Lds& l = s[n & 1];
+            if (n == w.len - 1 || n % C == C - 1) {
+                keep(a.dS, first + n / C, a, x);
+#pragma unroll
+                for (int i = 0; i < R; ++i) y[i] = x[i];
+            }
+            tokens_in<E>(l, a, w, n);
+            const float alpha = expf(*at<float>(a.g, w.b, n, w.h)), beta = *at<float>(a.beta, w.b, n, w.h);
+            const float o = real ? a.scale * to_float(at<E>(a.out_grad, w.b, n, w.h)[col]) : 0.f;
+            __syncthreads();
+            float zx = 0.f, zy = 0.f;
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const float k = l.k[row(i)], add = row(i) < a.dim_k && real ? l.q[row(i)] * o : 0.f;
+                x[i] += add; y[i] += add;
+                zx += x[i] * k; zy += y[i] * k;
+            }
+            l.a[g][c] = zx; l.b[g][c] = zy;
+            __syncthreads();
+            zx = zy = 0.f;
+            for (int i = 0; i < G; ++i) { zx += l.a[i][c]; zy += l.b[i][c]; }
+            const float dx = real ? beta * zx : 0.f;
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                x[i] = damp(alpha, row(i) < a.dim_k && real ? x[i] - l.k[row(i)] * dx : 0.f);
+                y[i] = damp(alpha, y[i]);
+            }
+            if (g == 0) {
+                a.dX[(first * C + n) * a.dvp + col] = dx;
+                a.dY[(first * C + n) * a.dvp + col] = real ? zy : 0.f;
+                if (real) at_out<E>(a.dv, w.b, n, w.h)[col] = from_float<E>(dx);
+            }
+        }
+        store(a.dstate, w, a, x);
+    }
+};
 struct ChunkGates {                         // of this lane's tokens i0 .. i0 + 3
     floatx4 gam, end, beta;
     float last;
@@ -889,6 +1012,8 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
     const int64_t first_k = ((int64_t)w.b * a.heads_k + w.hk) * a.chunks;
     ChunkGates G, Gn;                               // this chunk's, the next one's
     Chunks pG(a.G, first, GATES<C> * 4, 0, 1);
+    __shared__ int s_odd;                           // whether anything that is not finite has come up
+    if (threadIdx.x == 0) s_odd = 0;
     if (all < NW) {                                 // the chain
         typename RowsOf<M, C, DK, NT, AL>::T K(a.k, a.KO, first_k, w, dk, row, q, 0, 1);
         ColumnValues<M, C, NT, AL> V(a.v, w, dv, i0, c0 + c, 0, 1);
@@ -985,12 +1110,26 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
             }
             G = Gn;
         }
-        store_state<RS, NT>(a.state_out, w, wave, q, c0 + c, dk, dv, S);
+        float odd = 0.f;
+#pragma unroll
+        for (int s = 0; s < RS; ++s)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) odd = watch(odd, S[s][n]);
+        if (chunks > 0) {
+            if (odd != 0.f) s_odd = 1;
+            __syncthreads();
+        }
+        if (chunks == 0 || !s_odd) {
+            const int l = lane_anew();
+            store_state<RS, NT>(a.state_out, w, wave, l >> 4, c0 + (l & 15), dk, dv, S);
+            return;
+        }
     } else {                                        // the outputs: rounded to the tokens' type, two terms of S, P, Y are enough
         typename RowsOf<M, C, DK, NT, AL>::T Q(a.q, a.QO, first_k, w, dk, row, q, 0, 1);
         ColumnValues<M, C, NT, AL> O(a.out, w, dv, i0, c0 + c, 0, 1);
         Chunks pP(a.P, first, tri_bytes, 0, 1);
         typename M::Y P[KS];
+        float odd = 0.f;
         if (chunks > 0) {
             Q.load(); G.load<C>(pG, i0);
             load_tri<M, C, false>(pP, wave, l, P);
@@ -1030,13 +1169,19 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
             pP.go(more);
             load_tri<M, C, false>(pP, wave, l, P);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) o[n] *= a.scale;
+            for (int n = 0; n < NT; ++n) { o[n] *= a.scale; odd = watch(odd, o[n]); }
             O.put(a.steps - ch * C, o);
             O.go(true);
         }
         const int n = min(16 * NT, dv - c0);
         if (n > 0 && a.steps > chunks * C && all == NW) zero_rows<E>(a.out, w, chunks * C, a.steps, c0, n);
+        if (chunks == 0) return;
+        if (odd != 0.f) s_odd = 1;
+        __syncthreads();
+        if (!s_odd) return;
     }
+    static_assert(ByTokens<C, DK, NT>::BYTES <= L::BYTES, "what goes by tokens takes the tiles' place");
+    ByTokens<C, DK, NT>(lds, 64 * all + lane_anew(), c0, dv).template forward<E>(a, w, KEEP);
 }
 
 // =============================================================================================
@@ -1075,6 +1220,8 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
     const int end = max(chunks - 1, 0);
     ChunkGates G, Gn;
     Chunks pG(a.G, first, GATES<C> * 4, end, -1);
+    __shared__ int s_odd;
+    if (threadIdx.x == 0) s_odd = 0;
     if (all < NW) {                                 // the chain
         typename RowsOf<M, C, DK, NT, AL>::T K(a.k, a.KO, first_k, w, dk, row, q, end, -1);
         ColumnValues<M, C, NT, AL> dV(a.dv, w, dv, i0, c0 + c, end, -1);
@@ -1085,6 +1232,7 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
         typename M::X kt[RS][KS];
         typename M::Y T[KS];
         floatx4 S[RS][NT];
+        float odd = 0.f;
         if (chunks > 0) {
             K.load(); G.load<C>(pG, i0);
             load_tri<M, C, true>(pT, wave, l, T);
@@ -1171,12 +1319,26 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
             pK.go(more);
             load_kt<M, C, RS>(pK, wave, l, kt);
             G = Gn;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) odd = watch(odd, dx[n]);
             put_padded<NT>(pX.p, lane_r, 0, ld4, dx);
             pX.go(true);
             dV.put(a.steps - ch * C, dx);
             dV.go(true);
         }
-        store_state<RS, NT>(a.dstate, w, wave, q, c0 + c, dk, dv, S);
+#pragma unroll
+        for (int s = 0; s < RS; ++s)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) odd = watch(odd, S[s][n]);
+        if (chunks > 0) {
+            if (odd != 0.f) s_odd = 1;
+            __syncthreads();
+        }
+        if (chunks == 0 || !s_odd) {
+            const int l = lane_anew();
+            store_state<RS, NT>(a.dstate, w, wave, l >> 4, c0 + (l & 15), dk, dv, S);
+            return;
+        }
     } else {                                        // P^T dO and Q^T (gam o dO), a chunk ahead of the chain
         ColumnValues<M, C, NT, AL> O(a.out_grad, w, dv, i0, c0 + c, end, -1);
         Chunks pP(a.PT, first, tri_bytes, end, -1), pQ(a.QT, first_k, kt_bytes, end, -1);
@@ -1251,7 +1413,12 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
         }
         const int n = min(16 * NT, dv - c0);
         if (n > 0 && a.steps > chunks * C && all == NW) zero_rows<E>(a.dv, w, chunks * C, a.steps, c0, n);
+        if (chunks == 0) return;
+        __syncthreads();
+        if (!s_odd) return;
     }
+    static_assert(ByTokens<C, DK, NT>::BYTES <= L::BYTES, "what goes by tokens takes the tiles' place");
+    ByTokens<C, DK, NT>(lds, 64 * all + lane_anew(), c0, dv).template backward<E>(a, w);
 }
 
 // =============================================================================================
@@ -1415,7 +1582,7 @@ __global__ __launch_bounds__(8 * C) void delta_back_kernel(DeltaArgs a) {
                 const int i = i0 + r;
                 const float g = n <= strip && i >= j ? decay(s_g, i, j) : 0.f;
                 x[r] = half == 0 ? damp(a.scale * g, x[r]) : i > j ? damp(-g, x[r]) : 0.f;
-                y[r] = half == 0 ? x[r] : x[r] * beta;
+                y[r] = half == 0 ? x[r] : damp(x[r], beta);
             }
             // rows of the transposes are columns here: four consecutive elements of one row each; of the others one at a time
             if (half == 0) {

@@ -37,3 +37,118 @@ def test_finite_decays_that_leave_nothing(env, size, dtype, value):
         close(got[1], state, name + " state")
     for name, got, want in zip(GRADS, d.backward(d.forward(True)[2]), d.want_grads()):
         close(got, held(want), name)
+
+
+# ---- values that are not finite ----------------------------------------------------------------
+# An episode from token 5 to 11 or, for states, from the start to 11; good ones around it, in the same chunks.
+POISON = ["state inf", "state nan", "v inf", "v nan", "k nan", "k inf", "q nan", "beta nan", "decay nan"]
+
+
+def poisoned(env, size, dtype, kind, layout="dense"):
+    torch = env[0]
+    t = size[1]
+    whole = kind.startswith("state")
+    d = Delta(env, *size, dtype=dtype, layout=layout, resets=[(0, i) for i in ((12, 40, 64, t - 2) if whole else (5, 12, 40, 64, t - 2))], seed=t + 1)
+    what, value = kind.split()
+    value = float(value)
+    if whole:
+        d.state[0, 0, 1, 2] = value
+        d.host_state[0, 0, 1, 2] = value
+    else:
+        at = {"v": (0, 7, 0, 2), "k": (0, 7, 0, 1), "q": (0, 7, 0, 1), "beta": (0, 7, 0), "decay": (0, 7, 0)}[what]
+        i = ["q", "k", "v", "decay", "beta"].index(what)
+        (d.q, d.k, d.v, d.g, d.beta)[i][at] = value
+        d.host[i][at] = value
+    torch.cuda.synchronize()
+    return d, (range(0, 12) if whole else range(5, 12))
+
+
+SICK = [(2, 70, 1, 2, 32, 40), (2, 70, 1, 1, 128, 24), (64, 66, 2, 4, 20, 36), (64, 66, 2, 4, 72, 64), (1, 577, 1, 1, 64, 20), (1, 577, 1, 2, 128, 33)]
+
+
+@pytest.mark.parametrize("kind", POISON)
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size", SICK)
+@pytest.mark.filterwarnings("ignore:invalid value:RuntimeWarning")
+def test_values_that_are_not_finite_stay_in_their_episode(env, size, dtype, kind):
+    """Both forms give what the recurrence gives: finite wherever that is, in other episodes of the same chunk and
+    before the value, and gradients of all other episodes as if there were none."""
+    d, bad = poisoned(env, size, dtype, kind)
+    out, state = d.want()
+    kept = d.forward(True)
+    for name, got in (("step", d.step()), ("forward", d.forward()), ("forward, kept", kept[:2])):
+        for part, x, y in zip((" out", " state"), got, (out, state)):
+            host, fine = x.double().cpu().numpy(), np.isfinite(y)
+            assert np.array_equal(np.isfinite(host), fine), name + part + ": finite in other places than the recurrence's"
+            close(x[torch_mask(x, fine)], y[fine], name + part)
+    good = np.ones(size[1], bool)
+    good[list(bad)] = False
+    want = d.want_grads()
+    grads = d.backward(kept[2])
+    for name, x, y in zip(GRADS[:5], grads, want):
+        assert np.isfinite(y[:, good]).all(), name
+        close(x[:, torch_mask(x, good)], y[:, good], name)
+    fine = np.isfinite(want[5])
+    if not kind.startswith("state"):
+        assert fine.all()
+    close(grads[5][torch_mask(grads[5], fine)], want[5][fine], "dstate")
+
+
+def torch_mask(x, mask):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(mask)).to(x.device)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("layout", ["offset", "packed"])
+@pytest.mark.filterwarnings("ignore:invalid value:RuntimeWarning")
+def test_values_that_are_not_finite_in_other_layouts(env, layout, dtype):
+    d, bad = poisoned(env, (2, 70, 1, 2, 33, 20), dtype, "v nan", layout)
+    out, state = d.want()
+    got = d.forward(True)
+    fine = np.isfinite(out)
+    assert np.array_equal(np.isfinite(got[0].double().cpu().numpy()), fine)
+    close(got[0][torch_mask(got[0], fine)], out[fine], "out")
+    close(got[1], state, "state")
+    good = np.ones(70, bool)
+    good[list(bad)] = False
+    for name, x, y in zip(GRADS[:5], d.backward(got[2]), d.want_grads()):
+        close(x[:, torch_mask(x, good)], y[:, good], name)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.filterwarnings("ignore:invalid value:RuntimeWarning")
+def test_gradients_that_are_not_finite_stay_in_their_episode(env, dtype):
+    """A row gradient, and the gradient of a last state, that are not finite: earlier tokens of the episode get none that
+    is finite, other episodes theirs; states are updated in place."""
+    torch, S, ctx = env
+    for size in ((2, 70, 1, 2, 32, 40), (64, 66, 2, 4, 72, 64), (1, 577, 1, 1, 128, 20)):
+        t = size[1]
+        d = Delta(env, *size, dtype=dtype, resets=[(0, 5), (0, 20), (0, t - 10)], lengths=[t] * size[0], seed=4)
+        clean = d.want_grads()
+        d.do[0, 11, 0, 3] = float("nan")
+        d.ds[0, 0, 1, 1] = float("inf")
+        grads = d.backward(d.forward(True)[2])
+        for b in range(1, size[0]):
+            for name, x, y in zip(GRADS, grads, clean):
+                close(x[b], y[b], name)
+        good = np.ones(t, bool)
+        good[5:20] = good[t - 10:] = False
+        for name, x, y in zip(GRADS[:5], grads, clean):
+            close(x[0][torch_mask(x, good)], y[0][good], name)
+        close(grads[5][0], clean[5][0], "dstate")
+        dv = grads[2][0, :, 0].float().cpu().numpy()
+        assert not np.isfinite(dv[5:12, 3]).any() and not np.isfinite(dv[t - 10:, 1]).any()
+        close(grads[2][0, 5:20, 0, :3], clean[2][0, 5:20, 0, :3], "columns beside it")
+        s, out = d.state.clone(), d.out()[0]
+        given = S.DeltaInput(d.q, d.k, d.v, d.g, d.beta, None, s)
+        s[0, 0] = float("nan")
+        want = O_forward(d, s)
+        ctx.pql_delta_forward(d.shape, given, S.Sequence(out), s, None, S.workspace(ctx.delta_workspace_bytes(d.shape, False)))
+        close(s, want[1], "state in place")
+        close(out[:, 5:], want[0][:, 5:], "out")
+
+
+def O_forward(d, state):
+    from oracle import student_oracle as O
+    return O.delta_forward(*d.host, d.scale, None, state.double().cpu().numpy())
