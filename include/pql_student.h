@@ -132,7 +132,9 @@ int32_t pql_distill_loss(pql_ctx* ctx, pql_logits logits, pql_teacher teacher, f
 
 /* The gradient alone, for a loss sum_n loss_grad[n] L_n with L_n the loss above at w_n = 1, from the lse_out of
  * that call: grad_nj = loss_grad[n] t (q_j - ...).  Rows with loss_grad[n] = 0 or without a valid entry are not
- * read and get zeros.  grad may be the logits themselves. */
+ * read and get zeros; rows of weight 0 in that call have no log-sum-exp, and must have loss_grad[n] = 0 here.  The
+ * rounding of lse_out costs q 2e-7 |lse|; rows with |lse| > 32 are therefore read once more for the maximum and sum
+ * of their own.  grad may be the logits themselves. */
 int32_t pql_distill_backward(pql_ctx* ctx, pql_logits logits, pql_teacher teacher, float temperature, const float* lse,
                              const float* loss_grad, pql_logits grad, void* stream);
 

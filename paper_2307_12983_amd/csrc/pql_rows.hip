@@ -12,8 +12,12 @@ namespace pql {
 namespace {
 
 constexpr int SMALL_VOCAB = 1024;
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LOG2E = 1.4426950408889634f;
 constexpr float NEG_INF = -__builtin_inff();
+
+// The gradient by itself takes q = exp(z / t - lse) from the one number a row's caller keeps, which is rounded three times on its way: up to
+// 2e-7 |lse| of every q.  Beyond this bound (6e-6) rows work out their maximum and sum again, as the loss does.
+constexpr float FAR = 32.f;
 
 // 2^x by the one instruction: results below 2^-126 become 0, which no sum or gradient here can tell from their value.
 __device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -272,28 +276,27 @@ __global__ __launch_bounds__(256) void distill_small_kernel(DistillArgs a) {
     }
     __syncthreads();
     const float c = LOG2E * a.inv_temp;
-    float m = 0.f, inv = 0.f;
-    if (BACK) {
-        m = read ? a.lse[n] : 0.f;                          // q = exp(z / t - lse)
-    } else {
+    float m = BACK && read ? a.lse[n] : 0.f, t_m = a.temp, inv = 1.f;      // q = exp((z - m t_m) / t) inv
+    const bool stats = !BACK || __any(fabsf(m) > FAR);      // -inf among them
+    if (stats) {
         m = z[0];
 #pragma unroll
         for (int r = 1; r < R; ++r) m = fmaxf(m, z[r]);
         m = group_max<G>(m);
         if (m == NEG_INF) m = 0.f;
+        t_m = 1.f;
     }
     float s = 0.f, q[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        q[r] = BACK ? exp2_raw(fmaf(-m, a.temp, z[r]) * c) : exp2_raw((z[r] - m) * c);
+        q[r] = exp2_raw(fmaf(-m, t_m, z[r]) * c);
         s += q[r];
     }
-    if (BACK) {
-        inv = 1.f;
-        if (m == NEG_INF) inv = 0.f;
-    } else {
+    if (stats) {
         s = group_sum<G>(s);
         inv = s > 0.f || s != s ? 1.f / s : 0.f;
+    }
+    if (!BACK) {
         const float log_s = logf(s);
         float loss = plogp;
 #pragma unroll
@@ -390,12 +393,10 @@ __global__ __launch_bounds__(256) void distill_wave_kernel(DistillArgs a) {
         sum_of_answer(s_index, s_p, a.top, l + 64 * q, index[q], first, sum[q]);
         owner[q] = owner[q] && first;
     }
-    const float c = LOG2E * a.inv_temp, t_m = BACK ? a.temp : 1.f;
-    float m, inv;
-    if (BACK) {
-        m = lse == NEG_INF ? 0.f : lse;
-        inv = lse == NEG_INF ? 0.f : 1.f;
-    } else {
+    const float c = LOG2E * a.inv_temp;
+    float m = lse, inv = 1.f, t_m = a.temp;
+    if (!BACK || fabsf(lse) > FAR) {
+        t_m = 1.f;
         m = NEG_INF;
         h.each([&](float x, int) { m = fmaxf(m, x); });
         m = group_max<64>(m);
@@ -404,20 +405,22 @@ __global__ __launch_bounds__(256) void distill_wave_kernel(DistillArgs a) {
         h.each([&](float x, int j) { part[j & 3] += exp2_raw((x - m) * c); });
         const float s = group_sum<64>((part[0] + part[1]) + (part[2] + part[3])), log_s = logf(s);
         inv = s > 0.f || s != s ? 1.f / s : 0.f;
-        float loss = 0.f;
+        if (!BACK) {
+            float loss = 0.f;
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            Entry e;
-            e.p = y[q];
-            e.log_p = lp[q];
-            if (index[q] >= 0) loss += entry_loss(e, zk[q], m, a.inv_temp, log_s);
+            for (int q = 0; q < Q; ++q) {
+                Entry e;
+                e.p = y[q];
+                e.log_p = lp[q];
+                if (index[q] >= 0) loss += entry_loss(e, zk[q], m, a.inv_temp, log_s);
+            }
+            loss = group_sum<64>(loss);
+            if (l == 0) {
+                a.loss_out[n] = w * a.temp * a.temp * loss;
+                a.lse_out[n] = m * a.inv_temp + log_s;
+            }
+            if (!a.grad) return;
         }
-        loss = group_sum<64>(loss);
-        if (l == 0) {
-            a.loss_out[n] = w * a.temp * a.temp * loss;
-            a.lse_out[n] = m * a.inv_temp + log_s;
-        }
-        if (!a.grad) return;
     }
 #pragma unroll
     for (int q = 0; q < Q; ++q) asm volatile("" ::"v"(zk[q]));       // they are there before the gradient may be written over them
@@ -604,7 +607,8 @@ __global__ __launch_bounds__(NT) void distill_part_kernel(DistillArgs a) {
         o[1] = s;
     }
 }
-// Second launch (JOIN), or the whole backward call: the gradient of one piece.
+// Second launch (JOIN), or the whole backward call: the gradient of one piece.  A piece of a FAR row reads the whole row first; where
+// the gradient takes the logits' place and rows have several pieces, those rows go in a launch of their own, a workgroup each (a.part_rows).
 template <typename E, int NT, bool JOIN>
 __global__ __launch_bounds__(NT) void distill_piece_kernel(DistillArgs a) {
     __shared__ __align__(16) int s_index[PQL_MAX_TOP];
@@ -614,15 +618,14 @@ __global__ __launch_bounds__(NT) void distill_piece_kernel(DistillArgs a) {
     Entry e;
     const float w = entry_of(a, n, e);
     E* out = (E*)a.grad + n * a.grad_stride + j0;
-    if (!__syncthreads_or(e.index >= 0) || w == 0.f) {
+    if (!__syncthreads_or(e.index >= 0) || w == 0.f) {          // in both launches of a call in parts
         if (JOIN && blockIdx.x == 0 && threadIdx.x == 0) { a.loss_out[n] = 0.f; a.lse_out[n] = 0.f; }
         if (a.grad) zero_stretch<E, NT>(out, len);
         return;
     }
     const E* row = (const E*)a.z + n * a.stride + j0;
     const float c = LOG2E * a.inv_temp, f = w * a.temp;
-    float m, inv, zk = 0.f;
-    const float t_m = JOIN ? 1.f : a.temp;
+    float m, inv, zk = 0.f, t_m = 1.f;
     const bool mine = e.index >= j0 && e.index < j0 + len;
     if (JOIN) {
         float pm = NEG_INF, ps = 0.f;
@@ -646,9 +649,18 @@ __global__ __launch_bounds__(NT) void distill_piece_kernel(DistillArgs a) {
         }
         if (!a.grad) return;
     } else {
-        const float lse = a.lse[n];
-        m = lse == NEG_INF ? 0.f : lse;                     // exp(z / t - lse) = exp2((z - t lse) c)
-        inv = lse == NEG_INF ? 0.f : 1.f;
+        m = a.lse[n];                                       // exp(z / t - lse) = exp2((z - t lse) c)
+        t_m = a.temp;
+        inv = 1.f;
+        const bool far = fabsf(m) > FAR;
+        if (a.part_rows != ROWS_ALL && far != (a.part_rows == ROWS_FAR)) return;
+        if (far) {
+            float s;
+            stretch_stats<E, NT>(Stretch<E>(row - j0, a.vocab), c, m, s);
+            join_stats<NT>(c, m, s, s_red);
+            inv = s > 0.f || s != s ? 1.f / s : 0.f;
+            t_m = 1.f;
+        }
         if (mine) zk = to_float(row[e.index - j0]);
         __syncthreads();                                    // read before the gradient may be written over the logits
         stretch_grad<E, NT>(Stretch<E>(row, len), out, c, m, t_m, inv, f);
@@ -1163,11 +1175,21 @@ template <typename E> hipError_t distill_launch(const DistillArgs& a, bool back,
 #undef PQL_WAVE
         prof_commit(ps, back ? KID_DISTILL_GRAD : KID_DISTILL, 0.0, bytes);
     } else if (back) {
+        // in the logits' place, rows that read all of themselves for every piece would find some of it written over
+        const bool apart = a.grad == a.z && a.pieces > 1;
         for (int64_t n = 0; n < a.rows; n += ROWS_PER_LAUNCH) {
-            const DistillArgs b = from_row<E>(a, n, a.rows - n < ROWS_PER_LAUNCH ? a.rows - n : ROWS_PER_LAUNCH);
-            const ProfSlot ps = prof_slot();
+            DistillArgs b = from_row<E>(a, n, a.rows - n < ROWS_PER_LAUNCH ? a.rows - n : ROWS_PER_LAUNCH);
+            b.part_rows = apart ? ROWS_NEAR : ROWS_ALL;
+            ProfSlot ps = prof_slot();
             PQL_LAUNCH(ps, (distill_piece_kernel<E, NT_LONG, false>), dim3(a.pieces, (unsigned)b.rows), dim3(NT_LONG), 0, st, b);
             prof_commit(ps, KID_DISTILL_GRAD, 0.0, bytes * b.rows / a.rows);
+            if (!apart) continue;
+            b.part_rows = ROWS_FAR;
+            b.pieces = 1;
+            b.piece = a.vocab;
+            ps = prof_slot();
+            PQL_LAUNCH(ps, (distill_piece_kernel<E, NT_LONG, false>), dim3(1, (unsigned)b.rows), dim3(NT_LONG), 0, st, b);
+            prof_commit(ps, KID_DISTILL_GRAD, 0.0, 0.0);
         }
     } else if (a.pieces > 1) {
         ProfSlot ps = prof_slot();

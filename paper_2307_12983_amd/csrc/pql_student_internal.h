@@ -11,6 +11,9 @@ __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(bf16_t x) { return (float)x; }
 template <typename E> __device__ __forceinline__ E from_float(float x) { return (E)x; }      // bf16: to nearest even
 
+// Which rows a launch of the gradient by itself takes: all, or by whether their log-sum-exp is too large to take q from it.
+enum PartRows : int { ROWS_ALL = 0, ROWS_NEAR = 1, ROWS_FAR = 2 };
+
 struct DistillArgs {
     const void* z;
     int64_t rows, stride, grad_stride;
@@ -23,6 +26,7 @@ struct DistillArgs {
     void* grad;
     float* part;                        // [rows][pieces][2]: maximum (-inf: nothing finite) and sum of each piece
     float* part_z;                      // [rows][top]: logits of the listed answers
+    int part_rows;                      // PartRows
 };
 
 struct TopArgs {

@@ -11,8 +11,9 @@ LOWEST = float(np.finfo(np.float32).min)
 
 
 def held(x):
-    """What 32 bits hold of a value: nothing below half their smallest number."""
-    return np.where(np.abs(x) < 2.0 ** -150, 0.0, x)
+    """What 32 bits hold of a value: nothing below half their smallest number, infinity from 2^128 on."""
+    x = np.where(np.abs(x) < 2.0 ** -150, 0.0, x)
+    return np.where(np.abs(x) >= 2.0 ** 128, np.copysign(np.inf, x), x)
 
 
 def set_gate(d, places, value):
@@ -152,3 +153,41 @@ def test_gradients_that_are_not_finite_stay_in_their_episode(env, dtype):
 def O_forward(d, state):
     from oracle import student_oracle as O
     return O.delta_forward(*d.host, d.scale, None, state.double().cpu().numpy())
+
+
+# ---- gradient of the distillation by itself ----------------------------------------------------
+@pytest.mark.parametrize("rows,vocab", [(5, 50), (40, 900), (5, 2500), (2051, 1500), (3, 70001), (300, 20011)])
+@pytest.mark.parametrize("dtype,temp", [("float32", 1.0), ("float32", 0.3), ("bfloat16", 1.5)])
+@pytest.mark.parametrize("offset", [40.0, -1000.0, 3e4, LOWEST])
+def test_gradient_alone_of_logits_far_from_zero(env, rows, vocab, dtype, temp, offset):
+    """Log-sum-exps that 32 bits hold to some 1e-3 or to nothing at all; rows near zero beside them."""
+    torch, S, ctx = env
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    z = 2 * torch.randn((rows, vocab), generator=g, device="cuda")
+    low = torch.finfo(getattr(torch, dtype)).min
+    z[:-2] = low if offset == LOWEST else z[:-2] + offset
+    z = z.to(getattr(torch, dtype))
+    z[-1, 9:] = float("-inf")
+    pick = sorted({0, 1, 2, rows // 2, rows - 2, rows - 1})
+    host = lambda x: x[pick].double().cpu().numpy()  # noqa: E731
+    top = 6
+    index = torch.randint(0, vocab, (rows, top), generator=g, device="cuda", dtype=torch.int32)
+    index[-1] = torch.arange(top, device="cuda", dtype=torch.int32)
+    value = torch.randn((rows, top), generator=g, device="cuda")
+    weight = torch.rand((rows,), generator=g, device="cuda") + 0.5
+    d, t = S.Logits(z), S.Teacher(index, value)
+    loss, lse = (torch.empty((rows,), device="cuda") for _ in range(2))
+    ctx.pql_distill_loss(d, t, temp, None, loss, lse, None, S.workspace(ctx.distill_workspace_bytes(d)))
+    _, want_lse, want = O_distill(host(z), index[pick].cpu().numpy(), host(value), temp, host(weight))
+    close(lse[pick], held(want_lse), "lse")
+    grad = torch.full_like(z, 7.0)
+    ctx.pql_distill_backward(d, t, temp, lse, weight, S.Logits(grad))
+    close(grad[pick], want, "gradient by itself")
+    ctx.pql_distill_backward(d, t, temp, lse, weight, d)
+    close(z[pick], want, "gradient in place")
+    assert torch.equal(z, grad)
+
+
+def O_distill(*a):
+    from oracle import student_oracle as O
+    return O.distill(*a)
