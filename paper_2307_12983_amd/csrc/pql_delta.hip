@@ -87,10 +87,6 @@ struct Acc {
     }
     __device__ __forceinline__ floatx4 sum() const { return a[2] + a[1] + a[0]; }
 };
-// Products for results that are rounded to bf16: the first two terms (16 bits) of what has been computed.
-__device__ __forceinline__ void mma_out(floatx4& c, const F1& a, const F3& b) { c = mm(a.h, b.m, c); c = mm(a.h, b.h, c); }
-__device__ __forceinline__ void mma_out(floatx4& c, const F3& a, const F3& b) { c = mm(a.m, b.h, c); c = mm(a.h, b.m, c); c = mm(a.h, b.h, c); }
-__device__ __forceinline__ void mma_out(floatx4& c, const FF& a, const FF& b) { mma(c, a, b); }
 
 // Results of matrix instructions must not be read for some cycles.  The compiler sees to that, but not on every path where
 // branches lie between (a short side of a branch is missed when a long one has been looked at first; a result was read too
@@ -1124,7 +1120,7 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
             store_state<RS, NT>(a.state_out, w, wave, l >> 4, c0 + (l & 15), dk, dv, S);
             return;
         }
-    } else {                                        // the outputs: rounded to the tokens' type, two terms of S, P, Y are enough
+    } else {                                        // the outputs
         typename RowsOf<M, C, DK, NT, AL>::T Q(a.q, a.QO, first_k, w, dk, row, q, 0, 1);
         ColumnValues<M, C, NT, AL> O(a.out, w, dv, i0, c0 + c, 0, 1);
         Chunks pP(a.P, first, tri_bytes, 0, 1);
@@ -1144,7 +1140,7 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
 #pragma unroll
                 for (int d = 0; d < ND; ++d)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma_out(o[n], Q.f[d], f[d][n]);
+                    for (int n = 0; n < NT; ++n) mma(o[n], Q.f[d], f[d][n]);
             }
             pG.go(more);
             Gn.load<C>(pG, i0);
@@ -1163,7 +1159,7 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma_out(o[n], P[k], f[k][n]);
+                    for (int n = 0; n < NT; ++n) mma(o[n], P[k], f[k][n]);
                 }
             }
             pP.go(more);

@@ -191,3 +191,30 @@ def test_gradient_alone_of_logits_far_from_zero(env, rows, vocab, dtype, temp, o
 def O_distill(*a):
     from oracle import student_oracle as O
     return O.distill(*a)
+
+
+# ---- one rounding to 16 bits -------------------------------------------------------------------
+@pytest.mark.parametrize("t", [1, 40, 600])
+def test_outputs_in_16_bits_are_rounded_once(env, t):
+    """Outputs a little above the middle of two bfloat16 values, by what lies in the last bits of a state (1 + 2^-9 + 2^-20 and
+    2^-9, sum 1 + 2^-8 + 2^-20) and of a product ((1 + 2^-9)^2 = 1 + 2^-8 + 2^-18): both are exact in 32 bits and round up to
+    1 + 2^-7; to 1 if any of those bits is lost before."""
+    torch, S, ctx = env
+    for what in ("state", "product"):
+        q, k, v = (torch.zeros((1, t, 1, n), dtype=torch.bfloat16, device="cuda") for n in (2, 2, 1))
+        g, beta = torch.zeros((1, t, 1), device="cuda"), torch.zeros((1, t, 1), device="cuda")
+        state = torch.zeros((1, 1, 2, 1), device="cuda")
+        q[0, 0, 0] = 1.0
+        if what == "state":
+            state[0, 0, 0, 0], state[0, 0, 1, 0] = 1 + 2.0 ** -9 + 2.0 ** -20, 2.0 ** -9
+        else:
+            k[0, 0, 0, 0], k[0, 0, 0, 1] = 1.0, 2.0 ** -9
+            v[0, 0], beta[0, 0] = 1.0, 1 + 2.0 ** -9
+        shape, given = S.delta_shape(q, v, 1.0), S.DeltaInput(q, k, v, g, beta, None, state)
+        for call in ("step", "forward"):
+            out, last = torch.full_like(v, 7.0), torch.empty_like(state)
+            if call == "step":
+                ctx.pql_delta_step(shape, given, last, S.Sequence(out))
+            else:
+                ctx.pql_delta_forward(shape, given, S.Sequence(out), last, None, S.workspace(ctx.delta_workspace_bytes(shape, False)))
+            assert float(out[0, 0, 0, 0]) == 1 + 2.0 ** -7, (what, call)
