@@ -1142,6 +1142,7 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
 #pragma unroll
                     for (int n = 0; n < NT; ++n) mma(o[n], Q.f[d], f[d][n]);
             }
+            if constexpr (!AL) settle();            // loads of rows that are not aligned have branches
             pG.go(more);
             Gn.load<C>(pG, i0);
             Q.go(more);
