@@ -2,7 +2,8 @@
 
 Like ``binding``: argument marshalling only, every method of ``StudentContext`` forwards device pointers and
 sizes to the C entry point of the same name.  Tensors are described once by the small classes below (they
-hold the tensor and its C descriptor, so that a call made every step costs no repeated marshalling).
+hold the tensor, its C descriptor and what a call compares), so that a call made every step repeats little; it
+still checks that what it is given belongs together, since the kernels would read and write out of range.
 """
 from __future__ import annotations
 
@@ -76,12 +77,23 @@ def load_library() -> C.CDLL:
     return lib
 
 
+_INT32 = -1                                     # of lists; no type of tokens or logits
+_codes = {}
+
+
+def _code(t):
+    """PQL_F32, PQL_BF16, _INT32, or None for any other type."""
+    if not _codes:
+        import torch
+        _codes.update({torch.float32: PQL_F32, torch.bfloat16: PQL_BF16, torch.int32: _INT32})
+    return _codes.get(t.dtype)
+
+
 def dtype_code(t) -> int:
-    import torch
-    codes = {torch.float32: PQL_F32, torch.bfloat16: PQL_BF16}
-    if t.dtype not in codes:
+    code = _code(t)
+    if code is None or code == _INT32:
         raise TypeError("tokens and logits are float32 or bfloat16, not %s" % t.dtype)
-    return codes[t.dtype]
+    return code
 
 
 def workspace(nbytes: int, device="cuda"):
@@ -96,12 +108,12 @@ def workspace(nbytes: int, device="cuda"):
     return t
 
 
-def _f32(t, what: str, like=None):
-    import torch
+def _dense(t, what: str, like, code=PQL_F32):
+    """The pointer of a contiguous float32 (or int32) tensor of that shape; None stays None."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or not t.is_contiguous() or (like is not None and tuple(t.shape) != tuple(like)):
-        raise ValueError("%s: expected a contiguous float32 tensor%s" % (what, "" if like is None else " of shape %s" % (tuple(like),)))
+    if t.shape != like or _code(t) != code or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous %s tensor of shape %s" % (what, "int32" if code == _INT32 else "float32", like))
     return t.data_ptr()
 
 
@@ -115,6 +127,7 @@ class Sequence:
         if t.dim() == 4 and t.shape[3] > 1 and t.stride(3) != 1 and t.numel() > 0:
             raise ValueError("the last dimension of a token tensor must be contiguous")
         self.tensor = t
+        self.key = (*t.shape, _code(t))
         self.c = PqlSeq(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
 
 
@@ -139,10 +152,12 @@ class _Described:
               (beta, (n, t, hv), torch.float32))
         self.tensors = (q, k, v, log_decay, beta, state)
         self.shape = tuple(q.shape) + (hv, dv)
+        self.key = (*self.shape, dtype_code(q))
+        self.out_key, self.state_shape = (n, t, hv, dv, self.key[-1]), (n, hv, q.shape[3], dv)
         self.c = struct()
         for name, x in zip(("q", "k", "v", "log_decay", "beta"), self.tensors):
             setattr(self.c, name, Sequence(x).c)
-        self.c.state = _f32(state, what + ": state", (n, hv, q.shape[3], dv))
+        self.c.state = _dense(state, what + ": state", self.state_shape)
         self.ref = C.byref(self.c)
 
 
@@ -215,38 +230,53 @@ class StudentContext(B.Context):
 
     # ---- device calls
     @staticmethod
-    def _fits(shape, given, out):
-        want = (shape.batch, shape.steps, shape.heads_k, shape.dim_k, shape.heads_v, shape.dim_v)
-        if given.shape != want or tuple(out.tensor.shape) != (shape.batch, shape.steps, shape.heads_v, shape.dim_v) or \
-                dtype_code(out.tensor) != shape.dtype or dtype_code(given.tensors[0]) != shape.dtype:
+    def _fits(s, given, out):
+        if given.key != (s.batch, s.steps, s.heads_k, s.dim_k, s.heads_v, s.dim_v, s.dtype) or out.key != given.out_key:
             raise ValueError("tensors and shape of the call do not agree")
+
+    @staticmethod
+    def _state(given, t, what):
+        return given.c.state if t is given.tensors[5] else _dense(t, what, given.state_shape)
 
     def pql_delta_step(self, shape, given: DeltaInput, state_out, out: Sequence, stream=None):
         self._fits(shape, given, out)
-        self._check(self.lib.pql_delta_step(self.h, C.byref(shape), given.ref, B._ptr(state_out), out.c, B._stream(stream)))
+        state_out = self._state(given, state_out, "state_out")
+        self._check(self.lib.pql_delta_step(self.h, C.byref(shape), given.ref, state_out, out.c, B._stream(stream)))
 
     def pql_delta_forward(self, shape, given: DeltaInput, out: Sequence, state_out, saved, workspace, stream=None):
         self._fits(shape, given, out)
-        self._check(self.lib.pql_delta_forward(self.h, C.byref(shape), given.ref, out.c, B._ptr(state_out), B._ptr(saved),
+        state_out = self._state(given, state_out, "state_out")
+        self._check(self.lib.pql_delta_forward(self.h, C.byref(shape), given.ref, out.c, state_out, B._ptr(saved),
                                                B._ptr(workspace), B._stream(stream)))
 
     def pql_delta_backward(self, shape, given: DeltaInput, saved, out_grad: Sequence, state_out_grad, grads: DeltaGrad,
                            workspace, stream=None):
         self._fits(shape, given, out_grad)
         self._fits(shape, grads, out_grad)
+        state_out_grad = self._state(given, state_out_grad, "state_out_grad")
         self._check(self.lib.pql_delta_backward(self.h, C.byref(shape), given.ref, B._ptr(saved), out_grad.c,
-                                                B._ptr(state_out_grad), grads.ref, B._ptr(workspace), B._stream(stream)))
+                                                state_out_grad, grads.ref, B._ptr(workspace), B._stream(stream)))
 
     def pql_top_logits(self, logits: Logits, top, index_out, value_out, workspace, stream=None):
-        self._check(self.lib.pql_top_logits(self.h, logits.c, top, B._ptr(index_out), B._ptr(value_out), B._ptr(workspace),
-                                            B._stream(stream)))
+        like = (logits.c.rows, top)
+        index_out, value_out = _dense(index_out, "index_out", like, _INT32), _dense(value_out, "value_out", like)
+        self._check(self.lib.pql_top_logits(self.h, logits.c, top, index_out, value_out, B._ptr(workspace), B._stream(stream)))
+
+    @staticmethod
+    def _per_row(logits, teacher, *named):
+        rows = logits.c.rows
+        if teacher.index.shape[0] != rows:
+            raise ValueError("the teacher's lists are of %d rows, the logits of %d" % (teacher.index.shape[0], rows))
+        return [_dense(t, what, (rows,)) for what, t in named]
 
     def pql_distill_loss(self, logits: Logits, teacher: Teacher, temperature, row_weight, loss_out, lse_out, grad,
                          workspace, stream=None):
-        self._check(self.lib.pql_distill_loss(self.h, logits.c, teacher.c, temperature, B._ptr(row_weight), B._ptr(loss_out),
-                                              B._ptr(lse_out), NO_GRAD if grad is None else grad.c, B._ptr(workspace),
-                                              B._stream(stream)))
+        row_weight, loss_out, lse_out = self._per_row(logits, teacher, ("row_weight", row_weight), ("loss_out", loss_out),
+                                                      ("lse_out", lse_out))
+        self._check(self.lib.pql_distill_loss(self.h, logits.c, teacher.c, temperature, row_weight, loss_out, lse_out,
+                                              NO_GRAD if grad is None else grad.c, B._ptr(workspace), B._stream(stream)))
 
     def pql_distill_backward(self, logits: Logits, teacher: Teacher, temperature, lse, loss_grad, grad: Logits, stream=None):
-        self._check(self.lib.pql_distill_backward(self.h, logits.c, teacher.c, temperature, B._ptr(lse), B._ptr(loss_grad),
-                                                  grad.c, B._stream(stream)))
+        lse, loss_grad = self._per_row(logits, teacher, ("lse", lse), ("loss_grad", loss_grad))
+        self._check(self.lib.pql_distill_backward(self.h, logits.c, teacher.c, temperature, lse, loss_grad, grad.c,
+                                                  B._stream(stream)))

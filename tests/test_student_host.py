@@ -252,3 +252,38 @@ def test_reference_gradient_of_the_distillation_agrees_with_differences():
     assert loss[3] == 0 and not grad[3].any()
     want = _differences(lambda: float(np.sum(O.distill(z, index, value, 1.7, weight)[0])), z)
     assert np.max(np.abs(grad - want)) < 1e-7
+
+
+def test_calls_refuse_tensors_that_do_not_belong_together():
+    """Before anything is launched: the kernels take sizes from the logits or the shape alone."""
+    import torch
+    ctx = S.StudentContext()
+    z = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt)  # noqa: E731
+    rows, vocab, top = 6, 40, 4
+    logits, lists = S.Logits(z(rows, vocab)), lambda n: S.Teacher(z(n, top, dt=torch.int32), z(n, top))  # noqa: E731
+    for i, v in ((z(rows - 1, top, dt=torch.int32), z(rows, top)), (z(rows, top, dt=torch.int64), z(rows, top)), (z(rows, top), z(rows, top)),
+                 (z(rows, top, dt=torch.int32), z(rows, top + 1)), (z(rows, top, dt=torch.int32), z(rows, top, dt=torch.bfloat16)),
+                 (z(rows, top, dt=torch.int32), z(top, rows).t())):
+        with pytest.raises(ValueError):
+            ctx.pql_top_logits(logits, top, i, v, None)
+    good = dict(teacher=lists(rows), row_weight=None, loss=z(rows), lse=z(rows))
+    for bad in (dict(teacher=lists(rows - 1)), dict(row_weight=z(rows - 1)), dict(loss=z(1)), dict(lse=z(rows, dt=torch.float64)), dict(loss=z(2 * rows)[::2])):
+        a = {**good, **bad}
+        with pytest.raises(ValueError):
+            ctx.pql_distill_loss(logits, a["teacher"], 1.0, a["row_weight"], a["loss"], a["lse"], None, None)
+        if "row_weight" not in bad:
+            with pytest.raises(ValueError):
+                ctx.pql_distill_backward(logits, a["teacher"], 1.0, a["lse"], a["loss"], logits)
+    q, v, g = z(2, 8, 2, 16), z(2, 8, 4, 24), z(2, 8, 4)
+    shape, given, out = S.delta_shape(q, v, 0.25), S.DeltaInput(q, q, v, g, g), S.Sequence(z(2, 8, 4, 24))
+    grads = S.DeltaGrad(z(2, 8, 2, 16), z(2, 8, 2, 16), z(2, 8, 4, 24), z(2, 8, 4), z(2, 8, 4))
+    for state in (z(2, 4, 24, 16), z(1, 4, 16, 24), z(2, 4, 16, 24, dt=torch.bfloat16), z(2, 4, 24, 16).transpose(2, 3)):
+        with pytest.raises(ValueError):
+            ctx.pql_delta_step(shape, given, state, out)
+        with pytest.raises(ValueError):
+            ctx.pql_delta_forward(shape, given, out, state, None, None)
+        with pytest.raises(ValueError):
+            ctx.pql_delta_backward(shape, given, None, out, state, grads, None)
+    for wrong in (z(2, 8, 4, 23), z(2, 8, 4, 24, dt=torch.bfloat16), z(2, 7, 4, 24)):
+        with pytest.raises(ValueError):
+            ctx.pql_delta_step(shape, given, None, S.Sequence(wrong))
