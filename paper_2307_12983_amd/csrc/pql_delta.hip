@@ -808,8 +808,8 @@ template <typename M, int C, int DK, int NT> struct ScanLds {
     static constexpr int S0 = 0, X0 = S0 + S::BYTES, Y0 = X0 + X::BYTES, Z0 = Y0 + X::BYTES, BYTES = Z0 + X::BYTES;
 };
 // By one wavefront.
-template <typename E> __device__ __forceinline__ void zero_rows(const DeltaSeq& s, const Where& w, int from, int to, int c0, int n) {
-    for (int i = threadIdx.x & 63; i < (to - from) * n; i += 64) at_out<E>(s, w.b, from + i / n, w.h)[c0 + i % n] = from_float<E>(0.f);
+template <typename E, int COLS> __device__ __forceinline__ void zero_rows(const DeltaSeq& s, const Where& w, int from, int to, int c0, int n) {
+    each_of_rows<COLS>(threadIdx.x & 63, from, to, n, [&](int64_t t, int c) { at_out<E>(s, w.b, t, w.h)[c0 + c] = from_float<E>(0.f); });
 }
 // The C / 32 blocks of a wavefront's rows of T, P or their transposes.  Blocks that are zero are not there: they are asked for
 // outside the descriptor and come as zeros, so that no branch stands among a chunk's loads and products.
@@ -1171,7 +1171,7 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
             O.go(true);
         }
         const int n = min(16 * NT, dv - c0);
-        if (n > 0 && a.steps > chunks * C && all == NW) zero_rows<E>(a.out, w, chunks * C, a.steps, c0, n);
+        if (n > 0 && a.steps > chunks * C && all == NW) zero_rows<E, 16 * NT>(a.out, w, chunks * C, a.steps, c0, n);
         if (chunks == 0) return;
         if (odd != 0.f) s_odd = 1;
         __syncthreads();
@@ -1409,7 +1409,7 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
             hand_over();
         }
         const int n = min(16 * NT, dv - c0);
-        if (n > 0 && a.steps > chunks * C && all == NW) zero_rows<E>(a.dv, w, chunks * C, a.steps, c0, n);
+        if (n > 0 && a.steps > chunks * C && all == NW) zero_rows<E, 16 * NT>(a.dv, w, chunks * C, a.steps, c0, n);
         if (chunks == 0) return;
         __syncthreads();
         if (!s_odd) return;

@@ -37,6 +37,13 @@ struct TopArgs {
     int* part_index; float* part_value; // [rows][pieces][top]
 };
 
+// f(row, column) for rows from .. to - 1 and the first n of COLS columns, by the 64 lanes of one wavefront.  Rows are counted as
+// they are: rows times columns may pass 32 bits.
+template <int COLS, typename F> __host__ __device__ inline void each_of_rows(int lane, int64_t from, int64_t to, int n, F&& f) {
+    if (lane % COLS >= n) return;
+    for (int64_t row = from + lane / COLS; row < to; row += 64 / COLS) f(row, lane % COLS);
+}
+
 struct DeltaSeq { void* p; int64_t b, t, h; };
 struct DeltaArgs {
     int batch, steps, heads_k, heads_v, group, dim_k, dim_v;

@@ -287,3 +287,28 @@ def test_calls_refuse_tensors_that_do_not_belong_together():
     for wrong in (z(2, 8, 4, 23), z(2, 8, 4, 24, dt=torch.bfloat16), z(2, 7, 4, 24)):
         with pytest.raises(ValueError):
             ctx.pql_delta_step(shape, given, None, S.Sequence(wrong))
+
+
+def test_rows_are_walked_beyond_32_bits_of_elements(tmp_path):
+    """The walk over rows behind a sequence's length, on the host: 2^27 rows of 16 columns are 2^31 elements."""
+    from paper_2307_12983_amd import build
+    src, exe = tmp_path / "rows.hip", tmp_path / "rows"
+    src.write_text("""
+#include <cstdio>
+#include "pql_student_internal.h"
+template <int COLS> void walk(int64_t from, int64_t to, int n) {
+    int64_t seen = 0, first = to, last = -1, bad = 0;
+    for (int lane = 0; lane < 64; lane += lane == 0 ? 1 : 62)        // lanes 0, 1 and 63
+        pql::each_of_rows<COLS>(lane, from, to, n, [&](int64_t row, int c) {
+            ++seen; first = row < first ? row : first; last = row > last ? row : last; bad += c != lane % COLS || c >= n;
+        });
+    printf("%lld %lld %lld %lld\\n", (long long)seen, (long long)first, (long long)last, (long long)bad);
+}
+int main() { walk<16>(3, 3 + (1ll << 27), 16); walk<32>(0, 7, 20); walk<32>(5, 5, 32); return 0; }
+""")
+    r = subprocess.run([build._hipcc(), "-O1", "-std=c++17", "--offload-arch=gfx950", "--offload-host-only", "-I" + build.CSRC,
+                        "-I" + os.path.join(ROOT, "include"), str(src), "-o", str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    got = [[int(x) for x in l.split()] for l in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.splitlines()]
+    quarter = 2 ** 25
+    assert got == [[3 * quarter, 3, 2 + 2 ** 27, 0], [4 + 4, 0, 6, 0], [0, 5, -1, 0]]
