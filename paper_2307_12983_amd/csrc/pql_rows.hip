@@ -1146,8 +1146,8 @@ template <typename E> hipError_t top_small_launch(const TopArgs& a, double bytes
     return hipErrorInvalidValue;
 }
 
-// grid.y holds at most 65535 rows: longer calls go in parts
-constexpr int64_t ROWS_PER_LAUNCH = 65535;
+// grid.y holds at most 65535 rows, and a grid at most 2^32 - 1 threads, which rows of up to 512 threads each reach: longer calls go in parts
+constexpr int64_t ROWS_PER_LAUNCH = 65535, ROWS_PER_PART = 1 << 22;
 template <typename E> DistillArgs from_row(DistillArgs a, int64_t n, int64_t rows) {
     a.z = (const E*)a.z + n * a.stride;
     if (a.grad) a.grad = (E*)a.grad + n * a.grad_stride;
@@ -1159,7 +1159,7 @@ template <typename E> DistillArgs from_row(DistillArgs a, int64_t n, int64_t row
     a.rows = rows;
     return a;
 }
-template <typename E> hipError_t distill_launch(const DistillArgs& a, bool back, hipStream_t st) {
+template <typename E> hipError_t distill_part(const DistillArgs& a, bool back, hipStream_t st) {
     const double read = (double)a.rows * a.vocab * sizeof(E), lists = (double)a.rows * a.top * 8;
     const double bytes = read * (a.grad ? 2 : 1) + lists + 12.0 * a.rows;
     if (a.vocab <= SMALL_VOCAB)
@@ -1210,7 +1210,19 @@ template <typename E> hipError_t distill_launch(const DistillArgs& a, bool back,
     }
     return hipGetLastError();
 }
-template <typename E> hipError_t top_launch(const TopArgs& a, hipStream_t st) {
+template <typename E> hipError_t distill_launch(const DistillArgs& a, bool back, hipStream_t st) {
+    hipError_t e = hipSuccess;
+    for (int64_t n = 0; n < a.rows && e == hipSuccess; n += ROWS_PER_PART)
+        e = distill_part<E>(from_row<E>(a, n, a.rows - n < ROWS_PER_PART ? a.rows - n : ROWS_PER_PART), back, st);
+    return e;
+}
+template <typename E> TopArgs from_row(TopArgs a, int64_t n, int64_t rows) {
+    a.z = (const E*)a.z + n * a.stride;
+    a.index_out += n * a.top; a.value_out += n * a.top;
+    a.rows = rows;
+    return a;
+}
+template <typename E> hipError_t top_part(const TopArgs& a, hipStream_t st) {
     const double bytes = (double)a.rows * a.vocab * sizeof(E) + (double)a.rows * a.top * 8;
     if (a.vocab <= SMALL_VOCAB) return top_small_launch<E>(a, bytes, st);
     const int64_t vecs = (int64_t)a.piece * (int)sizeof(E) / 16;
@@ -1224,10 +1236,7 @@ template <typename E> hipError_t top_launch(const TopArgs& a, hipStream_t st) {
         return hipGetLastError();
     }
     for (int64_t n = 0; n < a.rows; n += ROWS_PER_LAUNCH) {
-        TopArgs b = a;
-        b.rows = a.rows - n < ROWS_PER_LAUNCH ? a.rows - n : ROWS_PER_LAUNCH;
-        b.z = (const E*)a.z + n * a.stride;
-        b.index_out += n * a.top; b.value_out += n * a.top;
+        const TopArgs b = from_row<E>(a, n, a.rows - n < ROWS_PER_LAUNCH ? a.rows - n : ROWS_PER_LAUNCH);
         const ProfSlot ps = prof_slot();
         const dim3 grid(a.pieces, (unsigned)b.rows);
         if (vecs <= 256 * 4) PQL_LAUNCH(ps, (top_row_kernel<E, 256, 4>), grid, dim3(256), 0, st, b);
@@ -1245,6 +1254,12 @@ template <typename E> hipError_t top_launch(const TopArgs& a, hipStream_t st) {
         prof_commit(ps, KID_TOP_MERGE, 0.0, (double)a.rows * a.top * 8 * (a.pieces + 1));
     }
     return hipGetLastError();
+}
+template <typename E> hipError_t top_launch(const TopArgs& a, hipStream_t st) {
+    hipError_t e = hipSuccess;
+    for (int64_t n = 0; n < a.rows && e == hipSuccess; n += ROWS_PER_PART)
+        e = top_part<E>(from_row<E>(a, n, a.rows - n < ROWS_PER_PART ? a.rows - n : ROWS_PER_PART), st);
+    return e;
 }
 // The lists of a row's pieces are merged in registers: at most 8192 entries.  The 64 largest of one row of 20000 whole 12 us,
 // in five pieces 19.

@@ -3,7 +3,7 @@ double-precision reference.  Tolerances: those of test_gpu_student.py, derived t
 import numpy as np
 import pytest
 
-from test_gpu_student import Delta, close, env  # noqa: F401
+from test_gpu_student import NORM, Delta, close, env  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 GRADS = ("dq", "dk", "dv", "dg", "dbeta", "dstate")
@@ -218,3 +218,103 @@ def test_outputs_in_16_bits_are_rounded_once(env, t):
             else:
                 ctx.pql_delta_forward(shape, given, S.Sequence(out), last, None, S.workspace(ctx.delta_workspace_bytes(shape, False)))
             assert float(out[0, 0, 0, 0]) == 1 + 2.0 ** -7, (what, call)
+
+
+# ---- more rows than one launch takes -------------------------------------------------------------
+# Rows repeat with a period that no launch's share is a multiple of, so that the reference is small.  Selections and what is summed
+# over tokens repeat bit for bit; sums over a row do not, since where its 16-byte granules lie goes by the row's address.
+def periodic(torch, x, n):
+    return x.repeat(-(-n // x.shape[0]), *[1] * (x.dim() - 1))[:n].contiguous()
+
+
+def repeats(x, period):
+    return bool((x[period:] == x[:-period]).all())
+
+
+def close_everywhere(torch, x, want, what):
+    """close() for rows that repeat, on the device."""
+    want = torch.from_numpy(want).cuda()
+    rms, part, err = want.square().mean().sqrt(), len(want) * 40000, 0.0
+    for i in range(0, len(x), part):
+        got = x[i:i + part].double()
+        y = periodic(torch, want, len(got))
+        off = (got - y).abs()
+        if x.dtype == torch.bfloat16:
+            off = (off - torch.exp2(torch.floor(torch.log2(torch.maximum(got.abs(), y.abs()).clamp(min=1e-37))) - 8)).clamp(min=0)
+        assert bool((off <= 40 * NORM * torch.maximum(rms, y.abs())).all()), what
+        err += float(off.square().sum())
+    assert err ** 0.5 <= NORM * float(rms) * x.numel() ** 0.5, what
+
+
+@pytest.mark.parametrize("rows,vocab,top,dtype", [(2 ** 29 + 3, 2, 1, "bfloat16"), (65539, 1025, 65, "float32"), (65539, 8300, 70, "bfloat16")])
+def test_more_rows_than_one_launch_takes(env, rows, vocab, top, dtype):
+    torch, S, ctx = env
+    period = 97
+    rng = np.random.default_rng(top)
+    z = torch.from_numpy(2 * rng.standard_normal((period, vocab))).to(getattr(torch, dtype)).cuda()
+    host = z.double().cpu().numpy()
+    z = periodic(torch, z, rows)
+    d = S.Logits(z)
+    index, value = torch.full((rows, top), 7, dtype=torch.int32, device="cuda"), torch.full((rows, top), 7.0, device="cuda")
+    ctx.pql_top_logits(d, top, index, value, S.workspace(ctx.top_logits_workspace_bytes(d, top)))
+    from oracle import student_oracle as O
+    want_i, want_v = O.top_logits(host, top)
+    assert np.array_equal(index[:period].cpu().numpy(), want_i) and np.array_equal(value[:period].double().cpu().numpy(), want_v)
+    assert repeats(index, period) and repeats(value, period)
+    value.add_(1.0)
+    t = S.Teacher(index, value)
+    loss, lse, weight = (torch.full((rows,), 7.0, device="cuda") for _ in range(3))
+    grad = torch.full_like(z, 7.0)
+    ctx.pql_distill_loss(d, t, 1.0, weight, loss, lse, S.Logits(grad), S.workspace(ctx.distill_workspace_bytes(d)))
+    want = O.distill(host, want_i, want_v + 1.0, 1.0, np.full(period, 7.0))
+    for name, x, y in zip(("loss", "lse", "grad"), (loss, lse, grad), want):
+        close_everywhere(torch, x, y, name)
+    ctx.pql_distill_backward(d, t, 1.0, lse, weight, S.Logits(grad.fill_(7)))
+    close_everywhere(torch, grad, want[2], "gradient by itself")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_more_sequences_than_one_launch_takes(env, dtype):
+    torch, S, ctx = env
+    from oracle import student_oracle as O
+    n, period, t, hk, hv, dk, dv = 65539, 37, 3, 1, 2, 4, 3
+    d = Delta(env, period, t, hk, hv, dk, dv, dtype=dtype, lengths=[i % (t + 1) for i in range(period)], resets=[(3, 1)], seed=6)
+    wide = lambda x: periodic(torch, x, n)  # noqa: E731
+    q, k, v, g, beta, do, state, ds = map(wide, (d.q, d.k, d.v, d.g, d.beta, d.do, d.state, d.ds))
+    lengths = wide(d.lengths)
+    shape, given = S.delta_shape(q, v, d.scale), S.DeltaInput(q, k, v, g, beta, lengths, state)
+    out, last = torch.full_like(v, 7.0), torch.full_like(state, 7.0)
+    saved = S.workspace(ctx.delta_saved_bytes(shape))
+    ctx.pql_delta_forward(shape, given, S.Sequence(out), last, saved, None)
+    grads = [torch.full_like(x, 7.0) for x in (q, k, v, g, beta, state)]
+    ctx.pql_delta_backward(shape, given, saved, S.Sequence(do), ds, S.DeltaGrad(*grads), S.workspace(ctx.delta_workspace_bytes(shape, True)))
+    for name, x, y in zip(("out", "state") + GRADS, [out, last] + grads, [*d.want(), *d.want_grads()]):
+        close(x[:period], y, name)
+        assert repeats(x, period), name
+
+
+def test_more_heads_than_one_launch_takes(env):
+    """Two sequences in launches of their own, and a key head whose gradient is the sum over 40000 value heads."""
+    torch, S, ctx = env
+    n, t, period, times, dk, dv = 2, 3, 40, 1000, 4, 3
+    d = Delta(env, n, t, 1, period, dk, dv, resets=[(1, 1)], seed=8)
+    wide = lambda x, at: x.repeat(*[times if i == at else 1 for i in range(x.dim())])  # noqa: E731
+    v, g, beta, do = (wide(x, 2) for x in (d.v, d.g, d.beta, d.do))
+    state, ds = wide(d.state, 1), wide(d.ds, 1)
+    shape, given = S.delta_shape(d.q, v, d.scale), S.DeltaInput(d.q, d.k, v, g, beta, None, state)
+    out, last = torch.full_like(v, 7.0), torch.full_like(state, 7.0)
+    saved = S.workspace(ctx.delta_saved_bytes(shape))
+    ctx.pql_delta_forward(shape, given, S.Sequence(out), last, saved, None)
+    grads = [torch.full_like(x, 7.0) for x in (d.q, d.k, v, g, beta, state)]
+    ctx.pql_delta_backward(shape, given, saved, S.Sequence(do), ds, S.DeltaGrad(*grads), S.workspace(ctx.delta_workspace_bytes(shape, True)))
+    want = d.want_grads()
+    # the sum of 40000 terms in order: the error of one sum of 32-bit numbers grows with sqrt(40000) roundings of 6e-8, 1.2e-5; of terms
+    # that repeat, with up to 40000 of them, 2.4e-3
+    for name, x, y in zip(("dq", "dk"), grads, want):
+        off = np.abs(x.double().cpu().numpy() - times * y)
+        assert np.linalg.norm(off) <= 2.4e-3 * np.linalg.norm(times * y), name
+    for name, x, y in zip(("out", "state") + GRADS[2:], [out, last] + grads[2:], [*d.want(), *want[2:]]):
+        at = 1 if name in ("state", "dstate") else 2
+        x = x.transpose(0, at)
+        close(x[:period].transpose(0, at), y, name)
+        assert repeats(x, period), name
