@@ -32,23 +32,25 @@ BINS, TOP = 51, 8
 
 
 class DeltaRule(torch.autograd.Function):
-    """The gated delta rule over whole windows, from states of zeros."""
+    """The gated delta rule over whole windows, from states of zeros.  It has no second derivative."""
 
     @staticmethod
     def forward(fn, ctx, q, k, v, log_decay, beta):
         shape = S.delta_shape(q, v, q.shape[-1] ** -0.5)
-        given = S.DeltaInput(q, k, v, log_decay, beta)
         out = torch.empty_like(v)
         saved = S.workspace(ctx.delta_saved_bytes(shape))
-        ctx.pql_delta_forward(shape, given, S.Sequence(out), None, saved, None)
-        fn.held = ctx, shape, given, saved
+        ctx.pql_delta_forward(shape, S.DeltaInput(q, k, v, log_decay, beta), S.Sequence(out), None, saved, None)
+        fn.call = ctx, shape
+        fn.save_for_backward(q, k, v, log_decay, beta, saved)
         return out
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(fn, out_grad):
-        ctx, shape, given, saved = fn.held
-        grads = [torch.empty_like(t) for t in given.tensors[:5]]
-        ctx.pql_delta_backward(shape, given, saved, S.Sequence(out_grad.contiguous()), None, S.DeltaGrad(*grads),
+        ctx, shape = fn.call
+        *tensors, saved = fn.saved_tensors
+        grads = [torch.empty_like(t) for t in tensors]
+        ctx.pql_delta_backward(shape, S.DeltaInput(*tensors), saved, S.Sequence(out_grad.contiguous()), None, S.DeltaGrad(*grads),
                                S.workspace(ctx.delta_workspace_bytes(shape, True)))
         return (None, *grads)
 
