@@ -1086,19 +1086,23 @@ constexpr int NT_LONG = 512;
 constexpr int64_t WAVE_VECS = 64 * 16, WAVE_ROWS = 2048;
 constexpr int64_t MAX_GRID = 0x7fffffff;
 
-// Pieces of a long row, of `least` elements or more: one where there is a row for every CU, else as many as give 1024
-// workgroups.  fp32 rows of 131072, in pieces and whole: loss and gradient of one row 11 and 46 us, of 128 rows 46 and 55, of
-// 255 rows 75 and 69; the 8 largest of one row 13 and 22 us, of 128 rows 27 and 30, of 255 rows 40 and 39.
-int pieces_of(int64_t rows, int vocab, int least, int most) {
-    if (rows >= 256 || vocab <= SMALL_VOCAB) return 1;
+// Pieces of a long row, of `least` elements or more: as many as give 1024 workgroups, but one where `most_rows` rows or more
+// (of 131072 logits; in proportion more of longer ones) keep the CUs busy by themselves.
+int pieces_of(int64_t rows, int vocab, int least, int most, int most_rows) {
+    if (rows >= 256 || vocab <= SMALL_VOCAB || rows * 131072 > (int64_t)most_rows * (vocab > 131072 ? vocab : 131072)) return 1;
     int64_t p = (1024 + rows - 1) / (rows > 0 ? rows : 1);
     const int64_t by_len = vocab / least;
     if (p > by_len) p = by_len;
     if (p > most) p = most;
     return (int)(p < 1 ? 1 : p);
 }
-// A second launch takes 4 us: one row of 5000 whole 8 us, in two pieces 10; of 20000 whole 13 us, in five 11.
-int distill_pieces(const pql_logits& z, int most) { return pieces_of(z.rows, z.vocab, 4096, most); }
+// A second launch takes 4 us, so rows have to be long: of 80 KB for loss and gradient, of 192 KB for the loss alone.  In pieces and whole, us, fp32:
+// loss and gradient, 1 row of 20000 9 and 11, 64 of 40000 14 and 18, 128 of 131072 42 and 53, 192 58 and 54, 160 of 600000 290 and
+// 367; loss, 1 row of 40000 9 and 7, 1 of 131072 8 and 13, 128 17 and 16.  bf16, loss and gradient: 1 row of 20000 9 and 8, of 40000 10 and 11.
+int distill_pieces(const pql_logits& z, bool grad) {
+    const int64_t bytes = (int64_t)z.vocab * (z.dtype == PQL_F32 ? 4 : 2);
+    return bytes < (grad ? 80000 : 192000) ? 1 : pieces_of(z.rows, z.vocab, 4096, 256, 128);
+}
 int piece_len(int vocab, int pieces) {      // a multiple of 64 elements: pieces keep the row's alignment
     const int len = (vocab + pieces - 1) / pieces;
     return pieces == 1 ? vocab : (len + 63) / 64 * 64;
@@ -1261,10 +1265,13 @@ template <typename E> hipError_t top_launch(const TopArgs& a, hipStream_t st) {
         e = top_part<E>(from_row<E>(a, n, a.rows - n < ROWS_PER_PART ? a.rows - n : ROWS_PER_PART), st);
     return e;
 }
-// The lists of a row's pieces are merged in registers: at most 8192 entries.  The 64 largest of one row of 20000 whole 12 us,
-// in five pieces 19.
+// The lists of a row's pieces are merged in registers: at most 8192 entries.  That costs the more the longer the lists, and the more of
+// their values are equal, as many 16-bit ones are.  In pieces and whole, us, fp32: the 8 largest of 1 row of 65536 16 and 16, of 1 of 131072 15 and 21,
+// of 128 26 and 29, of 192 34 and 33; the 64 largest of 1 21 and 25, of 64 36 and 27, of 64 of 600000 62 and 115; the 128 largest of 1 of 200000
+// 50 and 35.  bf16: the 8 largest of 1 of 131072 17 and 20, the 24 largest 25 and 22, the 64 largest 63 and 27.
 int top_pieces(const pql_logits& z, int top) {
-    return pieces_of(z.rows, z.vocab, 16384, 8192 / top);
+    const int weight = z.dtype == PQL_F32 ? top : 2 * top;
+    return z.vocab < 131072 || weight > 64 ? 1 : pieces_of(z.rows, z.vocab, 16384, 8192 / top, weight <= 32 ? 128 : 48);
 }
 bool misaligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) != 0; }
 int32_t check_logits(pql_ctx* c, const pql_logits& z, const char* text) {
@@ -1309,7 +1316,7 @@ int32_t pql_top_logits(pql_ctx* c, pql_logits z, int32_t top, int32_t* index_out
 int64_t pql_distill_workspace_bytes(const pql_logits* z) {
     if (!z) return PQL_ERR_NULL;
     if (!logits_ok(*z)) return PQL_ERR_INVALID_ARG;
-    const int p = distill_pieces(*z, 256);
+    const int p = distill_pieces(*z, true);
     return p > 1 ? (int64_t)up256((size_t)z->rows * (2 * p + PQL_MAX_TOP) * 4) : 0;
 }
 
@@ -1348,7 +1355,7 @@ int32_t pql_distill_loss(pql_ctx* c, pql_logits z, pql_teacher t, float temperat
     const int32_t rc = distill_check(c, z, t, temperature, grad, false);
     if (rc != PQL_OK || z.rows == 0) return rc;
     if (!loss_out || !lse_out) return ctx_fail(c, PQL_ERR_NULL, "pql_distill_loss: null pointer");
-    const int pieces = distill_pieces(z, 256);
+    const int pieces = distill_pieces(z, grad.data != nullptr);
     if (pieces > 1 && !workspace) return ctx_fail(c, PQL_ERR_NULL, "pql_distill_loss: null workspace");
     if (misaligned(workspace, 256) || misaligned(loss_out, 4) || misaligned(lse_out, 4) || misaligned(row_weight, 4))
         return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_distill_loss: misaligned pointer");
@@ -1370,7 +1377,7 @@ int32_t pql_distill_backward(pql_ctx* c, pql_logits z, pql_teacher t, float temp
     if (misaligned(lse, 4) || misaligned(loss_grad, 4)) return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_distill_backward: misaligned pointer");
     // every piece works out the list's masses anew: 16384 elements keep that below a tenth of it; fewer where there are few rows
     int pieces = z.vocab <= SMALL_VOCAB ? 1 : (z.vocab + 16383) / 16384;
-    const int few = distill_pieces(z, 1 << 30);
+    const int few = pieces_of(z.rows, z.vocab, 4096, 1 << 30, 256);
     if (few > pieces) pieces = few;
     DistillArgs a = distill_args(z, t, temperature, loss_grad, grad, pieces);
     a.lse = lse;

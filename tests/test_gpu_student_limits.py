@@ -3,7 +3,7 @@ double-precision reference.  Tolerances: those of test_gpu_student.py, derived t
 import numpy as np
 import pytest
 
-from test_gpu_student import NORM, Delta, close, env  # noqa: F401
+from test_gpu_student import NORM, Delta, close, env, lists, logits  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 GRADS = ("dq", "dk", "dv", "dg", "dbeta", "dstate")
@@ -318,3 +318,48 @@ def test_more_heads_than_one_launch_takes(env):
         x = x.transpose(0, at)
         close(x[:period].transpose(0, at), y, name)
         assert repeats(x, period), name
+
+
+@pytest.mark.parametrize("rows,vocab,top,dtype", [(1, 131072, 32, "float32"), (128, 131072, 9, "float32"), (100, 140009, 1, "bfloat16"),
+                                                  (5, 200003, 64, "float32"), (3, 600011, 16, "bfloat16"), (2, 1300021, 64, "float32")])
+@pytest.mark.parametrize("levels", [0, 3])
+def test_selection_of_long_rows_in_pieces(env, rows, vocab, top, dtype, levels):
+    """Lists of pieces joined: distinct logits and a few values that all pieces hold, rows that begin with nothing to select."""
+    torch, S, ctx = env
+    rng = np.random.default_rng(vocab + levels)
+    x = rng.integers(0, levels, (rows, vocab)) if levels else rng.standard_normal((rows, vocab))
+    z = torch.from_numpy(x.astype(np.float32)).to(getattr(torch, dtype)).cuda()
+    z[0, : vocab // 2] = float("-inf")
+    z[-1, vocab // 3:] = float("-inf")
+    d = S.Logits(z)
+    assert ctx.top_logits_workspace_bytes(d, top) > 0
+    index = torch.full((rows, top), 7, dtype=torch.int32, device="cuda")
+    value = torch.full((rows, top), 7.0, device="cuda")
+    ctx.pql_top_logits(d, top, index, value, S.workspace(ctx.top_logits_workspace_bytes(d, top)))
+    from oracle import student_oracle as O
+    want_i, want_v = O.top_logits(z.float().cpu().numpy(), top)
+    assert np.array_equal(index.cpu().numpy(), want_i)
+    assert np.array_equal(value.double().cpu().numpy(), want_v)
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(1, 20011, "float32"), (128, 20000, "float32"), (129, 20000, "float32"), (3, 40009, "bfloat16"), (2, 50021, "float32"),
+                                              (1, 300007, "float32"), (1, 300007, "bfloat16")])
+def test_loss_of_long_rows_in_pieces_and_whole(env, rows, vocab, dtype):
+    """Either side of the rules that cut rows: loss and gradient in one call, each by itself."""
+    torch, S, ctx = env
+    z, host = logits(torch, rows, vocab, dtype, vocab, True, mask=0.0)
+    index, value, weight = lists(rows, vocab, 40, vocab + 1)
+    z[:], host = torch.nan_to_num(z, neginf=-1.0), np.nan_to_num(host, neginf=-1.0)
+    d, t, w = S.Logits(z), S.Teacher(torch.from_numpy(index).cuda(), torch.from_numpy(value).cuda()), torch.from_numpy(weight).cuda()
+    loss, lse = (torch.full((rows,), 7.0, device="cuda") for _ in range(2))
+    grad = torch.full((rows, vocab), 7.0, dtype=z.dtype, device="cuda")
+    ws = S.workspace(ctx.distill_workspace_bytes(d))
+    want = O_distill(host, index, value, 1.5, weight)
+    ctx.pql_distill_loss(d, t, 1.5, w, loss, lse, S.Logits(grad), ws)
+    for name, x, y in zip(("loss", "lse", "grad"), (loss, lse, grad), want):
+        close(x, y, name)
+    ctx.pql_distill_loss(d, t, 1.5, w, loss.fill_(7), lse.fill_(7), None, ws)
+    close(loss, want[0], "loss alone")
+    ctx.pql_distill_loss(d, t, 1.5, None, loss, lse, None, ws)
+    ctx.pql_distill_backward(d, t, 1.5, lse, w, S.Logits(grad.fill_(7)))
+    close(grad, want[2], "gradient by itself")
