@@ -166,18 +166,6 @@ template <typename M, int ROWS, int COLS, bool EXACT> struct Tile {
             o[0] = (E)x;
         }
     }
-    __device__ __forceinline__ floatx4 get4(int row, int k) const {       // exact tiles only
-        const E* o = p + row * LD + k;
-        floatx4 x;
-        if constexpr (sizeof(E) == 4) {
-            x = *(const floatx4*)o;
-        } else {
-            const bf16x4 h = *(const bf16x4*)o;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = (float)h[i];
-        }
-        return x;
-    }
     // the operands of N 16-row tiles (rows row + 16 n) over K steps of 32, all requested at once
     template <int K, int N, typename F> __device__ __forceinline__ void frags(int row, int k, F (&f)[K][N]) const {
 #pragma unroll

@@ -77,21 +77,23 @@ def load_library() -> C.CDLL:
     return lib
 
 
-_INT32 = -1                                     # of lists; no type of tokens or logits
 _codes = {}
+_f32 = _i32 = None                              # torch's types, found with the first tensor that is described
 
 
 def _code(t):
-    """PQL_F32, PQL_BF16, _INT32, or None for any other type."""
+    """PQL_F32, PQL_BF16, or None for any other type."""
+    global _f32, _i32
     if not _codes:
         import torch
-        _codes.update({torch.float32: PQL_F32, torch.bfloat16: PQL_BF16, torch.int32: _INT32})
+        _f32, _i32 = torch.float32, torch.int32
+        _codes.update({torch.float32: PQL_F32, torch.bfloat16: PQL_BF16})
     return _codes.get(t.dtype)
 
 
 def dtype_code(t) -> int:
     code = _code(t)
-    if code is None or code == _INT32:
+    if code is None:
         raise TypeError("tokens and logits are float32 or bfloat16, not %s" % t.dtype)
     return code
 
@@ -108,12 +110,21 @@ def workspace(nbytes: int, device="cuda"):
     return t
 
 
-def _dense(t, what: str, like, code=PQL_F32):
-    """The pointer of a contiguous float32 (or int32) tensor of that shape; None stays None."""
+def _state(t, what: str, like):
+    """The pointer of a contiguous float32 tensor of that shape; None stays None."""
     if t is None:
         return None
-    if t.shape != like or _code(t) != code or not t.is_contiguous():
-        raise ValueError("%s: expected a contiguous %s tensor of shape %s" % (what, "int32" if code == _INT32 else "float32", like))
+    if t.dtype is not _f32 or t.shape != like or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous float32 tensor of shape %s" % (what, like))
+    return t.data_ptr()
+
+
+def _values(t, what: str, count: int, dtype):
+    """The pointer of a contiguous tensor of so many elements; None stays None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != count or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous tensor of %d elements of %s" % (what, count, dtype))
     return t.data_ptr()
 
 
@@ -157,7 +168,7 @@ class _Described:
         self.c = struct()
         for name, x in zip(("q", "k", "v", "log_decay", "beta"), self.tensors):
             setattr(self.c, name, Sequence(x).c)
-        self.c.state = _dense(state, what + ": state", self.state_shape)
+        self.c.state = _state(state, what + ": state", self.state_shape)
         self.ref = C.byref(self.c)
 
 
@@ -187,7 +198,7 @@ class Logits:
     def __init__(self, t):
         if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
             raise ValueError("logits: [rows, vocab], contiguous within a row")
-        self.tensor = t
+        self.tensor, self.rows = t, t.shape[0]
         stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
         self.c = PqlLogits(t.data_ptr(), t.shape[0], stride, t.shape[1], dtype_code(t))
 
@@ -200,7 +211,7 @@ class Teacher:
         if index.dim() != 2 or index.shape != value.shape or index.dtype != torch.int32 or value.dtype != torch.float32 \
                 or not index.is_contiguous() or not value.is_contiguous():
             raise ValueError("lists are contiguous int32 and float32 tensors [rows, top]")
-        self.index, self.value = index, value
+        self.index, self.value, self.rows = index, value, index.shape[0]
         self.c = PqlTeacher(index.data_ptr(), value.data_ptr(), index.shape[1])
 
 
@@ -236,7 +247,7 @@ class StudentContext(B.Context):
 
     @staticmethod
     def _state(given, t, what):
-        return given.c.state if t is given.tensors[5] else _dense(t, what, given.state_shape)
+        return given.c.state if t is given.tensors[5] else _state(t, what, given.state_shape)
 
     def pql_delta_step(self, shape, given: DeltaInput, state_out, out: Sequence, stream=None):
         self._fits(shape, given, out)
@@ -258,25 +269,24 @@ class StudentContext(B.Context):
                                                 state_out_grad, grads.ref, B._ptr(workspace), B._stream(stream)))
 
     def pql_top_logits(self, logits: Logits, top, index_out, value_out, workspace, stream=None):
-        like = (logits.c.rows, top)
-        index_out, value_out = _dense(index_out, "index_out", like, _INT32), _dense(value_out, "value_out", like)
+        n = logits.rows * top
+        index_out, value_out = _values(index_out, "index_out", n, _i32), _values(value_out, "value_out", n, _f32)
         self._check(self.lib.pql_top_logits(self.h, logits.c, top, index_out, value_out, B._ptr(workspace), B._stream(stream)))
 
     @staticmethod
-    def _per_row(logits, teacher, *named):
-        rows = logits.c.rows
-        if teacher.index.shape[0] != rows:
-            raise ValueError("the teacher's lists are of %d rows, the logits of %d" % (teacher.index.shape[0], rows))
-        return [_dense(t, what, (rows,)) for what, t in named]
+    def _rows(logits, teacher):
+        if teacher.rows != logits.rows:
+            raise ValueError("the teacher's lists are of %d rows, the logits of %d" % (teacher.rows, logits.rows))
+        return logits.rows
 
     def pql_distill_loss(self, logits: Logits, teacher: Teacher, temperature, row_weight, loss_out, lse_out, grad,
                          workspace, stream=None):
-        row_weight, loss_out, lse_out = self._per_row(logits, teacher, ("row_weight", row_weight), ("loss_out", loss_out),
-                                                      ("lse_out", lse_out))
-        self._check(self.lib.pql_distill_loss(self.h, logits.c, teacher.c, temperature, row_weight, loss_out, lse_out,
+        n = self._rows(logits, teacher)
+        self._check(self.lib.pql_distill_loss(self.h, logits.c, teacher.c, temperature, _values(row_weight, "row_weight", n, _f32),
+                                              _values(loss_out, "loss_out", n, _f32), _values(lse_out, "lse_out", n, _f32),
                                               NO_GRAD if grad is None else grad.c, B._ptr(workspace), B._stream(stream)))
 
     def pql_distill_backward(self, logits: Logits, teacher: Teacher, temperature, lse, loss_grad, grad: Logits, stream=None):
-        lse, loss_grad = self._per_row(logits, teacher, ("lse", lse), ("loss_grad", loss_grad))
-        self._check(self.lib.pql_distill_backward(self.h, logits.c, teacher.c, temperature, lse, loss_grad, grad.c,
-                                                  B._stream(stream)))
+        n = self._rows(logits, teacher)
+        self._check(self.lib.pql_distill_backward(self.h, logits.c, teacher.c, temperature, _values(lse, "lse", n, _f32),
+                                                  _values(loss_grad, "loss_grad", n, _f32), grad.c, B._stream(stream)))
