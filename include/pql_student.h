@@ -74,7 +74,7 @@ typedef struct {
  *     out_t = scale S_t^T q_t
  * with S_0 = input.state; the last state of each sequence goes to state_out (may be input.state itself).
  * Sequences of length 0 keep their state; outputs behind a length are zeros.  Time grows with steps:
- * pql_delta_forward is the faster call from about 8 tokens (16384 states of 64 x 64) to 12 (1024 states) on.
+ * pql_delta_forward is the faster call from about 12 tokens on (1024 or 16384 states of 64 x 64, fp32).
  * Errors: PQL_ERR_NULL, PQL_ERR_INVALID_ARG, PQL_ERR_ALIGNMENT. */
 int32_t pql_delta_step(pql_ctx* ctx, const pql_delta_shape* shape, const pql_delta_input* input,
                        float* state_out, pql_seq out, void* stream);
@@ -122,8 +122,8 @@ int32_t pql_top_logits(pql_ctx* ctx, pql_logits logits, int32_t top, int32_t* in
  * t = temperature > 0, w = row_weight ([device] float[rows], NULL: ones).  With grad.data set (same rows,
  * vocab and dtype, a stride of its own; may be the logits themselves), the gradient of sum_n loss_out[n],
  *     grad_nj = w_n t (q_j - sum_{k: index_k = j} p_k),
- * is written in the same pass.  Rows with w_n = 0 or without a valid entry are not read: loss, lse and
- * gradient 0.  A listed answer that the student has at -inf gives loss +inf; a row of nothing but -inf has
+ * is written in the same pass.  Nothing is used of rows with w_n = 0 or without a valid entry,
+ * whatever they hold: loss, lse and gradient 0.  A listed answer that the student has at -inf gives loss +inf; a row of nothing but -inf has
  * lse -inf, q = 0.  workspace as above, pql_distill_workspace_bytes. */
 int64_t pql_distill_workspace_bytes(const pql_logits* logits);
 int32_t pql_distill_loss(pql_ctx* ctx, pql_logits logits, pql_teacher teacher, float temperature,
@@ -131,10 +131,10 @@ int32_t pql_distill_loss(pql_ctx* ctx, pql_logits logits, pql_teacher teacher, f
                          void* stream);
 
 /* The gradient alone, for a loss sum_n loss_grad[n] L_n with L_n the loss above at w_n = 1, from the lse_out of
- * that call: grad_nj = loss_grad[n] t (q_j - ...).  Rows with loss_grad[n] = 0 or without a valid entry are not
- * read and get zeros; rows of weight 0 in that call have no log-sum-exp, and must have loss_grad[n] = 0 here.  The
- * rounding of lse_out costs q 2e-7 |lse|; rows with |lse| > 32 are therefore read once more for the maximum and sum
- * of their own.  grad may be the logits themselves. */
+ * that call: grad_nj = loss_grad[n] t (q_j - ...).  Nothing is used of rows with loss_grad[n] = 0 or without a
+ * valid entry, which get zeros; rows of weight 0 in that call have no log-sum-exp, and must have loss_grad[n] = 0
+ * here.  The rounding of lse_out costs q 2e-7 |lse|; rows with |lse| > 32 are therefore read once more for the
+ * maximum and sum of their own.  grad may be the logits themselves. */
 int32_t pql_distill_backward(pql_ctx* ctx, pql_logits logits, pql_teacher teacher, float temperature, const float* lse,
                              const float* loss_grad, pql_logits grad, void* stream);
 

@@ -318,8 +318,9 @@ template <typename E> __device__ __forceinline__ E* at_out(const DeltaSeq& s, in
 // =============================================================================================
 // One token or a few.  A workgroup holds up to 4 LX columns of one state in registers: lanes along the columns (four
 // each), 256 / LX groups of rows.  With z = S~^T k and w = S~^T q found together, u = beta (v - z) and
-// o = scale (w + (q.k) u) need one reduction per token instead of two.  One token of 16384 environments, 4 heads of 64 x 64:
-// 363 us, 5.9 TB/s of states read and written (a large copy reaches 4.8); of 64 environments, 2 heads of 32 x 32: 5 us, a launch.
+// o = scale (w + (q.k) u) need one reduction per token instead of two.  One token of 16384 environments, 4 heads of 64 x 64,
+// bf16: 361 us, 6.0 TB/s of states read and written to another buffer, in place 385 us (a large copy reaches 5.0 TB/s); fp32 393 and 398 us; of
+// 64 environments, 2 heads of 32 x 32: 4 us, a launch.
 // =============================================================================================
 template <typename E, int LX, bool VEC>
 __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a) {
@@ -676,7 +677,7 @@ template <int NT> __device__ __forceinline__ void put_padded(const char* p, int 
 // One workgroup per chunk and value head, a wavefront per 16 tokens: K K^T and Q K^T (lower halves), the gates, the inverse, and
 // all of it out in the order in which the scans' lanes want it, so that these load operands straight into registers; K^T and
 // Q^T by one head of each group.  Bound by the latency of its steps, four workgroups to a CU, and by what it writes: long
-// 99 us, sequences 60 us (each about 3 TB/s), windows 29 us; without the inverse 9 % less, without K^T and Q^T 18 to 34 %.
+// 98 us, sequences 57 us (each about 3 TB/s), windows 26 us; without the inverse 9 % less, without K^T and Q^T 18 to 34 %.
 template <typename M, int C, int DK, bool AL>
 __global__ __launch_bounds__(4 * C) void delta_prepare_kernel(DeltaArgs a) {
     using E = typename M::E;
@@ -786,9 +787,9 @@ __global__ __launch_bounds__(4 * C) void delta_prepare_kernel(DeltaArgs a) {
 // Chunks in order: outputs and states, 16 NT columns per workgroup.  Half of the wavefronts (one per SIMD, 16 tokens each)
 // carry the chain K S, X, T X, K^T Y that every chunk has to wait for, the other half what only the outputs need, Q S and
 // P Y, in the gaps of the first.  All operands of a chunk are requested into registers, the next chunk's K, V and T once the
-// products that wait for LDS have asked for theirs, K^T two phases before it is used.  Bound by the chain: long 435 us, 1.7 us
-// for each of 256 chunks (336 us in all if nothing had to be loaded), sequences 142 us, there with 0.33 GB of states and errors
-// kept for the gradient, windows 55 us.  (Every wavefront doing both: long 662 us.)
+// products that wait for LDS have asked for theirs, K^T two phases before it is used.  Bound by the chain: long 448 us, 1.75 us
+// for each of 256 chunks (a quarter less if nothing had to be loaded), sequences 147 us, there with 0.33 GB of states and errors
+// kept for the gradient, windows 53 us; long in fp32 812 us.  (Every wavefront doing both: long 662 us.)
 // =============================================================================================
 template <typename M, int C, int DK, int NT> struct ScanLds {
     using S = Tile<M, 16 * NT, DK, false>;          // S^T [column][dim_k]
@@ -1173,7 +1174,7 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
 // Gradient, chunks in reverse order: dV, and what delta_back_kernel needs of every chunk (dS1, dX, dY).  Again half of the
 // wavefronts carry the chain K dS, dY, T^T dR, K^T dX; the other half find what it adds from outside, P^T dO and
 // Q^T (gam o dO), one chunk ahead, and hand it over in LDS in the layout of the results.  Bound by the chain and by what it
-// writes (dX, dY, dS: 0.4 GB in the sequences): sequences 167 us, windows 66 us.
+// writes (dX, dY, dS: 0.4 GB in the sequences): sequences 163 us, windows 67 us; sequences in fp32 221 us.
 // =============================================================================================
 template <typename M, int C, int DK, int NT> struct BackScanLds {
     using S = Tile<M, 16 * NT, DK, false>;          // dS^T [column][dim_k]
@@ -1412,7 +1413,8 @@ __global__ __launch_bounds__(8 * C) __attribute__((amdgpu_waves_per_eu(DK == 128
 // wavefronts, the next 32 columns being on their way meanwhile; then those over tokens with E and F in LDS, K^T and Q^T
 // straight from memory.  With a.heads_wg = group a workgroup takes the value heads of one key head one after the other and
 // adds dQ and dK up in registers; where that leaves too few workgroups, it takes one, and delta_group_kernel adds.  With keys of
-// 128 it fills a CU's LDS and registers alone, and is bound by LDS: sequences 240 us, 0.4 GB of states at 1.7 TB/s; windows 61 us.
+// 128 it fills a CU's LDS and registers alone, and is bound by LDS: sequences 220 us, 0.4 GB of states at 1.8 TB/s; windows 58 us.
+// fp32 with keys of 128, chunks of 64 and several heads a workgroup keeps 27 to 36 registers in scratch memory: sequences in fp32 350 us.
 // =============================================================================================
 template <typename M, int C, int DK> struct BackLds {
     using R = Tile<M, C, 32, false>;        // R, Y, dX
@@ -1718,7 +1720,9 @@ bool shape_ok(const pql_delta_shape& s) {
 // kernel moves the states of every chunk through LDS, which then takes longer than its products.  Measured with 32 and with 64
 // tokens, us: forward, fp32, 64 x 64: 2048 sequences times heads of 32 tokens 66 and 123, 1024 of 256 198 and 246, 32 of 1024 65 and 59; bf16,
 // 128 x 128: 256 of 128 51 and 57, 16 of 16384 690 and 533.  Forward and gradient, bf16, 128 x 128: 256 of 128 204
-// and 170, 64 of 2048 815 and 579; few, 4 of 128, 49 and 58; fp32, 128 x 128: 256 of 256 465 and 477, 32 of 64 59 and 75.
+// and 170, 64 of 2048 815 and 579; few, 4 of 128, 49 and 58; fp32, 128 x 128: 256 of 256 465 and 477, 32 of 64 59 and 75.  Few and short,
+// forward: fp32, 64 x 64: 1 of 64 13 and 19, 16 of 256 22 and 26, 32 of 512 34 and 37; bf16, 128 x 128: 1 of 64 14 and 17, 16 of 256 23 and 24, 32 of 512
+// 37 and 35; just above, 16 of 1024: fp32 51 and 51, bf16 55 and 45.
 int chunk_of(const pql_delta_shape& s, bool train) {
     const int64_t pairs = (int64_t)s.batch * s.heads_v;
     if (s.steps <= 32) return 32;

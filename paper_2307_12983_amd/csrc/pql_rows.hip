@@ -214,7 +214,7 @@ __device__ __forceinline__ float entry_loss(const Entry& e, float z, float m, fl
 
 // =============================================================================================
 // Small vocabularies: a group of G lanes per row, which it reads once and holds; bound by memory.  327680 rows of 51, fp32, lists
-// of 8, loss and gradient: 35 us, 4.5 TB/s.
+// of 8, loss and gradient: 45 us, 3.5 TB/s (34 us where the caches hold them); loss and gradient in calls of their own 29 and 31 us.
 // =============================================================================================
 template <typename E, int G, int R, bool BACK>
 __global__ __launch_bounds__(256) void distill_small_kernel(DistillArgs a) {
@@ -512,7 +512,8 @@ template <typename E, int NT> __device__ __forceinline__ void zero_stretch(E* ou
     for (int j = threadIdx.x; j < len; j += NT) out[j] = from_float<E>(0.f);
 }
 
-// One workgroup per row; bound by memory: 4096 rows of 65536, bf16, lists of 64, loss and gradient 213 us, 5.0 TB/s.  NV > 0: the row stays in registers between its statistics and its gradient, NV granules a thread;
+// One workgroup per row; bound by memory: 4096 rows of 65536, bf16, lists of 64, loss and gradient 201 us, 5.3 TB/s; loss
+// alone 130 us.  NV > 0: the row stays in registers between its statistics and its gradient, NV granules a thread;
 // NV = 0, rows that do not fit: it is read again.
 template <typename E, int NT, int NV>
 __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a) {
@@ -585,7 +586,8 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a) {
 
 // Few rows: pieces of a.piece elements.  First launch: each piece's maximum and sum, and the logits of the listed
 // answers that lie in it (a second launch that writes over the logits could no longer read them).  16 rows of 131072, fp32:
-// 4 us each launch, and 11 us for the gradient in a call of its own (8.4 MB read, 8.4 MB written: 3.5 us at a copy's rate).
+// 4 us each launch, and 11 us for the gradient in a call of its own (8.4 MB read, 8.4 MB written: 3.5 us at a copy's rate; bf16 9 us; 4096 rows
+// of 65536, bf16, 160 us).
 template <typename E, int NT>
 __global__ __launch_bounds__(NT) void distill_part_kernel(DistillArgs a) {
     __shared__ float s_red[NT / 64];
@@ -976,7 +978,7 @@ __global__ __launch_bounds__(256) void top_wave_kernel(TopArgs a) {
 }
 
 // One workgroup per row or piece.  NV > 0: the stretch stays in registers between the two passes, NV granules a thread; else it
-// is read again, from L2 for the most part.  1024 rows of 131072, bf16, lists of 64: 78 us, 3.5 TB/s.
+// is read again, from L2 for the most part.  1024 rows of 131072, lists of 64: bf16 82 us, 3.3 TB/s, fp32 150 us, 3.6 TB/s.
 template <typename E, int NT, int NV, bool MERGE>
 __device__ __forceinline__ void top_of_stretch(const TopArgs& a) {
     __shared__ __align__(16) unsigned s_key[CAND];
@@ -1082,7 +1084,8 @@ constexpr int NT_LONG = 512;
 // One wavefront per row: rows of at most 16 KB, and enough of them to give every SIMD two.  Loss and gradient, bf16, by
 // wavefronts and by workgroups: 2048 rows of 1500 8 and 12 us, of 4000 12 and 14, of 8000 19 and 18; 65536 rows of 1500 121
 // and 263, of 4000 208 and 318, of 8000 415 and 414; 512 rows of 8000 11 and 9.  Selection of 32, 65536 rows: 116 and 357,
-// 158 and 384, 289 and 408 us.
+// 158 and 384, 289 and 408 us.  fp32, loss and gradient: 2048 rows of 1100 10 and 10, of 2000 13 and 12, of 4000 20 and 20; 65536 rows 182 and 229, 262 and 298,
+// 480 and 446; selection: 2048 rows 7 and 14, 10 and 15, 12 and 16; 65536 rows 96 and 313, 113 and 329, 218 and 342.
 constexpr int64_t WAVE_VECS = 64 * 16, WAVE_ROWS = 2048;
 constexpr int64_t MAX_GRID = 0x7fffffff;
 
@@ -1114,6 +1117,7 @@ bool logits_ok(const pql_logits& z) {
 }
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
+// Seven registers a lane, for 33 to 56 logits: 327680 rows of 40, fp32, loss and gradient 31.6 us, with eight 32.5; 8 largest 31.8 and 32.9.
 #define SMALL_CASES(X) X(8, 4) X(8, 7) X(8, 8) X(16, 8) X(32, 8) X(64, 8) X(64, 16)
 template <typename E, bool BACK> hipError_t distill_small_launch(const DistillArgs& a, int kid, double bytes, hipStream_t st) {
 #define PQL_SMALL(G, R)                                                                                              \
