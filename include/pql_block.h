@@ -1,0 +1,103 @@
+/*
+ * libpql, operators around a student's memory (pql_student.h): the lookup of its tokens' embeddings, and the norms
+ * before and after a block with the block's gate and residual sum; each with its gradient.
+ *
+ * The conventions of pql.h and pql_student.h hold (return values, caller-owned memory, streams, threads, graphs,
+ * error text of the context; PQL_F32 and PQL_BF16; sums, statistics and products held in fp32 or more).  Differences:
+ *   Rows        Token tensors are batch * steps rows of contiguous elements, described by pql_rows: row n (= sequence *
+ *               steps + step) starts at data + n * stride elements, stride >= its columns.  data must be aligned to its
+ *               element; rows that all start on 16-byte boundaries load faster.  Rows may repeat (a stride of 0) where
+ *               they are read; gradients and outputs have rows of their own.
+ *   Lengths     lengths[batch] ([device] int32, or NULL: all `steps`): tokens of each sequence that count, clamped to
+ *               [0, steps].  What lies behind them is not read, outputs and gradients there are written as zeros, and
+ *               it has no part in the gradients of weights.
+ *   Order       Every sum is taken in one order: equal calls give equal bits.
+ *   Aliasing    Outputs must not overlap inputs or each other except where a call says so.
+ */
+#ifndef PQL_BLOCK_H
+#define PQL_BLOCK_H
+
+#include "pql_student.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* [device] rows of a matrix, see "Rows". */
+typedef struct { void* data; int64_t stride; } pql_rows;
+
+/* ---- embeddings ------------------------------------------------------------------------------- */
+
+/* batch * steps rows of `per_row` tokens each (at least 1; a token for every action dimension, say), whose embeddings
+ * are added; vocab and dim at least 1; dtype of the table, the output and their gradients.  batch * steps * per_row
+ * must stay below 2^31. */
+typedef struct {
+    int32_t batch, steps, per_row, vocab, dim, dtype;
+    float   scale;
+} pql_embed_shape;
+
+/* out_n = scale * sum_j table[tokens[n][j]].  tokens: [device] int32 [batch * steps][per_row], dense; a token outside
+ * [0, vocab) adds nothing.  table: vocab rows of dim.
+ * Errors: PQL_ERR_NULL, PQL_ERR_INVALID_ARG, PQL_ERR_ALIGNMENT (of these and all calls below). */
+int32_t pql_embed_forward(pql_ctx* ctx, const pql_embed_shape* shape, const int32_t* tokens, const int32_t* lengths,
+                          const pql_rows* table, const pql_rows* out, void* stream);
+
+/* table_grad_v = scale * sum over (n, j) with tokens[n][j] = v of out_grad_n, in ascending order of (n, j); every row
+ * of table_grad is written.  workspace: [device] pql_embed_workspace_bytes(shape) bytes, 256-byte aligned. */
+int64_t pql_embed_workspace_bytes(const pql_embed_shape* shape);
+int32_t pql_embed_backward(pql_ctx* ctx, const pql_embed_shape* shape, const int32_t* tokens, const int32_t* lengths,
+                           const pql_rows* out_grad, const pql_rows* table_grad, void* workspace, void* stream);
+
+/* ---- norms, gate and residual sum around a block ------------------------------------------------ */
+
+#define PQL_ACT_NONE    0              /* x */
+#define PQL_ACT_SIGMOID 1              /* 1 / (1 + exp(-x)) */
+#define PQL_ACT_SILU    2              /* x / (1 + exp(-x)) */
+#define PQL_ACT_GELU    3              /* x (1 + erf(x / sqrt 2)) / 2 */
+#define PQL_ACT_RELU    4              /* max(x, 0), derivative 0 at 0 */
+
+#define PQL_RESIDUAL_MAX_DIM    8192
+#define PQL_RESIDUAL_MAX_GROUPS 256
+
+/* Rows of dim elements in `groups` equal parts (the heads of a memory; groups divides dim).  gate_cols: columns of the
+ * gate: 0 (no gate), groups (one value for each part) or dim; gate_act: PQL_ACT_*.  eps_post, eps_pre: 0 for no norm
+ * in that place, or what is added to the mean square. */
+typedef struct {
+    int32_t batch, steps, dim, groups, dtype, gate_cols, gate_act;
+    float   eps_post, eps_pre, scale_x, scale_y;
+} pql_residual_shape;
+
+/* x: the residual stream (data NULL: zeros); y: the block's output (data NULL: zeros; then no gate); gate;
+ * post, pre: [device] fp32 [dim] weights after and before a block, or NULL: ones. */
+typedef struct {
+    pql_rows x, y, gate;
+    const float *post, *pre;
+    const int32_t* lengths;
+} pql_residual_input;
+
+/* Gradients with the layouts of what they belong to; any may be NULL (data or pointer) and is then not computed. */
+typedef struct {
+    pql_rows x, y, gate;
+    float *post, *pre;
+} pql_residual_grad;
+
+/* With N(z) = z / sqrt(mean(z^2) + eps), the mean taken over each part of the row for y and over the row for sum,
+ *     sum_n = scale_x x_n + scale_y act(gate_n) post N(y_n),        next_n = pre N(sum_n)
+ * where what is left out (a norm of eps 0, a gate, a weight) is the factor 1 or the identity.  sum may be x or y itself,
+ * next may be y; either may have data NULL, not both.  next follows from the sum before that is rounded to dtype. */
+int32_t pql_residual_forward(pql_ctx* ctx, const pql_residual_shape* shape, const pql_residual_input* input,
+                             const pql_rows* sum, const pql_rows* next, void* stream);
+
+/* Gradient of a loss whose gradients with respect to the outputs are sum_grad and next_grad (data NULL: zeros, not
+ * both).  input: as given to pql_residual_forward; it must still hold what that call read.  grads->x may be sum_grad,
+ * grads->y next_grad.  workspace: [device] pql_residual_workspace_bytes(shape) bytes, 256-byte aligned, or NULL where
+ * neither post nor pre has a gradient. */
+int64_t pql_residual_workspace_bytes(const pql_residual_shape* shape);
+int32_t pql_residual_backward(pql_ctx* ctx, const pql_residual_shape* shape, const pql_residual_input* input,
+                              const pql_rows* sum_grad, const pql_rows* next_grad, const pql_residual_grad* grads,
+                              void* workspace, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* PQL_BLOCK_H */

@@ -1,0 +1,222 @@
+"""Thin ctypes binding over the operators around a student's memory (declared in ``include/pql_block.h``).
+
+Like ``student``: argument marshalling only, every method of ``BlockContext`` forwards device pointers and sizes to the
+C entry point of the same name.  Tensors are described once by the small classes below; a call checks that what it is
+given belongs together, since the kernels would read and write out of range.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+from . import binding as B
+from . import student as S
+
+PQL_F32, PQL_BF16 = S.PQL_F32, S.PQL_BF16
+ACTIVATIONS = {"none": 0, "sigmoid": 1, "silu": 2, "gelu": 3, "relu": 4}
+PQL_RESIDUAL_MAX_DIM, PQL_RESIDUAL_MAX_GROUPS = 8192, 256
+workspace = S.workspace
+
+# every symbol include/pql_block.h declares
+EXPORTS = ["pql_embed_forward", "pql_embed_workspace_bytes", "pql_embed_backward", "pql_residual_forward",
+           "pql_residual_workspace_bytes", "pql_residual_backward"]
+
+
+class PqlRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64)]
+
+
+class PqlEmbedShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "steps", "per_row", "vocab", "dim", "dtype")] + [("scale", C.c_float)]
+
+
+class PqlResidualShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "steps", "dim", "groups", "dtype", "gate_cols", "gate_act")] + \
+               [(n, C.c_float) for n in ("eps_post", "eps_pre", "scale_x", "scale_y")]
+
+
+class PqlResidualInput(C.Structure):
+    _fields_ = [(n, PqlRows) for n in ("x", "y", "gate")] + [(n, C.c_void_p) for n in ("post", "pre", "lengths")]
+
+
+class PqlResidualGrad(C.Structure):
+    _fields_ = [(n, PqlRows) for n in ("x", "y", "gate")] + [(n, C.c_void_p) for n in ("post", "pre")]
+
+
+_ready = None
+
+
+def load_library() -> C.CDLL:
+    """libpql.so with the prototypes of this module's entry points set."""
+    global _ready
+    if _ready is not None:
+        return _ready
+    lib = S.load_library()
+    P, I32, I64 = C.c_void_p, C.c_int32, C.c_int64
+    rows = C.POINTER(PqlRows)
+    embed, residual = C.POINTER(PqlEmbedShape), C.POINTER(PqlResidualShape)
+    r_in, r_grad = C.POINTER(PqlResidualInput), C.POINTER(PqlResidualGrad)
+    sig = {
+        "pql_embed_forward": (I32, [P, embed, P, P, rows, rows, P]),
+        "pql_embed_workspace_bytes": (I64, [embed]),
+        "pql_embed_backward": (I32, [P, embed, P, P, rows, rows, P, P]),
+        "pql_residual_forward": (I32, [P, residual, r_in, rows, rows, P]),
+        "pql_residual_workspace_bytes": (I64, [residual]),
+        "pql_residual_backward": (I32, [P, residual, r_in, rows, rows, r_grad, P, P]),
+    }
+    for name, (res, args) in sig.items():
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = res, args
+    _ready = lib
+    return lib
+
+
+class Rows:
+    """A matrix [rows, cols] or token tensor [batch, steps, cols] whose rows are contiguous and equally far apart."""
+
+    def __init__(self, t):
+        if t.dim() not in (2, 3):
+            raise ValueError("rows are tensors [rows, cols] or [batch, steps, cols]")
+        cols = t.shape[-1]
+        if cols > 1 and t.stride(-1) != 1 and t.numel() > 0:
+            raise ValueError("the last dimension of rows must be contiguous")
+        n, stride = (t.shape[0], t.stride(0)) if t.dim() == 2 or t.shape[1] == 1 else (t.shape[0] * t.shape[1], t.stride(1))
+        if t.dim() == 3 and t.shape[0] > 1 and t.shape[1] > 1 and t.stride(0) != t.shape[1] * stride and t.numel() > 0:
+            raise ValueError("the rows of a token tensor must be equally far apart")
+        self.tensor = t
+        self.key = (n, cols, S.dtype_code(t))
+        self.c = PqlRows(t.data_ptr(), stride if n > 1 else cols)
+        self.ref = C.byref(self.c)
+
+
+NONE = PqlRows(None, 0)
+_NO_ROWS = C.byref(NONE)
+
+
+def _ref(rows, key, what):
+    """The descriptor of rows that have to be like key; None stays none."""
+    if rows is None:
+        return _NO_ROWS
+    if rows.key != key:
+        raise ValueError("%s: %d rows of %d (type %d) expected, got %d rows of %d (type %d)" % ((what,) + key + rows.key))
+    return rows.ref
+
+
+def _rows(t, key, what):
+    if t is None:
+        return NONE
+    r = Rows(t)
+    _ref(r, key, what)
+    return r.c
+
+
+def _floats(t, count, what):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != count or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous float32 tensor of %d elements" % (what, count))
+    return t.data_ptr()
+
+
+def _ints(t, count, what):
+    import torch
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() != count or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous int32 tensor of %d elements" % (what, count))
+    return t.data_ptr()
+
+
+def embed_shape(tokens, table, scale: float) -> PqlEmbedShape:
+    """The shape of a call from its tokens [batch, steps, per_row] and its table [vocab, dim]."""
+    if tokens.dim() != 3 or table.dim() != 2:
+        raise ValueError("tokens: [batch, steps, per_row]; table: [vocab, dim]")
+    return PqlEmbedShape(*tokens.shape, *table.shape, S.dtype_code(table), scale)
+
+
+def residual_shape(batch, steps, dim, dtype, groups=1, gate_cols=0, gate_act="none", eps_post=0.0, eps_pre=0.0, scale_x=1.0,
+                   scale_y=1.0) -> PqlResidualShape:
+    """dtype: torch.float32 or torch.bfloat16; gate_act: a name of ACTIVATIONS; an eps of 0: no norm in that place."""
+    import torch
+    code = {torch.float32: PQL_F32, torch.bfloat16: PQL_BF16}.get(dtype)
+    if code is None:
+        raise TypeError("rows are float32 or bfloat16, not %s" % dtype)
+    return PqlResidualShape(batch, steps, dim, groups, code, gate_cols, ACTIVATIONS[gate_act], eps_post, eps_pre, scale_x, scale_y)
+
+
+class _Residual:
+    def __init__(self, struct, shape, x, y, gate, post, pre, what):
+        n, dim, dtype = shape.batch * shape.steps, shape.dim, shape.dtype
+        self.key = (n, dim, dtype)
+        self.tensors = (x, y, gate, post, pre)
+        self.c = struct()
+        self.c.x = _rows(x, self.key, what + ": x")
+        self.c.y = _rows(y, self.key, what + ": y")
+        self.c.gate = _rows(gate, (n, shape.gate_cols, dtype), what + ": gate")
+        self.c.post, self.c.pre = _floats(post, dim, what + ": post"), _floats(pre, dim, what + ": pre")
+        self.shape = bytes(shape)
+        self.ref = C.byref(self.c)
+
+
+class ResidualInput(_Residual):
+    """What pql_residual_forward reads: x, y [batch, steps, dim], gate [batch, steps, gate_cols], post, pre: float32 [dim],
+    lengths: int32 [batch]; each may be None."""
+
+    def __init__(self, shape, x=None, y=None, gate=None, post=None, pre=None, lengths=None):
+        super().__init__(PqlResidualInput, shape, x, y, gate, post, pre, "ResidualInput")
+        self.lengths = lengths
+        self.c.lengths = _ints(lengths, shape.batch, "ResidualInput: lengths")
+
+
+class ResidualGrad(_Residual):
+    """Where the gradients go; the shapes of the inputs, each may be None."""
+
+    def __init__(self, shape, x=None, y=None, gate=None, post=None, pre=None):
+        super().__init__(PqlResidualGrad, shape, x, y, gate, post, pre, "ResidualGrad")
+
+
+class BlockContext(S.StudentContext):
+    """A context whose methods are the entry points of a block beside those of ``StudentContext``."""
+
+    def __init__(self, cfg: B.PqlConfig = None):
+        load_library()
+        super().__init__(cfg)
+
+    # ---- host queries
+    def embed_workspace_bytes(self, shape: PqlEmbedShape) -> int:
+        return self.lib.pql_embed_workspace_bytes(C.byref(shape))
+
+    def residual_workspace_bytes(self, shape: PqlResidualShape) -> int:
+        return self.lib.pql_residual_workspace_bytes(C.byref(shape))
+
+    # ---- device calls
+    @staticmethod
+    def _embed(s, tokens, lengths, table, out):
+        n = s.batch * s.steps
+        return (C.byref(s), _ints(tokens, n * s.per_row, "tokens"), _ints(lengths, s.batch, "lengths"),
+                _ref(table, (s.vocab, s.dim, s.dtype), "table"), _ref(out, (n, s.dim, s.dtype), "rows"))
+
+    def pql_embed_forward(self, shape, tokens, lengths, table: Rows, out: Rows, stream=None):
+        self._check(self.lib.pql_embed_forward(self.h, *self._embed(shape, tokens, lengths, table, out), B._stream(stream)))
+
+    def pql_embed_backward(self, shape, tokens, lengths, out_grad: Rows, table_grad: Rows, workspace, stream=None):
+        s, t, n, table, rows = self._embed(shape, tokens, lengths, table_grad, out_grad)
+        self._check(self.lib.pql_embed_backward(self.h, s, t, n, rows, table, B._ptr(workspace), B._stream(stream)))
+
+    @staticmethod
+    def _of(shape, *described):
+        for d in described:
+            if d.shape != bytes(shape):
+                raise ValueError("tensors and shape of the call do not agree")
+
+    def pql_residual_forward(self, shape, given: ResidualInput, sum: Rows, next: Rows, stream=None):
+        self._of(shape, given)
+        self._check(self.lib.pql_residual_forward(self.h, C.byref(shape), given.ref, _ref(sum, given.key, "sum"),
+                                                  _ref(next, given.key, "next"), B._stream(stream)))
+
+    def pql_residual_backward(self, shape, given: ResidualInput, sum_grad: Rows, next_grad: Rows, grads: ResidualGrad, workspace,
+                              stream=None):
+        self._of(shape, given, grads)
+        self._check(self.lib.pql_residual_backward(self.h, C.byref(shape), given.ref, _ref(sum_grad, given.key, "sum_grad"),
+                                                   _ref(next_grad, given.key, "next_grad"), grads.ref, B._ptr(workspace),
+                                                   B._stream(stream)))

@@ -85,6 +85,19 @@ const char* kernel_name(int kid) {
         case KID_DELTA_BACK_SCAN: return "delta_back_scan_kernel";
         case KID_DELTA_BACK: return "delta_back_kernel";
         case KID_DELTA_GROUP: return "delta_group_kernel";
+        case KID_EMBED: return "embed_kernel";
+        case KID_EMBED_SORT: return "embed_sort_kernel";
+        case KID_EMBED_SUM: return "embed_sum_kernel";
+        case KID_EMBED_JOIN: return "embed_join_kernel";
+        case KID_RESIDUAL: return "residual_kernel";
+        case KID_RESIDUAL_BACK: return "residual_back_kernel";
+        case KID_RESIDUAL_JOIN: return "residual_join_kernel";
+        case KID_FFN_PREPARE: return "ffn_prepare_kernel";
+        case KID_FFN_GATED: return "ffn_gated_kernel";
+        case KID_FFN_PRODUCT: return "ffn_product_kernel";
+        case KID_FFN_BACK: return "ffn_back_kernel";
+        case KID_FFN_JOIN: return "ffn_join_kernel";
+        case KID_FFN_ROWS: return "ffn_rows_kernel";
         default: return "?";
     }
 }

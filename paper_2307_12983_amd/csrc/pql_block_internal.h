@@ -1,0 +1,75 @@
+// Internal declarations of the operators around a student's memory (include/pql_block.h).
+#pragma once
+
+#include "pql_block.h"
+#include "pql_student_internal.h"
+
+namespace pql {
+
+constexpr int ROW_ALIGN = 16;               // bytes of the widest load or store
+
+inline int elem_size(int32_t dtype) { return dtype == PQL_F32 ? 4 : 2; }
+inline size_t to256(size_t x) { return (x + 255) / 256 * 256; }
+inline bool off_by(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) != 0; }
+// Rows that all start on 16-byte boundaries.
+inline bool rows_aligned(const pql_rows& r, int32_t dtype) {
+    return !off_by(r.data, ROW_ALIGN) && r.stride * elem_size(dtype) % ROW_ALIGN == 0;
+}
+// Rows that may be written: each has a place of its own (one row needs none).
+inline bool own_rows(const pql_rows& r, int64_t rows, int64_t cols) { return rows <= 1 || r.stride >= cols; }
+inline bool read_rows(const pql_rows& r) { return r.stride >= 0; }
+
+// Which rows count: row = sequence * steps + step.
+struct Live {
+    const int* lengths;
+    unsigned steps;
+    __device__ __forceinline__ bool operator()(unsigned row) const {
+        if (!lengths) return true;
+        const unsigned b = row / steps;
+        return (int)(row - b * steps) < lengths[b];
+    }
+};
+
+// ---- 16 bytes of elements as floats ----------------------------------------------------------------
+template <typename E> constexpr int VEC_OF = ROW_ALIGN / (int)sizeof(E);
+__device__ __forceinline__ void widen(uint4 g, float* x, float) {
+    x[0] = __uint_as_float(g.x); x[1] = __uint_as_float(g.y); x[2] = __uint_as_float(g.z); x[3] = __uint_as_float(g.w);
+}
+__device__ __forceinline__ void widen(uint4 g, float* x, bf16_t) {
+    const unsigned u[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ uint4 narrow(const float* x, float) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+typedef __bf16 block_bf16x2 __attribute__((ext_vector_type(2)));
+typedef float block_floatx2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ unsigned narrow2(float a, float b) {      // to nearest even, both in one register
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((block_floatx2{a, b}), block_bf16x2));
+}
+__device__ __forceinline__ uint4 narrow(const float* x, bf16_t) {
+    return make_uint4(narrow2(x[0], x[1]), narrow2(x[2], x[3]), narrow2(x[4], x[5]), narrow2(x[6], x[7]));
+}
+
+// ---- activations -----------------------------------------------------------------------------------
+// f(x) and f'(x).  Factors that vanish do so before they meet a large x, so that finite x give finite results.
+struct Act { float f, d; };
+template <int ACT> __device__ __forceinline__ Act activate(float x) {
+    if constexpr (ACT == PQL_ACT_SIGMOID) {
+        const float s = 1.f / (1.f + expf(-x));
+        return {s, s * (1.f - s)};
+    } else if constexpr (ACT == PQL_ACT_SILU) {
+        const float s = 1.f / (1.f + expf(-x));
+        return {x * s, s * (1.f + x * (1.f - s))};
+    } else if constexpr (ACT == PQL_ACT_GELU) {
+        const float h = 0.5f * erfcf(-0.70710678f * x);
+        return {x * h, h + 0.39894228f * x * expf(-0.5f * x * x)};
+    } else if constexpr (ACT == PQL_ACT_RELU) {
+        return {x > 0.f ? x : (x != x ? x : 0.f), x > 0.f ? 1.f : 0.f};
+    } else {
+        return {x, 1.f};
+    }
+}
+
+}  // namespace pql

@@ -25,7 +25,10 @@ enum KernelId : int {
     KID_SPLIT_POLICY = 44,
     KID_DISTILL = 45, KID_DISTILL_JOIN = 46, KID_DISTILL_GRAD = 47, KID_TOP_LOGITS = 48, KID_TOP_MERGE = 49, KID_DELTA_STEP = 50,
     KID_DELTA_PREPARE = 51, KID_DELTA_SCAN = 52, KID_DELTA_BACK_SCAN = 53, KID_DELTA_BACK = 54, KID_DELTA_GROUP = 55,
-    KID_COUNT = 56
+    KID_EMBED = 56, KID_EMBED_SORT = 57, KID_EMBED_SUM = 58, KID_EMBED_JOIN = 59, KID_RESIDUAL = 60, KID_RESIDUAL_BACK = 61,
+    KID_RESIDUAL_JOIN = 62, KID_FFN_PREPARE = 63, KID_FFN_GATED = 64, KID_FFN_PRODUCT = 65, KID_FFN_BACK = 66, KID_FFN_JOIN = 67,
+    KID_FFN_ROWS = 68,
+    KID_COUNT = 69
 };
 const char* kernel_name(int kid);
 bool prof_active();

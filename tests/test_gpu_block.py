@@ -1,0 +1,371 @@
+"""The operators around a student's memory on the GPU against the double-precision reference.
+
+Tolerances, from the arithmetic (u = 2^-24, the rounding of a 32-bit operation):
+  embeddings   a sum of k terms and a factor: relative to the sum of the terms' sizes at most (k + 1) u, taken element by element.
+  residual     a mean over d squares and some ten operations: 2-norm within (sqrt(d) / 2 + 20) u of the result's, d at most 8192:
+               4e-6.  Weights' gradients are sums over rows of such terms, each sum rounded at most `rows` times, at random: the
+               same bound with the rows' number in the place of d, at the size of the terms.
+  ffn          products over K elements of terms with an error of u each, accumulated in 32 bits: (sqrt(K) + 10) u of the 2-norm
+               for each of at most three products in a row; K at most 16384: 3 * 138 u = 2.5e-5.  In bf16 what lies between
+               two products (m, da, db) is rounded to bf16 once: 2^-8 / sqrt 3 / 2 = 1.2e-3 of its 2-norm at most, which the next
+               product passes on to a result whose terms have random signs as it is, or up to twice that where one factor is smooth.
+An output in bf16 is rounded once more, by at most half the spacing of its values, which is taken off first.  Single elements
+may be off by 40 times the bound of the norm, relative to the larger of the element and the root mean square.  """
+import numpy as np
+import pytest
+
+from oracle import block_oracle as O
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible: the gpu-marked tests need a real MI355X")
+    from paper_2307_12983_amd import block as K
+    return torch, K, K.BlockContext()
+
+
+def error_of(got, want):
+    """Absolute errors beyond the rounding of the output's type; both hold the same values that are not finite."""
+    bf16 = str(got.dtype) == "torch.bfloat16"
+    got, want = got.detach().double().cpu().numpy(), np.asarray(want, np.float64)
+    assert got.shape == want.shape
+    assert np.all(np.isfinite(got)) and np.all(np.isfinite(want))
+    off = np.abs(got - want)
+    if bf16:                                            # 8 significant bits: half a spacing is 2^(exponent - 8)
+        size = np.maximum(np.abs(got), np.abs(want))
+        off = np.maximum(0.0, off - np.exp2(np.floor(np.log2(np.maximum(size, 1e-37))) - 8))
+    return off, want
+
+
+def close(got, want, what, bound):
+    off, want = error_of(got, want)
+    norm = np.linalg.norm(want)
+    err = np.linalg.norm(off)
+    assert err <= bound * norm, "%s: error %.3g of the norm, %.3g allowed" % (what, err / norm if norm else np.inf, bound)
+    if norm:
+        worst = np.max(off / np.maximum(norm / np.sqrt(want.size), np.abs(want)))
+        assert worst <= 40 * bound, "%s: an element off by %.3g" % (what, worst)
+
+
+class Made:
+    """Tensors in a layout, kept with their values in double precision."""
+
+    def __init__(self, env, seed, dtype, layout="dense", lengths=None):
+        self.torch = env[0]
+        self.rng, self.dt, self.layout, self.lengths = np.random.default_rng(seed), getattr(env[0], dtype), layout, lengths
+
+    def place(self, values, shape=None):
+        """Rows of those values; what does not count is poisoned."""
+        torch = self.torch
+        v = np.array(values, np.float64)
+        if self.lengths is not None and v.ndim == 3:
+            v[~O.counted(v.shape[:2], self.lengths)] = np.nan
+        t = torch.tensor(v).to(self.dt).cuda()
+        if self.layout == "offset":                     # rows on no 16-byte boundary, something else between them
+            big = torch.full((*t.shape[:-1], t.shape[-1] + 3), float("nan"), dtype=t.dtype, device="cuda")
+            big[..., 1:1 + t.shape[-1]] = t
+            t = big[..., 1:1 + t.shape[-1]]
+        elif self.layout == "wide":                     # aligned rows, something else between them
+            big = torch.full((*t.shape[:-1], t.shape[-1] + 24), float("nan"), dtype=t.dtype, device="cuda")
+            big[..., 8:8 + t.shape[-1]] = t
+            t = big[..., 8:8 + t.shape[-1]]
+        return t
+
+    def normal(self, *shape, by=1.0):
+        return self.place(by * self.rng.standard_normal(shape))
+
+    def out(self, *shape):
+        return self.place(np.full(shape, 7.0))
+
+    def host(self, t):
+        return None if t is None else t.double().cpu().numpy()
+
+
+def lengths_of(torch, lengths):
+    return None if lengths is None else torch.tensor(lengths, dtype=torch.int32).cuda()
+
+
+def label(c):
+    return "-".join(str(v).replace(" ", "") for v in (c.values() if isinstance(c, dict) else c))
+
+
+# ---- embeddings -----------------------------------------------------------------------------------------
+EMBED = [
+    # batch, steps, per_row, vocab, dim, dtype, layout, lengths, tokens
+    (1, 1, 1, 1, 1, "float32", "dense", None, "any"),
+    (1, 1, 3, 7, 64, "bfloat16", "dense", None, "any"),
+    (64, 1, 8, 408, 256, "float32", "dense", None, "any"),
+    (5, 33, 20, 1020, 72, "bfloat16", "dense", [33, 0, 1, 12, 40], "any"),
+    (3, 70, 1, 50, 100, "float32", "offset", [70, -3, 69], "any"),
+    (4, 64, 2, 300, 513, "bfloat16", "offset", None, "any"),
+    (2, 40, 5, 9, 1024, "float32", "wide", None, "any"),
+    (8, 100, 1, 5, 40, "float32", "dense", None, "equal"),              # one token everywhere
+    (6, 50, 1, 100000, 24, "bfloat16", "dense", None, "any"),           # few of many
+    (2, 31, 1, 40, 16, "float32", "dense", None, "none"),               # no token at all
+    (2, 31, 1, 40, 16, "float32", "dense", [0, 0], "any"),              # nothing that counts
+    (40, 256, 1, 1000, 32, "float32", "dense", None, "any"),            # more places than are sorted in one launch
+    (40, 256, 1, 1023, 32, "float32", "dense", None, "any"),            # keys of ten bits and the one beyond them
+    (40, 256, 1, 1024, 32, "float32", "dense", None, "any"),
+    (40, 64, 4, 70000, 8, "bfloat16", "dense", list(range(40)), "any"),
+    (40, 256, 2, 2000000, 4, "float32", "dense", None, "far"),          # three digits
+    (64, 512, 1, 300, 8, "float32", "dense", None, "equal"),
+    (300, 512, 1, 64, 12, "float32", "dense", None, "any"),             # chunks of more than 32 places
+]
+
+
+def embed_inputs(env, case, seed=0):
+    torch = env[0]
+    n, t, m, vocab, dim, dtype, layout, lengths, which = case
+    made = Made(env, seed, dtype, layout, None)
+    tokens = made.rng.integers(-1, vocab + 1, (n, t, m))                # the ends are no tokens
+    if which == "equal":
+        tokens[:] = vocab // 2
+    elif which == "none":
+        tokens[:] = np.where(tokens % 2 == 0, -5, vocab + 3)
+    elif which == "far":
+        tokens = vocab - 1 - tokens % 100
+    table = made.normal(vocab, dim)
+    made.lengths = lengths
+    return made, torch.tensor(tokens, dtype=torch.int32).cuda(), tokens, table, made.normal(n, t, dim), lengths_of(torch, lengths)
+
+
+@pytest.mark.parametrize("case", EMBED, ids=label)
+def test_embeddings_and_their_gradient(env, case):
+    torch, K, ctx = env
+    made, tokens, host, table, out_grad, lengths = embed_inputs(env, case)
+    n, t, m, vocab, dim = case[:5]
+    scale = float(np.float32(dim ** 0.5))
+    shape = K.embed_shape(tokens, table, scale)
+    out = made.out(n, t, dim)
+    ctx.pql_embed_forward(shape, tokens, lengths, K.Rows(table), K.Rows(out))
+    size = O.embed(host, np.abs(made.host(table)), scale, case[7])
+    off, want = error_of(out, O.embed(host, made.host(table), scale, case[7]))
+    assert np.all(off <= (m + 1) * U * size)
+    made.lengths = None
+    grad = made.out(vocab, dim)
+    ctx.pql_embed_backward(shape, tokens, lengths, K.Rows(out_grad), K.Rows(grad), K.workspace(ctx.embed_workspace_bytes(shape)))
+    clean = np.nan_to_num(made.host(out_grad))
+    size, count = O.embed_grad(host, vocab, scale, np.abs(clean), case[7]), O.embed_grad(host, vocab, 1.0, np.ones((n, t, 1)), case[7])
+    off, want = error_of(grad, O.embed_grad(host, vocab, scale, clean, case[7]))
+    assert np.all(off <= (count + 1) * U * size)
+
+
+def test_embedding_gradients_have_one_order(env):
+    torch, K, ctx = env
+    made, tokens, _, table, out_grad, _ = embed_inputs(env, (40, 256, 3, 200, 96, "float32", "dense", None, "any"))
+    shape = K.embed_shape(tokens, table, 1.0)
+    results = []
+    for _ in range(3):
+        grad, space = made.out(200, 96), K.workspace(ctx.embed_workspace_bytes(shape))
+        space.random_(0, 255)
+        ctx.pql_embed_backward(shape, tokens, None, K.Rows(out_grad), K.Rows(grad), space)
+        results.append(grad)
+    assert all(torch.equal(results[0], r) for r in results)
+
+
+def test_embeddings_leave_what_is_not_theirs(env):
+    """Neither the gaps between rows nor what lies behind the last one are written."""
+    torch, K, ctx = env
+    tokens = torch.randint(0, 30, (3, 5, 2), dtype=torch.int32, device="cuda")
+    table, big, grad = torch.randn(30, 20, device="cuda"), torch.full((17, 28), 7.0, device="cuda"), torch.full((33, 28), 7.0, device="cuda")
+    shape = K.embed_shape(tokens, table, 1.0)
+    ctx.pql_embed_forward(shape, tokens, None, K.Rows(table), K.Rows(big[:15, 4:24]))
+    ctx.pql_embed_backward(shape, tokens, None, K.Rows(big[:15, 4:24]), K.Rows(grad[:30, 4:24]), K.workspace(ctx.embed_workspace_bytes(shape)))
+    for x, n in ((big, 15), (grad, 30)):
+        assert bool((x[n:] == 7).all()) and bool((x[:, :4] == 7).all()) and bool((x[:, 24:] == 7).all())
+        assert not bool((x[:n, 4:24] == 7).any())
+
+
+# ---- norms, gate and residual sum --------------------------------------------------------------------------
+def residual_case(batch, steps, dim, dtype, groups=1, form="both", gate="full", act="sigmoid", layout="dense", lengths=None, eps=(1e-5, 1e-5),
+                  weights=True, scales=(1.0, 0.5)):
+    return dict(locals())
+
+
+# Parts of one element have an eps of their values' size: with a small one y / |y| hardly depends on y, and its gradient is what is
+# left of two terms that cancel.
+RESIDUAL = [
+    residual_case(1, 1, 1, "float32", eps=(0.5, 0.5)),
+    residual_case(1, 1, 8, "bfloat16"),
+    residual_case(64, 1, 256, "float32"),
+    residual_case(5, 33, 1024, "bfloat16", lengths=[33, 0, 1, 12, 40]),
+    residual_case(3, 9, 2048, "bfloat16", act="silu"),
+    residual_case(2, 5, 4096, "float32", act="gelu"),
+    residual_case(2, 3, 8192, "float32"),
+    residual_case(2, 3, 8191, "bfloat16", layout="offset"),
+    residual_case(7, 11, 600, "float32", groups=6, form="after", act="silu", layout="offset", lengths=[11, 0, 1, 5, 9, -1, 99]),
+    residual_case(7, 11, 600, "float32", groups=6, act="silu"),
+    residual_case(3, 17, 512, "bfloat16", groups=4, gate="part", act="sigmoid", lengths=[17, 2, 9]),
+    residual_case(3, 17, 512, "float32", groups=8, form="after", gate="part", act="none"),
+    residual_case(9, 4, 72, "float32", groups=3, layout="wide"),
+    residual_case(9, 4, 75, "bfloat16", groups=25, layout="offset", act="relu"),
+    residual_case(2, 6, 256, "float32", groups=256, eps=(0.5, 1e-5)),
+    residual_case(2, 6, 8160, "float32", groups=240),
+    residual_case(2, 6, 2304, "bfloat16", groups=256),
+    residual_case(1, 5, 8190, "float32", groups=2, form="after"),
+    residual_case(4, 40, 128, "float32", form="before"),
+    residual_case(4, 40, 128, "float32", eps=(0.0, 1e-5)),
+    residual_case(4, 40, 128, "bfloat16", eps=(1e-5, 0.0), weights=False),
+    residual_case(4, 40, 130, "float32", eps=(0.0, 0.0), gate="none", scales=(0.7, -1.5)),
+    residual_case(300, 20, 64, "float32", scales=(1.0, 1.0)),
+    residual_case(2000, 9, 24, "bfloat16", act="gelu"),
+    residual_case(3, 1, 256, "float32", lengths=[0, 0, 0]),
+]
+
+
+class ResidualCall:
+    def __init__(self, env, c, seed=0, by=1.0):
+        torch, K, ctx = self.env = env
+        self.c = c
+        self.made = m = Made(env, seed, c["dtype"], c["layout"], c["lengths"])
+        n, t, d = c["batch"], c["steps"], c["dim"]
+        has_x, has_y = c["form"] != "after", c["form"] != "before"
+        self.x = m.normal(n, t, d, by=2.0 * by) if has_x else None
+        self.y = m.normal(n, t, d, by=by) if has_y else None
+        cols = {"none": 0, "part": c["groups"], "full": d}[c["gate"] if has_y else "none"]
+        self.gate = m.normal(n, t, cols) if cols else None
+        weight = lambda: torch.tensor(1 + 0.3 * m.rng.standard_normal(d)).float().cuda()  # noqa: E731
+        self.post = weight() if has_y and c["weights"] else None
+        self.pre = weight() if has_x and c["weights"] else None
+        self.sum_grad, self.next_grad = m.normal(n, t, d), m.normal(n, t, d) if has_x else None
+        self.scales = [float(np.float32(x)) for x in c["scales"]]
+        self.eps = [float(np.float32(x)) for x in c["eps"]]
+        self.lengths = lengths_of(torch, c["lengths"])
+        self.shape = K.residual_shape(n, t, d, self.made.dt, c["groups"], cols, c["act"], *self.eps, *self.scales)
+        self.given = K.ResidualInput(self.shape, self.x, self.y, self.gate, self.post, self.pre, self.lengths)
+        h = m.host
+        self.want = O.Residual(h(self.x), h(self.y), h(self.gate), h(self.post), h(self.pre), c["groups"], c["act"], *self.eps, *self.scales, c["lengths"])
+
+    def outs(self, clean=True):
+        keep, self.made.lengths = self.made.lengths, None
+        n, t, d = self.c["batch"], self.c["steps"], self.c["dim"]
+        r = self.made.out(n, t, d), (self.made.out(n, t, d) if self.x is not None else None)
+        self.made.lengths = keep
+        return r
+
+    def forward(self):
+        _, K, ctx = self.env
+        total, after = self.outs()
+        ctx.pql_residual_forward(self.shape, self.given, K.Rows(total), None if after is None else K.Rows(after))
+        return total, after
+
+    def backward(self, leave=()):
+        torch, K, ctx = self.env
+        keep, self.made.lengths = self.made.lengths, None
+        g = {k: None if getattr(self, k) is None or k in leave else self.made.out(*getattr(self, k).shape) for k in ("x", "y", "gate")}
+        self.made.lengths = keep
+        g.update({k: torch.full((self.c["dim"],), 7.0, device="cuda") if getattr(self, k) is not None and k not in leave else None for k in ("post", "pre")})
+        if self.x is not None and self.pre is None and "pre" not in leave:
+            g["pre"] = torch.full((self.c["dim"],), 7.0, device="cuda")
+        rows = lambda t: None if t is None else K.Rows(t)  # noqa: E731
+        ctx.pql_residual_backward(self.shape, self.given, rows(self.sum_grad), rows(self.next_grad), K.ResidualGrad(self.shape, **g),
+                                  K.workspace(ctx.residual_workspace_bytes(self.shape)))
+        return g
+
+    def wanted_grad(self):
+        clean = lambda t: None if t is None else np.nan_to_num(self.made.host(t))  # noqa: E731
+        return self.want.grad(clean(self.sum_grad), clean(self.next_grad))
+
+
+RES = (8192 ** 0.5 / 2 + 20) * U
+
+
+@pytest.mark.parametrize("c", RESIDUAL, ids=label)
+def test_norms_gate_and_sum(env, c):
+    call = ResidualCall(env, c)
+    total, after = call.forward()
+    close(total, call.want.sum, "sum", RES)
+    if after is not None:
+        close(after, call.want.next, "next", RES)
+
+
+@pytest.mark.parametrize("c", RESIDUAL, ids=label)
+def test_gradients_of_norms_gate_and_sum(env, c):
+    call = ResidualCall(env, c, seed=1)
+    want, got = call.wanted_grad(), call.backward()
+    for k, g in got.items():
+        if g is not None:
+            close(g, want[k], k, 2 * RES)
+
+
+def test_gradients_that_are_not_asked_for(env):
+    c = residual_case(6, 7, 96, "float32")
+    whole = ResidualCall(env, c).backward()
+    for leave in (("x",), ("y", "gate"), ("post", "pre"), ("x", "y", "gate"), ("pre", "y")):
+        some = ResidualCall(env, c).backward(leave)
+        for k, g in some.items():
+            assert (g is None) == (k in leave)
+            if g is not None:
+                assert env[0].equal(g, whole[k]), k
+
+
+def test_only_one_of_the_two_outputs(env):
+    torch, K, ctx = env
+    call = ResidualCall(env, residual_case(6, 7, 96, "bfloat16"))
+    total, after = call.forward()
+    alone, next_alone = call.outs()
+    ctx.pql_residual_forward(call.shape, call.given, K.Rows(alone), None)
+    ctx.pql_residual_forward(call.shape, call.given, None, K.Rows(next_alone))
+    assert torch.equal(alone, total) and torch.equal(next_alone, after)
+
+
+def test_outputs_in_the_inputs_places(env):
+    torch, K, ctx = env
+    for c in (residual_case(50, 3, 520, "float32"), residual_case(50, 3, 2048, "bfloat16", groups=16, gate="part")):
+        call = ResidualCall(env, c, seed=3)
+        total, after = call.forward()
+        grads = call.backward()
+        x, y = call.x.clone(), call.y.clone()
+        given = K.ResidualInput(call.shape, x, y, call.gate, call.post, call.pre, call.lengths)
+        ctx.pql_residual_forward(call.shape, given, K.Rows(x), K.Rows(y))
+        assert torch.equal(x, total) and torch.equal(y, after)
+        dx, dy = call.sum_grad.clone(), call.next_grad.clone()
+        ctx.pql_residual_backward(call.shape, call.given, K.Rows(dx), K.Rows(dy), K.ResidualGrad(call.shape, x=dx, y=dy), None)
+        assert torch.equal(dx, grads["x"]) and torch.equal(dy, grads["y"])
+
+
+def test_rows_that_repeat(env):
+    """One row of x for all of them: every repetition has its own gradient."""
+    torch, K, ctx = env
+    call = ResidualCall(env, residual_case(4, 6, 160, "float32"), seed=4)
+    one = call.x[:1, :1]
+    spread = K.ResidualInput(call.shape, one.expand(4, 6, 160).contiguous(), call.y, call.gate, call.post, call.pre)
+    same = K.ResidualInput(call.shape, one.contiguous().as_strided((4, 6, 160), (0, 0, 1)), call.y, call.gate, call.post, call.pre)
+    assert same.c.x.stride == 0
+    results = []
+    for given in (spread, same):
+        total, after = call.outs()
+        ctx.pql_residual_forward(call.shape, given, K.Rows(total), K.Rows(after))
+        dx = call.outs()[0]
+        ctx.pql_residual_backward(call.shape, given, K.Rows(call.sum_grad), K.Rows(call.next_grad), K.ResidualGrad(call.shape, x=dx), None)
+        results.append((total, after, dx))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("by", [1e-15, 1e-6, 1e6, 1e15])
+def test_sizes_of_values(env, by):
+    call = ResidualCall(env, residual_case(4, 6, 160, "float32"), seed=5, by=by)
+    total, after = call.forward()
+    close(total, call.want.sum, "sum", RES)
+    close(after, call.want.next, "next", RES)
+    for k, g in call.backward().items():
+        close(g, call.wanted_grad()[k], k, 2 * RES)
+
+
+def test_large_gates(env):
+    torch, K, ctx = env
+    for act in ("sigmoid", "silu", "gelu", "relu"):
+        call = ResidualCall(env, residual_case(2, 2, 64, "float32", act=act), seed=6)
+        call.gate.copy_(torch.tensor([-3e38, -1e4, -100.0, -0.0, 0.0, 30.0, 100.0, 60.0], device="cuda").repeat(2, 2, 8))
+        h = call.made.host
+        with np.errstate(all="ignore"):
+            call.want = O.Residual(h(call.x), h(call.y), h(call.gate), h(call.post), h(call.pre), 1, act, *call.eps, *call.scales)
+            want = call.wanted_grad()
+        close(call.forward()[0], call.want.sum, "sum", RES)
+        for k, g in call.backward().items():
+            close(g, want[k], k, 2 * RES)
