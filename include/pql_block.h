@@ -59,7 +59,8 @@ int32_t pql_embed_backward(pql_ctx* ctx, const pql_embed_shape* shape, const int
 #define PQL_RESIDUAL_MAX_DIM    8192
 #define PQL_RESIDUAL_MAX_GROUPS 256
 
-/* Rows of dim elements in `groups` equal parts (the heads of a memory; groups divides dim).  gate_cols: columns of the
+/* Rows of dim elements in `groups` equal parts (the heads of a memory; groups divides dim).  Where there are several, each
+ * counts as a power of two of elements, at least 8, and together they must not exceed PQL_RESIDUAL_MAX_DIM.  gate_cols: columns of the
  * gate: 0 (no gate), groups (one value for each part) or dim; gate_act: PQL_ACT_*.  eps_post, eps_pre: 0 for no norm
  * in that place, or what is added to the mean square. */
 typedef struct {

@@ -6,7 +6,7 @@
 //
 // Bound by memory: every tensor is read or written once, a row stays in registers from its loads to its stores, and the
 // gradient works h out again instead of reading it (which would also be rounded).  A part of a row is held by `lanes`
-// lanes (a power of two), EPT elements each; a row's parts lie in one workgroup.  Workgroups stay for many rows: they keep
+// lanes (a power of two), 8 elements each; a row's parts lie in one workgroup.  Workgroups stay for many rows: they keep
 // the weights, and the sums of the weights' gradients, in registers.
 #include "pql_block_internal.h"
 #include "pql_lanes.h"
@@ -32,7 +32,8 @@ struct ResidualArgs {
 
 // ---- a thread's elements of one row ----------------------------------------------------------------
 // AL: granules of 16 bytes, element i at granule i / V of this lane; otherwise every lanes-th element.
-template <typename E, bool AL, int EPT> struct Slice {
+constexpr int EPT = 8;                      // elements a thread
+template <typename E, bool AL> struct Slice {
     static constexpr int V = AL ? VEC_OF<E> : 1, N = EPT / V;
     int base, lane, lanes, part;
     bool on;
@@ -113,8 +114,8 @@ struct Sums {
     }
 };
 
-template <int EPT> __device__ __forceinline__ void open_gate(int act, float (&g)[EPT], float (&d)[EPT]) {
-#define PQL_GATE(A) case A: _Pragma("unroll") for (int i = 0; i < EPT; ++i) { const Act a = activate<A>(g[i]); g[i] = a.f; d[i] = a.d; } break;
+template <int N> __device__ __forceinline__ void open_gate(int act, float (&g)[N], float (&d)[N]) {
+#define PQL_GATE(A) case A: _Pragma("unroll") for (int i = 0; i < N; ++i) { const Act a = activate<A>(g[i]); g[i] = a.f; d[i] = a.d; } break;
     switch (act) {
         PQL_GATE(PQL_ACT_SIGMOID)
         PQL_GATE(PQL_ACT_SILU)
@@ -125,7 +126,7 @@ template <int EPT> __device__ __forceinline__ void open_gate(int act, float (&g)
 #undef PQL_GATE
 }
 // The gate's elements (or its one value for the part), opened: g = act(gate), d = act'(gate); ones without a gate.
-template <typename E, bool AL, int EPT> __device__ __forceinline__ void load_gate(const ResidualArgs& a, const Slice<E, AL, EPT>& s, unsigned row,
+template <typename E, bool AL> __device__ __forceinline__ void load_gate(const ResidualArgs& a, const Slice<E, AL>& s, unsigned row,
                                                                                int group, float (&g)[EPT], float (&d)[EPT]) {
     if (!a.gate) {
 #pragma unroll
@@ -145,19 +146,20 @@ template <typename E, bool AL, int EPT> __device__ __forceinline__ void load_gat
 }
 
 // ---- forward ---------------------------------------------------------------------------------------
-template <typename E, bool AL, int EPT> __global__ void __launch_bounds__(1024) residual_kernel(ResidualArgs a) {
+template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT) residual_kernel(ResidualArgs a) {
+    constexpr bool KEEP = NT < 1024;        // the weights, between rows: 1024 threads have 128 registers each
     __shared__ float lds[2 * 16], units[2 * 1024];
     const int unit = threadIdx.x / a.lanes, group = unit % a.groups, slot = unit / a.groups, slots = (int)blockDim.x / (a.lanes * a.groups);
-    Slice<E, AL, EPT> s{group * a.part, (int)threadIdx.x & (a.lanes - 1), a.lanes, a.part, false};
+    Slice<E, AL> s{group * a.part, (int)threadIdx.x & (a.lanes - 1), a.lanes, a.part, false};
     const Sums sums{lds, a.lanes};
     float post[EPT], pre[EPT];
     s.on = slot < slots;
-    s.load_weights(a.post, post);
-    s.load_weights(a.pre, pre);
+    if constexpr (KEEP) { s.load_weights(a.post, post); s.load_weights(a.pre, pre); }
     for (unsigned first = blockIdx.x * slots; first < a.rows; first += gridDim.x * slots) {
         const unsigned row = first + slot;
         const bool here = slot < slots && row < a.rows, live = here && a.live(row);
         s.on = live;
+        if constexpr (!KEEP) { s.load_weights(a.post, post); s.load_weights(a.pre, pre); }
         float h[EPT] = {};
         if (a.x) {
             s.load((const E*)a.x + row * a.x_stride, h);
@@ -202,20 +204,21 @@ template <typename E, bool AL, int EPT> __global__ void __launch_bounds__(1024) 
 }
 
 // ---- gradient --------------------------------------------------------------------------------------
-template <typename E, bool AL, int EPT> __global__ void __launch_bounds__(1024) residual_back_kernel(ResidualArgs a) {
+template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT) residual_back_kernel(ResidualArgs a) {
+    constexpr bool KEEP = NT < 1024;        // the weights, between rows: 1024 threads have 128 registers each
     __shared__ float lds[2 * 16], units[2 * 1024];
     const int unit = threadIdx.x / a.lanes, group = unit % a.groups, slot = unit / a.groups, slots = (int)blockDim.x / (a.lanes * a.groups);
-    Slice<E, AL, EPT> s{group * a.part, (int)threadIdx.x & (a.lanes - 1), a.lanes, a.part, false};
+    Slice<E, AL> s{group * a.part, (int)threadIdx.x & (a.lanes - 1), a.lanes, a.part, false};
     const Sums sums{lds, a.lanes};
     float post[EPT], pre[EPT], dpost[EPT] = {}, dpre[EPT] = {};
     s.on = slot < slots;
-    s.load_weights(a.post, post);
-    s.load_weights(a.pre, pre);
+    if constexpr (KEEP) { s.load_weights(a.post, post); s.load_weights(a.pre, pre); }
     const float over_part = 1.f / a.part, over_dim = 1.f / a.dim;
     for (unsigned first = blockIdx.x * slots; first < a.rows; first += gridDim.x * slots) {
         const unsigned row = first + slot;
         const bool here = slot < slots && row < a.rows;
         s.on = here && a.live(row);
+        if constexpr (!KEEP) { s.load_weights(a.post, post); s.load_weights(a.pre, pre); }
         float y[EPT] = {}, g[EPT], slope[EPT], h[EPT] = {}, dh[EPT] = {};
         float r = 1.f;
         if (a.x) {
@@ -342,24 +345,26 @@ __global__ void __launch_bounds__(1024) residual_join_kernel(const float* partia
 }
 
 // ---- host ------------------------------------------------------------------------------------------
+// Lanes a part: a power of two.
+int part_lanes(const pql_residual_shape& s) {
+    int lanes = 1;
+    while (lanes * EPT < s.dim / s.groups) lanes *= 2;
+    return lanes;
+}
 bool finite(float x) { return x - x == 0.f; }
 bool residual_ok(const pql_residual_shape& s) {
-    return s.batch >= 0 && s.steps >= 0 && (double)s.batch * s.steps < 2147483648.0 && s.dim >= 1 && s.dim <= PQL_RESIDUAL_MAX_DIM &&
+    const bool ok = s.batch >= 0 && s.steps >= 0 && (double)s.batch * s.steps < 2147483648.0 && s.dim >= 1 && s.dim <= PQL_RESIDUAL_MAX_DIM &&
            s.groups >= 1 && s.groups <= PQL_RESIDUAL_MAX_GROUPS && s.dim % s.groups == 0 && (s.dtype == PQL_F32 || s.dtype == PQL_BF16) &&
            (s.gate_cols == 0 || s.gate_cols == s.groups || s.gate_cols == s.dim) && s.gate_act >= PQL_ACT_NONE && s.gate_act <= PQL_ACT_RELU &&
            s.eps_post >= 0.f && s.eps_pre >= 0.f && finite(s.eps_post) && finite(s.eps_pre) && finite(s.scale_x) && finite(s.scale_y);
+    return ok && part_lanes(s) * s.groups * EPT <= PQL_RESIDUAL_MAX_DIM;
 }
 unsigned residual_rows(const pql_residual_shape& s) { return (unsigned)((int64_t)s.batch * s.steps); }
 
-struct ResidualPlan { int ept, lanes, threads, slots; unsigned grid; };
-// Elements a thread and lanes a part.
+struct ResidualPlan { int lanes, threads, slots; unsigned grid; };
 ResidualPlan residual_plan(const pql_residual_shape& s, bool back) {
     ResidualPlan p{};
-    const int part = s.dim / s.groups;
-    p.ept = 8;
-    p.lanes = 1;
-    while (p.lanes * p.ept < part) p.lanes *= 2;
-    if (p.lanes * s.groups > 1024) { p.ept = 16; p.lanes /= 2; }        // below 2 * 8192 / 8 before, since lanes < 2 * part / 8 unless it is 1
+    p.lanes = part_lanes(s);
     const int threads = p.lanes * s.groups;
     p.threads = threads <= 256 ? 256 : (threads + 63) / 64 * 64;
     p.slots = p.threads / threads;
@@ -417,12 +422,14 @@ template <typename E, bool AL> hipError_t residual_launch(const ResidualArgs& a,
     const double in = size * (!!a.x + !!a.y + (a.gate && !a.gate_part)), out = size * (!!a.sum + !!a.next);
     const ProfSlot ps = prof_slot();
     if (!back) {
-        if (p.ept == 8) PQL_LAUNCH(ps, (residual_kernel<E, AL, 8>), dim3(p.grid), dim3(p.threads), 0, st, a);
-        else PQL_LAUNCH(ps, (residual_kernel<E, AL, 16>), dim3(p.grid), dim3(p.threads), 0, st, a);
+        if (p.threads <= 256) PQL_LAUNCH(ps, (residual_kernel<E, AL, 256>), dim3(p.grid), dim3(p.threads), 0, st, a);
+        else if (p.threads <= 512) PQL_LAUNCH(ps, (residual_kernel<E, AL, 512>), dim3(p.grid), dim3(p.threads), 0, st, a);
+        else PQL_LAUNCH(ps, (residual_kernel<E, AL, 1024>), dim3(p.grid), dim3(p.threads), 0, st, a);
         prof_commit(ps, KID_RESIDUAL, 0.0, in + out);
     } else {
-        if (p.ept == 8) PQL_LAUNCH(ps, (residual_back_kernel<E, AL, 8>), dim3(p.grid), dim3(p.threads), 0, st, a);
-        else PQL_LAUNCH(ps, (residual_back_kernel<E, AL, 16>), dim3(p.grid), dim3(p.threads), 0, st, a);
+        if (p.threads <= 256) PQL_LAUNCH(ps, (residual_back_kernel<E, AL, 256>), dim3(p.grid), dim3(p.threads), 0, st, a);
+        else if (p.threads <= 512) PQL_LAUNCH(ps, (residual_back_kernel<E, AL, 512>), dim3(p.grid), dim3(p.threads), 0, st, a);
+        else PQL_LAUNCH(ps, (residual_back_kernel<E, AL, 1024>), dim3(p.grid), dim3(p.threads), 0, st, a);
         prof_commit(ps, KID_RESIDUAL_BACK, 0.0, in + out + size * (!!a.dx + !!a.dy + (a.dgate && !a.gate_part)));
     }
     return hipGetLastError();

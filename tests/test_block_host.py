@@ -153,7 +153,7 @@ def residual_calls(ctx, s, i=None, total=rows(5 * P), after=rows(6 * P), g=None,
 
 
 @pytest.mark.parametrize("kw", [dict(batch=-1), dict(steps=-1), dict(batch=1 << 16, steps=1 << 15), dict(dim=0), dict(dim=8193), dict(groups=0),
-                                dict(groups=5), dict(dim=514, groups=257), dict(dtype=2), dict(gate_cols=2), dict(gate_cols=-1), dict(gate_act=5),
+                                dict(groups=5), dict(dim=514, groups=257), dict(dim=8184, groups=248, gate_cols=0), dict(dim=8190, groups=3, gate_cols=0), dict(dtype=2), dict(gate_cols=2), dict(gate_cols=-1), dict(gate_act=5),
                                 dict(gate_act=-1), dict(eps_post=-1e-5), dict(eps_pre=float("nan")), dict(eps_pre=float("inf")),
                                 dict(scale_x=float("nan")), dict(scale_y=float("inf"))])
 def test_residuals_refuse_bad_shapes(kw):

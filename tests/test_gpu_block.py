@@ -205,7 +205,7 @@ RESIDUAL = [
     residual_case(9, 4, 72, "float32", groups=3, layout="wide"),
     residual_case(9, 4, 75, "bfloat16", groups=25, layout="offset", act="relu"),
     residual_case(2, 6, 256, "float32", groups=256, eps=(0.5, 1e-5)),
-    residual_case(2, 6, 8160, "float32", groups=240),
+    residual_case(2, 6, 7936, "float32", groups=248),
     residual_case(2, 6, 2304, "bfloat16", groups=256),
     residual_case(1, 5, 8190, "float32", groups=2, form="after"),
     residual_case(4, 40, 128, "float32", form="before"),
