@@ -1,6 +1,7 @@
 /*
- * libpql, operators around a student's memory (pql_student.h): the lookup of its tokens' embeddings, and the norms
- * before and after a block with the block's gate and residual sum; each with its gradient.
+ * libpql, operators around a student's memory (pql_student.h): the lookup of its tokens' embeddings, the norms
+ * before and after a block with the block's gate and residual sum, and the gated feed-forward block; each with its
+ * gradient.
  *
  * The conventions of pql.h and pql_student.h hold (return values, caller-owned memory, streams, threads, graphs,
  * error text of the context; PQL_F32 and PQL_BF16; sums, statistics and products held in fp32 or more).  Differences:
@@ -11,6 +12,8 @@
  *   Lengths     lengths[batch] ([device] int32, or NULL: all `steps`): tokens of each sequence that count, clamped to
  *               [0, steps].  What lies behind them is not read, outputs and gradients there are written as zeros, and
  *               it has no part in the gradients of weights.
+ *   Matrices    Weights are matrices of rows [out][in] (y_o = sum_i W_oi x_i) of the tokens' type, with a stride of their
+ *               own; their gradients have that form and type, and are written, not added to.
  *   Order       Every sum is taken in one order: equal calls give equal bits.
  *   Aliasing    Outputs must not overlap inputs or each other except where a call says so.
  */
@@ -50,7 +53,7 @@ int32_t pql_embed_backward(pql_ctx* ctx, const pql_embed_shape* shape, const int
 
 /* ---- norms, gate and residual sum around a block ------------------------------------------------ */
 
-#define PQL_ACT_NONE    0              /* x */
+#define PQL_ACT_NONE    0              /* x (a gated feed-forward block without an activation is bilinear) */
 #define PQL_ACT_SIGMOID 1              /* 1 / (1 + exp(-x)) */
 #define PQL_ACT_SILU    2              /* x / (1 + exp(-x)) */
 #define PQL_ACT_GELU    3              /* x (1 + erf(x / sqrt 2)) / 2 */
@@ -97,6 +100,43 @@ int64_t pql_residual_workspace_bytes(const pql_residual_shape* shape);
 int32_t pql_residual_backward(pql_ctx* ctx, const pql_residual_shape* shape, const pql_residual_input* input,
                               const pql_rows* sum_grad, const pql_rows* next_grad, const pql_residual_grad* grads,
                               void* workspace, void* stream);
+
+/* ---- the gated feed-forward block ---------------------------------------------------------------- */
+
+#define PQL_FFN_MAX_DIM 65536
+
+/* calls to ask a workspace's size for */
+#define PQL_FFN_FORWARD        0
+#define PQL_FFN_BACKWARD       1       /* with saved */
+#define PQL_FFN_BACKWARD_ALONE 2       /* without */
+
+/* batch * steps rows (below 2^30) of dim elements, `hidden` elements between the projections (both 1..PQL_FFN_MAX_DIM);
+ * dtype of tokens, weights and their gradients; act: PQL_ACT_*. */
+typedef struct { int32_t batch, steps, dim, hidden, dtype, act; } pql_ffn_shape;
+
+/* x: rows of dim; gate, up: hidden rows of dim; down: dim rows of hidden. */
+typedef struct {
+    pql_rows x, gate, up, down;
+    const int32_t* lengths;
+} pql_ffn_input;
+
+/* Gradients; any may have data NULL and is then not computed. */
+typedef struct { pql_rows x, gate, up, down; } pql_ffn_grad;
+
+/*     a = gate x_n,  b = up x_n,  m = act(a) b (element by element),  out_n = down m.
+ * saved: NULL, or [device] pql_ffn_saved_bytes(shape) bytes that keep a and b (fp32) for pql_ffn_backward.
+ * workspace: [device] pql_ffn_workspace_bytes(shape, PQL_FFN_FORWARD) bytes; both 256-byte aligned.  bf16: m is rounded to bf16 once
+ * as an operand of the second product; a and b are not. */
+int64_t pql_ffn_saved_bytes(const pql_ffn_shape* shape);
+int64_t pql_ffn_workspace_bytes(const pql_ffn_shape* shape, int32_t call);
+int32_t pql_ffn_forward(pql_ctx* ctx, const pql_ffn_shape* shape, const pql_ffn_input* input, const pql_rows* out,
+                        void* saved, void* workspace, void* stream);
+
+/* Gradient of a loss whose gradient with respect to out is out_grad.  saved: as left by pql_ffn_forward of the same
+ * shape and input, or NULL: a and b are worked out again.  workspace: pql_ffn_workspace_bytes(shape, PQL_FFN_BACKWARD or, without
+ * saved, PQL_FFN_BACKWARD_ALONE) bytes. */
+int32_t pql_ffn_backward(pql_ctx* ctx, const pql_ffn_shape* shape, const pql_ffn_input* input, const void* saved,
+                         const pql_rows* out_grad, const pql_ffn_grad* grads, void* workspace, void* stream);
 
 #ifdef __cplusplus
 }

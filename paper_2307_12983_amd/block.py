@@ -13,12 +13,14 @@ from . import student as S
 
 PQL_F32, PQL_BF16 = S.PQL_F32, S.PQL_BF16
 ACTIVATIONS = {"none": 0, "sigmoid": 1, "silu": 2, "gelu": 3, "relu": 4}
-PQL_RESIDUAL_MAX_DIM, PQL_RESIDUAL_MAX_GROUPS = 8192, 256
+PQL_RESIDUAL_MAX_DIM, PQL_RESIDUAL_MAX_GROUPS, PQL_FFN_MAX_DIM = 8192, 256, 65536
+FFN_FORWARD, FFN_BACKWARD, FFN_BACKWARD_ALONE = 0, 1, 2
 workspace = S.workspace
 
 # every symbol include/pql_block.h declares
 EXPORTS = ["pql_embed_forward", "pql_embed_workspace_bytes", "pql_embed_backward", "pql_residual_forward",
-           "pql_residual_workspace_bytes", "pql_residual_backward"]
+           "pql_residual_workspace_bytes", "pql_residual_backward", "pql_ffn_saved_bytes", "pql_ffn_workspace_bytes",
+           "pql_ffn_forward", "pql_ffn_backward"]
 
 
 class PqlRows(C.Structure):
@@ -42,6 +44,18 @@ class PqlResidualGrad(C.Structure):
     _fields_ = [(n, PqlRows) for n in ("x", "y", "gate")] + [(n, C.c_void_p) for n in ("post", "pre")]
 
 
+class PqlFfnShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "steps", "dim", "hidden", "dtype", "act")]
+
+
+class PqlFfnInput(C.Structure):
+    _fields_ = [(n, PqlRows) for n in ("x", "gate", "up", "down")] + [("lengths", C.c_void_p)]
+
+
+class PqlFfnGrad(C.Structure):
+    _fields_ = [(n, PqlRows) for n in ("x", "gate", "up", "down")]
+
+
 _ready = None
 
 
@@ -53,8 +67,8 @@ def load_library() -> C.CDLL:
     lib = S.load_library()
     P, I32, I64 = C.c_void_p, C.c_int32, C.c_int64
     rows = C.POINTER(PqlRows)
-    embed, residual = C.POINTER(PqlEmbedShape), C.POINTER(PqlResidualShape)
-    r_in, r_grad = C.POINTER(PqlResidualInput), C.POINTER(PqlResidualGrad)
+    embed, residual, ffn = C.POINTER(PqlEmbedShape), C.POINTER(PqlResidualShape), C.POINTER(PqlFfnShape)
+    r_in, r_grad, f_in, f_grad = (C.POINTER(x) for x in (PqlResidualInput, PqlResidualGrad, PqlFfnInput, PqlFfnGrad))
     sig = {
         "pql_embed_forward": (I32, [P, embed, P, P, rows, rows, P]),
         "pql_embed_workspace_bytes": (I64, [embed]),
@@ -62,6 +76,10 @@ def load_library() -> C.CDLL:
         "pql_residual_forward": (I32, [P, residual, r_in, rows, rows, P]),
         "pql_residual_workspace_bytes": (I64, [residual]),
         "pql_residual_backward": (I32, [P, residual, r_in, rows, rows, r_grad, P, P]),
+        "pql_ffn_saved_bytes": (I64, [ffn]),
+        "pql_ffn_workspace_bytes": (I64, [ffn, I32]),
+        "pql_ffn_forward": (I32, [P, ffn, f_in, rows, P, P, P]),
+        "pql_ffn_backward": (I32, [P, ffn, f_in, P, rows, f_grad, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -175,6 +193,44 @@ class ResidualGrad(_Residual):
         super().__init__(PqlResidualGrad, shape, x, y, gate, post, pre, "ResidualGrad")
 
 
+def ffn_shape(x, gate, act: str) -> PqlFfnShape:
+    """The shape of a call from its tokens [batch, steps, dim] and its gate's weights [hidden, dim]; act: of ACTIVATIONS."""
+    if x.dim() != 3 or gate.dim() != 2 or gate.shape[1] != x.shape[2] or gate.dtype != x.dtype:
+        raise ValueError("x: [batch, steps, dim], gate: [hidden, dim], of one type")
+    return PqlFfnShape(*x.shape, gate.shape[0], S.dtype_code(x), ACTIVATIONS[act])
+
+
+class _Ffn:
+    def __init__(self, struct, shape, x, gate, up, down, what):
+        n, dim, hidden, dtype = shape.batch * shape.steps, shape.dim, shape.hidden, shape.dtype
+        self.key = (n, dim, dtype)
+        self.tensors = (x, gate, up, down)
+        self.c = struct()
+        self.c.x = _rows(x, self.key, what + ": x")
+        self.c.gate = _rows(gate, (hidden, dim, dtype), what + ": gate")
+        self.c.up = _rows(up, (hidden, dim, dtype), what + ": up")
+        self.c.down = _rows(down, (dim, hidden, dtype), what + ": down")
+        self.shape = bytes(shape)
+        self.ref = C.byref(self.c)
+
+
+class FfnInput(_Ffn):
+    """What pql_ffn_forward reads: x [batch, steps, dim], gate and up [hidden, dim], down [dim, hidden], lengths int32 [batch]
+    or None."""
+
+    def __init__(self, shape, x, gate, up, down, lengths=None):
+        super().__init__(PqlFfnInput, shape, x, gate, up, down, "FfnInput")
+        self.lengths = lengths
+        self.c.lengths = _ints(lengths, shape.batch, "FfnInput: lengths")
+
+
+class FfnGrad(_Ffn):
+    """Where the gradients go; the shapes of the inputs, each may be None."""
+
+    def __init__(self, shape, x=None, gate=None, up=None, down=None):
+        super().__init__(PqlFfnGrad, shape, x, gate, up, down, "FfnGrad")
+
+
 class BlockContext(S.StudentContext):
     """A context whose methods are the entry points of a block beside those of ``StudentContext``."""
 
@@ -188,6 +244,12 @@ class BlockContext(S.StudentContext):
 
     def residual_workspace_bytes(self, shape: PqlResidualShape) -> int:
         return self.lib.pql_residual_workspace_bytes(C.byref(shape))
+
+    def ffn_saved_bytes(self, shape: PqlFfnShape) -> int:
+        return self.lib.pql_ffn_saved_bytes(C.byref(shape))
+
+    def ffn_workspace_bytes(self, shape: PqlFfnShape, call: int) -> int:
+        return self.lib.pql_ffn_workspace_bytes(C.byref(shape), call)
 
     # ---- device calls
     @staticmethod
@@ -220,3 +282,13 @@ class BlockContext(S.StudentContext):
         self._check(self.lib.pql_residual_backward(self.h, C.byref(shape), given.ref, _ref(sum_grad, given.key, "sum_grad"),
                                                    _ref(next_grad, given.key, "next_grad"), grads.ref, B._ptr(workspace),
                                                    B._stream(stream)))
+
+    def pql_ffn_forward(self, shape, given: FfnInput, out: Rows, saved, workspace, stream=None):
+        self._of(shape, given)
+        self._check(self.lib.pql_ffn_forward(self.h, C.byref(shape), given.ref, _ref(out, given.key, "out"), B._ptr(saved),
+                                             B._ptr(workspace), B._stream(stream)))
+
+    def pql_ffn_backward(self, shape, given: FfnInput, saved, out_grad: Rows, grads: FfnGrad, workspace, stream=None):
+        self._of(shape, given, grads)
+        self._check(self.lib.pql_ffn_backward(self.h, C.byref(shape), given.ref, B._ptr(saved), _ref(out_grad, given.key, "out_grad"),
+                                              grads.ref, B._ptr(workspace), B._stream(stream)))

@@ -1,0 +1,49 @@
+// Internal declarations of the gated feed-forward block (include/pql_block.h): its argument blocks and the launches of
+// its two families of kernels, products of row tiles (pql_ffn.hip) and of few rows (pql_ffn_rows.hip).
+#pragma once
+
+#include "pql_block_internal.h"
+
+namespace pql {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+// Results of matrix instructions must not be read for some cycles; behind branches the compiler's own waits have been found to
+// miss a short side, so they are waited for here before a branch can lie between.
+__device__ __forceinline__ void settle_products() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 3");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// x = h + m + l exactly: the nearest bf16 (8 bits), the next 8 bits of the rest, and what is left.  Values that are not finite
+// are their first term alone.
+struct Terms { float t[3]; };
+__device__ __forceinline__ Terms three_terms(float x) {
+    Terms s;
+    s.t[0] = (float)(bf16_t)x;
+    float r = x - s.t[0];
+    if (!(fabsf(s.t[0]) < __builtin_inff())) {                  // too large for a bf16, infinite or NaN
+        s.t[0] = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+        if (x != x) s.t[0] = x;
+        r = fabsf(x) < __builtin_inff() ? x - s.t[0] : 0.f;
+    }
+    s.t[1] = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
+    s.t[2] = r - s.t[1];
+    return s;
+}
+
+constexpr int FFN_FEW_ROWS = 64;                // calls of at most so many rows take the kernels for few rows
+
+struct FfnRowsArgs {
+    Live live;
+    int rows, dim, hidden, act;
+    const void *x, *gate, *up, *down;
+    int64_t x_stride, gate_stride, up_stride, down_stride;
+    void* m; int64_t m_stride;                  // [rows][m_stride], of the tokens' type
+    void* out; int64_t out_stride;
+};
+hipError_t ffn_rows_launch(const FfnRowsArgs& a, int32_t dtype, hipStream_t st);
+
+}  // namespace pql

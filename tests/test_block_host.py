@@ -305,3 +305,85 @@ def test_feed_forward_gradients_of_the_reference(act, lengths):
     loss = lambda: (O.only(w, real) * O.ffn(*t.values(), act, lengths)).sum()  # noqa: E731
     for k, g in O.ffn_grad(*t.values(), act, w, lengths).items():
         assert np.allclose(g, differences(loss, t[k]), atol=1e-7), k
+
+
+# ---- gated feed-forward block -----------------------------------------------------------------------------------------
+def ffn_shape(**kw):
+    d = dict(batch=2, steps=8, dim=64, hidden=64, dtype=0, act=2)
+    d.update(kw)
+    return K.PqlFfnShape(*[d[f] for f, _ in K.PqlFfnShape._fields_])
+
+
+def ffn_input(**kw):
+    i = K.PqlFfnInput(rows(), rows(), rows(), rows(), None)
+    for k, x in kw.items():
+        setattr(i, k, x)
+    return i
+
+
+def ffn_calls(ctx, s, i=None, out=rows(5 * P), g=None, saved=None, ws=P):
+    i, g = i or ffn_input(), g or K.PqlFfnGrad(*[rows()] * 4)
+    return (ctx.lib.pql_ffn_forward(ctx.h, r(s), r(i), r(out), saved, ws, None),
+            ctx.lib.pql_ffn_backward(ctx.h, r(s), r(i), saved, r(out), r(g), ws, None))
+
+
+@pytest.mark.parametrize("kw", [dict(batch=-1), dict(steps=-1), dict(batch=1 << 15, steps=1 << 15), dict(dim=0), dict(dim=65537), dict(hidden=0),
+                                dict(hidden=65537), dict(dtype=2), dict(act=-1), dict(act=5)])
+def test_feed_forward_blocks_refuse_bad_shapes(kw):
+    ctx, s = K.BlockContext(), ffn_shape(**kw)
+    assert ffn_calls(ctx, s) == (INVALID, INVALID) and ctx.ffn_saved_bytes(s) == INVALID
+    assert all(ctx.ffn_workspace_bytes(s, c) == INVALID for c in range(3))
+    assert "bad shape" in ctx.last_error()
+
+
+def test_feed_forward_blocks_refuse_bad_pointers_and_strides():
+    ctx, s = K.BlockContext(), ffn_shape()
+    both = lambda code, **kw: ffn_calls(ctx, s, **kw) == (code, code)  # noqa: E731
+    assert ffn_calls(ctx, None) == (NULL, NULL) and both(NULL, out=None) and both(NULL, out=rows(None)) and both(NULL, ws=None)
+    for n in ("x", "gate", "up", "down"):
+        assert both(NULL, i=ffn_input(**{n: rows(None)})) and both(ALIGNMENT, i=ffn_input(**{n: rows(P + 2)}))
+        assert both(INVALID, i=ffn_input(**{n: rows(P, -64)}))
+    assert both(ALIGNMENT, i=ffn_input(lengths=P + 2)) and both(ALIGNMENT, out=rows(P + 2)) and both(ALIGNMENT, ws=P + 128) and both(ALIGNMENT, saved=P + 16)
+    assert ffn_calls(ctx, s, out=rows(stride=63))[0] == INVALID
+    assert ctx.lib.pql_ffn_backward(ctx.h, r(s), r(ffn_input()), None, r(rows()), None, P, None) == NULL
+    for n in ("x", "gate", "up", "down"):
+        for bad, code in ((rows(P + 2), ALIGNMENT), (rows(P, 63), INVALID)):
+            g = K.PqlFfnGrad(*[rows()] * 4)
+            setattr(g, n, bad)
+            assert ffn_calls(ctx, s, g=g)[1] == code
+    assert ctx.ffn_workspace_bytes(s, 3) == INVALID and ctx.ffn_workspace_bytes(s, -1) == INVALID
+    none = rows(None, 0)
+    for kw in (dict(batch=0), dict(steps=0)):
+        e = ffn_shape(**kw)
+        assert ctx.lib.pql_ffn_forward(ctx.h, r(e), r(K.PqlFfnInput(none, none, none, none, None)), r(none), None, None, None) == 0
+
+
+def test_feed_forward_workspaces():
+    ctx = K.BlockContext()
+    for kw in (dict(), dict(batch=0), dict(dim=1, hidden=1), dict(dtype=1), dict(batch=1 << 14, dim=4096, hidden=65536)):
+        s = ffn_shape(**kw)
+        sizes = [ctx.ffn_workspace_bytes(s, c) for c in (K.FFN_FORWARD, K.FFN_BACKWARD, K.FFN_BACKWARD_ALONE)]
+        assert all(x >= 0 and x % 256 == 0 for x in sizes)
+        assert sizes[2] == sizes[1] + ctx.ffn_saved_bytes(s)
+
+
+def test_binding_refuses_matrices_that_do_not_fit():
+    import torch
+    z = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt)  # noqa: E731
+    ctx, x, w, down = K.BlockContext(), z(2, 3, 8), z(12, 8), z(8, 12)
+    s = K.ffn_shape(x, w, "silu")
+    good = dict(x=x, gate=w, up=w, down=down)
+    given = K.FfnInput(s, **good)
+    for bad in (dict(x=z(2, 3, 7)), dict(x=z(3, 3, 8)), dict(gate=z(11, 8)), dict(up=z(12, 8).bfloat16()), dict(down=w), dict(lengths=z(3, dt=torch.int32))):
+        with pytest.raises(ValueError):
+            K.FfnInput(s, **{**good, **bad})
+    other = K.ffn_shape(x, w, "gelu")
+    with pytest.raises(ValueError):
+        ctx.pql_ffn_forward(other, given, K.Rows(z(2, 3, 8)), None, None, 0)
+    with pytest.raises(ValueError):
+        ctx.pql_ffn_forward(s, given, K.Rows(z(2, 3, 7)), None, None, 0)
+    with pytest.raises(ValueError):
+        ctx.pql_ffn_backward(s, given, None, K.Rows(z(2, 3, 8)), K.FfnGrad(other), None, 0)
+    for bad in ((z(2, 8), w), (x, z(12, 7)), (x, w.bfloat16())):
+        with pytest.raises(ValueError):
+            K.ffn_shape(*bad, "silu")

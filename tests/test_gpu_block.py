@@ -91,7 +91,7 @@ def lengths_of(torch, lengths):
 
 
 def label(c):
-    return "-".join(str(v).replace(" ", "") for v in (c.values() if isinstance(c, dict) else c))
+    return "-".join(str(v).replace(" ", "")[:40] for v in (c.values() if isinstance(c, dict) else c))
 
 
 # ---- embeddings -----------------------------------------------------------------------------------------
@@ -369,3 +369,113 @@ def test_large_gates(env):
         close(call.forward()[0], call.want.sum, "sum", RES)
         for k, g in call.backward().items():
             close(g, want[k], k, 2 * RES)
+
+
+# ---- gated feed-forward block ----------------------------------------------------------------------------------
+FFN = [
+    # batch, steps, dim, hidden, dtype, act, layout, lengths
+    (1, 1, 1, 1, "float32", "silu", "dense", None),
+    (1, 1, 8, 8, "bfloat16", "silu", "dense", None),
+    (1, 1, 1024, 4096, "bfloat16", "silu", "dense", None),
+    (64, 1, 256, 1024, "float32", "gelu", "dense", None),
+    (3, 7, 203, 677, "float32", "silu", "offset", [7, 0, 3]),
+    (2, 16, 200, 72, "bfloat16", "relu", "wide", [20, -1]),
+    (5, 13, 100, 333, "bfloat16", "sigmoid", "offset", None),
+    (1, 65, 64, 64, "float32", "silu", "dense", None),
+    (1, 65, 64, 64, "bfloat16", "silu", "dense", None),
+    (3, 50, 128, 256, "bfloat16", "gelu", "dense", None),
+    (3, 50, 128, 256, "float32", "none", "dense", [50, 1, 0]),
+    (5, 33, 203, 677, "float32", "silu", "offset", [33, 0, 1, 12, 40]),
+    (5, 33, 203, 677, "bfloat16", "gelu", "offset", [33, 0, 1, 12, 40]),
+    (7, 40, 72, 136, "bfloat16", "silu", "wide", [0, 40, 39, 0, 0, 7, 40]),
+    (130, 1, 9, 5, "float32", "sigmoid", "dense", [1, 0] * 65),
+    (6, 64, 520, 1104, "float32", "silu", "wide", None),
+    (6, 64, 520, 1104, "bfloat16", "silu", "dense", None),
+    (2, 80, 64, 4096, "bfloat16", "silu", "dense", None),       # few tiles, a long contraction
+    (2, 80, 1024, 40, "float32", "gelu", "dense", [80, 33]),
+    (4, 512, 48, 48, "float32", "silu", "dense", None),         # many rows, small weights
+    (700, 3, 16, 24, "bfloat16", "relu", "dense", list(range(-350, 350))),
+    (3, 30, 64, 128, "float32", "silu", "dense", [0, 0, 0]),
+]
+
+
+class FfnCall:
+    def __init__(self, env, case, seed=0, by=1.0):
+        torch, K, ctx = self.env = env
+        n, t, d, f, dtype, act, layout, lengths = self.case = case
+        self.made = m = Made(env, seed, dtype, layout, lengths)
+        self.x, self.out_grad = m.normal(n, t, d, by=by), m.normal(n, t, d)
+        self.gate, self.up, self.down = m.normal(f, d, by=d ** -0.5), m.normal(f, d, by=d ** -0.5), m.normal(d, f, by=f ** -0.5)
+        m.lengths = None
+        self.lengths = lengths_of(torch, lengths)
+        self.shape = K.ffn_shape(self.x, self.gate, act)
+        self.given = K.FfnInput(self.shape, self.x, self.gate, self.up, self.down, self.lengths)
+        h = [np.nan_to_num(m.host(z)) for z in (self.x, self.gate, self.up, self.down)]
+        self.want = O.ffn(*h, act, lengths)
+        self.want_grad = O.ffn_grad(*h, act, np.nan_to_num(m.host(self.out_grad)), lengths)
+
+    def space(self, call):
+        torch, K, ctx = self.env
+        s = K.workspace(ctx.ffn_workspace_bytes(self.shape, call))
+        s.fill_(255)                                    # NaN wherever it is read before it is written
+        return s
+
+    def forward(self, keep):
+        torch, K, ctx = self.env
+        out = self.made.out(*self.x.shape)
+        saved = K.workspace(ctx.ffn_saved_bytes(self.shape)) if keep else None
+        if keep:
+            saved.fill_(255)
+        ctx.pql_ffn_forward(self.shape, self.given, K.Rows(out), saved, self.space(K.FFN_FORWARD))
+        return out, saved
+
+    def backward(self, saved, leave=()):
+        torch, K, ctx = self.env
+        g = {k: None if k in leave else self.made.out(*getattr(self, k).shape) for k in ("x", "gate", "up", "down")}
+        ctx.pql_ffn_backward(self.shape, self.given, saved, K.Rows(self.out_grad), K.FfnGrad(self.shape, **g),
+                             self.space(K.FFN_BACKWARD if saved is not None else K.FFN_BACKWARD_ALONE))
+        return g
+
+    def close(self, got, want, what):
+        k = max(self.case[0] * self.case[1], self.case[2], self.case[3])
+        bound = 3 * (k ** 0.5 + 10) * U
+        if self.case[4] == "float32":
+            return close(got, want, what, bound)
+        # what lies between two products, rounded to bf16: by 2^-8 / sqrt 3 of its norm at most
+        off, want = error_of(got, want)
+        bound, norm = bound + 2 * 2.0 ** -8 / 3 ** 0.5, np.linalg.norm(want)
+        assert np.linalg.norm(off) <= bound * norm, what
+        if norm:
+            assert np.max(off / np.maximum(norm / np.sqrt(want.size), np.abs(want))) <= 8 * bound, what
+
+
+@pytest.mark.parametrize("case", FFN, ids=label)
+def test_feed_forward_block(env, case):
+    call = FfnCall(env, case)
+    out, _ = call.forward(False)
+    call.close(out, call.want, "out")
+    kept, saved = call.forward(True)
+    call.close(kept, call.want, "out with saved")
+    again, _ = call.forward(True)
+    assert env[0].equal(kept, again)
+
+
+@pytest.mark.parametrize("case", FFN, ids=label)
+def test_gradients_of_the_feed_forward_block(env, case):
+    call = FfnCall(env, case, seed=1)
+    _, saved = call.forward(True)
+    first = call.backward(saved)
+    for k, g in first.items():
+        call.close(g, call.want_grad[k], k)
+    for k, g in call.backward(None).items():
+        assert env[0].equal(g, first[k]), k + " without saved"
+
+
+def test_feed_forward_gradients_that_are_not_asked_for(env):
+    call = FfnCall(env, (3, 50, 136, 260, "float32", "silu", "dense", [50, 20, 0]), seed=2)
+    _, saved = call.forward(True)
+    whole = call.backward(saved)
+    for leave in (("x",), ("gate",), ("down", "up"), ("x", "gate", "up", "down"), ("gate", "up", "down")):
+        for k, g in call.backward(saved, leave).items():
+            assert (g is None) == (k in leave)
+            assert g is None or env[0].equal(g, whole[k]), k
