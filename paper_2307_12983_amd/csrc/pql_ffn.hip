@@ -21,6 +21,7 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
 constexpr int BK = 64;                          // of the contraction a step: 128 bytes
+constexpr int BIG_TILES = 192;
 constexpr int NOWHERE = 0x7fffff00;             // an offset behind every buffer: reads give zeros
 
 // One operand: rows of a matrix, `plane` elements from one term's to the next.
@@ -62,7 +63,7 @@ template <int I, bool ALONG, int WAVES> struct Tile {
     static constexpr int BYTES = I * BK * 2, LOADS = BYTES / 1024 / WAVES, PER_ROW = ALONG ? 8 : I / 8, ROWS_A_LOAD = 64 / PER_ROW;
     static_assert(LOADS * 1024 * WAVES == BYTES, "whole loads for every wavefront");
     int at[LOADS];                              // byte offsets of this lane's granules from the tile's corner
-    int first_k[LOADS];                         // ALONG: the first element of the granule along the contraction
+    int first_k;                                // ALONG: the first element of its granules along the contraction
 
     __device__ __forceinline__ void init(int wave, int lane, int64_t stride) {
 #pragma unroll
@@ -70,21 +71,15 @@ template <int I, bool ALONG, int WAVES> struct Tile {
             const int row = (wave * LOADS + j) * ROWS_A_LOAD + lane / PER_ROW, place = lane % PER_ROW;
             const int g = place ^ (ALONG ? row & 7 : ((row & 3) << 1 | (row >> 3 & 1) << 3));
             at[j] = row * (int)stride * 2 + g * 16;
-            first_k[j] = ALONG ? g * 8 : 0;
         }
+        first_k = 8 * ((lane & 7) ^ (lane >> 3));
     }
-    // From the corner p; `rows` rows and `cols` columns of memory are there (rows are padded to whole granules).
-    __device__ __forceinline__ void load(char* lds, int wave, const bf16_t* p, int64_t stride, int rows, int cols) const {
-        const int bytes = rows > 0 ? ((rows - 1) * (int)stride + (cols + 7) / 8 * 8) * 2 : 0;
+    // From the corner p, where `bytes` bytes can be read; `left` elements of the contraction are.
+    __device__ __forceinline__ void load(char* lds, int wave, const bf16_t* p, int bytes, int left) const {
         const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00020000);
         char* to = lds + wave * LOADS * 1024;
-        if (!ALONG || cols >= BK) {
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) load_to_lds(rs, to + j * 1024, at[j]);
-        } else {                                // the contraction's last step
-#pragma unroll
-            for (int j = 0; j < LOADS; ++j) load_to_lds(rs, to + j * 1024, first_k[j] < cols ? at[j] : NOWHERE);
-        }
+        for (int j = 0; j < LOADS; ++j) load_to_lds(rs, to + j * 1024, !ALONG || first_k < left ? at[j] : NOWHERE);
     }
 };
 // A wavefront's operands of 16 x 16 x 32 products: lane l holds row l % 16 of 16, elements 8 (l / 16) .. + 7 of 32.
@@ -114,6 +109,21 @@ template <int I, bool ALONG> struct Reader {
     }
 };
 
+// Where an operand's next tile lies: `others` rows (or columns) of the result from `first` on, the contraction from `k` on.
+template <bool ALONG> struct Corner {
+    const bf16_t* p;
+    int64_t step;                               // to the next tile, in elements
+    int stride, fixed;                          // bytes of the other rows, or elements of the row
+    __device__ __forceinline__ void set(const FfnOperand& o, int first, int others, int k) {
+        stride = (int)o.stride;
+        p = o.p + (ALONG ? first * o.stride + k : k * o.stride + first);
+        step = ALONG ? BK : BK * o.stride;
+        fixed = ALONG ? (others - 1) * stride * 2 : (others + 7) / 8 * 16;
+    }
+    // Rows are padded to whole granules.
+    __device__ __forceinline__ int bytes(int left) const { return ALONG ? fixed + (left + 7) / 8 * 16 : (min(left, BK) - 1) * stride * 2 + fixed; }
+};
+
 // The terms whose products are taken, small ones first; with one term the last alone.
 __device__ __forceinline__ int term_a(int c) { return 0x001102 >> 4 * c & 15; }         // 2 0 1 1 0 0
 __device__ __forceinline__ int term_b(int c) { return 0x010120 >> 4 * c & 15; }         // 0 2 1 0 1 0
@@ -138,6 +148,12 @@ __device__ __forceinline__ Act act_of(int act, float x) {
         case PQL_ACT_RELU: return activate<PQL_ACT_RELU>(x);
         default: return activate<PQL_ACT_NONE>(x);
     }
+}
+
+// All but the last N of this wavefront's loads to LDS are done, and every other's; all have read what they asked for.
+template <int N> __device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // ---- products -------------------------------------------------------------------------------------------
@@ -175,43 +191,70 @@ __global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
     ra.init(wm * TM * 16, lane);
     rb.init(wn * TN * 16, lane);
 
-    const int combos = a.terms == 1 ? 1 : 6, ksteps = (K + BK - 1) / BK, all = ksteps * combos * a.segments;
-    const int per_split = (all + a.splits - 1) / a.splits, from = min(split * per_split, all), to = min(from + per_split, all);
-    // where the next step to load stands
-    int combo = from % combos, kstep = from / combos % max(ksteps, 1), seg = from / combos / max(ksteps, 1);
-    auto load = [&](int buffer) {
-        const int k = kstep * BK, pa = combos == 1 ? 0 : term_a(combo), pb = combos == 1 ? 0 : term_b(combo);
-        const FfnOperand &oa = pr.a[seg], &ob = pr.b[GATED ? half : seg];
-        const bf16_t* A = oa.p + pa * oa.plane + (A_ALONG ? m0 * oa.stride + k : k * oa.stride + m0);
-        const bf16_t* B = ob.p + pb * ob.plane + (B_ALONG ? n0 * ob.stride + k : k * ob.stride + n0);
-        ta.load(lds[buffer], wave, A, oa.stride, A_ALONG ? min(M - m0, BM) : min(K - k, BK), A_ALONG ? K - k : min(M - m0, BM));
-        tb.load(lds[buffer] + TA::BYTES, wave, B, ob.stride, B_ALONG ? min(N - n0, BN) : min(K - k, BK), B_ALONG ? K - k : min(N - n0, BN));
-        if (++combo == combos) {
-            combo = 0;
-            if (++kstep == ksteps) { kstep = 0; ++seg; }
-        }
+    constexpr int COMBOS = sizeof(E) == 4 ? 6 : 1;
+    const int ksteps = (K + BK - 1) / BK, all = ksteps * COMBOS * a.segments;
+    const int per_split = (all + a.splits - 1) / a.splits, from = min(split * per_split, all), n = min(from + per_split, all) - from;
+    // where the next tiles to load stand
+    int combo = from % COMBOS, seg = from / COMBOS / max(ksteps, 1), left = K - from / COMBOS % max(ksteps, 1) * BK;
+    Corner<A_ALONG> ca;
+    Corner<B_ALONG> cb;
+    const int64_t plane_a = pr.a[0].plane, plane_b = pr.b[0].plane;
+    auto corners = [&] {
+        ca.set(pr.a[seg], m0, min(M - m0, BM), K - left);
+        cb.set(pr.b[GATED ? half : seg], n0, min(N - n0, BN), K - left);
     };
+    corners();
+    auto load = [&](int buffer) {
+        const bf16_t *pa = ca.p, *pb = cb.p;
+        if constexpr (COMBOS > 1) { pa += term_a(combo) * plane_a; pb += term_b(combo) * plane_b; }
+        ta.load(lds[buffer], wave, pa, ca.bytes(left), left);
+        tb.load(lds[buffer] + TA::BYTES, wave, pb, cb.bytes(left), left);
+        if (COMBOS > 1 && ++combo < COMBOS) return;
+        combo = 0;
+        ca.p += ca.step;
+        cb.p += cb.step;
+        left -= BK;
+        if (left <= 0 && seg + 1 < a.segments) { ++seg; left = K; corners(); }
+    };
+    // Two sets of operands: while the products of one half of a step run, the other half's come from LDS, and in the middle of a step
+    // all wavefronts have done with its tiles, so that those of the step after next can be asked for.
     floatx4 acc[TM][TN] = {};
-    if (from < to) load(0);
-    for (int it = from; it < to; ++it) {
-        const int buffer = (it - from) & 1;
-        // this step's tiles are in LDS, all wavefronts' parts of them, and all have read the other buffer
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        if (it + 1 < to) load(buffer ^ 1);
+    bf16x8 fa[2][TM], fb[2][TN];
+    auto read = [&](int buffer, int kk) {
         const char *la = lds[buffer], *lb = la + TA::BYTES;
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            bf16x8 fa[TM], fb[TN];
+        for (int j = 0; j < TN; ++j) fb[kk][j] = rb.get(lb, j, kk);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fa[i] = ra.get(la, i, kk);
+        for (int i = 0; i < TM; ++i) fa[kk][i] = ra.get(la, i, kk);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto multiply = [&](int kk) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = rb.get(lb, j, kk);
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[kk][j], fa[kk][i], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (n > 0) {
+        load(0);
+        if (n > 1) {
+            load(1);
+            wait_loads<TA::LOADS + TB::LOADS>();
+        } else {
+            wait_loads<0>();
         }
+        read(0, 0);
+        for (int s = 0; s + 1 < n; ++s) {
+            read(s & 1, 1);
+            multiply(0);
+            wait_loads<0>();
+            read(s + 1 & 1, 0);
+            if (s + 2 < n) load(s & 1);
+            multiply(1);
+        }
+        read(n - 1 & 1, 1);
+        multiply(0);
+        multiply(1);
     }
     settle_products();
 
@@ -377,12 +420,13 @@ int up8(int x) { return (x + 7) / 8 * 8; }
 int tiles_of(int x, int b) { return (x + b - 1) / b; }
 
 // Parts of the contraction: where the tiles do not fill the card, as many as do, each of at least 8 steps.
-int ffn_splits(int tiles, int steps) {
-    int s = tiles > 0 ? 512 / tiles : 1;
+int ffn_splits(int tiles, int edge, int steps) {
+    int s = tiles > 0 ? (edge == 256 ? 256 : 512) / tiles : 1;
     if (s > steps / 8) s = steps / 8;
     return s < 1 ? 1 : s > 64 ? 64 : s;
 }
-constexpr int TILE_M = 128, TILE_N = 128;
+// Edge of the tiles of a product of `problems` m x n results: 256 where such tiles fill the card.
+int tile_edge(int64_t m, int n, int problems) { return (int64_t)tiles_of((int)m, 256) * tiles_of(n, 256) * problems >= BIG_TILES ? 256 : 128; }
 
 struct FfnPlan {
     int rows, terms, dim_p, hidden_p, out_splits, dx_splits, weight_splits;
@@ -409,12 +453,15 @@ FfnPlan ffn_plan(const pql_ffn_shape& s, int call) {
     p.down = planes(p.down_plane);
     p.m = planes(p.m_plane);
     const int combos = p.terms == 1 ? 1 : 6;
-    const int row_tiles = tiles_of(p.rows, TILE_M), dim_tiles = tiles_of(s.dim, TILE_N), hidden_tiles = tiles_of(s.hidden, TILE_N);
+    auto splits = [](int64_t m, int n, int problems, int steps) {
+        const int e = tile_edge(m, n, problems);
+        return ffn_splits(tiles_of((int)m, e) * tiles_of(n, e) * problems, e, steps);
+    };
     size_t part = 0;
     auto parts = [&](int splits, size_t floats) { if (splits > 1 && splits * floats * 4 > part) part = splits * floats * 4; };
-    p.out_splits = ffn_splits(row_tiles * dim_tiles, tiles_of(s.hidden, BK) * combos);
-    p.dx_splits = ffn_splits(row_tiles * dim_tiles, 2 * tiles_of(s.hidden, BK) * combos);
-    p.weight_splits = ffn_splits(3 * dim_tiles * hidden_tiles, tiles_of(p.rows, BK) * combos);
+    p.out_splits = splits(p.rows, s.dim, 1, tiles_of(s.hidden, BK) * combos);
+    p.dx_splits = splits(p.rows, s.dim, 1, 2 * tiles_of(s.hidden, BK) * combos);
+    p.weight_splits = splits(s.hidden, s.dim, 3, tiles_of(p.rows, BK) * combos);
     if (call == PQL_FFN_FORWARD) {
         parts(p.out_splits, (size_t)p.rows * s.dim);
     } else {
@@ -430,8 +477,9 @@ FfnPlan ffn_plan(const pql_ffn_shape& s, int call) {
     return p;
 }
 
-template <typename E, bool A_ALONG, bool B_ALONG, Epilogue EPI> void launch_product(const ProfSlot& ps, dim3 grid, const FfnArgs& a, hipStream_t st) {
-    PQL_LAUNCH(ps, (ffn_product_kernel<E, TILE_M, TILE_N, 2, 2, A_ALONG, B_ALONG, EPI>), grid, dim3(256), 0, st, a);
+template <typename E, bool A_ALONG, bool B_ALONG, Epilogue EPI> void launch_product(const ProfSlot& ps, int edge, dim3 grid, const FfnArgs& a, hipStream_t st) {
+    if (edge == 256) PQL_LAUNCH(ps, (ffn_product_kernel<E, 256, 256, 2, 4, A_ALONG, B_ALONG, EPI>), grid, dim3(512), 0, st, a);
+    else PQL_LAUNCH(ps, (ffn_product_kernel<E, 128, 128, 2, 2, A_ALONG, B_ALONG, EPI>), grid, dim3(256), 0, st, a);
 }
 
 struct FfnRun {
@@ -458,12 +506,18 @@ struct FfnRun {
         count = at<int>(p.count);
     }
     // The matrix as an operand: where it is, or as planes at `to`.
-    FfnOperand operand(const pql_rows& r, int rows, int cols, size_t to, int64_t plane, bool tokens) {
-        if (s.dtype == PQL_BF16 && !(tokens && map) && cols % 8 == 0 && rows_aligned(r, s.dtype) && r.stride >= cols && r.stride <= 1 << 20)
+    FfnOperand operand(const pql_rows& r, int rows, int cols, size_t to, int64_t plane, bool tokens, bool direct = true) {
+        if (direct && s.dtype == PQL_BF16 && !(tokens && map) && cols % 8 == 0 && rows_aligned(r, s.dtype) && r.stride >= cols && r.stride <= 1 << 20)
             return {(const bf16_t*)r.data, r.stride, 0};
         FfnCopy& c = copies.c[copies.n++];
         c = {r.data, r.stride, at<bf16_t>(to), plane, rows, cols, up8(cols), tokens ? map : nullptr};
         return {at<bf16_t>(to), up8(cols), plane};
+    }
+    // Both projections' weights, alike.
+    void projections(const pql_ffn_input& in, FfnOperand& gate, FfnOperand& up) {
+        const bool alike = in.gate.stride == in.up.stride && rows_aligned(in.gate, s.dtype) && rows_aligned(in.up, s.dtype);
+        gate = operand(in.gate, s.hidden, s.dim, p.gate, p.gate_plane, false, alike);
+        up = operand(in.up, s.hidden, s.dim, p.up, p.gate_plane, false, alike);
     }
     // Rows of the output that do not count.
     void clear(const pql_rows& out) {
@@ -495,24 +549,26 @@ struct FfnRun {
         a.hidden_p = p.hidden_p; a.m_plane = p.m_plane;
         return a;
     }
-    template <bool A_ALONG, bool B_ALONG, Epilogue EPI> void product(FfnArgs& a, int problems, int kid) {
+    // whole: problems of a full call, which the plan has counted with
+    template <bool A_ALONG, bool B_ALONG, Epilogue EPI> void product(FfnArgs& a, int problems, int whole, int kid) {
         if (e != hipSuccess) return;
         const FfnProblem& pr = a.prob[0];
-        const int each = (tiles_of(pr.m, TILE_M) * tiles_of(pr.n, EPI == EPI_GATED ? TILE_N / 2 : TILE_N) + 7) / 8;     // problems are alike or transposed
+        const int edge = EPI == EPI_GATED ? tile_edge(pr.m, 2 * pr.n, 1) : tile_edge(pr.m, pr.n, whole);
+        const int each = (tiles_of(pr.m, edge) * tiles_of(pr.n, EPI == EPI_GATED ? edge / 2 : edge) + 7) / 8;           // problems are alike or transposed
         const dim3 grid(each * 8, problems * a.splits);
         const ProfSlot ps = prof_slot();
-        if (s.dtype == PQL_F32) launch_product<float, A_ALONG, B_ALONG, EPI>(ps, grid, a, st);
-        else launch_product<bf16_t, A_ALONG, B_ALONG, EPI>(ps, grid, a, st);
+        if (s.dtype == PQL_F32) launch_product<float, A_ALONG, B_ALONG, EPI>(ps, edge, grid, a, st);
+        else launch_product<bf16_t, A_ALONG, B_ALONG, EPI>(ps, edge, grid, a, st);
         prof_commit(ps, kid, 2.0 * problems * (EPI == EPI_GATED ? 2 : 1) * a.segments * pr.m * pr.n * (double)a.k, 0.0);
         e = hipGetLastError();
     }
     // The product of rows or weights, in parts where that fills the card.
-    template <bool A_ALONG, bool B_ALONG> void result(FfnArgs& a, int problems, int splits) {
+    template <bool A_ALONG, bool B_ALONG> void result(FfnArgs& a, int problems, int whole, int splits) {
         a.splits = splits;
-        if (splits == 1) return product<A_ALONG, B_ALONG, EPI_OUT>(a, problems, KID_FFN_PRODUCT);
+        if (splits == 1) return product<A_ALONG, B_ALONG, EPI_OUT>(a, problems, whole, KID_FFN_PRODUCT);
         a.part = at<float>(p.part);
         a.part_stride = (int64_t)splits * a.prob[0].m * a.prob[0].n;
-        product<A_ALONG, B_ALONG, EPI_PART>(a, problems, KID_FFN_PRODUCT);
+        product<A_ALONG, B_ALONG, EPI_PART>(a, problems, whole, KID_FFN_PRODUCT);
         if (e != hipSuccess) return;
         const int64_t blocks = ((int64_t)a.prob[0].m * a.prob[0].n + 255) / 256;
         const ProfSlot ps = prof_slot();
@@ -527,7 +583,7 @@ struct FfnRun {
         a.prob[0] = {{x, x}, {gate, up}, p.rows, s.hidden, nullptr, 0};
         a.k = s.dim;
         a.va = va; a.vb = vb; a.m = m;
-        product<true, true, EPI_GATED>(a, 1, KID_FFN_GATED);
+        product<true, true, EPI_GATED>(a, 1, 1, KID_FFN_GATED);
     }
 };
 
@@ -581,8 +637,8 @@ int32_t pql_ffn_forward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input*
         FfnRun r{*s, p, (char*)workspace, st};
         r.pack(in->lengths);
         const FfnOperand x = r.operand(in->x, p.rows, s->dim, p.x, p.x_plane, true);
-        const FfnOperand gate = r.operand(in->gate, s->hidden, s->dim, p.gate, p.gate_plane, false);
-        const FfnOperand up = r.operand(in->up, s->hidden, s->dim, p.up, p.gate_plane, false);
+        FfnOperand gate, up;
+        r.projections(*in, gate, up);
         const FfnOperand down = r.operand(in->down, s->dim, s->hidden, p.down, p.down_plane, false);
         r.clear(*out);
         r.prepare();
@@ -593,7 +649,7 @@ int32_t pql_ffn_forward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input*
         const FfnOperand om{m, p.hidden_p, p.m_plane};
         a.prob[0] = {{om, om}, {down, down}, p.rows, s->dim, out->data, out->stride};
         a.k = s->hidden;
-        r.result<true, true>(a, 1, p.out_splits);
+        r.result<true, true>(a, 1, 1, p.out_splits);
         e = r.e;
     }
     return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_ffn_forward", e);
@@ -620,8 +676,8 @@ int32_t pql_ffn_backward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input
         r.pack(in->lengths);
         x = r.operand(in->x, rows, s->dim, p.x, p.x_plane, true);
         dout = r.operand(*out_grad, rows, s->dim, p.dout, p.x_plane, true);
-        const FfnOperand gate = r.operand(in->gate, s->hidden, s->dim, p.gate, p.gate_plane, false);
-        const FfnOperand up = r.operand(in->up, s->hidden, s->dim, p.up, p.gate_plane, false);
+        FfnOperand gate, up;
+        r.projections(*in, gate, up);
         r.prepare();
         r.copies.n = 0;
         const FfnOperand down = r.operand(in->down, s->dim, s->hidden, p.down, p.down_plane, false);
@@ -639,13 +695,13 @@ int32_t pql_ffn_backward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input
         a.prob[0] = {{dout, dout}, {down, down}, rows, s->hidden, nullptr, 0};
         a.k = s->dim;
         a.va = va; a.vb = vb; a.m = (bf16_t*)m.p; a.da = (bf16_t*)da.p; a.db = (bf16_t*)db.p;
-        r.product<true, false, EPI_BACK>(a, 1, KID_FFN_BACK);
+        r.product<true, false, EPI_BACK>(a, 1, 1, KID_FFN_BACK);
         if (g->x.data) {
             a = r.args();
             a.prob[0] = {{da, db}, {gate, up}, rows, s->dim, g->x.data, g->x.stride};
             a.k = s->hidden;
             a.segments = 2;
-            r.result<true, false>(a, 1, p.dx_splits);
+            r.result<true, false>(a, 1, 1, p.dx_splits);
         }
     }
     FfnArgs w = r.args();
@@ -656,7 +712,7 @@ int32_t pql_ffn_backward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input
     w.k = rows;
     w.count_is_k = 1;
     w.map = nullptr;
-    if (n > 0) r.result<false, false>(w, n, p.weight_splits);
+    if (n > 0) r.result<false, false>(w, n, 3, p.weight_splits);
     return r.e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_ffn_backward", r.e);
 }
 

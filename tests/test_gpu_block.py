@@ -471,6 +471,23 @@ def test_gradients_of_the_feed_forward_block(env, case):
         assert env[0].equal(g, first[k]), k + " without saved"
 
 
+def test_projections_of_different_layouts(env):
+    torch, K, ctx = env
+    for dtype in ("bfloat16", "float32"):
+        call = FfnCall(env, (3, 50, 136, 264, dtype, "silu", "dense", None), seed=3)
+        whole = call.forward(False)[0], call.backward(None)
+        for wide, at in ((160, 8), (144, 8), (139, 1)):
+            for which in ("gate", "up"):
+                big = torch.full((264, wide), float("nan"), dtype=call.x.dtype, device="cuda")
+                big[:, at:at + 136] = getattr(call, which)
+                weights = dict(gate=call.gate, up=call.up, down=call.down)
+                weights[which] = big[:, at:at + 136]
+                call.given = K.FfnInput(call.shape, call.x, **weights)
+                assert torch.equal(call.forward(False)[0], whole[0])
+                for k, g in call.backward(None).items():
+                    assert torch.equal(g, whole[1][k]), k
+
+
 def test_feed_forward_gradients_that_are_not_asked_for(env):
     call = FfnCall(env, (3, 50, 136, 260, "float32", "silu", "dense", [50, 20, 0]), seed=2)
     _, saved = call.forward(True)
