@@ -53,23 +53,54 @@ __device__ __forceinline__ uint4 narrow(const float* x, bf16_t) {
 }
 
 // ---- activations -----------------------------------------------------------------------------------
-// f(x) and f'(x).  Factors that vanish do so before they meet a large x, so that finite x give finite results.
+// exp(x): 2^t by the one instruction, t = x log2 e rounded, times what the rounding has left out, to first order: below 3 u
+// everywhere but for results that are no normal numbers.  Arguments are brought to where t is finite; NaN stays.
+__device__ __forceinline__ float exp_near(float x) {
+    x = x > 128.f ? 128.f : x < -128.f ? -128.f : x;
+    const float t = x * 1.44269504f, r = fmaf(x, 1.44269504f, -t) + x * 1.92596299e-8f;
+    return __builtin_amdgcn_exp2f(t) * fmaf(r, 0.693147181f, 1.f);
+}
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + exp_near(-x)); }
+// Half of erfc(-x / sqrt 2), the normal distribution's share below x.  fp32: by the library's erfc.  bf16: by the rational
+// approximation 7.1.26 of Abramowitz and Stegun, off by 1.5e-7 at most (its tail is not exact relative to itself, only to 1), a
+// quarter of the time: a step of 16384 rows took 131 us for its projections with erfc.
+__device__ __forceinline__ float share_below(float x, float) { return 0.5f * erfcf(-0.70710678f * x); }
+__device__ __forceinline__ float share_below(float x, bf16_t) {
+    const float z = fabsf(x) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.f));
+    const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float tail = 0.5f * p * __builtin_amdgcn_exp2f(-1.44269504f * z * z);
+    return x > 0.f ? 1.f - tail : tail;
+}
+// f(x) and f'(x).  Factors that vanish do so before they meet a large x, so that finite x give finite results.  E: the type of what
+// is worked out from them.
 struct Act { float f, d; };
-template <int ACT> __device__ __forceinline__ Act activate(float x) {
+template <int ACT, typename E> __device__ __forceinline__ Act activate(float x) {
     if constexpr (ACT == PQL_ACT_SIGMOID) {
-        const float s = 1.f / (1.f + expf(-x));
+        const float s = sigmoid(x);
         return {s, s * (1.f - s)};
     } else if constexpr (ACT == PQL_ACT_SILU) {
-        const float s = 1.f / (1.f + expf(-x));
+        const float s = sigmoid(x);
         return {x * s, s * (1.f + x * (1.f - s))};
     } else if constexpr (ACT == PQL_ACT_GELU) {
-        const float h = 0.5f * erfcf(-0.70710678f * x);
-        return {x * h, h + 0.39894228f * x * expf(-0.5f * x * x)};
+        const float h = share_below(x, E{});
+        return {x * h, h + x * (0.39894228f * __builtin_amdgcn_exp2f(-0.72134752f * x * x))};
     } else if constexpr (ACT == PQL_ACT_RELU) {
         return {x > 0.f ? x : (x != x ? x : 0.f), x > 0.f ? 1.f : 0.f};
     } else {
         return {x, 1.f};
     }
+}
+// The same for N values at a time, by the activation's number.
+template <typename E, int N> __device__ __forceinline__ void activate_all(int act, const float (&x)[N], float (&f)[N], float (&d)[N]) {
+#define PQL_ACTIVATE(A) case A: _Pragma("unroll") for (int i = 0; i < N; ++i) { const Act y = activate<A, E>(x[i]); f[i] = y.f; d[i] = y.d; } break;
+    switch (act) {
+        PQL_ACTIVATE(PQL_ACT_SIGMOID)
+        PQL_ACTIVATE(PQL_ACT_SILU)
+        PQL_ACTIVATE(PQL_ACT_GELU)
+        PQL_ACTIVATE(PQL_ACT_RELU)
+        PQL_ACTIVATE(PQL_ACT_NONE)
+    }
+#undef PQL_ACTIVATE
 }
 
 }  // namespace pql

@@ -128,27 +128,24 @@ template <bool ALONG> struct Corner {
 __device__ __forceinline__ int term_a(int c) { return 0x001102 >> 4 * c & 15; }         // 2 0 1 1 0 0
 __device__ __forceinline__ int term_b(int c) { return 0x010120 >> 4 * c & 15; }         // 0 2 1 0 1 0
 
-template <typename E> __device__ __forceinline__ void store_terms(bf16_t* p, int64_t plane, const float* x) {
+// Eight values as planes of terms.
+template <typename E> __device__ __forceinline__ void store_terms(bf16_t* p, int64_t plane, const float (&x)[8]) {
     if constexpr (sizeof(E) == 2) {
-        *(uint2*)p = make_uint2(narrow2(x[0], x[1]), narrow2(x[2], x[3]));
+        *(uint4*)p = narrow(x, bf16_t{});
     } else {
-        Terms t[4];
+        float t[3][8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) t[e] = three_terms(x[e]);
+        for (int e = 0; e < 8; ++e) {
+            const Terms s = three_terms(x[e]);
+            t[0][e] = s.t[0]; t[1][e] = s.t[1]; t[2][e] = s.t[2];
+        }
 #pragma unroll
-        for (int q = 0; q < 3; ++q) *(uint2*)(p + q * plane) = make_uint2(narrow2(t[0].t[q], t[1].t[q]), narrow2(t[2].t[q], t[3].t[q]));
+        for (int q = 0; q < 3; ++q) *(uint4*)(p + q * plane) = narrow(t[q], bf16_t{});
     }
 }
 
-__device__ __forceinline__ Act act_of(int act, float x) {
-    switch (act) {
-        case PQL_ACT_SIGMOID: return activate<PQL_ACT_SIGMOID>(x);
-        case PQL_ACT_SILU: return activate<PQL_ACT_SILU>(x);
-        case PQL_ACT_GELU: return activate<PQL_ACT_GELU>(x);
-        case PQL_ACT_RELU: return activate<PQL_ACT_RELU>(x);
-        default: return activate<PQL_ACT_NONE>(x);
-    }
-}
+template <typename E, Epilogue EPI> struct Output { using T = E; };
+template <typename E> struct Output<E, EPI_PART> { using T = float; };
 
 // All but the last N of this wavefront's loads to LDS are done, and every other's; all have read what they asked for.
 template <int N> __device__ __forceinline__ void wait_loads() {
@@ -164,7 +161,8 @@ __global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
     constexpr bool GATED = EPI == EPI_GATED;
     using TA = Tile<BM, A_ALONG, WAVES>;
     using TB = Tile<BN, B_ALONG, WAVES>;
-    __shared__ __align__(1024) char lds[2][TA::BYTES + TB::BYTES];
+    constexpr int LDS = TA::BYTES + TB::BYTES;
+    __shared__ __align__(1024) char lds[2][LDS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
     const int which = blockIdx.y / a.splits, split = blockIdx.y % a.splits;
     const FfnProblem& pr = a.prob[which];
@@ -258,69 +256,87 @@ __global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
     }
     settle_products();
 
-    // results: column l % 16 of a product is a row of C, its rows 4 (l / 16) .. + 3 are columns
-    const int row0 = m0 + wm * TM * 16 + (lane & 15), col4 = (lane >> 4) * 4;
+    // Results go through LDS, so that whole lines of memory are read and written: column l % 16 of a product is a row of C, its rows
+    // 4 (l / 16) .. + 3 are columns.  Granules of four columns lie at g ^ (row & 15).  Then eight columns of a row a thread.
+    constexpr int PASSES = BM * BN * 4 / (2 * LDS), PM = TM / PASSES, ROWS = BM / PASSES, NT = 64 * WAVES;
+    constexpr int UNITS = GATED ? BN / 16 : BN / 8, EACH = ROWS * UNITS / NT, AHEAD = EPI == EPI_BACK ? 2 : EACH;
+    static_assert(PASSES * PM == TM && EACH % AHEAD == 0, "whole passes");
+    char* stage = lds[0];
+    auto granule = [&](int row, int g) { return (floatx4*)(stage + row * BN * 4 + ((g ^ (row & 15)) << 4)); };
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int row = row0 + 16 * i;
-        if (row >= M) continue;
-        if constexpr (GATED) {
+    for (int pass = 0; pass < PASSES; ++pass) {
+        __syncthreads();
 #pragma unroll
-            for (int j = 0; j < TN / 2; ++j) {
-                const int col = n0 + wn * (TN * 8) + 16 * j + col4;
-                if (col >= a.hidden_p) continue;
-                const int64_t at = (int64_t)row * a.hidden_p + col;
-                const floatx4 va = acc[i][j], vb = acc[i][j + TN / 2];
-                if (a.va) { *(floatx4*)(a.va + at) = va; *(floatx4*)(a.vb + at) = vb; }
-                if (a.m) {
-                    float x[4];
+        for (int i = 0; i < PM; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = act_of(a.act, va[e]).f * vb[e];
-                    store_terms<E>(a.m + at, a.m_plane, x);
+            for (int j = 0; j < TN; ++j)
+                *granule((wm * PM + i) * 16 + (lane & 15), (wn * TN + j) * 4 + (lane >> 4)) = acc[pass * PM + i][j];
+        __syncthreads();
+#pragma unroll 1
+        for (int u0 = 0; u0 < EACH; u0 += AHEAD) {
+            floatx4 va[AHEAD][2], vb[AHEAD][2];
+            int row[AHEAD], col[AHEAD], local[AHEAD];
+            bool on[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int unit = (u0 + u) * NT + threadIdx.x;
+                local[u] = unit / UNITS;
+                row[u] = m0 + (local[u] / (PM * 16) * TM + pass * PM) * 16 + local[u] % (PM * 16);
+                col[u] = n0 + unit % UNITS * 8;
+                on[u] = row[u] < M && col[u] < (GATED || EPI == EPI_BACK ? a.hidden_p : N);
+                if constexpr (EPI == EPI_BACK) {
+                    const int64_t at = on[u] ? (int64_t)row[u] * a.hidden_p + col[u] : 0;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) { va[u][h] = *(const floatx4*)(a.va + at + 4 * h); vb[u][h] = *(const floatx4*)(a.vb + at + 4 * h); }
                 }
             }
-        } else if constexpr (EPI == EPI_BACK) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const int col = n0 + wn * TN * 16 + 16 * j + col4;
-                if (col >= a.hidden_p) continue;
-                const int64_t at = (int64_t)row * a.hidden_p + col;
-                const floatx4 va = *(const floatx4*)(a.va + at), vb = *(const floatx4*)(a.vb + at), dm = acc[i][j];
-                float x[4], y[4], z[4];
+            for (int u = 0; u < AHEAD; ++u) {
+                const int unit = ((u0 + u) * NT + threadIdx.x) % UNITS, g = GATED ? unit / 4 * 16 + unit % 4 * 2 : unit * 2;
+                float x[8];
+                *(floatx4*)x = *granule(local[u], g);
+                *(floatx4*)(x + 4) = *granule(local[u], g + 1);
+                const int64_t at = (int64_t)row[u] * a.hidden_p + col[u];
+                if constexpr (GATED) {
+                    float y[8], f[8], d[8];
+                    *(floatx4*)y = *granule(local[u], g + 8);
+                    *(floatx4*)(y + 4) = *granule(local[u], g + 9);
+                    if (!on[u]) continue;
+                    if (a.va) {
+                        *(floatx4*)(a.va + at) = *(floatx4*)x; *(floatx4*)(a.va + at + 4) = *(floatx4*)(x + 4);
+                        *(floatx4*)(a.vb + at) = *(floatx4*)y; *(floatx4*)(a.vb + at + 4) = *(floatx4*)(y + 4);
+                    }
+                    if (a.m) {
+                        activate_all<E>(a.act, x, f, d);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const Act f = act_of(a.act, va[e]);
-                    x[e] = dm[e] * vb[e] * f.d;
-                    y[e] = dm[e] * f.f;
-                    z[e] = f.f * vb[e];
-                }
-                store_terms<E>(a.da + at, a.m_plane, x);
-                store_terms<E>(a.db + at, a.m_plane, y);
-                store_terms<E>(a.m + at, a.m_plane, z);
-            }
-        } else if constexpr (EPI == EPI_PART) {
-            float* p = a.part + which * a.part_stride + ((int64_t)split * pr.m + row) * pr.n;
+                        for (int e = 0; e < 8; ++e) f[e] *= y[e];
+                        store_terms<E>(a.m + at, a.m_plane, f);
+                    }
+                } else if constexpr (EPI == EPI_BACK) {
+                    if (!on[u]) continue;
+                    float p[8], b[8], f[8], d[8];
+                    *(floatx4*)p = va[u][0]; *(floatx4*)(p + 4) = va[u][1];
+                    *(floatx4*)b = vb[u][0]; *(floatx4*)(b + 4) = vb[u][1];
+                    activate_all<E>(a.act, p, f, d);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const int col = n0 + wn * TN * 16 + 16 * j + col4;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (col + e < N) p[col + e] = acc[i][j][e];
-            }
-        } else {
-            E* p = (E*)pr.out + (int64_t)(a.map ? a.map[row] : row) * pr.out_stride;
-            const bool whole = ((uintptr_t)p & (4 * sizeof(E) - 1)) == 0;
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const int col = n0 + wn * TN * 16 + 16 * j + col4;
-                const floatx4 c = acc[i][j];
-                if (whole && col + 3 < N) {
-                    if constexpr (sizeof(E) == 4) *(floatx4*)(p + col) = c;
-                    else *(uint2*)(p + col) = make_uint2(narrow2(c[0], c[1]), narrow2(c[2], c[3]));
+                    for (int e = 0; e < 8; ++e) { p[e] = x[e] * b[e] * d[e]; x[e] *= f[e]; f[e] *= b[e]; }
+                    store_terms<E>(a.da + at, a.m_plane, p);
+                    store_terms<E>(a.db + at, a.m_plane, x);
+                    store_terms<E>(a.m + at, a.m_plane, f);
                 } else {
+                    if (!on[u]) continue;
+                    using O = typename Output<E, EPI>::T;
+                    O* p = EPI == EPI_PART ? (O*)(a.part + which * a.part_stride + ((int64_t)split * pr.m + row[u]) * pr.n)
+                                           : (O*)pr.out + (int64_t)(a.map ? a.map[row[u]] : row[u]) * pr.out_stride;
+                    p += col[u];
+                    if (((uintptr_t)p & 15) == 0 && col[u] + 8 <= N) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (col + e < N) p[col + e] = from_float<E>(c[e]);
+                        for (int h = 0; h < 8 / VEC_OF<O>; ++h) ((uint4*)p)[h] = narrow(x + h * VEC_OF<O>, O{});
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (col[u] + e < N) p[e] = from_float<O>(x[e]);
+                    }
                 }
             }
         }
@@ -406,7 +422,6 @@ template <typename E> __global__ void __launch_bounds__(256) ffn_prepare_kernel(
         }
         bf16_t* to = c.to + (int64_t)row * c.cols_p + col;
         store_terms<E>(to, c.plane, x);
-        store_terms<E>(to + 4, c.plane, x + 4);
     }
 }
 

@@ -105,15 +105,9 @@ template <typename E, int T, bool AL, bool GATED> __global__ void __launch_bound
         }
         if (n >= a.rows || out >= outputs) continue;
         if constexpr (GATED) {
-            float f = s[0];
-            switch (a.act) {
-                case PQL_ACT_SIGMOID: f = activate<PQL_ACT_SIGMOID>(f).f; break;
-                case PQL_ACT_SILU: f = activate<PQL_ACT_SILU>(f).f; break;
-                case PQL_ACT_GELU: f = activate<PQL_ACT_GELU>(f).f; break;
-                case PQL_ACT_RELU: f = activate<PQL_ACT_RELU>(f).f; break;
-                default: break;
-            }
-            ((E*)a.m)[(int64_t)n * a.m_stride + out] = from_float<E>(f * s[M - 1]);
+            float f[1] = {s[0]}, d[1];
+            activate_all<E>(a.act, f, f, d);
+            ((E*)a.m)[(int64_t)n * a.m_stride + out] = from_float<E>(f[0] * s[M - 1]);
         } else {
             ((E*)a.out)[(int64_t)n * a.out_stride + out] = from_float<E>(a.live(n) ? s[0] : 0.f);
         }

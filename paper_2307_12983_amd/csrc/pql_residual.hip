@@ -114,17 +114,6 @@ struct Sums {
     }
 };
 
-template <int N> __device__ __forceinline__ void open_gate(int act, float (&g)[N], float (&d)[N]) {
-#define PQL_GATE(A) case A: _Pragma("unroll") for (int i = 0; i < N; ++i) { const Act a = activate<A>(g[i]); g[i] = a.f; d[i] = a.d; } break;
-    switch (act) {
-        PQL_GATE(PQL_ACT_SIGMOID)
-        PQL_GATE(PQL_ACT_SILU)
-        PQL_GATE(PQL_ACT_GELU)
-        PQL_GATE(PQL_ACT_RELU)
-        PQL_GATE(PQL_ACT_NONE)
-    }
-#undef PQL_GATE
-}
 // The gate's elements (or its one value for the part), opened: g = act(gate), d = act'(gate); ones without a gate.
 template <typename E, bool AL> __device__ __forceinline__ void load_gate(const ResidualArgs& a, const Slice<E, AL>& s, unsigned row,
                                                                                int group, float (&g)[EPT], float (&d)[EPT]) {
@@ -136,13 +125,13 @@ template <typename E, bool AL> __device__ __forceinline__ void load_gate(const R
     const E* p = (const E*)a.gate + row * a.gate_stride;
     if (a.gate_part) {
         float one[1] = {s.on ? to_float(p[group]) : 0.f}, slope[1];
-        open_gate(a.gate_act, one, slope);
+        activate_all<E>(a.gate_act, one, one, slope);
 #pragma unroll
         for (int i = 0; i < EPT; ++i) { g[i] = one[0]; d[i] = slope[0]; }
         return;
     }
     s.load(p, g);
-    open_gate(a.gate_act, g, d);
+    activate_all<E>(a.gate_act, g, g, d);
 }
 
 // ---- forward ---------------------------------------------------------------------------------------
