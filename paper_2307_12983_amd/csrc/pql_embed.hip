@@ -3,9 +3,9 @@
 //
 // The lookup is bound by memory: a row of the output is one group of lanes, 16 bytes each.  The gradient sorts the
 // places (n, j) by token, keeping their order, so that every row of the table has one run of places whose sum is taken in
-// one order and written once.  Runs that lie within one chunk of the sorted list are summed by the wavefront that writes
-// the table's row (rows without a run get zeros there); of the others each chunk sums its part in the same launch, and
-// a second launch joins the parts in order.  That bounds the work on one run, however often its token occurs.
+// one order.  The table's rows are cleared while the list is sorted.  Then a wavefront works through a chunk of the list: runs
+// that begin and end in it are written, of the others it sums its part, and a last launch joins the parts in order.  That
+// bounds the work on one run, however often its token occurs.
 #include "pql_block_internal.h"
 
 namespace pql {
@@ -25,6 +25,8 @@ struct EmbedArgs {
     unsigned *key, *row, *key_to, *row_to;          // sorted tokens and the rows of their places; where a pass puts them
     unsigned *count, *total;                        // sort: [tiles][digits], [digits]
     int bits, shift, tiles;                         // of a digit
+    unsigned sort_blocks;                           // the first launch's blocks behind them clear the table
+    int elem;                                       // bytes of an element
     float* part;                                    // [chunks][2][dim]: a chunk's first and last run, where those cross its ends
 };
 
@@ -59,44 +61,73 @@ template <typename E, bool AL> __global__ void __launch_bounds__(256) embed_kern
 
 // ---- sort ----------------------------------------------------------------------------------------
 // A place's key: its token, or vocab for a place that counts for nothing.
-__device__ __forceinline__ unsigned key_of(const EmbedArgs& a, unsigned i, unsigned row) {
-    const int t = a.tokens[i];
-    return (unsigned)t < (unsigned)a.vocab && a.live(row) ? (unsigned)t : (unsigned)a.vocab;
+__device__ __forceinline__ unsigned row_of(const EmbedArgs& a, unsigned i) { return a.per_row == 1 ? i : i / a.per_row; }
+__device__ __forceinline__ unsigned key_of(const EmbedArgs& a, unsigned i) {
+    const unsigned t = min((unsigned)a.tokens[i], (unsigned)a.vocab);
+    return !a.live.lengths || a.live(row_of(a, i)) ? t : (unsigned)a.vocab;
+}
+// Zeros for rows of the table, by the blocks from sort_blocks on: 16 bytes a lane where rows allow it.
+__device__ __forceinline__ void clear_table(const EmbedArgs& a) {
+    const int64_t bytes = (int64_t)a.dim * a.elem, stride = a.table_stride * a.elem;
+    const int unit = ((uintptr_t)a.table | bytes | stride) % 16 == 0 ? 16 : a.elem, each = (int)(bytes / unit);
+    // lanes of a row, a power of two; rows of a workgroup
+    int lanes = 1;
+    while (lanes < (int)blockDim.x && lanes < each) lanes *= 2;
+    const int by = blockDim.x / lanes, lane = threadIdx.x & (lanes - 1);
+    for (int64_t v = (int64_t)(blockIdx.x - a.sort_blocks) * by + threadIdx.x / lanes; v < a.vocab; v += (int64_t)(gridDim.x - a.sort_blocks) * by) {
+        char* p = (char*)a.table + v * stride;
+        for (int i = lane; i < each; i += lanes) {
+            if (unit == 16) *(uint4*)(p + i * 16ll) = make_uint4(0, 0, 0, 0);
+            else if (unit == 4) *(unsigned*)(p + i * 4ll) = 0;
+            else *(unsigned short*)(p + i * 2ll) = 0;
+        }
+    }
 }
 
 // Few places (at most RANK_MAX): each one's place in the sorted list is the number of smaller keys and of equal ones before it.  All
-// pairs are compared, with the keys in LDS: one launch where a pass over a digit takes three.
-constexpr int RANK_MAX = 8192, RANK_WG = 256, RANK_LANES = 8;
-__global__ void __launch_bounds__(RANK_WG) embed_rank_kernel(EmbedArgs a) {
+// pairs are compared, with the keys in LDS: one launch where a pass over a digit takes three.  PACKED: key and place in one number
+// (vocab below 2^19), so that one comparison decides.
+constexpr int RANK_BITS = 13, RANK_MAX = 1 << RANK_BITS, RANK_WG = 256, RANK_LANES = 8;
+template <bool PACKED> __global__ void __launch_bounds__(RANK_WG) embed_rank_kernel(EmbedArgs a) {
     __shared__ uint4 keys4[RANK_MAX / 4];
     unsigned* keys = (unsigned*)keys4;
-    const unsigned padded = (a.n + 31) / 32 * 32;
-    for (unsigned i = threadIdx.x; i < padded; i += RANK_WG) keys[i] = i < a.n ? key_of(a, i, i / a.per_row) : ~0u;
+    if (blockIdx.x >= a.sort_blocks) return clear_table(a);
+    const unsigned padded = (a.n + 4 * RANK_LANES - 1) / (4 * RANK_LANES) * (4 * RANK_LANES);
+#pragma unroll 8
+    for (unsigned i = threadIdx.x; i < padded; i += RANK_WG) {
+        const unsigned k = i < a.n ? key_of(a, i) : ~0u;
+        keys[i] = PACKED && i < a.n ? k << RANK_BITS | i : k;
+    }
     __syncthreads();
     // lane l of a place's RANK_LANES compares it with every RANK_LANES-th four of keys
     const unsigned i = blockIdx.x * (RANK_WG / RANK_LANES) + threadIdx.x / RANK_LANES, lane = threadIdx.x % RANK_LANES;
     const unsigned mine = keys[min(i, a.n - 1)];
     unsigned before = 0;
+#pragma unroll 4
     for (unsigned q = lane; q < padded / 4; q += RANK_LANES) {
         const uint4 k = keys4[q];
-        // equal keys count where they stand before
-        const unsigned j = 4 * q;
-        before += (k.x < mine || (k.x == mine && j < i)) + (k.y < mine || (k.y == mine && j + 1 < i))
-                + (k.z < mine || (k.z == mine && j + 2 < i)) + (k.w < mine || (k.w == mine && j + 3 < i));
+        if constexpr (PACKED) {
+            before += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
+        } else {                                    // equal keys count where they stand before
+            const unsigned j = 4 * q;
+            before += (k.x < mine || (k.x == mine && j < i)) + (k.y < mine || (k.y == mine && j + 1 < i))
+                    + (k.z < mine || (k.z == mine && j + 2 < i)) + (k.w < mine || (k.w == mine && j + 3 < i));
+        }
     }
 #pragma unroll
     for (int d = 1; d < RANK_LANES; d <<= 1) before += __shfl_xor(before, d);
-    if (lane == 0 && i < a.n) { a.key_to[before] = mine; a.row_to[before] = i / a.per_row; }
+    if (lane == 0 && i < a.n) { a.key_to[before] = PACKED ? mine >> RANK_BITS : mine; a.row_to[before] = row_of(a, i); }
 }
 
 // More places: passes over digits of at most DIGIT_BITS bits, from the lowest, each keeping the order of equal digits.
 constexpr int DIGIT_BITS = 10, SORT_WG = 256, SORT_WAVES = SORT_WG / 64, TILE = 2048, PER_WAVE = TILE / SORT_WAVES;
 template <bool FIRST> __device__ __forceinline__ unsigned sort_key(const EmbedArgs& a, unsigned i, unsigned& row) {
-    if constexpr (FIRST) { row = i / a.per_row; return key_of(a, i, row); }
+    if constexpr (FIRST) { row = row_of(a, i); return key_of(a, i); }
     else { row = a.row[i]; return a.key[i]; }
 }
 template <bool FIRST> __global__ void __launch_bounds__(SORT_WG) embed_count_kernel(EmbedArgs a) {
     __shared__ unsigned count[1 << DIGIT_BITS];
+    if (FIRST && blockIdx.x >= a.sort_blocks) return clear_table(a);
     const int digits = 1 << a.bits;
     for (int d = threadIdx.x; d < digits; d += SORT_WG) count[d] = 0;
     __syncthreads();
@@ -199,54 +230,6 @@ template <bool FIRST> __global__ void __launch_bounds__(SORT_WG) embed_move_kern
 }
 
 // ---- sums over runs ------------------------------------------------------------------------------
-// Sum of out_grad's rows of places [from, to), for `count` columns from `col`: 64 lanes, NV granules of V columns each.
-template <typename E, bool AL, int NV> __device__ __forceinline__ void add_places(const EmbedArgs& a, unsigned from, unsigned to, int col, float* sum) {
-    constexpr int V = AL ? VEC_OF<E> : 1;
-    const int lane = threadIdx.x & 63;
-    for (unsigned i = from; i < to; i += 64) {
-        const unsigned row = a.row[min(i + lane, to - 1)];
-        const int here = (int)min(to - i, 64u);
-        constexpr int AHEAD = 4;
-        for (int j = 0; j < here; j += AHEAD) {
-            uint4 g[AHEAD][NV];
-            float one[AHEAD][NV];
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const unsigned n = __builtin_amdgcn_readlane(row, min(j + u, here - 1));
-                const E* p = (const E*)a.out + n * a.out_stride;
-#pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    const int at = min(col + (v * 64 + lane) * V, a.dim - V);
-                    if constexpr (AL) g[u][v] = *(const uint4*)(p + at); else one[u][v] = to_float(p[at]);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                if (j + u >= here) break;
-#pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    float x[V];
-                    if constexpr (AL) widen(g[u][v], x, E{}); else x[0] = one[u][v];
-#pragma unroll
-                    for (int k = 0; k < V; ++k) sum[v * V + k] += x[k];
-                }
-            }
-        }
-    }
-}
-template <typename E, bool AL, int NV> __device__ __forceinline__ void put_row(const EmbedArgs& a, unsigned v, int col, const float* sum) {
-    constexpr int V = AL ? VEC_OF<E> : 1;
-    E* p = (E*)a.table + v * a.table_stride;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int at = col + (i * 64 + (int)(threadIdx.x & 63)) * V;
-        if (at >= a.dim) continue;
-        float x[V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) x[k] = a.scale * sum[i * V + k];
-        if constexpr (AL) *(uint4*)(p + at) = narrow(x, E{}); else p[at] = from_float<E>(x[0]);
-    }
-}
 // The first place whose key is at least v, by 64 lanes at a time.
 __device__ __forceinline__ unsigned first_place(const EmbedArgs& a, unsigned v) {
     unsigned from = 0, to = a.n;                // the answer lies in [from, to]
@@ -263,41 +246,22 @@ __device__ __forceinline__ unsigned first_place(const EmbedArgs& a, unsigned v) 
     return from;
 }
 
-constexpr int ROWS_A_WAVE = 8;
-// Workgroups of the first `parts` blocks sum what crosses a chunk's ends, one wavefront a chunk; the others write the table's rows.
-template <typename E, bool AL, int NV> __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedArgs a, unsigned parts) {
-    constexpr int COLS = 64 * NV * (AL ? VEC_OF<E> : 1);
-    const int col = blockIdx.y * COLS, lane = threadIdx.x & 63;
-    if (blockIdx.x < parts) {
-        const unsigned c = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-        if (c >= (unsigned)a.chunks) return;
-        const unsigned from = c * a.chunk, to = min(from + a.chunk, a.n);
-        const unsigned first = a.key[from], last = a.key[to - 1];
-        const bool in = from > 0 && a.key[from - 1] == first && first < (unsigned)a.vocab;
-        const bool out = to < a.n && a.key[to] == last && last < (unsigned)a.vocab;
-        for (int slot = 0; slot < 2; ++slot) {
-            // a run that goes on at both ends belongs to the first slot alone
-            if (slot == 0 ? !in : !out || (in && first == last)) continue;
-            unsigned i = from, e = to;
-            if (slot == 0) {
-                for (e = from; e < to;) {                           // the run's end
-                    const uint64_t same = __ballot(e + lane < to && a.key[min(e + lane, to - 1)] == first);
-                    const int k = __popcll(same);
-                    e += k;
-                    if (k < 64) break;
-                }
-            } else {
-                for (i = to; i > from;) {                           // its beginning
-                    const uint64_t same = __ballot(i > from + lane && a.key[max(i, from + lane + 1) - lane - 1] == last);
-                    const int k = __popcll(same);
-                    i -= k;
-                    if (k < 64) break;
-                }
-            }
-            constexpr int V = AL ? VEC_OF<E> : 1;
-            float sum[NV * V] = {};
-            add_places<E, AL, NV>(a, i, e, col, sum);
-            float* p = a.part + ((int64_t)c * 2 + slot) * a.dim;
+// A wavefront a chunk, NV granules of V columns a lane.
+template <typename E, bool AL, int NV> __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedArgs a) {
+    constexpr int V = AL ? VEC_OF<E> : 1, AHEAD = 8;
+    const unsigned c = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (c >= (unsigned)a.chunks) return;
+    const int lane = threadIdx.x & 63, col = blockIdx.y * 64 * NV * V;
+    const unsigned from = c * a.chunk, to = min(from + a.chunk, a.n);
+    const unsigned previous = from > 0 ? a.key[from - 1] : ~0u, next = to < a.n ? a.key[to] : ~0u;
+    unsigned run = a.key[from];
+    float sum[NV * V] = {};
+    // the run's sum goes to its row of the table, or to the chunk's parts if it begins before it (slot 0) or goes on behind it
+    auto put = [&](bool last) {
+        if (run >= (unsigned)a.vocab) return;
+        const bool before = run == previous, behind = last && run == next;
+        if (before || behind) {
+            float* p = a.part + ((int64_t)c * 2 + (before ? 0 : 1)) * a.dim;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int at = col + (v * 64 + lane) * V;
@@ -305,44 +269,74 @@ template <typename E, bool AL, int NV> __global__ void __launch_bounds__(256) em
 #pragma unroll
                 for (int k = 0; k < V; ++k) p[at + k] = sum[v * V + k];
             }
+            return;
         }
-        return;
+        E* p = (E*)a.table + run * a.table_stride;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int at = col + (v * 64 + lane) * V;
+            if (at >= a.dim) continue;
+            float x[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) x[k] = a.scale * sum[v * V + k];
+            if constexpr (AL) *(uint4*)(p + at) = narrow(x, E{}); else p[at] = from_float<E>(x[0]);
+        }
+    };
+    bool end = false;
+    for (unsigned w = from; w < to && !end; w += 64) {
+        const unsigned keys = a.key[min(w + lane, to - 1)], rows = a.row[min(w + lane, to - 1)];
+        // places that count for nothing lie at the end
+        const int here = __popcll(__ballot(w + lane < to && keys < (unsigned)a.vocab));
+        end = here < 64;
+        for (int j = 0; j < here; j += AHEAD) {
+            uint4 g[AHEAD][NV];
+            float one[AHEAD][NV];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const unsigned n = __builtin_amdgcn_readlane(rows, min(j + u, here - 1));
+                const E* p = (const E*)a.out + n * a.out_stride;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const int at = min(col + (v * 64 + lane) * V, a.dim - V);
+                    if constexpr (AL) g[u][v] = *(const uint4*)(p + at); else one[u][v] = to_float(p[at]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (j + u >= here) break;
+                const unsigned k = __builtin_amdgcn_readlane(keys, j + u);
+                if (k != run) {
+                    put(false);
+                    run = k;
+#pragma unroll
+                    for (int i = 0; i < NV * V; ++i) sum[i] = 0.f;
+                }
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    float x[V];
+                    if constexpr (AL) widen(g[u][v], x, E{}); else x[0] = one[u][v];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum[v * V + i] += x[i];
+                }
+            }
+        }
     }
-    const unsigned v0 = __builtin_amdgcn_readfirstlane(((blockIdx.x - parts) * 4 + (threadIdx.x >> 6)) * ROWS_A_WAVE);
-    unsigned i = v0 < (unsigned)a.vocab ? first_place(a, v0) : a.n;
-    for (unsigned v = v0; v < v0 + ROWS_A_WAVE && v < (unsigned)a.vocab; ++v) {
-        // the run's end, or that it crosses a chunk's
-        const unsigned bound = min((i / a.chunk + 1) * a.chunk, a.n);
-        unsigned e = i;
-        while (e < bound) {
-            const uint64_t same = __ballot(e + lane < bound && a.key[min(e + lane, a.n - 1)] == v);
-            const int k = __popcll(same);
-            e += k;
-            if (k < 64) break;
-        }
-        if (e > i && e == bound && e < a.n && a.key[e] == v) {      // joined by another launch
-            i = first_place(a, v + 1);
-            continue;
-        }
-        float sum[NV * (AL ? VEC_OF<E> : 1)] = {};
-        add_places<E, AL, NV>(a, i, e, col, sum);
-        put_row<E, AL, NV>(a, v, col, sum);
-        i = e;
-    }
+    put(true);
 }
 // Runs that cross a chunk's end: the workgroup of the chunk where one begins adds its parts, a wavefront a quarter of them.
 template <typename E> __global__ void __launch_bounds__(256) embed_join_kernel(EmbedArgs a) {
     __shared__ float sums[4][256];
     const unsigned c = blockIdx.x, from = c * a.chunk, to = min(from + a.chunk, a.n);
     if (to >= a.n) return;
-    const unsigned v = a.key[to - 1];
-    if (v >= (unsigned)a.vocab || a.key[to] != v) return;
-    if (a.key[from] == v && from > 0 && a.key[from - 1] == v) return;           // begins before
+    const unsigned v = a.key[to - 1], next = a.key[to], first = a.key[from], previous = a.key[from > 0 ? from - 1 : 0];
+    if (v >= (unsigned)a.vocab || next != v) return;
+    if (first == v && from > 0 && previous == v) return;                        // begins before
     const unsigned lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const unsigned end = first_place(a, v + 1), last = (end - 1) / a.chunk, parts = last - c + 1;
     const unsigned each = (parts + 3) / 4, p0 = min(wave * each, parts), p1 = min(p0 + each, parts);
     const int col = blockIdx.y * 256 + lane * 4;
     float sum[4] = {};
+#pragma unroll 4
     for (unsigned p = p0; p < p1; ++p) {
         const float* x = a.part + ((int64_t)(c + p) * 2 + (p == 0)) * a.dim;
 #pragma unroll
@@ -373,8 +367,8 @@ struct EmbedPlan {
 EmbedPlan embed_plan(const pql_embed_shape& s) {
     EmbedPlan p{};
     p.n = embed_rows(s) * (unsigned)s.per_row;
-    p.chunk = 32;
-    while (p.chunk < 256 && p.n / p.chunk > 4096) p.chunk *= 2;
+    p.chunk = 16;
+    while (p.chunk < 256 && p.n / p.chunk > 8192) p.chunk *= 2;
     p.chunks = (int)((p.n + (unsigned)p.chunk - 1) / p.chunk);
     size_t o = 0;
     auto take = [&](size_t b) { const size_t at = o; o += to256(b); return at; };
@@ -399,6 +393,7 @@ EmbedArgs embed_args(const pql_embed_shape& s, const int32_t* tokens, const int3
     a.tokens = tokens;
     a.live = {lengths, (unsigned)s.steps};
     a.rows = embed_rows(s);
+    a.elem = elem_size(s.dtype);
     a.per_row = s.per_row; a.vocab = s.vocab; a.dim = s.dim; a.scale = s.scale;
     a.table = table.data; a.table_stride = table.stride;
     a.out = out.data; a.out_stride = out.stride;
@@ -418,23 +413,29 @@ template <typename E, bool AL> hipError_t embed_launch(const EmbedArgs& a, hipSt
     return hipGetLastError();
 }
 hipError_t embed_sort(EmbedArgs& a, const EmbedPlan& p, char* ws, hipStream_t st) {
+    // workgroups that clear the table: four 16-byte stores a lane, at most four workgroups a CU
+    const double stores = (double)a.vocab * a.dim * a.elem / (4 * 16 * 256);
+    const unsigned clear = stores < 1 ? 1 : stores < 1024 ? (unsigned)stores + 1 : 1024;
     unsigned* key[2] = {(unsigned*)(ws + p.key[0]), (unsigned*)(ws + p.key[1])};
     unsigned* row[2] = {(unsigned*)(ws + p.row[0]), (unsigned*)(ws + p.row[1])};
-    a.n = p.n;
     if (p.n <= RANK_MAX) {
         a.key_to = key[0]; a.row_to = row[0];
         const ProfSlot ps = prof_slot();
-        PQL_LAUNCH(ps, embed_rank_kernel, dim3((a.n * RANK_LANES + RANK_WG - 1) / RANK_WG), dim3(RANK_WG), 0, st, a);
+        a.sort_blocks = (a.n * RANK_LANES + RANK_WG - 1) / RANK_WG;
+        const dim3 grid(a.sort_blocks + clear);
+        if (a.vocab < 1 << (32 - RANK_BITS)) PQL_LAUNCH(ps, embed_rank_kernel<true>, grid, dim3(RANK_WG), 0, st, a);
+        else PQL_LAUNCH(ps, embed_rank_kernel<false>, grid, dim3(RANK_WG), 0, st, a);
         prof_commit(ps, KID_EMBED_SORT, 0.0, 12.0 * a.n);
     } else {
         a.count = (unsigned*)(ws + p.count); a.total = (unsigned*)(ws + p.total);
         a.bits = p.bits; a.tiles = p.tiles;
+        a.sort_blocks = p.tiles;
         int to = (p.passes - 1) & 1;                    // the last pass ends in the first pair
         for (int i = 0; i < p.passes; ++i, to ^= 1) {
             a.shift = i * p.bits;
             a.key = key[to ^ 1]; a.row = row[to ^ 1]; a.key_to = key[to]; a.row_to = row[to];
             ProfSlot ps = prof_slot();
-            if (i == 0) PQL_LAUNCH(ps, embed_count_kernel<true>, dim3(p.tiles), dim3(SORT_WG), 0, st, a);
+            if (i == 0) PQL_LAUNCH(ps, embed_count_kernel<true>, dim3(p.tiles + clear), dim3(SORT_WG), 0, st, a);
             else PQL_LAUNCH(ps, embed_count_kernel<false>, dim3(p.tiles), dim3(SORT_WG), 0, st, a);
             prof_commit(ps, KID_EMBED_SORT, 0.0, 4.0 * a.n);
             ps = prof_slot();
@@ -451,10 +452,9 @@ hipError_t embed_sort(EmbedArgs& a, const EmbedPlan& p, char* ws, hipStream_t st
 }
 template <typename E, bool AL, int NV> void embed_sum_launch(const EmbedArgs& a, hipStream_t st) {
     constexpr int COLS = 64 * NV * (AL ? VEC_OF<E> : 1);
-    const unsigned parts = a.chunks > 1 ? (a.chunks + 3) / 4 : 0, rows = ((unsigned)a.vocab + 4 * ROWS_A_WAVE - 1) / (4 * ROWS_A_WAVE);
     const ProfSlot ps = prof_slot();
-    PQL_LAUNCH(ps, (embed_sum_kernel<E, AL, NV>), dim3(parts + rows, (a.dim + COLS - 1) / COLS), dim3(256), 0, st, a, parts);
-    prof_commit(ps, KID_EMBED_SUM, 0.0, ((double)a.n + a.vocab) * a.dim * sizeof(E));
+    PQL_LAUNCH(ps, (embed_sum_kernel<E, AL, NV>), dim3((a.chunks + 3) / 4, (a.dim + COLS - 1) / COLS), dim3(256), 0, st, a);
+    prof_commit(ps, KID_EMBED_SUM, 0.0, (double)a.n * a.dim * sizeof(E));
 }
 template <typename E> hipError_t embed_back_launch(const EmbedArgs& a, bool aligned, hipStream_t st) {
     if (aligned) {
@@ -524,11 +524,12 @@ int32_t pql_embed_backward(pql_ctx* c, const pql_embed_shape* s, const int32_t* 
     EmbedArgs a = embed_args(*s, tokens, lengths, *table_grad, *out_grad);
     const hipStream_t st = (hipStream_t)stream;
     hipError_t e = hipSuccess;
-    if (p.n > 0) e = embed_sort(a, p, (char*)workspace, st);
+    a.n = p.n;
+    e = embed_sort(a, p, (char*)workspace, st);
     a.chunk = p.chunk; a.chunks = p.chunks;
     a.part = (float*)((char*)workspace + p.part);
     const bool al = embed_aligned(*s, *table_grad, *out_grad);
-    if (e == hipSuccess) e = s->dtype == PQL_F32 ? embed_back_launch<float>(a, al, st) : embed_back_launch<bf16_t>(a, al, st);
+    if (e == hipSuccess && p.n > 0) e = s->dtype == PQL_F32 ? embed_back_launch<float>(a, al, st) : embed_back_launch<bf16_t>(a, al, st);
     return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_embed_backward", e);
 }
 

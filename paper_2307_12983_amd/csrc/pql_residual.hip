@@ -39,15 +39,19 @@ template <typename E, bool AL> struct Slice {
     bool on;
     __device__ __forceinline__ int place(int i) const { return (i * lanes + lane) * V; }           // within the part, of granule i
     __device__ __forceinline__ bool there(int i) const { return on && place(i) < part; }
-    __device__ __forceinline__ void load(const E* p, float* x) const {
+    // As they come from memory, and as floats.
+    struct Raw { uint4 g[AL ? N : 1]; float x[AL ? 1 : N]; };
+    __device__ __forceinline__ void fetch(const E* p, Raw& r) const {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            if constexpr (AL) {
-                const uint4 g = there(i) ? *(const uint4*)(p + base + place(i)) : make_uint4(0, 0, 0, 0);
-                widen(g, x + i * V, E{});
-            } else {
-                x[i] = there(i) ? to_float(p[base + place(i)]) : 0.f;
-            }
+            if constexpr (AL) r.g[i] = there(i) ? *(const uint4*)(p + base + place(i)) : make_uint4(0, 0, 0, 0);
+            else r.x[i] = there(i) ? to_float(p[base + place(i)]) : 0.f;
+        }
+    }
+    __device__ __forceinline__ void open(const Raw& r, float* x) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (AL) widen(r.g[i], x + i * V, E{}); else x[i] = r.x[i];
         }
     }
     __device__ __forceinline__ void load_weights(const float* p, float* x) const {
@@ -114,25 +118,45 @@ struct Sums {
     }
 };
 
-// The gate's elements (or its one value for the part), opened: g = act(gate), d = act'(gate); ones without a gate.
-template <typename E, bool AL> __device__ __forceinline__ void load_gate(const ResidualArgs& a, const Slice<E, AL>& s, unsigned row,
-                                                                               int group, float (&g)[EPT], float (&d)[EPT]) {
-    if (!a.gate) {
-#pragma unroll
-        for (int i = 0; i < EPT; ++i) { g[i] = 1.f; d[i] = 0.f; }
-        return;
+// What is read of one row, asked for while the row before is worked on.
+template <typename E, bool AL, bool BACK> struct Row {
+    using S = Slice<E, AL>;
+    typename S::Raw x, y, gate, sum, next;
+    float one;                              // the gate's value for the part
+    unsigned row;
+    bool here, live;
+    __device__ __forceinline__ void fetch(const ResidualArgs& a, S s, unsigned first, int slot, int slots, int group) {
+        row = first + slot;
+        here = first < a.rows && slot < slots && row < a.rows;
+        live = here && a.live(row);
+        s.on = live;
+        if (a.x) s.fetch((const E*)a.x + row * a.x_stride, x);
+        if (a.y) s.fetch((const E*)a.y + row * a.y_stride, y);
+        if (a.gate) {
+            if (a.gate_part) one = live ? to_float(((const E*)a.gate)[row * a.gate_stride + group]) : 0.f;
+            else s.fetch((const E*)a.gate + row * a.gate_stride, gate);
+        }
+        if constexpr (BACK) {
+            if (a.sum) s.fetch((const E*)a.sum + row * a.sum_stride, sum);
+            if (a.next) s.fetch((const E*)a.next + row * a.next_stride, next);
+        }
     }
-    const E* p = (const E*)a.gate + row * a.gate_stride;
-    if (a.gate_part) {
-        float one[1] = {s.on ? to_float(p[group]) : 0.f}, slope[1];
-        activate_all<E>(a.gate_act, one, one, slope);
+    // The gate opened: g = act(gate), d = act'(gate); ones without a gate.
+    __device__ __forceinline__ void open_gate(const ResidualArgs& a, const S& s, float (&g)[EPT], float (&d)[EPT]) const {
+        if (!a.gate) {
 #pragma unroll
-        for (int i = 0; i < EPT; ++i) { g[i] = one[0]; d[i] = slope[0]; }
-        return;
+            for (int i = 0; i < EPT; ++i) { g[i] = 1.f; d[i] = 0.f; }
+        } else if (a.gate_part) {
+            float f[1] = {one}, slope[1];
+            activate_all<E>(a.gate_act, f, f, slope);
+#pragma unroll
+            for (int i = 0; i < EPT; ++i) { g[i] = f[0]; d[i] = slope[0]; }
+        } else {
+            s.open(gate, g);
+            activate_all<E>(a.gate_act, g, g, d);
+        }
     }
-    s.load(p, g);
-    activate_all<E>(a.gate_act, g, g, d);
-}
+};
 
 // ---- forward ---------------------------------------------------------------------------------------
 template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT) residual_kernel(ResidualArgs a) {
@@ -144,21 +168,25 @@ template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT) res
     float post[EPT], pre[EPT];
     s.on = slot < slots;
     if constexpr (KEEP) { s.load_weights(a.post, post); s.load_weights(a.pre, pre); }
+    Row<E, AL, false> now, after;
+    after.fetch(a, s, blockIdx.x * slots, slot, slots, group);
     for (unsigned first = blockIdx.x * slots; first < a.rows; first += gridDim.x * slots) {
-        const unsigned row = first + slot;
-        const bool here = slot < slots && row < a.rows, live = here && a.live(row);
+        now = after;
+        after.fetch(a, s, first + gridDim.x * slots, slot, slots, group);
+        const unsigned row = now.row;
+        const bool here = now.here, live = now.live;
         s.on = live;
         if constexpr (!KEEP) { s.load_weights(a.post, post); s.load_weights(a.pre, pre); }
         float h[EPT] = {};
         if (a.x) {
-            s.load((const E*)a.x + row * a.x_stride, h);
+            s.open(now.x, h);
 #pragma unroll
             for (int i = 0; i < EPT; ++i) h[i] *= a.scale_x;
         }
         if (a.y) {
             float y[EPT], g[EPT], d[EPT];
-            s.load((const E*)a.y + row * a.y_stride, y);
-            load_gate(a, s, row, group, g, d);
+            s.open(now.y, y);
+            now.open_gate(a, s, g, d);
             float r = 1.f;
             if (a.eps_post > 0.f) {
                 float q[1] = {};
@@ -203,22 +231,26 @@ template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT) res
     s.on = slot < slots;
     if constexpr (KEEP) { s.load_weights(a.post, post); s.load_weights(a.pre, pre); }
     const float over_part = 1.f / a.part, over_dim = 1.f / a.dim;
+    Row<E, AL, true> now, after;
+    after.fetch(a, s, blockIdx.x * slots, slot, slots, group);
     for (unsigned first = blockIdx.x * slots; first < a.rows; first += gridDim.x * slots) {
-        const unsigned row = first + slot;
-        const bool here = slot < slots && row < a.rows;
-        s.on = here && a.live(row);
+        now = after;
+        after.fetch(a, s, first + gridDim.x * slots, slot, slots, group);
+        const unsigned row = now.row;
+        const bool here = now.here;
+        s.on = now.live;
         if constexpr (!KEEP) { s.load_weights(a.post, post); s.load_weights(a.pre, pre); }
         float y[EPT] = {}, g[EPT], slope[EPT], h[EPT] = {}, dh[EPT] = {};
         float r = 1.f;
         if (a.x) {
-            s.load((const E*)a.x + row * a.x_stride, h);
+            s.open(now.x, h);
 #pragma unroll
             for (int i = 0; i < EPT; ++i) h[i] *= a.scale_x;
         }
-        if (a.sum) s.load((const E*)a.sum + row * a.sum_stride, dh);
+        if (a.sum) s.open(now.sum, dh);
         if (a.y) {
-            s.load((const E*)a.y + row * a.y_stride, y);
-            load_gate(a, s, row, group, g, slope);
+            s.open(now.y, y);
+            now.open_gate(a, s, g, slope);
             if (a.eps_post > 0.f) {
                 float q[1] = {};
 #pragma unroll
@@ -234,7 +266,7 @@ template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT) res
         }
         if (a.next) {
             float du[EPT];
-            s.load((const E*)a.next + row * a.next_stride, du);
+            s.open(now.next, du);
             float f = 1.f, c = 0.f;
             if (a.eps_pre > 0.f) {
                 float q[2] = {};
@@ -316,21 +348,29 @@ template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT) res
         }
     }
 }
-// Sums over the workgroups: 64 columns a workgroup, 16 stretches of it.
+// Sums over the workgroups, in order within 32 stretches of it and over those: 64 columns a workgroup, half a wavefront a stretch.
 __global__ void __launch_bounds__(1024) residual_join_kernel(const float* partial, int parts, int dim, float* dpost, float* dpre) {
-    __shared__ float sums[16][64];
-    const int col = blockIdx.x * 64 + (threadIdx.x & 63), stretch = threadIdx.x >> 6, each = (parts + 15) / 16;
-    const int from = stretch * each, to = min(from + each, parts);
-    float s = 0.f;
-    if (col < 2 * dim)
-        for (int p = from; p < to; ++p) s += partial[(int64_t)p * 2 * dim + col];
-    sums[stretch][threadIdx.x & 63] = s;
+    __shared__ float2 sums[32][32];
+    const int stretch = threadIdx.x >> 5, each = (parts + 31) / 32, from = stretch * each, to = min(from + each, parts);
+    const int col = blockIdx.x * 64 + (threadIdx.x & 31) * 2;           // 2 * dim columns: pairs are whole
+    float2 s = {0.f, 0.f};
+    if (col < 2 * dim) {
+#pragma unroll 8
+        for (int p = from; p < to; ++p) {
+            const float2 x = *(const float2*)(partial + (int64_t)p * 2 * dim + col);
+            s.x += x.x;
+            s.y += x.y;
+        }
+    }
+    sums[stretch][threadIdx.x & 31] = s;
     __syncthreads();
-    if (stretch || col >= 2 * dim) return;
-    s = 0.f;
-    for (int i = 0; i < 16; ++i) s += sums[i][threadIdx.x];
-    if (col < dim) { if (dpost) dpost[col] = s; }
-    else if (dpre) dpre[col - dim] = s;
+    const int mine = blockIdx.x * 64 + threadIdx.x;
+    if (threadIdx.x >= 64 || mine >= 2 * dim) return;
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) t += ((const float*)sums[i])[threadIdx.x];
+    if (mine < dim) { if (dpost) dpost[mine] = t; }
+    else if (dpre) dpre[mine - dim] = t;
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -358,7 +398,7 @@ ResidualPlan residual_plan(const pql_residual_shape& s, bool back) {
     p.threads = threads <= 256 ? 256 : (threads + 63) / 64 * 64;
     p.slots = p.threads / threads;
     const unsigned rows = residual_rows(s), all = (rows + p.slots - 1) / p.slots;
-    const unsigned most = (back ? 1024u : 2048u) * 256u / p.threads;
+    const unsigned most = (back ? 512u : 1024u) * 256u / p.threads;
     p.grid = all < most ? all : most;
     return p;
 }
