@@ -17,10 +17,12 @@ namespace pql {
 namespace {
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
-constexpr int BK = 64;                          // of the contraction a step: 128 bytes
+// Terms of a value, elements of the contraction a step, steps in LDS at a time.
+template <typename E> struct Mode;
+template <> struct Mode<bf16_t> { static constexpr int TERMS = 1, BK = 64, STAGES = 2; };
+template <> struct Mode<float> { static constexpr int TERMS = 3, BK = 32, STAGES = 3; };
 constexpr int BIG_TILES = 192;
 constexpr int NOWHERE = 0x7fffff00;             // an offset behind every buffer: reads give zeros
 
@@ -32,7 +34,7 @@ enum Epilogue : int { EPI_GATED, EPI_BACK, EPI_OUT, EPI_PART };
 
 struct FfnArgs {
     FfnProblem prob[3];
-    int k, segments, terms;                     // length of the contraction, of each of `segments` pairs of operands; terms a value
+    int k, segments;                            // length of the contraction, of each of `segments` pairs of operands
     const int* count;                           // rows that count, NULL: all
     int count_is_k;                             // whether they are the contraction or the rows of the result
     int splits;                                 // parts of the contraction
@@ -47,20 +49,33 @@ struct FfnArgs {
     int64_t m_plane;
 };
 
-// 16 bytes of every lane from the buffer to LDS, lane after lane.  (The host's pass knows no loads of that size.)
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rs, char* lds, int offset) {
+// 16 bytes of every lane from the buffer to LDS, lane after lane; `lds` and the buffer are the wavefront's.  In text, so that the
+// compiler does not wait for it before each transposing read of other parts of LDS, as it does behind its own instruction (there is no
+// result in registers: what is in flight is counted and waited for below).
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uintx4 buffer_of(const void* p, int bytes) {
+    const uint64_t at = (uint64_t)p;
+    return uintx4{(unsigned)at, (unsigned)(at >> 32) & 0xffffu, (unsigned)bytes, 0x00020000u};
+}
+__device__ __forceinline__ void load_to_lds(uintx4 buffer, unsigned lds, int offset) {
 #ifdef __HIP_DEVICE_COMPILE__
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)lds, 16, offset, 0, 0, 0);
+    // m0 is the compiler's own and kept; five cycles lie between an SGPR that a vector instruction has written and its use here
+    unsigned m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(lds), "v"(offset), "s"(buffer) : "memory");
 #endif
 }
+__device__ __forceinline__ unsigned lds_address(const char* p) { return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 
 // ---- tiles in LDS -------------------------------------------------------------------------------------
-// ALONG (the contraction runs along the rows in memory): [I][64 elements], 8 granules of 16 bytes a row, granule g of row i at
-// place g ^ (i & 7).  A wavefront's load brings 8 rows.
-// ACROSS: [64][I elements], I / 8 granules a row k, granule g at place g ^ f(k), f(k) = (k & 3) << 1 | (k >> 3 & 1) << 3: the
-// transposing read of 16 lanes takes 32 bytes from each of four rows.
-template <int I, bool ALONG, int WAVES> struct Tile {
-    static constexpr int BYTES = I * BK * 2, LOADS = BYTES / 1024 / WAVES, PER_ROW = ALONG ? 8 : I / 8, ROWS_A_LOAD = 64 / PER_ROW;
+// ALONG (the contraction runs along the rows in memory): [I][BK elements], BK / 8 granules of 16 bytes a row, granule g of row i at
+// place g ^ along(i).  The reads take one granule from each of 16 rows.
+// ACROSS: [BK][I elements], I / 8 granules a row k, granule g at place g ^ across(k): the transposing read of 16 lanes takes 32 bytes
+// from each of four rows.
+template <int BK> __device__ __forceinline__ int along(int i) { return BK == 64 ? i & 7 : (i >> 1 & 3) ^ (i >> 3 & 1); }
+__device__ __forceinline__ int across(int k) { return (k & 3) << 1 | (k >> 3 & 1) << 3; }
+template <int I, bool ALONG, int WAVES, int BK> struct Tile {
+    static constexpr int BYTES = I * BK * 2, LOADS = BYTES / 1024 / WAVES, PER_ROW = ALONG ? BK / 8 : I / 8, ROWS_A_LOAD = 64 / PER_ROW;
     static_assert(LOADS * 1024 * WAVES == BYTES, "whole loads for every wavefront");
     int at[LOADS];                              // byte offsets of this lane's granules from the tile's corner
     int first_k;                                // ALONG: the first element of its granules along the contraction
@@ -69,38 +84,38 @@ template <int I, bool ALONG, int WAVES> struct Tile {
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int row = (wave * LOADS + j) * ROWS_A_LOAD + lane / PER_ROW, place = lane % PER_ROW;
-            const int g = place ^ (ALONG ? row & 7 : ((row & 3) << 1 | (row >> 3 & 1) << 3));
+            const int g = place ^ (ALONG ? along<BK>(row) : across(row));
             at[j] = row * (int)stride * 2 + g * 16;
         }
-        first_k = 8 * ((lane & 7) ^ (lane >> 3));
+        first_k = 8 * ((lane % PER_ROW) ^ along<BK>(lane / PER_ROW));          // the same for all loads: of 8 or 16 rows each
     }
     // From the corner p, where `bytes` bytes can be read; `left` elements of the contraction are.
     __device__ __forceinline__ void load(char* lds, int wave, const bf16_t* p, int bytes, int left) const {
-        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00020000);
-        char* to = lds + wave * LOADS * 1024;
+        const uintx4 rs = buffer_of(p, bytes);
+        const unsigned to = __builtin_amdgcn_readfirstlane(lds_address(lds)) + wave * LOADS * 1024;
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) load_to_lds(rs, to + j * 1024, !ALONG || first_k < left ? at[j] : NOWHERE);
     }
 };
 // A wavefront's operands of 16 x 16 x 32 products: lane l holds row l % 16 of 16, elements 8 (l / 16) .. + 7 of 32.
-template <int I, bool ALONG> struct Reader {
-    int at[ALONG ? 2 : 4];
-    __device__ __forceinline__ void init(int first, int lane) {         // first: the wavefront's first row, a multiple of 64
+template <int I, bool ALONG, int BK> struct Reader {
+    int at[ALONG ? BK / 32 : 4];
+    __device__ __forceinline__ void init(int first, int lane) {         // first: the wavefront's first row, a multiple of 32
         if constexpr (ALONG) {
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) at[kk] = (first + (lane & 15)) * 128 + (((kk * 4 + (lane >> 4)) ^ (lane & 7)) * 16);
+            for (int kk = 0; kk < BK / 32; ++kk) at[kk] = (first + (lane & 15)) * BK * 2 + (((kk * 4 + (lane >> 4)) ^ along<BK>(lane & 15)) * 16);
         } else {
-            const int k = 8 * (lane >> 4) + ((lane & 15) >> 2), f = (k & 3) << 1 | (k >> 3 & 1) << 3;
+            const int k = 8 * (lane >> 4) + ((lane & 15) >> 2);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) at[i] = k * I * 2 + (((first >> 3) + 2 * i + ((lane & 3) >> 1)) ^ f) * 16 + (lane & 1) * 8;
+            for (int i = 0; i < 4; ++i) at[i] = k * I * 2 + (((first >> 3) + 2 * i + ((lane & 3) >> 1)) ^ across(k)) * 16 + (lane & 1) * 8;
         }
     }
     // rows 16 i .. + 15, elements 32 kk .. + 31
     __device__ __forceinline__ bf16x8 get(const char* lds, int i, int kk) const {
         if constexpr (ALONG) {
-            return *(const bf16x8*)(lds + at[kk] + i * 2048);
+            return *(const bf16x8*)(lds + at[kk] + i * 32 * BK);
         } else {
-            // 64 rows on: the granules' places differ by 8 as their numbers do, in bit 3 of both or by carry alone
+            // 64 rows on (from a multiple of 128): the granules' numbers differ in bit 3 alone, and so do their places
             const char* p = lds + (i < 4 ? at[i & 3] : at[i & 3] ^ 128) + kk * 32 * I * 2;
             const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)p);
             const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(p + 4 * I * 2));
@@ -110,7 +125,7 @@ template <int I, bool ALONG> struct Reader {
 };
 
 // Where an operand's next tile lies: `others` rows (or columns) of the result from `first` on, the contraction from `k` on.
-template <bool ALONG> struct Corner {
+template <bool ALONG, int BK> struct Corner {
     const bf16_t* p;
     int64_t step;                               // to the next tile, in elements
     int stride, fixed;                          // bytes of the other rows, or elements of the row
@@ -123,10 +138,6 @@ template <bool ALONG> struct Corner {
     // Rows are padded to whole granules.
     __device__ __forceinline__ int bytes(int left) const { return ALONG ? fixed + (left + 7) / 8 * 16 : (min(left, BK) - 1) * stride * 2 + fixed; }
 };
-
-// The terms whose products are taken, small ones first; with one term the last alone.
-__device__ __forceinline__ int term_a(int c) { return 0x001102 >> 4 * c & 15; }         // 2 0 1 1 0 0
-__device__ __forceinline__ int term_b(int c) { return 0x010120 >> 4 * c & 15; }         // 0 2 1 0 1 0
 
 // Eight values as planes of terms.
 template <typename E> __device__ __forceinline__ void store_terms(bf16_t* p, int64_t plane, const float (&x)[8]) {
@@ -148,8 +159,12 @@ template <typename E, Epilogue EPI> struct Output { using T = E; };
 template <typename E> struct Output<E, EPI_PART> { using T = float; };
 
 // All but the last N of this wavefront's loads to LDS are done, and every other's; all have read what they asked for.
+// (The builtin and not text, so that the compiler knows what has been waited for and adds no waits of its own to the products.)
 template <int N> __device__ __forceinline__ void wait_loads() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4);        // vmcnt(N) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -158,107 +173,145 @@ template <int N> __device__ __forceinline__ void wait_loads() {
 template <typename E, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, Epilogue EPI>
 __global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
     constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
+    constexpr int TERMS = Mode<E>::TERMS, BK = Mode<E>::BK, STAGES = Mode<E>::STAGES;
     constexpr bool GATED = EPI == EPI_GATED;
-    using TA = Tile<BM, A_ALONG, WAVES>;
-    using TB = Tile<BN, B_ALONG, WAVES>;
-    constexpr int LDS = TA::BYTES + TB::BYTES;
-    __shared__ __align__(1024) char lds[2][LDS];
+    using TA = Tile<BM, A_ALONG, WAVES, BK>;
+    using TB = Tile<BN, B_ALONG, WAVES, BK>;
+    constexpr int STAGE = TERMS * (TA::BYTES + TB::BYTES), LOADS = TERMS * (TA::LOADS + TB::LOADS);
+    __shared__ __align__(1024) char lds[STAGES][STAGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
     const int which = blockIdx.y / a.splits, split = blockIdx.y % a.splits;
     const FfnProblem& pr = a.prob[which];
-    // tiles that share rows of A or B run on one die, whose cache then holds them: dies take consecutive stretches of tiles
-    const int tiles_m = (pr.m + BM - 1) / BM, tiles_n = GATED ? (pr.n + BN / 2 - 1) / (BN / 2) : (pr.n + BN - 1) / BN, tiles = tiles_m * tiles_n;
+    const int count = a.count ? *a.count : 0;
+    const int M = a.count && !a.count_is_k ? count : pr.m, N = pr.n, K = a.count && a.count_is_k ? count : a.k;
+    // Tiles that share rows of A or B run on one die, whose cache then holds them: dies take consecutive stretches of the tiles that
+    // rows which count make.
+    const int tiles_m = (M + BM - 1) / BM, tiles_n = GATED ? (N + BN / 2 - 1) / (BN / 2) : (N + BN - 1) / BN, tiles = tiles_m * tiles_n;
     const int each = (tiles + 7) / 8, id = blockIdx.x % 8 * each + blockIdx.x / 8;
     if ((int)blockIdx.x / 8 >= each || id >= tiles) return;
     constexpr int BAND = 8;                     // rows of tiles that are worked through together
     const int band = id / (BAND * tiles_n), in_band = id - band * BAND * tiles_n, high = min(BAND, tiles_m - band * BAND);
     const int m0 = (band * BAND + in_band % high) * BM, n0 = in_band / high * (GATED ? BN / 2 : BN);
-    const int count = a.count ? *a.count : 0;
-    const int M = a.count && !a.count_is_k ? count : pr.m, N = pr.n, K = a.count && a.count_is_k ? count : a.k;
-    if (m0 >= M) return;
 
     TA ta;
     TB tb;
     ta.init(wave, lane, pr.a[0].stride);
-    // gated: rows of the tile are 32 of the gate's and 32 of the other projection's in turn; a wavefront loads from one of them
+    // gated: half of a wavefront's columns are the gate's and half the other projection's, in turn; it loads from one of them
     const int half = GATED ? wave & 1 : 0;
-    static_assert(!GATED || TB::LOADS * TB::ROWS_A_LOAD == 32, "a wavefront loads from one of the two projections");
+    static_assert(!GATED || TB::LOADS * TB::ROWS_A_LOAD == TN * 8, "a wavefront loads from one of the two projections");
     tb.init(GATED ? wave >> 1 : wave, lane, pr.b[0].stride);
-    Reader<BM, A_ALONG> ra;
-    Reader<BN, B_ALONG> rb;
+    Reader<BM, A_ALONG, BK> ra;
+    Reader<BN, B_ALONG, BK> rb;
     ra.init(wm * TM * 16, lane);
     rb.init(wn * TN * 16, lane);
 
-    constexpr int COMBOS = sizeof(E) == 4 ? 6 : 1;
-    const int ksteps = (K + BK - 1) / BK, all = ksteps * COMBOS * a.segments;
+    const int ksteps = (K + BK - 1) / BK, all = ksteps * a.segments;
     const int per_split = (all + a.splits - 1) / a.splits, from = min(split * per_split, all), n = min(from + per_split, all) - from;
     // where the next tiles to load stand
-    int combo = from % COMBOS, seg = from / COMBOS / max(ksteps, 1), left = K - from / COMBOS % max(ksteps, 1) * BK;
-    Corner<A_ALONG> ca;
-    Corner<B_ALONG> cb;
+    int seg = from / max(ksteps, 1), left = K - from % max(ksteps, 1) * BK;
+    Corner<A_ALONG, BK> ca;
+    Corner<B_ALONG, BK> cb;
     const int64_t plane_a = pr.a[0].plane, plane_b = pr.b[0].plane;
     auto corners = [&] {
         ca.set(pr.a[seg], m0, min(M - m0, BM), K - left);
         cb.set(pr.b[GATED ? half : seg], n0, min(N - n0, BN), K - left);
     };
     corners();
-    auto load = [&](int buffer) {
-        const bf16_t *pa = ca.p, *pb = cb.p;
-        if constexpr (COMBOS > 1) { pa += term_a(combo) * plane_a; pb += term_b(combo) * plane_b; }
-        ta.load(lds[buffer], wave, pa, ca.bytes(left), left);
-        tb.load(lds[buffer] + TA::BYTES, wave, pb, cb.bytes(left), left);
-        if (COMBOS > 1 && ++combo < COMBOS) return;
-        combo = 0;
+    auto load = [&](int stage) {
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) {
+            ta.load(lds[stage] + t * TA::BYTES, wave, ca.p + t * plane_a, ca.bytes(left), left);
+            tb.load(lds[stage] + TERMS * TA::BYTES + t * TB::BYTES, wave, cb.p + t * plane_b, cb.bytes(left), left);
+        }
         ca.p += ca.step;
         cb.p += cb.step;
         left -= BK;
         if (left <= 0 && seg + 1 < a.segments) { ++seg; left = K; corners(); }
     };
-    // Two sets of operands: while the products of one half of a step run, the other half's come from LDS, and in the middle of a step
-    // all wavefronts have done with its tiles, so that those of the step after next can be asked for.
     floatx4 acc[TM][TN] = {};
-    bf16x8 fa[2][TM], fb[2][TN];
-    auto read = [&](int buffer, int kk) {
-        const char *la = lds[buffer], *lb = la + TA::BYTES;
+    // Two sets of operands, so that one comes from LDS while the products of the other run.
+    bf16x8 fa[2][TERMS][TM], fb[2][TERMS][TN];
+    auto read = [&](int stage, int set, int kk) {
+        const char *la = lds[stage], *lb = la + TERMS * TA::BYTES;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) fb[kk][j] = rb.get(lb, j, kk);
+        for (int t = 0; t < TERMS; ++t) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i) fa[kk][i] = ra.get(la, i, kk);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    auto multiply = [&](int kk) {
+            for (int j = 0; j < TN; ++j) fb[set][t][j] = rb.get(lb + t * TB::BYTES, j, kk);
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[kk][j], fa[kk][i], acc[i][j], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    if (n > 0) {
-        load(0);
-        if (n > 1) {
-            load(1);
-            wait_loads<TA::LOADS + TB::LOADS>();
-        } else {
-            wait_loads<0>();
+            for (int i = 0; i < TM; ++i) fa[set][t][i] = ra.get(la + t * TA::BYTES, i, kk);
         }
-        read(0, 0);
-        for (int s = 0; s + 1 < n; ++s) {
-            read(s & 1, 1);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // the products of terms above 2^-24, small ones first
+    auto multiply = [&](int set) {
+#pragma unroll
+        for (int order = TERMS - 1; order >= 0; --order)
+#pragma unroll
+            for (int t = 0; t <= order; ++t)
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set][order - t][j], fa[set][t][i], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if constexpr (TERMS == 1) {
+        // A step is two sets.  In its middle all wavefronts have done with its tiles, so that those of the step after next are asked for.
+        if (n > 0) {
+            load(0);
+            if (n > 1) { load(1); wait_loads<LOADS>(); } else { wait_loads<0>(); }
+            read(0, 0, 0);
+            for (int s = 0; s + 1 < n; ++s) {
+                read(s & 1, 1, 1);
+                multiply(0);
+                wait_loads<0>();
+                read(s + 1 & 1, 0, 0);
+                if (s + 2 < n) load(s & 1);
+                multiply(1);
+            }
+            read(n - 1 & 1, 1, 1);
             multiply(0);
-            wait_loads<0>();
-            read(s + 1 & 1, 0);
-            if (s + 2 < n) load(s & 1);
             multiply(1);
         }
-        read(n - 1 & 1, 1);
-        multiply(0);
-        multiply(1);
+    } else {
+        // A step is one set.  It begins with the next one's operands and the loads of the third one on, into the place of its own.
+        if (n > 0) {
+            load(0);
+            if (n > 1) load(1);
+            if (n > 2) load(2);
+            if (n > 2) wait_loads<2 * LOADS>(); else if (n > 1) wait_loads<LOADS>(); else wait_loads<0>();
+            read(0, 0, 0);
+            int stage = 0, s = 0;               // of the step
+            auto full = [&](int set) {
+                const int next = stage == 2 ? 0 : stage + 1;
+                wait_loads<LOADS>();
+                read(next, set ^ 1, 0);
+                load(stage);
+                multiply(set);
+                stage = next;
+            };
+            for (; s + 4 < n; s += 2) { full(0); full(1); }
+            auto step = [&](int s, int set) {   // the last ones
+                const int next = stage == 2 ? 0 : stage + 1;
+                if (s + 1 < n) {
+                    if (s + 2 < n) wait_loads<LOADS>(); else wait_loads<0>();
+                    read(next, set ^ 1, 0);
+                    if (s + 3 < n) load(stage);
+                }
+                multiply(set);
+                stage = next;
+            };
+            for (; s < n; s += 2) {
+                step(s, 0);
+                if (s + 1 < n) step(s + 1, 1);
+            }
+        }
     }
     settle_products();
 
     // Results go through LDS, so that whole lines of memory are read and written: column l % 16 of a product is a row of C, its rows
     // 4 (l / 16) .. + 3 are columns.  Granules of four columns lie at g ^ (row & 15).  Then eight columns of a row a thread.
-    constexpr int PASSES = BM * BN * 4 / (2 * LDS), PM = TM / PASSES, ROWS = BM / PASSES, NT = 64 * WAVES;
+    constexpr int ALL = STAGES * STAGE, PASSES = (BM * BN * 4 + ALL - 1) / ALL, PM = TM / PASSES, ROWS = BM / PASSES, NT = 64 * WAVES;
     constexpr int UNITS = GATED ? BN / 16 : BN / 8, EACH = ROWS * UNITS / NT, AHEAD = EPI == EPI_BACK ? 2 : EACH;
     static_assert(PASSES * PM == TM && EACH % AHEAD == 0, "whole passes");
     char* stage = lds[0];
@@ -292,15 +345,15 @@ __global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
             }
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                const int unit = ((u0 + u) * NT + threadIdx.x) % UNITS, g = GATED ? unit / 4 * 16 + unit % 4 * 2 : unit * 2;
+                const int unit = ((u0 + u) * NT + threadIdx.x) % UNITS, g = GATED ? unit / TN * TN * 4 + unit % TN * 2 : unit * 2;
                 float x[8];
                 *(floatx4*)x = *granule(local[u], g);
                 *(floatx4*)(x + 4) = *granule(local[u], g + 1);
                 const int64_t at = (int64_t)row[u] * a.hidden_p + col[u];
                 if constexpr (GATED) {
                     float y[8], f[8], d[8];
-                    *(floatx4*)y = *granule(local[u], g + 8);
-                    *(floatx4*)(y + 4) = *granule(local[u], g + 9);
+                    *(floatx4*)y = *granule(local[u], g + TN * 2);
+                    *(floatx4*)(y + 4) = *granule(local[u], g + TN * 2 + 1);
                     if (!on[u]) continue;
                     if (a.va) {
                         *(floatx4*)(a.va + at) = *(floatx4*)x; *(floatx4*)(a.va + at + 4) = *(floatx4*)(x + 4);
@@ -435,13 +488,13 @@ int up8(int x) { return (x + 7) / 8 * 8; }
 int tiles_of(int x, int b) { return (x + b - 1) / b; }
 
 // Parts of the contraction: where the tiles do not fill the card, as many as do, each of at least 8 steps.
-int ffn_splits(int tiles, int edge, int steps) {
-    int s = tiles > 0 ? (edge == 256 ? 256 : 512) / tiles : 1;
+int ffn_splits(int tiles, int at_a_time, int steps) {
+    int s = tiles > 0 ? at_a_time / tiles : 1;
     if (s > steps / 8) s = steps / 8;
     return s < 1 ? 1 : s > 64 ? 64 : s;
 }
 // Edge of the tiles of a product of `problems` m x n results: 256 where such tiles fill the card.
-int tile_edge(int64_t m, int n, int problems) { return (int64_t)tiles_of((int)m, 256) * tiles_of(n, 256) * problems >= BIG_TILES ? 256 : 128; }
+int tile_edge(int32_t dtype, int64_t m, int n, int problems) { return dtype == PQL_BF16 && (int64_t)tiles_of((int)m, 256) * tiles_of(n, 256) * problems >= BIG_TILES ? 256 : 128; }
 
 struct FfnPlan {
     int rows, terms, dim_p, hidden_p, out_splits, dx_splits, weight_splits;
@@ -467,16 +520,17 @@ FfnPlan ffn_plan(const pql_ffn_shape& s, int call) {
     p.up = planes(p.gate_plane);
     p.down = planes(p.down_plane);
     p.m = planes(p.m_plane);
-    const int combos = p.terms == 1 ? 1 : 6;
-    auto splits = [](int64_t m, int n, int problems, int steps) {
-        const int e = tile_edge(m, n, problems);
-        return ffn_splits(tiles_of((int)m, e) * tiles_of(n, e) * problems, e, steps);
+    const int bk = s.dtype == PQL_F32 ? Mode<float>::BK : Mode<bf16_t>::BK;
+    // two workgroups a compute unit with the small tiles of bf16, one otherwise
+    auto splits = [&](int64_t m, int n, int problems, int steps) {
+        const int e = tile_edge(s.dtype, m, n, problems);
+        return ffn_splits(tiles_of((int)m, e) * tiles_of(n, e) * problems, s.dtype == PQL_BF16 && e == 128 ? 512 : 256, steps);
     };
     size_t part = 0;
     auto parts = [&](int splits, size_t floats) { if (splits > 1 && splits * floats * 4 > part) part = splits * floats * 4; };
-    p.out_splits = splits(p.rows, s.dim, 1, tiles_of(s.hidden, BK) * combos);
-    p.dx_splits = splits(p.rows, s.dim, 1, 2 * tiles_of(s.hidden, BK) * combos);
-    p.weight_splits = splits(s.hidden, s.dim, 3, tiles_of(p.rows, BK) * combos);
+    p.out_splits = splits(p.rows, s.dim, 1, tiles_of(s.hidden, bk));
+    p.dx_splits = splits(p.rows, s.dim, 1, 2 * tiles_of(s.hidden, bk));
+    p.weight_splits = splits(s.hidden, s.dim, 3, tiles_of(p.rows, bk));
     if (call == PQL_FFN_FORWARD) {
         parts(p.out_splits, (size_t)p.rows * s.dim);
     } else {
@@ -493,7 +547,8 @@ FfnPlan ffn_plan(const pql_ffn_shape& s, int call) {
 }
 
 template <typename E, bool A_ALONG, bool B_ALONG, Epilogue EPI> void launch_product(const ProfSlot& ps, int edge, dim3 grid, const FfnArgs& a, hipStream_t st) {
-    if (edge == 256) PQL_LAUNCH(ps, (ffn_product_kernel<E, 256, 256, 2, 4, A_ALONG, B_ALONG, EPI>), grid, dim3(512), 0, st, a);
+    if constexpr (sizeof(E) == 4) PQL_LAUNCH(ps, (ffn_product_kernel<E, 128, 128, 2, 4, A_ALONG, B_ALONG, EPI>), grid, dim3(512), 0, st, a);
+    else if (edge == 256) PQL_LAUNCH(ps, (ffn_product_kernel<E, 256, 256, 2, 4, A_ALONG, B_ALONG, EPI>), grid, dim3(512), 0, st, a);
     else PQL_LAUNCH(ps, (ffn_product_kernel<E, 128, 128, 2, 2, A_ALONG, B_ALONG, EPI>), grid, dim3(256), 0, st, a);
 }
 
@@ -559,7 +614,7 @@ struct FfnRun {
     }
     FfnArgs args() const {
         FfnArgs a{};
-        a.terms = p.terms; a.segments = 1; a.splits = 1;
+        a.segments = 1; a.splits = 1;
         a.count = count; a.map = map; a.act = s.act;
         a.hidden_p = p.hidden_p; a.m_plane = p.m_plane;
         return a;
@@ -568,7 +623,7 @@ struct FfnRun {
     template <bool A_ALONG, bool B_ALONG, Epilogue EPI> void product(FfnArgs& a, int problems, int whole, int kid) {
         if (e != hipSuccess) return;
         const FfnProblem& pr = a.prob[0];
-        const int edge = EPI == EPI_GATED ? tile_edge(pr.m, 2 * pr.n, 1) : tile_edge(pr.m, pr.n, whole);
+        const int edge = EPI == EPI_GATED ? tile_edge(s.dtype, pr.m, 2 * pr.n, 1) : tile_edge(s.dtype, pr.m, pr.n, whole);
         const int each = (tiles_of(pr.m, edge) * tiles_of(pr.n, EPI == EPI_GATED ? edge / 2 : edge) + 7) / 8;           // problems are alike or transposed
         const dim3 grid(each * 8, problems * a.splits);
         const ProfSlot ps = prof_slot();
