@@ -20,26 +20,23 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
 // Terms of a value, elements of the contraction a step, steps in LDS at a time.
-template <typename E> struct Mode;
-template <> struct Mode<bf16_t> { static constexpr int TERMS = 1, BK = 64, STAGES = 2; };
-template <> struct Mode<float> { static constexpr int TERMS = 3, BK = 32, STAGES = 3; };
+template <typename E, int BM> struct Mode { static constexpr int TERMS = 1, BK = 64, STAGES = 2; };
+template <> struct Mode<float, 128> { static constexpr int TERMS = 3, BK = 32, STAGES = 3; };
+template <> struct Mode<float, 256> { static constexpr int TERMS = 3, BK = 32, STAGES = 2; };
 constexpr int BIG_TILES = 192;
 constexpr int NOWHERE = 0x7fffff00;             // an offset behind every buffer: reads give zeros
 
 // One operand: rows of a matrix, `plane` elements from one term's to the next.
 struct FfnOperand { const bf16_t* p; int64_t stride, plane; };
-// ROWS: the contraction runs along the rows (element (i, k) at i * stride + k); otherwise along the columns (k * stride + i).
 struct FfnProblem { FfnOperand a[2], b[2]; int m, n; void* out; int64_t out_stride; };
-enum Epilogue : int { EPI_GATED, EPI_BACK, EPI_OUT, EPI_PART };
+enum Epilogue : int { EPI_GATED, EPI_BACK, EPI_OUT };
 
 struct FfnArgs {
     FfnProblem prob[3];
-    int k, segments;                            // length of the contraction, of each of `segments` pairs of operands
+    int problems, k, segments;                  // length of the contraction, of each of `segments` pairs of operands
     const int* count;                           // rows that count, NULL: all
     int count_is_k;                             // whether they are the contraction or the rows of the result
-    int splits;                                 // parts of the contraction
-    float* part;                                // [problem][splits][m][n] sums of the parts
-    int64_t part_stride;                        // of a problem
+    float* part;                                // [workgroups][2][tile] sums over parts of the contraction
     const int* map;                             // packed row -> row of the output, NULL: the same
     int act;
     // gated, back: [row][hidden_p]
@@ -155,8 +152,88 @@ template <typename E> __device__ __forceinline__ void store_terms(bf16_t* p, int
     }
 }
 
-template <typename E, Epilogue EPI> struct Output { using T = E; };
-template <typename E> struct Output<E, EPI_PART> { using T = float; };
+// Eight columns of a row of the result from their sums; gated: those of both projections.
+template <typename E, Epilogue EPI> __device__ __forceinline__ void finish(const FfnArgs& a, const FfnProblem& pr, int row, int col, float (&x)[8], float (&y)[8],
+                                                                       const floatx4 (&va)[2], const floatx4 (&vb)[2]) {
+    const int64_t at = (int64_t)row * a.hidden_p + col;
+    if constexpr (EPI == EPI_GATED) {
+        if (a.va) {
+            *(floatx4*)(a.va + at) = *(floatx4*)x; *(floatx4*)(a.va + at + 4) = *(floatx4*)(x + 4);
+            *(floatx4*)(a.vb + at) = *(floatx4*)y; *(floatx4*)(a.vb + at + 4) = *(floatx4*)(y + 4);
+        }
+        float f[8], d[8];
+        activate_all<E>(a.act, x, f, d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= y[e];
+        store_terms<E>(a.m + at, a.m_plane, f);
+    } else if constexpr (EPI == EPI_BACK) {
+        float p[8], b[8], f[8], d[8];
+        *(floatx4*)p = va[0]; *(floatx4*)(p + 4) = va[1];
+        *(floatx4*)b = vb[0]; *(floatx4*)(b + 4) = vb[1];
+        activate_all<E>(a.act, p, f, d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { p[e] = x[e] * b[e] * d[e]; x[e] *= f[e]; }
+        store_terms<E>(a.da + at, a.m_plane, p);
+        store_terms<E>(a.db + at, a.m_plane, x);
+    } else {
+        E* p = (E*)pr.out + (int64_t)(a.map ? a.map[row] : row) * pr.out_stride + col;
+        if (((uintptr_t)p & 15) == 0 && col + 8 <= pr.n) {
+#pragma unroll
+            for (int h = 0; h < 8 / VEC_OF<E>; ++h) ((uint4*)p)[h] = narrow(x + h * VEC_OF<E>, E{});
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < pr.n) p[e] = from_float<E>(x[e]);
+        }
+    }
+}
+
+// ---- how the tiles are shared out ------------------------------------------------------------------------
+// `slots` workgroups run at a time.  As many whole rounds of tiles as there are go to a workgroup each; the `rest` tiles behind
+// them are cut into steps of their contractions, of which each of `sharers` workgroups takes `per` in a row, at most a tile's.
+// What is not a whole tile is left as sums, joined by another launch.  Known where the rows that count are: on the device.
+constexpr int JOIN_STEPS = 6;                   // that the other launch takes as long as: fewer are not worth it
+struct Shares {
+    int whole, rest, steps, per, sharers;
+    __host__ __device__ Shares(int tiles, int slots, int steps_) : steps(steps_) {
+        whole = tiles / slots * slots;
+        rest = tiles - whole;
+        per = (int)(((int64_t)rest * steps + slots - 1) / slots);
+        if (per > steps - JOIN_STEPS) per = steps;
+        sharers = per > 0 ? (int)(((int64_t)rest * steps + per - 1) / per) : rest;
+    }
+    __host__ __device__ bool joins() const { return rest > 0 && per < steps; }
+};
+// The i-th of n things for workgroups of which every eighth runs on the same die: dies take consecutive stretches.  -1: nothing.
+__device__ __forceinline__ int stretch(int i, int n) {
+    const int each = (n + 7) / 8, id = i % 8 * each + i / 8;
+    return i / 8 < each && id < n ? id : -1;
+}
+// A tile's problem and corner: in bands of BAND rows of tiles, that share what they read in one die's cache.
+struct Place { int which, m0, n0; };
+template <int BM, int COLS> __host__ __device__ inline int tiles_in(int m, int n) { return ((m + BM - 1) / BM) * ((n + COLS - 1) / COLS); }
+template <int BM, int COLS> __device__ __forceinline__ Place place_of(const FfnArgs& a, int rows, int id) {
+    constexpr int BAND = 8;
+    Place p{0, 0, 0};
+    int m = rows >= 0 ? rows : a.prob[0].m;
+    for (; p.which + 1 < a.problems; ++p.which) {
+        m = rows >= 0 ? rows : a.prob[p.which].m;
+        const int t = tiles_in<BM, COLS>(m, a.prob[p.which].n);
+        if (id < t) break;
+        id -= t;
+    }
+    m = rows >= 0 ? rows : a.prob[p.which].m;
+    const int tiles_m = (m + BM - 1) / BM, tiles_n = (a.prob[p.which].n + COLS - 1) / COLS;
+    const int band = id / (BAND * tiles_n), in_band = id - band * BAND * tiles_n, high = min(BAND, tiles_m - band * BAND);
+    p.m0 = (band * BAND + in_band % high) * BM;
+    p.n0 = in_band / high * COLS;
+    return p;
+}
+template <int BM, int COLS> __device__ __forceinline__ int all_tiles(const FfnArgs& a, int rows) {
+    int t = 0;
+    for (int i = 0; i < a.problems; ++i) t += tiles_in<BM, COLS>(rows >= 0 ? rows : a.prob[i].m, a.prob[i].n);
+    return t;
+}
 
 // All but the last N of this wavefront's loads to LDS are done, and every other's; all have read what they asked for.
 // (The builtin and not text, so that the compiler knows what has been waited for and adds no waits of its own to the products.)
@@ -169,29 +246,45 @@ template <int N> __device__ __forceinline__ void wait_loads() {
 }
 
 // ---- products -------------------------------------------------------------------------------------------
-// C[m][n] = sum_k A(m, k) B(n, k).  A tile of BM x BN by WM x WN wavefronts.
+// C[m][n] = sum_k A(m, k) B(n, k).  Tiles of BM x BN by WM x WN wavefronts; *_ALONG: the contraction runs along the operand's rows in
+// memory, otherwise across them.
 template <typename E, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, Epilogue EPI>
-__global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
+__global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a, int slots) {
     constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-    constexpr int TERMS = Mode<E>::TERMS, BK = Mode<E>::BK, STAGES = Mode<E>::STAGES;
+    constexpr int TERMS = Mode<E, BM>::TERMS, BK = Mode<E, BM>::BK, STAGES = Mode<E, BM>::STAGES;
     constexpr bool GATED = EPI == EPI_GATED;
     using TA = Tile<BM, A_ALONG, WAVES, BK>;
     using TB = Tile<BN, B_ALONG, WAVES, BK>;
     constexpr int STAGE = TERMS * (TA::BYTES + TB::BYTES), LOADS = TERMS * (TA::LOADS + TB::LOADS);
     __shared__ __align__(1024) char lds[STAGES][STAGE];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
-    const int which = blockIdx.y / a.splits, split = blockIdx.y % a.splits;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+    constexpr int COLS = GATED ? BN / 2 : BN;
+    const int count = a.count ? *a.count : 0, rows = a.count && !a.count_is_k ? count : -1, K = a.count && a.count_is_k ? count : a.k;
+    const int ksteps = (K + BK - 1) / BK;
+    const Shares sh(all_tiles<BM, COLS>(a, rows), slots, ksteps * a.segments);
+    // this workgroup's steps, of `tile` and perhaps the one behind it
+    int tile, from, left_steps;
+    if ((int)blockIdx.x < sh.whole) {
+        tile = stretch(blockIdx.x, sh.whole);
+        from = 0;
+        left_steps = sh.steps;
+    } else {
+        const int w = stretch(blockIdx.x - sh.whole, sh.sharers);
+        if (w < 0) return;
+        const int64_t first = (int64_t)w * sh.per, all = (int64_t)sh.rest * sh.steps;
+        tile = sh.whole + (sh.steps > 0 ? (int)(first / sh.steps) : w);
+        from = sh.steps > 0 ? (int)(first % sh.steps) : 0;
+        left_steps = (int)min((int64_t)sh.per, all - first);
+    }
+    const int sharer = blockIdx.x < sh.whole ? 0 : stretch(blockIdx.x - sh.whole, sh.sharers);
+    for (;;) {
+    int lane = threadIdx.x & 63;
+    asm("" : "+v"(lane));                       // addresses are found anew for each tile: there are no registers to keep them in
+    const int n = min(left_steps, sh.steps - from);
+    const Place at = place_of<BM, COLS>(a, rows, tile);
+    const int which = at.which, m0 = at.m0, n0 = at.n0;
     const FfnProblem& pr = a.prob[which];
-    const int count = a.count ? *a.count : 0;
-    const int M = a.count && !a.count_is_k ? count : pr.m, N = pr.n, K = a.count && a.count_is_k ? count : a.k;
-    // Tiles that share rows of A or B run on one die, whose cache then holds them: dies take consecutive stretches of the tiles that
-    // rows which count make.
-    const int tiles_m = (M + BM - 1) / BM, tiles_n = GATED ? (N + BN / 2 - 1) / (BN / 2) : (N + BN - 1) / BN, tiles = tiles_m * tiles_n;
-    const int each = (tiles + 7) / 8, id = blockIdx.x % 8 * each + blockIdx.x / 8;
-    if ((int)blockIdx.x / 8 >= each || id >= tiles) return;
-    constexpr int BAND = 8;                     // rows of tiles that are worked through together
-    const int band = id / (BAND * tiles_n), in_band = id - band * BAND * tiles_n, high = min(BAND, tiles_m - band * BAND);
-    const int m0 = (band * BAND + in_band % high) * BM, n0 = in_band / high * (GATED ? BN / 2 : BN);
+    const int M = rows >= 0 ? rows : pr.m, N = pr.n;
 
     TA ta;
     TB tb;
@@ -205,8 +298,6 @@ __global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
     ra.init(wm * TM * 16, lane);
     rb.init(wn * TN * 16, lane);
 
-    const int ksteps = (K + BK - 1) / BK, all = ksteps * a.segments;
-    const int per_split = (all + a.splits - 1) / a.splits, from = min(split * per_split, all), n = min(from + per_split, all) - from;
     // where the next tiles to load stand
     int seg = from / max(ksteps, 1), left = K - from % max(ksteps, 1) * BK;
     Corner<A_ALONG, BK> ca;
@@ -229,8 +320,30 @@ __global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
         if (left <= 0 && seg + 1 < a.segments) { ++seg; left = K; corners(); }
     };
     floatx4 acc[TM][TN] = {};
-    // Two sets of operands, so that one comes from LDS while the products of the other run.
-    bf16x8 fa[2][TERMS][TM], fb[2][TERMS][TN];
+    // Two sets of operands, so that one comes from LDS while the products of the other run; STREAM: of A's only 16 rows each.
+    constexpr bool STREAM = TERMS == 3 && BM == 256;
+    bf16x8 fa[2][TERMS][STREAM ? 1 : TM], fb[2][TERMS][TN];
+    auto read_a = [&](int stage, int set, int i) {
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) fa[set][t][0] = ra.get(lds[stage] + t * TA::BYTES, i, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto read_b = [&](int stage, int set) {
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fb[set][t][j] = rb.get(lds[stage] + TERMS * TA::BYTES + t * TB::BYTES, j, 0);
+    };
+    auto multiply_row = [&](int set_a, int set_b, int i) {
+#pragma unroll
+        for (int order = TERMS - 1; order >= 0; --order)
+#pragma unroll
+            for (int t = 0; t <= order; ++t)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set_b][order - t][j], fa[set_a][t][0], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
     auto read = [&](int stage, int set, int kk) {
         const char *la = lds[stage], *lb = la + TERMS * TA::BYTES;
 #pragma unroll
@@ -238,7 +351,7 @@ __global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
 #pragma unroll
             for (int j = 0; j < TN; ++j) fb[set][t][j] = rb.get(lb + t * TB::BYTES, j, kk);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fa[set][t][i] = ra.get(la + t * TA::BYTES, i, kk);
+            for (int i = 0; i < (STREAM ? 0 : TM); ++i) fa[set][t][i] = ra.get(la + t * TA::BYTES, i, kk);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -249,7 +362,7 @@ __global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
 #pragma unroll
             for (int t = 0; t <= order; ++t)
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
+                for (int i = 0; i < (STREAM ? 0 : TM); ++i)
 #pragma unroll
                     for (int j = 0; j < TN; ++j)
                         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set][order - t][j], fa[set][t][i], acc[i][j], 0, 0, 0);
@@ -272,6 +385,49 @@ __global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
             read(n - 1 & 1, 1, 1);
             multiply(0);
             multiply(1);
+        }
+    } else if constexpr (STREAM) {
+        // A step goes through A 16 rows at a time; with the last of them begin the next step's operands and the loads of the one after.
+        static_assert(!STREAM || (TM % 2 == 0 && STAGES == 2), "sets alternate");
+        if (n > 0) {
+            load(0);
+            if (n > 1) { load(1); wait_loads<LOADS>(); } else { wait_loads<0>(); }
+            read_b(0, 0);
+            read_a(0, 0, 0);
+            auto rows = [&](int stage, int set) {
+#pragma unroll
+                for (int i = 0; i + 1 < TM; ++i) {
+                    read_a(stage, i + 1 & 1, i + 1);
+                    multiply_row(i & 1, set, i);
+                }
+            };
+            auto next = [&](int stage, int set) {
+                wait_loads<0>();
+                read_b(stage ^ 1, set ^ 1);
+                read_a(stage ^ 1, 0, 0);
+            };
+            int s = 0;
+            for (; s + 3 < n; s += 2) {
+                rows(0, 0);
+                next(0, 0);
+                load(0);
+                multiply_row(1, 0, TM - 1);
+                rows(1, 1);
+                next(1, 1);
+                load(1);
+                multiply_row(1, 1, TM - 1);
+            }
+            for (; s < n; s += 2) {
+                rows(0, 0);
+                if (s + 1 < n) next(0, 0);
+                if (s + 2 < n) load(0);
+                multiply_row(1, 0, TM - 1);
+                if (s + 1 == n) break;
+                rows(1, 1);
+                if (s + 2 < n) next(1, 1);
+                if (s + 3 < n) load(1);
+                multiply_row(1, 1, TM - 1);
+            }
         }
     } else {
         // A step is one set.  It begins with the next one's operands and the loads of the third one on, into the place of its own.
@@ -310,21 +466,33 @@ __global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
     settle_products();
 
     // Results go through LDS, so that whole lines of memory are read and written: column l % 16 of a product is a row of C, its rows
-    // 4 (l / 16) .. + 3 are columns.  Granules of four columns lie at g ^ (row & 15).  Then eight columns of a row a thread.
+    // 4 (l / 16) .. + 3 are columns.  Then eight columns of a row a thread: the first four of each eight lie together, then the last
+    // four, both in an order that depends on the row, so that neither side meets bank conflicts.
     constexpr int ALL = STAGES * STAGE, PASSES = (BM * BN * 4 + ALL - 1) / ALL, PM = TM / PASSES, ROWS = BM / PASSES, NT = 64 * WAVES;
-    constexpr int UNITS = GATED ? BN / 16 : BN / 8, EACH = ROWS * UNITS / NT, AHEAD = EPI == EPI_BACK ? 2 : EACH;
+    constexpr int UNITS = GATED ? BN / 16 : BN / 8, EACH = ROWS * UNITS / NT, AHEAD = 2;
     static_assert(PASSES * PM == TM && EACH % AHEAD == 0, "whole passes");
     char* stage = lds[0];
-    auto granule = [&](int row, int g) { return (floatx4*)(stage + row * BN * 4 + ((g ^ (row & 15)) << 4)); };
+    auto granule = [&](int row, int g) { return (floatx4*)(stage + row * BN * 4 + ((((g >> 1) + (g & 1) * (BN / 8)) ^ (row & 15)) << 4)); };
+    float* part = n == sh.steps ? nullptr : a.part + ((int64_t)sharer * 2 + (from == 0)) * (BM * BN);
 #pragma unroll
     for (int pass = 0; pass < PASSES; ++pass) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < PM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
-                *granule((wm * PM + i) * 16 + (lane & 15), (wn * TN + j) * 4 + (lane >> 4)) = acc[pass * PM + i][j];
+            for (int j = 0; j < TN; ++j) {
+                // gated: the gate's columns, then the other projection's
+                const int g = GATED ? (wn * (TN / 2) + j % (TN / 2)) * 4 + j / (TN / 2) * (BN / 8) : (wn * TN + j) * 4;
+                *granule((wm * PM + i) * 16 + (lane & 15), g + (lane >> 4)) = acc[pass * PM + i][j];
+            }
         __syncthreads();
+        if (part) {
+            for (int i = threadIdx.x; i < ROWS * (BN / 4); i += NT) {
+                const int local = i / (BN / 4), g = i % (BN / 4), row = (local / (PM * 16) * TM + pass * PM) * 16 + local % (PM * 16);
+                *(floatx4*)(part + row * BN + g * 4) = *granule(local, g);
+            }
+            continue;
+        }
 #pragma unroll 1
         for (int u0 = 0; u0 < EACH; u0 += AHEAD) {
             floatx4 va[AHEAD][2], vb[AHEAD][2];
@@ -336,77 +504,72 @@ __global__ void __launch_bounds__(64 * WM * WN) ffn_product_kernel(FfnArgs a) {
                 local[u] = unit / UNITS;
                 row[u] = m0 + (local[u] / (PM * 16) * TM + pass * PM) * 16 + local[u] % (PM * 16);
                 col[u] = n0 + unit % UNITS * 8;
-                on[u] = row[u] < M && col[u] < (GATED || EPI == EPI_BACK ? a.hidden_p : N);
+                on[u] = row[u] < M && col[u] < (EPI == EPI_OUT ? N : a.hidden_p);
                 if constexpr (EPI == EPI_BACK) {
-                    const int64_t at = on[u] ? (int64_t)row[u] * a.hidden_p + col[u] : 0;
+                    const int64_t p = on[u] ? (int64_t)row[u] * a.hidden_p + col[u] : 0;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) { va[u][h] = *(const floatx4*)(a.va + at + 4 * h); vb[u][h] = *(const floatx4*)(a.vb + at + 4 * h); }
+                    for (int h = 0; h < 2; ++h) { va[u][h] = *(const floatx4*)(a.va + p + 4 * h); vb[u][h] = *(const floatx4*)(a.vb + p + 4 * h); }
                 }
             }
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                const int unit = ((u0 + u) * NT + threadIdx.x) % UNITS, g = GATED ? unit / TN * TN * 4 + unit % TN * 2 : unit * 2;
-                float x[8];
+                const int g = ((u0 + u) * NT + threadIdx.x) % UNITS * 2;
+                float x[8], y[8];
                 *(floatx4*)x = *granule(local[u], g);
                 *(floatx4*)(x + 4) = *granule(local[u], g + 1);
-                const int64_t at = (int64_t)row[u] * a.hidden_p + col[u];
                 if constexpr (GATED) {
-                    float y[8], f[8], d[8];
-                    *(floatx4*)y = *granule(local[u], g + TN * 2);
-                    *(floatx4*)(y + 4) = *granule(local[u], g + TN * 2 + 1);
-                    if (!on[u]) continue;
-                    if (a.va) {
-                        *(floatx4*)(a.va + at) = *(floatx4*)x; *(floatx4*)(a.va + at + 4) = *(floatx4*)(x + 4);
-                        *(floatx4*)(a.vb + at) = *(floatx4*)y; *(floatx4*)(a.vb + at + 4) = *(floatx4*)(y + 4);
-                    }
-                    if (a.m) {
-                        activate_all<E>(a.act, x, f, d);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) f[e] *= y[e];
-                        store_terms<E>(a.m + at, a.m_plane, f);
-                    }
-                } else if constexpr (EPI == EPI_BACK) {
-                    if (!on[u]) continue;
-                    float p[8], b[8], f[8], d[8];
-                    *(floatx4*)p = va[u][0]; *(floatx4*)(p + 4) = va[u][1];
-                    *(floatx4*)b = vb[u][0]; *(floatx4*)(b + 4) = vb[u][1];
-                    activate_all<E>(a.act, p, f, d);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) { p[e] = x[e] * b[e] * d[e]; x[e] *= f[e]; f[e] *= b[e]; }
-                    store_terms<E>(a.da + at, a.m_plane, p);
-                    store_terms<E>(a.db + at, a.m_plane, x);
-                    store_terms<E>(a.m + at, a.m_plane, f);
-                } else {
-                    if (!on[u]) continue;
-                    using O = typename Output<E, EPI>::T;
-                    O* p = EPI == EPI_PART ? (O*)(a.part + which * a.part_stride + ((int64_t)split * pr.m + row[u]) * pr.n)
-                                           : (O*)pr.out + (int64_t)(a.map ? a.map[row[u]] : row[u]) * pr.out_stride;
-                    p += col[u];
-                    if (((uintptr_t)p & 15) == 0 && col[u] + 8 <= N) {
-#pragma unroll
-                        for (int h = 0; h < 8 / VEC_OF<O>; ++h) ((uint4*)p)[h] = narrow(x + h * VEC_OF<O>, O{});
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (col[u] + e < N) p[e] = from_float<O>(x[e]);
-                    }
+                    *(floatx4*)y = *granule(local[u], g + BN / 8);
+                    *(floatx4*)(y + 4) = *granule(local[u], g + BN / 8 + 1);
                 }
+                if (on[u]) finish<E, EPI>(a, pr, row[u], col[u], x, y, va[u], vb[u]);
             }
         }
     }
+    left_steps -= n;
+    if (left_steps <= 0) break;
+    ++tile;
+    from = 0;
+    __syncthreads();                            // the next tiles overwrite the results' place
+    }
 }
 
-// Sums of the parts of a split contraction, in order.
-template <typename E> __global__ void __launch_bounds__(256) ffn_join_kernel(FfnArgs a) {
-    const FfnProblem& pr = a.prob[blockIdx.y];
-    const int M = a.count && !a.count_is_k ? *a.count : pr.m;
-    const int64_t all = (int64_t)M * pr.n, whole = (int64_t)pr.m * pr.n;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
-        const float* p = a.part + blockIdx.y * a.part_stride + i;
-        float s = 0.f;
-        for (int q = 0; q < a.splits; ++q) s += p[q * whole];
-        const int row = (int)(i / pr.n), col = (int)(i - (int64_t)row * pr.n);
-        ((E*)pr.out)[(int64_t)(a.map ? a.map[row] : row) * pr.out_stride + col] = from_float<E>(s);
+// Tiles whose sums are in parts: those of consecutive workgroups, added in order.  Eight columns of a row a thread.
+template <typename E, int BM, int BN, Epilogue EPI> __global__ void __launch_bounds__(256) ffn_join_kernel(FfnArgs a, int slots, int bk) {
+    constexpr int COLS = EPI == EPI_GATED ? BN / 2 : BN, UNITS = COLS / 8;
+    const int count = a.count ? *a.count : 0, rows = a.count && !a.count_is_k ? count : -1, K = a.count && a.count_is_k ? count : a.k;
+    const Shares sh(all_tiles<BM, COLS>(a, rows), slots, (K + bk - 1) / bk * a.segments);
+    if (!sh.joins()) return;
+    constexpr int BLOCKS = BM * UNITS / 256;    // of a tile
+    for (int b = blockIdx.x; b < sh.rest * BLOCKS; b += gridDim.x) {
+        const int j = b / BLOCKS, unit = b % BLOCKS * 256 + threadIdx.x, local = unit / UNITS, c = unit % UNITS * 8;
+        const int first = (int)((int64_t)j * sh.steps / sh.per), last = (int)((((int64_t)j + 1) * sh.steps - 1) / sh.per);
+        if (first == last) continue;
+        const Place at = place_of<BM, COLS>(a, rows, sh.whole + j);
+        const FfnProblem& pr = a.prob[at.which];
+        const int row = at.m0 + local, col = at.n0 + c;
+        if (row >= (rows >= 0 ? rows : pr.m) || col >= (EPI == EPI_OUT ? pr.n : a.hidden_p)) continue;
+        float x[8] = {}, y[8] = {};
+        for (int w = first; w <= last; ++w) {
+            const float* p = a.part + ((int64_t)w * 2 + (w == first)) * (BM * BN) + local * BN + c;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const floatx4 v = *(const floatx4*)(p + 4 * h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[4 * h + e] += v[e];
+                if constexpr (EPI == EPI_GATED) {
+                    const floatx4 u = *(const floatx4*)(p + COLS + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[4 * h + e] += u[e];
+                }
+            }
+        }
+        floatx4 va[2], vb[2];
+        if constexpr (EPI == EPI_BACK) {
+            const int64_t p = (int64_t)row * a.hidden_p + col;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) { va[h] = *(const floatx4*)(a.va + p + 4 * h); vb[h] = *(const floatx4*)(a.vb + p + 4 * h); }
+        }
+        finish<E, EPI>(a, pr, row, col, x, y, va, vb);
     }
 }
 
@@ -446,7 +609,7 @@ __global__ void __launch_bounds__(256) ffn_map_kernel(const int* lengths, int ba
 // Matrices as planes of padded rows, packed by the map where there is one.  Rows of `clear` that do not count become zeros.
 struct FfnCopy { const void* from; int64_t stride; bf16_t* to; int64_t plane; int rows, cols, cols_p; const int* map; };
 struct FfnCopies {
-    FfnCopy c[4];
+    FfnCopy c[5];
     int n;
     const int* count;
     void* clear; int64_t clear_stride; int clear_cols, clear_rows;
@@ -487,17 +650,31 @@ int ffn_rows(const pql_ffn_shape& s) { return (int)((int64_t)s.batch * s.steps);
 int up8(int x) { return (x + 7) / 8 * 8; }
 int tiles_of(int x, int b) { return (x + b - 1) / b; }
 
-// Parts of the contraction: where the tiles do not fill the card, as many as do, each of at least 8 steps.
-int ffn_splits(int tiles, int at_a_time, int steps) {
-    int s = tiles > 0 ? at_a_time / tiles : 1;
-    if (s > steps / 8) s = steps / 8;
-    return s < 1 ? 1 : s > 64 ? 64 : s;
+// Rows of the tiles of a product of `problems` m x n results, 256 where such tiles fill the card, and columns.
+int tile_cols(int32_t dtype, int rows) { return dtype == PQL_BF16 ? rows : 128; }
+int tile_rows(int32_t dtype, int64_t m, int n, int problems) {
+    return (int64_t)tiles_of((int)m, 256) * tiles_of(n, tile_cols(dtype, 256)) * problems >= BIG_TILES ? 256 : 128;
 }
-// Edge of the tiles of a product of `problems` m x n results: 256 where such tiles fill the card.
-int tile_edge(int32_t dtype, int64_t m, int n, int problems) { return dtype == PQL_BF16 && (int64_t)tiles_of((int)m, 256) * tiles_of(n, 256) * problems >= BIG_TILES ? 256 : 128; }
 
+// One product's tiles, workgroups at a time, and the steps of its contraction, at most.
+struct FfnTiles { int rows, cols, tiles, slots, steps; };
+FfnTiles ffn_tiles(int32_t dtype, int64_t m, int n, int problems, int of, int64_t k, int segments, bool gated) {
+    FfnTiles t{};
+    t.rows = tile_rows(dtype, m, gated ? 2 * n : n, of);
+    t.cols = tile_cols(dtype, t.rows);
+    t.tiles = tiles_of((int)m, t.rows) * tiles_of(n, gated ? t.cols / 2 : t.cols) * problems;
+    t.slots = dtype == PQL_BF16 && t.rows == 128 ? 512 : 256;          // two workgroups a compute unit, one where LDS holds no more
+    t.steps = tiles_of((int)k, dtype == PQL_F32 ? 32 : 64) * segments;
+    return t;
+}
+// Bytes of the parts that as many workgroups may leave.
+size_t part_bytes(const FfnTiles& t) {
+    if (t.steps <= JOIN_STEPS) return 0;
+    const int64_t most = (int64_t)t.tiles * t.steps;
+    return (size_t)(most < t.slots ? most : t.slots) * 2 * t.rows * t.cols * 4;
+}
 struct FfnPlan {
-    int rows, terms, dim_p, hidden_p, out_splits, dx_splits, weight_splits;
+    int rows, terms, dim_p, hidden_p;
     size_t map, count, x, dout, gate, up, down, m, da, db, va, vb, part, bytes;
     int64_t x_plane, gate_plane, down_plane, m_plane;
 };
@@ -510,46 +687,61 @@ FfnPlan ffn_plan(const pql_ffn_shape& s, int call) {
     p.gate_plane = (int64_t)s.hidden * p.dim_p;
     p.down_plane = (int64_t)s.dim * p.hidden_p;
     p.m_plane = (int64_t)p.rows * p.hidden_p;
-    size_t o = 0;
+    size_t o = 0, part = 0;
     auto take = [&](size_t b) { const size_t at = o; o += to256(b); return at; };
     auto planes = [&](int64_t plane) { return take((size_t)plane * p.terms * 2); };
+    auto parts = [&](const FfnTiles& t) { const size_t b = part_bytes(t); part = b > part ? b : part; };
     p.map = take((size_t)p.rows * 4);
     p.count = take(4);
     p.x = planes(p.x_plane);
     p.gate = planes(p.gate_plane);
     p.up = planes(p.gate_plane);
     p.down = planes(p.down_plane);
-    p.m = planes(p.m_plane);
-    const int bk = s.dtype == PQL_F32 ? Mode<float>::BK : Mode<bf16_t>::BK;
-    // two workgroups a compute unit with the small tiles of bf16, one otherwise
-    auto splits = [&](int64_t m, int n, int problems, int steps) {
-        const int e = tile_edge(s.dtype, m, n, problems);
-        return ffn_splits(tiles_of((int)m, e) * tiles_of(n, e) * problems, s.dtype == PQL_BF16 && e == 128 ? 512 : 256, steps);
-    };
-    size_t part = 0;
-    auto parts = [&](int splits, size_t floats) { if (splits > 1 && splits * floats * 4 > part) part = splits * floats * 4; };
-    p.out_splits = splits(p.rows, s.dim, 1, tiles_of(s.hidden, bk));
-    p.dx_splits = splits(p.rows, s.dim, 1, 2 * tiles_of(s.hidden, bk));
-    p.weight_splits = splits(s.hidden, s.dim, 3, tiles_of(p.rows, bk));
+    if (call != PQL_FFN_BACKWARD) {
+        parts(ffn_tiles(s.dtype, p.rows, s.hidden, 1, 1, s.dim, 1, true));
+        p.m = planes(p.m_plane);
+    }
     if (call == PQL_FFN_FORWARD) {
-        parts(p.out_splits, (size_t)p.rows * s.dim);
+        parts(ffn_tiles(s.dtype, p.rows, s.dim, 1, 1, s.hidden, 1, false));
     } else {
         p.dout = planes(p.x_plane);
         p.da = planes(p.m_plane);
         p.db = planes(p.m_plane);
         if (call == PQL_FFN_BACKWARD_ALONE) { p.va = take((size_t)p.m_plane * 4); p.vb = take((size_t)p.m_plane * 4); }
-        parts(p.dx_splits, (size_t)p.rows * s.dim);
-        parts(p.weight_splits, 3 * (size_t)s.dim * s.hidden);
+        parts(ffn_tiles(s.dtype, p.rows, s.hidden, 1, 1, s.dim, 1, false));
+        parts(ffn_tiles(s.dtype, p.rows, s.dim, 1, 1, s.hidden, 2, false));
+        // the weights' gradients: three products, some of them the others' transposes
+        for (int i = 0; i < 2; ++i) parts(ffn_tiles(s.dtype, i ? s.dim : s.hidden, i ? s.hidden : s.dim, 3, 3, p.rows, 1, false));
     }
     p.part = take(part);
     p.bytes = o;
     return p;
 }
+// What a forward call saves: a, b, m.
+struct FfnSaved {
+    size_t b, m, bytes;
+    explicit FfnSaved(const FfnPlan& p) {
+        b = to256((size_t)p.m_plane * 4);
+        m = 2 * b;
+        bytes = m + to256((size_t)p.m_plane * p.terms * 2);
+    }
+};
 
-template <typename E, bool A_ALONG, bool B_ALONG, Epilogue EPI> void launch_product(const ProfSlot& ps, int edge, dim3 grid, const FfnArgs& a, hipStream_t st) {
-    if constexpr (sizeof(E) == 4) PQL_LAUNCH(ps, (ffn_product_kernel<E, 128, 128, 2, 4, A_ALONG, B_ALONG, EPI>), grid, dim3(512), 0, st, a);
-    else if (edge == 256) PQL_LAUNCH(ps, (ffn_product_kernel<E, 256, 256, 2, 4, A_ALONG, B_ALONG, EPI>), grid, dim3(512), 0, st, a);
-    else PQL_LAUNCH(ps, (ffn_product_kernel<E, 128, 128, 2, 2, A_ALONG, B_ALONG, EPI>), grid, dim3(256), 0, st, a);
+template <typename E, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, Epilogue EPI>
+hipError_t launch_product(const FfnTiles& t, const FfnArgs& a, int kid, double flops, hipStream_t st) {
+    ProfSlot ps = prof_slot();
+    const Shares sh(t.tiles, t.slots, t.steps);
+    // with rows that are counted on the device, fewer tiles may be shared out otherwise
+    const int grid = a.count ? t.tiles / t.slots * t.slots + t.slots : sh.whole + (sh.sharers + 7) / 8 * 8;
+    PQL_LAUNCH(ps, (ffn_product_kernel<E, BM, BN, WM, WN, A_ALONG, B_ALONG, EPI>), dim3(grid), dim3(64 * WM * WN), 0, st, a, t.slots);
+    prof_commit(ps, kid, flops, 0.0);
+    if (a.count ? t.steps > JOIN_STEPS : sh.joins()) {
+        const int blocks = (a.count ? t.slots : sh.rest) * (BM * (EPI == EPI_GATED ? BN / 2 : BN) / 8 / 256);
+        ps = prof_slot();
+        PQL_LAUNCH(ps, (ffn_join_kernel<E, BM, BN, EPI>), dim3(blocks < 1024 ? blocks : 1024), dim3(256), 0, st, a, t.slots, sizeof(E) == 4 ? 32 : 64);
+        prof_commit(ps, KID_FFN_JOIN, 0.0, 0.0);
+    }
+    return hipGetLastError();
 }
 
 struct FfnRun {
@@ -614,46 +806,34 @@ struct FfnRun {
     }
     FfnArgs args() const {
         FfnArgs a{};
-        a.segments = 1; a.splits = 1;
+        a.problems = 1; a.segments = 1;
         a.count = count; a.map = map; a.act = s.act;
         a.hidden_p = p.hidden_p; a.m_plane = p.m_plane;
+        a.part = at<float>(p.part);
         return a;
     }
-    // whole: problems of a full call, which the plan has counted with
-    template <bool A_ALONG, bool B_ALONG, Epilogue EPI> void product(FfnArgs& a, int problems, int whole, int kid) {
+    // of: the problems of a full call, which the plan has counted with.
+    template <bool A_ALONG, bool B_ALONG, Epilogue EPI> void product(const FfnArgs& a, int of, int kid) {
         if (e != hipSuccess) return;
         const FfnProblem& pr = a.prob[0];
-        const int edge = EPI == EPI_GATED ? tile_edge(s.dtype, pr.m, 2 * pr.n, 1) : tile_edge(s.dtype, pr.m, pr.n, whole);
-        const int each = (tiles_of(pr.m, edge) * tiles_of(pr.n, EPI == EPI_GATED ? edge / 2 : edge) + 7) / 8;           // problems are alike or transposed
-        const dim3 grid(each * 8, problems * a.splits);
-        const ProfSlot ps = prof_slot();
-        if (s.dtype == PQL_F32) launch_product<float, A_ALONG, B_ALONG, EPI>(ps, edge, grid, a, st);
-        else launch_product<bf16_t, A_ALONG, B_ALONG, EPI>(ps, edge, grid, a, st);
-        prof_commit(ps, kid, 2.0 * problems * (EPI == EPI_GATED ? 2 : 1) * a.segments * pr.m * pr.n * (double)a.k, 0.0);
-        e = hipGetLastError();
-    }
-    // The product of rows or weights, in parts where that fills the card.
-    template <bool A_ALONG, bool B_ALONG> void result(FfnArgs& a, int problems, int whole, int splits) {
-        a.splits = splits;
-        if (splits == 1) return product<A_ALONG, B_ALONG, EPI_OUT>(a, problems, whole, KID_FFN_PRODUCT);
-        a.part = at<float>(p.part);
-        a.part_stride = (int64_t)splits * a.prob[0].m * a.prob[0].n;
-        product<A_ALONG, B_ALONG, EPI_PART>(a, problems, whole, KID_FFN_PRODUCT);
-        if (e != hipSuccess) return;
-        const int64_t blocks = ((int64_t)a.prob[0].m * a.prob[0].n + 255) / 256;
-        const ProfSlot ps = prof_slot();
-        const dim3 grid((unsigned)(blocks < 1024 ? blocks : 1024), problems);
-        if (s.dtype == PQL_F32) PQL_LAUNCH(ps, ffn_join_kernel<float>, grid, dim3(256), 0, st, a);
-        else PQL_LAUNCH(ps, ffn_join_kernel<bf16_t>, grid, dim3(256), 0, st, a);
-        prof_commit(ps, KID_FFN_JOIN, 0.0, 4.0 * problems * splits * a.prob[0].m * a.prob[0].n);
-        e = hipGetLastError();
+        FfnTiles t = ffn_tiles(s.dtype, pr.m, pr.n, 1, of, a.k, a.segments, EPI == EPI_GATED);
+        t.tiles = 0;
+        for (int i = 0; i < a.problems; ++i)
+            t.tiles += tiles_of(a.prob[i].m, t.rows) * tiles_of(a.prob[i].n, EPI == EPI_GATED ? t.cols / 2 : t.cols);
+        const double flops = 2.0 * a.problems * (EPI == EPI_GATED ? 2 : 1) * a.segments * pr.m * pr.n * a.k;
+        if (s.dtype == PQL_F32)
+            e = t.rows == 256 ? launch_product<float, 256, 128, 2, 4, A_ALONG, B_ALONG, EPI>(t, a, kid, flops, st)
+                              : launch_product<float, 128, 128, 2, 4, A_ALONG, B_ALONG, EPI>(t, a, kid, flops, st);
+        else
+            e = t.rows == 256 ? launch_product<bf16_t, 256, 256, 2, 4, A_ALONG, B_ALONG, EPI>(t, a, kid, flops, st)
+                              : launch_product<bf16_t, 128, 128, 2, 2, A_ALONG, B_ALONG, EPI>(t, a, kid, flops, st);
     }
     void gated(const FfnOperand& x, const FfnOperand& gate, const FfnOperand& up, float* va, float* vb, bf16_t* m) {
         FfnArgs a = args();
         a.prob[0] = {{x, x}, {gate, up}, p.rows, s.hidden, nullptr, 0};
         a.k = s.dim;
         a.va = va; a.vb = vb; a.m = m;
-        product<true, true, EPI_GATED>(a, 1, 1, KID_FFN_GATED);
+        product<true, true, EPI_GATED>(a, 1, KID_FFN_GATED);
     }
 };
 
@@ -681,7 +861,7 @@ extern "C" {
 int64_t pql_ffn_saved_bytes(const pql_ffn_shape* s) {
     if (!s) return PQL_ERR_NULL;
     if (!ffn_ok(*s)) return PQL_ERR_INVALID_ARG;
-    return (int64_t)(2 * to256((size_t)ffn_rows(*s) * up8(s->hidden) * 4));
+    return (int64_t)FfnSaved(ffn_plan(*s, PQL_FFN_FORWARD)).bytes;
 }
 
 int64_t pql_ffn_workspace_bytes(const pql_ffn_shape* s, int32_t call) {
@@ -712,14 +892,14 @@ int32_t pql_ffn_forward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input*
         const FfnOperand down = r.operand(in->down, s->dim, s->hidden, p.down, p.down_plane, false);
         r.clear(*out);
         r.prepare();
-        bf16_t* m = r.at<bf16_t>(p.m);
-        float* va = (float*)saved;
-        r.gated(x, gate, up, va, saved ? (float*)((char*)saved + to256((size_t)p.m_plane * 4)) : nullptr, m);
+        const FfnSaved keep(p);
+        bf16_t* m = saved ? (bf16_t*)((char*)saved + keep.m) : r.at<bf16_t>(p.m);
+        r.gated(x, gate, up, (float*)saved, saved ? (float*)((char*)saved + keep.b) : nullptr, m);
         FfnArgs a = r.args();
         const FfnOperand om{m, p.hidden_p, p.m_plane};
         a.prob[0] = {{om, om}, {down, down}, p.rows, s->dim, out->data, out->stride};
         a.k = s->hidden;
-        r.result<true, true>(a, 1, 1, p.out_splits);
+        r.product<true, true, EPI_OUT>(a, 1, KID_FFN_PRODUCT);
         e = r.e;
     }
     return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_ffn_forward", e);
@@ -748,30 +928,26 @@ int32_t pql_ffn_backward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input
         dout = r.operand(*out_grad, rows, s->dim, p.dout, p.x_plane, true);
         FfnOperand gate, up;
         r.projections(*in, gate, up);
-        r.prepare();
-        r.copies.n = 0;
         const FfnOperand down = r.operand(in->down, s->dim, s->hidden, p.down, p.down_plane, false);
         if (g->x.data) r.clear(g->x);
         r.prepare();
-        float *va = (float*)saved, *vb = (float*)((char*)saved + to256((size_t)p.m_plane * 4));
-        if (!saved) {
-            va = r.at<float>(p.va); vb = r.at<float>(p.vb);
-            r.gated(x, gate, up, va, vb, nullptr);
-        }
-        m = {r.at<bf16_t>(p.m), p.hidden_p, p.m_plane};
+        const FfnSaved keep(p);
+        float *va = saved ? (float*)saved : r.at<float>(p.va), *vb = saved ? (float*)((char*)saved + keep.b) : r.at<float>(p.vb);
+        m = {saved ? (const bf16_t*)((const char*)saved + keep.m) : r.at<bf16_t>(p.m), p.hidden_p, p.m_plane};
+        if (!saved) r.gated(x, gate, up, va, vb, (bf16_t*)m.p);
         da = {r.at<bf16_t>(p.da), p.hidden_p, p.m_plane};
         db = {r.at<bf16_t>(p.db), p.hidden_p, p.m_plane};
         FfnArgs a = r.args();
         a.prob[0] = {{dout, dout}, {down, down}, rows, s->hidden, nullptr, 0};
         a.k = s->dim;
-        a.va = va; a.vb = vb; a.m = (bf16_t*)m.p; a.da = (bf16_t*)da.p; a.db = (bf16_t*)db.p;
-        r.product<true, false, EPI_BACK>(a, 1, 1, KID_FFN_BACK);
+        a.va = va; a.vb = vb; a.da = (bf16_t*)da.p; a.db = (bf16_t*)db.p;
+        r.product<true, false, EPI_BACK>(a, 1, KID_FFN_BACK);
         if (g->x.data) {
             a = r.args();
             a.prob[0] = {{da, db}, {gate, up}, rows, s->dim, g->x.data, g->x.stride};
             a.k = s->hidden;
             a.segments = 2;
-            r.result<true, false>(a, 1, 1, p.dx_splits);
+            r.product<true, false, EPI_OUT>(a, 1, KID_FFN_PRODUCT);
         }
     }
     FfnArgs w = r.args();
@@ -782,7 +958,8 @@ int32_t pql_ffn_backward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input
     w.k = rows;
     w.count_is_k = 1;
     w.map = nullptr;
-    if (n > 0) r.result<false, false>(w, n, 3, p.weight_splits);
+    w.problems = n;
+    if (n > 0) r.product<false, false, EPI_OUT>(w, 3, KID_FFN_PRODUCT);
     return r.e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_ffn_backward", r.e);
 }
 
