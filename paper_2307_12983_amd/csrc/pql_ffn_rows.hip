@@ -8,7 +8,13 @@
 namespace pql {
 namespace {
 
+
+// Wavefronts of a workgroup (one token through a block of 4096 and 16384 in bf16: 85.6 us a call, with 4 of them 89, with 16 90; twice as
+// many steps ahead change nothing).
 constexpr int WAVES = 8, NT = 64 * WAVES;
+// Weights of at most so many bytes stay in the caches: each 16 rows have workgroups of their own, which read them again
+// (64 rows through a block of 256 and 1024 in fp32: 11 us a call, 22 with one workgroup for all of them).
+constexpr double CACHED = 8 << 20;
 
 // ---- operands: lane l holds row l % 16, and CHUNK elements of the contraction from CHUNK (l / 16) on, of 4 CHUNK a step ----
 template <typename E> struct Frag;
@@ -65,7 +71,7 @@ template <typename E, int T, bool AL, bool GATED> __global__ void __launch_bound
     bool live[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-        const int n = t * 16 + r;
+        const int n = (blockIdx.y * T + t) * 16 + r;
         live[t] = n < a.rows && a.live(n);
         x[t] = GATED ? (const E*)a.x + (int64_t)(live[t] ? n : 0) * a.x_stride : (const E*)a.m + (int64_t)(live[t] ? n : 0) * a.m_stride;
     }
@@ -95,7 +101,7 @@ template <typename E, int T, bool AL, bool GATED> __global__ void __launch_bound
     __syncthreads();
     // results: column l % 16 is the row, outputs 4 (l / 16) .. + 3; one of them a thread
     for (int i = threadIdx.x; i < T * 256; i += NT) {
-        const int t = i >> 8, l = i >> 2 & 63, e = i & 3, n = t * 16 + (l & 15), out = blockIdx.x * 16 + (l >> 4) * 4 + e;
+        const int t = i >> 8, l = i >> 2 & 63, e = i & 3, n = (blockIdx.y * T + t) * 16 + (l & 15), out = blockIdx.x * 16 + (l >> 4) * 4 + e;
         float s[M];
 #pragma unroll
         for (int m = 0; m < M; ++m) {
@@ -114,24 +120,28 @@ template <typename E, int T, bool AL, bool GATED> __global__ void __launch_bound
     }
 }
 
-template <typename E, int T, bool GATED> void launch(const FfnRowsArgs& a, bool al, hipStream_t st) {
+template <typename E, int T, bool GATED> void launch(const FfnRowsArgs& a, bool al, int y, hipStream_t st) {
     const int outputs = GATED ? a.hidden : a.dim, size = GATED ? a.dim : a.hidden;
-    const dim3 grid((outputs + 15) / 16);
+    const dim3 grid((outputs + 15) / 16, y);
     const ProfSlot ps = prof_slot();
     if (al) PQL_LAUNCH(ps, (ffn_rows_kernel<E, T, true, GATED>), grid, dim3(NT), 0, st, a);
     else PQL_LAUNCH(ps, (ffn_rows_kernel<E, T, false, GATED>), grid, dim3(NT), 0, st, a);
     prof_commit(ps, KID_FFN_ROWS, 2.0 * (GATED ? 2 : 1) * a.rows * outputs * size, (double)(GATED ? 2 : 1) * outputs * size * sizeof(E));
 }
+template <typename E, bool GATED> void launch_rows(const FfnRowsArgs& a, bool al, hipStream_t st) {
+    const int tiles = (a.rows + 15) / 16;
+    const double bytes = (double)(GATED ? 2 : 1) * a.dim * a.hidden * sizeof(E);
+    if (tiles == 1) launch<E, 1, GATED>(a, al, 1, st);
+    else if (bytes <= CACHED) launch<E, 1, GATED>(a, al, tiles, st);
+    else if (tiles == 2) launch<E, 2, GATED>(a, al, 1, st);
+    else launch<E, 4, GATED>(a, al, 1, st);
+}
 template <typename E> hipError_t rows_of(const FfnRowsArgs& a, hipStream_t st) {
     const int32_t dt = sizeof(E) == 4 ? PQL_F32 : PQL_BF16;
     const int v = VEC_OF<E>;
     auto fits = [&](const void* p, int64_t stride) { return rows_aligned({(void*)p, stride}, dt); };
-    const bool al = a.dim % v == 0 && fits(a.x, a.x_stride) && fits(a.gate, a.gate_stride) && fits(a.up, a.up_stride);
-    const bool down = a.hidden % v == 0 && fits(a.m, a.m_stride) && fits(a.down, a.down_stride);
-    const int tiles = (a.rows + 15) / 16;
-    if (tiles == 1) { launch<E, 1, true>(a, al, st); launch<E, 1, false>(a, down, st); }
-    else if (tiles == 2) { launch<E, 2, true>(a, al, st); launch<E, 2, false>(a, down, st); }
-    else { launch<E, 4, true>(a, al, st); launch<E, 4, false>(a, down, st); }
+    launch_rows<E, true>(a, a.dim % v == 0 && fits(a.x, a.x_stride) && fits(a.gate, a.gate_stride) && fits(a.up, a.up_stride), st);
+    launch_rows<E, false>(a, a.hidden % v == 0 && fits(a.m, a.m_stride) && fits(a.down, a.down_stride), st);
     return hipGetLastError();
 }
 
