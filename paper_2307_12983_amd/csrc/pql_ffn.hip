@@ -699,7 +699,8 @@ FfnPlan ffn_plan(const pql_ffn_shape& s, int call) {
     p.down = planes(p.down_plane);
     if (call != PQL_FFN_BACKWARD) {
         parts(ffn_tiles(s.dtype, p.rows, s.hidden, 1, 1, s.dim, 1, true));
-        p.m = planes(p.m_plane);
+        // the kernels for few rows keep two terms
+        p.m = take((size_t)p.m_plane * 2 * (p.terms == 1 && call == PQL_FFN_FORWARD && p.rows <= FFN_FEW_ROWS ? 2 : p.terms));
     }
     if (call == PQL_FFN_FORWARD) {
         parts(ffn_tiles(s.dtype, p.rows, s.dim, 1, 1, s.hidden, 1, false));
@@ -881,7 +882,7 @@ int32_t pql_ffn_forward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input*
     hipError_t e;
     if (p.rows <= FFN_FEW_ROWS && !saved) {
         FfnRowsArgs a{{in->lengths, (unsigned)s->steps}, p.rows, s->dim, s->hidden, s->act, in->x.data, in->gate.data, in->up.data, in->down.data,
-                      in->x.stride, in->gate.stride, in->up.stride, in->down.stride, (char*)workspace + p.m, p.hidden_p, out->data, out->stride};
+                      in->x.stride, in->gate.stride, in->up.stride, in->down.stride, (char*)workspace + p.m, p.hidden_p, p.m_plane, out->data, out->stride};
         e = ffn_rows_launch(a, s->dtype, st);
     } else {
         FfnRun r{*s, p, (char*)workspace, st};

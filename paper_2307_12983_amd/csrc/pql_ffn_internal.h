@@ -41,7 +41,7 @@ struct FfnRowsArgs {
     int rows, dim, hidden, act;
     const void *x, *gate, *up, *down;
     int64_t x_stride, gate_stride, up_stride, down_stride;
-    void* m; int64_t m_stride;                  // [rows][m_stride], of the tokens' type
+    void* m; int64_t m_stride, m_plane;         // [rows][m_stride] of the tokens' type; bf16: two planes of terms
     void* out; int64_t out_stride;
 };
 hipError_t ffn_rows_launch(const FfnRowsArgs& a, int32_t dtype, hipStream_t st);

@@ -2,7 +2,8 @@
 //
 // A workgroup takes 16 outputs of a projection and all rows, its wavefronts each a part of the contraction; weights go from
 // memory to the matrix instructions' registers without LDS between (nothing of them is used twice), 16 bytes a lane, the rows
-// come from the caches.  Two launches: both projections, the activation and the product, then the last projection.
+// come from the caches.  Two launches: both projections, the activation and the product, then the last projection.  In bf16 the
+// product between them is kept as two bf16 terms (16 bits): a second product on weights that are there costs no time.
 #include "pql_ffn_internal.h"
 
 namespace pql {
@@ -17,6 +18,7 @@ constexpr int WAVES = 8, NT = 64 * WAVES;
 constexpr double CACHED = 8 << 20;
 
 // ---- operands: lane l holds row l % 16, and CHUNK elements of the contraction from CHUNK (l / 16) on, of 4 CHUNK a step ----
+template <typename E> constexpr int M_TERMS = sizeof(E) == 2 ? 2 : 1;     // of the product between the two launches
 template <typename E> struct Frag;
 template <> struct Frag<bf16_t> {
     static constexpr int CHUNK = 8;
@@ -75,23 +77,28 @@ template <typename E, int T, bool AL, bool GATED> __global__ void __launch_bound
         live[t] = n < a.rows && a.live(n);
         x[t] = GATED ? (const E*)a.x + (int64_t)(live[t] ? n : 0) * a.x_stride : (const E*)a.m + (int64_t)(live[t] ? n : 0) * a.m_stride;
     }
+    constexpr int X = GATED ? 1 : M_TERMS<E>;
     floatx4 acc[M][T] = {};
     // the wavefronts take turns of AHEAD steps, all of whose loads go out together
     for (int k = wave * AHEAD * STEP; k < size; k += WAVES * AHEAD * STEP) {
-        Frag<E> wf[AHEAD][M], xf[AHEAD][T];
+        Frag<E> wf[AHEAD][M], xf[AHEAD][X][T];
 #pragma unroll
         for (int s = 0; s < AHEAD; ++s) {
 #pragma unroll
             for (int m = 0; m < M; ++m) wf[s][m] = fetch<E, AL>(w[m], true, k + s * STEP + k0, size);
 #pragma unroll
-            for (int t = 0; t < T; ++t) xf[s][t] = fetch<E, AL>(x[t], live[t], k + s * STEP + k0, size);
+            for (int q = 0; q < X; ++q)
+#pragma unroll
+                for (int t = 0; t < T; ++t) xf[s][q][t] = fetch<E, AL>(x[t] + q * a.m_plane, live[t], k + s * STEP + k0, size);
         }
 #pragma unroll
         for (int s = 0; s < AHEAD; ++s)
 #pragma unroll
             for (int m = 0; m < M; ++m)
 #pragma unroll
-                for (int t = 0; t < T; ++t) product(acc[m][t], wf[s][m], xf[s][t]);
+                for (int t = 0; t < T; ++t)
+#pragma unroll
+                    for (int q = X - 1; q >= 0; --q) product(acc[m][t], wf[s][m], xf[s][q][t]);
     }
     settle_products();
 #pragma unroll
@@ -113,7 +120,12 @@ template <typename E, int T, bool AL, bool GATED> __global__ void __launch_bound
         if constexpr (GATED) {
             float f[1] = {s[0]}, d[1];
             activate_all<E>(a.act, f, f, d);
-            ((E*)a.m)[(int64_t)n * a.m_stride + out] = from_float<E>(f[0] * s[M - 1]);
+            E* p = (E*)a.m + (int64_t)n * a.m_stride + out;
+            const float m = f[0] * s[M - 1];
+            const E high = from_float<E>(m);
+            p[0] = high;
+            // an infinite term has no rest
+            if constexpr (M_TERMS<E> == 2) p[a.m_plane] = from_float<E>(fabsf(to_float(high)) < __builtin_inff() ? m - to_float(high) : 0.f);
         } else {
             ((E*)a.out)[(int64_t)n * a.out_stride + out] = from_float<E>(a.live(n) ? s[0] : 0.f);
         }
