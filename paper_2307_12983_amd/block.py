@@ -100,10 +100,33 @@ class Rows:
         n, stride = (t.shape[0], t.stride(0)) if t.dim() == 2 or t.shape[1] == 1 else (t.shape[0] * t.shape[1], t.stride(1))
         if t.dim() == 3 and t.shape[0] > 1 and t.shape[1] > 1 and t.stride(0) != t.shape[1] * stride and t.numel() > 0:
             raise ValueError("the rows of a token tensor must be equally far apart")
-        self.tensor = t
+        self.tensor, self.dev = t, t.get_device()
         self.key = (n, cols, S.dtype_code(t))
         self.c = PqlRows(t.data_ptr(), stride if n > 1 else cols)
         self.ref = C.byref(self.c)
+
+
+def _one_device(what, *tensors):
+    devices = {t.get_device() for t in tensors if t is not None}
+    if len(devices) > 1:
+        raise ValueError("%s: tensors of different devices" % what)
+    return devices.pop() if devices else None
+
+
+def _stream(stream, *devices):
+    """The stream's handle; what a call is given has to lie on its device (the current one's stream, if it is None)."""
+    if stream is None:
+        import torch
+        stream = torch.cuda.current_stream()
+    here = getattr(stream, "device_index", None)
+    for d in devices:
+        if d is not None and (d < 0 or here is not None and d != here):
+            raise ValueError("tensors of another device than the stream's")
+    return B._stream(stream)
+
+
+def _dev(*tensors):
+    return [t.get_device() for t in tensors if t is not None]
 
 
 NONE = PqlRows(None, 0)
@@ -167,6 +190,7 @@ class _Residual:
         n, dim, dtype = shape.batch * shape.steps, shape.dim, shape.dtype
         self.key = (n, dim, dtype)
         self.tensors = (x, y, gate, post, pre)
+        self.dev = _one_device(what, *self.tensors)
         self.c = struct()
         self.c.x = _rows(x, self.key, what + ": x")
         self.c.y = _rows(y, self.key, what + ": y")
@@ -184,6 +208,7 @@ class ResidualInput(_Residual):
         super().__init__(PqlResidualInput, shape, x, y, gate, post, pre, "ResidualInput")
         self.lengths = lengths
         self.c.lengths = _ints(lengths, shape.batch, "ResidualInput: lengths")
+        _one_device("ResidualInput", x, y, lengths)
 
 
 class ResidualGrad(_Residual):
@@ -205,6 +230,7 @@ class _Ffn:
         n, dim, hidden, dtype = shape.batch * shape.steps, shape.dim, shape.hidden, shape.dtype
         self.key = (n, dim, dtype)
         self.tensors = (x, gate, up, down)
+        self.dev = _one_device(what, *self.tensors)
         self.c = struct()
         self.c.x = _rows(x, self.key, what + ": x")
         self.c.gate = _rows(gate, (hidden, dim, dtype), what + ": gate")
@@ -222,6 +248,7 @@ class FfnInput(_Ffn):
         super().__init__(PqlFfnInput, shape, x, gate, up, down, "FfnInput")
         self.lengths = lengths
         self.c.lengths = _ints(lengths, shape.batch, "FfnInput: lengths")
+        _one_device("FfnInput", x, lengths)
 
 
 class FfnGrad(_Ffn):
@@ -259,11 +286,14 @@ class BlockContext(S.StudentContext):
                 _ref(table, (s.vocab, s.dim, s.dtype), "table"), _ref(out, (n, s.dim, s.dtype), "rows"))
 
     def pql_embed_forward(self, shape, tokens, lengths, table: Rows, out: Rows, stream=None):
-        self._check(self.lib.pql_embed_forward(self.h, *self._embed(shape, tokens, lengths, table, out), B._stream(stream)))
+        given = self._embed(shape, tokens, lengths, table, out)
+        stream = _stream(stream, tokens.get_device(), table.dev, out.dev, *_dev(lengths))
+        self._check(self.lib.pql_embed_forward(self.h, *given, stream))
 
     def pql_embed_backward(self, shape, tokens, lengths, out_grad: Rows, table_grad: Rows, workspace, stream=None):
         s, t, n, table, rows = self._embed(shape, tokens, lengths, table_grad, out_grad)
-        self._check(self.lib.pql_embed_backward(self.h, s, t, n, rows, table, B._ptr(workspace), B._stream(stream)))
+        stream = _stream(stream, tokens.get_device(), out_grad.dev, table_grad.dev, *_dev(lengths, workspace))
+        self._check(self.lib.pql_embed_backward(self.h, s, t, n, rows, table, B._ptr(workspace), stream))
 
     @staticmethod
     def _of(shape, *described):
@@ -273,22 +303,25 @@ class BlockContext(S.StudentContext):
 
     def pql_residual_forward(self, shape, given: ResidualInput, sum: Rows, next: Rows, stream=None):
         self._of(shape, given)
-        self._check(self.lib.pql_residual_forward(self.h, C.byref(shape), given.ref, _ref(sum, given.key, "sum"),
-                                                  _ref(next, given.key, "next"), B._stream(stream)))
+        total, after = _ref(sum, given.key, "sum"), _ref(next, given.key, "next")
+        stream = _stream(stream, given.dev, *(r.dev for r in (sum, next) if r is not None))
+        self._check(self.lib.pql_residual_forward(self.h, C.byref(shape), given.ref, total, after, stream))
 
     def pql_residual_backward(self, shape, given: ResidualInput, sum_grad: Rows, next_grad: Rows, grads: ResidualGrad, workspace,
                               stream=None):
         self._of(shape, given, grads)
-        self._check(self.lib.pql_residual_backward(self.h, C.byref(shape), given.ref, _ref(sum_grad, given.key, "sum_grad"),
-                                                   _ref(next_grad, given.key, "next_grad"), grads.ref, B._ptr(workspace),
-                                                   B._stream(stream)))
+        total, after = _ref(sum_grad, given.key, "sum_grad"), _ref(next_grad, given.key, "next_grad")
+        stream = _stream(stream, given.dev, grads.dev, *(r.dev for r in (sum_grad, next_grad) if r is not None), *_dev(workspace))
+        self._check(self.lib.pql_residual_backward(self.h, C.byref(shape), given.ref, total, after, grads.ref, B._ptr(workspace), stream))
 
     def pql_ffn_forward(self, shape, given: FfnInput, out: Rows, saved, workspace, stream=None):
         self._of(shape, given)
-        self._check(self.lib.pql_ffn_forward(self.h, C.byref(shape), given.ref, _ref(out, given.key, "out"), B._ptr(saved),
-                                             B._ptr(workspace), B._stream(stream)))
+        rows = _ref(out, given.key, "out")
+        stream = _stream(stream, given.dev, *(() if out is None else (out.dev,)), *_dev(saved, workspace))
+        self._check(self.lib.pql_ffn_forward(self.h, C.byref(shape), given.ref, rows, B._ptr(saved), B._ptr(workspace), stream))
 
     def pql_ffn_backward(self, shape, given: FfnInput, saved, out_grad: Rows, grads: FfnGrad, workspace, stream=None):
         self._of(shape, given, grads)
-        self._check(self.lib.pql_ffn_backward(self.h, C.byref(shape), given.ref, B._ptr(saved), _ref(out_grad, given.key, "out_grad"),
-                                              grads.ref, B._ptr(workspace), B._stream(stream)))
+        rows = _ref(out_grad, given.key, "out_grad")
+        stream = _stream(stream, given.dev, grads.dev, *(() if out_grad is None else (out_grad.dev,)), *_dev(saved, workspace))
+        self._check(self.lib.pql_ffn_backward(self.h, C.byref(shape), given.ref, B._ptr(saved), rows, grads.ref, B._ptr(workspace), stream))

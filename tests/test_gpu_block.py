@@ -496,3 +496,212 @@ def test_feed_forward_gradients_that_are_not_asked_for(env):
         for k, g in call.backward(saved, leave).items():
             assert (g is None) == (k in leave)
             assert g is None or env[0].equal(g, whole[k]), k
+
+
+# ---- calls as programs make them ---------------------------------------------------------------------------------
+def every_call(env, dtype="bfloat16", lengths=(40, 7, 0, 33), seed=7):
+    """One of each call on inputs of its own, as (run, inputs, outputs): run(stream) writes the outputs from the inputs."""
+    torch, K, ctx = env
+    lengths = None if lengths is None else list(lengths)
+    made, tokens, _, table, out_grad, lens = embed_inputs(env, (4, 40, 3, 90, 136, dtype, "dense", lengths, "any"), seed)
+    shape = K.embed_shape(tokens, table, 0.5)
+    out, dtable, space = torch.empty_like(out_grad), torch.empty_like(table), K.workspace(ctx.embed_workspace_bytes(shape))
+
+    def embed(stream=None):
+        ctx.pql_embed_forward(shape, tokens, lens, K.Rows(table), K.Rows(out), stream)
+        ctx.pql_embed_backward(shape, tokens, lens, K.Rows(out_grad), K.Rows(dtable), space, stream)
+    yield embed, [table, out_grad], [out, dtable]
+
+    r = ResidualCall(env, residual_case(4, 40, 136, dtype, groups=2, lengths=lengths), seed)
+    total, after = r.outs()
+    grads = {k: torch.empty_like(getattr(r, k)) for k in ("x", "y", "gate", "post", "pre")}
+    rgrad, rspace = K.ResidualGrad(r.shape, **grads), K.workspace(ctx.residual_workspace_bytes(r.shape))
+
+    def residual(stream=None):
+        ctx.pql_residual_forward(r.shape, r.given, K.Rows(total), K.Rows(after), stream)
+        ctx.pql_residual_backward(r.shape, r.given, K.Rows(r.sum_grad), K.Rows(r.next_grad), rgrad, rspace, stream)
+    yield residual, [r.x, r.y, r.gate], [total, after, *grads.values()]
+
+    f = FfnCall(env, (4, 40, 136, 264, dtype, "silu", "dense", lengths), seed)
+    result, fgrads = torch.empty_like(f.x), {k: torch.empty_like(getattr(f, k)) for k in ("x", "gate", "up", "down")}
+    fgrad, saved = K.FfnGrad(f.shape, **fgrads), K.workspace(ctx.ffn_saved_bytes(f.shape))
+    fspace = K.workspace(max(ctx.ffn_workspace_bytes(f.shape, c) for c in (K.FFN_FORWARD, K.FFN_BACKWARD)))
+
+    def ffn(stream=None):
+        ctx.pql_ffn_forward(f.shape, f.given, K.Rows(result), saved, fspace, stream)
+        ctx.pql_ffn_backward(f.shape, f.given, saved, K.Rows(f.out_grad), fgrad, fspace, stream)
+    yield ffn, [f.x, f.gate, f.out_grad], [result, *fgrads.values()]
+
+    few = FfnCall(env, (10, 1, 136, 264, dtype, "silu", "dense", None), seed)
+    one, space1 = torch.empty_like(few.x), K.workspace(ctx.ffn_workspace_bytes(few.shape, K.FFN_FORWARD))
+    yield (lambda stream=None: ctx.pql_ffn_forward(few.shape, few.given, K.Rows(one), None, space1, stream)), [few.x, few.gate], [one]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_calls_repeat_bit_for_bit_on_another_stream_and_in_graphs(env, dtype):
+    torch = env[0]
+    for run, inputs, outputs in every_call(env, dtype):
+        run()
+        first = [x.clone() for x in outputs]
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        for x in outputs:
+            x.fill_(7)
+        stream.wait_stream(torch.cuda.current_stream())
+        run(stream)
+        stream.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first, outputs))
+        # two graphs that share the call's workspace, replayed in turn, with eager work and other inputs between
+        graphs = []
+        for _ in range(2):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1]):
+                run()
+        for i in range(4):
+            for x in inputs:
+                x.mul_(1.25)
+            run()
+            want = [x.clone() for x in outputs]
+            for x in outputs:
+                x.zero_()
+            graphs[i % 2].replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, outputs)), i
+
+
+def test_calls_of_two_contexts_at_once(env):
+    """Two streams, contexts and workspaces: the calls of one do not meet those of the other."""
+    torch, K, _ = env
+    sets = [list(every_call((torch, K, K.BlockContext()), "float32", seed=s)) for s in (1, 2)]
+    for calls in sets:
+        for run, _, _ in calls:
+            run()
+    torch.cuda.synchronize()
+    want = [[[x.clone() for x in outputs] for _, _, outputs in calls] for calls in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    for calls in sets:
+        for _, _, outputs in calls:
+            for x in outputs:
+                x.zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i in range(len(sets[0])):
+            for calls, stream in zip(sets, streams):
+                calls[i][0](stream)
+    torch.cuda.synchronize()
+    for calls, kept in zip(sets, want):
+        for (_, _, outputs), w in zip(calls, kept):
+            assert all(torch.equal(a, b) for a, b in zip(w, outputs))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan"), 3.0e38])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_values_that_are_not_finite_stay_in_their_row(env, dtype, bad):
+    """Of tokens' results; the weights' gradients are sums over all rows."""
+    torch, K, ctx = env
+    for rows in ((4, 40), (10, 1)):
+        f, clean = (FfnCall(env, (*rows, 136, 264, dtype, "silu", "dense", None), 5) for _ in range(2))
+        f.x[1, 0, 3] = bad
+        keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+        keep[1, 0] = False
+        for save in (False, True):
+            (a, sa), (b, sb) = f.forward(save), clean.forward(save)
+            assert torch.equal(a[keep], b[keep])
+        assert torch.equal(f.backward(sa)["x"][keep], clean.backward(sb)["x"][keep])
+    r, clean = (ResidualCall(env, residual_case(4, 40, 136, dtype, groups=2), 5) for _ in range(2))
+    r.y[1, 0, 3] = bad
+    keep = torch.ones(4, 40, dtype=torch.bool, device="cuda")
+    keep[1, 0] = False
+    assert all(torch.equal(a[keep], b[keep]) for a, b in zip(r.forward(), clean.forward()))
+    got, want = r.backward(), clean.backward()
+    assert all(torch.equal(got[k][keep], want[k][keep]) for k in ("x", "y", "gate"))
+
+
+def test_values_of_any_size_in_three_terms(env):
+    """fp32 values of very different sizes: each product is as exact as in fp32, relative to the sum of the terms' sizes."""
+    torch, K, ctx = env
+    rng = np.random.default_rng(3)
+    d, f = 128, 64
+    spread = lambda *s: rng.standard_normal(s) * 10.0 ** rng.uniform(-12, 12, s)  # noqa: E731
+    dev = lambda x: torch.tensor(x).float().cuda()  # noqa: E731
+    x, gate, up, down = dev(spread(1, 100, d)), dev(1e-14 * rng.standard_normal((f, d))), dev(spread(f, d)), dev(spread(d, f))
+    shape = K.ffn_shape(x, gate, "none")
+    out = torch.empty_like(x)
+    ctx.pql_ffn_forward(shape, K.FfnInput(shape, x, gate, up, down), K.Rows(out), K.workspace(ctx.ffn_saved_bytes(shape)),
+                        K.workspace(ctx.ffn_workspace_bytes(shape, K.FFN_FORWARD)))
+    h = [t.double().cpu().numpy() for t in (x, gate, up, down)]
+    size = (np.abs(h[0]) @ np.abs(h[1]).T * (np.abs(h[0]) @ np.abs(h[2]).T)) @ np.abs(h[3]).T
+    # three products of at most 128 terms, each off by 128 roundings and the three left out terms
+    assert np.all(np.abs(out.double().cpu().numpy() - O.ffn(*h, "none")) <= 3 * (128 + 4) * U * size)
+
+
+def test_places_further_apart_than_32_bits_reach(env):
+    torch, K, ctx = env
+    # a table of 2^31 elements and more
+    vocab, dim = 70000, 32768
+    table = torch.empty(vocab, dim, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([[0], [vocab - 1], [35000], [vocab - 1]], dtype=torch.int32, device="cuda").view(1, 4, 1)
+    table[0], table[vocab - 1], table[35000] = 1, 2, 3
+    out = torch.empty(1, 4, dim, dtype=torch.bfloat16, device="cuda")
+    shape = K.embed_shape(at, table, 0.5)
+    ctx.pql_embed_forward(shape, at, None, K.Rows(table), K.Rows(out))
+    assert [float(out[0, i].min()) for i in range(4)] == [0.5, 1.0, 1.5, 1.0] == [float(out[0, i].max()) for i in range(4)]
+    ctx.pql_embed_backward(shape, at, None, K.Rows(out), K.Rows(table), K.workspace(ctx.embed_workspace_bytes(shape)))
+    rows = table.float().sum(1)
+    want = torch.zeros_like(rows)
+    want[0], want[vocab - 1], want[35000] = 0.25 * dim, dim, 0.75 * dim
+    assert torch.equal(rows, want)
+    del table
+    # rows 2^20 elements apart, 2100 of them
+    big = torch.empty(2100 * (1 << 20), dtype=torch.bfloat16, device="cuda")
+    far = big.as_strided((2100, 1, 64), (1 << 20, 1 << 20, 1))
+    near = torch.randn(2100, 1, 64, device="cuda").bfloat16()
+    far.copy_(near)
+    weights = [torch.randn(*s, device="cuda").mul_(0.1).bfloat16() for s in ((64, 64), (64, 64), (64, 64))]
+    shape = K.ffn_shape(near, weights[0], "silu")
+    given = [K.FfnInput(shape, x, *weights) for x in (near, far)]
+    outs = [torch.empty_like(near) for _ in range(2)]
+    grads = [[torch.empty_like(t) for t in (near, *weights)] for _ in range(2)]
+    do = torch.randn_like(near)
+    for g, o, dg in zip(given, outs, grads):
+        ctx.pql_ffn_forward(shape, g, K.Rows(o), None, K.workspace(ctx.ffn_workspace_bytes(shape, K.FFN_FORWARD)))
+        ctx.pql_ffn_backward(shape, g, None, K.Rows(do), K.FfnGrad(shape, *dg), K.workspace(ctx.ffn_workspace_bytes(shape, K.FFN_BACKWARD_ALONE)))
+    assert torch.equal(*outs) and all(torch.equal(a, b) for a, b in zip(*grads))
+    shape = K.residual_shape(2100, 1, 64, torch.bfloat16, eps_pre=1e-5)
+    results = [torch.empty_like(near) for _ in range(2)]
+    for x, o in zip((near, far), results):
+        ctx.pql_residual_forward(shape, K.ResidualInput(shape, x), None, K.Rows(o))
+    assert torch.equal(*results)
+    ctx.pql_residual_forward(shape, K.ResidualInput(shape, near), None, K.Rows(far))
+    assert torch.equal(far, results[0])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_rows_calls_leave_what_is_not_theirs(env, dtype):
+    """Neither the gaps between rows nor what lies behind the last one are written, by results or gradients."""
+    torch, K, ctx = env
+    dt = getattr(torch, dtype)
+
+    def framed(n, cols):
+        big = torch.full((n + 3, cols + 16), 7.0, dtype=dt, device="cuda")
+        return big, big[:n, 8:8 + cols]
+
+    for cols, hidden in ((136, 264), (61, 35)):
+        for rows in (12, 150):                          # few rows, tiles
+            x, do = (torch.randn(rows, 1, cols, device="cuda").to(dt) for _ in range(2))
+            weights = [torch.randn(*s, device="cuda").mul_(0.1).to(dt) for s in ((hidden, cols), (hidden, cols), (cols, hidden))]
+            shape = K.ffn_shape(x, weights[0], "silu")
+            given = K.FfnInput(shape, x, *weights)
+            out, grads = framed(rows, cols), [framed(rows, cols), framed(hidden, cols), framed(hidden, cols), framed(cols, hidden)]
+            ctx.pql_ffn_forward(shape, given, K.Rows(out[1]), None, K.workspace(ctx.ffn_workspace_bytes(shape, K.FFN_FORWARD)))
+            ctx.pql_ffn_backward(shape, given, None, K.Rows(do), K.FfnGrad(shape, *[g[1] for g in grads]),
+                                 K.workspace(ctx.ffn_workspace_bytes(shape, K.FFN_BACKWARD_ALONE)))
+            shape = K.residual_shape(rows, 1, cols, dt, gate_cols=cols, gate_act="silu", eps_post=1e-5, eps_pre=1e-5)
+            given = K.ResidualInput(shape, x, do, x)
+            more = [framed(rows, cols) for _ in range(5)]
+            ctx.pql_residual_forward(shape, given, K.Rows(more[0][1]), K.Rows(more[1][1]))
+            ctx.pql_residual_backward(shape, given, K.Rows(do), K.Rows(x), K.ResidualGrad(shape, *[m[1] for m in more[2:]]), None)
+            for big, inner in [out] + grads + more:
+                n, c = inner.shape
+                assert bool((big[n:] == 7).all()) and bool((big[:, :8] == 7).all()) and bool((big[:, 8 + c:] == 7).all())
+                assert not bool((inner == 7).all(1).any())
