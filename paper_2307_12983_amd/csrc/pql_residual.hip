@@ -158,8 +158,13 @@ template <typename E, bool AL, bool BACK> struct Row {
     }
 };
 
+// Wavefronts a SIMD: what registers allow where rows are read 16 bytes at a time, less by one than without a bound on them; more spill
+// (8192 rows of 2048, half of them counting, bf16: gradient 72 us with two, 57 with three, 92 with four; 16384 rows of 1024 forward 41 us with
+// four, 37 with five).
+constexpr int wavefronts(bool al, int threads, bool back) { return threads == 1024 ? 4 : back ? (al ? 3 : 2) : (al ? 5 : 4); }
+
 // ---- forward ---------------------------------------------------------------------------------------
-template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT) residual_kernel(ResidualArgs a) {
+template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT, wavefronts(AL, NT, false)) residual_kernel(ResidualArgs a) {
     constexpr bool KEEP = NT < 1024;        // the weights, between rows: 1024 threads have 128 registers each
     __shared__ float lds[2 * 16], units[2 * 1024];
     const int unit = threadIdx.x / a.lanes, group = unit % a.groups, slot = unit / a.groups, slots = (int)blockDim.x / (a.lanes * a.groups);
@@ -221,7 +226,7 @@ template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT) res
 }
 
 // ---- gradient --------------------------------------------------------------------------------------
-template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT) residual_back_kernel(ResidualArgs a) {
+template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT, wavefronts(AL, NT, true)) residual_back_kernel(ResidualArgs a) {
     constexpr bool KEEP = NT < 1024;        // the weights, between rows: 1024 threads have 128 registers each
     __shared__ float lds[2 * 16], units[2 * 1024];
     const int unit = threadIdx.x / a.lanes, group = unit % a.groups, slot = unit / a.groups, slots = (int)blockDim.x / (a.lanes * a.groups);
@@ -391,14 +396,16 @@ bool residual_ok(const pql_residual_shape& s) {
 unsigned residual_rows(const pql_residual_shape& s) { return (unsigned)((int64_t)s.batch * s.steps); }
 
 struct ResidualPlan { int lanes, threads, slots; unsigned grid; };
-ResidualPlan residual_plan(const pql_residual_shape& s, bool back) {
+// As many workgroups as run at a time: they stay for several rows.
+ResidualPlan residual_plan(const pql_residual_shape& s, bool back, bool al) {
     ResidualPlan p{};
     p.lanes = part_lanes(s);
     const int threads = p.lanes * s.groups;
     p.threads = threads <= 256 ? 256 : (threads + 63) / 64 * 64;
     p.slots = p.threads / threads;
     const unsigned rows = residual_rows(s), all = (rows + p.slots - 1) / p.slots;
-    const unsigned most = (back ? 512u : 1024u) * 256u / p.threads;
+    const int of = p.threads <= 256 ? 256 : p.threads <= 512 ? 512 : 1024;
+    const unsigned most = 256u * (wavefronts(al, of, back) * 256 / of);
     p.grid = all < most ? all : most;
     return p;
 }
@@ -423,11 +430,11 @@ int32_t residual_check(pql_ctx* c, const pql_residual_shape* s, const pql_residu
         return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_residual: misaligned pointer");
     return PQL_OK;
 }
-ResidualArgs residual_args(const pql_residual_shape& s, const pql_residual_input& in, const pql_rows& sum, const pql_rows& next, const ResidualPlan& p) {
+ResidualArgs residual_args(const pql_residual_shape& s, const pql_residual_input& in, const pql_rows& sum, const pql_rows& next) {
     ResidualArgs a{};
     a.live = {in.lengths, (unsigned)s.steps};
     a.rows = residual_rows(s);
-    a.dim = s.dim; a.groups = s.groups; a.part = s.dim / s.groups; a.lanes = p.lanes;
+    a.dim = s.dim; a.groups = s.groups; a.part = s.dim / s.groups; a.lanes = part_lanes(s);
     a.gate_act = s.gate_act; a.gate_part = s.gate_cols != s.dim;
     a.eps_post = s.eps_post; a.eps_pre = s.eps_pre; a.scale_x = s.scale_x; a.scale_y = s.scale_y;
     a.x = in.x.data; a.x_stride = in.x.stride;
@@ -463,8 +470,9 @@ template <typename E, bool AL> hipError_t residual_launch(const ResidualArgs& a,
     }
     return hipGetLastError();
 }
-hipError_t residual_run(const pql_residual_shape& s, const ResidualArgs& a, const ResidualPlan& p, bool back, hipStream_t st) {
+hipError_t residual_run(const pql_residual_shape& s, const ResidualArgs& a, bool back, hipStream_t st) {
     const bool al = residual_aligned(s, a);
+    const ResidualPlan p = residual_plan(s, back, al);
     if (s.dtype == PQL_F32) return al ? residual_launch<float, true>(a, p, back, st) : residual_launch<float, false>(a, p, back, st);
     return al ? residual_launch<bf16_t, true>(a, p, back, st) : residual_launch<bf16_t, false>(a, p, back, st);
 }
@@ -480,16 +488,14 @@ int32_t pql_residual_forward(pql_ctx* c, const pql_residual_shape* s, const pql_
     if (!c) return PQL_ERR_NULL;
     const int32_t rc = residual_check(c, s, in, sum, next, false);
     if (rc != PQL_OK || residual_rows(*s) == 0) return rc;
-    const ResidualPlan p = residual_plan(*s, false);
-    const hipError_t e = residual_run(*s, residual_args(*s, *in, *sum, *next, p), p, false, (hipStream_t)stream);
+    const hipError_t e = residual_run(*s, residual_args(*s, *in, *sum, *next), false, (hipStream_t)stream);
     return e == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_residual_forward", e);
 }
 
 int64_t pql_residual_workspace_bytes(const pql_residual_shape* s) {
     if (!s) return PQL_ERR_NULL;
     if (!residual_ok(*s)) return PQL_ERR_INVALID_ARG;
-    const ResidualPlan p = residual_plan(*s, true);
-    return (int64_t)to256((size_t)p.grid * 2 * s->dim * 4);
+    return (int64_t)to256((size_t)residual_plan(*s, true, true).grid * 2 * s->dim * 4);         // fewer workgroups where rows are not aligned
 }
 
 int32_t pql_residual_backward(pql_ctx* c, const pql_residual_shape* s, const pql_residual_input* in, const pql_rows* sum_grad,
@@ -512,21 +518,22 @@ int32_t pql_residual_backward(pql_ctx* c, const pql_residual_shape* s, const pql
     if (off_by(g->x.data, e) || off_by(g->y.data, e) || off_by(g->gate.data, e) || off_by(g->post, 4) || off_by(g->pre, 4) || off_by(workspace, 256))
         return ctx_fail(c, PQL_ERR_ALIGNMENT, "pql_residual_backward: misaligned pointer");
     const hipStream_t st = (hipStream_t)stream;
-    const ResidualPlan p = residual_plan(*s, true);
     hipError_t err = hipSuccess;
+    unsigned parts = 0;
     if (rows > 0) {
-        ResidualArgs a = residual_args(*s, *in, *sum_grad, *next_grad, p);
+        ResidualArgs a = residual_args(*s, *in, *sum_grad, *next_grad);
         a.dx = g->x.data; a.dx_stride = g->x.stride;
         a.dy = g->y.data; a.dy_stride = g->y.stride;
         a.dgate = g->gate.data; a.dgate_stride = g->gate.stride;
         if (weights) a.partial = (float*)workspace;
-        err = residual_run(*s, a, p, true, st);
+        parts = residual_plan(*s, true, residual_aligned(*s, a)).grid;
+        err = residual_run(*s, a, true, st);
     }
     if (err == hipSuccess && weights) {
         const ProfSlot ps = prof_slot();
         PQL_LAUNCH(ps, residual_join_kernel, dim3((2 * s->dim + 63) / 64), dim3(1024), 0, st, (const float*)workspace,
-                   rows > 0 ? (int)p.grid : 0, (int)s->dim, g->post, g->pre);
-        prof_commit(ps, KID_RESIDUAL_JOIN, 0.0, 8.0 * p.grid * s->dim);
+                   (int)parts, (int)s->dim, g->post, g->pre);
+        prof_commit(ps, KID_RESIDUAL_JOIN, 0.0, 8.0 * parts * s->dim);
         err = hipGetLastError();
     }
     return err == hipSuccess ? PQL_OK : ctx_fail(c, PQL_ERR_HIP, "pql_residual_backward", err);
