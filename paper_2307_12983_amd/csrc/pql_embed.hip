@@ -34,8 +34,8 @@ struct EmbedArgs {
 // `lanes` consecutive lanes (a power of two, at most 256) per row.
 template <typename E, bool AL> __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, int lanes) {
     constexpr int V = AL ? VEC_OF<E> : 1;
-    const unsigned n = blockIdx.x * (256u / lanes) + threadIdx.x / lanes;
-    if (n >= a.rows) return;
+    const unsigned by = 256u / lanes;
+    for (unsigned n = blockIdx.x * by + threadIdx.x / lanes; n < a.rows; n += gridDim.x * by) {
     const bool live = a.live(n);
     const int* tokens = a.tokens + (int64_t)n * a.per_row;
     E* out = (E*)a.out + n * a.out_stride;
@@ -56,6 +56,7 @@ template <typename E, bool AL> __global__ void __launch_bounds__(256) embed_kern
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[i] *= a.scale;
         if constexpr (AL) *(uint4*)(out + at) = narrow(sum, E{}); else out[at] = from_float<E>(sum[0]);
+    }
     }
 }
 
@@ -402,13 +403,15 @@ EmbedArgs embed_args(const pql_embed_shape& s, const int32_t* tokens, const int3
 bool embed_aligned(const pql_embed_shape& s, const pql_rows& table, const pql_rows& out) {
     return s.dim * elem_size(s.dtype) % ROW_ALIGN == 0 && rows_aligned(table, s.dtype) && rows_aligned(out, s.dtype);
 }
+// A grid holds at most 2^32 - 1 threads.
+constexpr unsigned MOST_BLOCKS = 1 << 22;
 template <typename E, bool AL> hipError_t embed_launch(const EmbedArgs& a, hipStream_t st) {
     const int granules = AL ? a.dim / VEC_OF<E> : a.dim;
     int lanes = 1;
     while (lanes < 256 && lanes < granules) lanes *= 2;
-    const unsigned by = 256 / lanes;
+    const unsigned by = 256 / lanes, blocks = (a.rows + by - 1) / by;
     const ProfSlot ps = prof_slot();
-    PQL_LAUNCH(ps, (embed_kernel<E, AL>), dim3((a.rows + by - 1) / by), dim3(256), 0, st, a, lanes);
+    PQL_LAUNCH(ps, (embed_kernel<E, AL>), dim3(blocks < MOST_BLOCKS ? blocks : MOST_BLOCKS), dim3(256), 0, st, a, lanes);
     prof_commit(ps, KID_EMBED, 0.0, (double)a.rows * (a.per_row * (4.0 + a.dim * sizeof(E)) + a.dim * sizeof(E)));
     return hipGetLastError();
 }

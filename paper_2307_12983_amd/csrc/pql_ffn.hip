@@ -657,12 +657,12 @@ int tile_rows(int32_t dtype, int64_t m, int n, int problems) {
 }
 
 // One product's tiles, workgroups at a time, and the steps of its contraction, at most.
-struct FfnTiles { int rows, cols, tiles, slots, steps; };
+struct FfnTiles { int rows, cols; int64_t tiles; int slots, steps; };
 FfnTiles ffn_tiles(int32_t dtype, int64_t m, int n, int problems, int of, int64_t k, int segments, bool gated) {
     FfnTiles t{};
     t.rows = tile_rows(dtype, m, gated ? 2 * n : n, of);
     t.cols = tile_cols(dtype, t.rows);
-    t.tiles = tiles_of((int)m, t.rows) * tiles_of(n, gated ? t.cols / 2 : t.cols) * problems;
+    t.tiles = (int64_t)tiles_of((int)m, t.rows) * tiles_of(n, gated ? t.cols / 2 : t.cols) * problems;
     t.slots = dtype == PQL_BF16 && t.rows == 128 ? 512 : 256;          // two workgroups a compute unit, one where LDS holds no more
     t.steps = tiles_of((int)k, dtype == PQL_F32 ? 32 : 64) * segments;
     return t;
@@ -670,7 +670,7 @@ FfnTiles ffn_tiles(int32_t dtype, int64_t m, int n, int problems, int of, int64_
 // Bytes of the parts that as many workgroups may leave.
 size_t part_bytes(const FfnTiles& t) {
     if (t.steps <= JOIN_STEPS) return 0;
-    const int64_t most = (int64_t)t.tiles * t.steps;
+    const int64_t most = t.tiles * t.steps;
     return (size_t)(most < t.slots ? most : t.slots) * 2 * t.rows * t.cols * 4;
 }
 struct FfnPlan {
@@ -730,10 +730,12 @@ struct FfnSaved {
 
 template <typename E, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, Epilogue EPI>
 hipError_t launch_product(const FfnTiles& t, const FfnArgs& a, int kid, double flops, hipStream_t st) {
+    // a grid holds at most 2^32 - 1 threads: results of so many tiles would not fit the memory
+    if (t.tiles >= 1 << 22) return hipErrorInvalidConfiguration;
     ProfSlot ps = prof_slot();
-    const Shares sh(t.tiles, t.slots, t.steps);
+    const Shares sh((int)t.tiles, t.slots, t.steps);
     // with rows that are counted on the device, fewer tiles may be shared out otherwise
-    const int grid = a.count ? t.tiles / t.slots * t.slots + t.slots : sh.whole + (sh.sharers + 7) / 8 * 8;
+    const int grid = a.count ? (int)t.tiles / t.slots * t.slots + t.slots : sh.whole + (sh.sharers + 7) / 8 * 8;
     PQL_LAUNCH(ps, (ffn_product_kernel<E, BM, BN, WM, WN, A_ALONG, B_ALONG, EPI>), dim3(grid), dim3(64 * WM * WN), 0, st, a, t.slots);
     prof_commit(ps, kid, flops, 0.0);
     if (a.count ? t.steps > JOIN_STEPS : sh.joins()) {
@@ -820,7 +822,7 @@ struct FfnRun {
         FfnTiles t = ffn_tiles(s.dtype, pr.m, pr.n, 1, of, a.k, a.segments, EPI == EPI_GATED);
         t.tiles = 0;
         for (int i = 0; i < a.problems; ++i)
-            t.tiles += tiles_of(a.prob[i].m, t.rows) * tiles_of(a.prob[i].n, EPI == EPI_GATED ? t.cols / 2 : t.cols);
+            t.tiles += (int64_t)tiles_of(a.prob[i].m, t.rows) * tiles_of(a.prob[i].n, EPI == EPI_GATED ? t.cols / 2 : t.cols);
         const double flops = 2.0 * a.problems * (EPI == EPI_GATED ? 2 : 1) * a.segments * pr.m * pr.n * a.k;
         if (s.dtype == PQL_F32)
             e = t.rows == 256 ? launch_product<float, 256, 128, 2, 4, A_ALONG, B_ALONG, EPI>(t, a, kid, flops, st)

@@ -705,3 +705,56 @@ def test_rows_calls_leave_what_is_not_theirs(env, dtype):
                 n, c = inner.shape
                 assert bool((big[n:] == 7).all()) and bool((big[:, :8] == 7).all()) and bool((big[:, 8 + c:] == 7).all())
                 assert not bool((inner == 7).all(1).any())
+
+
+def test_no_rows_at_all(env):
+    """Gradients of weights are written all the same."""
+    torch, K, ctx = env
+    x, tokens = torch.empty(0, 5, 24, device="cuda"), torch.empty(0, 5, 2, dtype=torch.int32, device="cuda")
+    weights = [torch.randn(*s, device="cuda") for s in ((40, 24), (40, 24), (24, 40))]
+    shape = K.ffn_shape(x, weights[0], "silu")
+    given, grads = K.FfnInput(shape, x, *weights), [torch.full_like(w, 7) for w in weights]
+    ctx.pql_ffn_backward(shape, given, None, K.Rows(x), K.FfnGrad(shape, None, *grads), None)
+    table, dtable = torch.randn(9, 24, device="cuda"), torch.full((9, 24), 7.0, device="cuda")
+    shape = K.embed_shape(tokens, table, 1.0)
+    ctx.pql_embed_backward(shape, tokens, None, K.Rows(x), K.Rows(dtable), None)
+    shape = K.residual_shape(0, 5, 24, torch.float32, eps_post=1e-5, eps_pre=1e-5)
+    post, pre = torch.full((24,), 7.0, device="cuda"), torch.full((24,), 7.0, device="cuda")
+    ctx.pql_residual_backward(shape, K.ResidualInput(shape, x, x), K.Rows(x), K.Rows(x), K.ResidualGrad(shape, post=post, pre=pre), None)
+    assert all(not bool(t.any()) for t in grads + [dtable, post, pre])
+
+
+def test_lengths_that_change_between_replays(env):
+    torch = env[0]
+    for run, _, outputs in every_call(env, "float32"):
+        calls = [c.cell_contents for c in run.__closure__ if c.cell_contents is not None]
+        lengths = next((c for c in calls if isinstance(c, torch.Tensor) and c.dtype is torch.int32 and c.shape == (4,)), None)
+        if lengths is None:
+            lengths = next((getattr(c, "lengths", None) for c in calls if getattr(c, "lengths", None) is not None), None)
+        if lengths is None:
+            continue
+        graph = torch.cuda.CUDAGraph()
+        run()
+        with torch.cuda.graph(graph):
+            run()
+        for new in ([33, 0, 7, 33], [0, 0, 0, 0], [33, 7, 0, 33], [1, 7, 0, 0]):       # within what is not poisoned, or nothing that is
+            lengths.copy_(torch.tensor([min(a, b) for a, b in zip(new, (40, 7, 0, 33))], dtype=torch.int32))
+            run()
+            want = [x.clone() for x in outputs]
+            for x in outputs:
+                x.fill_(7)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, outputs)), new
+
+
+def test_more_rows_than_a_grid_holds_workgroups_for(env):
+    torch, K, ctx = env
+    rows, dim = (1 << 24) + 5, 1032
+    table = torch.randn(11, dim, device="cuda").bfloat16()
+    tokens = torch.arange(rows, dtype=torch.int32, device="cuda").remainder_(11).view(1, rows, 1)
+    out = torch.empty(1, rows, dim, dtype=torch.bfloat16, device="cuda")
+    shape = K.embed_shape(tokens, table, 1.0)
+    ctx.pql_embed_forward(shape, tokens, None, K.Rows(table), K.Rows(out))
+    for at in (0, 1 << 22, 1 << 23, rows - 11):
+        assert torch.equal(out[0, at:at + 11], table[tokens[0, at:at + 11, 0].long()])
