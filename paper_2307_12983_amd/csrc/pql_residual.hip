@@ -124,11 +124,12 @@ template <typename E, bool AL, bool BACK> struct Row {
     typename S::Raw x, y, gate, sum, next;
     float one;                              // the gate's value for the part
     unsigned row;
-    bool here, live;
+    bool here, live, work;                  // work: the workgroup's, whether any of its rows may count
     __device__ __forceinline__ void fetch(const ResidualArgs& a, S s, unsigned first, int slot, int slots, int group) {
         row = first + slot;
         here = first < a.rows && slot < slots && row < a.rows;
         live = here && a.live(row);
+        work = slots > 1 || (first < a.rows && a.live(first));
         s.on = live;
         if (a.x) s.fetch((const E*)a.x + row * a.x_stride, x);
         if (a.y) s.fetch((const E*)a.y + row * a.y_stride, y);
@@ -182,44 +183,47 @@ template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT, wav
         const bool here = now.here, live = now.live;
         s.on = live;
         if constexpr (!KEEP) { s.load_weights(a.post, post); s.load_weights(a.pre, pre); }
-        float h[EPT] = {};
-        if (a.x) {
-            s.open(now.x, h);
+        float h[EPT] = {}, f = 1.f;
+        if (now.work) {                         // rows that do not count: 37 us become 33 at 8192 rows of 2048 with half of them, bf16
+            if (a.x) {
+                s.open(now.x, h);
 #pragma unroll
-            for (int i = 0; i < EPT; ++i) h[i] *= a.scale_x;
-        }
-        if (a.y) {
-            float y[EPT], g[EPT], d[EPT];
-            s.open(now.y, y);
-            now.open_gate(a, s, g, d);
-            float r = 1.f;
-            if (a.eps_post > 0.f) {
+                for (int i = 0; i < EPT; ++i) h[i] *= a.scale_x;
+            }
+            if (a.y) {
+                float y[EPT], g[EPT], d[EPT];
+                s.open(now.y, y);
+                now.open_gate(a, s, g, d);
+                float r = 1.f;
+                if (a.eps_post > 0.f) {
+                    float q[1] = {};
+#pragma unroll
+                    for (int i = 0; i < EPT; ++i) q[0] += y[i] * y[i];
+                    sums.of_part(q);
+                    r = 1.f / sqrtf(q[0] / a.part + a.eps_post);
+                }
+                r *= a.scale_y;
+#pragma unroll
+                for (int i = 0; i < EPT; ++i) h[i] += r * y[i] * (g[i] * post[i]);
+            }
+            if (a.next && a.eps_pre > 0.f) {
                 float q[1] = {};
 #pragma unroll
-                for (int i = 0; i < EPT; ++i) q[0] += y[i] * y[i];
-                sums.of_part(q);
-                r = 1.f / sqrtf(q[0] / a.part + a.eps_post);
+                for (int i = 0; i < EPT; ++i) q[0] += h[i] * h[i];
+                sums.of_row(q, a.groups, unit, units);
+                f = 1.f / sqrtf(q[0] / a.dim + a.eps_pre);
             }
-            r *= a.scale_y;
-#pragma unroll
-            for (int i = 0; i < EPT; ++i) h[i] += r * y[i] * (g[i] * post[i]);
-        }
-        float f = 1.f;
-        if (a.next && a.eps_pre > 0.f) {
-            float q[1] = {};
-#pragma unroll
-            for (int i = 0; i < EPT; ++i) q[0] += h[i] * h[i];
-            sums.of_row(q, a.groups, unit, units);
-            f = 1.f / sqrtf(q[0] / a.dim + a.eps_pre);
         }
         s.on = here;
-        if (!live)
+        if (a.sum) {
+            float out[EPT];
 #pragma unroll
-            for (int i = 0; i < EPT; ++i) h[i] = 0.f;
-        if (a.sum) s.store((E*)a.sum + row * a.sum_stride, h);
+            for (int i = 0; i < EPT; ++i) out[i] = live ? h[i] : 0.f;
+            s.store((E*)a.sum + row * a.sum_stride, out);
+        }
         if (a.next) {
 #pragma unroll
-            for (int i = 0; i < EPT; ++i) h[i] *= f * pre[i];
+            for (int i = 0; i < EPT; ++i) h[i] = live ? h[i] * (f * pre[i]) : 0.f;
             s.store((E*)a.next + row * a.next_stride, h);
         }
     }
@@ -244,6 +248,17 @@ template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT, wav
         const unsigned row = now.row;
         const bool here = now.here;
         s.on = now.live;
+        if (!now.work) {                        // 57 us become 48 there
+            const float zero[EPT] = {};
+            s.on = here;
+            if (a.dx) s.store((E*)a.dx + row * a.dx_stride, zero);
+            if (a.dy) s.store((E*)a.dy + row * a.dy_stride, zero);
+            if (a.dgate) {
+                if (!a.gate_part) s.store((E*)a.dgate + row * a.dgate_stride, zero);
+                else if (here && s.lane == 0) ((E*)a.dgate)[row * a.dgate_stride + group] = from_float<E>(0.f);
+            }
+            continue;
+        }
         if constexpr (!KEEP) { s.load_weights(a.post, post); s.load_weights(a.pre, pre); }
         float y[EPT] = {}, g[EPT], slope[EPT], h[EPT] = {}, dh[EPT] = {};
         float r = 1.f;
