@@ -192,7 +192,7 @@ template <typename E, Epilogue EPI> __device__ __forceinline__ void finish(const
 // `slots` workgroups run at a time.  As many whole rounds of tiles as there are go to a workgroup each; the `rest` tiles behind
 // them are cut into steps of their contractions, of which each of `sharers` workgroups takes `per` in a row, at most a tile's.
 // What is not a whole tile is left as sums, joined by another launch.  Known where the rows that count are: on the device.
-constexpr int JOIN_STEPS = 6;                   // that the other launch takes as long as: fewer are not worth it
+constexpr int JOIN_STEPS = 7;                   // that the other launch takes as long as: fewer are not worth it, and never launch it
 struct Shares {
     int whole, rest, steps, per, sharers;
     __host__ __device__ Shares(int tiles, int slots, int steps_) : steps(steps_) {
@@ -574,44 +574,14 @@ template <typename E, int BM, int BN, Epilogue EPI> __global__ void __launch_bou
 }
 
 // ---- preparation ------------------------------------------------------------------------------------------
-// Which row each packed one is, and how many there are.  A workgroup takes `per` rows of all and counts those before it itself.
-__global__ void __launch_bounds__(256) ffn_map_kernel(const int* lengths, int batch, int steps, int64_t rows, int64_t per, int* map, int* count) {
-    __shared__ int sums[4];
-    const int64_t first = blockIdx.x * per, last = min(first + per, rows);
-    auto length = [&](int b) { return min(max(lengths[b], 0), steps); };
-    // rows that count before `first`: whole sequences, and the beginning of the one it lies in
-    const int b0 = (int)(first / steps);
-    int mine = 0;
-    for (int b = threadIdx.x; b < b0; b += 256) mine += length(b);
-    for (int d = 1; d < 64; d <<= 1) mine += __shfl_xor(mine, d);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = mine;
-    __syncthreads();
-    const int base = sums[0] + sums[1] + sums[2] + sums[3];
-    // 256 rows at a time: their places follow from counts of the lanes and wavefronts before
-    const int t0 = (int)(first - (int64_t)b0 * steps);
-    int done = base + (t0 > 0 ? min(t0, length(b0)) : 0);
-    for (int64_t r0 = first; r0 < last; r0 += 256) {
-        const int64_t r = r0 + threadIdx.x;
-        const int b = (int)(r / steps);
-        const bool live = r < last && (int)(r - (int64_t)b * steps) < length(b);
-        const uint64_t mask = __ballot(live);
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = __popcll(mask);
-        __syncthreads();
-        int at = done + __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1));
-        for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) at += sums[w];
-        if (live) map[at] = (int)r;
-        done += sums[0] + sums[1] + sums[2] + sums[3];
-    }
-    if (last == rows && threadIdx.x == 0) *count = done;
-}
-
-// Matrices as planes of padded rows, packed by the map where there is one.  Rows of `clear` that do not count become zeros.
-struct FfnCopy { const void* from; int64_t stride; bf16_t* to; int64_t plane; int rows, cols, cols_p; const int* map; };
+// Matrices as planes of padded rows.  Rows of tokens are packed where sequences have lengths, and `clear`'s that do not count become
+// zeros.  A workgroup of packed rows takes a stretch of all rows, counts those that count before it itself, and finds the places of its
+// own from counts of the lanes and wavefronts before; one matrix's note which row each packed one is, and how many there are.
+struct FfnCopy { const void* from; int64_t stride; bf16_t* to; int64_t plane; int rows, cols, cols_p, packed; };
 struct FfnCopies {
     FfnCopy c[5];
-    int n;
-    const int* count;
+    int n, token_blocks;
+    int *map, *count;
     void* clear; int64_t clear_stride; int clear_cols, clear_rows;
     Live live;
 };
@@ -623,11 +593,10 @@ template <typename E> __global__ void __launch_bounds__(256) ffn_prepare_kernel(
         return;
     }
     const FfnCopy& c = a.c[blockIdx.y];
-    const int rows = c.map ? *a.count : c.rows, each = c.cols_p / 8;
+    const int each = c.cols_p / 8;
     const bool al = (c.stride * sizeof(E)) % 16 == 0 && ((uintptr_t)c.from & 15) == 0;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < (int64_t)rows * each; i += gridDim.x * 256ll) {
-        const int row = (int)(i / each), col = (int)(i - (int64_t)row * each) * 8;
-        const E* p = (const E*)c.from + (int64_t)(c.map ? c.map[row] : row) * c.stride + col;
+    auto copy = [&](int64_t from, int64_t to, int col) {
+        const E* p = (const E*)c.from + from * c.stride + col;
         float x[8];
         if (al && col + 8 <= c.cols) {
 #pragma unroll
@@ -636,9 +605,49 @@ template <typename E> __global__ void __launch_bounds__(256) ffn_prepare_kernel(
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = col + e < c.cols ? to_float(p[e]) : 0.f;
         }
-        bf16_t* to = c.to + (int64_t)row * c.cols_p + col;
-        store_terms<E>(to, c.plane, x);
+        store_terms<E>(c.to + to * c.cols_p + col, c.plane, x);
+    };
+    if (!c.packed) {
+        for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < (int64_t)c.rows * each; i += gridDim.x * 256ll) {
+            const int row = (int)(i / each);
+            copy(row, row, (int)(i - (int64_t)row * each) * 8);
+        }
+        return;
     }
+    __shared__ int sums[4], places[256];
+    const int per = (c.rows + a.token_blocks - 1) / a.token_blocks, steps = (int)a.live.steps;
+    const int64_t first = (int64_t)blockIdx.x * per, last = min(first + per, (int64_t)c.rows);
+    if ((int)blockIdx.x >= a.token_blocks || first >= last) return;
+    auto length = [&](int b) { return min(max(a.live.lengths[b], 0), steps); };
+    // rows that count before `first`: whole sequences, and the beginning of the one it lies in
+    const int b0 = (int)(first / steps), t0 = (int)(first - (int64_t)b0 * steps);
+    int mine = 0;
+    for (int b = threadIdx.x; b < b0; b += 256) mine += length(b);
+    for (int d = 1; d < 64; d <<= 1) mine += __shfl_xor(mine, d);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    int done = sums[0] + sums[1] + sums[2] + sums[3] + (t0 > 0 ? min(t0, length(b0)) : 0);
+    const bool notes = c.packed == 2;
+    for (int64_t r0 = first; r0 < last; r0 += 256) {
+        const int64_t r = r0 + threadIdx.x;
+        const bool live = r < last && a.live((unsigned)r);
+        const uint64_t mask = __ballot(live);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = __popcll(mask);
+        __syncthreads();
+        int at = done + __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1));
+        for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) at += sums[w];
+        places[threadIdx.x] = live ? at : -1;
+        if (live && notes) a.map[at] = (int)r;
+        done += sums[0] + sums[1] + sums[2] + sums[3];
+        __syncthreads();
+        const int all = (int)min(last - r0, (int64_t)256) * each;
+        for (int i = threadIdx.x; i < all; i += 256) {
+            const int row = i / each;
+            if (places[row] >= 0) copy(r0 + row, places[row], (i - row * each) * 8);
+        }
+    }
+    if (notes && last == c.rows && threadIdx.x == 0) *a.count = done;
 }
 
 // ---- host -------------------------------------------------------------------------------------------------
@@ -755,27 +764,25 @@ struct FfnRun {
     hipError_t e = hipSuccess;
     const int *map = nullptr, *count = nullptr;
     FfnCopies copies{};
+    bool noted = false;
     int elem() const { return s.dtype == PQL_F32 ? 4 : 2; }
 
     template <typename T> T* at(size_t o) const { return (T*)(ws + o); }
     void pack(const int32_t* lengths) {
         copies.live = {lengths, (unsigned)s.steps};
         if (!lengths) return;
-        const int64_t rows = p.rows;
-        int64_t per = (rows + 255) / 256;
-        per = per < 1024 ? 1024 : (per + 255) / 256 * 256;
-        const ProfSlot ps = prof_slot();
-        PQL_LAUNCH(ps, ffn_map_kernel, dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, lengths, s.batch, s.steps, rows, per, at<int>(p.map), at<int>(p.count));
-        prof_commit(ps, KID_FFN_PREPARE, 0.0, 4.0 * rows);
-        map = at<int>(p.map);
-        count = at<int>(p.count);
+        map = copies.map = at<int>(p.map);
+        count = copies.count = at<int>(p.count);
+        const int blocks = (p.rows + 7) / 8;
+        copies.token_blocks = blocks < 512 ? blocks : 512;
     }
     // The matrix as an operand: where it is, or as planes at `to`.
     FfnOperand operand(const pql_rows& r, int rows, int cols, size_t to, int64_t plane, bool tokens, bool direct = true) {
         if (direct && s.dtype == PQL_BF16 && !(tokens && map) && cols % 8 == 0 && rows_aligned(r, s.dtype) && r.stride >= cols && r.stride <= 1 << 20)
             return {(const bf16_t*)r.data, r.stride, 0};
-        FfnCopy& c = copies.c[copies.n++];
-        c = {r.data, r.stride, at<bf16_t>(to), plane, rows, cols, up8(cols), tokens ? map : nullptr};
+        const int packed = tokens && map ? (noted ? 1 : 2) : 0;         // 2: with the notes, that all of them would make alike
+        if (packed) noted = true;
+        copies.c[copies.n++] = {r.data, r.stride, at<bf16_t>(to), plane, rows, cols, up8(cols), packed};
         return {at<bf16_t>(to), up8(cols), plane};
     }
     // Both projections' weights, alike.
@@ -792,14 +799,14 @@ struct FfnRun {
     void prepare() {
         const int y = copies.n + (copies.clear ? 1 : 0);
         if (y == 0 || e != hipSuccess) return;
-        copies.count = count;
         int64_t most = copies.clear ? copies.clear_rows * 256ll : 0, bytes = 0;
         for (int i = 0; i < copies.n; ++i) {
             const int64_t n = (int64_t)copies.c[i].rows * copies.c[i].cols_p / 8;
             most = n > most ? n : most;
             bytes += n * 8 * (elem() + 2 * p.terms);
         }
-        const int64_t blocks = (most + 255) / 256;
+        int64_t blocks = (most + 255) / 256;
+        blocks = blocks < copies.token_blocks ? copies.token_blocks : blocks;
         const ProfSlot ps = prof_slot();
         const dim3 grid((unsigned)(blocks < 2048 ? blocks : 2048), y);
         if (s.dtype == PQL_F32) PQL_LAUNCH(ps, ffn_prepare_kernel<float>, grid, dim3(256), 0, st, copies);
