@@ -889,7 +889,7 @@ int32_t pql_ffn_forward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input*
     const FfnPlan p = ffn_plan(*s, PQL_FFN_FORWARD);
     const hipStream_t st = (hipStream_t)stream;
     hipError_t e;
-    if (p.rows <= FFN_FEW_ROWS && !saved) {
+    if (p.rows <= ffn_few_rows(s->dtype, (double)s->dim * s->hidden * elem_size(s->dtype)) && !saved) {
         FfnRowsArgs a{{in->lengths, (unsigned)s->steps}, p.rows, s->dim, s->hidden, s->act, in->x.data, in->gate.data, in->up.data, in->down.data,
                       in->x.stride, in->gate.stride, in->up.stride, in->down.stride, (char*)workspace + p.m, p.hidden_p, p.m_plane, out->data, out->stride};
         e = ffn_rows_launch(a, s->dtype, st);

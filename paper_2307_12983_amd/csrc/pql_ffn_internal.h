@@ -34,7 +34,13 @@ __device__ __forceinline__ Terms three_terms(float x) {
     return s;
 }
 
-constexpr int FFN_FEW_ROWS = 64;                // calls of at most so many rows take the kernels for few rows
+// Calls of at most so many rows take the kernels for few rows, which read the rows again for each 16 outputs; the tiles' kernels read
+// them once, but split 32-bit weights into planes and join sums.  us a call, rows / tiles: fp32, 64 rows, 1000 and 4000: 37 / 81, 2048
+// and 8192: 136 / 195, 4096 and 16384: 491 / 747.  bf16, by the bytes of a projection: 64 rows, 1024 and 4096 (8 MiB): 22 / 52, 1408
+// and 5632 (15 MiB): 50 / 50; 2048 and 8192 (32 MiB): 32 rows 45 / 54, 48 rows 62 / 53; 4096 and 16384 (128 MiB): 16 rows 117 / 118,
+// 24 rows 142 / 121.
+constexpr int FFN_FEW_ROWS = 64;
+inline int ffn_few_rows(int32_t dtype, double projection) { return dtype == PQL_F32 || projection <= 16 << 20 ? FFN_FEW_ROWS : projection <= 64 << 20 ? 32 : 16; }
 
 struct FfnRowsArgs {
     Live live;

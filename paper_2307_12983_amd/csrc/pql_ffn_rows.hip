@@ -9,13 +9,15 @@
 namespace pql {
 namespace {
 
-
 // Wavefronts of a workgroup (one token through a block of 4096 and 16384 in bf16: 85.6 us a call, with 4 of them 89, with 16 90; twice as
 // many steps ahead change nothing).
 constexpr int WAVES = 8, NT = 64 * WAVES;
-// Weights of at most so many bytes stay in the caches: each 16 rows have workgroups of their own, which read them again
-// (64 rows through a block of 256 and 1024 in fp32: 11 us a call, 22 with one workgroup for all of them).
-constexpr double CACHED = 8 << 20;
+// Sixteens of rows share a workgroup, that reads its weights once for all of them, where that leaves FILL workgroups or the weights are
+// more than CACHED bytes; others have one for each, or for two, and read weights again, from the caches (the last holds 256 MiB).  us a
+// call of 64 rows in fp32, shared / by this rule / never shared: 256 and 1024 22 / 11 / 11, 1000 and 4000 67 / 37 / 47, 2048 and 8192
+// 179 / 136 / 177; FILL of 96 or 384 instead: 48 or 41 and 179 or 146.  More than CACHED, 4096 and 16384: 491, never shared 768.
+constexpr int FILL = 192;
+constexpr double CACHED = 128 << 20;
 
 // ---- operands: lane l holds row l % 16, and CHUNK elements of the contraction from CHUNK (l / 16) on, of 4 CHUNK a step ----
 template <typename E> constexpr int M_TERMS = sizeof(E) == 2 ? 2 : 1;     // of the product between the two launches
@@ -141,12 +143,14 @@ template <typename E, int T, bool GATED> void launch(const FfnRowsArgs& a, bool 
     prof_commit(ps, KID_FFN_ROWS, 2.0 * (GATED ? 2 : 1) * a.rows * outputs * size, (double)(GATED ? 2 : 1) * outputs * size * sizeof(E));
 }
 template <typename E, bool GATED> void launch_rows(const FfnRowsArgs& a, bool al, hipStream_t st) {
-    const int tiles = (a.rows + 15) / 16;
-    const double bytes = (double)(GATED ? 2 : 1) * a.dim * a.hidden * sizeof(E);
-    if (tiles == 1) launch<E, 1, GATED>(a, al, 1, st);
-    else if (bytes <= CACHED) launch<E, 1, GATED>(a, al, tiles, st);
-    else if (tiles == 2) launch<E, 2, GATED>(a, al, 1, st);
-    else launch<E, 4, GATED>(a, al, 1, st);
+    const int tiles = (a.rows + 15) / 16, groups = ((GATED ? a.hidden : a.dim) + 15) / 16;
+    int each = tiles == 3 ? 4 : tiles;          // sixteens of rows of a workgroup
+    if ((GATED ? 2.0 : 1.0) * a.dim * a.hidden * sizeof(E) <= CACHED)
+        while (each > 1 && groups * ((tiles + each - 1) / each) < FILL) each /= 2;
+    const int y = (tiles + each - 1) / each;
+    if (each == 1) launch<E, 1, GATED>(a, al, y, st);
+    else if (each == 2) launch<E, 2, GATED>(a, al, y, st);
+    else launch<E, 4, GATED>(a, al, y, st);
 }
 template <typename E> hipError_t rows_of(const FfnRowsArgs& a, hipStream_t st) {
     const int32_t dt = sizeof(E) == 4 ? PQL_F32 : PQL_BF16;

@@ -460,6 +460,24 @@ def test_feed_forward_block(env, case):
     assert env[0].equal(kept, again)
 
 
+# Rows around the sizes where other kernels, or other shares of the rows for a workgroup, take over: by the rows, by how many outputs
+# there are and by the bytes of the weights.
+FEW = [(rows, 1, d, f, dtype, "silu", "dense", None)
+       for dtype in ("float32", "bfloat16")
+       for rows, d, f in ((32, 24, 3100), (33, 3100, 24), (48, 1600, 1544), (49, 40, 1530), (64, 1530, 40), (65, 64, 3100))]
+FEW += [(32, 1, 2048, 4104, "bfloat16", "gelu", "dense", None), (33, 1, 2048, 4104, "bfloat16", "gelu", "dense", None),
+        (16, 1, 4096, 8200, "bfloat16", "relu", "dense", None), (17, 1, 4096, 8200, "bfloat16", "relu", "dense", None),
+        (40, 1, 2048, 8208, "float32", "silu", "dense", [i % 2 for i in range(40)])]
+
+
+@pytest.mark.parametrize("case", FEW, ids=label)
+def test_feed_forward_block_of_few_rows(env, case):
+    call = FfnCall(env, case, seed=4)
+    out, _ = call.forward(False)
+    call.close(out, call.want, "out")
+    assert env[0].equal(out, call.forward(False)[0])
+
+
 @pytest.mark.parametrize("case", FFN, ids=label)
 def test_gradients_of_the_feed_forward_block(env, case):
     call = FfnCall(env, case, seed=1)
