@@ -36,27 +36,27 @@ template <typename E, bool AL> __global__ void __launch_bounds__(256) embed_kern
     constexpr int V = AL ? VEC_OF<E> : 1;
     const unsigned by = 256u / lanes;
     for (unsigned n = blockIdx.x * by + threadIdx.x / lanes; n < a.rows; n += gridDim.x * by) {
-    const bool live = a.live(n);
-    const int* tokens = a.tokens + (int64_t)n * a.per_row;
-    E* out = (E*)a.out + n * a.out_stride;
-    for (int at = (threadIdx.x & (lanes - 1)) * V; at < a.dim; at += lanes * V) {
-        float sum[V] = {};
-        if (live) {
+        const bool live = a.live(n);
+        const int* tokens = a.tokens + (int64_t)n * a.per_row;
+        E* out = (E*)a.out + n * a.out_stride;
+        for (int at = (threadIdx.x & (lanes - 1)) * V; at < a.dim; at += lanes * V) {
+            float sum[V] = {};
+            if (live) {
 #pragma unroll 4
-            for (int j = 0; j < a.per_row; ++j) {
-                const int t = tokens[j];
-                const bool there = (unsigned)t < (unsigned)a.vocab;
-                const E* p = (const E*)a.table + (there ? t : 0) * a.table_stride + at;
-                float x[V];
-                if constexpr (AL) widen(*(const uint4*)p, x, E{}); else x[0] = to_float(*p);
+                for (int j = 0; j < a.per_row; ++j) {
+                    const int t = tokens[j];
+                    const bool there = (unsigned)t < (unsigned)a.vocab;
+                    const E* p = (const E*)a.table + (there ? t : 0) * a.table_stride + at;
+                    float x[V];
+                    if constexpr (AL) widen(*(const uint4*)p, x, E{}); else x[0] = to_float(*p);
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum[i] += there ? x[i] : 0.f;
+                    for (int i = 0; i < V; ++i) sum[i] += there ? x[i] : 0.f;
+                }
             }
-        }
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] *= a.scale;
-        if constexpr (AL) *(uint4*)(out + at) = narrow(sum, E{}); else out[at] = from_float<E>(sum[0]);
-    }
+            for (int i = 0; i < V; ++i) sum[i] *= a.scale;
+            if constexpr (AL) *(uint4*)(out + at) = narrow(sum, E{}); else out[at] = from_float<E>(sum[0]);
+        }
     }
 }
 

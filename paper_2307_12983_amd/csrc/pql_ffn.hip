@@ -3,14 +3,23 @@
 //     dm = dout D,  da = dm b act'(a),  db = dm act(a),  dx = da G + db U,  dG = da^T x,  dU = db^T x,  dD = dout^T m.
 //
 // All products run on the bf16 matrix instructions with sums in fp32.  fp32 values are three bf16 terms each (24 bits, exactly),
-// of whose nine products the three below 2^-24 are left out: six products a pair.  Operands lie in memory as planes, one for
-// each term; bf16 tensors whose rows start on 16-byte boundaries are used where they are.
+// of whose nine products the three below 2^-24 are left out: six products a pair.  Operands lie in memory as planes, one for each
+// term; bf16 tensors whose rows start on 16-byte boundaries are used where they are, and so are fp32 weights where there are few
+// rows.  bf16: m, da and db are rounded once, as operands of the next products; a and b are kept in fp32.
 //
 // Rows that count are packed together first where sequences have lengths, so that no work is done for the others.
 //
 // A workgroup computes one tile of the result.  Tiles of both operands go from memory to LDS without registers between, one
 // step ahead of the products, and are laid out there so that neither the contiguous reads (operands whose contraction runs along
-// a row) nor the transposing ones (along a column) meet bank conflicts: no operand is ever transposed in memory.
+// a row) nor the transposing ones (along a column) meet bank conflicts: no operand is ever transposed in memory.  bf16 takes tiles of
+// 256 x 256 by eight wavefronts, since what bounds it is the way from L2 to LDS, 64 KB a step of 64: 4 x 2048 rows of 2048 and 8192
+// with gradients take 2.25 ms, with tiles of 128 x 128 2.71 ms, of 256 x 128 by two workgroups a compute unit 2.57 ms; three to five
+// steps of 32 in LDS 2.38 ms.  Its products reach 975 (projections), 1230 (out, dx, weights' gradients) and 730 TFLOP/s (dm, da, db:
+// half of its time goes to reading a and b and writing da and db, 0.8 GB at 5 TB/s); the loop without its products takes 77 % of the
+// time with them.  fp32 takes 256 x 128, six products a pair, and is bound by those: 512 x 32 rows of 256 and 1024 with gradients
+// take 0.40 ms.
+#include <type_traits>
+
 #include "pql_ffn_internal.h"
 
 namespace pql {
@@ -24,10 +33,15 @@ template <typename E, int BM> struct Mode { static constexpr int TERMS = 1, BK =
 template <> struct Mode<float, 128> { static constexpr int TERMS = 3, BK = 32, STAGES = 3; };
 template <> struct Mode<float, 256> { static constexpr int TERMS = 3, BK = 32, STAGES = 2; };
 constexpr int BIG_TILES = 192;
+// Calls of at most so many rows read 32-bit weights as they are and make their terms in the product's kernel, for each 128 rows anew;
+// others make planes of them first (us a call with gradients, as they are / planes: 128 rows, 1024 and 4096: 182 / 219, 4096 and 16384:
+// 1216 / 2060; 768 rows: 454 / 457 and 5231 / 5402; 1024 rows: 529 / 494 and 6894 / 6983; 2048 rows: 953 / 842 and 13594 / 12616).
+constexpr int WHOLE_ROWS = 768;
 constexpr int NOWHERE = 0x7fffff00;             // an offset behind every buffer: reads give zeros
 
 // One operand: rows of a matrix, `plane` elements from one term's to the next.
-struct FfnOperand { const bf16_t* p; int64_t stride, plane; };
+// whole: 32-bit values, the stride in halves of them.
+struct FfnOperand { const bf16_t* p; int64_t stride, plane; bool whole; };
 struct FfnProblem { FfnOperand a[2], b[2]; int m, n; void* out; int64_t out_stride; };
 enum Epilogue : int { EPI_GATED, EPI_BACK, EPI_OUT };
 
@@ -120,6 +134,54 @@ template <int I, bool ALONG, int BK> struct Reader {
         }
     }
 };
+
+// The same of 32-bit values as they are, whose terms are made here: tiles of twice as many 16-bit elements (ALONG: a row, ACROSS: I).
+template <int I, bool ALONG> struct WholeReader {
+    int at[ALONG ? 2 : 8];
+    __device__ __forceinline__ void init(int first, int lane) {         // first: a multiple of 32; two sets of 16 rows from it on
+        const int r = lane & 15, q = lane >> 4;
+        if constexpr (ALONG) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) at[h] = (first + r) * 128 + (((2 * q + h) ^ along<64>(r)) * 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {                               // set i / 4, elements i % 4 and + 4 of the contraction's eight
+                const int k = 8 * q + (i & 3);
+                at[i] = k * I * 4 + ((((first + (i >> 2) * 16 + r) >> 2) ^ across(k)) * 16) + (r & 3) * 4;
+            }
+        }
+    }
+    __device__ __forceinline__ void get(const char* lds, int i, float (&x)[8]) const {
+        if constexpr (ALONG) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) *(floatx4*)(x + 4 * h) = *(const floatx4*)(lds + at[h] + i * 16 * 128);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = *(const float*)(lds + at[i * 4 + (e & 3)] + (e >> 2) * 4 * I * 4);
+        }
+    }
+};
+__device__ __forceinline__ void terms_of(const float (&x)[8], bf16x8 (&t)[3]) {
+    float f[3][8];
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        f[0][e] = (float)(bf16_t)x[e];
+        odd |= !(fabsf(f[0][e]) < __builtin_inff());
+        const float r = x[e] - f[0][e];
+        f[1][e] = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
+        f[2][e] = r - f[1][e];
+    }
+    if (__ballot(odd)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const Terms s = three_terms(x[e]);
+            f[0][e] = s.t[0]; f[1][e] = s.t[1]; f[2][e] = s.t[2];
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) t[q] = __builtin_bit_cast(bf16x8, narrow(f[q], bf16_t{}));
+}
 
 // Where an operand's next tile lies: `others` rows (or columns) of the result from `first` on, the contraction from `k` on.
 template <bool ALONG, int BK> struct Corner {
@@ -248,14 +310,18 @@ template <int N> __device__ __forceinline__ void wait_loads() {
 // ---- products -------------------------------------------------------------------------------------------
 // C[m][n] = sum_k A(m, k) B(n, k).  Tiles of BM x BN by WM x WN wavefronts; *_ALONG: the contraction runs along the operand's rows in
 // memory, otherwise across them.
-template <typename E, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, Epilogue EPI>
+template <typename E, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, Epilogue EPI, bool WHOLE>
 __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a, int slots) {
     constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int TERMS = Mode<E, BM>::TERMS, BK = Mode<E, BM>::BK, STAGES = Mode<E, BM>::STAGES;
     constexpr bool GATED = EPI == EPI_GATED;
     using TA = Tile<BM, A_ALONG, WAVES, BK>;
-    using TB = Tile<BN, B_ALONG, WAVES, BK>;
-    constexpr int STAGE = TERMS * (TA::BYTES + TB::BYTES), LOADS = TERMS * (TA::LOADS + TB::LOADS);
+    // WHOLE: B's 32-bit values are two elements of 16 bits each to what loads them
+    constexpr int BI = WHOLE && !B_ALONG ? 2 * BN : BN, BK_B = WHOLE && B_ALONG ? 2 * BK : BK, N_BY = BI / BN, K_BY = BK_B / BK;
+    constexpr int B_TERMS = WHOLE ? 1 : TERMS;
+    static_assert(!WHOLE || (TERMS == 3 && BM == 128 && TN == 2), "as few registers as that");
+    using TB = Tile<BI, B_ALONG, WAVES, BK_B>;
+    constexpr int STAGE = TERMS * TA::BYTES + B_TERMS * TB::BYTES, LOADS = TERMS * TA::LOADS + B_TERMS * TB::LOADS;
     __shared__ __align__(1024) char lds[STAGES][STAGE];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
     constexpr int COLS = GATED ? BN / 2 : BN;
@@ -278,258 +344,271 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
     }
     const int sharer = blockIdx.x < sh.whole ? 0 : stretch(blockIdx.x - sh.whole, sh.sharers);
     for (;;) {
-    int lane = threadIdx.x & 63;
-    asm("" : "+v"(lane));                       // addresses are found anew for each tile: there are no registers to keep them in
-    const int n = min(left_steps, sh.steps - from);
-    const Place at = place_of<BM, COLS>(a, rows, tile);
-    const int which = at.which, m0 = at.m0, n0 = at.n0;
-    const FfnProblem& pr = a.prob[which];
-    const int M = rows >= 0 ? rows : pr.m, N = pr.n;
+        int lane = threadIdx.x & 63;
+        asm("" : "+v"(lane));                       // addresses are found anew for each tile: there are no registers to keep them in
+        const int n = min(left_steps, sh.steps - from);
+        const Place at = place_of<BM, COLS>(a, rows, tile);
+        const int which = at.which, m0 = at.m0, n0 = at.n0;
+        const FfnProblem& pr = a.prob[which];
+        const int M = rows >= 0 ? rows : pr.m, N = pr.n;
 
-    TA ta;
-    TB tb;
-    ta.init(wave, lane, pr.a[0].stride);
-    // gated: half of a wavefront's columns are the gate's and half the other projection's, in turn; it loads from one of them
-    const int half = GATED ? wave & 1 : 0;
-    static_assert(!GATED || TB::LOADS * TB::ROWS_A_LOAD == TN * 8, "a wavefront loads from one of the two projections");
-    tb.init(GATED ? wave >> 1 : wave, lane, pr.b[0].stride);
-    Reader<BM, A_ALONG, BK> ra;
-    Reader<BN, B_ALONG, BK> rb;
-    ra.init(wm * TM * 16, lane);
-    rb.init(wn * TN * 16, lane);
+        TA ta;
+        TB tb;
+        ta.init(wave, lane, pr.a[0].stride);
+        // gated: half of a wavefront's columns are the gate's and half the other projection's, in turn; it loads from one of them
+        const int half = GATED ? wave & 1 : 0;
+        static_assert(!GATED || TB::LOADS * TB::ROWS_A_LOAD == TN * 8, "a wavefront loads from one of the two projections");
+        tb.init(GATED ? wave >> 1 : wave, lane, pr.b[0].stride);
+        Reader<BM, A_ALONG, BK> ra;
+        std::conditional_t<WHOLE, WholeReader<BN, B_ALONG>, Reader<BN, B_ALONG, BK>> rb;
+        ra.init(wm * TM * 16, lane);
+        rb.init(wn * TN * 16, lane);
 
-    // where the next tiles to load stand
-    int seg = from / max(ksteps, 1), left = K - from % max(ksteps, 1) * BK;
-    Corner<A_ALONG, BK> ca;
-    Corner<B_ALONG, BK> cb;
-    const int64_t plane_a = pr.a[0].plane, plane_b = pr.b[0].plane;
-    auto corners = [&] {
-        ca.set(pr.a[seg], m0, min(M - m0, BM), K - left);
-        cb.set(pr.b[GATED ? half : seg], n0, min(N - n0, BN), K - left);
-    };
-    corners();
-    auto load = [&](int stage) {
+        // where the next tiles to load stand
+        int seg = from / max(ksteps, 1), left = K - from % max(ksteps, 1) * BK;
+        Corner<A_ALONG, BK> ca;
+        Corner<B_ALONG, BK_B> cb;
+        const int64_t plane_a = pr.a[0].plane, plane_b = pr.b[0].plane;
+        auto corners = [&] {
+            ca.set(pr.a[seg], m0, min(M - m0, BM), K - left);
+            cb.set(pr.b[GATED ? half : seg], n0 * N_BY, min(N - n0, BN) * N_BY, (K - left) * K_BY);
+        };
+        corners();
+        auto load = [&](int stage) {
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
-            ta.load(lds[stage] + t * TA::BYTES, wave, ca.p + t * plane_a, ca.bytes(left), left);
-            tb.load(lds[stage] + TERMS * TA::BYTES + t * TB::BYTES, wave, cb.p + t * plane_b, cb.bytes(left), left);
-        }
-        ca.p += ca.step;
-        cb.p += cb.step;
-        left -= BK;
-        if (left <= 0 && seg + 1 < a.segments) { ++seg; left = K; corners(); }
-    };
-    floatx4 acc[TM][TN] = {};
-    // Two sets of operands, so that one comes from LDS while the products of the other run; STREAM: of A's only 16 rows each.
-    constexpr bool STREAM = TERMS == 3 && BM == 256;
-    bf16x8 fa[2][TERMS][STREAM ? 1 : TM], fb[2][TERMS][TN];
-    auto read_a = [&](int stage, int set, int i) {
+            for (int t = 0; t < TERMS; ++t) {
+                ta.load(lds[stage] + t * TA::BYTES, wave, ca.p + t * plane_a, ca.bytes(left), left);
+                if (t < B_TERMS) tb.load(lds[stage] + TERMS * TA::BYTES + t * TB::BYTES, wave, cb.p + t * plane_b, cb.bytes(left * K_BY), left * K_BY);
+            }
+            ca.p += ca.step;
+            cb.p += cb.step;
+            left -= BK;
+            if (left <= 0 && seg + 1 < a.segments) { ++seg; left = K; corners(); }
+        };
+        floatx4 acc[TM][TN] = {};
+        // Two sets of operands, so that one comes from LDS while the products of the other run; STREAM: of A's only 16 rows each.
+        constexpr bool STREAM = TERMS == 3 && BM == 256;
+        bf16x8 fa[2][TERMS][STREAM ? 1 : TM], fb[WHOLE ? 1 : 2][TERMS][TN];
+        float whole[2][WHOLE ? TN : 1][8];
+        auto read_a = [&](int stage, int set, int i) {
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t) fa[set][t][0] = ra.get(lds[stage] + t * TA::BYTES, i, 0);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    auto read_b = [&](int stage, int set) {
+            for (int t = 0; t < TERMS; ++t) fa[set][t][0] = ra.get(lds[stage] + t * TA::BYTES, i, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto read_b = [&](int stage, int set) {
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) fb[set][t][j] = rb.get(lds[stage] + TERMS * TA::BYTES + t * TB::BYTES, j, 0);
-    };
-    auto multiply_row = [&](int set_a, int set_b, int i) {
-#pragma unroll
-        for (int order = TERMS - 1; order >= 0; --order)
-#pragma unroll
-            for (int t = 0; t <= order; ++t)
+            for (int t = 0; t < TERMS; ++t)
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set_b][order - t][j], fa[set_a][t][0], acc[i][j], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    auto read = [&](int stage, int set, int kk) {
-        const char *la = lds[stage], *lb = la + TERMS * TA::BYTES;
+                    if constexpr (!WHOLE) fb[set][t][j] = rb.get(lds[stage] + TERMS * TA::BYTES + t * TB::BYTES, j, 0);
+        };
+        auto multiply_row = [&](int set_a, int set_b, int i) {
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
+            for (int order = TERMS - 1; order >= 0; --order)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[set][t][j] = rb.get(lb + t * TB::BYTES, j, kk);
-#pragma unroll
-            for (int i = 0; i < (STREAM ? 0 : TM); ++i) fa[set][t][i] = ra.get(la + t * TA::BYTES, i, kk);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    // the products of terms above 2^-24, small ones first
-    auto multiply = [&](int set) {
-#pragma unroll
-        for (int order = TERMS - 1; order >= 0; --order)
-#pragma unroll
-            for (int t = 0; t <= order; ++t)
-#pragma unroll
-                for (int i = 0; i < (STREAM ? 0 : TM); ++i)
+                for (int t = 0; t <= order; ++t)
 #pragma unroll
                     for (int j = 0; j < TN; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set][order - t][j], fa[set][t][i], acc[i][j], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    if constexpr (TERMS == 1) {
-        // A step is two sets.  In its middle all wavefronts have done with its tiles, so that those of the step after next are asked for.
-        if (n > 0) {
-            load(0);
-            if (n > 1) { load(1); wait_loads<LOADS>(); } else { wait_loads<0>(); }
-            read(0, 0, 0);
-            for (int s = 0; s + 1 < n; ++s) {
-                read(s & 1, 1, 1);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set_b][order - t][j], fa[set_a][t][0], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto read = [&](int stage, int set, int kk) {
+            const char *la = lds[stage], *lb = la + TERMS * TA::BYTES;
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    if constexpr (!WHOLE) fb[set][t][j] = rb.get(lb + t * TB::BYTES, j, kk);
+                    else if (t == 0) rb.get(lb, j, whole[set][j]);
+                }
+#pragma unroll
+                for (int i = 0; i < (STREAM ? 0 : TM); ++i) fa[set][t][i] = ra.get(la + t * TA::BYTES, i, kk);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        // the products of terms above 2^-24, small ones first
+        auto multiply = [&](int set) {
+            if constexpr (WHOLE) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    bf16x8 t[3];
+                    terms_of(whole[set][j], t);
+                    fb[0][0][j] = t[0]; fb[0][1][j] = t[1]; fb[0][2][j] = t[2];
+                }
+            }
+#pragma unroll
+            for (int order = TERMS - 1; order >= 0; --order)
+#pragma unroll
+                for (int t = 0; t <= order; ++t)
+#pragma unroll
+                    for (int i = 0; i < (STREAM ? 0 : TM); ++i)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[WHOLE ? 0 : set][order - t][j], fa[set][t][i], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        if constexpr (TERMS == 1) {
+            // A step is two sets.  In its middle all wavefronts have done with its tiles, so that those of the step after next are asked for.
+            if (n > 0) {
+                load(0);
+                if (n > 1) { load(1); wait_loads<LOADS>(); } else { wait_loads<0>(); }
+                read(0, 0, 0);
+                for (int s = 0; s + 1 < n; ++s) {
+                    read(s & 1, 1, 1);
+                    multiply(0);
+                    wait_loads<0>();
+                    read(s + 1 & 1, 0, 0);
+                    if (s + 2 < n) load(s & 1);
+                    multiply(1);
+                }
+                read(n - 1 & 1, 1, 1);
                 multiply(0);
-                wait_loads<0>();
-                read(s + 1 & 1, 0, 0);
-                if (s + 2 < n) load(s & 1);
                 multiply(1);
             }
-            read(n - 1 & 1, 1, 1);
-            multiply(0);
-            multiply(1);
-        }
-    } else if constexpr (STREAM) {
-        // A step goes through A 16 rows at a time; with the last of them begin the next step's operands and the loads of the one after.
-        static_assert(!STREAM || (TM % 2 == 0 && STAGES == 2), "sets alternate");
-        if (n > 0) {
-            load(0);
-            if (n > 1) { load(1); wait_loads<LOADS>(); } else { wait_loads<0>(); }
-            read_b(0, 0);
-            read_a(0, 0, 0);
-            auto rows = [&](int stage, int set) {
-#pragma unroll
-                for (int i = 0; i + 1 < TM; ++i) {
-                    read_a(stage, i + 1 & 1, i + 1);
-                    multiply_row(i & 1, set, i);
-                }
-            };
-            auto next = [&](int stage, int set) {
-                wait_loads<0>();
-                read_b(stage ^ 1, set ^ 1);
-                read_a(stage ^ 1, 0, 0);
-            };
-            int s = 0;
-            for (; s + 3 < n; s += 2) {
-                rows(0, 0);
-                next(0, 0);
+        } else if constexpr (STREAM) {
+            // A step goes through A 16 rows at a time; with the last of them begin the next step's operands and the loads of the one after.
+            static_assert(!STREAM || (TM % 2 == 0 && STAGES == 2), "sets alternate");
+            if (n > 0) {
                 load(0);
-                multiply_row(1, 0, TM - 1);
-                rows(1, 1);
-                next(1, 1);
-                load(1);
-                multiply_row(1, 1, TM - 1);
+                if (n > 1) { load(1); wait_loads<LOADS>(); } else { wait_loads<0>(); }
+                read_b(0, 0);
+                read_a(0, 0, 0);
+                auto rows = [&](int stage, int set) {
+#pragma unroll
+                    for (int i = 0; i + 1 < TM; ++i) {
+                        read_a(stage, i + 1 & 1, i + 1);
+                        multiply_row(i & 1, set, i);
+                    }
+                };
+                auto next = [&](int stage, int set) {
+                    wait_loads<0>();
+                    read_b(stage ^ 1, set ^ 1);
+                    read_a(stage ^ 1, 0, 0);
+                };
+                int s = 0;
+                for (; s + 3 < n; s += 2) {
+                    rows(0, 0);
+                    next(0, 0);
+                    load(0);
+                    multiply_row(1, 0, TM - 1);
+                    rows(1, 1);
+                    next(1, 1);
+                    load(1);
+                    multiply_row(1, 1, TM - 1);
+                }
+                for (; s < n; s += 2) {
+                    rows(0, 0);
+                    if (s + 1 < n) next(0, 0);
+                    if (s + 2 < n) load(0);
+                    multiply_row(1, 0, TM - 1);
+                    if (s + 1 == n) break;
+                    rows(1, 1);
+                    if (s + 2 < n) next(1, 1);
+                    if (s + 3 < n) load(1);
+                    multiply_row(1, 1, TM - 1);
+                }
             }
-            for (; s < n; s += 2) {
-                rows(0, 0);
-                if (s + 1 < n) next(0, 0);
-                if (s + 2 < n) load(0);
-                multiply_row(1, 0, TM - 1);
-                if (s + 1 == n) break;
-                rows(1, 1);
-                if (s + 2 < n) next(1, 1);
-                if (s + 3 < n) load(1);
-                multiply_row(1, 1, TM - 1);
-            }
-        }
-    } else {
-        // A step is one set.  It begins with the next one's operands and the loads of the third one on, into the place of its own.
-        if (n > 0) {
-            load(0);
-            if (n > 1) load(1);
-            if (n > 2) load(2);
-            if (n > 2) wait_loads<2 * LOADS>(); else if (n > 1) wait_loads<LOADS>(); else wait_loads<0>();
-            read(0, 0, 0);
-            int stage = 0, s = 0;               // of the step
-            auto full = [&](int set) {
-                const int next = stage == 2 ? 0 : stage + 1;
-                wait_loads<LOADS>();
-                read(next, set ^ 1, 0);
-                load(stage);
-                multiply(set);
-                stage = next;
-            };
-            for (; s + 4 < n; s += 2) { full(0); full(1); }
-            auto step = [&](int s, int set) {   // the last ones
-                const int next = stage == 2 ? 0 : stage + 1;
-                if (s + 1 < n) {
-                    if (s + 2 < n) wait_loads<LOADS>(); else wait_loads<0>();
+        } else {
+            // A step is one set.  It begins with the next one's operands and the loads of the third one on, into the place of its own.
+            if (n > 0) {
+                load(0);
+                if (n > 1) load(1);
+                if (n > 2) load(2);
+                if (n > 2) wait_loads<2 * LOADS>(); else if (n > 1) wait_loads<LOADS>(); else wait_loads<0>();
+                read(0, 0, 0);
+                int stage = 0, s = 0;               // of the step
+                auto full = [&](int set) {
+                    const int next = stage == 2 ? 0 : stage + 1;
+                    wait_loads<LOADS>();
                     read(next, set ^ 1, 0);
-                    if (s + 3 < n) load(stage);
+                    load(stage);
+                    multiply(set);
+                    stage = next;
+                };
+                for (; s + 4 < n; s += 2) { full(0); full(1); }
+                auto step = [&](int s, int set) {   // the last ones
+                    const int next = stage == 2 ? 0 : stage + 1;
+                    if (s + 1 < n) {
+                        if (s + 2 < n) wait_loads<LOADS>(); else wait_loads<0>();
+                        read(next, set ^ 1, 0);
+                        if (s + 3 < n) load(stage);
+                    }
+                    multiply(set);
+                    stage = next;
+                };
+                for (; s < n; s += 2) {
+                    step(s, 0);
+                    if (s + 1 < n) step(s + 1, 1);
                 }
-                multiply(set);
-                stage = next;
-            };
-            for (; s < n; s += 2) {
-                step(s, 0);
-                if (s + 1 < n) step(s + 1, 1);
             }
         }
-    }
-    settle_products();
+        settle_products();
 
-    // Results go through LDS, so that whole lines of memory are read and written: column l % 16 of a product is a row of C, its rows
-    // 4 (l / 16) .. + 3 are columns.  Then eight columns of a row a thread: the first four of each eight lie together, then the last
-    // four, both in an order that depends on the row, so that neither side meets bank conflicts.
-    constexpr int ALL = STAGES * STAGE, PASSES = (BM * BN * 4 + ALL - 1) / ALL, PM = TM / PASSES, ROWS = BM / PASSES, NT = 64 * WAVES;
-    constexpr int UNITS = GATED ? BN / 16 : BN / 8, EACH = ROWS * UNITS / NT, AHEAD = 2;
-    static_assert(PASSES * PM == TM && EACH % AHEAD == 0, "whole passes");
-    char* stage = lds[0];
-    auto granule = [&](int row, int g) { return (floatx4*)(stage + row * BN * 4 + ((((g >> 1) + (g & 1) * (BN / 8)) ^ (row & 15)) << 4)); };
-    float* part = n == sh.steps ? nullptr : a.part + ((int64_t)sharer * 2 + (from == 0)) * (BM * BN);
+        // Results go through LDS, so that whole lines of memory are read and written: column l % 16 of a product is a row of C, its rows
+        // 4 (l / 16) .. + 3 are columns.  Then eight columns of a row a thread: the first four of each eight lie together, then the last
+        // four, both in an order that depends on the row, so that neither side meets bank conflicts.
+        constexpr int ALL = STAGES * STAGE, PASSES = (BM * BN * 4 + ALL - 1) / ALL, PM = TM / PASSES, ROWS = BM / PASSES, NT = 64 * WAVES;
+        constexpr int UNITS = GATED ? BN / 16 : BN / 8, EACH = ROWS * UNITS / NT, AHEAD = 2;
+        static_assert(PASSES * PM == TM && EACH % AHEAD == 0, "whole passes");
+        char* stage = lds[0];
+        auto granule = [&](int row, int g) { return (floatx4*)(stage + row * BN * 4 + ((((g >> 1) + (g & 1) * (BN / 8)) ^ (row & 15)) << 4)); };
+        float* part = n == sh.steps ? nullptr : a.part + ((int64_t)sharer * 2 + (from == 0)) * (BM * BN);
 #pragma unroll
-    for (int pass = 0; pass < PASSES; ++pass) {
-        __syncthreads();
+        for (int pass = 0; pass < PASSES; ++pass) {
+            __syncthreads();
 #pragma unroll
-        for (int i = 0; i < PM; ++i)
+            for (int i = 0; i < PM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                // gated: the gate's columns, then the other projection's
-                const int g = GATED ? (wn * (TN / 2) + j % (TN / 2)) * 4 + j / (TN / 2) * (BN / 8) : (wn * TN + j) * 4;
-                *granule((wm * PM + i) * 16 + (lane & 15), g + (lane >> 4)) = acc[pass * PM + i][j];
+                for (int j = 0; j < TN; ++j) {
+                    // gated: the gate's columns, then the other projection's
+                    const int g = GATED ? (wn * (TN / 2) + j % (TN / 2)) * 4 + j / (TN / 2) * (BN / 8) : (wn * TN + j) * 4;
+                    *granule((wm * PM + i) * 16 + (lane & 15), g + (lane >> 4)) = acc[pass * PM + i][j];
+                }
+            __syncthreads();
+            if (part) {
+                for (int i = threadIdx.x; i < ROWS * (BN / 4); i += NT) {
+                    const int local = i / (BN / 4), g = i % (BN / 4), row = (local / (PM * 16) * TM + pass * PM) * 16 + local % (PM * 16);
+                    *(floatx4*)(part + row * BN + g * 4) = *granule(local, g);
+                }
+                continue;
             }
-        __syncthreads();
-        if (part) {
-            for (int i = threadIdx.x; i < ROWS * (BN / 4); i += NT) {
-                const int local = i / (BN / 4), g = i % (BN / 4), row = (local / (PM * 16) * TM + pass * PM) * 16 + local % (PM * 16);
-                *(floatx4*)(part + row * BN + g * 4) = *granule(local, g);
-            }
-            continue;
-        }
 #pragma unroll 1
-        for (int u0 = 0; u0 < EACH; u0 += AHEAD) {
-            floatx4 va[AHEAD][2], vb[AHEAD][2];
-            int row[AHEAD], col[AHEAD], local[AHEAD];
-            bool on[AHEAD];
+            for (int u0 = 0; u0 < EACH; u0 += AHEAD) {
+                floatx4 va[AHEAD][2], vb[AHEAD][2];
+                int row[AHEAD], col[AHEAD], local[AHEAD];
+                bool on[AHEAD];
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const int unit = (u0 + u) * NT + threadIdx.x;
-                local[u] = unit / UNITS;
-                row[u] = m0 + (local[u] / (PM * 16) * TM + pass * PM) * 16 + local[u] % (PM * 16);
-                col[u] = n0 + unit % UNITS * 8;
-                on[u] = row[u] < M && col[u] < (EPI == EPI_OUT ? N : a.hidden_p);
-                if constexpr (EPI == EPI_BACK) {
-                    const int64_t p = on[u] ? (int64_t)row[u] * a.hidden_p + col[u] : 0;
+                for (int u = 0; u < AHEAD; ++u) {
+                    const int unit = (u0 + u) * NT + threadIdx.x;
+                    local[u] = unit / UNITS;
+                    row[u] = m0 + (local[u] / (PM * 16) * TM + pass * PM) * 16 + local[u] % (PM * 16);
+                    col[u] = n0 + unit % UNITS * 8;
+                    on[u] = row[u] < M && col[u] < (EPI == EPI_OUT ? N : a.hidden_p);
+                    if constexpr (EPI == EPI_BACK) {
+                        const int64_t p = on[u] ? (int64_t)row[u] * a.hidden_p + col[u] : 0;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) { va[u][h] = *(const floatx4*)(a.va + p + 4 * h); vb[u][h] = *(const floatx4*)(a.vb + p + 4 * h); }
+                        for (int h = 0; h < 2; ++h) { va[u][h] = *(const floatx4*)(a.va + p + 4 * h); vb[u][h] = *(const floatx4*)(a.vb + p + 4 * h); }
+                    }
                 }
-            }
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const int g = ((u0 + u) * NT + threadIdx.x) % UNITS * 2;
-                float x[8], y[8];
-                *(floatx4*)x = *granule(local[u], g);
-                *(floatx4*)(x + 4) = *granule(local[u], g + 1);
-                if constexpr (GATED) {
-                    *(floatx4*)y = *granule(local[u], g + BN / 8);
-                    *(floatx4*)(y + 4) = *granule(local[u], g + BN / 8 + 1);
+                for (int u = 0; u < AHEAD; ++u) {
+                    const int g = ((u0 + u) * NT + threadIdx.x) % UNITS * 2;
+                    float x[8], y[8];
+                    *(floatx4*)x = *granule(local[u], g);
+                    *(floatx4*)(x + 4) = *granule(local[u], g + 1);
+                    if constexpr (GATED) {
+                        *(floatx4*)y = *granule(local[u], g + BN / 8);
+                        *(floatx4*)(y + 4) = *granule(local[u], g + BN / 8 + 1);
+                    }
+                    if (on[u]) finish<E, EPI>(a, pr, row[u], col[u], x, y, va[u], vb[u]);
                 }
-                if (on[u]) finish<E, EPI>(a, pr, row[u], col[u], x, y, va[u], vb[u]);
             }
         }
-    }
-    left_steps -= n;
-    if (left_steps <= 0) break;
-    ++tile;
-    from = 0;
-    __syncthreads();                            // the next tiles overwrite the results' place
+        left_steps -= n;
+        if (left_steps <= 0) break;
+        ++tile;
+        from = 0;
+        __syncthreads();                            // the next tiles overwrite the results' place
     }
 }
 
@@ -667,9 +746,9 @@ int tile_rows(int32_t dtype, int64_t m, int n, int problems) {
 
 // One product's tiles, workgroups at a time, and the steps of its contraction, at most.
 struct FfnTiles { int rows, cols; int64_t tiles; int slots, steps; };
-FfnTiles ffn_tiles(int32_t dtype, int64_t m, int n, int problems, int of, int64_t k, int segments, bool gated) {
+FfnTiles ffn_tiles(int32_t dtype, int64_t m, int n, int problems, int of, int64_t k, int segments, bool gated, bool whole = false) {
     FfnTiles t{};
-    t.rows = tile_rows(dtype, m, gated ? 2 * n : n, of);
+    t.rows = whole ? 128 : tile_rows(dtype, m, gated ? 2 * n : n, of);
     t.cols = tile_cols(dtype, t.rows);
     t.tiles = (int64_t)tiles_of((int)m, t.rows) * tiles_of(n, gated ? t.cols / 2 : t.cols) * problems;
     t.slots = dtype == PQL_BF16 && t.rows == 128 ? 512 : 256;          // two workgroups a compute unit, one where LDS holds no more
@@ -737,7 +816,7 @@ struct FfnSaved {
     }
 };
 
-template <typename E, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, Epilogue EPI>
+template <typename E, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, Epilogue EPI, bool WHOLE = false>
 hipError_t launch_product(const FfnTiles& t, const FfnArgs& a, int kid, double flops, hipStream_t st) {
     // a grid holds at most 2^32 - 1 threads: results of so many tiles would not fit the memory
     if (t.tiles >= 1 << 22) return hipErrorInvalidConfiguration;
@@ -745,7 +824,7 @@ hipError_t launch_product(const FfnTiles& t, const FfnArgs& a, int kid, double f
     const Shares sh((int)t.tiles, t.slots, t.steps);
     // with rows that are counted on the device, fewer tiles may be shared out otherwise
     const int grid = a.count ? (int)t.tiles / t.slots * t.slots + t.slots : sh.whole + (sh.sharers + 7) / 8 * 8;
-    PQL_LAUNCH(ps, (ffn_product_kernel<E, BM, BN, WM, WN, A_ALONG, B_ALONG, EPI>), dim3(grid), dim3(64 * WM * WN), 0, st, a, t.slots);
+    PQL_LAUNCH(ps, (ffn_product_kernel<E, BM, BN, WM, WN, A_ALONG, B_ALONG, EPI, WHOLE>), dim3(grid), dim3(64 * WM * WN), 0, st, a, t.slots);
     prof_commit(ps, kid, flops, 0.0);
     if (a.count ? t.steps > JOIN_STEPS : sh.joins()) {
         const int blocks = (a.count ? t.slots : sh.rest) * (BM * (EPI == EPI_GATED ? BN / 2 : BN) / 8 / 256);
@@ -754,6 +833,12 @@ hipError_t launch_product(const FfnTiles& t, const FfnArgs& a, int kid, double f
         prof_commit(ps, KID_FFN_JOIN, 0.0, 0.0);
     }
     return hipGetLastError();
+}
+
+// Whether 32-bit weights can be read as they are: whole granules of what becomes 16 bits, too.
+bool whole_ok(const pql_ffn_shape& s, const pql_rows& r, int cols) {
+    return s.dtype == PQL_F32 && ffn_rows(s) <= WHOLE_ROWS && s.dim % 8 == 0 && s.hidden % 8 == 0 && rows_aligned(r, s.dtype) && r.stride >= cols &&
+           r.stride <= 1 << 20;
 }
 
 struct FfnRun {
@@ -779,11 +864,13 @@ struct FfnRun {
     // The matrix as an operand: where it is, or as planes at `to`.
     FfnOperand operand(const pql_rows& r, int rows, int cols, size_t to, int64_t plane, bool tokens, bool direct = true) {
         if (direct && s.dtype == PQL_BF16 && !(tokens && map) && cols % 8 == 0 && rows_aligned(r, s.dtype) && r.stride >= cols && r.stride <= 1 << 20)
-            return {(const bf16_t*)r.data, r.stride, 0};
+            return {(const bf16_t*)r.data, r.stride, 0, false};
+        if (direct && !tokens && whole_ok(s, r, cols))
+            return {(const bf16_t*)r.data, 2 * r.stride, 0, true};
         const int packed = tokens && map ? (noted ? 1 : 2) : 0;         // 2: with the notes, that all of them would make alike
         if (packed) noted = true;
         copies.c[copies.n++] = {r.data, r.stride, at<bf16_t>(to), plane, rows, cols, up8(cols), packed};
-        return {at<bf16_t>(to), up8(cols), plane};
+        return {at<bf16_t>(to), up8(cols), plane, false};
     }
     // Both projections' weights, alike.
     void projections(const pql_ffn_input& in, FfnOperand& gate, FfnOperand& up) {
@@ -826,12 +913,15 @@ struct FfnRun {
     template <bool A_ALONG, bool B_ALONG, Epilogue EPI> void product(const FfnArgs& a, int of, int kid) {
         if (e != hipSuccess) return;
         const FfnProblem& pr = a.prob[0];
-        FfnTiles t = ffn_tiles(s.dtype, pr.m, pr.n, 1, of, a.k, a.segments, EPI == EPI_GATED);
+        const bool whole = pr.b[0].whole;
+        FfnTiles t = ffn_tiles(s.dtype, pr.m, pr.n, 1, of, a.k, a.segments, EPI == EPI_GATED, whole);
         t.tiles = 0;
         for (int i = 0; i < a.problems; ++i)
             t.tiles += (int64_t)tiles_of(a.prob[i].m, t.rows) * tiles_of(a.prob[i].n, EPI == EPI_GATED ? t.cols / 2 : t.cols);
         const double flops = 2.0 * a.problems * (EPI == EPI_GATED ? 2 : 1) * a.segments * pr.m * pr.n * a.k;
-        if (s.dtype == PQL_F32)
+        if (whole) {
+            if constexpr (A_ALONG) e = launch_product<float, 128, 128, 2, 4, A_ALONG, B_ALONG, EPI, true>(t, a, kid, flops, st);
+        } else if (s.dtype == PQL_F32)
             e = t.rows == 256 ? launch_product<float, 256, 128, 2, 4, A_ALONG, B_ALONG, EPI>(t, a, kid, flops, st)
                               : launch_product<float, 128, 128, 2, 4, A_ALONG, B_ALONG, EPI>(t, a, kid, flops, st);
         else
@@ -889,7 +979,8 @@ int32_t pql_ffn_forward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input*
     const FfnPlan p = ffn_plan(*s, PQL_FFN_FORWARD);
     const hipStream_t st = (hipStream_t)stream;
     hipError_t e;
-    if (p.rows <= ffn_few_rows(s->dtype, (double)s->dim * s->hidden * elem_size(s->dtype)) && !saved) {
+    const bool whole = in->gate.stride == in->up.stride && whole_ok(*s, in->gate, s->dim) && whole_ok(*s, in->up, s->dim) && whole_ok(*s, in->down, s->hidden);
+    if (p.rows <= ffn_few_rows(s->dtype, (double)s->dim * s->hidden * elem_size(s->dtype), whole) && !saved) {
         FfnRowsArgs a{{in->lengths, (unsigned)s->steps}, p.rows, s->dim, s->hidden, s->act, in->x.data, in->gate.data, in->up.data, in->down.data,
                       in->x.stride, in->gate.stride, in->up.stride, in->down.stride, (char*)workspace + p.m, p.hidden_p, p.m_plane, out->data, out->stride};
         e = ffn_rows_launch(a, s->dtype, st);
@@ -906,7 +997,7 @@ int32_t pql_ffn_forward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input*
         bf16_t* m = saved ? (bf16_t*)((char*)saved + keep.m) : r.at<bf16_t>(p.m);
         r.gated(x, gate, up, (float*)saved, saved ? (float*)((char*)saved + keep.b) : nullptr, m);
         FfnArgs a = r.args();
-        const FfnOperand om{m, p.hidden_p, p.m_plane};
+        const FfnOperand om{m, p.hidden_p, p.m_plane, false};
         a.prob[0] = {{om, om}, {down, down}, p.rows, s->dim, out->data, out->stride};
         a.k = s->hidden;
         r.product<true, true, EPI_OUT>(a, 1, KID_FFN_PRODUCT);
@@ -943,10 +1034,10 @@ int32_t pql_ffn_backward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input
         r.prepare();
         const FfnSaved keep(p);
         float *va = saved ? (float*)saved : r.at<float>(p.va), *vb = saved ? (float*)((char*)saved + keep.b) : r.at<float>(p.vb);
-        m = {saved ? (const bf16_t*)((const char*)saved + keep.m) : r.at<bf16_t>(p.m), p.hidden_p, p.m_plane};
+        m = {saved ? (const bf16_t*)((const char*)saved + keep.m) : r.at<bf16_t>(p.m), p.hidden_p, p.m_plane, false};
         if (!saved) r.gated(x, gate, up, va, vb, (bf16_t*)m.p);
-        da = {r.at<bf16_t>(p.da), p.hidden_p, p.m_plane};
-        db = {r.at<bf16_t>(p.db), p.hidden_p, p.m_plane};
+        da = {r.at<bf16_t>(p.da), p.hidden_p, p.m_plane, false};
+        db = {r.at<bf16_t>(p.db), p.hidden_p, p.m_plane, false};
         FfnArgs a = r.args();
         a.prob[0] = {{dout, dout}, {down, down}, rows, s->hidden, nullptr, 0};
         a.k = s->dim;

@@ -506,6 +506,34 @@ def test_projections_of_different_layouts(env):
                     assert torch.equal(g, whole[1][k]), k
 
 
+@pytest.mark.parametrize("odd", [None, float("inf"), float("nan"), 3.4e38, 1e-39])
+@pytest.mark.parametrize("rows,d,f,lengths", [(65, 264, 520, None), (300, 136, 72, [1, 0] * 150), (760, 40, 1048, None), (9, 8, 8, None)])
+def test_32_bit_weights_as_they_are_and_as_planes(env, rows, d, f, lengths, odd):
+    """Weights whose rows start on 16-byte boundaries and others take two ways to the same terms: equal bits."""
+    torch, K, ctx = env
+    call = FfnCall(env, (rows, 1, d, f, "float32", "silu", "dense", lengths), seed=6)
+    weights = [call.gate, call.up, call.down]
+    if odd is not None:
+        for w in weights:
+            w[w.shape[0] // 2, w.shape[1] // 3] = odd
+    apart = []
+    for w in weights:
+        wide = torch.full((w.shape[0], w.shape[1] + 3), float("nan"), device="cuda")
+        wide[:, 1:1 + w.shape[1]] = w
+        apart.append(wide[:, 1:1 + w.shape[1]])
+    got = []
+    for w in (weights, apart):
+        call.given = K.FfnInput(call.shape, call.x, *w, call.lengths)
+        out, saved = call.forward(True)
+        got.append(dict(call.backward(saved), out=out))
+    for k, x in got[0].items():
+        assert torch.equal(x.view(torch.int32), got[1][k].view(torch.int32)), k
+    if odd is None:
+        call.close(got[0]["out"], call.want, "out")
+        for k, want in call.want_grad.items():
+            call.close(got[0][k], want, k)
+
+
 def test_feed_forward_gradients_that_are_not_asked_for(env):
     call = FfnCall(env, (3, 50, 136, 260, "float32", "silu", "dense", [50, 20, 0]), seed=2)
     _, saved = call.forward(True)
