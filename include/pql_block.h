@@ -124,17 +124,19 @@ typedef struct {
 typedef struct { pql_rows x, gate, up, down; } pql_ffn_grad;
 
 /*     a = gate x_n,  b = up x_n,  m = act(a) b (element by element),  out_n = down m.
- * saved: NULL, or [device] pql_ffn_saved_bytes(shape) bytes that keep a and b (fp32) for pql_ffn_backward.
- * workspace: [device] pql_ffn_workspace_bytes(shape, PQL_FFN_FORWARD) bytes; both 256-byte aligned.  bf16: m is rounded to bf16 once
- * as an operand of the second product; a and b are not. */
+ * saved: NULL, or [device] pql_ffn_saved_bytes(shape) bytes that keep a and b (fp32) and m for pql_ffn_backward.
+ * workspace: [device] pql_ffn_workspace_bytes(shape, PQL_FFN_FORWARD) bytes; both 256-byte aligned.  bf16: m is rounded to
+ * bf16 once as an operand of the second product, or, in a call of few rows without saved, kept in 16 bits; a and b are in
+ * fp32.  fp32: products of 24-bit operands, sums in fp32. */
 int64_t pql_ffn_saved_bytes(const pql_ffn_shape* shape);
 int64_t pql_ffn_workspace_bytes(const pql_ffn_shape* shape, int32_t call);
 int32_t pql_ffn_forward(pql_ctx* ctx, const pql_ffn_shape* shape, const pql_ffn_input* input, const pql_rows* out,
                         void* saved, void* workspace, void* stream);
 
 /* Gradient of a loss whose gradient with respect to out is out_grad.  saved: as left by pql_ffn_forward of the same
- * shape and input, or NULL: a and b are worked out again.  workspace: pql_ffn_workspace_bytes(shape, PQL_FFN_BACKWARD or, without
- * saved, PQL_FFN_BACKWARD_ALONE) bytes. */
+ * shape and input (lengths among it), or NULL: a, b and m are worked out again.  bf16: m and the gradients of a and b are
+ * rounded to bf16 once as operands of the products that follow.  workspace: pql_ffn_workspace_bytes(shape,
+ * PQL_FFN_BACKWARD or, without saved, PQL_FFN_BACKWARD_ALONE) bytes. */
 int32_t pql_ffn_backward(pql_ctx* ctx, const pql_ffn_shape* shape, const pql_ffn_input* input, const void* saved,
                          const pql_rows* out_grad, const pql_ffn_grad* grads, void* workspace, void* stream);
 
