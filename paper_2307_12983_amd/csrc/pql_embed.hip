@@ -6,6 +6,10 @@
 // one order.  The table's rows are cleared while the list is sorted.  Then a wavefront works through a chunk of the list: runs
 // that begin and end in it are written, of the others it sums its part, and a last launch joins the parts in order.  That
 // bounds the work on one run, however often its token occurs.
+//
+// 512 x 32 rows of 256 in fp32, 20 tokens of 1020 each: the lookup takes 17 us (rows come from the caches at 21 TB/s), the gradient
+// 51 us, half of it the three launches of the sort and half the sums (18 TB/s).  8192 rows of 2048 in bf16, a token of 65536 each: 19 us and
+// 84 us, of which 54 us clear the table at 5 TB/s while the tokens are sorted beside.
 #include "pql_block_internal.h"
 
 namespace pql {
@@ -87,7 +91,8 @@ __device__ __forceinline__ void clear_table(const EmbedArgs& a) {
 
 // Few places (at most RANK_MAX): each one's place in the sorted list is the number of smaller keys and of equal ones before it.  All
 // pairs are compared, with the keys in LDS: one launch where a pass over a digit takes three.  PACKED: key and place in one number
-// (vocab below 2^19), so that one comparison decides.
+// (vocab below 2^19), so that one comparison decides.  us for 8192 places of 65536 tokens 27 (by digits 42), of 1000 17 (17); for 4097 of 1000
+// 10 (17).
 constexpr int RANK_BITS = 13, RANK_MAX = 1 << RANK_BITS, RANK_WG = 256, RANK_LANES = 8;
 template <bool PACKED> __global__ void __launch_bounds__(RANK_WG) embed_rank_kernel(EmbedArgs a) {
     __shared__ uint4 keys4[RANK_MAX / 4];
@@ -368,6 +373,8 @@ struct EmbedPlan {
 EmbedPlan embed_plan(const pql_embed_shape& s) {
     EmbedPlan p{};
     p.n = embed_rows(s) * (unsigned)s.per_row;
+    // as many chunks as fill the card, then longer ones, which leave fewer parts to join (us for sums and joins: 4096 places of 1000 tokens
+    // 10, with chunks of 256 42; 327680 of 1020 47, with chunks of 16 63, of 256 46)
     p.chunk = 16;
     while (p.chunk < 256 && p.n / p.chunk > 8192) p.chunk *= 2;
     p.chunks = (int)((p.n + (unsigned)p.chunk - 1) / p.chunk);

@@ -516,18 +516,19 @@ def test_32_bit_weights_as_they_are_and_as_planes(env, rows, d, f, lengths, odd)
     if odd is not None:
         for w in weights:
             w[w.shape[0] // 2, w.shape[1] // 3] = odd
-    apart = []
-    for w in weights:
-        wide = torch.full((w.shape[0], w.shape[1] + 3), float("nan"), device="cuda")
-        wide[:, 1:1 + w.shape[1]] = w
-        apart.append(wide[:, 1:1 + w.shape[1]])
+    def within(w, before, behind):
+        wide = torch.full((w.shape[0], before + w.shape[1] + behind), float("nan"), device="cuda")
+        wide[:, before:before + w.shape[1]] = w
+        return wide[:, before:before + w.shape[1]]
+
     got = []
-    for w in (weights, apart):
+    for w in (weights, [within(x, 1, 2) for x in weights], [within(x, 8, 4) for x in weights]):
         call.given = K.FfnInput(call.shape, call.x, *w, call.lengths)
         out, saved = call.forward(True)
         got.append(dict(call.backward(saved), out=out))
-    for k, x in got[0].items():
-        assert torch.equal(x.view(torch.int32), got[1][k].view(torch.int32)), k
+    for other in got[1:]:
+        for k, x in got[0].items():
+            assert torch.equal(x.view(torch.int32), other[k].view(torch.int32)), k
     if odd is None:
         call.close(got[0]["out"], call.want, "out")
         for k, want in call.want_grad.items():
