@@ -285,6 +285,10 @@ template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT, wav
                 h[i] += a.scale_y * y[i] * (g[i] * post[i]);
             }
         }
+        // rows that do not count, beside others that do: weights that are not finite must not make anything of their zeros
+        if (!s.on)
+#pragma unroll
+            for (int i = 0; i < EPT; ++i) h[i] = 0.f;
         if (a.next) {
             float du[EPT];
             s.open(now.next, du);
@@ -304,6 +308,9 @@ template <typename E, bool AL, int NT> __global__ void __launch_bounds__(NT, wav
             }
         }
         const bool live = s.on;
+        if (!live)
+#pragma unroll
+            for (int i = 0; i < EPT; ++i) dh[i] = 0.f;
         if (a.dx) {
             float out[EPT];
 #pragma unroll

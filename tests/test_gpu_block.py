@@ -329,6 +329,26 @@ def test_outputs_in_the_inputs_places(env):
         assert torch.equal(dx, grads["x"]) and torch.equal(dy, grads["y"])
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("dim,groups", [(64, 1), (96, 3), (2048, 1), (4096, 8)])
+def test_rows_that_do_not_count_meet_no_weights(env, dim, groups, dtype):
+    """Zeros where nothing counts, and no part in any gradient, also under weights that are not finite."""
+    torch, K, ctx = env
+    n, t, dt = 5, 7, getattr(torch, dtype)
+    odd = lambda: torch.tensor([float("inf"), float("nan"), -float("inf"), 1.0] * (dim // 4), device="cuda")  # noqa: E731
+    rows = lambda: torch.full((n, t, dim), float("nan"), dtype=dt, device="cuda")  # noqa: E731
+    shape = K.residual_shape(n, t, dim, dt, groups=groups, gate_cols=dim, gate_act="silu", eps_post=1e-5, eps_pre=1e-5)
+    given = K.ResidualInput(shape, rows(), rows(), rows(), odd(), odd(), torch.zeros(n, dtype=torch.int32, device="cuda"))
+    got = {k: rows() for k in ("sum", "next", "x", "y", "gate")}
+    got.update({k: torch.full((dim,), float("nan"), device="cuda") for k in ("post", "pre")})
+    ctx.pql_residual_forward(shape, given, K.Rows(got["sum"]), K.Rows(got["next"]))
+    grads = K.ResidualGrad(shape, **{k: got[k] for k in ("x", "y", "gate", "post", "pre")})
+    work = K.workspace(ctx.residual_workspace_bytes(shape))
+    ctx.pql_residual_backward(shape, given, K.Rows(rows()), K.Rows(rows()), grads, work)
+    for k, x in got.items():
+        assert torch.equal(x, torch.zeros_like(x)), k
+
+
 def test_rows_that_repeat(env):
     """One row of x for all of them: every repetition has its own gradient."""
     torch, K, ctx = env
