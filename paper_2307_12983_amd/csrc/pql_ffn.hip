@@ -28,10 +28,13 @@ namespace {
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
-// Terms of a value, elements of the contraction a step, steps in LDS at a time.
-template <typename E, int BM> struct Mode { static constexpr int TERMS = 1, BK = 64, STAGES = 2; };
-template <> struct Mode<float, 128> { static constexpr int TERMS = 3, BK = 32, STAGES = 3; };
-template <> struct Mode<float, 256> { static constexpr int TERMS = 3, BK = 32, STAGES = 2; };
+// Terms of a value, elements of the contraction a step, steps in LDS at a time; the fewest steps that a part of a tile is worth, whose
+// sums are written and read again (us a call with 1 / 4 / 8 / 12 of them: bf16, 65 rows of 1000 and 4000 53 / 38 / 36 / 38, 2048 rows
+// of 1024 and 1024 45 / 45 / 41 / 33, 300 rows of 512 and 2048 with gradients 92 / 70 / 67 / 75; fp32, the last 144 / 138 / 140 / 167, 1665
+// rows of 203 and 677 with gradients 130 / 131 / 137 / 146, 512 x 32 rows of 256 and 1024 with gradients 401 / 417).
+template <typename E, int BM> struct Mode { static constexpr int TERMS = 1, BK = 64, STAGES = 2, LEAST = BM == 128 ? 8 : 4; };
+template <> struct Mode<float, 128> { static constexpr int TERMS = 3, BK = 32, STAGES = 3, LEAST = 1; };
+template <> struct Mode<float, 256> { static constexpr int TERMS = 3, BK = 32, STAGES = 2, LEAST = 1; };
 // As many tiles of 256 rows make them worth it, fewer leave compute units without one (us a launch, 256 / 128 rows: 256 tiles, 2048 rows of
 // 2048 and 2048 in fp32 162 / 193, 4096 rows in bf16 65 / 68; 128 tiles, the same calls' last product 100 with its join / 100 and 57 / 36).
 constexpr int BIG_TILES = 192;
@@ -254,15 +257,16 @@ template <typename E, Epilogue EPI> __device__ __forceinline__ void finish(const
 
 // ---- how the tiles are shared out ------------------------------------------------------------------------
 // `slots` workgroups run at a time.  As many whole rounds of tiles as there are go to a workgroup each; the `rest` tiles behind
-// them are cut into steps of their contractions, of which each of `sharers` workgroups takes `per` in a row, at most a tile's.
-// What is not a whole tile is left as sums, joined by another launch.  Known where the rows that count are: on the device.
+// them are cut into steps of their contractions, of which each of `sharers` workgroups takes `per` in a row, `least` or more and at
+// most a tile's.  What is not a whole tile is left as sums, joined by another launch.  Known where the rows that count are: on the device.
 constexpr int JOIN_STEPS = 7;                   // that the other launch takes as long as: fewer are not worth it, and never launch it
 struct Shares {
     int whole, rest, steps, per, sharers;
-    __host__ __device__ Shares(int tiles, int slots, int steps_) : steps(steps_) {
+    __host__ __device__ Shares(int tiles, int slots, int steps_, int least) : steps(steps_) {
         whole = tiles / slots * slots;
         rest = tiles - whole;
         per = (int)(((int64_t)rest * steps + slots - 1) / slots);
+        if (per > 0 && per < least) per = least;
         if (per > steps - JOIN_STEPS) per = steps;
         sharers = per > 0 ? (int)(((int64_t)rest * steps + per - 1) / per) : rest;
     }
@@ -329,7 +333,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
     constexpr int COLS = GATED ? BN / 2 : BN;
     const int count = a.count ? *a.count : 0, rows = a.count && !a.count_is_k ? count : -1, K = a.count && a.count_is_k ? count : a.k;
     const int ksteps = (K + BK - 1) / BK;
-    const Shares sh(all_tiles<BM, COLS>(a, rows), slots, ksteps * a.segments);
+    const Shares sh(all_tiles<BM, COLS>(a, rows), slots, ksteps * a.segments, Mode<E, BM>::LEAST);
     // this workgroup's steps, of `tile` and perhaps the one behind it
     int tile, from, left_steps;
     if ((int)blockIdx.x < sh.whole) {
@@ -618,7 +622,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
 template <typename E, int BM, int BN, Epilogue EPI> __global__ void __launch_bounds__(256) ffn_join_kernel(FfnArgs a, int slots, int bk) {
     constexpr int COLS = EPI == EPI_GATED ? BN / 2 : BN, UNITS = COLS / 8;
     const int count = a.count ? *a.count : 0, rows = a.count && !a.count_is_k ? count : -1, K = a.count && a.count_is_k ? count : a.k;
-    const Shares sh(all_tiles<BM, COLS>(a, rows), slots, (K + bk - 1) / bk * a.segments);
+    const Shares sh(all_tiles<BM, COLS>(a, rows), slots, (K + bk - 1) / bk * a.segments, Mode<E, BM>::LEAST);
     if (!sh.joins()) return;
     constexpr int BLOCKS = BM * UNITS / 256;    // of a tile
     for (int b = blockIdx.x; b < sh.rest * BLOCKS; b += gridDim.x) {
@@ -823,12 +827,12 @@ hipError_t launch_product(const FfnTiles& t, const FfnArgs& a, int kid, double f
     // a grid holds at most 2^32 - 1 threads: results of so many tiles would not fit the memory
     if (t.tiles >= 1 << 22) return hipErrorInvalidConfiguration;
     ProfSlot ps = prof_slot();
-    const Shares sh((int)t.tiles, t.slots, t.steps);
+    const Shares sh((int)t.tiles, t.slots, t.steps, Mode<E, BM>::LEAST);
     // with rows that are counted on the device, fewer tiles may be shared out otherwise
     const int grid = a.count ? (int)t.tiles / t.slots * t.slots + t.slots : sh.whole + (sh.sharers + 7) / 8 * 8;
     PQL_LAUNCH(ps, (ffn_product_kernel<E, BM, BN, WM, WN, A_ALONG, B_ALONG, EPI, WHOLE>), dim3(grid), dim3(64 * WM * WN), 0, st, a, t.slots);
     prof_commit(ps, kid, flops, 0.0);
-    if (a.count ? t.steps > JOIN_STEPS : sh.joins()) {
+    if (a.count ? t.steps >= JOIN_STEPS + Mode<E, BM>::LEAST : sh.joins()) {
         const int blocks = (a.count ? t.slots : sh.rest) * (BM * (EPI == EPI_GATED ? BN / 2 : BN) / 8 / 256);
         ps = prof_slot();
         PQL_LAUNCH(ps, (ffn_join_kernel<E, BM, BN, EPI>), dim3(blocks < 1024 ? blocks : 1024), dim3(256), 0, st, a, t.slots, sizeof(E) == 4 ? 32 : 64);
@@ -982,7 +986,7 @@ int32_t pql_ffn_forward(pql_ctx* c, const pql_ffn_shape* s, const pql_ffn_input*
     const hipStream_t st = (hipStream_t)stream;
     hipError_t e;
     const bool whole = in->gate.stride == in->up.stride && whole_ok(*s, in->gate, s->dim) && whole_ok(*s, in->up, s->dim) && whole_ok(*s, in->down, s->hidden);
-    if (p.rows <= ffn_few_rows(s->dtype, (double)s->dim * s->hidden * elem_size(s->dtype), whole) && !saved) {
+    if (p.rows <= ffn_few_rows(s->dtype, (int64_t)s->dim * s->hidden, whole) && !saved) {
         FfnRowsArgs a{{in->lengths, (unsigned)s->steps}, p.rows, s->dim, s->hidden, s->act, in->x.data, in->gate.data, in->up.data, in->down.data,
                       in->x.stride, in->gate.stride, in->up.stride, in->down.stride, (char*)workspace + p.m, p.hidden_p, p.m_plane, out->data, out->stride};
         e = ffn_rows_launch(a, s->dtype, st);

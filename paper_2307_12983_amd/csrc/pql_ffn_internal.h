@@ -35,15 +35,14 @@ __device__ __forceinline__ Terms three_terms(float x) {
 }
 
 // Calls of at most so many rows take the kernels for few rows, which read the rows again for each 16 outputs; the tiles' kernels read
-// them once, but split rows and 32-bit weights into terms and join sums.  By the bytes of a projection; whole: the tiles' kernels can
-// read 32-bit weights as they are.  us a call, rows / tiles.  64 rows: fp32, 1024 and 4096 (16 MiB) 37 / 60, 1408 and 5632 (30 MiB) 95 /
-// 78, with planes of 2048 and 8192 136 / 195; bf16, 1024 and 4096 (8 MiB) 22 / 52, 1408 and 5632 (15 MiB) 50 / 50.  2048 and 8192: fp32
-// (64 MiB) 32 rows 82 / 112, 48 rows 127 / 112; bf16 (32 MiB) 45 / 54 and 62 / 53.  4096 and 16384: fp32 (256 MiB) 32 rows 311 / 332, 48
-// rows 447 / 333; bf16 (128 MiB) 16 rows 117 / 118, 24 rows 142 / 121.
+// them once, but split rows and 32-bit weights into terms and join sums.  By the elements of a projection; whole: the tiles' kernels can
+// read 32-bit weights as they are.  us a call, rows / tiles.  1024 and 4096 (4 Mi), 64 rows: fp32 37 / 60, bf16 22 / 31.  1408 and 5632, 64
+// rows: 95 / 78 and 50 / 37, 32 rows: 54 / 76 and 29 / 36.  2048 and 8192, 32 rows: 82 / 112 and 43 / 48; with planes of fp32 weights 64 rows 136 /
+// 195.  4096 and 16384 (64 Mi): fp32 32 rows 311 / 332, bf16 16 rows 117 / 128, 24 rows 142 / 121.
 constexpr int FFN_FEW_ROWS = 64;
-inline int ffn_few_rows(int32_t dtype, double projection, bool whole) {
-    if (projection <= 16 << 20 || (dtype == PQL_F32 && !whole)) return FFN_FEW_ROWS;
-    return dtype == PQL_F32 || projection <= 64 << 20 ? 32 : 16;
+inline int ffn_few_rows(int32_t dtype, int64_t elements, bool whole) {
+    if (elements <= 4 << 20 || (dtype == PQL_F32 && !whole)) return FFN_FEW_ROWS;
+    return dtype == PQL_F32 || elements <= 32 << 20 ? 32 : 16;
 }
 
 struct FfnRowsArgs {
