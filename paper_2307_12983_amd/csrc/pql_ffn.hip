@@ -259,7 +259,9 @@ template <typename E, Epilogue EPI> __device__ __forceinline__ void finish(const
 // `slots` workgroups run at a time.  As many whole rounds of tiles as there are go to a workgroup each; the `rest` tiles behind
 // them are cut into steps of their contractions, of which each of `sharers` workgroups takes `per` in a row, `least` or more and at
 // most a tile's.  What is not a whole tile is left as sums, joined by another launch.  Known where the rows that count are: on the device.
-constexpr int JOIN_STEPS = 7;                   // that the other launch takes as long as: fewer are not worth it, and never launch it
+// Steps that the other launch takes as long as: fewer saved are not worth it, and contractions of no more never launch it (us a call with
+// gradients for 6 / 7 / 8 of them: 5 x 333 rows of 203 and 677 165 / 156 / 156, 512 x 32 rows of 256 and 1024 422 / 414 / 431).
+constexpr int JOIN_STEPS = 7;
 struct Shares {
     int whole, rest, steps, per, sharers;
     __host__ __device__ Shares(int tiles, int slots, int steps_, int least) : steps(steps_) {
