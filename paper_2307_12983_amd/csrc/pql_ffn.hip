@@ -219,6 +219,13 @@ template <typename E> __device__ __forceinline__ void store_terms(bf16_t* p, int
     }
 }
 
+// Columns behind the last, whose sums are those of zeros and NaN in a row that holds an infinite value: they are operands of the next
+// products, against zeros.
+__device__ __forceinline__ void clear_behind(int n, int col, float (&x)[8]) {
+    if (col + 8 <= n) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = col + e < n ? x[e] : 0.f;
+}
 // Eight columns of a row of the result from their sums; gated: those of both projections.
 template <typename E, Epilogue EPI> __device__ __forceinline__ void finish(const FfnArgs& a, const FfnProblem& pr, int row, int col, float (&x)[8], float (&y)[8],
                                                                        const floatx4 (&va)[2], const floatx4 (&vb)[2]) {
@@ -232,6 +239,7 @@ template <typename E, Epilogue EPI> __device__ __forceinline__ void finish(const
         activate_all<E>(a.act, x, f, d);
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] *= y[e];
+        clear_behind(pr.n, col, f);
         store_terms<E>(a.m + at, a.m_plane, f);
     } else if constexpr (EPI == EPI_BACK) {
         float p[8], b[8], f[8], d[8];
@@ -240,6 +248,8 @@ template <typename E, Epilogue EPI> __device__ __forceinline__ void finish(const
         activate_all<E>(a.act, p, f, d);
 #pragma unroll
         for (int e = 0; e < 8; ++e) { p[e] = x[e] * b[e] * d[e]; x[e] *= f[e]; }
+        clear_behind(pr.n, col, p);
+        clear_behind(pr.n, col, x);
         store_terms<E>(a.da + at, a.m_plane, p);
         store_terms<E>(a.db + at, a.m_plane, x);
     } else {

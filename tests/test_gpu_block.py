@@ -825,3 +825,46 @@ def test_more_rows_than_a_grid_holds_workgroups_for(env):
     ctx.pql_embed_forward(shape, tokens, None, K.Rows(table), K.Rows(out))
     for at in (0, 1 << 22, 1 << 23, rows - 11):
         assert torch.equal(out[0, at:at + 11], table[tokens[0, at:at + 11, 0].long()])
+
+
+# ---- infinite values -----------------------------------------------------------------------------------------------
+def infinite_rows(env, dtype, rows, d, f, lengths=None, act="none", seed=8):
+    """A call whose weights' signs and sizes make every result of the rows with an infinite element infinite, of one sign a column."""
+    torch, K, ctx = env
+    call = FfnCall(env, (1, rows, d, f, dtype, act, "dense", lengths), seed)
+    m = call.made
+    sign = np.where(np.arange(d) % 3 == 0, -1.0, 1.0)
+    size = lambda *s: np.where(m.rng.random(s) < 0.5, 1.0, 1.1 + m.rng.random(s))  # noqa: E731  of one term and of three
+    call.gate, call.up = m.place(size(f, d)), m.place(size(f, d))
+    call.down = m.place(sign[:, None] * size(d, f))
+    at = [r for r in (3, rows // 2) if lengths is None or r < lengths[0]]
+    for r in at:
+        call.x[0, r], call.out_grad[0, r] = m.place(size(d)), m.place(sign * size(d))
+        call.x[0, r, r % d] = float("inf")
+    call.given = K.FfnInput(call.shape, call.x, call.gate, call.up, call.down, call.lengths)
+    h = [np.nan_to_num(m.host(z), nan=0.0, posinf=np.inf) for z in (call.x, call.gate, call.up, call.down)]
+    with np.errstate(invalid="ignore"):
+        call.want = O.ffn(*h, act, lengths)
+        call.want_grad = O.ffn_grad(*h, act, np.nan_to_num(m.host(call.out_grad)), lengths)
+    return call, at
+
+
+def same_kind(call, got, want, what):
+    """Infinite where the definition is, with its sign, NaN where it is, and close to it elsewhere."""
+    off = got.double().cpu().numpy()
+    finite = np.isfinite(want)
+    assert np.array_equal(np.where(finite, 0.0, want), np.where(finite, 0.0, off), equal_nan=True), what
+    call.close(got.masked_fill(~call.made.torch.tensor(finite, device="cuda"), 0), np.where(finite, want, 0.0), what)
+
+
+@pytest.mark.parametrize("rows,d,f", [(9, 13, 21), (70, 13, 21), (70, 24, 37), (300, 61, 203)])
+def test_infinite_tokens_next_to_columns_that_are_not_there(env, rows, d, f):
+    """Widths of no whole granule in bf16: what stands behind the last column of m and its gradient meets zeros."""
+    call, at = infinite_rows(env, "bfloat16", rows, d, f)
+    assert all(np.all(np.isinf(call.want[0, r])) and np.all(np.isinf(call.want_grad["x"][0, r])) for r in at)
+    outs = call.forward(False)[0], *call.forward(True)
+    for out in outs[:2]:
+        same_kind(call, out, call.want, "out")
+    for saved in (outs[2], None):
+        for k, g in call.backward(saved).items():
+            same_kind(call, g, call.want_grad[k], k)
