@@ -51,8 +51,9 @@ def activate(act, x):
     if act == "gelu":
         half = 0.5 * (1 + _erf(x / math.sqrt(2)))
         return x * half, half + x * np.exp(-0.5 * x * x) / math.sqrt(2 * math.pi)
-    s = 0.5 * (1 + np.tanh(0.5 * x))
-    return (s, s * (1 - s)) if act == "sigmoid" else (x * s, s * (1 + x * (1 - s)))
+    e = np.exp(-np.abs(x))                              # s and 1 - s, neither from the other
+    s, rest = np.where(x < 0, e, 1.0) / (1 + e), np.where(x < 0, 1.0, e) / (1 + e)
+    return (s, s * rest) if act == "sigmoid" else (x * s, s * (1 + x * rest))
 
 
 # ---- norms, gate and residual sum -----------------------------------------------------------------------

@@ -60,7 +60,12 @@ __device__ __forceinline__ float exp_near(float x) {
     const float t = x * 1.44269504f, r = fmaf(x, 1.44269504f, -t) + x * 1.92596299e-8f;
     return __builtin_amdgcn_exp2f(t) * fmaf(r, 0.693147181f, 1.f);
 }
-__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + exp_near(-x)); }
+// s = 1 / (1 + exp(-x)) and 1 - s, neither from the other: both keep all their bits where they are small.
+struct Sigmoid { float s, rest; };
+__device__ __forceinline__ Sigmoid sigmoid(float x) {
+    const float e = exp_near(-fabsf(x)), large = __builtin_amdgcn_rcpf(1.f + e), small = e * large;
+    return x < 0.f ? Sigmoid{small, large} : Sigmoid{large, small};
+}
 // Half of erfc(-x / sqrt 2), the normal distribution's share below x.  fp32: by the library's erfc.  bf16: by the rational
 // approximation 7.1.26 of Abramowitz and Stegun, off by 1.5e-7 at most (its tail is not exact relative to itself, only to 1), a
 // quarter of the time: a step of 16384 rows took 131 us for its projections with erfc.
@@ -76,11 +81,11 @@ __device__ __forceinline__ float share_below(float x, bf16_t) {
 struct Act { float f, d; };
 template <int ACT, typename E> __device__ __forceinline__ Act activate(float x) {
     if constexpr (ACT == PQL_ACT_SIGMOID) {
-        const float s = sigmoid(x);
-        return {s, s * (1.f - s)};
+        const Sigmoid g = sigmoid(x);
+        return {g.s, g.s * g.rest};
     } else if constexpr (ACT == PQL_ACT_SILU) {
-        const float s = sigmoid(x);
-        return {x * s, s * (1.f + x * (1.f - s))};
+        const Sigmoid g = sigmoid(x);
+        return {x * g.s, g.s * (1.f + x * g.rest)};
     } else if constexpr (ACT == PQL_ACT_GELU) {
         const float h = share_below(x, E{});
         return {x * h, h + x * (0.39894228f * __builtin_amdgcn_exp2f(-0.72134752f * x * x))};

@@ -868,3 +868,28 @@ def test_infinite_tokens_next_to_columns_that_are_not_there(env, rows, d, f):
     for saved in (outs[2], None):
         for k, g in call.backward(saved).items():
             same_kind(call, g, call.want_grad[k], k)
+
+
+# ---- activations far from zero -------------------------------------------------------------------------------------
+def gate_values(env, dtype, act, x):
+    """act(x) and act'(x) as a residual call and its gradient give them: y and the sum's gradient are ones, there are no norms."""
+    torch, K, ctx = env
+    gate = torch.tensor(x).to(getattr(torch, dtype)).cuda().view(1, 1, -1)
+    one, d = torch.ones_like(gate), gate.shape[-1]
+    shape = K.residual_shape(1, 1, d, gate.dtype, gate_cols=d, gate_act=act)
+    given = K.ResidualInput(shape, None, one, gate)
+    f, slope = torch.empty_like(one), torch.empty_like(one)
+    ctx.pql_residual_forward(shape, given, K.Rows(f), None)
+    ctx.pql_residual_backward(shape, given, K.Rows(one), None, K.ResidualGrad(shape, gate=slope), None)
+    return f, slope, gate.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("act", ["sigmoid", "silu"])
+def test_activations_far_from_zero(env, act):
+    """Relative to the terms they are sums of: e = exp(-|x|) is off by 3 u, 1 / (1 + e) by 1.5 + 1 + 2 u, e times that by 7 u at most,
+    and the products and sums that follow by u each: 8 u for x s, 14.5 u for either slope."""
+    f, slope, x = gate_values(env, "float32", act, np.linspace(-80, 80, 8192))
+    s, q = 1 / (1 + np.exp(-x)), 1 / (1 + np.exp(x))
+    want, terms = (s, s * q) if act == "sigmoid" else (x * s, s * (1 + np.abs(x) * q))
+    assert np.all(np.abs(f.double().cpu().numpy() - want) <= 10 * U * np.abs(want))
+    assert np.all(np.abs(slope.double().cpu().numpy() - (s * q if act == "sigmoid" else s * (1 + x * q))) <= 16 * U * terms)
