@@ -57,6 +57,7 @@ struct FfnArgs {
     int count_is_k;                             // whether they are the contraction or the rows of the result
     float* part;                                // [workgroups][2][tile] sums over parts of the contraction
     const int* map;                             // packed row -> row of the output, NULL: the same
+    int a_along, b_along;                       // whether the contraction runs along the operand's rows in memory
     int act;
     // gated, back: [row][hidden_p]
     int hidden_p;
@@ -219,12 +220,44 @@ template <typename E> __device__ __forceinline__ void store_terms(bf16_t* p, int
     }
 }
 
-// Columns behind the last, whose sums are those of zeros and NaN in a row that holds an infinite value: they are operands of the next
-// products, against zeros.
-__device__ __forceinline__ void clear_behind(int n, int col, float (&x)[8]) {
-    if (col + 8 <= n) return;
+// Sums of 32-bit values that came out as NaN, once more and as fp32 products: an infinite value is one term, and meets all terms of the
+// other operand, of which some are zero or of the other sign; so do products that overflow.  What is NaN by itself is found out as
+// soon as it is, and stays.  Nothing of this runs where sums are finite: the check takes no time that could be measured.
+__device__ __forceinline__ float value_of(const FfnOperand& o, bool along, int i, int k) {
+    if (o.whole) return ((const float*)o.p)[along ? i * (o.stride / 2) + k : k * (o.stride / 2) + i];
+    const bf16_t* p = o.p + (along ? i * o.stride + k : k * o.stride + i);
+    return (float)p[0] + ((float)p[o.plane] + (float)p[2 * o.plane]);
+}
+__device__ __forceinline__ bool any_nan(const float (&x)[8]) {
+    return __builtin_isunordered(x[0], x[1]) | __builtin_isunordered(x[2], x[3]) | __builtin_isunordered(x[4], x[5]) | __builtin_isunordered(x[6], x[7]);
+}
+// Whether there was such a sum.
+__device__ __forceinline__ bool sum_again(const FfnArgs& a, const FfnProblem& pr, int K, int row, int col, int first_b, float (&x)[8]) {
+    if (__builtin_expect(!any_nan(x), 1)) return false;
+    float s[8] = {};
+#pragma unroll 1
+    for (int seg = 0; seg < a.segments; ++seg) {
+        const FfnOperand &oa = pr.a[seg], &ob = pr.b[first_b + seg];
+#pragma unroll 1
+        for (int k = 0; k < K; ++k) {
+            const float u = value_of(oa, a.a_along, row, k);
+            bool open = false;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = col + e < n ? x[e] : 0.f;
+            for (int e = 0; e < 8; ++e) {
+                s[e] = fmaf(u, value_of(ob, a.b_along, min(col + e, pr.n - 1), k), s[e]);
+                open |= x[e] != x[e] && s[e] == s[e];
+            }
+            if (!open) return true;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = x[e] != x[e] && s[e] == s[e] ? s[e] : x[e];
+    return true;
+}
+// a and b of eight columns.
+__device__ __forceinline__ void read_saved(const FfnArgs& a, int64_t at, floatx4 (&va)[2], floatx4 (&vb)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) { va[h] = *(const floatx4*)(a.va + at + 4 * h); vb[h] = *(const floatx4*)(a.vb + at + 4 * h); }
 }
 // Eight columns of a row of the result from their sums; gated: those of both projections.
 template <typename E, Epilogue EPI> __device__ __forceinline__ void finish(const FfnArgs& a, const FfnProblem& pr, int row, int col, float (&x)[8], float (&y)[8],
@@ -239,7 +272,6 @@ template <typename E, Epilogue EPI> __device__ __forceinline__ void finish(const
         activate_all<E>(a.act, x, f, d);
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] *= y[e];
-        clear_behind(pr.n, col, f);
         store_terms<E>(a.m + at, a.m_plane, f);
     } else if constexpr (EPI == EPI_BACK) {
         float p[8], b[8], f[8], d[8];
@@ -248,8 +280,6 @@ template <typename E, Epilogue EPI> __device__ __forceinline__ void finish(const
         activate_all<E>(a.act, p, f, d);
 #pragma unroll
         for (int e = 0; e < 8; ++e) { p[e] = x[e] * b[e] * d[e]; x[e] *= f[e]; }
-        clear_behind(pr.n, col, p);
-        clear_behind(pr.n, col, x);
         store_terms<E>(a.da + at, a.m_plane, p);
         store_terms<E>(a.db + at, a.m_plane, x);
     } else {
@@ -583,6 +613,17 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
                     *granule((wm * PM + i) * 16 + (lane & 15), g + (lane >> 4)) = acc[pass * PM + i][j];
                 }
             __syncthreads();
+            // What stands behind the last column is an operand of the next products, against zeros: its sums are those of zeros, and NaN in
+            // a row that holds an infinite value.
+            if (EPI != EPI_OUT && N % 8 != 0 && n0 + COLS > N) {
+                const int from = N - n0, behind = 8 - N % 8;
+                for (int i = threadIdx.x; i < ROWS * behind; i += NT) {
+                    const int row = i / behind, c = from + i % behind;
+#pragma unroll
+                    for (int h = 0; h < (GATED ? 2 : 1); ++h) ((float*)granule(row, (c >> 2) + h * (BN / 8)))[c & 3] = 0.f;
+                }
+                __syncthreads();
+            }
             if (part) {
                 for (int i = threadIdx.x; i < ROWS * (BN / 4); i += NT) {
                     const int local = i / (BN / 4), g = i % (BN / 4), row = (local / (PM * 16) * TM + pass * PM) * 16 + local % (PM * 16);
@@ -590,6 +631,24 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
                 }
                 continue;
             }
+            // Eight columns of a row: where they are, and their sums from LDS.
+            auto place = [&](int u, int& local, int& row, int& col) {
+                const int unit = u * NT + threadIdx.x;
+                local = unit / UNITS;
+                row = m0 + (local / (PM * 16) * TM + pass * PM) * 16 + local % (PM * 16);
+                col = n0 + unit % UNITS * 8;
+                return row < M && col < (EPI == EPI_OUT ? N : a.hidden_p);
+            };
+            auto sums = [&](int u, int local, float (&x)[8], float (&y)[8]) {
+                const int g = (u * NT + threadIdx.x) % UNITS * 2;
+                *(floatx4*)x = *granule(local, g);
+                *(floatx4*)(x + 4) = *granule(local, g + 1);
+                if constexpr (GATED) {
+                    *(floatx4*)y = *granule(local, g + BN / 8);
+                    *(floatx4*)(y + 4) = *granule(local, g + BN / 8 + 1);
+                }
+            };
+            bool odd = false;
 #pragma unroll 1
             for (int u0 = 0; u0 < EACH; u0 += AHEAD) {
                 floatx4 va[AHEAD][2], vb[AHEAD][2];
@@ -597,28 +656,32 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
                 bool on[AHEAD];
 #pragma unroll
                 for (int u = 0; u < AHEAD; ++u) {
-                    const int unit = (u0 + u) * NT + threadIdx.x;
-                    local[u] = unit / UNITS;
-                    row[u] = m0 + (local[u] / (PM * 16) * TM + pass * PM) * 16 + local[u] % (PM * 16);
-                    col[u] = n0 + unit % UNITS * 8;
-                    on[u] = row[u] < M && col[u] < (EPI == EPI_OUT ? N : a.hidden_p);
-                    if constexpr (EPI == EPI_BACK) {
-                        const int64_t p = on[u] ? (int64_t)row[u] * a.hidden_p + col[u] : 0;
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) { va[u][h] = *(const floatx4*)(a.va + p + 4 * h); vb[u][h] = *(const floatx4*)(a.vb + p + 4 * h); }
-                    }
+                    on[u] = place(u0 + u, local[u], row[u], col[u]);
+                    if constexpr (EPI == EPI_BACK) read_saved(a, on[u] ? (int64_t)row[u] * a.hidden_p + col[u] : 0, va[u], vb[u]);
                 }
 #pragma unroll
                 for (int u = 0; u < AHEAD; ++u) {
-                    const int g = ((u0 + u) * NT + threadIdx.x) % UNITS * 2;
                     float x[8], y[8];
-                    *(floatx4*)x = *granule(local[u], g);
-                    *(floatx4*)(x + 4) = *granule(local[u], g + 1);
-                    if constexpr (GATED) {
-                        *(floatx4*)y = *granule(local[u], g + BN / 8);
-                        *(floatx4*)(y + 4) = *granule(local[u], g + BN / 8 + 1);
-                    }
+                    sums(u0 + u, local[u], x, y);
+                    if constexpr (TERMS == 3) odd |= any_nan(x) || (GATED && any_nan(y));
                     if (on[u]) finish<E, EPI>(a, pr, row[u], col[u], x, y, va[u], vb[u]);
+                }
+            }
+            if constexpr (TERMS == 3) {
+                static_assert(TERMS != 3 || PASSES == 1, "all sums are in LDS still");
+                if (__builtin_expect(!odd, 1)) continue;
+#pragma unroll 1
+                for (int u = 0; u < EACH; ++u) {
+                    floatx4 va[2], vb[2];
+                    float x[8], y[8];
+                    int row, col, local;
+                    if (!place(u, local, row, col)) continue;
+                    sums(u, local, x, y);
+                    bool again = sum_again(a, pr, K, row, col, 0, x);
+                    if constexpr (GATED) again |= sum_again(a, pr, K, row, col, 1, y);
+                    if (!again) continue;
+                    if constexpr (EPI == EPI_BACK) read_saved(a, (int64_t)row * a.hidden_p + col, va, vb);
+                    finish<E, EPI>(a, pr, row, col, x, y, va, vb);
                 }
             }
         }
@@ -631,7 +694,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
 }
 
 // Tiles whose sums are in parts: those of consecutive workgroups, added in order.  Eight columns of a row a thread.
-template <typename E, int BM, int BN, Epilogue EPI> __global__ void __launch_bounds__(256) ffn_join_kernel(FfnArgs a, int slots, int bk) {
+template <typename E, int BM, int BN, Epilogue EPI> __global__ void __launch_bounds__(256, 8) ffn_join_kernel(FfnArgs a, int slots, int bk) {
     constexpr int COLS = EPI == EPI_GATED ? BN / 2 : BN, UNITS = COLS / 8;
     const int count = a.count ? *a.count : 0, rows = a.count && !a.count_is_k ? count : -1, K = a.count && a.count_is_k ? count : a.k;
     const Shares sh(all_tiles<BM, COLS>(a, rows), slots, (K + bk - 1) / bk * a.segments, Mode<E, BM>::LEAST);
@@ -661,10 +724,10 @@ template <typename E, int BM, int BN, Epilogue EPI> __global__ void __launch_bou
             }
         }
         floatx4 va[2], vb[2];
-        if constexpr (EPI == EPI_BACK) {
-            const int64_t p = (int64_t)row * a.hidden_p + col;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) { va[h] = *(const floatx4*)(a.va + p + 4 * h); vb[h] = *(const floatx4*)(a.vb + p + 4 * h); }
+        if constexpr (EPI == EPI_BACK) read_saved(a, (int64_t)row * a.hidden_p + col, va, vb);
+        if constexpr (Mode<E, BM>::TERMS == 3) {
+            sum_again(a, pr, K, row, col, 0, x);
+            if constexpr (EPI == EPI_GATED) sum_again(a, pr, K, row, col, 1, y);
         }
         finish<E, EPI>(a, pr, row, col, x, y, va, vb);
     }
@@ -928,8 +991,9 @@ struct FfnRun {
         return a;
     }
     // of: the problems of a full call, which the plan has counted with.
-    template <bool A_ALONG, bool B_ALONG, Epilogue EPI> void product(const FfnArgs& a, int of, int kid) {
+    template <bool A_ALONG, bool B_ALONG, Epilogue EPI> void product(FfnArgs a, int of, int kid) {
         if (e != hipSuccess) return;
+        a.a_along = A_ALONG; a.b_along = B_ALONG;
         const FfnProblem& pr = a.prob[0];
         const bool whole = pr.b[0].whole;
         FfnTiles t = ffn_tiles(s.dtype, pr.m, pr.n, 1, of, a.k, a.segments, EPI == EPI_GATED, whole);

@@ -17,8 +17,8 @@ __device__ __forceinline__ void settle_products() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// x = h + m + l exactly: the nearest bf16 (8 bits), the next 8 bits of the rest, and what is left.  Values that are not finite
-// are their first term alone.
+// x = h + m + l, exactly from 2^-110 on (below, terms fall under the smallest normal number, 2^-126): the nearest bf16 (8 bits), the
+// next 8 bits of the rest, and what is left.  Values that are not finite are their first term alone.
 struct Terms { float t[3]; };
 __device__ __forceinline__ Terms three_terms(float x) {
     Terms s;

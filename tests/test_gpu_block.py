@@ -893,3 +893,56 @@ def test_activations_far_from_zero(env, act):
     want, terms = (s, s * q) if act == "sigmoid" else (x * s, s * (1 + np.abs(x) * q))
     assert np.all(np.abs(f.double().cpu().numpy() - want) <= 10 * U * np.abs(want))
     assert np.all(np.abs(slope.double().cpu().numpy() - (s * q if act == "sigmoid" else s * (1 + x * q))) <= 16 * U * terms)
+
+
+@pytest.mark.parametrize("act", ["none", "sigmoid"])
+@pytest.mark.parametrize("rows,d,f,lengths", [
+    (9, 24, 40, None), (64, 264, 520, None), (65, 264, 520, None), (65, 13, 21, None),       # few rows and tiles, aligned weights and others
+    (300, 136, 264, [190]), (70, 24, 1544, None), (2100, 40, 24, None)])                      # rows that do not count, joined parts
+def test_infinite_tokens_in_32_bits(env, rows, d, f, lengths, act):
+    """What fp32 arithmetic gives, whatever the number of rows: three terms of a value must not make NaN of an infinite one."""
+    call, at = infinite_rows(env, "float32", rows, d, f, lengths, act)
+    assert all(np.all(np.isinf(call.want[0, r])) for r in at)
+    outs = call.forward(False)[0], *call.forward(True)
+    for out in outs[:2]:
+        same_kind(call, out, call.want, "out")
+    for saved in (outs[2], None):
+        for k, g in call.backward(saved).items():
+            same_kind(call, g, call.want_grad[k], k)
+
+
+@pytest.mark.parametrize("rows", [33, 200])
+@pytest.mark.parametrize("which", ["gate", "up", "down"])
+@pytest.mark.parametrize("odd", [float("inf"), float("-inf"), float("nan")])
+def test_infinite_weights_in_32_bits(env, rows, which, odd, monkeypatch):
+    """The activation and its derivative are those of 32 bits: rows of ones sum to a = 120, where the sigmoid's derivative, e^-120 = 8e-53,
+    is below half the smallest 32-bit number, 2^-150 = 7e-46, so that it is 0 and an infinite up makes NaN of its product with it."""
+    call, _ = infinite_rows(env, "float32", rows, 72, 104, act="sigmoid")
+    call.x.copy_(env[0].where(call.x.isinf(), 1.0, call.x))
+    getattr(call, which)[5, 7] = odd
+    h = [call.made.host(z) for z in (call.x, call.gate, call.up, call.down)]
+    exact = O.activate
+    monkeypatch.setattr(O, "activate", lambda act, x: tuple(v.astype(np.float32).astype(np.float64) for v in exact(act, x)))
+    with np.errstate(invalid="ignore"):
+        call.want, call.want_grad = O.ffn(*h, "sigmoid"), O.ffn_grad(*h, "sigmoid", call.made.host(call.out_grad))
+    out, saved = call.forward(True)
+    same_kind(call, call.forward(False)[0], call.want, "out")
+    same_kind(call, out, call.want, "out with saved")
+    for k, g in call.backward(saved).items():
+        same_kind(call, g, call.want_grad[k], k)
+
+
+def test_sums_that_overflow_in_32_bits(env):
+    """Products of finite values beyond the largest one: infinite in a call of few rows and in one of many."""
+    torch, K, ctx = env
+    for rows in (20, 100):
+        x = torch.randn(1, rows, 40, device="cuda")
+        gate, up, down = (torch.rand(*s, device="cuda") + 0.1 for s in ((56, 40), (56, 40), (40, 56)))
+        x[0, 3], x[0, 5] = 3.1e30, -2.7e30                      # m: 1e31 squared
+        shape = K.ffn_shape(x, gate, "none")
+        out, saved = torch.empty_like(x), K.workspace(ctx.ffn_saved_bytes(shape))
+        for keep in (None, saved):
+            ctx.pql_ffn_forward(shape, K.FfnInput(shape, x, gate, up, down), K.Rows(out), keep, K.workspace(ctx.ffn_workspace_bytes(shape, K.FFN_FORWARD)))
+            odd = out.isinf()
+            assert bool((out[0, 3] == float("inf")).all()) and bool((out[0, 5] == float("inf")).all())
+            assert int(odd.sum()) == 80 and not bool(out.isnan().any())
