@@ -222,7 +222,7 @@ template <typename E> __device__ __forceinline__ void store_terms(bf16_t* p, int
 
 // Sums of 32-bit values that came out as NaN, once more and as fp32 products: an infinite value is one term, and meets all terms of the
 // other operand, of which some are zero or of the other sign; so do products that overflow.  What is NaN by itself is found out as
-// soon as it is, and stays.  Nothing of this runs where sums are finite: the check takes no time that could be measured.
+// soon as it is, and stays.  Where sums are finite the check takes 2 of 405 us (512 x 32 rows of 256 and 1024 with gradients).
 __device__ __forceinline__ float value_of(const FfnOperand& o, bool along, int i, int k) {
     if (o.whole) return ((const float*)o.p)[along ? i * (o.stride / 2) + k : k * (o.stride / 2) + i];
     const bf16_t* p = o.p + (along ? i * o.stride + k : k * o.stride + i);

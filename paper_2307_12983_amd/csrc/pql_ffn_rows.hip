@@ -121,6 +121,15 @@ template <typename E, int T, bool AL, bool GATED> __global__ void __launch_bound
             for (int v = 0; v < WAVES; ++v) s[m] += sums[v][m * T + t][l][e];
         }
         if (n >= a.rows || out >= outputs) continue;
+        if constexpr (!GATED && M_TERMS<E> == 2) {
+            // an infinite weight met both terms of m, the second of which is zero or of either sign: m itself decides
+            if (__builtin_expect(s[0] != s[0], 0)) {
+                const E *m = (const E*)a.m + (int64_t)n * a.m_stride, *down = (const E*)a.down + out * a.down_stride;
+                float sum = 0.f;
+                for (int k = 0; k < size && sum == sum; ++k) sum = fmaf(to_float(m[k]) + to_float(m[a.m_plane + k]), to_float(down[k]), sum);
+                s[0] = sum;
+            }
+        }
         if constexpr (GATED) {
             float f[1] = {s[0]}, d[1];
             activate_all<E>(a.act, f, f, d);

@@ -932,6 +932,24 @@ def test_infinite_weights_in_32_bits(env, rows, which, odd, monkeypatch):
         same_kind(call, g, call.want_grad[k], k)
 
 
+@pytest.mark.parametrize("rows", [12, 33, 200])
+@pytest.mark.parametrize("which", ["gate", "up", "down"])
+@pytest.mark.parametrize("odd", [float("inf"), float("-inf"), float("nan")])
+def test_infinite_weights_in_16_bits(env, rows, which, odd):
+    """In calls of few rows as well, whose m has two terms."""
+    call, _ = infinite_rows(env, "bfloat16", rows, 72, 104)
+    call.x.copy_(env[0].where(call.x.isinf(), 1.0, call.x))
+    getattr(call, which)[5, 7] = odd
+    h = [call.made.host(z) for z in (call.x, call.gate, call.up, call.down)]
+    with np.errstate(invalid="ignore"):
+        call.want, call.want_grad = O.ffn(*h, "none"), O.ffn_grad(*h, "none", call.made.host(call.out_grad))
+    out, saved = call.forward(True)
+    same_kind(call, call.forward(False)[0], call.want, "out")
+    same_kind(call, out, call.want, "out with saved")
+    for k, g in call.backward(saved).items():
+        same_kind(call, g, call.want_grad[k], k)
+
+
 def test_sums_that_overflow_in_32_bits(env):
     """Products of finite values beyond the largest one: infinite in a call of few rows and in one of many."""
     torch, K, ctx = env
