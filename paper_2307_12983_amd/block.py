@@ -170,6 +170,15 @@ def _ints(t, count, what):
     return t.data_ptr()
 
 
+def _space(t, size, what):
+    """The pointer of memory of at least so many bytes; None stays None."""
+    if t is None:
+        return None
+    if t.numel() * t.element_size() < size or not t.is_contiguous():
+        raise ValueError("%s: expected at least %d contiguous bytes, got %d" % (what, size, t.nbytes))
+    return t.data_ptr()
+
+
 def embed_shape(tokens, table, scale: float) -> PqlEmbedShape:
     """The shape of a call from its tokens [batch, steps, per_row] and its table [vocab, dim]."""
     if tokens.dim() != 3 or table.dim() != 2:
@@ -248,7 +257,7 @@ class FfnInput(_Ffn):
 
     def __init__(self, shape, x, gate, up, down, lengths=None):
         super().__init__(PqlFfnInput, shape, x, gate, up, down, "FfnInput")
-        self.lengths = lengths
+        self.lengths, self.sizes = lengths, {}
         self.c.lengths = _ints(lengths, shape.batch, "FfnInput: lengths")
         _one_device("FfnInput", x, lengths)
 
@@ -294,8 +303,9 @@ class BlockContext(S.StudentContext):
 
     def pql_embed_backward(self, shape, tokens, lengths, out_grad: Rows, table_grad: Rows, workspace, stream=None):
         s, t, n, table, rows = self._embed(shape, tokens, lengths, table_grad, out_grad)
+        space = _space(workspace, self.lib.pql_embed_workspace_bytes(s), "workspace")
         stream = _stream(stream, tokens.get_device(), out_grad.dev, table_grad.dev, *_dev(lengths, workspace))
-        self._check(self.lib.pql_embed_backward(self.h, s, t, n, rows, table, B._ptr(workspace), stream))
+        self._check(self.lib.pql_embed_backward(self.h, s, t, n, rows, table, space, stream))
 
     @staticmethod
     def _of(shape, *described):
@@ -313,17 +323,28 @@ class BlockContext(S.StudentContext):
                               stream=None):
         self._of(shape, given, grads)
         total, after = _ref(sum_grad, given.key, "sum_grad"), _ref(next_grad, given.key, "next_grad")
+        used = workspace is not None and (grads.c.post or grads.c.pre)
+        space = _space(workspace, self.residual_workspace_bytes(shape) if used else 0, "workspace")
         stream = _stream(stream, given.dev, grads.dev, *(r.dev for r in (sum_grad, next_grad) if r is not None), *_dev(workspace))
-        self._check(self.lib.pql_residual_backward(self.h, C.byref(shape), given.ref, total, after, grads.ref, B._ptr(workspace), stream))
+        self._check(self.lib.pql_residual_backward(self.h, C.byref(shape), given.ref, total, after, grads.ref, space, stream))
+
+    def _spaces(self, shape, given, saved, workspace, call):
+        need = given.sizes.get(call)                # asked for once for each description
+        if need is None:
+            rows = shape.batch * shape.steps        # none: nothing of either is used
+            need = given.sizes[call] = (self.ffn_saved_bytes(shape), self.ffn_workspace_bytes(shape, call)) if rows else (0, 0)
+        return _space(saved, need[0], "saved"), _space(workspace, need[1], "workspace")
 
     def pql_ffn_forward(self, shape, given: FfnInput, out: Rows, saved, workspace, stream=None):
         self._of(shape, given)
         rows = _ref(out, given.key, "out")
+        kept, space = self._spaces(shape, given, saved, workspace, FFN_FORWARD)
         stream = _stream(stream, given.dev, *(() if out is None else (out.dev,)), *_dev(saved, workspace))
-        self._check(self.lib.pql_ffn_forward(self.h, C.byref(shape), given.ref, rows, B._ptr(saved), B._ptr(workspace), stream))
+        self._check(self.lib.pql_ffn_forward(self.h, C.byref(shape), given.ref, rows, kept, space, stream))
 
     def pql_ffn_backward(self, shape, given: FfnInput, saved, out_grad: Rows, grads: FfnGrad, workspace, stream=None):
         self._of(shape, given, grads)
         rows = _ref(out_grad, given.key, "out_grad")
+        kept, space = self._spaces(shape, given, saved, workspace, FFN_BACKWARD_ALONE if saved is None else FFN_BACKWARD)
         stream = _stream(stream, given.dev, grads.dev, *(() if out_grad is None else (out_grad.dev,)), *_dev(saved, workspace))
-        self._check(self.lib.pql_ffn_backward(self.h, C.byref(shape), given.ref, B._ptr(saved), rows, grads.ref, B._ptr(workspace), stream))
+        self._check(self.lib.pql_ffn_backward(self.h, C.byref(shape), given.ref, kept, rows, grads.ref, space, stream))

@@ -387,3 +387,58 @@ def test_binding_refuses_matrices_that_do_not_fit():
     for bad in ((z(2, 8), w), (x, z(12, 7)), (x, w.bfloat16())):
         with pytest.raises(ValueError):
             K.ffn_shape(*bad, "silu")
+
+
+# ---- what a call is refused for: arguments that fit get as far as the check of the device, which tensors of the host do not pass ----
+AWAY = "tensors of another device"
+
+
+def blocks(torch):
+    """A call of each kind on tensors of the host, as (function of its arguments, arguments that fit, memory that it needs)."""
+    ctx = K.BlockContext()
+    z = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt)  # noqa: E731
+    space = lambda n: torch.zeros(n, dtype=torch.uint8)  # noqa: E731
+    tokens, table, out = z(2, 3, 4, dt=torch.int32), z(9, 6), z(2, 3, 6)
+    es = K.embed_shape(tokens, table, 1.0)
+    rs = K.residual_shape(2, 3, 8, torch.float32, 2, 2, "silu", 1e-5, 1e-5)
+    given = K.ResidualInput(rs, z(2, 3, 8), z(2, 3, 8), z(2, 3, 2), z(8), z(8))
+    fs = K.ffn_shape(z(2, 3, 8), z(12, 8), "silu")
+    f = K.FfnInput(fs, z(2, 3, 8), z(12, 8), z(12, 8), z(8, 12))
+    need = [ctx.ffn_workspace_bytes(fs, c) for c in range(3)]
+    x = lambda: K.Rows(z(2, 3, 8))  # noqa: E731
+    return z, space, [
+        (ctx.pql_embed_forward, dict(shape=es, tokens=tokens, lengths=None, table=K.Rows(table), out=K.Rows(out)), {}),
+        (ctx.pql_embed_backward, dict(shape=es, tokens=tokens, lengths=None, out_grad=K.Rows(out), table_grad=K.Rows(table),
+                                      workspace=space(ctx.embed_workspace_bytes(es))), dict(workspace=ctx.embed_workspace_bytes(es))),
+        (ctx.pql_residual_forward, dict(shape=rs, given=given, sum=x(), next=x()), {}),
+        (ctx.pql_residual_backward, dict(shape=rs, given=given, sum_grad=x(), next_grad=x(), grads=K.ResidualGrad(rs, post=z(8)),
+                                         workspace=space(ctx.residual_workspace_bytes(rs))), dict(workspace=ctx.residual_workspace_bytes(rs))),
+        (ctx.pql_ffn_forward, dict(shape=fs, given=f, out=x(), saved=space(ctx.ffn_saved_bytes(fs)), workspace=space(need[0])),
+         dict(saved=ctx.ffn_saved_bytes(fs), workspace=need[0])),
+        (ctx.pql_ffn_backward, dict(shape=fs, given=f, saved=space(ctx.ffn_saved_bytes(fs)), out_grad=x(), grads=K.FfnGrad(fs), workspace=space(need[1])),
+         dict(saved=ctx.ffn_saved_bytes(fs), workspace=need[1])),
+        (ctx.pql_ffn_backward, dict(shape=fs, given=f, saved=None, out_grad=x(), grads=K.FfnGrad(fs), workspace=space(need[2])), dict(workspace=need[2])),
+    ]
+
+
+def refused(call, args, match, **bad):
+    with pytest.raises(ValueError, match=match):
+        call(**{**args, **bad}, stream=0)
+
+
+def test_binding_refuses_memory_that_is_too_small():
+    import torch
+    _, space, calls = blocks(torch)
+    for call, args, need in calls:
+        refused(call, args, AWAY)
+        for name, size in need.items():
+            assert size > 0
+            refused(call, args, "%s: expected at least %d contiguous bytes, got %d" % (name, size, size - 1), **{name: space(size - 1)})
+            refused(call, args, name + ": expected at least", **{name: space(2 * size)[::2]})
+            refused(call, args, AWAY, **{name: space(size + 8)[8:]})
+    # one shape, three sizes: what is enough with saved is not without
+    call, args, need = calls[-1]
+    refused(call, args, "workspace: expected at least", workspace=calls[-2][1]["workspace"])
+    # no gradient of a weight: no workspace is used
+    call, args, _ = calls[3]
+    refused(call, args, AWAY, workspace=space(1), grads=K.ResidualGrad(args["shape"]))
