@@ -442,3 +442,57 @@ def test_binding_refuses_memory_that_is_too_small():
     # no gradient of a weight: no workspace is used
     call, args, _ = calls[3]
     refused(call, args, AWAY, workspace=space(1), grads=K.ResidualGrad(args["shape"]))
+
+
+def test_binding_refuses_calls_by_what_does_not_fit():
+    """Each refusal by its own message; what fits is refused for its device alone."""
+    import torch
+    z, space, calls = blocks(torch)
+    e, er = calls[0], calls[1]
+    tokens, table = e[1]["tokens"], torch.zeros(9, 6)
+    for bad, match in ((dict(tokens=tokens.long()), "tokens: expected a contiguous int32 tensor of 24"), (dict(tokens=tokens[:1]), "tokens: expected"),
+                       (dict(tokens=tokens.transpose(0, 1)), "tokens: expected a contiguous"), (dict(lengths=z(2)), "lengths: expected a contiguous int32"),
+                       (dict(lengths=z(3, dt=torch.int32)), "lengths: expected a contiguous int32 tensor of 2")):
+        refused(e[0], e[1], match, **bad)
+        refused(er[0], er[1], match, **bad)
+    for bad in (K.Rows(z(8, 6)), K.Rows(table.bfloat16()), K.Rows(z(9, 5))):
+        refused(e[0], e[1], "table: 9 rows of 6 \\(type 0\\) expected", table=bad)
+        refused(er[0], er[1], "table: 9 rows of 6 \\(type 0\\) expected", table_grad=bad)
+    for bad in (K.Rows(z(2, 3, 5)), K.Rows(z(2, 4, 6)), K.Rows(z(2, 3, 6).bfloat16())):
+        refused(e[0], e[1], "rows: 6 rows of 6 \\(type 0\\) expected", out=bad)
+        refused(er[0], er[1], "rows: 6 rows of 6 \\(type 0\\) expected", out_grad=bad)
+    x, narrow = K.Rows(z(2, 3, 8)), K.Rows(z(2, 3, 7))
+    other = K.residual_shape(2, 3, 8, torch.float32, 2, 2, "gelu", 1e-5, 1e-5)
+    for call, args, _ in calls[2:4]:
+        refused(call, args, "do not agree", shape=other)
+        refused(call, args, "do not agree", given=K.ResidualInput(other, z(2, 3, 8), z(2, 3, 8), z(2, 3, 2)))
+    refused(*calls[3][:2], "do not agree", grads=K.ResidualGrad(other))
+    for names, (call, args, _) in zip((("sum", "next"), ("sum_grad", "next_grad")), calls[2:4]):
+        for name in names:
+            refused(call, args, name + ": 6 rows of 8", **{name: narrow})
+            refused(call, args, name + ": 6 rows of 8", **{name: K.Rows(z(2, 3, 8).bfloat16())})
+            refused(call, args, AWAY, **{name: None})
+    other = K.ffn_shape(z(2, 3, 8), z(12, 8), "gelu")
+    away = K.FfnInput(other, z(2, 3, 8), z(12, 8), z(12, 8), z(8, 12))
+    for call, args, _ in calls[4:]:
+        refused(call, args, "do not agree", shape=other)
+        refused(call, args, "do not agree", given=away)
+        name = "out" if "out" in args else "out_grad"
+        refused(call, args, name + ": 6 rows of 8", **{name: narrow})
+        refused(call, args, AWAY, **{name: x})
+        if "grads" in args:
+            refused(call, args, "do not agree", grads=K.FfnGrad(other))
+    # the descriptions
+    rs, fs = calls[2][1]["shape"], calls[4][1]["shape"]
+    good = dict(x=z(2, 3, 8), y=z(2, 3, 8), gate=z(2, 3, 2), post=z(8), pre=z(8))
+    for bad, match in ((dict(x=z(2, 3, 7)), "x: 6 rows of 8"), (dict(y=z(2, 2, 8)), "y: 6 rows of 8"), (dict(gate=z(2, 3, 8)), "gate: 6 rows of 2"),
+                       (dict(post=z(7)), "post: expected a contiguous float32 tensor of 8"), (dict(pre=z(8).bfloat16()), "pre: expected"),
+                       (dict(x=z(2, 3, 8).bfloat16()), "x: 6 rows of 8"), (dict(lengths=z(2, dt=torch.int64)), "lengths: expected")):
+        with pytest.raises(ValueError, match="ResidualInput: " + match):
+            K.ResidualInput(rs, **{**good, **bad})
+    good = dict(x=z(2, 3, 8), gate=z(12, 8), up=z(12, 8), down=z(8, 12))
+    for bad, match in ((dict(x=z(2, 3, 7)), "x: 6 rows of 8"), (dict(x=z(3, 3, 8)), "x: 6 rows of 8"), (dict(gate=z(11, 8)), "gate: 12 rows of 8"),
+                       (dict(up=z(12, 8).bfloat16()), "up: 12 rows of 8"), (dict(down=z(12, 8)), "down: 8 rows of 12"),
+                       (dict(lengths=z(3, dt=torch.int32)), "lengths: expected a contiguous int32 tensor of 2")):
+        with pytest.raises(ValueError, match="FfnInput: " + match):
+            K.FfnInput(fs, **{**good, **bad})
