@@ -11,6 +11,8 @@ Tolerances, from the arithmetic (u = 2^-24, the rounding of a 32-bit operation):
                product passes on to a result whose terms have random signs as it is, or up to twice that where one factor is smooth.
 An output in bf16 is rounded once more, by at most half the spacing of its values, which is taken off first.  Single elements
 may be off by 40 times the bound of the norm, relative to the larger of the element and the root mean square.  """
+import math
+
 import numpy as np
 import pytest
 
@@ -893,6 +895,18 @@ def test_activations_far_from_zero(env, act):
     want, terms = (s, s * q) if act == "sigmoid" else (x * s, s * (1 + np.abs(x) * q))
     assert np.all(np.abs(f.double().cpu().numpy() - want) <= 10 * U * np.abs(want))
     assert np.all(np.abs(slope.double().cpu().numpy() - (s * q if act == "sigmoid" else s * (1 + x * q))) <= 16 * U * terms)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_gelu_far_from_zero(env, dtype):
+    """Relative to the terms, beyond the rounding to the type: 7.5 u for the share's polynomial, 3 u for its argument, 2 u for an
+    exponential and 3 u for products, and 2.5 u x^2 for the rounding of its exponent; erfc of the library is within 16 u."""
+    f, slope, x = gate_values(env, dtype, "gelu", np.linspace(-12, 12, 8192))
+    below = 0.5 * np.array([math.erfc(-v / math.sqrt(2)) for v in x.ravel()]).reshape(x.shape)
+    far = x * np.exp(-0.5 * x * x) / math.sqrt(2 * math.pi)
+    bound = (16 + 2.5 * x * x) * U
+    assert np.all(error_of(f, x * below)[0] <= bound * np.abs(x) * below)
+    assert np.all(error_of(slope, below + far)[0] <= bound * (below + np.abs(far)))
 
 
 @pytest.mark.parametrize("act", ["none", "sigmoid"])
