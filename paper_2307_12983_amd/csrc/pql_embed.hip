@@ -171,6 +171,12 @@ __global__ void __launch_bounds__(1024) embed_tiles_kernel(EmbedArgs a) {
     }
     if (part == 0) a.total[d] = all;
 }
+// What lanes of a wavefront have read from and written to LDS before comes before what they read and write behind it.
+__device__ __forceinline__ void lanes_meet() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
 template <bool FIRST> __global__ void __launch_bounds__(SORT_WG) embed_move_kernel(EmbedArgs a) {
     __shared__ unsigned at[SORT_WAVES][1 << DIGIT_BITS];
     __shared__ unsigned sums[SORT_WAVES];
@@ -227,11 +233,11 @@ template <bool FIRST> __global__ void __launch_bounds__(SORT_WG) embed_move_kern
             const unsigned go = at[wave][d] + before;
             a.key_to[go] = key[r];
             a.row_to[go] = row[r];
-            // the last lane of a digit counts on; the others have read by then, in lockstep
-            __builtin_amdgcn_wave_barrier();
+            // the last lane of a digit counts on, when the others have read, and for those of the next 64 places
+            lanes_meet();
             if (same >> lane == 1) at[wave][d] = go + 1;
         }
-        __builtin_amdgcn_wave_barrier();
+        lanes_meet();
     }
 }
 

@@ -829,6 +829,24 @@ def test_more_rows_than_a_grid_holds_workgroups_for(env):
         assert torch.equal(out[0, at:at + 11], table[tokens[0, at:at + 11, 0].long()])
 
 
+@pytest.mark.parametrize("vocab", [3, 700, 40000])
+@pytest.mark.parametrize("which", ["equal", "in turn", "runs", "pairs", "any"])
+def test_every_place_is_counted_once(env, vocab, which):
+    """More places than are sorted in one launch, in patterns that meet in one wavefront; whole numbers, whose sums are exact."""
+    torch, K, ctx = env
+    n, dim = 20011, 8
+    at = torch.arange(n, device="cuda")
+    tokens = {"equal": at * 0 + vocab - 1, "in turn": at % min(vocab, 65), "runs": at // 63 % vocab, "pairs": at // 2 * 31 % vocab,
+              "any": torch.randint(0, vocab, (n,), device="cuda")}[which].int().view(1, n, 1)
+    grad = torch.randint(-8, 9, (1, n, dim), device="cuda").float()
+    table = torch.empty(vocab, dim, device="cuda")
+    shape = K.embed_shape(tokens, table, 1.0)
+    ctx.pql_embed_backward(shape, tokens, None, K.Rows(grad), K.Rows(table), K.workspace(ctx.embed_workspace_bytes(shape)))
+    want = np.zeros((vocab, dim))
+    np.add.at(want, tokens.flatten().cpu().numpy(), grad[0].double().cpu().numpy())
+    assert np.array_equal(table.double().cpu().numpy(), want)
+
+
 # ---- infinite values -----------------------------------------------------------------------------------------------
 def infinite_rows(env, dtype, rows, d, f, lengths=None, act="none", seed=8):
     """A call whose weights' signs and sizes make every result of the rows with an infinite element infinite, of one sign a column."""
