@@ -899,8 +899,9 @@ struct FfnSaved {
 
 template <typename E, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, Epilogue EPI, bool WHOLE = false>
 hipError_t launch_product(const FfnTiles& t, const FfnArgs& a, int kid, double flops, hipStream_t st) {
-    // a grid holds at most 2^32 - 1 threads: results of so many tiles would not fit the memory
-    if (t.tiles >= 1 << 22) return hipErrorInvalidConfiguration;
+    // A grid holds at most 2^32 - 1 threads, 2^23 workgroups of 512.  Rows are fewer than 2^30, so that two columns of tiles stay below that,
+    // and m of three columns or more (64 KB a tile) would not fit the memory.
+    if ((t.tiles + t.slots) * 64 * WM * WN > 0xffffffffll) return hipErrorInvalidConfiguration;
     ProfSlot ps = prof_slot();
     const Shares sh((int)t.tiles, t.slots, t.steps, Mode<E, BM>::LEAST);
     // with rows that are counted on the device, fewer tiles may be shared out otherwise

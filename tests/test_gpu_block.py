@@ -829,6 +829,56 @@ def test_more_rows_than_a_grid_holds_workgroups_for(env):
         assert torch.equal(out[0, at:at + 11], table[tokens[0, at:at + 11, 0].long()])
 
 
+def test_as_many_rows_as_a_feed_forward_call_takes(env):
+    """2^22 tiles of one column; small whole numbers, so that results are exact."""
+    torch, K, ctx = env
+    rows = (1 << 30) - 1
+    x = torch.randint(-3, 4, (1, rows, 1), dtype=torch.int8, device="cuda").bfloat16()
+    one = torch.ones(1, 1, dtype=torch.bfloat16, device="cuda")
+    shape = K.ffn_shape(x, one, "none")
+    out = torch.empty_like(x)
+    ctx.pql_ffn_forward(shape, K.FfnInput(shape, x, one, one, one), K.Rows(out), None, K.workspace(ctx.ffn_workspace_bytes(shape, K.FFN_FORWARD)))
+    assert torch.equal(out, x * x)
+
+
+@pytest.mark.parametrize("dtype,rows", [("bfloat16", (1 << 28) + 77), ("float32", (1 << 26) + 77)])
+def test_gradients_of_sums_over_very_many_rows(env, dtype, rows):
+    """Of which a few, far apart, are not zero; small whole numbers, so that results are exact."""
+    torch, K, ctx = env
+    dt = getattr(torch, dtype)
+    at = torch.tensor([0, 63, 64, 4095, rows // 3, rows // 2, rows - 78, rows - 1], device="cuda")
+    x, grad = (torch.zeros(1, rows, 8, dtype=dt, device="cuda") for _ in range(2))
+    few = torch.randint(-2, 3, (2, len(at), 8), device="cuda")
+    x[0, at], grad[0, at] = few[0].to(dt), few[1].to(dt)
+    weights = [torch.randint(-1, 2, (8, 8), device="cuda").to(dt) for _ in range(3)]
+    shape = K.ffn_shape(x, weights[0], "none")
+    got = [torch.empty_like(t) for t in (x, *weights)]
+    ctx.pql_ffn_backward(shape, K.FfnInput(shape, x, *weights), None, K.Rows(grad), K.FfnGrad(shape, *got),
+                         K.workspace(ctx.ffn_workspace_bytes(shape, K.FFN_BACKWARD_ALONE)))
+    h = [t.double().cpu().numpy() for t in (few[0].view(1, -1, 8), *weights)]
+    want = O.ffn_grad(*h, "none", few[1].view(1, -1, 8).double().cpu().numpy())
+    exact = lambda g, w: np.array_equal(g.double().cpu().numpy(), torch.tensor(w).to(dt).double().numpy())  # noqa: E731
+    assert exact(got[0][0, at], want["x"][0]) and int(got[0].count_nonzero()) == np.count_nonzero(want["x"])
+    assert all(exact(g, want[k]) for g, k in zip(got[1:], ("gate", "up", "down")))
+
+
+def test_the_widest_embeddings(env):
+    """2^24 columns on no 16-byte boundary, in runs that cross the ends of two chunks."""
+    torch, K, ctx = env
+    dim, n = 1 << 24, 37
+    grad = torch.randint(-8, 9, (1, n, dim + 1), dtype=torch.int8, device="cuda").bfloat16()[..., 1:]
+    tokens = torch.zeros(1, n, 1, dtype=torch.int32, device="cuda")
+    tokens[0, -1] = 1
+    table = torch.empty(2, dim + 1, dtype=torch.bfloat16, device="cuda")[:, 1:]
+    shape = K.embed_shape(tokens, table, 0.25)
+    ctx.pql_embed_backward(shape, tokens, None, K.Rows(grad), K.Rows(table), K.workspace(ctx.embed_workspace_bytes(shape)))
+    want = sum(grad[0, i].float() for i in range(n - 1)) * 0.25
+    assert torch.equal(table[0], want.bfloat16()) and torch.equal(table[1], grad[0, -1] * 0.25)
+    out = torch.empty_like(grad)
+    ctx.pql_embed_forward(shape, tokens, None, K.Rows(table), K.Rows(out))
+    assert torch.equal(out[0, 0], (table[0].float() * 0.25).bfloat16()) and torch.equal(out[0, -1], table[1] * 0.25)
+
+
 @pytest.mark.parametrize("vocab", [3, 700, 40000])
 @pytest.mark.parametrize("which", ["equal", "in turn", "runs", "pairs", "any"])
 def test_every_place_is_counted_once(env, vocab, which):
