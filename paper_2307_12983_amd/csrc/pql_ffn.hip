@@ -57,7 +57,6 @@ struct FfnArgs {
     int count_is_k;                             // whether they are the contraction or the rows of the result
     float* part;                                // [workgroups][2][tile] sums over parts of the contraction
     const int* map;                             // packed row -> row of the output, NULL: the same
-    int a_along, b_along;                       // whether the contraction runs along the operand's rows in memory
     int act;
     // gated, back: [row][hidden_p]
     int hidden_p;
@@ -220,40 +219,6 @@ template <typename E> __device__ __forceinline__ void store_terms(bf16_t* p, int
     }
 }
 
-// Sums of 32-bit values that came out as NaN, once more and as fp32 products: an infinite value is one term, and meets all terms of the
-// other operand, of which some are zero or of the other sign; so do products that overflow.  What is NaN by itself is found out as
-// soon as it is, and stays.  Where sums are finite the check takes 2 of 405 us (512 x 32 rows of 256 and 1024 with gradients).
-__device__ __forceinline__ float value_of(const FfnOperand& o, bool along, int i, int k) {
-    if (o.whole) return ((const float*)o.p)[along ? i * (o.stride / 2) + k : k * (o.stride / 2) + i];
-    const bf16_t* p = o.p + (along ? i * o.stride + k : k * o.stride + i);
-    return (float)p[0] + ((float)p[o.plane] + (float)p[2 * o.plane]);
-}
-__device__ __forceinline__ bool any_nan(const float (&x)[8]) {
-    return __builtin_isunordered(x[0], x[1]) | __builtin_isunordered(x[2], x[3]) | __builtin_isunordered(x[4], x[5]) | __builtin_isunordered(x[6], x[7]);
-}
-// Whether there was such a sum.
-__device__ __forceinline__ bool sum_again(const FfnArgs& a, const FfnProblem& pr, int K, int row, int col, int first_b, float (&x)[8]) {
-    if (__builtin_expect(!any_nan(x), 1)) return false;
-    float s[8] = {};
-#pragma unroll 1
-    for (int seg = 0; seg < a.segments; ++seg) {
-        const FfnOperand &oa = pr.a[seg], &ob = pr.b[first_b + seg];
-#pragma unroll 1
-        for (int k = 0; k < K; ++k) {
-            const float u = value_of(oa, a.a_along, row, k);
-            bool open = false;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                s[e] = fmaf(u, value_of(ob, a.b_along, min(col + e, pr.n - 1), k), s[e]);
-                open |= x[e] != x[e] && s[e] == s[e];
-            }
-            if (!open) return true;
-        }
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = x[e] != x[e] && s[e] == s[e] ? s[e] : x[e];
-    return true;
-}
 // a and b of eight columns.
 __device__ __forceinline__ void read_saved(const FfnArgs& a, int64_t at, floatx4 (&va)[2], floatx4 (&vb)[2]) {
 #pragma unroll
@@ -413,7 +378,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
         rb.init(wn * TN * 16, lane);
 
         // where the next tiles to load stand
-        int seg = from / max(ksteps, 1), left = K - from % max(ksteps, 1) * BK;
+        int seg, left;
         Corner<A_ALONG, BK> ca;
         Corner<B_ALONG, BK_B> cb;
         const int64_t plane_a = pr.a[0].plane, plane_b = pr.b[0].plane;
@@ -421,10 +386,15 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
             ca.set(pr.a[seg], m0, min(M - m0, BM), K - left);
             cb.set(pr.b[GATED ? half : seg], n0 * N_BY, min(N - n0, BN) * N_BY, (K - left) * K_BY);
         };
-        corners();
-        auto load = [&](int stage) {
+        auto begin = [&] {
+            seg = from / max(ksteps, 1);
+            left = K - from % max(ksteps, 1) * BK;
+            corners();
+        };
+        begin();
+        auto load_terms = [&](int stage, int terms) {
 #pragma unroll
-            for (int t = 0; t < TERMS; ++t) {
+            for (int t = 0; t < terms; ++t) {
                 ta.load(lds[stage] + t * TA::BYTES, wave, ca.p + t * plane_a, ca.bytes(left), left);
                 if (t < B_TERMS) tb.load(lds[stage] + TERMS * TA::BYTES + t * TB::BYTES, wave, cb.p + t * plane_b, cb.bytes(left * K_BY), left * K_BY);
             }
@@ -433,6 +403,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
             left -= BK;
             if (left <= 0 && seg + 1 < a.segments) { ++seg; left = K; corners(); }
         };
+        auto load = [&](int stage) { load_terms(stage, TERMS); };
         floatx4 acc[TM][TN] = {};
         // Two sets of operands, so that one comes from LDS while the products of the other run; STREAM: of A's only 16 rows each.
         constexpr bool STREAM = TERMS == 3 && BM == 256;
@@ -591,6 +562,59 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
             }
         }
         settle_products();
+        if constexpr (TERMS == 3) {
+            // An infinite value is one term, and met all terms of the other operand, of which some are zero or of the other sign; so did
+            // products that overflow.  A tile with sums that are NaN takes its steps again with first terms alone: infinite or NaN as in fp32
+            // arithmetic.  us for 512 x 32 rows of 256 and 1024 with gradients: 402 without the check, 406 with it, 500 if every tile does so.
+            __shared__ unsigned odd[WAVES];
+            bool nan = false;
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) nan |= __builtin_isunordered(acc[i][j][0], acc[i][j][1]) | __builtin_isunordered(acc[i][j][2], acc[i][j][3]);
+            const unsigned any = __ballot(nan) != 0;
+            if (lane == 0) odd[wave] = any;
+            __syncthreads();                            // behind all reads of the last step
+            unsigned all = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) all |= odd[w];
+            if (__builtin_expect(all, 0)) {
+                floatx4 first[TM][TN] = {};
+                begin();
+#pragma unroll 1
+                for (int s = 0; s < n; ++s) {
+                    load_terms(0, 1);
+                    wait_loads<0>();
+                    bf16x8 x, y[TN];
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        if constexpr (WHOLE) {
+                            float v[8];
+                            bf16x8 t[3];
+                            rb.get(lds[0] + TERMS * TA::BYTES, j, v);
+                            terms_of(v, t);
+                            y[j] = t[0];
+                        } else {
+                            y[j] = rb.get(lds[0] + TERMS * TA::BYTES, j, 0);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) {
+                        x = ra.get(lds[0], i, 0);
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) first[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[j], x, first[i][j], 0, 0, 0);
+                    }
+                    __syncthreads();                    // the next step's loads overwrite this one's
+                }
+                settle_products();
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] != acc[i][j][e] ? first[i][j][e] : acc[i][j][e];
+            }
+        }
 
         // Results go through LDS, so that whole lines of memory are read and written: column l % 16 of a product is a row of C, its rows
         // 4 (l / 16) .. + 3 are columns.  Then eight columns of a row a thread: the first four of each eight lie together, then the last
@@ -598,12 +622,13 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
         constexpr int ALL = STAGES * STAGE, PASSES = (BM * BN * 4 + ALL - 1) / ALL, PM = TM / PASSES, ROWS = BM / PASSES, NT = 64 * WAVES;
         constexpr int UNITS = GATED ? BN / 16 : BN / 8, EACH = ROWS * UNITS / NT, AHEAD = 2;
         static_assert(PASSES * PM == TM && EACH % AHEAD == 0, "whole passes");
+        static_assert(TERMS != 3 || PASSES == 1, "the check above has been waited for");
         char* stage = lds[0];
         auto granule = [&](int row, int g) { return (floatx4*)(stage + row * BN * 4 + ((((g >> 1) + (g & 1) * (BN / 8)) ^ (row & 15)) << 4)); };
         float* part = n == sh.steps ? nullptr : a.part + ((int64_t)sharer * 2 + (from == 0)) * (BM * BN);
 #pragma unroll
         for (int pass = 0; pass < PASSES; ++pass) {
-            __syncthreads();
+            if (TERMS != 3) __syncthreads();
 #pragma unroll
             for (int i = 0; i < PM; ++i)
 #pragma unroll
@@ -631,24 +656,6 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
                 }
                 continue;
             }
-            // Eight columns of a row: where they are, and their sums from LDS.
-            auto place = [&](int u, int& local, int& row, int& col) {
-                const int unit = u * NT + threadIdx.x;
-                local = unit / UNITS;
-                row = m0 + (local / (PM * 16) * TM + pass * PM) * 16 + local % (PM * 16);
-                col = n0 + unit % UNITS * 8;
-                return row < M && col < (EPI == EPI_OUT ? N : a.hidden_p);
-            };
-            auto sums = [&](int u, int local, float (&x)[8], float (&y)[8]) {
-                const int g = (u * NT + threadIdx.x) % UNITS * 2;
-                *(floatx4*)x = *granule(local, g);
-                *(floatx4*)(x + 4) = *granule(local, g + 1);
-                if constexpr (GATED) {
-                    *(floatx4*)y = *granule(local, g + BN / 8);
-                    *(floatx4*)(y + 4) = *granule(local, g + BN / 8 + 1);
-                }
-            };
-            bool odd = false;
 #pragma unroll 1
             for (int u0 = 0; u0 < EACH; u0 += AHEAD) {
                 floatx4 va[AHEAD][2], vb[AHEAD][2];
@@ -656,32 +663,24 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
                 bool on[AHEAD];
 #pragma unroll
                 for (int u = 0; u < AHEAD; ++u) {
-                    on[u] = place(u0 + u, local[u], row[u], col[u]);
+                    const int unit = (u0 + u) * NT + threadIdx.x;
+                    local[u] = unit / UNITS;
+                    row[u] = m0 + (local[u] / (PM * 16) * TM + pass * PM) * 16 + local[u] % (PM * 16);
+                    col[u] = n0 + unit % UNITS * 8;
+                    on[u] = row[u] < M && col[u] < (EPI == EPI_OUT ? N : a.hidden_p);
                     if constexpr (EPI == EPI_BACK) read_saved(a, on[u] ? (int64_t)row[u] * a.hidden_p + col[u] : 0, va[u], vb[u]);
                 }
 #pragma unroll
                 for (int u = 0; u < AHEAD; ++u) {
+                    const int g = ((u0 + u) * NT + threadIdx.x) % UNITS * 2;
                     float x[8], y[8];
-                    sums(u0 + u, local[u], x, y);
-                    if constexpr (TERMS == 3) odd |= any_nan(x) || (GATED && any_nan(y));
+                    *(floatx4*)x = *granule(local[u], g);
+                    *(floatx4*)(x + 4) = *granule(local[u], g + 1);
+                    if constexpr (GATED) {
+                        *(floatx4*)y = *granule(local[u], g + BN / 8);
+                        *(floatx4*)(y + 4) = *granule(local[u], g + BN / 8 + 1);
+                    }
                     if (on[u]) finish<E, EPI>(a, pr, row[u], col[u], x, y, va[u], vb[u]);
-                }
-            }
-            if constexpr (TERMS == 3) {
-                static_assert(TERMS != 3 || PASSES == 1, "all sums are in LDS still");
-                if (__builtin_expect(!odd, 1)) continue;
-#pragma unroll 1
-                for (int u = 0; u < EACH; ++u) {
-                    floatx4 va[2], vb[2];
-                    float x[8], y[8];
-                    int row, col, local;
-                    if (!place(u, local, row, col)) continue;
-                    sums(u, local, x, y);
-                    bool again = sum_again(a, pr, K, row, col, 0, x);
-                    if constexpr (GATED) again |= sum_again(a, pr, K, row, col, 1, y);
-                    if (!again) continue;
-                    if constexpr (EPI == EPI_BACK) read_saved(a, (int64_t)row * a.hidden_p + col, va, vb);
-                    finish<E, EPI>(a, pr, row, col, x, y, va, vb);
                 }
             }
         }
@@ -694,7 +693,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
 }
 
 // Tiles whose sums are in parts: those of consecutive workgroups, added in order.  Eight columns of a row a thread.
-template <typename E, int BM, int BN, Epilogue EPI> __global__ void __launch_bounds__(256, 8) ffn_join_kernel(FfnArgs a, int slots, int bk) {
+template <typename E, int BM, int BN, Epilogue EPI> __global__ void __launch_bounds__(256) ffn_join_kernel(FfnArgs a, int slots, int bk) {
     constexpr int COLS = EPI == EPI_GATED ? BN / 2 : BN, UNITS = COLS / 8;
     const int count = a.count ? *a.count : 0, rows = a.count && !a.count_is_k ? count : -1, K = a.count && a.count_is_k ? count : a.k;
     const Shares sh(all_tiles<BM, COLS>(a, rows), slots, (K + bk - 1) / bk * a.segments, Mode<E, BM>::LEAST);
@@ -725,10 +724,6 @@ template <typename E, int BM, int BN, Epilogue EPI> __global__ void __launch_bou
         }
         floatx4 va[2], vb[2];
         if constexpr (EPI == EPI_BACK) read_saved(a, (int64_t)row * a.hidden_p + col, va, vb);
-        if constexpr (Mode<E, BM>::TERMS == 3) {
-            sum_again(a, pr, K, row, col, 0, x);
-            if constexpr (EPI == EPI_GATED) sum_again(a, pr, K, row, col, 1, y);
-        }
         finish<E, EPI>(a, pr, row, col, x, y, va, vb);
     }
 }
@@ -992,9 +987,8 @@ struct FfnRun {
         return a;
     }
     // of: the problems of a full call, which the plan has counted with.
-    template <bool A_ALONG, bool B_ALONG, Epilogue EPI> void product(FfnArgs a, int of, int kid) {
+    template <bool A_ALONG, bool B_ALONG, Epilogue EPI> void product(const FfnArgs& a, int of, int kid) {
         if (e != hipSuccess) return;
-        a.a_along = A_ALONG; a.b_along = B_ALONG;
         const FfnProblem& pr = a.prob[0];
         const bool whole = pr.b[0].whole;
         FfnTiles t = ffn_tiles(s.dtype, pr.m, pr.n, 1, of, a.k, a.segments, EPI == EPI_GATED, whole);
