@@ -83,14 +83,19 @@ class Residual(torch.autograd.Function):
         return (None, None, None, *grads)
 
 
+def feed_forward(ctx, act, x, gate, up, down, keep):
+    """The block's result, and what its gradient is worked out from: without it, calls of few rows take kernels of their own."""
+    shape = K.ffn_shape(x, gate, act)
+    out = torch.empty_like(x)
+    saved = K.workspace(ctx.ffn_saved_bytes(shape)) if keep else None
+    ctx.pql_ffn_forward(shape, K.FfnInput(shape, x, gate, up, down), K.Rows(out), saved, K.workspace(ctx.ffn_workspace_bytes(shape, K.FFN_FORWARD)))
+    return out, saved, shape
+
+
 class FeedForward(torch.autograd.Function):
     @staticmethod
     def forward(fn, ctx, act, x, gate, up, down):
-        shape = K.ffn_shape(x, gate, act)
-        out = torch.empty_like(x)
-        saved = K.workspace(ctx.ffn_saved_bytes(shape)) if any(t.requires_grad for t in (x, gate, up, down)) else None
-        ctx.pql_ffn_forward(shape, K.FfnInput(shape, x, gate, up, down), K.Rows(out), saved,
-                            K.workspace(ctx.ffn_workspace_bytes(shape, K.FFN_FORWARD)))
+        out, saved, shape = feed_forward(ctx, act, x, gate, up, down, any(t.requires_grad for t in (x, gate, up, down)))
         fn.call = ctx, shape
         fn.save_for_backward(x, gate, up, down, saved)
         return out
@@ -140,7 +145,8 @@ class BlockStudent(torch.nn.Module):
         """Behind the memory: logits of every step and action dimension."""
         y, _ = Residual.apply(self.ctx, self.heads, "silu", None, memory.flatten(-2), gate, self.heads_norm, None)
         stream, u = Residual.apply(self.ctx, 1, "none", stream, self.outward(y), None, self.after, self.ready)
-        f = FeedForward.apply(self.ctx, "silu", u, self.up_gate, self.up, self.down)
+        block = self.ctx, "silu", u, self.up_gate, self.up, self.down
+        f = FeedForward.apply(*block) if torch.is_grad_enabled() else feed_forward(*block, keep=False)[0]
         _, u = Residual.apply(self.ctx, 1, "none", stream, f, None, self.last, self.final)
         return self.answer(u).view(-1, M.BINS)
 

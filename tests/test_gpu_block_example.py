@@ -102,3 +102,18 @@ def test_the_examples_functions_notice_changed_tensors_and_second_derivatives():
         first, = torch.autograd.grad(f(*x).square().sum(), x[0], create_graph=True)
         with pytest.raises(RuntimeError, match="once_differentiable"):
             first.sum().backward()
+
+
+def test_acting_takes_the_kernels_for_few_rows_and_training_those_of_tiles():
+    torch, X = example()
+    program = X.Program(envs=48, steps=6)
+    kernels = []
+    for run in (program.act, lambda: program.train(1)):
+        torch.cuda.synchronize()
+        program.ctx.pql_profile_begin(4096)
+        run()
+        torch.cuda.synchronize()
+        kernels.append({k["name"]: k["launches"] for k in program.ctx.pql_profile_end()})
+    acted, trained = kernels
+    assert acted["ffn_rows_kernel"] == 2 * program.steps        # every step; the window it is compared with has more rows
+    assert "ffn_rows_kernel" not in trained and trained["ffn_gated_kernel"] == 1 and "ffn_back_kernel" in trained
