@@ -511,6 +511,43 @@ def test_gradients_of_the_feed_forward_block(env, case):
         assert env[0].equal(g, first[k]), k + " without saved"
 
 
+# Enough tiles for the kernels of 256 rows (192 of them), and more than run at a time (256; 512 of 128 x 128 in bf16), so that whole rounds
+# go to a workgroup each and the rest is shared out by steps and joined.  By which products: both projections (p), out (o), dm (m), dx (x),
+# the weights' gradients (w).
+LARGE = [
+    (1, 4099, 264, 1032, "float32", "silu", "dense", None),                         # p; 128 rows, whole rounds: m
+    (4, 1025, 263, 1029, "float32", "silu", "offset", [1025, 700, 0, 1024]),        # the same by the lengths
+    (1, 13400, 520, 520, "float32", "silu", "wide", None),                          # p o m x
+    (4, 3350, 517, 520, "float32", "none", "offset", [3350, 0, 3349, 2000]),        # p o m x
+    (1, 1000, 1160, 2056, "float32", "silu", "dense", None),                        # w
+    (4, 250, 1157, 2051, "float32", "silu", "offset", [250, 3, 249, 0]),            # w
+    (1, 13400, 1032, 1032, "bfloat16", "silu", "dense", None),                      # p o m x
+    (4, 3350, 1029, 1032, "bfloat16", "silu", "offset", [3350, 0, 3349, 2000]),     # p o m x
+    (1, 1000, 2312, 2056, "bfloat16", "silu", "wide", None),                        # w
+    (4, 250, 2309, 2051, "bfloat16", "none", "offset", [250, 3, 249, 0]),           # w
+    (1, 4099, 1032, 2056, "bfloat16", "silu", "dense", None),                       # p; 128 rows, whole rounds: m
+]
+
+
+@pytest.mark.parametrize("case", LARGE, ids=label)
+def test_feed_forward_block_of_many_tiles(env, case):
+    """bf16: one rounding of m, da and db, by 2^-9 / sqrt 3 of their norms at most, is passed on as it is by products with terms of random
+    signs."""
+    call = FfnCall(env, case, seed=9)
+    k = max(case[0] * case[1], case[2], case[3])
+    bound = 3 * (k ** 0.5 + 10) * U + (2.0 ** -9 / 3 ** 0.5 if case[4] == "bfloat16" else 0.0)
+    out, saved = call.forward(True)
+    first = call.backward(saved)
+    for got, want, what in [(out, call.want, "out")] + [(g, call.want_grad[name], name) for name, g in first.items()]:
+        close(got, want, what, bound)
+    assert env[0].equal(out, call.forward(False)[0])
+    for name, g in call.backward(None).items():
+        assert env[0].equal(g, first[name]), name + " without saved"
+    if case[7] is not None:
+        real = env[0].tensor(O.counted(call.x.shape[:2], case[7]), device="cuda")
+        assert not bool(out[~real].any()) and not bool(first["x"][~real].any())
+
+
 def test_projections_of_different_layouts(env):
     torch, K, ctx = env
     for dtype in ("bfloat16", "float32"):
@@ -991,6 +1028,16 @@ def test_infinite_tokens_in_32_bits(env, rows, d, f, lengths, act):
     for saved in (outs[2], None):
         for k, g in call.backward(saved).items():
             same_kind(call, g, call.want_grad[k], k)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,d,f,lengths", [(4099, 264, 1029, None), (13400, 520, 520, [13300]), (13400, 1032, 1029, None), (1000, 2309, 2056, None)])
+def test_infinite_tokens_in_many_tiles(env, rows, d, f, lengths, dtype):
+    call, at = infinite_rows(env, dtype, rows, d, f, lengths)
+    out, saved = call.forward(True)
+    same_kind(call, out, call.want, "out")
+    for k, g in call.backward(saved).items():
+        same_kind(call, g, call.want_grad[k], k)
 
 
 @pytest.mark.parametrize("rows", [33, 200])
