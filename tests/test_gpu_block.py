@@ -500,6 +500,21 @@ def test_feed_forward_block_of_few_rows(env, case):
     assert env[0].equal(out, call.forward(False)[0])
 
 
+# rounded: by the tiles' kernels once to 8 bits, by those for few rows to 16
+@pytest.mark.parametrize("case", [c for c in FFN + FEW if c[4] == "bfloat16" and c[3] * c[0] * c[1] >= 4096], ids=label)
+def test_what_lies_between_the_products_is_rounded_once(env, case):
+    """Relative to its norm by 2^-9 / sqrt 3 at most (all significands at their smallest; random ones 0.7 of that), or 2^-17 / sqrt 3."""
+    call = FfnCall(env, case, seed=10)
+    k = max(case[0] * case[1], case[2], case[3])
+    bound = 3 * (k ** 0.5 + 10) * U
+    few = case[0] * case[1] <= (64 if case[2] * case[3] <= 4 << 20 else 16)
+    close(call.forward(False)[0], call.want, "out", bound + 2.0 ** (-17 if few else -9) / 3 ** 0.5)
+    out, saved = call.forward(True)
+    close(out, call.want, "out with saved", bound + 2.0 ** -9 / 3 ** 0.5)
+    for name, g in call.backward(saved).items():
+        close(g, call.want_grad[name], name, bound + 2 * 2.0 ** -9 / 3 ** 0.5)
+
+
 @pytest.mark.parametrize("case", FFN, ids=label)
 def test_gradients_of_the_feed_forward_block(env, case):
     call = FfnCall(env, case, seed=1)
