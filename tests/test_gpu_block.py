@@ -609,6 +609,64 @@ def test_32_bit_weights_as_they_are_and_as_planes(env, rows, d, f, lengths, odd)
             call.close(got[0][k], want, k)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows", [12, 150])
+def test_feed_forward_rows_that_repeat_or_overlap(env, dtype, rows):
+    """Tokens, the output's gradient and weights may; results are those of rows of their own."""
+    torch, K, ctx = env
+    d, f, dt = 40, 72, getattr(torch, dtype)
+
+    def strided(n, cols, stride, by):
+        flat = torch.randn((n - 1) * stride + cols, device="cuda").mul_(by).to(dt)
+        return flat.as_strided((n, cols), (stride, 1))
+
+    for stride in (0, 8, 37):
+        x, grad = (strided(rows, d, stride, 1.0).view(rows, 1, d) if stride else strided(rows, d, 0, 1.0)[:, None] for _ in range(2))
+        weights = [strided(f, d, stride, d ** -0.5), strided(f, d, stride, d ** -0.5), strided(d, f, stride, f ** -0.5)]
+        shape = K.ffn_shape(x, weights[0], "silu")
+        results = []
+        for tensors in ((x, *weights, grad), [t.clone(memory_format=torch.contiguous_format) for t in (x, *weights, grad)]):
+            *given, do = tensors
+            assert K.Rows(given[0]).c.stride == (stride if given[0] is x else d)
+            out = torch.empty(rows, 1, d, dtype=dt, device="cuda")
+            grads = [torch.empty(t.shape, dtype=dt, device="cuda") for t in given]
+            ctx.pql_ffn_forward(shape, K.FfnInput(shape, *given), K.Rows(out), None, K.workspace(ctx.ffn_workspace_bytes(shape, K.FFN_FORWARD)))
+            ctx.pql_ffn_backward(shape, K.FfnInput(shape, *given), None, K.Rows(do), K.FfnGrad(shape, *grads),
+                                 K.workspace(ctx.ffn_workspace_bytes(shape, K.FFN_BACKWARD_ALONE)))
+            results.append((out, *grads))
+        assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows", [3, 70])
+@pytest.mark.parametrize("d,f", [(65536, 16), (24, 65536), (65535, 9)])
+def test_the_widest_feed_forward_blocks(env, dtype, rows, d, f):
+    call = FfnCall(env, (rows, 1, d, f, dtype, "silu", "dense", None), seed=11)
+    out, saved = call.forward(True)
+    call.close(call.forward(False)[0], call.want, "out")
+    call.close(out, call.want, "out with saved")
+    for k, g in call.backward(saved).items():
+        call.close(g, call.want_grad[k], k)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_weights_whose_rows_are_far_apart(env, dtype):
+    """At the largest stride of weights that are read where they are, and beyond it."""
+    torch, K, ctx = env
+    call = FfnCall(env, (150, 1, 40, 264, dtype, "silu", "dense", None), seed=12)
+    want = call.forward(False)[0], call.backward(None)
+    for stride in (1 << 20, (1 << 20) + 8):
+        big = torch.empty(3 * 264 * stride, dtype=call.x.dtype, device="cuda")
+        weights = []
+        for i, w in enumerate((call.gate, call.up, call.down)):
+            weights.append(big[i * 264 * stride:].as_strided(w.shape, (stride, 1)))
+            weights[-1].copy_(w)
+        call.given = K.FfnInput(call.shape, call.x, *weights)
+        assert torch.equal(call.forward(False)[0], want[0])
+        for k, g in call.backward(None).items():
+            assert torch.equal(g, want[1][k]), k
+
+
 def test_feed_forward_gradients_that_are_not_asked_for(env):
     call = FfnCall(env, (3, 50, 136, 260, "float32", "silu", "dense", [50, 20, 0]), seed=2)
     _, saved = call.forward(True)
