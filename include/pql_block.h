@@ -85,7 +85,8 @@ typedef struct {
     float *post, *pre;
 } pql_residual_grad;
 
-/* With N(z) = z / sqrt(mean(z^2) + eps), the mean taken over each part of the row for y and over the row for sum,
+/* With N(z) = z / sqrt(mean(z^2) + eps), the mean taken over each part of the row for y and over the row for sum (in fp32: of
+ * values whose squares sum beyond its range, 1e19 and more, N is 0),
  *     sum_n = scale_x x_n + scale_y act(gate_n) post N(y_n),        next_n = pre N(sum_n)
  * where what is left out (a norm of eps 0, a gate, a weight) is the factor 1 or the identity.  sum may be x or y itself,
  * next may be y; either may have data NULL, not both.  next follows from the sum before that is rounded to dtype. */

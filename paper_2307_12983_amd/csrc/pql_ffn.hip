@@ -13,11 +13,11 @@
 // step ahead of the products, and are laid out there so that neither the contiguous reads (operands whose contraction runs along
 // a row) nor the transposing ones (along a column) meet bank conflicts: no operand is ever transposed in memory.  bf16 takes tiles of
 // 256 x 256 by eight wavefronts, since what bounds it is the way from L2 to LDS, 64 KB a step of 64: 4 x 2048 rows of 2048 and 8192
-// with gradients take 2.25 ms, with tiles of 128 x 128 2.71 ms, of 256 x 128 by two workgroups a compute unit 2.57 ms; three to five
+// with gradients take 2.22 ms, with tiles of 128 x 128 2.71 ms, of 256 x 128 by two workgroups a compute unit 2.57 ms; three to five
 // steps of 32 in LDS 2.38 ms.  Its products reach 975 (projections), 1230 (out, dx, weights' gradients) and 730 TFLOP/s (dm, da, db:
 // half of its time goes to reading a and b and writing da and db, 0.8 GB at 5 TB/s); the loop without its products takes 77 % of the
 // time with them.  fp32 takes 256 x 128, six products a pair, and is bound by those: 512 x 32 rows of 256 and 1024 with gradients
-// take 0.40 ms.
+// take 0.41 ms.
 #include <type_traits>
 
 #include "pql_ffn_internal.h"
@@ -565,7 +565,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
         if constexpr (TERMS == 3) {
             // An infinite value is one term, and met all terms of the other operand, of which some are zero or of the other sign; so did
             // products that overflow.  A tile with sums that are NaN takes its steps again with first terms alone: infinite or NaN as in fp32
-            // arithmetic.  us for 512 x 32 rows of 256 and 1024 with gradients: 402 without the check, 406 with it, 500 if every tile does so.
+            // arithmetic.  us for 512 x 32 rows of 256 and 1024 with gradients: 402 without the check, 406 with it, 150 more if every tile does so.
             __shared__ unsigned odd[WAVES];
             bool nan = false;
 #pragma unroll
