@@ -129,7 +129,8 @@ typedef struct { pql_rows x, gate, up, down; } pql_ffn_grad;
  * workspace: [device] pql_ffn_workspace_bytes(shape, PQL_FFN_FORWARD) bytes; both 256-byte aligned.  bf16: m is rounded to
  * bf16 once as an operand of the second product, or, in a call of few rows without saved, kept in 16 bits; a and b are in
  * fp32.  fp32: products of 24-bit operands, sums in fp32.  Infinite values
- * and sums that overflow give what fp32 arithmetic gives, in both types and in calls of any number of rows. */
+ * and sums that overflow give what fp32 arithmetic gives, in both types and in calls of any number of rows (values within a
+ * hundredth of the largest number may become infinite). */
 int64_t pql_ffn_saved_bytes(const pql_ffn_shape* shape);
 int64_t pql_ffn_workspace_bytes(const pql_ffn_shape* shape, int32_t call);
 int32_t pql_ffn_forward(pql_ctx* ctx, const pql_ffn_shape* shape, const pql_ffn_input* input, const pql_rows* out,
