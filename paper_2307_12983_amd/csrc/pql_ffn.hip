@@ -565,7 +565,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
         if constexpr (TERMS == 3) {
             // An infinite value is one term, and met all terms of the other operand, of which some are zero or of the other sign; so did
             // products that overflow.  A tile with sums that are NaN takes its steps again with first terms alone: infinite or NaN as in fp32
-            // arithmetic.  us for 512 x 32 rows of 256 and 1024 with gradients: 402 without the check, 406 with it, 150 more if every tile does so.
+            // arithmetic.  us for 512 x 32 rows of 256 and 1024 with gradients: 403 without the check, 408 with it, 150 more if every tile does so.
             __shared__ unsigned odd[WAVES];
             bool nan = false;
 #pragma unroll
@@ -579,6 +579,13 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(FfnArgs a,
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) all |= odd[w];
             if (__builtin_expect(all, 0)) {
+                if constexpr (WHOLE) {                  // no registers to keep addresses in until here
+                    asm("" : "+v"(lane));
+                    ta.init(wave, lane, pr.a[0].stride);
+                    tb.init(GATED ? wave >> 1 : wave, lane, pr.b[0].stride);
+                    ra.init(wm * TM * 16, lane);
+                    rb.init(wn * TN * 16, lane);
+                }
                 floatx4 first[TM][TN] = {};
                 begin();
 #pragma unroll 1
